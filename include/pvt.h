@@ -16,7 +16,9 @@
  *                                            outside S stay, Section 3.3)
  *
  * and the next step starts with dequantize_weights (Algorithm 3, first line).
- * This library is those three calls.
+ * This library is those three calls, and the operators of the pass between them that g comes from: products in
+ * 4-bit block floating point with their gradients (pvt_mx_*), and the loss that trains the quantised model against
+ * the one it was made from (pvt_distill_*).
  *
  * Conventions
  *   - A layer is `rows x cols`, row-major.  Weight groups are `group_dim` = 8
@@ -51,6 +53,7 @@ extern "C" {
 /* element types */
 #define PVT_F32 0
 #define PVT_F16 1
+#define PVT_BF16 2 /* calls on pvt_mx and pvt_distill only */
 #define PVT_U8 0
 #define PVT_U16 1
 
@@ -63,7 +66,8 @@ extern "C" {
 #define PVT_ETOOLARGE (-5)    /* pvt_vstep_select_noalloc only: the layer exceeds the built-in scratch */
 
 /* device-side status bits (pvt_status) */
-#define PVT_DEV_BAD_INDEX 1u    /* an entry of idx was >= G; that entry was skipped */
+#define PVT_DEV_BAD_INDEX 1u    /* an entry of idx was >= G (of a distillation's list: beyond the vocabulary, or repeated);
+                                   that entry was skipped */
 #define PVT_DEV_BAD_CODE 2u     /* a stored code was >= K; treated as code 0 (dequant) or left out of the pool */
 #define PVT_DEV_WAIT_EXPIRED 4u /* a bounded wait on an on-chip barrier ran out; results of the call are invalid */
 #define PVT_DEV_INTERNAL 8u     /* an internal consistency check failed (selection count mismatch), or a group has no finite
@@ -318,6 +322,137 @@ int pvt_vstep_block(const pvt_layer* layers, const uint64_t* k, int32_t n_layers
                     void* const* W_hat, int32_t out_dtype, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /*
+ * Microscaled 4-bit floating point (the Open Compute Project's MX specification, FP4 with blocks of 32, and the same
+ * elements under finer scales): the representation in which a training program runs the forward and backward pass
+ * that g comes from (Algorithm 3, lines between dequantize_weights and the V step; the paper runs them in mixed
+ * precision).  A matrix of rows x cols elements e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives: three
+ * bits that order them, and the sign above), blocks of 16 or 32 along a row with one scale each.
+ *   value[r, c] = element[r, c] * scale[r, c / block] * tensor_scale
+ *   PVT_MX_E8M0_32: block 32, scale 2^(byte - 127), byte 255 = NaN; no tensor_scale (NULL).
+ *   PVT_MX_E4M3_16: block 16, scale an 8-bit float e4m3 without its sign (byte 127 = NaN); tensor_scale one positive
+ *                   finite binary32 on the device, or NULL = 1.
+ * codes: ceil(cols / 2) bytes per row, the element of the even column in the lower half; rows are ld bytes apart, ld a
+ * multiple of 16, codes 16-byte aligned and rows * ld bytes readable.  After an odd last column the upper half is zero;
+ * bytes behind ceil(cols / 2) are left as they were and never looked at.
+ * scales: pvt_mx_scale_bytes bytes, 16-byte aligned, all of them written by pvt_mx_quantize.  Tiles of 128 rows x 4
+ * blocks, 512 bytes: byte 16 (r % 32) + 4 (r % 128 / 32) + b % 4 of tile (r / 128, b / 4) for block b of row r; the tiles
+ * of a strip of 128 rows lie one after the other, as many as ceil(cols / 256) * 256 columns need (2 or 4 for each 256),
+ * strip after strip.  Scales of rows and blocks that do not exist are 0.
+ */
+#define PVT_MX_E8M0_32 0
+#define PVT_MX_E4M3_16 1
+typedef struct pvt_mx {
+  int32_t rows, cols;
+  int32_t format;             /* PVT_MX_* */
+  int32_t reserved_;          /* set to 0 */
+  int64_t ld;                 /* bytes from one row of codes to the next */
+  uint8_t* codes;
+  uint8_t* scales;
+  const float* tensor_scale;
+} pvt_mx;
+
+/* Bytes of the scales of such a matrix; 0 if rows, cols or format is invalid. */
+size_t pvt_mx_scale_bytes(int32_t rows, int32_t cols, int32_t format);
+
+/*
+ * Quantisation of x (device, m->rows x m->cols of x_dtype PVT_F32 | PVT_F16 | PVT_BF16, rows ldx elements apart, any
+ * alignment of its type) into m->codes and m->scales.  With a = the largest |x| of a block (a last, shorter block
+ * included) and exact real arithmetic between the roundings that are named:
+ *   PVT_MX_E8M0_32: scale = 2^(floor(log2 a) - 2), at least 2^-127; a = 0: 2^-127
+ *   PVT_MX_E4M3_16: scale = a / (6 tensor_scale) rounded to e4m3 (to nearest even, at most 448)
+ *   element = x / (scale tensor_scale) rounded to e2m1 (to nearest, ties to the even code, at most 6 in magnitude);
+ *             zero if the scale is zero.  The sign of x stays, of a zero too.
+ * A block that holds a NaN or an infinity, and every block under a tensor_scale that is not positive and finite, has
+ * scale NaN and elements 0.
+ */
+int pvt_mx_quantize(const pvt_mx* m, const void* x, int32_t x_dtype, int64_t ldx, void* cuda_stream);
+
+/*
+ * The values of m, each product rounded once to binary32 (exact without a tensor_scale) and then, where out_dtype asks
+ * for it, once to binary16 or bfloat16.  values: device, m->rows x m->cols of out_dtype, rows ldv elements apart.
+ */
+int pvt_mx_dequant(const pvt_mx* m, void* values, int32_t out_dtype, int64_t ldv, void* cuda_stream);
+
+/*
+ * y[t, n] = sum over c of x[t, c] w[n, c]: x the activations (a row per token), w the weights of a linear layer, of one
+ * format and with equal cols.  Products are exact, sums are binary32 on the tensor cores, the tensor scales are
+ * applied to the sum, and the result is rounded once to y_dtype.  y: device, x->rows x w->rows, rows ldy
+ * elements apart; it may not overlap x or w.  Results depend on the shapes only, not on the run.
+ * `status` may be NULL or a device uint32 into which PVT_DEV_WAIT_EXPIRED is OR-ed (results are then invalid).
+ */
+int pvt_mx_product(const pvt_mx* x, const pvt_mx* w, void* y, int32_t y_dtype, int64_t ldy, uint32_t* status,
+                   void* cuda_stream);
+
+/*
+ * The gradients of that product, straight through the quantisation (Appendix E: the discretisation counts as the
+ * identity).  dy: device, tokens x w->rows (or n) of PVT_BF16, 16-byte aligned, rows lddy elements apart, lddy a
+ * multiple of 8.
+ *   pvt_mx_grad_input:  dx[t, c] = sum over n of dy[t, n] w[n, c]      dx: tokens x w->cols of dx_dtype (any of the three)
+ *   pvt_mx_grad_weight: dw[n, c] = sum over t of dy[t, n] x[t, c]      dw: n x x->cols of PVT_F32, tokens = x->rows; with
+ *                       accumulate != 0 it is added to what dw holds (Algorithm 3 sums the gradient of several batches).
+ * dw is what a pvt_layer of that shape takes as g.  Elements times scale are exact in bfloat16, sums are binary32, and
+ * the tensor scale is applied to the sum.  Results depend on the shapes only.  `status` as above.
+ */
+int pvt_mx_grad_input(const void* dy, int64_t lddy, int32_t tokens, const pvt_mx* w, void* dx, int32_t dx_dtype,
+                      int64_t lddx, uint32_t* status, void* cuda_stream);
+int pvt_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const pvt_mx* x, float* dw, int64_t lddw,
+                       int32_t accumulate, uint32_t* status, void* cuda_stream);
+
+/*
+ * A teacher's largest logits (the method trains against the predictions of the model before quantisation).  logits:
+ * device, rows x vocab of dtype (any of the three), rows ld elements apart.  Per row:
+ *   top_idx[r, 0..k): the k entries that come first in the order of (value descending, index ascending); NaN counts as
+ *                     larger than every number, -0 as 0.  Entries of -infinity (a masked vocabulary) are never
+ *                     listed: where fewer than k are left the list ends with index -1 and value -infinity.
+ *   top_logit[r, i]:  their values in binary32.
+ *   lse[r]:           log sum over the vocabulary of exp(logit / temperature), binary32; NULL if not wanted.
+ * 1 <= k <= PVT_DISTILL_MAX_K, k <= vocab; temperature positive and finite.
+ */
+#define PVT_DISTILL_MAX_K 1024
+int pvt_distill_top(const void* logits, int32_t dtype, int64_t ld, int64_t rows, int32_t vocab, int32_t k,
+                    float temperature, int32_t* top_idx, float* top_logit, float* lse, void* cuda_stream);
+
+/*
+ * Distillation from those: for each row, with q = softmax(logits / temperature) of the student,
+ *   teacher_lse == NULL: p = softmax of top_logit / temperature over the listed entries, p_rest = 0
+ *   otherwise:           p_i = exp(top_logit[i] / temperature - teacher_lse[r]), p_rest = max(0, 1 - sum p)
+ *   loss[r] = weight[r] * (sum over i of p_i (log p_i - log q_i) + p_rest (log p_rest - log q_rest))
+ * where q_rest is the student's probability of everything that is not listed.  Terms with p = 0 are 0.
+ * grad[r, v] = weight[r] upstream[r] / temperature * d(loss[r] / weight[r]) / d(logits[r, v] / temperature):
+ *   (P + p_rest) q_v - p_v for listed v, (P + p_rest - p_rest / q_rest) q_v for the others, P = sum p.
+ * Rows without effect have loss 0 and gradient 0, whatever their logits hold: weight[r] = 0; no listed entry, or none
+ * above -infinity; student logits that are all -infinity.  (An infinite loss, where q is 0 and p is not, is infinite.)
+ * An entry of top_idx below 0 is empty.  One that is vocab or more, or names an entry that a smaller i of the row
+ * names, is left out and sets PVT_DEV_BAD_INDEX.
+ */
+typedef struct pvt_distill {
+  int64_t rows;
+  int32_t vocab, k;           /* 1 <= vocab <= PVT_DISTILL_MAX_VOCAB, 1 <= k <= PVT_DISTILL_MAX_K */
+  const void* logits;         /* [rows][vocab] of dtype, rows ld elements apart */
+  int64_t ld;
+  int32_t dtype;              /* PVT_F32 | PVT_F16 | PVT_BF16 */
+  float temperature;          /* positive, finite */
+  const int32_t* top_idx;     /* [rows][k] */
+  const float* top_logit;     /* [rows][k] */
+  const float* teacher_lse;   /* [rows] or NULL */
+  const float* weight;        /* [rows] or NULL = 1 */
+} pvt_distill;
+#define PVT_DISTILL_MAX_VOCAB (1 << 20)
+#define PVT_DISTILL_STATS 8
+
+/*
+ * The loss of every row, and what the gradient needs: `grad` (the gradient in the same pass, of grad_dtype, rows ldg
+ * elements apart; it may be the logits themselves) or `stats` (device, rows x PVT_DISTILL_STATS floats, for
+ * pvt_distill_grad), both or neither.  upstream: device, rows floats, or NULL = 1; read with grad only.
+ * loss: device, rows floats.  `status` may be NULL or a device uint32 into which PVT_DEV_BAD_INDEX is OR-ed.
+ */
+int pvt_distill_loss(const pvt_distill* d, float* loss, float* stats, const float* upstream, void* grad,
+                     int32_t grad_dtype, int64_t ldg, uint32_t* status, void* cuda_stream);
+/* The gradient from the statistics of an earlier pvt_distill_loss on the same d; grad as there. */
+int pvt_distill_grad(const pvt_distill* d, const float* stats, const float* upstream, void* grad, int32_t grad_dtype,
+                     int64_t ldg, uint32_t* status, void* cuda_stream);
+
+/*
  * P step, the half that shares its inputs with the V step (Algorithm 3, P-step lines:
  * grad_codebooks = backprop(grad_phi)).  Chain rule through dequantize_weights,
  * W_hat[r, 8c+i] = scale[r] * v[j][i], v[j] = sum_m C_m[codes[j][m]] (the binary32 sum
@@ -415,6 +550,8 @@ void pvt_set_m1_search(int mode);
 #define PVT_KERNEL_ADAM 6        /* the kernel of pvt_adam_update */
 #define PVT_KERNEL_TRUST 7       /* ranking, norm and code saving of pvt_vstep_trust (before its search) */
 #define PVT_KERNEL_REFINE 8      /* the kernel of pvt_vstep_refine */
+#define PVT_KERNEL_MX 9          /* the kernels of the pvt_mx_* calls */
+#define PVT_KERNEL_DISTILL 10    /* the kernels of the pvt_distill_* calls */
 void pvt_timing_enable(int on);
 /* FP32 FMA throughput of the current device, measured: a kernel of independent FMA chains on every SM, timed with
  * CUDA events (synchronises).  scratch: device, at least 2048 floats per SM.  tflops_out: host. */

@@ -16,7 +16,7 @@ import torch
 
 from . import build as _build
 
-PVT_F32, PVT_F16 = 0, 1
+PVT_F32, PVT_F16, PVT_BF16 = 0, 1, 2
 PVT_U8, PVT_U16 = 0, 1
 PVT_OK, PVT_EINVAL, PVT_EUNSUPPORTED, PVT_EWORKSPACE, PVT_ECUDA, PVT_ETOOLARGE = 0, -1, -2, -3, -4, -5
 PVT_NOALLOC_MAX_GROUPS = 1 << 21
@@ -24,8 +24,11 @@ PVT_DEV_BAD_INDEX, PVT_DEV_BAD_CODE, PVT_DEV_WAIT_EXPIRED, PVT_DEV_INTERNAL = 1,
 PVT_KERNEL_SELECT, PVT_KERNEL_ENCODE_MAIN, PVT_KERNEL_ENCODE_AUX, PVT_KERNEL_DEQUANT = 0, 1, 2, 3
 PVT_KERNEL_ENCODE_RESCORE = 4
 PVT_KERNEL_PSTEP_GRAD, PVT_KERNEL_ADAM, PVT_KERNEL_TRUST, PVT_KERNEL_REFINE = 5, 6, 7, 8
+PVT_KERNEL_MX, PVT_KERNEL_DISTILL = 9, 10
 PVT_M1_AUTO, PVT_M1_FP32, PVT_M1_TENSOR = 0, 1, 2
 PVT_SAMPLE_UNIFORM, PVT_SAMPLE_PROPORTIONAL = 0, 1
+PVT_MX_E8M0_32, PVT_MX_E4M3_16 = 0, 1
+PVT_DISTILL_MAX_K, PVT_DISTILL_MAX_VOCAB, PVT_DISTILL_STATS = 1024, 1 << 20, 8
 
 
 _OUT_DTYPE = {torch.float32: PVT_F32, torch.float16: PVT_F16}
@@ -39,6 +42,22 @@ class pvt_layer(ctypes.Structure):
         ("eta", ctypes.c_float), ("reserved_", ctypes.c_int32),
         ("W", ctypes.c_void_p), ("g", ctypes.c_void_p), ("scale", ctypes.c_void_p),
         ("codebooks", ctypes.c_void_p), ("codes", ctypes.c_void_p),
+    ]
+
+
+class pvt_mx(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("format", ctypes.c_int32), ("reserved_", ctypes.c_int32),
+        ("ld", ctypes.c_int64), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("tensor_scale", ctypes.c_void_p),
+    ]
+
+
+class pvt_distill(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("vocab", ctypes.c_int32), ("k", ctypes.c_int32), ("logits", ctypes.c_void_p),
+        ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float),
+        ("top_idx", ctypes.c_void_p), ("top_logit", ctypes.c_void_p), ("teacher_lse", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p),
     ]
 
 
@@ -97,6 +116,25 @@ def lib():
                                       ctypes.c_int32, vp, sz, vp]
         L.pvt_dequant.restype = ctypes.c_int
         L.pvt_dequant.argtypes = [lp, vp, ctypes.c_int32, vp, vp]
+        i32, i64, mp, dp = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(pvt_mx), ctypes.POINTER(pvt_distill)
+        L.pvt_mx_scale_bytes.restype = sz
+        L.pvt_mx_scale_bytes.argtypes = [i32, i32, i32]
+        L.pvt_mx_quantize.restype = ctypes.c_int
+        L.pvt_mx_quantize.argtypes = [mp, vp, i32, i64, vp]
+        L.pvt_mx_dequant.restype = ctypes.c_int
+        L.pvt_mx_dequant.argtypes = [mp, vp, i32, i64, vp]
+        L.pvt_mx_product.restype = ctypes.c_int
+        L.pvt_mx_product.argtypes = [mp, mp, vp, i32, i64, vp, vp]
+        L.pvt_mx_grad_input.restype = ctypes.c_int
+        L.pvt_mx_grad_input.argtypes = [vp, i64, i32, mp, vp, i32, i64, vp, vp]
+        L.pvt_mx_grad_weight.restype = ctypes.c_int
+        L.pvt_mx_grad_weight.argtypes = [vp, i64, i32, mp, vp, i64, i32, vp, vp]
+        L.pvt_distill_top.restype = ctypes.c_int
+        L.pvt_distill_top.argtypes = [vp, i32, i64, i64, i32, i32, fl, vp, vp, vp, vp]
+        L.pvt_distill_loss.restype = ctypes.c_int
+        L.pvt_distill_loss.argtypes = [dp, vp, vp, vp, vp, i32, i64, vp, vp]
+        L.pvt_distill_grad.restype = ctypes.c_int
+        L.pvt_distill_grad.argtypes = [dp, vp, vp, vp, i32, i64, vp, vp]
         L.pvt_pstep_grad.restype = ctypes.c_int
         L.pvt_pstep_grad.argtypes = [lp, vp, vp, vp, vp]
         L.pvt_adam_update.restype = ctypes.c_int
@@ -263,6 +301,206 @@ def pvt_vstep_refine(layer: pvt_layer, idx: torch.Tensor, k: int, max_moves: int
 def pvt_dequant(layer: pvt_layer, W_hat: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
     _check(lib().pvt_dequant(ctypes.byref(layer), W_hat.data_ptr(), _OUT_DTYPE[W_hat.dtype], _ptr(status), _stream_ptr(stream)),
            "pvt_dequant")
+
+
+_DTYPE = {torch.float32: PVT_F32, torch.float16: PVT_F16, torch.bfloat16: PVT_BF16}
+
+
+def _on_device(device, *tensors) -> None:
+    """The calls enqueue on the current device: every tensor has to be there."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device != device):
+            raise ValueError("the tensors of a call lie on one CUDA device")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, what: str):
+    """(dtype, elements from row to row) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols) or t.dtype not in _DTYPE:
+        raise ValueError(f"{what} has to be a float32, float16 or bfloat16 matrix of {rows} x {cols}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {what} have to be contiguous")
+    if rows > 1 and t.stride(0) < cols:
+        raise ValueError(f"the rows of {what} overlap")
+    return _DTYPE[t.dtype], t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} has to be {n} contiguous {dtype}")
+    return t.data_ptr()
+
+
+def _status_word(t: Optional[torch.Tensor]) -> Optional[int]:
+    if t is not None and (t.element_size() != 4 or t.numel() < 1):
+        raise ValueError("status has to be a 4-byte integer")
+    return _ptr(t)
+
+
+class Mx:
+    """A matrix in 4-bit block floating point: its tensors and its descriptor."""
+
+    def __init__(self, codes, scales, rows, cols, fmt, tensor_scale):
+        self.codes, self.scales, self.tensor_scale = codes, scales, tensor_scale
+        self.rows, self.cols, self.format = int(rows), int(cols), int(fmt)
+        self.device = codes.device
+        self.desc = pvt_mx(self.rows, self.cols, self.format, 0, codes.stride(0) if self.rows > 1 else codes.shape[1],
+                           codes.data_ptr(), scales.data_ptr(), _ptr(tensor_scale))
+
+
+def make_mx(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt: int,
+            tensor_scale: Optional[torch.Tensor] = None) -> Mx:
+    """Describe a matrix whose arrays are CUDA tensors.  codes: uint8 [rows, at least ceil(cols / 2)], rows a multiple of 16
+    bytes apart; scales: uint8, pvt_mx_scale_bytes of them; tensor_scale: one float32, for PVT_MX_E4M3_16 only."""
+    if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.shape[0] != rows or codes.stride(1) != 1:
+        raise ValueError("codes have to be uint8 [rows, bytes] with contiguous rows")
+    # (a row is read in pieces of 16 bytes)
+    if codes.shape[1] < (cols + 31) // 32 * 16 or (rows > 1 and codes.stride(0) < codes.shape[1]):
+        raise ValueError("a row of codes has to hold ceil(cols / 32) * 16 bytes")
+    if codes.stride(0) % 16 and rows > 1 or codes.shape[1] % 16:
+        raise ValueError("rows of codes have to be a multiple of 16 bytes apart")
+    if scales.dtype != torch.uint8 or not scales.is_contiguous() or scales.numel() < pvt_mx_scale_bytes(rows, cols, fmt):
+        raise ValueError("scales have to be pvt_mx_scale_bytes contiguous uint8")
+    if tensor_scale is not None and (fmt != PVT_MX_E4M3_16 or tensor_scale.dtype != torch.float32 or tensor_scale.numel() != 1):
+        raise ValueError("tensor_scale has to be one float32, for PVT_MX_E4M3_16")
+    for t in (codes, scales, tensor_scale):
+        if t is not None and (not t.is_cuda or t.device != codes.device):
+            raise ValueError("the tensors of a matrix lie on one CUDA device")
+    return Mx(codes, scales, rows, cols, fmt, tensor_scale)
+
+
+def new_mx(rows: int, cols: int, fmt: int, tensor_scale: Optional[torch.Tensor] = None, device=None) -> Mx:
+    """Room for a matrix of that shape (its content is undefined until pvt_mx_quantize)."""
+    device = device or "cuda"
+    codes = torch.empty(rows, (cols + 31) // 32 * 16, dtype=torch.uint8, device=device)
+    scales = torch.empty(pvt_mx_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device=device)
+    return make_mx(codes, scales, rows, cols, fmt, tensor_scale)
+
+
+def pvt_mx_scale_bytes(rows: int, cols: int, fmt: int) -> int:
+    n = int(lib().pvt_mx_scale_bytes(rows, cols, fmt))
+    if n == 0:
+        raise PvtError(PVT_EINVAL, "pvt_mx_scale_bytes")
+    return n
+
+
+def pvt_mx_quantize(m: Mx, x: torch.Tensor, stream=None) -> None:
+    """x (float32, float16 or bfloat16 [rows, cols], rows of any distance) into m's codes and scales."""
+    dtype, ld = _matrix(x, m.rows, m.cols, "x")
+    _on_device(m.device, x)
+    _check(lib().pvt_mx_quantize(ctypes.byref(m.desc), x.data_ptr(), dtype, ld, _stream_ptr(stream)), "pvt_mx_quantize")
+
+
+def pvt_mx_dequant(m: Mx, values: torch.Tensor, stream=None) -> None:
+    """What m's codes and scales stand for."""
+    dtype, ld = _matrix(values, m.rows, m.cols, "values")
+    _on_device(m.device, values)
+    _check(lib().pvt_mx_dequant(ctypes.byref(m.desc), values.data_ptr(), dtype, ld, _stream_ptr(stream)), "pvt_mx_dequant")
+
+
+def pvt_mx_product(x: Mx, w: Mx, y: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y [tokens, outputs] = x w^T on the block-scaled tensor cores; x [tokens, inputs], w [outputs, inputs]."""
+    dtype, ld = _matrix(y, x.rows, w.rows, "y")
+    _on_device(x.device, w.codes, y, status)
+    _check(lib().pvt_mx_product(ctypes.byref(x.desc), ctypes.byref(w.desc), y.data_ptr(), dtype, ld, _status_word(status),
+                                _stream_ptr(stream)), "pvt_mx_product")
+
+
+def _gradient(dy: torch.Tensor, tokens: int, outputs: int) -> int:
+    """Elements from row to row of the gradient of a product's result."""
+    dtype, ld = _matrix(dy, tokens, outputs, "dy")
+    if dtype != PVT_BF16:
+        raise ValueError("dy has to be bfloat16")
+    return (ld + 7) // 8 * 8 if tokens == 1 else ld
+
+
+def pvt_mx_grad_input(dy: torch.Tensor, w: Mx, dx: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx [tokens, inputs] = dy w; dy bfloat16 [tokens, outputs], 16-byte aligned, rows a multiple of 8 elements apart."""
+    ldy = _gradient(dy, dy.shape[0], w.rows)
+    dtype, ld = _matrix(dx, dy.shape[0], w.cols, "dx")
+    _on_device(w.device, dy, dx, status)
+    _check(lib().pvt_mx_grad_input(dy.data_ptr(), ldy, dy.shape[0], ctypes.byref(w.desc), dx.data_ptr(), dtype, ld,
+                                   _status_word(status), _stream_ptr(stream)), "pvt_mx_grad_input")
+
+
+def pvt_mx_grad_weight(dy: torch.Tensor, x: Mx, dw: torch.Tensor, accumulate: bool = False,
+                       status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dw [outputs, inputs] (float32) = dy^T x, added to what it holds if accumulate; dy as for pvt_mx_grad_input."""
+    ldy = _gradient(dy, x.rows, dy.shape[1])
+    dtype, ld = _matrix(dw, dy.shape[1], x.cols, "dw")
+    if dtype != PVT_F32:
+        raise ValueError("dw has to be float32")
+    _on_device(x.device, dy, dw, status)
+    _check(lib().pvt_mx_grad_weight(dy.data_ptr(), ldy, dy.shape[1], ctypes.byref(x.desc), dw.data_ptr(), ld,
+                                    1 if accumulate else 0, _status_word(status), _stream_ptr(stream)), "pvt_mx_grad_weight")
+
+
+def pvt_distill_top(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                    temperature: float = 1.0, stream=None) -> None:
+    """The k largest logits of each row (int32 and float32 [rows, k], in order) and log sum exp(logits / temperature)."""
+    rows, vocab = logits.shape
+    dtype, ld = _matrix(logits, rows, vocab, "logits")
+    k = int(top_idx.shape[-1])
+    idx, val = _vector(top_idx, rows * k, torch.int32, "top_idx"), _vector(top_logit, rows * k, torch.float32, "top_logit")
+    out = _vector(lse, rows, torch.float32, "lse")
+    _on_device(logits.device, top_idx, top_logit, lse)
+    _check(lib().pvt_distill_top(logits.data_ptr(), dtype, ld, rows, vocab, k, temperature, idx, val, out,
+                                 _stream_ptr(stream)), "pvt_distill_top")
+
+
+class Distill:
+    """The student's logits and what they are trained against: the tensors and their descriptor."""
+
+    def __init__(self, desc, tensors):
+        self.desc, self.tensors = desc, tensors
+        self.device, self.rows, self.vocab = tensors[0].device, int(desc.rows), int(desc.vocab)
+
+
+def make_distill(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor,
+                 teacher_lse: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                 temperature: float = 1.0) -> Distill:
+    """logits [rows, vocab] against the teacher's list (int32 and float32 [rows, k]).  With teacher_lse (float32 [rows], of the
+    same temperature) everything that is not listed is one more outcome, without it the listed probabilities add up to 1."""
+    rows, vocab = logits.shape
+    dtype, ld = _matrix(logits, rows, vocab, "logits")
+    k = int(top_idx.shape[-1])
+    desc = pvt_distill(rows, vocab, k, logits.data_ptr(), ld, dtype, float(temperature),
+                       _vector(top_idx, rows * k, torch.int32, "top_idx"),
+                       _vector(top_logit, rows * k, torch.float32, "top_logit"),
+                       _vector(teacher_lse, rows, torch.float32, "teacher_lse"), _vector(weight, rows, torch.float32, "weight"))
+    tensors = (logits, top_idx, top_logit, teacher_lse, weight)
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device != logits.device):
+            raise ValueError("the tensors of a distillation lie on one CUDA device")
+    return Distill(desc, tensors)
+
+
+def pvt_distill_loss(d: Distill, loss: torch.Tensor, stats: Optional[torch.Tensor] = None,
+                     upstream: Optional[torch.Tensor] = None, grad: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """loss (float32 [rows]); with grad ([rows, vocab], may be the logits) the gradient in the same pass, with stats (float32
+    [rows, PVT_DISTILL_STATS]) what pvt_distill_grad needs."""
+    dtype, ld = _matrix(grad, d.rows, d.vocab, "grad") if grad is not None else (PVT_F32, 0)
+    out = _vector(loss, d.rows, torch.float32, "loss")
+    st = _vector(stats, d.rows * PVT_DISTILL_STATS, torch.float32, "stats")
+    up = _vector(upstream, d.rows, torch.float32, "upstream")
+    _on_device(d.device, loss, stats, upstream, grad, status)
+    _check(lib().pvt_distill_loss(ctypes.byref(d.desc), out, st, up, _ptr(grad), dtype, ld, _status_word(status),
+                                  _stream_ptr(stream)), "pvt_distill_loss")
+
+
+def pvt_distill_grad(d: Distill, stats: torch.Tensor, grad: torch.Tensor, upstream: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradient from the statistics of an earlier pvt_distill_loss on the same d."""
+    dtype, ld = _matrix(grad, d.rows, d.vocab, "grad")
+    st = _vector(stats, d.rows * PVT_DISTILL_STATS, torch.float32, "stats")
+    up = _vector(upstream, d.rows, torch.float32, "upstream")
+    _on_device(d.device, stats, upstream, grad, status)
+    _check(lib().pvt_distill_grad(ctypes.byref(d.desc), st, up, grad.data_ptr(), dtype, ld, _status_word(status),
+                                  _stream_ptr(stream)), "pvt_distill_grad")
 
 
 class Block:

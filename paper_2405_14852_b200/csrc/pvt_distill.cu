@@ -1,0 +1,315 @@
+// The distillation loss of a row and its gradient.
+//
+// The row is read once for its largest logit and the sum of exponentials relative to it (with the teacher's remaining mass as
+// one more outcome: also the sum over what is not listed, told from the rest by one bit per entry of the vocabulary in
+// shared memory, because the difference of the two sums would lose what a student near its teacher leaves there) and, for
+// the gradient, a second time, which the L2 serves: with y = 2^(c (x - largest)) every unlisted logit gets y times one factor.
+// The listed ones are overwritten after that.  What concerns the k listed entries alone, the teacher's probabilities and the loss, is
+// computed in binary64, where the remaining mass 1 - sum p is a small difference too.  Bound by HBM in long batches.
+// A few long rows are shared by clusters of blocks.
+#include "pvt_distill.cuh"
+
+namespace pvt {
+namespace {
+
+using namespace distill;
+using namespace mma;
+
+enum { kLoss = 1, kGrad = 2, kBoth = 3 };
+
+struct DistillParams {
+  const void* logits;
+  int64_t ld;
+  uint32_t vocab, k, blocks;
+  float c;          // log2(e) / temperature
+  double inv_t;
+  const int32_t* top_idx;
+  const float* top_logit;
+  const float* teacher_lse;
+  const float* weight;
+  const float* upstream;
+  float* loss;
+  float* stats;      // written with the loss, read for the gradient alone
+  void* grad;
+  int64_t ldg;
+  uint32_t* status;
+};
+
+// stats of a row: largest logit, factor of y at the listed and at the other logits, logarithm of the teacher's sum in two parts, whether
+// the row has any effect
+enum { kStatMax = 0, kStatListed = 1, kStatRest = 2, kStatNorm = 3, kStatNormLow = 4, kStatActive = 5 };
+
+struct DistillShared {
+  Running run[kThreads / 32];
+  Running mine;
+  double sum[kThreads / 32];
+  float top[kThreads / 32];
+  uint32_t repeated;
+  float stat[PVT_DISTILL_STATS];
+  int32_t idx[PVT_DISTILL_MAX_K];   // -1: left out
+  float x[PVT_DISTILL_MAX_K];       // the student's logit there
+  float val[PVT_DISTILL_MAX_K];
+};
+
+__device__ __forceinline__ double block_sum(double v, double* sh) {
+#pragma unroll
+  for (int s = 16; s >= 1; s /= 2) v += __shfl_xor_sync(0xffffffffu, v, s);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int w = 0; w < kThreads / 32; ++w) v += sh[w];
+  return v;
+}
+
+// zeros over this block's share of the gradient
+template <typename G>
+__device__ __forceinline__ void clear(G* grad, uint32_t from, uint32_t to) {
+  for (uint32_t i = from + threadIdx.x; i < to; i += kThreads) grad[i] = narrow<G>(0.0f);
+}
+
+template <typename T, typename G, int MODE>
+__global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillParams p) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  DistillShared& sm = *reinterpret_cast<DistillShared*>(raw);
+  uint32_t* const listed = reinterpret_cast<uint32_t*>(raw + sizeof(DistillShared));  // a bit per entry of the vocabulary
+  pdl_trigger();
+  pdl_wait();
+  constexpr uint32_t N = Piece<T>::N;
+  const uint32_t tid = threadIdx.x, rank = blockIdx.x % p.blocks, r = blockIdx.x / p.blocks, k = p.k;
+  const T* row = static_cast<const T*>(p.logits) + (int64_t)r * p.ld;
+  G* const grad = MODE & kGrad ? static_cast<G*>(p.grad) + (int64_t)r * p.ldg : nullptr;
+  const RowShare<T> s(row, p.vocab, rank, p.blocks);
+  const float weight = p.weight ? p.weight[r] : 1.0f;
+  const bool tail = p.teacher_lse != nullptr;
+  float* const stats = p.stats ? p.stats + (int64_t)r * PVT_DISTILL_STATS : nullptr;
+
+  // (the same in all blocks of the row: they leave together)
+  bool active = weight != 0.0f;
+  if (MODE == kGrad) active = active && stats[kStatActive] != 0.0f;
+
+  // the list: entries outside the vocabulary or named before are left out
+  if (active) {
+    for (uint32_t i = tid; i < (p.vocab + 31) / 32; i += kThreads) listed[i] = 0;
+    if (tid == 0) sm.repeated = 0;
+    __syncthreads();
+    bool bad = false;
+    for (uint32_t i = tid; i < k; i += kThreads) {
+      int32_t at = p.top_idx[(int64_t)r * k + i];
+      if (at >= (int32_t)p.vocab) bad = true, at = -1;
+      if (at >= 0 && (atomicOr(&listed[at / 32], 1u << (at % 32)) >> (at % 32) & 1u)) sm.repeated = 1;
+      sm.idx[i] = at < 0 ? -1 : at;
+      sm.val[i] = p.top_logit[(int64_t)r * k + i];
+      sm.x[i] = at >= 0 ? widen<T>(row[at]) : 0.0f;  // before any block writes the gradient over the logits
+    }
+    __syncthreads();
+    if (sm.repeated) {
+      uint32_t again = 0;  // of this thread's entries (two at most)
+      for (uint32_t i = tid, n = 0; i < k; i += kThreads, ++n)
+        for (uint32_t j = 0; j < i; ++j)
+          if (sm.idx[i] >= 0 && sm.idx[j] == sm.idx[i]) again |= 1u << n;
+      __syncthreads();
+      for (uint32_t i = tid, n = 0; i < k; i += kThreads, ++n)
+        if (again >> n & 1u) sm.idx[i] = -1, bad = true;
+      __syncthreads();
+    }
+    if (bad && p.status) atomicOr(p.status, PVT_DEV_BAD_INDEX);
+  }
+
+  if (MODE & kLoss) {
+    // the teacher: logarithm of its sum, its probabilities' sum
+    double norm = 0.0, mass = 0.0;
+    if (active) {
+      float top = kMinusInf;
+      for (uint32_t i = tid; i < k; i += kThreads)
+        if (sm.idx[i] >= 0) top = fmaxf(top, sm.val[i] == sm.val[i] ? sm.val[i] : -kMinusInf);  // (a NaN shows in the sum)
+#pragma unroll
+      for (int st = 16; st >= 1; st /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, st));
+      if ((tid & 31) == 0) sm.top[tid / 32] = top;
+      __syncthreads();
+      for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, sm.top[w]);
+      active = top != kMinusInf;
+      if (active) {
+        const double shift = tail ? (double)p.teacher_lse[r] : (double)top * p.inv_t;
+        double own = 0.0;
+        for (uint32_t i = tid; i < k; i += kThreads)
+          if (sm.idx[i] >= 0) own += exp((double)sm.val[i] * p.inv_t - shift);
+        mass = block_sum(own, sm.sum);
+        norm = shift;
+        if (!tail) norm += log(mass), mass = 1.0;
+      }
+    }
+
+    Running run;
+    if (active) {
+      auto add = [&](const float* x, uint32_t n, uint32_t at) {
+        float m = x[0];
+        for (uint32_t e = 1; e < n; ++e) m = fmaxf(m, x[e]);
+        run.raise(m, p.c);
+        for (uint32_t e = 0; e < n; ++e) {
+          const float y = run.term(x[e], p.c);
+          run.z += y;
+          if (tail && !(listed[(at + e) / 32] >> ((at + e) % 32) & 1u)) run.r += y;
+        }
+      };
+      for (uint32_t i = s.lo + tid; i < s.hi; i += kThreads) {
+        const Piece<T> piece = *reinterpret_cast<const Piece<T>*>(row + s.head + i * N);
+        float x[N];
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) x[e] = widen<T>(piece.v[e]);
+        add(x, N, s.head + i * N);
+      }
+      if (tid < s.loose()) {
+        const float x = widen<T>(row[s.loose_at(tid)]);
+        add(&x, 1, s.loose_at(tid));
+      }
+      run = block_merge(run, p.c, sm.run);
+    }
+    if (p.blocks > 1) {
+      if (tid == 0) sm.mine = run;
+      cluster_sync();
+      Running all;
+      for (uint32_t q = 0; q < p.blocks; ++q) {
+        Running other;
+        other.m = cluster_load(smem_u32(&sm.mine.m), q);
+        other.z = cluster_load(smem_u32(&sm.mine.z), q);
+        other.r = cluster_load(smem_u32(&sm.mine.r), q);
+        all = merge(all, other, p.c);
+      }
+      run = all;
+      cluster_sync();
+    }
+    // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
+    if (active && run.m == kMinusInf && run.z == 0.0f) active = false;
+
+    double value = 0.0;
+    float f_listed = 0.0f, f_rest = 0.0f;
+    if (active) {
+      const double z = run.z, log_z = log(z);
+      const double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
+      if (rank == 0) {
+        for (uint32_t i = tid; i < k; i += kThreads)
+          if (sm.idx[i] >= 0) {
+            const double log_p = (double)sm.val[i] * p.inv_t - norm, prob = exp(log_p);
+            const double log_q = ((double)sm.x[i] - (double)run.m) * p.inv_t - log_z;
+            if (prob != 0.0) value += prob * (log_p - log_q);
+          }
+        value = block_sum(value, sm.sum);
+        if (rest != 0.0) value += rest * (log(rest) - (log((double)run.r) - log_z));
+      }
+      const double whole = mass + rest;
+      f_listed = (float)(whole / z);
+      // nothing unlisted left in the student: no factor is needed there
+      f_rest = (float)(whole / z - (rest != 0.0 && run.r != 0.0f ? rest / (double)run.r : 0.0));
+    }
+    if (tid == 0) {
+      sm.stat[kStatMax] = run.m, sm.stat[kStatListed] = f_listed, sm.stat[kStatRest] = f_rest;
+      sm.stat[kStatNorm] = (float)norm, sm.stat[kStatNormLow] = (float)(norm - (double)(float)norm);
+      sm.stat[kStatActive] = active ? 1.0f : 0.0f, sm.stat[6] = sm.stat[7] = 0.0f;
+      if (rank == 0) p.loss[r] = active ? (float)((double)weight * value) : 0.0f;
+    }
+    __syncthreads();
+    if (rank == 0 && stats && tid < PVT_DISTILL_STATS) stats[tid] = sm.stat[tid];
+  }
+
+  if (MODE & kGrad) {
+    if (MODE == kGrad) {
+      if (tid < PVT_DISTILL_STATS) sm.stat[tid] = stats[tid];
+      // in place: no block overwrites logits that another has yet to gather
+      if (p.blocks > 1) cluster_sync();
+      __syncthreads();
+    }
+    if (!active) {
+      clear(grad, s.from(), s.to());
+      return;
+    }
+    const float up = (float)((double)weight * (p.upstream ? (double)p.upstream[r] : 1.0) * p.inv_t);
+    const float m = sm.stat[kStatMax], f_listed = sm.stat[kStatListed], f_rest = sm.stat[kStatRest] * up;
+    auto y_of = [&](float x) { return ex2((x - m) * p.c); };
+    if (sizeof(G) == sizeof(T) && (reinterpret_cast<uintptr_t>(grad) - reinterpret_cast<uintptr_t>(row)) % 16 == 0) {
+      for (uint32_t i = s.lo + tid; i < s.hi; i += kThreads) {
+        const Piece<T> piece = *reinterpret_cast<const Piece<T>*>(row + s.head + i * N);
+        Piece<G> out;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) out.v[e % Piece<G>::N] = narrow<G>(y_of(widen<T>(piece.v[e])) * f_rest);
+        *reinterpret_cast<Piece<G>*>(grad + s.head + i * N) = out;
+      }
+      if (tid < s.loose()) {
+        const uint32_t at = s.loose_at(tid);
+        grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
+      }
+    } else {
+      // rows of unlike alignment: element by element, a warp along the row
+      const uint32_t to = s.to();
+      uint32_t at = s.from() + tid;
+      for (; at + 3 * kThreads < to; at += 4 * kThreads) {
+        float x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = widen<T>(row[at + u * kThreads]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) grad[at + u * kThreads] = narrow<G>(y_of(x[u]) * f_rest);
+      }
+      for (; at < to; at += kThreads) grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
+    }
+    __syncthreads();
+    const double norm = (double)sm.stat[kStatNorm] + (double)sm.stat[kStatNormLow];
+    for (uint32_t i = tid; i < k; i += kThreads) {
+      const int32_t at = sm.idx[i];
+      if (at < 0 || (uint32_t)at < s.from() || (uint32_t)at >= s.to()) continue;
+      const float prob = (float)exp((double)sm.val[i] * p.inv_t - norm);
+      grad[at] = narrow<G>((y_of(sm.x[i]) * f_listed - prob) * up);
+    }
+  }
+}
+
+template <typename T, typename G, int MODE>
+cudaError_t start(const DistillParams& p, int64_t rows, cudaStream_t stream) {
+  const cudaError_t e = allow_smem<distill_kernel<T, G, MODE>>();
+  if (e != cudaSuccess) return e;
+  const size_t smem = sizeof(DistillShared) + (size_t)(p.vocab + 31) / 32 * 4;
+  return launch_clusters(distill_kernel<T, G, MODE>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
+}
+template <typename T, int MODE>
+cudaError_t by_grad(const DistillParams& p, int64_t rows, int32_t grad_dtype, cudaStream_t stream) {
+  return grad_dtype == PVT_F32   ? start<T, float, MODE>(p, rows, stream)
+         : grad_dtype == PVT_F16 ? start<T, __half, MODE>(p, rows, stream)
+                                 : start<T, __nv_bfloat16, MODE>(p, rows, stream);
+}
+template <typename T>
+cudaError_t by_mode(const DistillParams& p, int64_t rows, int32_t grad_dtype, cudaStream_t stream) {
+  if (!p.grad) return start<T, T, kLoss>(p, rows, stream);
+  return p.loss ? by_grad<T, kBoth>(p, rows, grad_dtype, stream) : by_grad<T, kGrad>(p, rows, grad_dtype, stream);
+}
+
+cudaError_t launch(const pvt_distill& d, DistillParams& p, int32_t grad_dtype, int sm_count, cudaStream_t stream) {
+  p.logits = d.logits, p.ld = d.ld, p.vocab = (uint32_t)d.vocab, p.k = (uint32_t)d.k;
+  p.c = (float)(1.4426950408889634 / (double)d.temperature), p.inv_t = 1.0 / (double)d.temperature;
+  p.top_idx = d.top_idx, p.top_logit = d.top_logit, p.teacher_lse = d.teacher_lse, p.weight = d.weight;
+  p.blocks = row_blocks(d.rows, (int64_t)d.vocab * (d.dtype == PVT_F32 ? 4 : 2), sm_count);
+  if (d.rows * p.blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  timing_begin(kKernDistill, stream);
+  const cudaError_t e = d.dtype == PVT_F32   ? by_mode<float>(p, d.rows, grad_dtype, stream)
+                        : d.dtype == PVT_F16 ? by_mode<__half>(p, d.rows, grad_dtype, stream)
+                                             : by_mode<__nv_bfloat16>(p, d.rows, grad_dtype, stream);
+  timing_end(kKernDistill, stream);
+  count_launches(1);
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_distill_loss(const pvt_distill& d, float* loss, float* stats, const float* upstream, void* grad,
+                                int32_t grad_dtype, int64_t ldg, uint32_t* status, int sm_count, cudaStream_t stream) {
+  DistillParams p = {};
+  p.loss = loss, p.stats = stats, p.upstream = upstream, p.grad = grad, p.ldg = ldg, p.status = status;
+  return launch(d, p, grad_dtype, sm_count, stream);
+}
+
+cudaError_t launch_distill_grad(const pvt_distill& d, const float* stats, const float* upstream, void* grad, int32_t grad_dtype,
+                                int64_t ldg, uint32_t* status, int sm_count, cudaStream_t stream) {
+  DistillParams p = {};
+  p.stats = const_cast<float*>(stats), p.upstream = upstream, p.grad = grad, p.ldg = ldg, p.status = status;
+  return launch(d, p, grad_dtype, sm_count, stream);
+}
+
+}  // namespace pvt

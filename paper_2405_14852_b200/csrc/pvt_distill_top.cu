@@ -1,0 +1,333 @@
+// The k largest logits of each row, in order, and the logarithm of the sum of all exponentials.
+//
+// One pass over the row keeps, besides the running sum, the largest value of each of 2048 parts of it (four per thread).  The
+// k-th largest of those maxima has at least k elements not below it, so everything that is listed is among the elements that
+// reach it; with parts in no relation to the values those are few more (n with 2048 ln(2048 / (2048 - k)) ~ n: 65 for k =
+// 64, 1420 for k = 1024).  A second pass over the row, which comes from the L2, collects them, and they are put in order
+// in shared memory.  A row in which too many elements are equal (or that is laid out against this) is settled by counting the digits
+// of its keys instead.  A few long rows are shared by clusters: each block lists its part, and an entry's place is its own plus
+// those that the other blocks' lists hold ahead of it.
+#include "pvt_distill.cuh"
+
+namespace pvt {
+namespace {
+
+using namespace distill;
+using namespace mma;
+
+constexpr int kParts = 4;           // of each thread
+constexpr int kCandidates = 2048;   // that are put in order at once
+constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
+
+// Order of the list: larger keys first; NaN above all, -0 as 0.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key ^ 0x80000000u : ~key); }
+// ascending: larger key first, then lower index
+__device__ __forceinline__ uint64_t entry_of(uint32_t key, uint32_t at) { return (uint64_t)(~key) << 32 | at; }
+
+struct TopParams {
+  const void* logits;
+  int64_t ld;
+  uint32_t vocab, k, blocks;
+  float c;            // log2(e) / temperature
+  float inv_t;
+  int32_t* top_idx;
+  float* top_logit;
+  float* lse;
+};
+
+struct TopShared {
+  Running run[kThreads / 32];
+  Running mine;
+  uint32_t parts[kThreads * kParts];
+  uint32_t hist[256];
+  uint32_t digit, above, count, n;
+  uint64_t entries[kCandidates];
+  uint64_t sorted[PVT_DISTILL_MAX_K];
+};
+
+// The digit (8 bits) in which the `want`-th largest key falls, and how many keys have larger digits: hist[d] holds the number of
+// keys with digit d.  If there are fewer than `want` keys the digit is 0.
+__device__ __forceinline__ void find_digit(TopShared& sm, uint32_t want) {
+  if (threadIdx.x < 32) {
+    const uint32_t lane = threadIdx.x;
+    uint32_t own[8], sum = 0;  // digits 255 - 8 lane downwards
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += own[i] = sm.hist[255 - 8 * lane - i];
+    uint32_t before = sum;
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) {
+      const uint32_t o = __shfl_up_sync(0xffffffffu, before, s);
+      if (lane >= s) before += o;
+    }
+    const uint32_t total = __shfl_sync(0xffffffffu, before, 31);
+    before -= sum;
+    if (before < want && want <= before + sum) {
+      int i = 0;
+      while (before + own[i] < want) before += own[i++];
+      sm.digit = 255 - 8 * lane - i;
+      sm.above = before;
+    }
+    if (lane == 0 && total < want) sm.digit = 0, sm.above = total - sm.hist[0];
+  }
+  __syncthreads();
+}
+
+template <typename T, typename F>
+__device__ __forceinline__ void for_each(const T* row, const RowShare<T>& s, F f) {
+  for (uint32_t i = s.lo + threadIdx.x; i < s.hi; i += kThreads) {
+    const Piece<T> p = *reinterpret_cast<const Piece<T>*>(row + s.head + i * Piece<T>::N);
+#pragma unroll
+    for (uint32_t e = 0; e < Piece<T>::N; ++e) f(key_of(widen<T>(p.v[e])), s.head + i * Piece<T>::N + e);
+  }
+  if (threadIdx.x < s.loose()) {
+    const uint32_t at = s.loose_at(threadIdx.x);
+    f(key_of(widen<T>(row[at])), at);
+  }
+}
+
+// n entries (at most kCandidates) in order; the first min(n, k) to sm.sorted
+__device__ __forceinline__ void put_in_order(TopShared& sm, uint32_t n, uint32_t k) {
+  if (n <= kThreads) {
+    if (threadIdx.x < n) {
+      const uint64_t own = sm.entries[threadIdx.x];
+      uint32_t place = 0;
+      for (uint32_t i = 0; i < n; ++i) place += sm.entries[i] < own;
+      if (place < k) sm.sorted[place] = own;
+    }
+  } else {
+    uint32_t size = 2 * kThreads;
+    while (size < n) size *= 2;
+    for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sm.entries[i] = ~0ull;
+    __syncthreads();
+    for (uint32_t run = 2; run <= size; run *= 2)
+      for (uint32_t step = run / 2; step > 0; step /= 2) {
+        for (uint32_t i = threadIdx.x; i < size / 2; i += kThreads) {
+          const uint32_t a = 2 * i - (i & (step - 1)), b = a + step;
+          const uint64_t x = sm.entries[a], y = sm.entries[b];
+          if ((x > y) == ((a & run) == 0)) sm.entries[a] = y, sm.entries[b] = x;
+        }
+        __syncthreads();
+      }
+    for (uint32_t i = threadIdx.x; i < min(n, k); i += kThreads) sm.sorted[i] = sm.entries[i];
+  }
+  __syncthreads();
+}
+
+// The same for a row whose candidates are too many: the k-th largest key by its digits, every larger one, and of its equals those
+// with the lowest indices.
+template <typename T>
+__device__ __noinline__ uint32_t by_digits(TopShared& sm, const T* row, const RowShare<T>& s, uint32_t k) {
+  uint32_t prefix = 0, want = k;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (uint32_t i = threadIdx.x; i < 256; i += kThreads) sm.hist[i] = 0;
+    __syncthreads();
+    const uint32_t above = shift == 24 ? 0 : prefix >> (shift + 8);
+    for_each(row, s, [&](uint32_t key, uint32_t) {
+      if (key > kLowest && (shift == 24 || key >> (shift + 8) == above)) atomicAdd(&sm.hist[key >> shift & 255], 1u);
+    });
+    __syncthreads();
+    find_digit(sm, want);
+    prefix |= sm.digit << shift;
+    want -= sm.above;
+    __syncthreads();
+  }
+  // `want` of those equal to prefix (more than kCandidates elements reach the bound, so k exist above -infinity)
+  if (threadIdx.x == 0) sm.count = 0;
+  __syncthreads();
+  for_each(row, s, [&](uint32_t key, uint32_t at) {
+    if (key > prefix) sm.entries[atomicAdd(&sm.count, 1u)] = entry_of(key, at);
+  });
+  __syncthreads();
+  const uint32_t larger = sm.count;
+  uint32_t found = 0;
+  for (uint32_t at0 = s.from(); at0 < s.to() && found < want; at0 += kThreads) {
+    const uint32_t at = at0 + threadIdx.x;
+    const bool equal = at < s.to() && key_of(widen<T>(row[at])) == prefix;
+    const uint32_t ballot = __ballot_sync(0xffffffffu, equal);
+    if ((threadIdx.x & 31) == 0) sm.hist[threadIdx.x / 32] = __popc(ballot);
+    __syncthreads();
+    uint32_t before = found, all = found;
+    for (uint32_t w = 0; w < kThreads / 32; ++w) {
+      if (w < threadIdx.x / 32) before += sm.hist[w];
+      all += sm.hist[w];
+    }
+    before += __popc(ballot & ((1u << (threadIdx.x & 31)) - 1));
+    if (equal && before < want) sm.entries[larger + before] = entry_of(prefix, at);
+    found = all;
+    __syncthreads();
+  }
+  put_in_order(sm, k, k);
+  return k;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) distill_top_kernel(const TopParams p) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  TopShared& sm = *reinterpret_cast<TopShared*>(raw);
+  pdl_trigger();
+  pdl_wait();
+  constexpr uint32_t N = Piece<T>::N;
+  const uint32_t tid = threadIdx.x, rank = blockIdx.x % p.blocks, r = blockIdx.x / p.blocks, k = p.k;
+  const T* row = static_cast<const T*>(p.logits) + (int64_t)r * p.ld;
+  const RowShare<T> s(row, p.vocab, rank, p.blocks);
+
+  Running run;
+  uint32_t part[kParts] = {};
+  auto add = [&](uint32_t& top, const float* x, int n) {
+    float m = x[0];
+    for (int e = 1; e < n; ++e) m = fmaxf(m, x[e]);
+    run.raise(m, p.c);
+    uint32_t key = key_of(m);
+    for (int e = 0; e < n; ++e) {
+      run.z += run.term(x[e], p.c);
+      if (x[e] != x[e]) key = 0xffffffffu;
+    }
+    top = max(top, key);
+  };
+  for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kParts * kThreads) {
+    Piece<T> piece[kParts];
+#pragma unroll
+    for (int u = 0; u < kParts; ++u)
+      if (i0 + u * kThreads < s.hi) piece[u] = *reinterpret_cast<const Piece<T>*>(row + s.head + (i0 + u * kThreads) * N);
+#pragma unroll
+    for (int u = 0; u < kParts; ++u)
+      if (i0 + u * kThreads < s.hi) {
+        float x[N];
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) x[e] = widen<T>(piece[u].v[e]);
+        add(part[u], x, N);
+      }
+  }
+  if (tid < s.loose()) {
+    const float x = widen<T>(row[s.loose_at(tid)]);
+    add(part[0], &x, 1);
+  }
+#pragma unroll
+  for (int u = 0; u < kParts; ++u) sm.parts[tid + u * kThreads] = part[u];
+  if (tid == 0) sm.count = 0;
+  run = block_merge(run, p.c, sm.run);
+  if (tid == 0) sm.mine = run;
+
+  // the k-th largest of the parts' maxima, its upper half: what is below reaches no place of the list
+  uint32_t bound = 0, want = k;
+#pragma unroll
+  for (int shift = 24; shift >= 16; shift -= 8) {
+    if (tid < 256) sm.hist[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kParts; ++u)
+      if (shift == 24 || part[u] >> 24 == bound >> 24) atomicAdd(&sm.hist[part[u] >> shift & 255], 1u);
+    __syncthreads();
+    find_digit(sm, want);
+    bound |= sm.digit << shift;
+    want -= sm.above;
+    __syncthreads();
+  }
+  bound = max(bound, kLowest + 1);
+  for_each(row, s, [&](uint32_t key, uint32_t at) {
+    if (key >= bound) {
+      const uint32_t n = atomicAdd(&sm.count, 1u);
+      if (n < kCandidates) sm.entries[n] = entry_of(key, at);
+    }
+  });
+  __syncthreads();
+  const uint32_t found = sm.count;
+  uint32_t n = min(found, k);
+  if (found <= kCandidates)
+    put_in_order(sm, found, k);
+  else
+    n = by_digits(sm, row, s, k);
+
+  int32_t* idx = p.top_idx + (int64_t)r * k;
+  float* val = p.top_logit + (int64_t)r * k;
+  auto put = [&](uint32_t place, uint64_t entry) {
+    idx[place] = (int32_t)(uint32_t)entry;
+    val[place] = value_of(~(uint32_t)(entry >> 32));
+  };
+  uint32_t total = n;
+  if (p.blocks == 1) {
+    for (uint32_t i = tid; i < n; i += kThreads) put(i, sm.sorted[i]);
+  } else {
+    if (tid == 0) sm.n = n;
+    cluster_sync();
+    // the other blocks' lists, one after the other, behind this block's own memory
+    uint64_t* lists = reinterpret_cast<uint64_t*>(raw + sizeof(TopShared));
+    uint32_t size[8];
+    run = sm.mine;
+    Running sum;
+    for (uint32_t q = 0; q < p.blocks; ++q) {
+      Running other;
+      other.m = cluster_load(smem_u32(&sm.mine.m), q);
+      other.z = cluster_load(smem_u32(&sm.mine.z), q);
+      sum = merge(sum, other, p.c);
+      size[q] = __float_as_uint(cluster_load(smem_u32(&sm.n), q));
+      for (uint32_t i = tid; i < 2 * size[q]; i += kThreads)
+        reinterpret_cast<float*>(lists + q * k)[i] = cluster_load(smem_u32(sm.sorted) + 4 * i, q);
+    }
+    run = sum;
+    __syncthreads();
+    for (uint32_t i = tid; i < n; i += kThreads) {
+      const uint64_t own = sm.sorted[i];
+      uint32_t place = i;
+      for (uint32_t q = 0; q < p.blocks; ++q) {
+        if (q == rank) continue;
+        uint32_t lo = 0, hi = size[q];
+        while (lo < hi) {
+          const uint32_t mid = (lo + hi) / 2;
+          if (lists[q * k + mid] < own)
+            lo = mid + 1;
+          else
+            hi = mid;
+        }
+        place += lo;
+      }
+      if (place < k) put(place, own);
+    }
+    total = 0;
+    for (uint32_t q = 0; q < p.blocks; ++q) total += size[q];
+    cluster_sync();  // no block leaves while another reads its lists
+  }
+  if (rank == 0) {
+    for (uint32_t i = total + tid; i < k; i += kThreads) {
+      idx[i] = -1;
+      val[i] = kMinusInf;
+    }
+    if (tid == 0 && p.lse)
+      p.lse[r] = run.m * p.inv_t + logf(run.z);  // (no logit above -infinity: log 0; an infinite one, or a NaN: itself)
+  }
+}
+
+template <typename T>
+cudaError_t top(const TopParams& p, int64_t rows, size_t smem, cudaStream_t stream) {
+  const cudaError_t e = allow_smem<distill_top_kernel<T>>();
+  if (e != cudaSuccess) return e;
+  return launch_clusters(distill_top_kernel<T>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_distill_top(const void* logits, int32_t dtype, int64_t ld, int64_t rows, int32_t vocab, int32_t k,
+                               float temperature, int32_t* top_idx, float* top_logit, float* lse, int sm_count,
+                               cudaStream_t stream) {
+  TopParams p = {};
+  p.logits = logits, p.ld = ld, p.vocab = (uint32_t)vocab, p.k = (uint32_t)k;
+  p.c = (float)(1.4426950408889634 / (double)temperature), p.inv_t = (float)(1.0 / (double)temperature);
+  p.top_idx = top_idx, p.top_logit = top_logit, p.lse = lse;
+  p.blocks = row_blocks(rows, (int64_t)vocab * (dtype == PVT_F32 ? 4 : 2), sm_count);
+  if (rows * p.blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  const size_t smem = sizeof(TopShared) + (p.blocks > 1 ? (size_t)p.blocks * p.k * 8 : 0);
+  timing_begin(kKernDistill, stream);
+  const cudaError_t e = dtype == PVT_F32   ? top<float>(p, rows, smem, stream)
+                        : dtype == PVT_F16 ? top<__half>(p, rows, smem, stream)
+                                           : top<__nv_bfloat16>(p, rows, smem, stream);
+  timing_end(kKernDistill, stream);
+  count_launches(1);
+  return e;
+}
+
+}  // namespace pvt

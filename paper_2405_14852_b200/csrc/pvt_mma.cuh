@@ -1,0 +1,157 @@
+// What the products on 4-bit matrices share: tensor maps, bounded waits, tcgen05 and cluster instructions.
+#pragma once
+
+#include <cuda.h>
+
+#include "pvt_encode_m1.cuh"
+
+namespace pvt {
+namespace mma {
+
+// Describes rows x cols elements of `size` bytes (1 or 2), rows pitch bytes apart, to the copy engine, in boxes of box_rows
+// rows of 128 bytes under the 128-byte swizzle; what lies outside reads as zero.  base and pitch: multiples of 16.
+cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows);
+
+#ifdef __CUDACC__
+using m1::bulk_g2s;
+using m1::mbar_arrive;
+using m1::mbar_expect_tx;
+using m1::mbar_init;
+using m1::mbar_try_wait;
+using m1::smem_u32;
+
+// Gives up after max_spins polls, or once another thread of the block has: the block is then abandoned.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* abandoned, uint32_t* status,
+                                     uint32_t max_spins) {
+  for (uint32_t spin = 0; spin < max_spins; ++spin) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (*abandoned) return false;
+    if (spin > 4096) __nanosleep(64);
+  }
+  *abandoned = 1;
+  if (status) atomicOr(status, PVT_DEV_WAIT_EXPIRED);
+  return false;
+}
+// For what has been issued and does complete: copies and products in flight when a block is abandoned.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+  for (uint32_t spin = 0; spin < m1::kMaxSpins; ++spin)
+    if (mbar_try_wait(bar, parity)) return;
+}
+
+// One box at column x (elements; x * size is a multiple of 16 bytes) and row y.
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish() {
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+// called by the whole warp: one arrival once everything its elected thread has issued so far has completed
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred one;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "@one tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+      : "memory");
+}
+
+// Shared-memory operand descriptors: start, the two strides (bytes), 128-byte swizzle or none.
+// Swizzled, K contiguous: rows of 128 bytes, groups of eight rows `strided` = 1024 apart.
+// Swizzled, M or N contiguous: 64 elements to a row of 128 bytes, one row per k, groups of eight k `strided` = 1024
+// apart, the next 64 elements `leading` further.
+__device__ __forceinline__ uint64_t operand(uint32_t saddr, uint32_t leading, uint32_t strided, bool swizzled) {
+  return (uint64_t)((saddr & 0x3ffffu) >> 4) | ((uint64_t)(leading >> 4) << 16) | ((uint64_t)(strided >> 4) << 32) |
+         (1ull << 46) | (swizzled ? 2ull << 61 : 0ull);
+}
+
+// 32 lanes x 32 columns of 32-bit accumulators
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr)
+      : "memory");
+}
+// 32 lanes x 16 columns
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
+// (the registers pass through the statement: no use of them can be scheduled ahead of the wait)
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; i += 8)
+    asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]),
+                      "+r"(v[i + 7]));
+}
+
+// ---- clusters: the blocks of a cluster share a sum, one part of it each ----
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float cluster_load(uint32_t saddr, uint32_t rank) {
+  uint32_t at;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(saddr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// a grid whose blocks form clusters of `cluster`, and whose start may overlap the kernel ahead (see launch_dependent)
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned grid, unsigned cluster, unsigned block, size_t smem,
+                            cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+#endif
+
+}  // namespace mma
+}  // namespace pvt

@@ -1,0 +1,311 @@
+// Product of two matrices in 4-bit block floating point, y = x w^T, on the tensor cores' block-scaled instructions
+// (tcgen05.mma kind::mxf4 / mxf4nvf4): elements and scales go in as they lie in memory, sums come out in binary32.
+//
+// A tile is 128 rows of w (the instruction's M) times 16 to 256 rows of x (its N): with the weights on the side of fixed size a
+// single token costs 16 columns instead of 128 rows, and the accumulator's lanes are consecutive outputs of a token.  One step
+// of a tile is 256 columns: 128 bytes of each row, copied by TMA under the 128-byte swizzle, and the scales of
+// those columns, 2 or 4 tiles per 128 rows, which lie in memory as tensor memory wants them (tcgen05.cp, each part of 32
+// lanes for all four).  Four products of 64 columns each follow.  Tensor memory holds the scales of every stage: a stage is
+// refilled once the products that read it have completed, so nothing is overwritten early.
+//
+// Few tiles leave most SMs idle, so the steps of a tile are then shared by a cluster of up to eight blocks, whose
+// partial sums meet in shared memory across the cluster, always in the order of ranks.
+#include "pvt_mma.cuh"
+#include "pvt_mx.cuh"
+
+namespace pvt {
+namespace {
+
+using namespace mx;
+using namespace mma;
+
+constexpr int kPThreads = 192;   // four warps read sums out, one copies, one multiplies
+constexpr int kCopyWarp = 4, kMmaWarp = 5;
+constexpr int kTileW = 128;      // rows of w
+constexpr int kRowBytes = 128;   // of a step
+constexpr int kMaxStages = 8;
+
+struct ProductParams {
+  const uint8_t* w_scales;
+  const uint8_t* x_scales;
+  const float* w_ts;
+  const float* x_ts;
+  void* y;
+  int64_t ldy;
+  uint32_t* status;
+  uint32_t w_rows, x_rows, x_strips;
+  uint32_t strip_bytes;   // scales of a strip of 128 rows
+  uint32_t steps;         // of 256 columns
+  uint32_t x_tiles;
+  uint32_t tile_x;        // rows of x per tile
+  uint32_t stages, stage_bytes, tmem_cols;
+  uint32_t split;         // blocks per tile
+  uint32_t max_spins, withhold;
+};
+
+struct ProductShared {
+  alignas(8) uint64_t full[kMaxStages];
+  uint64_t empty[kMaxStages];
+  uint64_t done, spare;
+  uint32_t tmem, abandoned;
+};
+
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc) {
+  asm volatile(
+      "{\n\t.reg .pred one;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "@one tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
+      : "memory");
+}
+template <int FMT>
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                         uint32_t onto) {
+  if (FMT == PVT_MX_E8M0_32) {
+    asm volatile(
+        "{\n\t.reg .pred one, p;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "@one tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred one, p;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "@one tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
+        : "memory");
+  }
+}
+
+template <typename T, int FMT>
+__global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_constant__ CUtensorMap w_map,
+                                                               const __grid_constant__ CUtensorMap x_map, const ProductParams p) {
+  constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;  // scale tiles of a step and strip
+  extern __shared__ __align__(1024) unsigned char raw[];
+  __shared__ ProductShared sm;
+  const uint32_t tid = threadIdx.x, warp = tid >> 5;
+  volatile uint32_t* abandoned = &sm.abandoned;
+  if (tid == 0) {
+    sm.abandoned = 0;
+    for (uint32_t s = 0; s < p.stages; ++s) {
+      mbar_init(smem_u32(&sm.full[s]), 1);
+      mbar_init(smem_u32(&sm.empty[s]), 1);
+    }
+    mbar_init(smem_u32(&sm.done), 1);
+    mbar_init(smem_u32(&sm.spare), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(&sm.tmem), p.tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_trigger();  // not before this block has its tensor memory: the next kernel's blocks hold theirs while they wait for this one
+  pdl_wait();
+
+  const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
+  const uint32_t rank = blockIdx.x % p.split, tile = blockIdx.x / p.split;
+  const uint32_t w0 = tile / p.x_tiles * kTileW, x0 = tile % p.x_tiles * p.tile_x;
+  const uint32_t first = p.steps * rank / p.split, last = p.steps * (rank + 1) / p.split;  // (steps < 2^20, split <= 8)
+  const uint32_t x_strips = min((p.tile_x + kStrip - 1) / kStrip, p.x_strips - x0 / kStrip);
+  // a stage: rows of w, rows of x, scales of w, scales of x
+  const uint32_t x_at = kTileW * kRowBytes, ws_at = x_at + p.tile_x * kRowBytes, xs_at = ws_at + KT * kTileBytes;
+
+  if (warp == kCopyWarp) {
+    if (elect_one()) {
+      const uint32_t bytes = (kTileW + p.tile_x) * kRowBytes + (1 + x_strips) * KT * kTileBytes;
+      const uint8_t* ws = p.w_scales + (size_t)(w0 / kStrip) * p.strip_bytes;
+      const uint8_t* xs = p.x_scales + (size_t)(x0 / kStrip) * p.strip_bytes;
+      uint32_t i = 0;
+      for (uint32_t step = first; step < last; ++step, ++i) {
+        const uint32_t s = i % p.stages, bar = smem_u32(&sm.full[s]), to = base + s * p.stage_bytes;
+        if (i >= p.stages && !wait(smem_u32(&sm.empty[s]), (i / p.stages - 1) & 1, abandoned, p.status, p.max_spins)) break;
+        if (i == p.withhold) continue;  // test hook: never issued
+        mbar_expect_tx(bar, bytes);
+        tma_load(to, &w_map, (int)(step * kRowBytes), (int)w0, bar);
+        tma_load(to + x_at, &x_map, (int)(step * kRowBytes), (int)x0, bar);
+        bulk_g2s(to + ws_at, ws + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
+        for (uint32_t q = 0; q < x_strips; ++q)
+          bulk_g2s(to + xs_at + q * (KT * kTileBytes), xs + (size_t)q * p.strip_bytes + (size_t)step * (KT * kTileBytes),
+                   KT * kTileBytes, bar);
+      }
+      if (*abandoned)  // what was issued lands before the block's memory is another's
+        for (uint32_t j = i > p.stages ? i - p.stages : 0; j < i; ++j)
+          if (j != p.withhold) drain(smem_u32(&sm.full[j % p.stages]), (j / p.stages) & 1);
+    }
+  } else if (warp == kMmaWarp) {
+    const uint32_t d_cols = max(p.tile_x, 32u);
+    // e2m1 both, N, M = 128, type of the scales
+    const uint32_t idesc = 1u << 7 | 1u << 10 | (p.tile_x >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | 1u << 27;
+    const uint32_t x_tiles = (p.tile_x + kStrip - 1) / kStrip, sf_cols = KT * 4 * (1 + x_tiles);
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint32_t step = first; step < last && ok; ++step, ++i) {
+      const uint32_t s = i % p.stages, from = base + s * p.stage_bytes;
+      ok = wait(smem_u32(&sm.full[s]), (i / p.stages) & 1, abandoned, p.status, p.max_spins);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t sfa = tmem + d_cols + s * sf_cols, sfb = sfa + KT * 4;
+      // a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart
+      for (uint32_t t = 0; t < KT; ++t) {
+        scales_to_tmem(sfa + t * 4, operand(from + ws_at + t * kTileBytes, 0, 128, false));
+        for (uint32_t q = 0; q < x_tiles; ++q)
+          scales_to_tmem(sfb + (t * x_tiles + q) * 4, operand(from + xs_at + (q * KT + t) * kTileBytes, 0, 128, false));
+      }
+      const uint64_t a = operand(from, 16, 1024, true), b = operand(from + x_at, 16, 1024, true);
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {  // 64 columns, 32 bytes
+        const uint32_t t = FMT == PVT_MX_E8M0_32 ? j / 2 : j, id = FMT == PVT_MX_E8M0_32 ? (j & 1) * 2 : 0;
+        multiply<FMT>(tmem, a + 2 * j, b + 2 * j, idesc | id << 4 | id << 29, sfa + t * 4, sfb + t * x_tiles * 4,
+                      (uint32_t)(i > 0 || j > 0));
+      }
+      commit(smem_u32(&sm.empty[s]));
+    }
+    if (ok) {
+      commit(smem_u32(&sm.done));
+    } else if (i > 0) {
+      commit(smem_u32(&sm.spare));
+      drain(smem_u32(&sm.spare), 0);
+    }
+  } else {
+    // the sums of 128 rows of w by 32 columns of x at a time; lanes are consecutive outputs of a token
+    const bool ok = wait(smem_u32(&sm.done), 0, abandoned, p.status, p.max_spins);
+    tc_fence_after();
+    float alpha = 1.0f;
+    if (p.w_ts) alpha = *p.w_ts;
+    if (p.x_ts) alpha *= *p.x_ts;
+    const uint32_t n_x = min(p.tile_x, p.x_rows - x0), col = w0 + tid;
+    T* y = static_cast<T*>(p.y) + (int64_t)x0 * p.ldy + col;
+    float* part = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
+    if (ok) {
+      for (uint32_t j0 = 0; j0 < n_x; j0 += 16) {
+        uint32_t v[16];
+        tmem_ld16(tmem + (warp << 21) + j0, v);
+        tmem_ld_wait<16>(v);
+        if (p.split == 1) {
+          if (col < p.w_rows) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (j0 + j < n_x) y[(int64_t)(j0 + j) * p.ldy] = narrow<T>(__uint_as_float(v[j]) * alpha);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) part[(j0 + j) * kTileW + tid] = __uint_as_float(v[j]);
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  if (p.split > 1) {
+    cluster_sync();
+    // every block adds up the tokens that are its share
+    if (tid < kTileW && !*abandoned) {
+      float alpha = 1.0f;
+      if (p.w_ts) alpha = *p.w_ts;
+      if (p.x_ts) alpha *= *p.x_ts;
+      const uint32_t n_x = min(p.tile_x, p.x_rows - x0), col = w0 + tid;
+      T* y = static_cast<T*>(p.y) + (int64_t)x0 * p.ldy + col;
+      for (uint32_t j = rank; j < n_x; j += p.split) {
+        float sum = 0.0f;
+        for (uint32_t r = 0; r < p.split; ++r) sum += cluster_load(base + (j * kTileW + tid) * 4, r);
+        if (col < p.w_rows) y[(int64_t)j * p.ldy] = narrow<T>(sum * alpha);
+      }
+    }
+    cluster_sync();
+  }
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+}
+
+template <typename T, int FMT>
+cudaError_t product(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
+  constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;
+  ProductParams p = {};
+  p.w_scales = w.scales, p.x_scales = x.scales, p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale;
+  p.y = y, p.ldy = ldy, p.status = status;
+  p.w_rows = (uint32_t)w.rows, p.x_rows = (uint32_t)x.rows, p.x_strips = (uint32_t)((x.rows + kStrip - 1) / kStrip);
+  p.strip_bytes = strip_tiles(w.cols, block_of(FMT)) * kTileBytes;
+  p.steps = (uint32_t)((w.cols + kSpan - 1) / kSpan);
+  p.tile_x = 16;
+  while (p.tile_x < 256 && p.tile_x < p.x_rows) p.tile_x *= 2;
+  p.x_tiles = (p.x_rows + p.tile_x - 1) / p.tile_x;
+  const uint32_t strips = (p.tile_x + kStrip - 1) / kStrip, sf_cols = KT * 4 * (1 + strips);
+  p.stage_bytes = (kTileW + p.tile_x) * kRowBytes + KT * kTileBytes * (1 + strips);
+  p.stage_bytes = (p.stage_bytes + 1023u) & ~1023u;
+  const bool two = p.tile_x <= 64;  // two blocks per SM
+  const uint32_t room = two ? 110 * 1024 : 224 * 1024;
+  p.stages = room / p.stage_bytes;
+  if (p.stages > (uint32_t)kMaxStages) p.stages = kMaxStages;
+  const uint32_t d_cols = p.tile_x < 32 ? 32 : p.tile_x;
+  while (p.stages > 1 && d_cols + p.stages * sf_cols > (two ? 256u : 512u)) --p.stages;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < d_cols + p.stages * sf_cols) p.tmem_cols *= 2;
+  const uint64_t tiles = (uint64_t)((w.rows + kTileW - 1) / kTileW) * p.x_tiles;
+  p.split = 1;
+  while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sm_count * (two ? 2 : 1) && p.split * 2 <= p.steps) p.split *= 2;
+  if (tiles * p.split > 0x7fffffffull) return cudaErrorInvalidConfiguration;
+  const m1::WaitTestHook hook = m1::wait_test_hook();
+  p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
+  CUtensorMap w_map, x_map;
+  cudaError_t e = make_map(&w_map, w.codes, 1, (uint64_t)w.rows, (uint64_t)(w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
+  if (e == cudaSuccess) e = make_map(&x_map, x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, p.tile_x);
+  if (e == cudaSuccess) e = allow_smem<mx_product_kernel<T, FMT>>();
+  if (e != cudaSuccess) return e;
+  size_t smem = (size_t)p.stages * p.stage_bytes;
+  if (p.split > 1 && smem < (size_t)p.tile_x * kTileW * 4) smem = (size_t)p.tile_x * kTileW * 4;
+  return launch_clusters(mx_product_kernel<T, FMT>, (unsigned)(tiles * p.split), p.split, kPThreads, smem + 1024, stream, w_map,
+                         x_map, p);
+}
+
+template <typename T>
+cudaError_t product(const pvt_mx& x, const pvt_mx& w, void* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
+  return w.format == PVT_MX_E8M0_32 ? product<T, PVT_MX_E8M0_32>(x, w, static_cast<T*>(y), ldy, status, sm_count, stream)
+                                    : product<T, PVT_MX_E4M3_16>(x, w, static_cast<T*>(y), ldy, status, sm_count, stream);
+}
+
+}  // namespace
+
+namespace mma {
+cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows, uint64_t cols, uint64_t pitch,
+                     uint32_t box_rows) {
+  static std::atomic<void*> known{nullptr};
+  void* f = known.load(std::memory_order_relaxed);
+  if (!f) {
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    if (e != cudaSuccess) return e;
+    if (found != cudaDriverEntryPointSuccess || !f) return cudaErrorSymbolNotFound;
+    known.store(f, std::memory_order_relaxed);
+  }
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {pitch};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / size), box_rows}, steps[2] = {1, 1};
+  const CUresult r = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(f)(
+      map, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
+      box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+}  // namespace mma
+
+cudaError_t launch_mx_product(const pvt_mx& x, const pvt_mx& w, void* y, int32_t dtype, int64_t ldy, uint32_t* status,
+                              int sm_count, cudaStream_t stream) {
+  timing_begin(kKernMx, stream);
+  const cudaError_t e = dtype == PVT_F32   ? product<float>(x, w, y, ldy, status, sm_count, stream)
+                        : dtype == PVT_F16 ? product<__half>(x, w, y, ldy, status, sm_count, stream)
+                                           : product<__nv_bfloat16>(x, w, y, ldy, status, sm_count, stream);
+  timing_end(kKernMx, stream);
+  count_launches(1);
+  return e;
+}
+
+}  // namespace pvt

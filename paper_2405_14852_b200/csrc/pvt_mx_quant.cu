@@ -1,0 +1,284 @@
+// Quantisation to 4-bit block floating point and back.
+//
+// One pass over the matrix: a warp takes 256 columns of a row, eight to a lane, so that the lane's elements are one 16- or
+// 32-byte load, its codes one 4-byte store, and a block's largest magnitude is an exchange between two (e4m3, 16
+// elements) or four (e8m0, 32) lanes.  The scale bytes of four blocks leave as one word into their tile.  Bound by HBM: what
+// is computed per element is one product and half a conversion instruction.
+//
+// Elements.  Under e8m0 the scale is a power of two, so x / scale is exact and the conversion rounds once.  Under e4m3 the
+// quotient x / (scale tensor_scale) is rounded before it is converted, which could carry it over a border between two
+// elements; it is therefore converted twice, a little larger and a little smaller than computed (2^-20; its error is below
+// 2^-22), and only where the two disagree are the borders themselves compared, in binary64, where their products with scale
+// and tensor_scale are exact (2 + 4 + 24 significant bits).  The scale's own rounding is settled the same way.
+#include "pvt_mx.cuh"
+
+namespace pvt {
+namespace {
+
+using namespace mx;
+
+constexpr int kQThreads = 256;
+constexpr int kQUnroll = 4;  // spans in flight per warp
+
+// two conversions of eight values each side by side: code of v[0] in the lowest four bits
+__device__ __forceinline__ uint32_t e2m1_codes(const float* v) {
+  uint32_t d;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(d)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return d;
+}
+
+// the element nearest to |x| / d, by its borders: n from (n - 1/2) on, in the order of codes
+__device__ __noinline__ uint32_t e2m1_exact(float x, double d) {
+  const double a = fabs((double)x);
+  uint32_t n = 0;
+  n += a > 0.25 * d;
+  n += a >= 0.75 * d;
+  n += a > 1.25 * d;
+  n += a >= 1.75 * d;
+  n += a > 2.5 * d;
+  n += a >= 3.5 * d;
+  n += a > 5.0 * d;
+  return n | (__float_as_uint(x) >> 31 << 3);
+}
+
+// the e4m3 number nearest to amax / six_ts (at most 448), ties to the even one
+__device__ __forceinline__ uint32_t e4m3_scale(float amax, double six_ts, double inv) {
+  const float q = (float)((double)amax * inv);
+  uint16_t two;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(q));
+  uint32_t c = two & 127u;
+  // q may have been rounded over a midpoint: compare with the midpoints themselves, exact in binary64
+  const double v = e4m3_value(c), a = amax;
+  if (c < 126) {
+    const double mid = 0.5 * (v + (double)e4m3_value(c + 1)) * six_ts;
+    if (a > mid || (a == mid && (c & 1))) return c + 1;
+  }
+  if (c > 0) {
+    const double mid = 0.5 * (v + (double)e4m3_value(c - 1)) * six_ts;
+    if (a < mid || (a == mid && (c & 1))) return c - 1;
+  }
+  return c;
+}
+
+template <typename T, int FMT, bool WIDE>
+__global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ld, uint8_t* scales,
+                                                                const float* tensor_scale, uint32_t rows, uint32_t cols,
+                                                                uint32_t tiles, FastDiv spans_div, uint32_t spans,
+                                                                uint64_t total) {
+  constexpr int LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;  // of a block
+  pdl_trigger();
+  pdl_wait();
+  const uint32_t lane = threadIdx.x & 31;
+  float ts = 1.0f;
+  bool bad_ts = false;
+  double six_ts = 6.0, inv_six = 1.0 / 6.0;
+  if (FMT == PVT_MX_E4M3_16 && tensor_scale) {
+    ts = *tensor_scale;
+    bad_ts = !(ts > 0.0f && ts < __uint_as_float(0x7f800000u));
+    six_ts = 6.0 * (double)ts;
+    inv_six = 1.0 / six_ts;
+  }
+  const uint64_t warps = (uint64_t)gridDim.x * (kQThreads / 32);
+  for (uint64_t at = ((uint64_t)blockIdx.x * (kQThreads / 32) + threadIdx.x / 32) * kQUnroll; at < total; at += warps * kQUnroll) {
+    float v[kQUnroll][8];
+    uint32_t row[kQUnroll], c0[kQUnroll];
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+      const uint64_t n = at + u;
+      // (a strip's rows that do not exist are spans too: their scales are written)
+      row[u] = n < total ? fast_div((uint32_t)n, spans_div) : 0xffffffffu;
+      c0[u] = ((uint32_t)n - row[u] * spans) * kSpan + 8 * lane;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
+      if (row[u] >= rows) continue;
+      const T* from = x + (int64_t)row[u] * ldx + c0[u];
+      if (WIDE && c0[u] + 8 <= cols) {
+        const Eight<T> e = *reinterpret_cast<const Eight<T>*>(from);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = widen<T>(e.v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (c0[u] + i < cols) v[u][i] = widen<T>(from[i]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+      if (row[u] == 0xffffffffu) break;
+      uint32_t top = 0;  // bits of the largest magnitude: NaN and infinity above every number
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
+#pragma unroll
+      for (int s = 1; s < LANES; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+      const bool bad = top >= 0x7f800000u || bad_ts;
+      uint32_t byte, word = 0;
+      if (FMT == PVT_MX_E8M0_32) {
+        // floor(log2 a) - 2, biased; numbers below 2^-126 have a scale of 2^-127 in any case
+        const int e = max((int)(top >> 23) - 2, 0);
+        byte = bad ? 255u : (uint32_t)e;
+        const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] *= inv;
+        if (!bad) word = e2m1_codes(v[u]);
+      } else {
+        byte = bad ? 127u : e4m3_scale(__uint_as_float(top), six_ts, inv_six);
+        if (!bad && byte) {
+          const float s = e4m3_value(byte), d = s * ts, r = 1.0f / d;
+          float hi[8], lo[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float y = v[u][i] * r;
+            hi[i] = y * 1.00000095367431640625f;  // 1 + 2^-20
+            lo[i] = y * 0.99999904632568359375f;
+          }
+          word = e2m1_codes(hi);
+          uint32_t differ = word ^ e2m1_codes(lo);
+          // where d or r leave the range of normal numbers every element is compared with its borders
+          if (!(d >= 1e-30f && d <= 1e30f)) differ = 0xffffffffu;
+          if (differ) {
+            const double dd = (double)s * (double)ts;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (differ >> (4 * i) & 15u) word = (word & ~(15u << (4 * i))) | e2m1_exact(v[u][i], dd) << (4 * i);
+          }
+        }
+      }
+      if (row[u] >= rows || c0[u] >= cols) byte = 0;  // no such block, whatever the tensor scale is
+      uint32_t four = byte | __shfl_down_sync(0xffffffffu, byte, LANES) << 8;
+      four |= __shfl_down_sync(0xffffffffu, four, 2 * LANES) << 16;
+      if (lane % (4 * LANES) == 0) {
+        const uint32_t block = c0[u] / (8 * LANES);
+        *reinterpret_cast<uint32_t*>(scales + scale_at(row[u], block, tiles)) = four;
+      }
+      if (row[u] < rows && c0[u] < cols) {
+        uint8_t* to = codes + (int64_t)row[u] * ld + c0[u] / 2;
+        if (c0[u] + 8 <= cols) {
+          *reinterpret_cast<uint32_t*>(to) = word;
+        } else {
+          for (uint32_t i = 0; 2 * i < cols - c0[u]; ++i) to[i] = (uint8_t)(word >> (8 * i));
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int FMT, bool WIDE>
+__global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* codes, int64_t ld, const uint8_t* scales,
+                                                               const float* tensor_scale, T* values, int64_t ldv, uint32_t rows,
+                                                               uint32_t cols, uint32_t tiles, FastDiv spans_div,
+                                                               uint32_t spans, uint64_t total) {
+  constexpr int LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;
+  pdl_trigger();
+  pdl_wait();
+  const uint32_t lane = threadIdx.x & 31;
+  const float ts = FMT == PVT_MX_E4M3_16 && tensor_scale ? *tensor_scale : 1.0f;
+  const uint64_t warps = (uint64_t)gridDim.x * (kQThreads / 32);
+  for (uint64_t at = ((uint64_t)blockIdx.x * (kQThreads / 32) + threadIdx.x / 32) * kQUnroll; at < total; at += warps * kQUnroll) {
+    uint32_t word[kQUnroll], byte[kQUnroll], row[kQUnroll], c0[kQUnroll];
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+      const uint64_t n = at + u;
+      row[u] = fast_div((uint32_t)n, spans_div);
+      c0[u] = ((uint32_t)n - row[u] * spans) * kSpan + 8 * lane;
+      if (n >= total) c0[u] = cols;
+      if (c0[u] >= cols) continue;
+      // (the four bytes lie in the row: ld is a multiple of 16)
+      word[u] = *reinterpret_cast<const uint32_t*>(codes + (int64_t)row[u] * ld + c0[u] / 2);
+      byte[u] = scales[scale_at(row[u], c0[u] / (8 * LANES), tiles)];
+    }
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+      if (c0[u] >= cols) continue;
+      const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(byte[u]) : e4m3_value(byte[u]);
+      Eight<T> e;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // the three bits of the magnitude as the low exponent bits and the first fraction bit of a binary32, whose bias
+        // is 126 more: a product with 2^126 gives the element, 0.5 from a number without its leading one included
+        const uint32_t c = word[u] >> (4 * i);
+        const float el = __uint_as_float((c & 7u) << 22 | (c & 8u) << 28) * 8.507059173023462e37f;
+        e.v[i] = narrow<T>(el * s * ts);
+      }
+      T* to = values + (int64_t)row[u] * ldv + c0[u];
+      if (WIDE && c0[u] + 8 <= cols) {
+        *reinterpret_cast<Eight<T>*>(to) = e;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (c0[u] + i < cols) to[i] = e.v[i];
+      }
+    }
+  }
+}
+
+bool rows_aligned(const void* p, int64_t ld, size_t size) {
+  return reinterpret_cast<uintptr_t>(p) % (8 * size) == 0 && ld % 8 == 0;
+}
+
+unsigned span_grid(uint64_t total, int sm_count) {
+  const uint64_t need = (total + kQThreads / 32 * kQUnroll - 1) / (kQThreads / 32 * kQUnroll);
+  const uint64_t most = (uint64_t)sm_count * 8;
+  return (unsigned)(need < most ? need : most);
+}
+
+template <typename T, int FMT>
+cudaError_t quantize(const pvt_mx& m, const T* x, int64_t ldx, int sm_count, cudaStream_t stream) {
+  const uint32_t spans = (uint32_t)((m.cols + kSpan - 1) / kSpan);
+  const uint64_t total = (uint64_t)((m.rows + kStrip - 1) / kStrip) * kStrip * spans;
+  auto kernel = rows_aligned(x, ldx, sizeof(T)) ? mx_quantize_kernel<T, FMT, true> : mx_quantize_kernel<T, FMT, false>;
+  return launch_dependent(kernel, span_grid(total, sm_count), kQThreads, 0, stream, x, ldx, m.codes, m.ld, m.scales, m.tensor_scale,
+                          (uint32_t)m.rows, (uint32_t)m.cols, strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans,
+                          total);
+}
+
+template <typename T, int FMT>
+cudaError_t dequant(const pvt_mx& m, T* values, int64_t ldv, int sm_count, cudaStream_t stream) {
+  const uint32_t spans = (uint32_t)((m.cols + kSpan - 1) / kSpan);
+  const uint64_t total = (uint64_t)m.rows * spans;
+  auto kernel = rows_aligned(values, ldv, sizeof(T)) ? mx_dequant_kernel<T, FMT, true> : mx_dequant_kernel<T, FMT, false>;
+  return launch_dependent(kernel, span_grid(total, sm_count), kQThreads, 0, stream, (const uint8_t*)m.codes, m.ld,
+                          (const uint8_t*)m.scales, m.tensor_scale, values, ldv, (uint32_t)m.rows, (uint32_t)m.cols,
+                          strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans, total);
+}
+
+template <typename T>
+cudaError_t quantize(const pvt_mx& m, const void* x, int64_t ldx, int sm_count, cudaStream_t stream) {
+  return m.format == PVT_MX_E8M0_32 ? quantize<T, PVT_MX_E8M0_32>(m, static_cast<const T*>(x), ldx, sm_count, stream)
+                                    : quantize<T, PVT_MX_E4M3_16>(m, static_cast<const T*>(x), ldx, sm_count, stream);
+}
+template <typename T>
+cudaError_t dequant(const pvt_mx& m, void* values, int64_t ldv, int sm_count, cudaStream_t stream) {
+  return m.format == PVT_MX_E8M0_32 ? dequant<T, PVT_MX_E8M0_32>(m, static_cast<T*>(values), ldv, sm_count, stream)
+                                    : dequant<T, PVT_MX_E4M3_16>(m, static_cast<T*>(values), ldv, sm_count, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_mx_quantize(const pvt_mx& m, const void* x, int32_t dtype, int64_t ldx, int sm_count, cudaStream_t stream) {
+  timing_begin(kKernMx, stream);
+  const cudaError_t e = dtype == PVT_F32   ? quantize<float>(m, x, ldx, sm_count, stream)
+                        : dtype == PVT_F16 ? quantize<__half>(m, x, ldx, sm_count, stream)
+                                           : quantize<__nv_bfloat16>(m, x, ldx, sm_count, stream);
+  timing_end(kKernMx, stream);
+  count_launches(1);
+  return e;
+}
+
+cudaError_t launch_mx_dequant(const pvt_mx& m, void* values, int32_t dtype, int64_t ldv, int sm_count, cudaStream_t stream) {
+  timing_begin(kKernMx, stream);
+  const cudaError_t e = dtype == PVT_F32   ? dequant<float>(m, values, ldv, sm_count, stream)
+                        : dtype == PVT_F16 ? dequant<__half>(m, values, ldv, sm_count, stream)
+                                           : dequant<__nv_bfloat16>(m, values, ldv, sm_count, stream);
+  timing_end(kKernMx, stream);
+  count_launches(1);
+  return e;
+}
+
+}  // namespace pvt
