@@ -15,6 +15,8 @@ namespace {
 using namespace distill;
 using namespace mma;
 
+constexpr int kUnroll = 4;  // pieces in flight per thread
+
 enum { kLoss = 1, kGrad = 2, kBoth = 3 };
 
 struct DistillParams {
@@ -69,10 +71,11 @@ __device__ __forceinline__ void clear(G* grad, uint32_t from, uint32_t to) {
 }
 
 template <typename T, typename G, int MODE>
-__global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillParams p) {
+__global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const DistillParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
   DistillShared& sm = *reinterpret_cast<DistillShared*>(raw);
-  uint32_t* const listed = reinterpret_cast<uint32_t*>(raw + sizeof(DistillShared));  // a bit per entry of the vocabulary
+  // a bit per entry of the vocabulary, moved so that a piece's bits lie in one word: piece i has those from (i + 1) N on
+  uint32_t* const listed = reinterpret_cast<uint32_t*>(raw + sizeof(DistillShared));
   pdl_trigger();
   pdl_wait();
   constexpr uint32_t N = Piece<T>::N;
@@ -80,6 +83,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillParam
   const T* row = static_cast<const T*>(p.logits) + (int64_t)r * p.ld;
   G* const grad = MODE & kGrad ? static_cast<G*>(p.grad) + (int64_t)r * p.ldg : nullptr;
   const RowShare<T> s(row, p.vocab, rank, p.blocks);
+  const Piece<T>* const pieces = reinterpret_cast<const Piece<T>*>(row + s.head);
   const float weight = p.weight ? p.weight[r] : 1.0f;
   const bool tail = p.teacher_lse != nullptr;
   float* const stats = p.stats ? p.stats + (int64_t)r * PVT_DISTILL_STATS : nullptr;
@@ -90,21 +94,24 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillParam
 
   // the list: entries outside the vocabulary or named before are left out
   if (active) {
-    for (uint32_t i = tid; i < (p.vocab + 31) / 32; i += kThreads) listed[i] = 0;
+    for (uint32_t i = tid; i < (p.vocab + N + 31) / 32; i += kThreads) listed[i] = 0;
     if (tid == 0) sm.repeated = 0;
     __syncthreads();
     bool bad = false;
     for (uint32_t i = tid; i < k; i += kThreads) {
       int32_t at = p.top_idx[(int64_t)r * k + i];
       if (at >= (int32_t)p.vocab) bad = true, at = -1;
-      if (at >= 0 && (atomicOr(&listed[at / 32], 1u << (at % 32)) >> (at % 32) & 1u)) sm.repeated = 1;
+      if (at >= 0) {
+        const uint32_t bit = (uint32_t)at + N - s.head;
+        if (atomicOr(&listed[bit / 32], 1u << (bit % 32)) >> (bit % 32) & 1u) sm.repeated = 1;
+      }
       sm.idx[i] = at < 0 ? -1 : at;
       sm.val[i] = p.top_logit[(int64_t)r * k + i];
       sm.x[i] = at >= 0 ? widen<T>(row[at]) : 0.0f;  // before any block writes the gradient over the logits
     }
     __syncthreads();
     if (sm.repeated) {
-      uint32_t again = 0;  // of this thread's entries (two at most)
+      uint32_t again = 0;  // of this thread's entries
       for (uint32_t i = tid, n = 0; i < k; i += kThreads, ++n)
         for (uint32_t j = 0; j < i; ++j)
           if (sm.idx[i] >= 0 && sm.idx[j] == sm.idx[i]) again |= 1u << n;
@@ -142,41 +149,46 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillParam
 
     Running run;
     if (active) {
-      auto add = [&](const float* x, uint32_t n, uint32_t at) {
-        float m = x[0];
-        for (uint32_t e = 1; e < n; ++e) m = fmaxf(m, x[e]);
-        run.raise(m, p.c);
-        for (uint32_t e = 0; e < n; ++e) {
-          const float y = run.term(x[e], p.c);
-          run.z += y;
-          if (tail && !(listed[(at + e) / 32] >> ((at + e) % 32) & 1u)) run.r += y;
-        }
-      };
-      for (uint32_t i = s.lo + tid; i < s.hi; i += kThreads) {
-        const Piece<T> piece = *reinterpret_cast<const Piece<T>*>(row + s.head + i * N);
-        float x[N];
+      for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kUnroll * kThreads) {
+        Piece<T> piece[kUnroll];
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) x[e] = widen<T>(piece.v[e]);
-        add(x, N, s.head + i * N);
+        for (int u = 0; u < kUnroll; ++u)
+          if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
+        float top = kMinusInf;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (i0 + u * kThreads < s.hi) top = fmaxf(top, largest(piece[u]));
+        run.raise(top, p.c);
+        const float base = run.base();
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (i0 + u * kThreads < s.hi) {
+            const float sum = terms(piece[u], base, p.c);
+            run.z += sum;
+            if (tail) {
+              const uint32_t i = i0 + u * kThreads, bit = (i + 1) * N, mask = listed[bit / 32] >> (bit % 32) & ((1u << N) - 1);
+              if (mask == 0)
+                run.r += sum;
+              else
+                for (uint32_t e = 0; e < N; ++e)
+                  if (!(mask >> e & 1u)) run.r += ex2((widen<T>(row[s.head + i * N + e]) - base) * p.c);
+            }
+          }
       }
       if (tid < s.loose()) {
-        const float x = widen<T>(row[s.loose_at(tid)]);
-        add(&x, 1, s.loose_at(tid));
+        const uint32_t at = s.loose_at(tid), bit = at + N - s.head;
+        const float x = widen<T>(row[at]);
+        run.raise(x, p.c);
+        const float y = ex2((x - run.base()) * p.c);
+        run.z += y;
+        if (tail && !(listed[bit / 32] >> (bit % 32) & 1u)) run.r += y;
       }
       run = block_merge(run, p.c, sm.run);
     }
     if (p.blocks > 1) {
       if (tid == 0) sm.mine = run;
       cluster_sync();
-      Running all;
-      for (uint32_t q = 0; q < p.blocks; ++q) {
-        Running other;
-        other.m = cluster_load(smem_u32(&sm.mine.m), q);
-        other.z = cluster_load(smem_u32(&sm.mine.z), q);
-        other.r = cluster_load(smem_u32(&sm.mine.r), q);
-        all = merge(all, other, p.c);
-      }
-      run = all;
+      run = cluster_merge(&sm.mine, p.blocks, p.c);
       cluster_sync();
     }
     // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
@@ -227,12 +239,24 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillParam
     const float m = sm.stat[kStatMax], f_listed = sm.stat[kStatListed], f_rest = sm.stat[kStatRest] * up;
     auto y_of = [&](float x) { return ex2((x - m) * p.c); };
     if (sizeof(G) == sizeof(T) && (reinterpret_cast<uintptr_t>(grad) - reinterpret_cast<uintptr_t>(row)) % 16 == 0) {
-      for (uint32_t i = s.lo + tid; i < s.hi; i += kThreads) {
-        const Piece<T> piece = *reinterpret_cast<const Piece<T>*>(row + s.head + i * N);
-        Piece<G> out;
+      const Two base = two(-m, -m), cc = two(p.c, p.c), ff = two(f_rest, f_rest);
+      for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kUnroll * kThreads) {
+        Piece<T> piece[kUnroll];
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) out.v[e % Piece<G>::N] = narrow<G>(y_of(widen<T>(piece.v[e])) * f_rest);
-        *reinterpret_cast<Piece<G>*>(grad + s.head + i * N) = out;
+        for (int u = 0; u < kUnroll; ++u)
+          if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          if (i0 + u * kThreads >= s.hi) continue;
+          Piece<G> out;
+#pragma unroll
+          for (uint32_t e = 0; e < N / 2; ++e) {
+            const float2 y = each(mul2(add2(pair_of(piece[u], e), base), cc));
+            const float2 g = each(mul2(two(ex2(y.x), ex2(y.y)), ff));
+            out.v[2 * e % Piece<G>::N] = narrow<G>(g.x), out.v[(2 * e + 1) % Piece<G>::N] = narrow<G>(g.y);
+          }
+          reinterpret_cast<Piece<G>*>(grad + s.head)[i0 + u * kThreads] = out;
+        }
       }
       if (tid < s.loose()) {
         const uint32_t at = s.loose_at(tid);
@@ -242,12 +266,12 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillParam
       // rows of unlike alignment: element by element, a warp along the row
       const uint32_t to = s.to();
       uint32_t at = s.from() + tid;
-      for (; at + 3 * kThreads < to; at += 4 * kThreads) {
-        float x[4];
+      for (; at + 7 * kThreads < to; at += 8 * kThreads) {
+        float x[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = widen<T>(row[at + u * kThreads]);
+        for (int u = 0; u < 8; ++u) x[u] = widen<T>(row[at + u * kThreads]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) grad[at + u * kThreads] = narrow<G>(y_of(x[u]) * f_rest);
+        for (int u = 0; u < 8; ++u) grad[at + u * kThreads] = narrow<G>(y_of(x[u]) * f_rest);
       }
       for (; at < to; at += kThreads) grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
     }
@@ -266,7 +290,7 @@ template <typename T, typename G, int MODE>
 cudaError_t start(const DistillParams& p, int64_t rows, cudaStream_t stream) {
   const cudaError_t e = allow_smem<distill_kernel<T, G, MODE>>();
   if (e != cudaSuccess) return e;
-  const size_t smem = sizeof(DistillShared) + (size_t)(p.vocab + 31) / 32 * 4;
+  const size_t smem = sizeof(DistillShared) + (size_t)(p.vocab + Piece<T>::N + 31) / 32 * 4;
   return launch_clusters(distill_kernel<T, G, MODE>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
 }
 template <typename T, int MODE>

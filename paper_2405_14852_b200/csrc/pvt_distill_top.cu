@@ -1,12 +1,13 @@
 // The k largest logits of each row, in order, and the logarithm of the sum of all exponentials.
 //
-// One pass over the row keeps, besides the running sum, the largest value of each of 2048 parts of it (four per thread).  The
-// k-th largest of those maxima has at least k elements not below it, so everything that is listed is among the elements that
-// reach it; with parts in no relation to the values those are few more (n with 2048 ln(2048 / (2048 - k)) ~ n: 65 for k =
-// 64, 1420 for k = 1024).  A second pass over the row, which comes from the L2, collects them, and they are put in order
-// in shared memory.  A row in which too many elements are equal (or that is laid out against this) is settled by counting the digits
-// of its keys instead.  A few long rows are shared by clusters: each block lists its part, and an entry's place is its own plus
-// those that the other blocks' lists hold ahead of it.
+// One pass over the row keeps, besides the running sum, the largest value of each of 2048 parts of it (eight per thread).  If every
+// warp takes the j-th largest of the maxima of its 256 parts, j = ceil(k / warps), at least k elements are not below the smallest
+// of these, so everything that is listed is among the elements that reach that bound; with parts in no relation to the values
+// those are few more.  A second pass over the row, which comes from the L2, collects them (a piece of 16 bytes is
+// dismissed by its largest element), and they are put in order in shared memory.  A row in which too many elements reach the bound
+// (equal ones, or a list nearly as long as the parts are many) is settled by counting the digits of its keys instead.  A few long
+// rows are shared by clusters: each block lists its part, and an entry's place is its own plus those that the other
+// blocks' lists hold ahead of it.
 #include "pvt_distill.cuh"
 
 namespace pvt {
@@ -15,7 +16,8 @@ namespace {
 using namespace distill;
 using namespace mma;
 
-constexpr int kParts = 4;           // of each thread
+constexpr int kParts = 8;           // of each thread
+constexpr int kWarps = kThreads / 32;
 constexpr int kCandidates = 2048;   // that are put in order at once
 constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
 
@@ -41,12 +43,12 @@ struct TopParams {
 };
 
 struct TopShared {
-  Running run[kThreads / 32];
+  Running run[kWarps];
   Running mine;
-  uint32_t parts[kThreads * kParts];
+  uint32_t bound[kWarps];
   uint32_t hist[256];
   uint32_t digit, above, count, n;
-  uint64_t entries[kCandidates];
+  alignas(8) uint64_t entries[kCandidates];
   uint64_t sorted[PVT_DISTILL_MAX_K];
 };
 
@@ -92,15 +94,21 @@ __device__ __forceinline__ void for_each(const T* row, const RowShare<T>& s, F f
 
 // n entries (at most kCandidates) in order; the first min(n, k) to sm.sorted
 __device__ __forceinline__ void put_in_order(TopShared& sm, uint32_t n, uint32_t k) {
-  if (n <= kThreads) {
-    if (threadIdx.x < n) {
-      const uint64_t own = sm.entries[threadIdx.x];
+  if (n <= 2 * kThreads) {
+    // an entry's place is the number of those ahead of it, counted by as many threads as there are for each
+    uint32_t each = 1;
+    while (each < 32 && 2 * each * n <= kThreads) each *= 2;
+    for (uint32_t at = threadIdx.x / each; at - threadIdx.x / each < n; at += kThreads / each) {
+      const bool real = at < n;
+      const uint64_t own = real ? sm.entries[at] : 0;
       uint32_t place = 0;
-      for (uint32_t i = 0; i < n; ++i) place += sm.entries[i] < own;
-      if (place < k) sm.sorted[place] = own;
+#pragma unroll 8
+      for (uint32_t i = threadIdx.x % each; i < n; i += each) place += sm.entries[i] < own;
+      for (uint32_t s = 1; s < each; s *= 2) place += __shfl_xor_sync(0xffffffffu, place, s);
+      if (real && threadIdx.x % each == 0 && place < k) sm.sorted[place] = own;
     }
   } else {
-    uint32_t size = 2 * kThreads;
+    uint32_t size = 4 * kThreads;
     while (size < n) size *= 2;
     for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sm.entries[i] = ~0ull;
     __syncthreads();
@@ -136,7 +144,7 @@ __device__ __noinline__ uint32_t by_digits(TopShared& sm, const T* row, const Ro
     want -= sm.above;
     __syncthreads();
   }
-  // `want` of those equal to prefix (more than kCandidates elements reach the bound, so k exist above -infinity)
+  // `want` of those equal to prefix (more than PVT_DISTILL_MAX_K elements reach the bound, so k exist above -infinity)
   if (threadIdx.x == 0) sm.count = 0;
   __syncthreads();
   for_each(row, s, [&](uint32_t key, uint32_t at) {
@@ -165,8 +173,25 @@ __device__ __noinline__ uint32_t by_digits(TopShared& sm, const T* row, const Ro
   return k;
 }
 
+// the upper half of the j-th largest of the warp's keys (kParts in each lane), with zeros below
+__device__ __forceinline__ uint32_t warp_bound(const uint32_t* key, uint32_t j) {
+  uint32_t lo = 0, hi = 0x10000;  // at least j keys reach lo, fewer reach hi
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    uint32_t n = 0;
+#pragma unroll
+    for (int u = 0; u < kParts; ++u) n += key[u] >> 16 >= mid;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (n >= j)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo << 16;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) distill_top_kernel(const TopParams p) {
+__global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const TopParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
   TopShared& sm = *reinterpret_cast<TopShared*>(raw);
   pdl_trigger();
@@ -175,70 +200,85 @@ __global__ void __launch_bounds__(kThreads, 2) distill_top_kernel(const TopParam
   const uint32_t tid = threadIdx.x, rank = blockIdx.x % p.blocks, r = blockIdx.x / p.blocks, k = p.k;
   const T* row = static_cast<const T*>(p.logits) + (int64_t)r * p.ld;
   const RowShare<T> s(row, p.vocab, rank, p.blocks);
+  const Piece<T>* const pieces = reinterpret_cast<const Piece<T>*>(row + s.head);
 
   Running run;
-  uint32_t part[kParts] = {};
-  auto add = [&](uint32_t& top, const float* x, int n) {
-    float m = x[0];
-    for (int e = 1; e < n; ++e) m = fmaxf(m, x[e]);
-    run.raise(m, p.c);
-    uint32_t key = key_of(m);
-    for (int e = 0; e < n; ++e) {
-      run.z += run.term(x[e], p.c);
-      if (x[e] != x[e]) key = 0xffffffffu;
-    }
-    top = max(top, key);
-  };
+  float part[kParts];
+#pragma unroll
+  for (int u = 0; u < kParts; ++u) part[u] = kMinusInf;
   for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kParts * kThreads) {
     Piece<T> piece[kParts];
 #pragma unroll
     for (int u = 0; u < kParts; ++u)
-      if (i0 + u * kThreads < s.hi) piece[u] = *reinterpret_cast<const Piece<T>*>(row + s.head + (i0 + u * kThreads) * N);
+      if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
+    float top = kMinusInf;
 #pragma unroll
     for (int u = 0; u < kParts; ++u)
       if (i0 + u * kThreads < s.hi) {
-        float x[N];
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) x[e] = widen<T>(piece[u].v[e]);
-        add(part[u], x, N);
+        const float m = largest(piece[u]);
+        part[u] = max_nan(part[u], m);
+        top = fmaxf(top, m);
       }
+    run.raise(top, p.c);
+    const float base = run.base();
+#pragma unroll
+    for (int u = 0; u < kParts; ++u)
+      if (i0 + u * kThreads < s.hi) run.z += terms(piece[u], base, p.c);
   }
   if (tid < s.loose()) {
     const float x = widen<T>(row[s.loose_at(tid)]);
-    add(part[0], &x, 1);
+    part[0] = max_nan(part[0], x);
+    run.raise(x, p.c);
+    run.z += ex2((x - run.base()) * p.c);
   }
+  {
+    uint32_t key[kParts];
 #pragma unroll
-  for (int u = 0; u < kParts; ++u) sm.parts[tid + u * kThreads] = part[u];
-  if (tid == 0) sm.count = 0;
+    for (int u = 0; u < kParts; ++u) key[u] = key_of(part[u]);
+    const uint32_t bound = warp_bound(key, (k + kWarps - 1) / kWarps);
+    if (tid % 32 == 0) sm.bound[tid / 32] = bound;
+  }
+  if (tid == 0) sm.count = sm.digit = 0;
   run = block_merge(run, p.c, sm.run);
   if (tid == 0) sm.mine = run;
-
-  // the k-th largest of the parts' maxima, its upper half: what is below reaches no place of the list
-  uint32_t bound = 0, want = k;
-#pragma unroll
-  for (int shift = 24; shift >= 16; shift -= 8) {
-    if (tid < 256) sm.hist[tid] = 0;
-    __syncthreads();
+  // what is below reaches no place of the list; -infinity never does
+  const uint32_t bound = max(__reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]), kLowest + 1);
+  const float least = value_of(bound);
+  uint32_t* const reached = reinterpret_cast<uint32_t*>(sm.sorted);  // pieces whose largest element reaches it
+  constexpr uint32_t kPieces = sizeof(sm.sorted) / 4;
+  for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kParts * kThreads) {
+    Piece<T> piece[kParts];
 #pragma unroll
     for (int u = 0; u < kParts; ++u)
-      if (shift == 24 || part[u] >> 24 == bound >> 24) atomicAdd(&sm.hist[part[u] >> shift & 255], 1u);
-    __syncthreads();
-    find_digit(sm, want);
-    bound |= sm.digit << shift;
-    want -= sm.above;
-    __syncthreads();
+      if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
+#pragma unroll
+    for (int u = 0; u < kParts; ++u)
+      if (i0 + u * kThreads < s.hi && !(largest(piece[u]) < least)) {
+        const uint32_t n = atomicAdd(&sm.digit, 1u);
+        if (n < kPieces) reached[n] = i0 + u * kThreads;
+      }
   }
-  bound = max(bound, kLowest + 1);
-  for_each(row, s, [&](uint32_t key, uint32_t at) {
-    if (key >= bound) {
+  __syncthreads();
+  // their elements, one to a thread
+  const uint32_t n_reached = sm.digit;
+  for (uint32_t i = tid; i < min(n_reached, kPieces) * N; i += kThreads) {
+    const uint32_t at = s.head + reached[i / N] * N + i % N;
+    const float x = widen<T>(row[at]);
+    if (x < least) continue;
+    const uint32_t n = atomicAdd(&sm.count, 1u);
+    if (n < kCandidates) sm.entries[n] = entry_of(key_of(x), at);
+  }
+  if (tid < s.loose()) {
+    const float x = widen<T>(row[s.loose_at(tid)]);
+    if (!(x < least)) {
       const uint32_t n = atomicAdd(&sm.count, 1u);
-      if (n < kCandidates) sm.entries[n] = entry_of(key, at);
+      if (n < kCandidates) sm.entries[n] = entry_of(key_of(x), s.loose_at(tid));
     }
-  });
+  }
   __syncthreads();
   const uint32_t found = sm.count;
   uint32_t n = min(found, k);
-  if (found <= kCandidates)
+  if (n_reached <= kPieces && found <= kCandidates)
     put_in_order(sm, found, k);
   else
     n = by_digits(sm, row, s, k);
@@ -255,26 +295,28 @@ __global__ void __launch_bounds__(kThreads, 2) distill_top_kernel(const TopParam
   } else {
     if (tid == 0) sm.n = n;
     cluster_sync();
-    // the other blocks' lists, one after the other, behind this block's own memory
+    run = cluster_merge(&sm.mine, p.blocks, p.c);
+    // the other blocks' lists, side by side, behind this block's own memory
     uint64_t* lists = reinterpret_cast<uint64_t*>(raw + sizeof(TopShared));
-    uint32_t size[8];
-    run = sm.mine;
-    Running sum;
-    for (uint32_t q = 0; q < p.blocks; ++q) {
-      Running other;
-      other.m = cluster_load(smem_u32(&sm.mine.m), q);
-      other.z = cluster_load(smem_u32(&sm.mine.z), q);
-      sum = merge(sum, other, p.c);
-      size[q] = __float_as_uint(cluster_load(smem_u32(&sm.n), q));
-      for (uint32_t i = tid; i < 2 * size[q]; i += kThreads)
-        reinterpret_cast<float*>(lists + q * k)[i] = cluster_load(smem_u32(sm.sorted) + 4 * i, q);
+    uint32_t size[kMaxBlocks];
+#pragma unroll
+    for (uint32_t q = 0; q < kMaxBlocks; ++q)
+      size[q] = q < p.blocks ? __float_as_uint(cluster_load(smem_u32(&sm.n), q)) : 0;
+    for (uint32_t i = tid; i < k; i += kThreads) {
+      uint64_t entry[kMaxBlocks];
+#pragma unroll
+      for (uint32_t q = 0; q < kMaxBlocks; ++q)
+        if (i < size[q]) entry[q] = cluster_load64(smem_u32(sm.sorted + i), q);
+#pragma unroll
+      for (uint32_t q = 0; q < kMaxBlocks; ++q)
+        if (i < size[q]) lists[q * k + i] = entry[q];
     }
-    run = sum;
     __syncthreads();
     for (uint32_t i = tid; i < n; i += kThreads) {
       const uint64_t own = sm.sorted[i];
       uint32_t place = i;
-      for (uint32_t q = 0; q < p.blocks; ++q) {
+#pragma unroll
+      for (uint32_t q = 0; q < kMaxBlocks; ++q) {
         if (q == rank) continue;
         uint32_t lo = 0, hi = size[q];
         while (lo < hi) {
@@ -289,7 +331,8 @@ __global__ void __launch_bounds__(kThreads, 2) distill_top_kernel(const TopParam
       if (place < k) put(place, own);
     }
     total = 0;
-    for (uint32_t q = 0; q < p.blocks; ++q) total += size[q];
+#pragma unroll
+    for (uint32_t q = 0; q < kMaxBlocks; ++q) total += size[q];
     cluster_sync();  // no block leaves while another reads its lists
   }
   if (rank == 0) {
@@ -298,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_top_kernel(const TopParam
       val[i] = kMinusInf;
     }
     if (tid == 0 && p.lse)
-      p.lse[r] = run.m * p.inv_t + logf(run.z);  // (no logit above -infinity: log 0; an infinite one, or a NaN: itself)
+      p.lse[r] = run.base() * p.inv_t + logf(run.z);
   }
 }
 

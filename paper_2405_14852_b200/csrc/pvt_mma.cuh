@@ -130,6 +130,13 @@ __device__ __forceinline__ float cluster_load(uint32_t saddr, uint32_t rank) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
+__device__ __forceinline__ uint64_t cluster_load64(uint32_t saddr, uint32_t rank) {
+  uint32_t at;
+  uint64_t v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(saddr), "r"(rank));
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
+  return v;
+}
 
 // a grid whose blocks form clusters of `cluster`, and whose start may overlap the kernel ahead (see launch_dependent)
 template <typename... KArgs, typename... Args>
