@@ -67,12 +67,31 @@ __device__ __forceinline__ uint32_t e4m3_scale(float amax, double six_ts, double
   return c;
 }
 
+// The span's elements from one of two orders to the other: eight consecutive ones in a lane, and (rows that no wide access can
+// take) element 32 i + lane in place i of a lane.  Eight numbers are padded to nine: no bank is met twice either way.
+template <bool TO_ROWS>
+__device__ __forceinline__ void turn(float* buffer, float* v, uint32_t lane) {
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t at = TO_ROWS ? 8 * lane + i : 32 * i + lane;
+    buffer[at + at / 8] = v[i];
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t at = TO_ROWS ? 32 * i + lane : 8 * lane + i;
+    v[i] = buffer[at + at / 8];
+  }
+}
+
 template <typename T, int FMT, bool WIDE>
 __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ld, uint8_t* scales,
                                                                 const float* tensor_scale, uint32_t rows, uint32_t cols,
                                                                 uint32_t tiles, FastDiv spans_div, uint32_t spans,
                                                                 uint64_t total) {
   constexpr int LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;  // of a block
+  __shared__ float buffer[WIDE ? 1 : kQThreads / 32][kSpan + 8 * kSpan / 32];
   pdl_trigger();
   pdl_wait();
   const uint32_t lane = threadIdx.x & 31;
@@ -98,20 +117,31 @@ __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int6
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
       if (row[u] >= rows) continue;
-      const T* from = x + (int64_t)row[u] * ldx + c0[u];
-      if (WIDE && c0[u] + 8 <= cols) {
-        const Eight<T> e = *reinterpret_cast<const Eight<T>*>(from);
+      const T* from = x + (int64_t)row[u] * ldx;
+      if (!WIDE) {  // lane by lane along the row, turned below
+        const uint32_t span0 = c0[u] - 8 * lane;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (span0 + 32 * i + lane < cols) v[u][i] = widen<T>(from[span0 + 32 * i + lane]);
+      } else if (c0[u] + 8 <= cols) {
+        const Eight<T> e = *reinterpret_cast<const Eight<T>*>(from + c0[u]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[u][i] = widen<T>(e.v[i]);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (c0[u] + i < cols) v[u][i] = widen<T>(from[i]);
+          if (c0[u] + i < cols) v[u][i] = widen<T>(from[c0[u] + i]);
       }
     }
 #pragma unroll
     for (int u = 0; u < kQUnroll; ++u) {
       if (row[u] == 0xffffffffu) break;
+      if (row[u] >= rows) {
+        if (lane % (4 * LANES) == 0)
+          *reinterpret_cast<uint32_t*>(scales + scale_at(row[u], c0[u] / (8 * LANES), tiles)) = 0;
+        continue;
+      }
+      if (!WIDE) turn<false>(buffer[threadIdx.x / 32], v[u], lane);
       uint32_t top = 0;  // bits of the largest magnitude: NaN and infinity above every number
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
@@ -150,14 +180,14 @@ __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int6
           }
         }
       }
-      if (row[u] >= rows || c0[u] >= cols) byte = 0;  // no such block, whatever the tensor scale is
+      if (c0[u] >= cols) byte = 0;  // no such block, whatever the tensor scale is
       uint32_t four = byte | __shfl_down_sync(0xffffffffu, byte, LANES) << 8;
       four |= __shfl_down_sync(0xffffffffu, four, 2 * LANES) << 16;
       if (lane % (4 * LANES) == 0) {
         const uint32_t block = c0[u] / (8 * LANES);
         *reinterpret_cast<uint32_t*>(scales + scale_at(row[u], block, tiles)) = four;
       }
-      if (row[u] < rows && c0[u] < cols) {
+      if (c0[u] < cols) {
         uint8_t* to = codes + (int64_t)row[u] * ld + c0[u] / 2;
         if (c0[u] + 8 <= cols) {
           *reinterpret_cast<uint32_t*>(to) = word;
@@ -175,6 +205,7 @@ __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* co
                                                                uint32_t cols, uint32_t tiles, FastDiv spans_div,
                                                                uint32_t spans, uint64_t total) {
   constexpr int LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;
+  __shared__ float buffer[WIDE ? 1 : kQThreads / 32][kSpan + 8 * kSpan / 32];
   pdl_trigger();
   pdl_wait();
   const uint32_t lane = threadIdx.x & 31;
@@ -187,32 +218,41 @@ __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* co
       const uint64_t n = at + u;
       row[u] = fast_div((uint32_t)n, spans_div);
       c0[u] = ((uint32_t)n - row[u] * spans) * kSpan + 8 * lane;
-      if (n >= total) c0[u] = cols;
-      if (c0[u] >= cols) continue;
+      word[u] = byte[u] = 0;
+      if (n >= total || c0[u] >= cols) continue;
       // (the four bytes lie in the row: ld is a multiple of 16)
       word[u] = *reinterpret_cast<const uint32_t*>(codes + (int64_t)row[u] * ld + c0[u] / 2);
       byte[u] = scales[scale_at(row[u], c0[u] / (8 * LANES), tiles)];
     }
 #pragma unroll
     for (int u = 0; u < kQUnroll; ++u) {
-      if (c0[u] >= cols) continue;
+      if (at + u >= total) break;
       const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(byte[u]) : e4m3_value(byte[u]);
-      Eight<T> e;
+      float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         // the three bits of the magnitude as the low exponent bits and the first fraction bit of a binary32, whose bias
         // is 126 more: a product with 2^126 gives the element, 0.5 from a number without its leading one included
         const uint32_t c = word[u] >> (4 * i);
         const float el = __uint_as_float((c & 7u) << 22 | (c & 8u) << 28) * 8.507059173023462e37f;
-        e.v[i] = narrow<T>(el * s * ts);
+        v[i] = el * s * ts;
       }
-      T* to = values + (int64_t)row[u] * ldv + c0[u];
-      if (WIDE && c0[u] + 8 <= cols) {
-        *reinterpret_cast<Eight<T>*>(to) = e;
+      T* to = values + (int64_t)row[u] * ldv;
+      if (!WIDE) {
+        turn<true>(buffer[threadIdx.x / 32], v, lane);
+        const uint32_t span0 = c0[u] - 8 * lane;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (span0 + 32 * i + lane < cols) to[span0 + 32 * i + lane] = narrow<T>(v[i]);
+      } else if (c0[u] + 8 <= cols) {
+        Eight<T> e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = narrow<T>(v[i]);
+        *reinterpret_cast<Eight<T>*>(to + c0[u]) = e;
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (c0[u] + i < cols) to[i] = e.v[i];
+          if (c0[u] + i < cols) to[c0[u] + i] = narrow<T>(v[i]);
       }
     }
   }
