@@ -306,24 +306,32 @@ def pvt_dequant(layer: pvt_layer, W_hat: torch.Tensor, status: Optional[torch.Te
 _DTYPE = {torch.float32: PVT_F32, torch.float16: PVT_F16, torch.bfloat16: PVT_BF16}
 
 
-def _on_device(device, *tensors) -> None:
-    """The calls enqueue on the current device: every tensor has to be there."""
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_for(device: int, stream, *tensors) -> int:
+    """The stream's handle.  The calls enqueue on the current device: every tensor has to be there."""
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device != device):
+        if t is not None and t.get_device() != device:
             raise ValueError("the tensors of a call lie on one CUDA device")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    if device < 0 or device != _current_device():
+        raise ValueError(f"the tensors are on device {device}, not on the current CUDA device")
+    return stream.cuda_stream if stream is not None else _raw_stream(device) if _raw_stream else _stream_ptr(None)
 
 
 def _matrix(t: torch.Tensor, rows: int, cols: int, what: str):
     """(dtype, elements from row to row) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or tuple(t.shape) != (rows, cols) or t.dtype not in _DTYPE:
+    dtype = _DTYPE.get(t.dtype)
+    if dtype is None or t.shape != (rows, cols):
         raise ValueError(f"{what} has to be a float32, float16 or bfloat16 matrix of {rows} x {cols}")
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
         raise ValueError(f"the rows of {what} have to be contiguous")
-    if rows > 1 and t.stride(0) < cols:
-        raise ValueError(f"the rows of {what} overlap")
-    return _DTYPE[t.dtype], t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"the rows of {what} overlap")
+        ld = cols
+    return dtype, ld
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype, what: str) -> Optional[int]:
@@ -345,36 +353,46 @@ class Mx:
 
     def __init__(self, codes, scales, rows, cols, fmt, tensor_scale):
         self.codes, self.scales, self.tensor_scale = codes, scales, tensor_scale
-        self.rows, self.cols, self.format = int(rows), int(cols), int(fmt)
-        self.device = codes.device
-        self.desc = pvt_mx(self.rows, self.cols, self.format, 0, codes.stride(0) if self.rows > 1 else codes.shape[1],
-                           codes.data_ptr(), scales.data_ptr(), _ptr(tensor_scale))
+        self.rows, self.cols, self.format = rows, cols, fmt
+        self.device = codes.get_device()
+        self.desc = pvt_mx(rows, cols, fmt, 0, codes.stride(0) if rows > 1 else codes.shape[1], codes.data_ptr(),
+                           scales.data_ptr(), None if tensor_scale is None else tensor_scale.data_ptr())
+        self.ref = ctypes.byref(self.desc)
 
 
 def make_mx(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt: int,
             tensor_scale: Optional[torch.Tensor] = None) -> Mx:
     """Describe a matrix whose arrays are CUDA tensors.  codes: uint8 [rows, at least ceil(cols / 2)], rows a multiple of 16
     bytes apart; scales: uint8, pvt_mx_scale_bytes of them; tensor_scale: one float32, for PVT_MX_E4M3_16 only."""
-    if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.shape[0] != rows or codes.stride(1) != 1:
-        raise ValueError("codes have to be uint8 [rows, bytes] with contiguous rows")
+    shape = codes.shape
+    if codes.dtype != torch.uint8 or len(shape) != 2 or shape[0] != rows or rows < 1 or cols < 1:
+        raise ValueError("codes have to be uint8 [rows, bytes], rows and cols positive")
     # (a row is read in pieces of 16 bytes)
-    if codes.shape[1] < (cols + 31) // 32 * 16 or (rows > 1 and codes.stride(0) < codes.shape[1]):
-        raise ValueError("a row of codes has to hold ceil(cols / 32) * 16 bytes")
-    if codes.stride(0) % 16 and rows > 1 or codes.shape[1] % 16:
+    ld, step = codes.stride()
+    if shape[1] % 16 or shape[1] < (cols + 31) // 32 * 16 or step != 1:
+        raise ValueError("a row of codes has to be contiguous and hold ceil(cols / 32) * 16 bytes or a larger multiple of 16")
+    if rows > 1 and (ld % 16 or ld < shape[1]):
         raise ValueError("rows of codes have to be a multiple of 16 bytes apart")
-    if scales.dtype != torch.uint8 or not scales.is_contiguous() or scales.numel() < pvt_mx_scale_bytes(rows, cols, fmt):
+    if fmt not in (PVT_MX_E8M0_32, PVT_MX_E4M3_16):
+        raise ValueError("unknown format")
+    need = -(-rows // 128) * -(-cols // 256) * (1024 if fmt == PVT_MX_E8M0_32 else 2048)
+    if scales.dtype != torch.uint8 or scales.numel() < need or not scales.is_contiguous():
         raise ValueError("scales have to be pvt_mx_scale_bytes contiguous uint8")
-    if tensor_scale is not None and (fmt != PVT_MX_E4M3_16 or tensor_scale.dtype != torch.float32 or tensor_scale.numel() != 1):
-        raise ValueError("tensor_scale has to be one float32, for PVT_MX_E4M3_16")
-    for t in (codes, scales, tensor_scale):
-        if t is not None and (not t.is_cuda or t.device != codes.device):
+    device = codes.get_device()
+    if tensor_scale is not None:
+        if fmt != PVT_MX_E4M3_16 or tensor_scale.dtype != torch.float32 or tensor_scale.numel() != 1:
+            raise ValueError("tensor_scale has to be one float32, for PVT_MX_E4M3_16")
+        if tensor_scale.get_device() != device:
             raise ValueError("the tensors of a matrix lie on one CUDA device")
+    if device < 0 or scales.get_device() != device:
+        raise ValueError("the tensors of a matrix lie on one CUDA device")
     return Mx(codes, scales, rows, cols, fmt, tensor_scale)
 
 
 def new_mx(rows: int, cols: int, fmt: int, tensor_scale: Optional[torch.Tensor] = None, device=None) -> Mx:
     """Room for a matrix of that shape (its content is undefined until pvt_mx_quantize)."""
     device = device or "cuda"
+    rows, cols = int(rows), int(cols)
     codes = torch.empty(rows, (cols + 31) // 32 * 16, dtype=torch.uint8, device=device)
     scales = torch.empty(pvt_mx_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device=device)
     return make_mx(codes, scales, rows, cols, fmt, tensor_scale)
@@ -390,23 +408,21 @@ def pvt_mx_scale_bytes(rows: int, cols: int, fmt: int) -> int:
 def pvt_mx_quantize(m: Mx, x: torch.Tensor, stream=None) -> None:
     """x (float32, float16 or bfloat16 [rows, cols], rows of any distance) into m's codes and scales."""
     dtype, ld = _matrix(x, m.rows, m.cols, "x")
-    _on_device(m.device, x)
-    _check(lib().pvt_mx_quantize(ctypes.byref(m.desc), x.data_ptr(), dtype, ld, _stream_ptr(stream)), "pvt_mx_quantize")
+    _check(lib().pvt_mx_quantize(m.ref, x.data_ptr(), dtype, ld, _stream_for(m.device, stream, x)), "pvt_mx_quantize")
 
 
 def pvt_mx_dequant(m: Mx, values: torch.Tensor, stream=None) -> None:
     """What m's codes and scales stand for."""
     dtype, ld = _matrix(values, m.rows, m.cols, "values")
-    _on_device(m.device, values)
-    _check(lib().pvt_mx_dequant(ctypes.byref(m.desc), values.data_ptr(), dtype, ld, _stream_ptr(stream)), "pvt_mx_dequant")
+    _check(lib().pvt_mx_dequant(m.ref, values.data_ptr(), dtype, ld, _stream_for(m.device, stream, values)),
+           "pvt_mx_dequant")
 
 
 def pvt_mx_product(x: Mx, w: Mx, y: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
     """y [tokens, outputs] = x w^T on the block-scaled tensor cores; x [tokens, inputs], w [outputs, inputs]."""
     dtype, ld = _matrix(y, x.rows, w.rows, "y")
-    _on_device(x.device, w.codes, y, status)
-    _check(lib().pvt_mx_product(ctypes.byref(x.desc), ctypes.byref(w.desc), y.data_ptr(), dtype, ld, _status_word(status),
-                                _stream_ptr(stream)), "pvt_mx_product")
+    _check(lib().pvt_mx_product(x.ref, w.ref, y.data_ptr(), dtype, ld, _status_word(status),
+                                _stream_for(x.device, stream, w.codes, y, status)), "pvt_mx_product")
 
 
 def _gradient(dy: torch.Tensor, tokens: int, outputs: int) -> int:
@@ -421,9 +437,8 @@ def pvt_mx_grad_input(dy: torch.Tensor, w: Mx, dx: torch.Tensor, status: Optiona
     """dx [tokens, inputs] = dy w; dy bfloat16 [tokens, outputs], 16-byte aligned, rows a multiple of 8 elements apart."""
     ldy = _gradient(dy, dy.shape[0], w.rows)
     dtype, ld = _matrix(dx, dy.shape[0], w.cols, "dx")
-    _on_device(w.device, dy, dx, status)
-    _check(lib().pvt_mx_grad_input(dy.data_ptr(), ldy, dy.shape[0], ctypes.byref(w.desc), dx.data_ptr(), dtype, ld,
-                                   _status_word(status), _stream_ptr(stream)), "pvt_mx_grad_input")
+    _check(lib().pvt_mx_grad_input(dy.data_ptr(), ldy, dy.shape[0], w.ref, dx.data_ptr(), dtype, ld, _status_word(status),
+                                   _stream_for(w.device, stream, dy, dx, status)), "pvt_mx_grad_input")
 
 
 def pvt_mx_grad_weight(dy: torch.Tensor, x: Mx, dw: torch.Tensor, accumulate: bool = False,
@@ -433,9 +448,9 @@ def pvt_mx_grad_weight(dy: torch.Tensor, x: Mx, dw: torch.Tensor, accumulate: bo
     dtype, ld = _matrix(dw, dy.shape[1], x.cols, "dw")
     if dtype != PVT_F32:
         raise ValueError("dw has to be float32")
-    _on_device(x.device, dy, dw, status)
-    _check(lib().pvt_mx_grad_weight(dy.data_ptr(), ldy, dy.shape[1], ctypes.byref(x.desc), dw.data_ptr(), ld,
-                                    1 if accumulate else 0, _status_word(status), _stream_ptr(stream)), "pvt_mx_grad_weight")
+    _check(lib().pvt_mx_grad_weight(dy.data_ptr(), ldy, dy.shape[1], x.ref, dw.data_ptr(), ld, 1 if accumulate else 0,
+                                    _status_word(status), _stream_for(x.device, stream, dy, dw, status)),
+           "pvt_mx_grad_weight")
 
 
 def pvt_distill_top(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor, lse: Optional[torch.Tensor] = None,
@@ -446,17 +461,16 @@ def pvt_distill_top(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torc
     k = int(top_idx.shape[-1])
     idx, val = _vector(top_idx, rows * k, torch.int32, "top_idx"), _vector(top_logit, rows * k, torch.float32, "top_logit")
     out = _vector(lse, rows, torch.float32, "lse")
-    _on_device(logits.device, top_idx, top_logit, lse)
     _check(lib().pvt_distill_top(logits.data_ptr(), dtype, ld, rows, vocab, k, temperature, idx, val, out,
-                                 _stream_ptr(stream)), "pvt_distill_top")
+                                 _stream_for(logits.get_device(), stream, top_idx, top_logit, lse)), "pvt_distill_top")
 
 
 class Distill:
     """The student's logits and what they are trained against: the tensors and their descriptor."""
 
     def __init__(self, desc, tensors):
-        self.desc, self.tensors = desc, tensors
-        self.device, self.rows, self.vocab = tensors[0].device, int(desc.rows), int(desc.vocab)
+        self.desc, self.ref, self.tensors = desc, ctypes.byref(desc), tensors
+        self.device, self.rows, self.vocab = tensors[0].get_device(), desc.rows, desc.vocab
 
 
 def make_distill(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor,
@@ -472,8 +486,9 @@ def make_distill(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.T
                        _vector(top_logit, rows * k, torch.float32, "top_logit"),
                        _vector(teacher_lse, rows, torch.float32, "teacher_lse"), _vector(weight, rows, torch.float32, "weight"))
     tensors = (logits, top_idx, top_logit, teacher_lse, weight)
+    device = logits.get_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device != logits.device):
+        if t is not None and (device < 0 or t.get_device() != device):
             raise ValueError("the tensors of a distillation lie on one CUDA device")
     return Distill(desc, tensors)
 
@@ -487,9 +502,8 @@ def pvt_distill_loss(d: Distill, loss: torch.Tensor, stats: Optional[torch.Tenso
     out = _vector(loss, d.rows, torch.float32, "loss")
     st = _vector(stats, d.rows * PVT_DISTILL_STATS, torch.float32, "stats")
     up = _vector(upstream, d.rows, torch.float32, "upstream")
-    _on_device(d.device, loss, stats, upstream, grad, status)
-    _check(lib().pvt_distill_loss(ctypes.byref(d.desc), out, st, up, _ptr(grad), dtype, ld, _status_word(status),
-                                  _stream_ptr(stream)), "pvt_distill_loss")
+    _check(lib().pvt_distill_loss(d.ref, out, st, up, _ptr(grad), dtype, ld, _status_word(status),
+                                  _stream_for(d.device, stream, loss, stats, upstream, grad, status)), "pvt_distill_loss")
 
 
 def pvt_distill_grad(d: Distill, stats: torch.Tensor, grad: torch.Tensor, upstream: Optional[torch.Tensor] = None,
@@ -498,9 +512,8 @@ def pvt_distill_grad(d: Distill, stats: torch.Tensor, grad: torch.Tensor, upstre
     dtype, ld = _matrix(grad, d.rows, d.vocab, "grad")
     st = _vector(stats, d.rows * PVT_DISTILL_STATS, torch.float32, "stats")
     up = _vector(upstream, d.rows, torch.float32, "upstream")
-    _on_device(d.device, stats, upstream, grad, status)
-    _check(lib().pvt_distill_grad(ctypes.byref(d.desc), st, up, grad.data_ptr(), dtype, ld, _status_word(status),
-                                  _stream_ptr(stream)), "pvt_distill_grad")
+    _check(lib().pvt_distill_grad(d.ref, st, up, grad.data_ptr(), dtype, ld, _status_word(status),
+                                  _stream_for(d.device, stream, stats, upstream, grad, status)), "pvt_distill_grad")
 
 
 class Block:
