@@ -149,46 +149,50 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
 
     Running run;
     if (active) {
-      for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kUnroll * kThreads) {
+      using Top = Tops<T>;
+      auto add = [&](const Piece<T>& piece, uint32_t i) {
+        const float sum = terms(piece, run.base(), p.c);
+        run.z += sum;
+        if (tail) {
+          const uint32_t bit = (i + 1) * N, mask = listed[bit / 32] >> (bit % 32) & ((1u << N) - 1);
+          if (mask == 0)
+            run.r += sum;
+          else
+            for (uint32_t e = 0; e < N; ++e)
+              if (!(mask >> e & 1u)) run.r += run.term(widen<T>(row[s.head + i * N + e]), p.c);
+        }
+      };
+      uint32_t i0 = s.lo + tid;
+      for (; i0 + (kUnroll - 1) * kThreads < s.hi; i0 += kUnroll * kThreads) {
         Piece<T> piece[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
-        float top = kMinusInf;
+        for (int u = 0; u < kUnroll; ++u) piece[u] = pieces[i0 + u * kThreads];
+        auto top = Top::of(piece[0]);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (i0 + u * kThreads < s.hi) top = fmaxf(top, largest(piece[u]));
-        run.raise(top, p.c);
-        const float base = run.base();
+        for (int u = 1; u < kUnroll; ++u) top = Top::max(top, Top::of(piece[u]));
+        run.raise(Top::value(top), p.c);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (i0 + u * kThreads < s.hi) {
-            const float sum = terms(piece[u], base, p.c);
-            run.z += sum;
-            if (tail) {
-              const uint32_t i = i0 + u * kThreads, bit = (i + 1) * N, mask = listed[bit / 32] >> (bit % 32) & ((1u << N) - 1);
-              if (mask == 0)
-                run.r += sum;
-              else
-                for (uint32_t e = 0; e < N; ++e)
-                  if (!(mask >> e & 1u)) run.r += ex2((widen<T>(row[s.head + i * N + e]) - base) * p.c);
-            }
-          }
+        for (int u = 0; u < kUnroll; ++u) add(piece[u], i0 + u * kThreads);
+      }
+      for (; i0 < s.hi; i0 += kThreads) {
+        const Piece<T> piece = pieces[i0];
+        run.raise(Top::value(Top::of(piece)), p.c);
+        add(piece, i0);
       }
       if (tid < s.loose()) {
         const uint32_t at = s.loose_at(tid), bit = at + N - s.head;
         const float x = widen<T>(row[at]);
         run.raise(x, p.c);
-        const float y = ex2((x - run.base()) * p.c);
+        const float y = run.term(x, p.c);
         run.z += y;
         if (tail && !(listed[bit / 32] >> (bit % 32) & 1u)) run.r += y;
       }
-      run = block_merge(run, p.c, sm.run);
+      run = block_merge<true>(run, p.c, sm.run);
     }
     if (p.blocks > 1) {
       if (tid == 0) sm.mine = run;
       cluster_sync();
-      run = cluster_merge(&sm.mine, p.blocks, p.c);
+      run = cluster_merge<true>(&sm.mine, p.blocks, p.c);
       cluster_sync();
     }
     // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
@@ -207,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
             if (prob != 0.0) value += prob * (log_p - log_q);
           }
         value = block_sum(value, sm.sum);
-        if (rest != 0.0) value += rest * (log(rest) - (log((double)run.r) - log_z));
+        if (rest != 0.0) value += rest * (log(rest) - log((double)run.r) + log(z));
       }
       const double whole = mass + rest;
       f_listed = (float)(whole / z);
@@ -239,25 +243,27 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
     const float m = sm.stat[kStatMax], f_listed = sm.stat[kStatListed], f_rest = sm.stat[kStatRest] * up;
     auto y_of = [&](float x) { return ex2((x - m) * p.c); };
     if (sizeof(G) == sizeof(T) && (reinterpret_cast<uintptr_t>(grad) - reinterpret_cast<uintptr_t>(row)) % 16 == 0) {
-      const Two base = two(-m, -m), cc = two(p.c, p.c), ff = two(f_rest, f_rest);
-      for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kUnroll * kThreads) {
+      const Two bb = two(-m, -m), cc = two(p.c, p.c), ff = two(f_rest, f_rest);
+      Piece<G>* const to = reinterpret_cast<Piece<G>*>(grad + s.head);
+      auto write = [&](const Piece<T>& piece, uint32_t i) {
+        Piece<G> out;
+#pragma unroll
+        for (uint32_t e = 0; e < N / 2; ++e) {
+          const float2 y = each(mul2(add2(pair_of(piece, e), bb), cc));
+          const float2 g = each(mul2(two(ex2(y.x), ex2(y.y)), ff));
+          out.v[2 * e % Piece<G>::N] = narrow<G>(g.x), out.v[(2 * e + 1) % Piece<G>::N] = narrow<G>(g.y);
+        }
+        to[i] = out;
+      };
+      uint32_t i0 = s.lo + tid;
+      for (; i0 + (kUnroll - 1) * kThreads < s.hi; i0 += kUnroll * kThreads) {
         Piece<T> piece[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
+        for (int u = 0; u < kUnroll; ++u) piece[u] = pieces[i0 + u * kThreads];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          if (i0 + u * kThreads >= s.hi) continue;
-          Piece<G> out;
-#pragma unroll
-          for (uint32_t e = 0; e < N / 2; ++e) {
-            const float2 y = each(mul2(add2(pair_of(piece[u], e), base), cc));
-            const float2 g = each(mul2(two(ex2(y.x), ex2(y.y)), ff));
-            out.v[2 * e % Piece<G>::N] = narrow<G>(g.x), out.v[(2 * e + 1) % Piece<G>::N] = narrow<G>(g.y);
-          }
-          reinterpret_cast<Piece<G>*>(grad + s.head)[i0 + u * kThreads] = out;
-        }
+        for (int u = 0; u < kUnroll; ++u) write(piece[u], i0 + u * kThreads);
       }
+      for (; i0 < s.hi; i0 += kThreads) write(pieces[i0], i0);
       if (tid < s.loose()) {
         const uint32_t at = s.loose_at(tid);
         grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);

@@ -8,7 +8,7 @@ namespace pvt {
 namespace distill {
 
 constexpr int kThreads = 256;
-constexpr int kResident = 4;  // blocks per SM: while some settle their lists the others' loads are in flight
+constexpr int kResident = 5;  // blocks per SM: while some settle their lists the others' loads are in flight
 constexpr int kMaxBlocks = 8;  // of a row
 
 #ifdef __CUDACC__
@@ -92,25 +92,51 @@ __device__ __forceinline__ Two pair_of(const Piece<__nv_bfloat16>& p, int i) {
   const uint32_t u = reinterpret_cast<const uint32_t*>(p.v)[i];
   return two(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
 }
-// the largest element, a NaN if there is one
-__device__ __forceinline__ float largest(const Piece<float>& p) {
-  return max_nan(max_nan(p.v[0], p.v[1]), max_nan(p.v[2], p.v[3]));
-}
-__device__ __forceinline__ float largest(const Piece<__half>& p) {
-  const __half2* h = reinterpret_cast<const __half2*>(p.v);
-  const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-  return __half2float(__hmax_nan(__low2half(m), __high2half(m)));
-}
-__device__ __forceinline__ float largest(const Piece<__nv_bfloat16>& p) {
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(p.v);
-  const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-  return __bfloat162float(__hmax_nan(__low2bfloat16(m), __high2bfloat16(m)));
-}
+// The largest elements, NaN where there is one: in as many places as a register holds (Top), and of those.
+template <typename T>
+struct Tops;
+template <>
+struct Tops<float> {
+  using Top = float;
+  static __device__ __forceinline__ Top lowest() { return kMinusInf; }
+  static __device__ __forceinline__ Top max(Top a, Top b) { return max_nan(a, b); }
+  static __device__ __forceinline__ Top of(const Piece<float>& p) { return max_nan(max_nan(p.v[0], p.v[1]), max_nan(p.v[2], p.v[3])); }
+  static __device__ __forceinline__ float value(Top a) { return a; }
+  static __device__ __forceinline__ Top limit(float x) { return x; }
+  static __device__ __forceinline__ bool reaches(Top a, Top least) { return !(a < least); }  // a NaN does
+};
+template <>
+struct Tops<__half> {
+  using Top = __half2;
+  static __device__ __forceinline__ Top lowest() { return __float2half2_rn(kMinusInf); }
+  static __device__ __forceinline__ Top max(Top a, Top b) { return __hmax2_nan(a, b); }
+  static __device__ __forceinline__ Top of(const Piece<__half>& p) {
+    const __half2* h = reinterpret_cast<const __half2*>(p.v);
+    return max(max(h[0], h[1]), max(h[2], h[3]));
+  }
+  static __device__ __forceinline__ float value(Top a) { return max_nan(__low2float(a), __high2float(a)); }
+  // the smallest one that is not below x
+  static __device__ __forceinline__ Top limit(float x) { return __half2half2(__float2half_ru(x)); }
+  static __device__ __forceinline__ bool reaches(Top a, Top least) { return __hgeu2_mask(a, least) != 0; }
+};
+template <>
+struct Tops<__nv_bfloat16> {
+  using Top = __nv_bfloat162;
+  static __device__ __forceinline__ Top lowest() { return __float2bfloat162_rn(kMinusInf); }
+  static __device__ __forceinline__ Top max(Top a, Top b) { return __hmax2_nan(a, b); }
+  static __device__ __forceinline__ Top of(const Piece<__nv_bfloat16>& p) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(p.v);
+    return max(max(h[0], h[1]), max(h[2], h[3]));
+  }
+  static __device__ __forceinline__ float value(Top a) { return max_nan(__low2float(a), __high2float(a)); }
+  static __device__ __forceinline__ Top limit(float x) { return __bfloat162bfloat162(__float2bfloat16_ru(x)); }
+  static __device__ __forceinline__ bool reaches(Top a, Top least) { return __hgeu2_mask(a, least) != 0; }
+};
 
 // ---- sums of exponentials ---------------------------------------------------------------------------------
 // Largest value so far, and sums of 2^(c (x - base)) where base is the largest value, or 0 as long as that is infinite: a sum
 // over -infinity alone is 0, one with infinity infinite, one with a NaN a NaN.  Differences are formed before the product
-// with c, for the terms that make up the sum have small ones.
+// with c: those of the terms that make up the sum are small, and no product overflows that matters.
 struct Running {
   float m = kMinusInf, z = 0.0f, r = 0.0f;
   __device__ __forceinline__ float base() const { return fabsf(m) == -kMinusInf ? 0.0f : m; }
@@ -120,57 +146,61 @@ struct Running {
       z *= f, r *= f, m = to;
     }
   }
+  __device__ __forceinline__ float term(float x, float c) const { return ex2((x - base()) * c); }
 };
 // the N terms of a piece, added in pairs
 template <typename T>
 __device__ __forceinline__ float terms(const Piece<T>& p, float base, float c) {
-  const Two b = two(-base, -base), cc = two(c, c);
+  const Two bb = two(-base, -base), cc = two(c, c);
   Two sum = 0;
 #pragma unroll
   for (uint32_t i = 0; i < Piece<T>::N / 2; ++i) {
-    const float2 y = each(mul2(add2(pair_of(p, i), b), cc));
-    sum = add2(sum, two(ex2(y.x), ex2(y.y)));
+    const float2 y = each(mul2(add2(pair_of(p, i), bb), cc));
+    const Two t = two(ex2(y.x), ex2(y.y));
+    sum = i ? add2(sum, t) : t;
   }
   const float2 s = each(sum);
   return s.x + s.y;
 }
 
-__device__ __forceinline__ Running merge(Running a, Running b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  a.raise(m, c), b.raise(m, c);
-  a.z += b.z, a.r += b.r;
-  return a;
+// order of numbers as that of integers (no NaN)
+__device__ __forceinline__ int ordered(float x) {
+  const int i = __float_as_int(x);
+  return i ^ (i >> 31 & 0x7fffffff);
 }
-// over `lanes` lanes (a power of two) that begin at a multiple of it
+__device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i ^ (i >> 31 & 0x7fffffff)); }
+// over `lanes` lanes (a power of two) that begin at a multiple of it; the same in all of them
+template <bool WITH_R>
 __device__ __forceinline__ Running warp_merge(Running a, float c, int lanes = 32) {
+  // (over all lanes: those beyond hold parts of the same sum)
+  a.raise(from_ordered(__reduce_max_sync(0xffffffffu, ordered(a.m))), c);
   for (int s = lanes / 2; s >= 1; s /= 2) {
-    Running b;
-    b.m = __shfl_xor_sync(0xffffffffu, a.m, s);
-    b.z = __shfl_xor_sync(0xffffffffu, a.z, s);
-    b.r = __shfl_xor_sync(0xffffffffu, a.r, s);
-    a = merge(a, b, c);
+    a.z += __shfl_xor_sync(0xffffffffu, a.z, s);
+    if (WITH_R) a.r += __shfl_xor_sync(0xffffffffu, a.r, s);
   }
   return a;
 }
 // over the block, the same in every thread; `sh`: a slot per warp
+template <bool WITH_R>
 __device__ __forceinline__ Running block_merge(Running a, float c, Running* sh) {
   constexpr int kWarps = kThreads / 32;
-  a = warp_merge(a, c);
+  a = warp_merge<WITH_R>(a, c);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x / 32] = a;
   __syncthreads();
-  return warp_merge(sh[threadIdx.x % kWarps], c, kWarps);
+  return warp_merge<WITH_R>(sh[threadIdx.x % kWarps], c, kWarps);
 }
 // over the cluster, the same in every thread; `mine`: the block's own sums, in shared memory before the cluster's barrier
+template <bool WITH_R>
 __device__ __forceinline__ Running cluster_merge(const Running* mine, uint32_t blocks, float c) {
   const uint32_t at = mma::smem_u32(mine), q = threadIdx.x % kMaxBlocks;
   Running a;
   if (q < blocks) {
     a.m = mma::cluster_load(at + (uint32_t)offsetof(Running, m), q);
     a.z = mma::cluster_load(at + (uint32_t)offsetof(Running, z), q);
-    a.r = mma::cluster_load(at + (uint32_t)offsetof(Running, r), q);
+    if (WITH_R) a.r = mma::cluster_load(at + (uint32_t)offsetof(Running, r), q);
   }
   __syncwarp();
-  return warp_merge(a, c, kMaxBlocks);
+  return warp_merge<WITH_R>(a, c, kMaxBlocks);
 }
 #endif
 

@@ -1,13 +1,14 @@
 // The k largest logits of each row, in order, and the logarithm of the sum of all exponentials.
 //
-// One pass over the row keeps, besides the running sum, the largest value of each of 2048 parts of it (eight per thread).  If every
-// warp takes the j-th largest of the maxima of its 256 parts, j = ceil(k / warps), at least k elements are not below the smallest
-// of these, so everything that is listed is among the elements that reach that bound; with parts in no relation to the values
-// those are few more.  A second pass over the row, which comes from the L2, collects them (a piece of 16 bytes is
-// dismissed by its largest element), and they are put in order in shared memory.  A row in which too many elements reach the bound
-// (equal ones, or a list nearly as long as the parts are many) is settled by counting the digits of its keys instead.  A few long
-// rows are shared by clusters: each block lists its part, and an entry's place is its own plus those that the other
-// blocks' lists hold ahead of it.
+// One pass over the row keeps, besides the running sum, the largest value of each of 256 or 2048 parts of it (one or eight per
+// thread).  The k-th largest of 256 maxima has at least k elements not below it, so everything that is listed is among the elements
+// that reach that bound; with parts in no relation to the values those are few more (74 for k = 64).  For k > 128 every
+// warp takes the j-th largest of its 256 maxima, j = ceil(k / warps), and the smallest of these serves.  A second pass
+// over the row, which comes from the L2, collects them (a piece of 16 bytes is dismissed by its largest element), and they
+// are put in order in shared memory.  A row in which too many elements reach the bound (equal ones, or a list nearly as
+// long as the parts are many) is settled by counting the digits of its keys instead.  A few long rows are shared by
+// clusters: each block lists its part, and an entry's place is its own plus those that the other blocks' lists hold
+// ahead of it.
 #include "pvt_distill.cuh"
 
 namespace pvt {
@@ -16,7 +17,7 @@ namespace {
 using namespace distill;
 using namespace mma;
 
-constexpr int kParts = 8;           // of each thread
+constexpr int kParts = 8;           // of each thread, and keys of each lane that looks for a bound
 constexpr int kWarps = kThreads / 32;
 constexpr int kCandidates = 2048;   // that are put in order at once
 constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
@@ -46,6 +47,7 @@ struct TopShared {
   Running run[kWarps];
   Running mine;
   uint32_t bound[kWarps];
+  uint32_t part[kThreads];
   uint32_t hist[256];
   uint32_t digit, above, count, n;
   alignas(8) uint64_t entries[kCandidates];
@@ -94,21 +96,20 @@ __device__ __forceinline__ void for_each(const T* row, const RowShare<T>& s, F f
 
 // n entries (at most kCandidates) in order; the first min(n, k) to sm.sorted
 __device__ __forceinline__ void put_in_order(TopShared& sm, uint32_t n, uint32_t k) {
-  if (n <= 2 * kThreads) {
+  if (n <= kThreads / 2) {
     // an entry's place is the number of those ahead of it, counted by as many threads as there are for each
-    uint32_t each = 1;
+    uint32_t each = 2;
     while (each < 32 && 2 * each * n <= kThreads) each *= 2;
-    for (uint32_t at = threadIdx.x / each; at - threadIdx.x / each < n; at += kThreads / each) {
-      const bool real = at < n;
-      const uint64_t own = real ? sm.entries[at] : 0;
-      uint32_t place = 0;
+    const uint32_t at = threadIdx.x / each;
+    const uint64_t own = at < n ? sm.entries[at] : 0;
+    uint32_t place = 0;
 #pragma unroll 8
-      for (uint32_t i = threadIdx.x % each; i < n; i += each) place += sm.entries[i] < own;
-      for (uint32_t s = 1; s < each; s *= 2) place += __shfl_xor_sync(0xffffffffu, place, s);
-      if (real && threadIdx.x % each == 0 && place < k) sm.sorted[place] = own;
-    }
+    for (uint32_t i = threadIdx.x % each; i < n; i += each) place += sm.entries[i] < own;
+    for (uint32_t s = 1; s < each; s *= 2) place += __shfl_xor_sync(0xffffffffu, place, s);
+    if (at < n && threadIdx.x % each == 0 && place < k) sm.sorted[place] = own;
   } else {
-    uint32_t size = 4 * kThreads;
+    // bitonic sort; steps of up to 32 stay within the 64 entries of a warp (300 entries 3 us, where counting takes 25)
+    uint32_t size = kThreads;
     while (size < n) size *= 2;
     for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sm.entries[i] = ~0ull;
     __syncthreads();
@@ -119,8 +120,12 @@ __device__ __forceinline__ void put_in_order(TopShared& sm, uint32_t n, uint32_t
           const uint64_t x = sm.entries[a], y = sm.entries[b];
           if ((x > y) == ((a & run) == 0)) sm.entries[a] = y, sm.entries[b] = x;
         }
-        __syncthreads();
+        if (step > 32 || (step == 1 && run > 32))
+          __syncthreads();
+        else
+          __syncwarp();
       }
+    __syncthreads();
     for (uint32_t i = threadIdx.x; i < min(n, k); i += kThreads) sm.sorted[i] = sm.entries[i];
   }
   __syncthreads();
@@ -190,74 +195,101 @@ __device__ __forceinline__ uint32_t warp_bound(const uint32_t* key, uint32_t j) 
   return lo << 16;
 }
 
-template <typename T>
+template <typename T, bool MANY>
 __global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const TopParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
   TopShared& sm = *reinterpret_cast<TopShared*>(raw);
   pdl_trigger();
   pdl_wait();
-  constexpr uint32_t N = Piece<T>::N;
+  using Top = Tops<T>;
+  constexpr uint32_t N = Piece<T>::N, PARTS = MANY ? kParts : 1, UNROLL = MANY ? kParts : 4;
   const uint32_t tid = threadIdx.x, rank = blockIdx.x % p.blocks, r = blockIdx.x / p.blocks, k = p.k;
   const T* row = static_cast<const T*>(p.logits) + (int64_t)r * p.ld;
   const RowShare<T> s(row, p.vocab, rank, p.blocks);
   const Piece<T>* const pieces = reinterpret_cast<const Piece<T>*>(row + s.head);
 
   Running run;
-  float part[kParts];
+  typename Top::Top part[PARTS];
 #pragma unroll
-  for (int u = 0; u < kParts; ++u) part[u] = kMinusInf;
-  for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kParts * kThreads) {
-    Piece<T> piece[kParts];
+  for (uint32_t u = 0; u < PARTS; ++u) part[u] = Top::lowest();
+  uint32_t i0 = s.lo + tid;
+  for (; i0 + (UNROLL - 1) * kThreads < s.hi; i0 += UNROLL * kThreads) {
+    Piece<T> piece[UNROLL];
 #pragma unroll
-    for (int u = 0; u < kParts; ++u)
-      if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
-    float top = kMinusInf;
+    for (uint32_t u = 0; u < UNROLL; ++u) piece[u] = pieces[i0 + u * kThreads];
+    auto top = Top::of(piece[0]);
+    if (MANY) part[0] = Top::max(part[0], top);
 #pragma unroll
-    for (int u = 0; u < kParts; ++u)
-      if (i0 + u * kThreads < s.hi) {
-        const float m = largest(piece[u]);
-        part[u] = max_nan(part[u], m);
-        top = fmaxf(top, m);
-      }
-    run.raise(top, p.c);
-    const float base = run.base();
+    for (uint32_t u = 1; u < UNROLL; ++u) {
+      const auto m = Top::of(piece[u]);
+      if (MANY) part[u % PARTS] = Top::max(part[u % PARTS], m);
+      top = Top::max(top, m);
+    }
+    if (!MANY) part[0] = Top::max(part[0], top);
+    run.raise(Top::value(top), p.c);
 #pragma unroll
-    for (int u = 0; u < kParts; ++u)
-      if (i0 + u * kThreads < s.hi) run.z += terms(piece[u], base, p.c);
+    for (uint32_t u = 0; u < UNROLL; ++u) run.z += terms(piece[u], run.base(), p.c);
   }
+#pragma unroll
+  for (uint32_t u = 0; u < UNROLL - 1; ++u) {
+    if (i0 + u * kThreads >= s.hi) break;
+    const Piece<T> piece = pieces[i0 + u * kThreads];
+    const auto m = Top::of(piece);
+    part[u % PARTS] = Top::max(part[u % PARTS], m);
+    run.raise(Top::value(m), p.c);
+    run.z += terms(piece, run.base(), p.c);
+  }
+  float loose = kMinusInf;
   if (tid < s.loose()) {
-    const float x = widen<T>(row[s.loose_at(tid)]);
-    part[0] = max_nan(part[0], x);
-    run.raise(x, p.c);
-    run.z += ex2((x - run.base()) * p.c);
-  }
-  {
-    uint32_t key[kParts];
-#pragma unroll
-    for (int u = 0; u < kParts; ++u) key[u] = key_of(part[u]);
-    const uint32_t bound = warp_bound(key, (k + kWarps - 1) / kWarps);
-    if (tid % 32 == 0) sm.bound[tid / 32] = bound;
+    loose = widen<T>(row[s.loose_at(tid)]);
+    run.raise(loose, p.c);
+    run.z += run.term(loose, p.c);
   }
   if (tid == 0) sm.count = sm.digit = 0;
-  run = block_merge(run, p.c, sm.run);
+  uint32_t bound;
+  if (MANY) {
+    uint32_t key[kParts];
+#pragma unroll
+    for (int u = 0; u < kParts; ++u) key[u] = key_of(max_nan(Top::value(part[u % PARTS]), u ? kMinusInf : loose));
+    bound = warp_bound(key, (k + kWarps - 1) / kWarps);
+    if (tid % 32 == 0) sm.bound[tid / 32] = bound;
+    run = block_merge<false>(run, p.c, sm.run);
+    bound = __reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]);
+  } else {
+    sm.part[tid] = key_of(max_nan(Top::value(part[0]), loose));
+    run = block_merge<false>(run, p.c, sm.run);
+    if (tid < 32) {
+      uint32_t key[kParts];
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) key[u] = sm.part[tid + 32 * u];
+      bound = warp_bound(key, k);
+      if (tid == 0) sm.bound[0] = bound;
+    }
+    __syncthreads();
+    bound = sm.bound[0];
+  }
   if (tid == 0) sm.mine = run;
   // what is below reaches no place of the list; -infinity never does
-  const uint32_t bound = max(__reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]), kLowest + 1);
+  bound = max(bound, kLowest + 1);
   const float least = value_of(bound);
+  const auto limit = Top::limit(least);
   uint32_t* const reached = reinterpret_cast<uint32_t*>(sm.sorted);  // pieces whose largest element reaches it
   constexpr uint32_t kPieces = sizeof(sm.sorted) / 4;
-  for (uint32_t i0 = s.lo + tid; i0 < s.hi; i0 += kParts * kThreads) {
-    Piece<T> piece[kParts];
+  auto look = [&](const Piece<T>& piece, uint32_t i) {
+    if (Top::reaches(Top::of(piece), limit)) {
+      const uint32_t n = atomicAdd(&sm.digit, 1u);
+      if (n < kPieces) reached[n] = i;
+    }
+  };
+  i0 = s.lo + tid;
+  for (; i0 + 3 * kThreads < s.hi; i0 += 4 * kThreads) {
+    Piece<T> piece[4];
 #pragma unroll
-    for (int u = 0; u < kParts; ++u)
-      if (i0 + u * kThreads < s.hi) piece[u] = pieces[i0 + u * kThreads];
+    for (uint32_t u = 0; u < 4; ++u) piece[u] = pieces[i0 + u * kThreads];
 #pragma unroll
-    for (int u = 0; u < kParts; ++u)
-      if (i0 + u * kThreads < s.hi && !(largest(piece[u]) < least)) {
-        const uint32_t n = atomicAdd(&sm.digit, 1u);
-        if (n < kPieces) reached[n] = i0 + u * kThreads;
-      }
+    for (uint32_t u = 0; u < 4; ++u) look(piece[u], i0 + u * kThreads);
   }
+  for (; i0 < s.hi; i0 += kThreads) look(pieces[i0], i0);
   __syncthreads();
   // their elements, one to a thread
   const uint32_t n_reached = sm.digit;
@@ -295,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const 
   } else {
     if (tid == 0) sm.n = n;
     cluster_sync();
-    run = cluster_merge(&sm.mine, p.blocks, p.c);
+    run = cluster_merge<false>(&sm.mine, p.blocks, p.c);
     // the other blocks' lists, side by side, behind this block's own memory
     uint64_t* lists = reinterpret_cast<uint64_t*>(raw + sizeof(TopShared));
     uint32_t size[kMaxBlocks];
@@ -345,11 +377,15 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const 
   }
 }
 
+template <typename T, bool MANY>
+cudaError_t top(const TopParams& p, int64_t rows, size_t smem, cudaStream_t stream) {
+  const cudaError_t e = allow_smem<distill_top_kernel<T, MANY>>();
+  if (e != cudaSuccess) return e;
+  return launch_clusters(distill_top_kernel<T, MANY>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
+}
 template <typename T>
 cudaError_t top(const TopParams& p, int64_t rows, size_t smem, cudaStream_t stream) {
-  const cudaError_t e = allow_smem<distill_top_kernel<T>>();
-  if (e != cudaSuccess) return e;
-  return launch_clusters(distill_top_kernel<T>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
+  return p.k <= (uint32_t)kThreads / 2 ? top<T, false>(p, rows, smem, stream) : top<T, true>(p, rows, smem, stream);
 }
 
 }  // namespace
