@@ -50,34 +50,46 @@ struct ProductShared {
   uint32_t tmem, abandoned;
 };
 
+template <int CTAS = 1>
 __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc) {
-  asm volatile(
-      "{\n\t.reg .pred one;\n\t"
-      "elect.sync _|one, 0xffffffff;\n\t"
-      "@one tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
-      : "memory");
+  if (CTAS == 1)
+    asm volatile(
+        "{\n\t.reg .pred one;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "@one tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred one;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
+        : "memory");
 }
-template <int FMT>
+#define PVT_MULTIPLY(GROUP, KIND)                                                                                     \
+  asm volatile(                                                                                                       \
+      "{\n\t.reg .pred one, p;\n\t"                                                                                   \
+      "elect.sync _|one, 0xffffffff;\n\t"                                                                             \
+      "setp.ne.u32 p, %6, 0;\n\t"                                                                                     \
+      "@one tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a),  \
+      "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)                                                               \
+      : "memory")
+// 64 columns of all rows of a tile
+template <int FMT, int CTAS = 1>
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                          uint32_t onto) {
   if (FMT == PVT_MX_E8M0_32) {
-    asm volatile(
-        "{\n\t.reg .pred one, p;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %6, 0;\n\t"
-        "@one tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
-        : "memory");
+    if (CTAS == 1)
+      PVT_MULTIPLY("1", "mxf4.block_scale.scale_vec::2X");
+    else
+      PVT_MULTIPLY("2", "mxf4.block_scale.scale_vec::2X");
   } else {
-    asm volatile(
-        "{\n\t.reg .pred one, p;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %6, 0;\n\t"
-        "@one tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
-        : "memory");
+    if (CTAS == 1)
+      PVT_MULTIPLY("1", "mxf4nvf4.block_scale.scale_vec::4X");
+    else
+      PVT_MULTIPLY("2", "mxf4nvf4.block_scale.scale_vec::4X");
   }
 }
+#undef PVT_MULTIPLY
 
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_constant__ CUtensorMap w_map,
@@ -226,9 +238,224 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
   }
 }
 
+// ---- pairs of blocks -------------------------------------------------------------------------------------------
+// With many rows of x a pair of blocks on neighbouring SMs multiplies 256 rows of w by 256 of x (tcgen05.mma cta_group::2): each block
+// holds 128 rows of either, so a step brings 32 KB of codes into an SM instead of 48 KB for the same 128 x 256 sums.  What an SM
+// can take in, about 60 bytes a cycle, is the bound of this product: four instructions of a step are 512 cycles.  The
+// blocks stay and take tile after tile; copies for the next one are under way while eight warps empty the sums into
+// registers, and those are stored while it is multiplied.
+constexpr int kPairReaders = 8;  // warps
+constexpr int kPairThreads = (kPairReaders + 2) * 32;
+constexpr int kPairCopyWarp = kPairReaders, kPairMmaWarp = kPairReaders + 1;
+constexpr uint32_t kPairRows = 256;   // of w and of x
+constexpr uint32_t kPairStages = 5;
+
+struct PairShared {
+  alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
+  uint64_t empty[kPairStages];            // of each
+  uint64_t sums_full;                     // of each
+  uint64_t sums_empty;                    // of the first: an arrival per reading warp of both
+  uint64_t spare;
+  uint32_t tmem, abandoned;
+};
+
+struct PairParams {
+  const float* w_ts;
+  const float* x_ts;
+  void* y;
+  int64_t ldy;
+  uint32_t* status;
+  uint32_t w_rows, x_rows;
+  uint32_t strip_rows;   // rows of 128 bytes that a strip's scales are
+  uint32_t steps;        // of 256 columns
+  uint32_t x_tiles, tiles;
+  uint32_t max_spins, withhold;
+};
+
+template <int FMT>
+struct PairSizes {
+  static constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;
+  static constexpr uint32_t kX = kTileW * kRowBytes, kWs = 2 * kX, kXs = kWs + KT * kTileBytes, kStage = kXs + 2 * KT * kTileBytes;
+  static constexpr uint32_t kStageAligned = (kStage + 1023) / 1024 * 1024;
+  static constexpr uint32_t kScaleCols = KT * 4 * 3;  // of a stage
+  static constexpr uint32_t kStages = kPairStages;
+  static_assert(256 + kStages * kScaleCols <= 512, "sums and scales fit tensor memory");
+};
+
+template <typename T, int FMT>
+__global__ void __launch_bounds__(kPairThreads, 1)
+    mx_product_pair_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
+                           const __grid_constant__ CUtensorMap ws_map, const __grid_constant__ CUtensorMap xs_map, const PairParams p) {
+  using S = PairSizes<FMT>;
+  constexpr uint32_t KT = S::KT, STAGES = S::kStages;
+  extern __shared__ __align__(1024) unsigned char raw[];
+  __shared__ PairShared sm;
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  volatile uint32_t* abandoned = &sm.abandoned;
+  if (tid == 0) {
+    sm.abandoned = 0;
+    for (uint32_t s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&sm.full[s]), 1);
+      mbar_init(smem_u32(&sm.empty[s]), 1);
+    }
+    mbar_init(smem_u32(&sm.sums_full), 1);
+    mbar_init(smem_u32(&sm.sums_empty), 2 * kPairReaders);
+    mbar_init(smem_u32(&sm.spare), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kPairMmaWarp) {
+    tmem_alloc<2>(smem_u32(&sm.tmem), 512);
+    tmem_relinquish<2>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_trigger();  // not before this block has its tensor memory: the next kernel's blocks hold theirs while they wait for this one
+  pdl_wait();
+  cluster_sync();  // the barriers of both blocks are set up
+
+  const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
+  const uint32_t rank = cluster_rank(), pairs = gridDim.x / 2;
+
+  if (warp == kPairCopyWarp) {
+    if (elect_one()) {
+      uint32_t i = 0;
+      bool ok = true;
+      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
+        const uint32_t w0 = tile / p.x_tiles * kPairRows + rank * kTileW, x_tile0 = tile % p.x_tiles * kPairRows;
+        const int ws = (int)(w0 / kStrip * p.strip_rows), xs = (int)(x_tile0 / kStrip * p.strip_rows);
+        for (uint32_t step = 0; step < p.steps; ++step, ++i) {
+          const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
+          if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
+          if (i == p.withhold) continue;  // test hook: never issued
+          if (rank == 0) mbar_expect_tx(smem_u32(&sm.full[s]), 2 * S::kStage);
+          const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), 0);
+          tma_load_pair(to, &w_map, (int)(step * kRowBytes), (int)w0, bar);
+          tma_load_pair(to + S::kX, &x_map, (int)(step * kRowBytes), (int)(x_tile0 + rank * kTileW), bar);
+          tma_load_pair(to + S::kWs, &ws_map, 0, ws + (int)(step * (KT * 4)), bar);
+          for (uint32_t q = 0; q < 2; ++q)  // both blocks multiply by all 256 rows of x
+            tma_load_pair(to + S::kXs + q * (KT * kTileBytes), &xs_map, 0, xs + (int)(q * p.strip_rows + step * (KT * 4)), bar);
+        }
+      }
+      if (*abandoned && rank == 0)  // what was issued lands before the blocks' memory is another's
+        for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+          if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
+    }
+  } else if (warp == kPairMmaWarp) {
+    if (rank == 0) {
+      // e2m1 both, N = 256, M = 256, type of the scales
+      constexpr uint32_t idesc =
+          1u << 7 | 1u << 10 | (kPairRows >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | (kPairRows >> 7) << 27;
+      uint32_t i = 0, n = 0;
+      bool ok = true;
+      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
+        if (n > 0) ok = wait(smem_u32(&sm.sums_empty), (n - 1) & 1, abandoned, p.status, p.max_spins);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        for (uint32_t step = 0; step < p.steps && ok; ++step) {
+          const uint32_t s = i % STAGES, from = base + s * S::kStageAligned;
+          ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t sfa = tmem + 256 + s * S::kScaleCols, sfb = sfa + KT * 4;
+          // a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart
+#pragma unroll
+          for (uint32_t t = 0; t < KT; ++t) {
+            scales_to_tmem<2>(sfa + t * 4, operand(from + S::kWs + t * kTileBytes, 0, 128, false));
+            for (uint32_t q = 0; q < 2; ++q)
+              scales_to_tmem<2>(sfb + (t * 2 + q) * 4, operand(from + S::kXs + (q * KT + t) * kTileBytes, 0, 128, false));
+          }
+          const uint64_t a = operand(from, 16, 1024, true), b = operand(from + S::kX, 16, 1024, true);
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t t = FMT == PVT_MX_E8M0_32 ? j / 2 : j, id = FMT == PVT_MX_E8M0_32 ? (j & 1) * 2 : 0;
+            multiply<FMT, 2>(tmem, a + 2 * j, b + 2 * j, idesc | id << 4 | id << 29, sfa + t * 4, sfb + t * 8,
+                             (uint32_t)(step > 0 || j > 0));
+          }
+          commit_pair(smem_u32(&sm.empty[s]));
+          ++i;
+        }
+        if (ok) commit_pair(smem_u32(&sm.sums_full));
+      }
+      if (!ok && i > 0) {
+        commit_pair(smem_u32(&sm.spare));
+        drain(smem_u32(&sm.spare), 0);
+      }
+    }
+  } else {
+    float alpha = 1.0f;
+    if (p.w_ts) alpha = *p.w_ts;
+    if (p.x_ts) alpha *= *p.x_ts;
+    const uint32_t quarter = warp % 4, half = warp / 4;
+    const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), 0);
+    uint32_t n = 0;
+    for (uint32_t tile = blockIdx.x / 2; tile < p.tiles; tile += pairs, ++n) {
+      bool ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t v[128];
+#pragma unroll
+      for (int j = 0; j < 128; j += 32) tmem_ld32(tmem + (quarter << 21) + half * 128 + j, v + j);
+      tmem_ld_wait<128>(v);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) cluster_arrive(sums_empty);
+      // lanes are consecutive outputs of a token
+      const uint32_t col = tile / p.x_tiles * kPairRows + rank * kTileW + quarter * 32 + lane;
+      const uint32_t row = tile % p.x_tiles * kPairRows + half * 128;
+      if (col < p.w_rows && row < p.x_rows) {
+        T* y = static_cast<T*>(p.y) + (int64_t)row * p.ldy + col;
+        const uint32_t rows = p.x_rows - row;
+#pragma unroll
+        for (uint32_t j = 0; j < 128; ++j) {
+          if (j < rows) *y = narrow<T>(__uint_as_float(v[j]) * alpha);
+          y += p.ldy;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  cluster_sync();  // neither block leaves while the other's copies or products reach it
+  if (warp == kPairMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc<2>(tmem, 512);
+  }
+}
+
+template <typename T, int FMT>
+cudaError_t product_pairs(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
+  using S = PairSizes<FMT>;
+  PairParams p = {};
+  p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale, p.y = y, p.ldy = ldy, p.status = status;
+  p.w_rows = (uint32_t)w.rows, p.x_rows = (uint32_t)x.rows;
+  p.strip_rows = strip_tiles(w.cols, block_of(FMT)) * (kTileBytes / 128);
+  p.steps = (uint32_t)((w.cols + kSpan - 1) / kSpan);
+  p.x_tiles = (p.x_rows + kPairRows - 1) / kPairRows;
+  p.tiles = (p.w_rows + kPairRows - 1) / kPairRows * p.x_tiles;
+  const m1::WaitTestHook hook = m1::wait_test_hook();
+  p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
+  CUtensorMap maps[4];
+  cudaError_t e = make_map(&maps[0], w.codes, 1, (uint64_t)w.rows, (uint64_t)(w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
+  if (e == cudaSuccess) e = make_map(&maps[1], x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, kTileW);
+  if (e == cudaSuccess) e = make_map(&maps[2], w.scales, 1, scale_bytes(w.rows, w.cols, FMT) / 128, 128, 128, S::KT * 4, false);
+  if (e == cudaSuccess) e = make_map(&maps[3], x.scales, 1, scale_bytes(x.rows, x.cols, FMT) / 128, 128, 128, S::KT * 4, false);
+  if (e == cudaSuccess) e = allow_smem<mx_product_pair_kernel<T, FMT>>();
+  if (e != cudaSuccess) return e;
+  uint32_t pairs = (uint32_t)sm_count / 2;
+  if (pairs > p.tiles) pairs = p.tiles;
+  constexpr size_t smem = S::kStages * S::kStageAligned + 1024;
+  static_assert(smem + 1024 <= 227 * 1024, "a block's shared memory");
+  return launch_clusters(mx_product_pair_kernel<T, FMT>, 2 * pairs, 2, kPairThreads, smem, stream, maps[0], maps[1], maps[2], maps[3],
+                         p);
+}
+
 template <typename T, int FMT>
 cudaError_t product(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
   constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;
+  if (x.rows > 128) return product_pairs<T, FMT>(x, w, y, ldy, status, sm_count, stream);
   ProductParams p = {};
   p.w_scales = w.scales, p.x_scales = x.scales, p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale;
   p.y = y, p.ldy = ldy, p.status = status;
@@ -276,7 +503,7 @@ cudaError_t product(const pvt_mx& x, const pvt_mx& w, void* y, int64_t ldy, uint
 
 namespace mma {
 cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows, uint64_t cols, uint64_t pitch,
-                     uint32_t box_rows) {
+                     uint32_t box_rows, bool swizzled) {
   static std::atomic<void*> known{nullptr};
   void* f = known.load(std::memory_order_relaxed);
   if (!f) {
@@ -291,7 +518,7 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows
   const cuuint32_t box[2] = {(cuuint32_t)(128 / size), box_rows}, steps[2] = {1, 1};
   const CUresult r = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(f)(
       map, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
-      box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+      box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }

@@ -32,7 +32,7 @@ def held(rows, cols, fmt, seed, scales=None, tensor_scale=None, fill=0xff):
 SHAPES = [  # tokens, inputs, outputs
     (1, 1, 1), (1, 32, 16), (1, 4096, 129), (2, 257, 128), (7, 1000, 300), (16, 512, 2048), (17, 255, 127), (33, 300, 64),
     (64, 2049, 640), (65, 256, 500), (128, 768, 128), (129, 513, 257), (256, 1024, 256), (257, 640, 384), (300, 33, 1000),
-    (513, 1537, 130),
+    (513, 1537, 130), (1100, 520, 4200),
 ]
 
 
@@ -225,12 +225,13 @@ def test_captured_calls_and_another_stream():
         assert ((y.double() - now @ wv.T).abs() <= 704 * 2.0 ** -23 * (now.abs() @ wv.abs().T)).all()
 
 
+@pytest.mark.parametrize("tokens", [40, 1300])
 @pytest.mark.parametrize("what", ["product", "input", "weight"])
-def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_correct(what):
-    x, xv = held(40, 3000, B.PVT_MX_E8M0_32, 19)
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_correct(what, tokens):
+    x, xv = held(tokens, 3000, B.PVT_MX_E8M0_32, 19)
     w, wv = held(2000, 3000, B.PVT_MX_E8M0_32, 20)
-    dy = gradient(40, 2000, 23)
-    out = {"product": torch.empty(40, 2000, device="cuda"), "input": torch.empty(40, 3000, device="cuda"),
+    dy = gradient(tokens, 2000, 23)
+    out = {"product": torch.empty(tokens, 2000, device="cuda"), "input": torch.empty(tokens, 3000, device="cuda"),
            "weight": torch.empty(2000, 3000, device="cuda")}[what]
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
 
