@@ -9,10 +9,10 @@ namespace pvt {
 namespace mma {
 
 // Describes rows x cols elements of `size` bytes (1 or 2), rows pitch bytes apart, to the copy engine, in boxes of box_rows
-// rows of 128 bytes, under the 128-byte swizzle or as they lie; what lies outside reads as zero.  base and pitch: multiples
-// of 16.
+// rows of box_bytes; rows of 128 bytes lie under the 128-byte swizzle unless they are to lie as they are.  What is outside reads
+// as zero.  base and pitch: multiples of 16.
 cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows,
-                     bool swizzled = true);
+                     uint32_t box_bytes = 128, bool swizzled = true);
 
 #ifdef __CUDACC__
 using m1::bulk_g2s;
@@ -27,6 +27,26 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uin
                                      uint32_t max_spins) {
   for (uint32_t spin = 0; spin < max_spins; ++spin) {
     if (mbar_try_wait(bar, parity)) return true;
+    if (*abandoned) return false;
+    if (spin > 4096) __nanosleep(64);
+  }
+  *abandoned = 1;
+  if (status) atomicOr(status, PVT_DEV_WAIT_EXPIRED);
+  return false;
+}
+// the same for a barrier at which threads of other blocks of the cluster arrive too
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abandoned, uint32_t* status,
+                                             uint32_t max_spins) {
+  for (uint32_t spin = 0; spin < max_spins; ++spin) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
     if (*abandoned) return false;
     if (spin > 4096) __nanosleep(64);
   }

@@ -6,9 +6,9 @@
 // bfloat16 on its way into shared memory (an element times its scale is exact there, with at most six significant
 // bits) and tcgen05.mma multiplies 16-bit operands.  A step is 64 rows of Q by 256 columns, stored with the columns contiguous (128
 // bytes = 64 columns to a row, under the 128-byte swizzle: eight threads that write 16 bytes each for eight rows meet no
-// bank twice); A's tiles arrive by TMA, contiguous along r or along p as they lie.  One widened step serves two tiles
-// of 128 rows of A where there are as many, so that the tensor cores and not the widening set the pace: 16384 elements
-// at 2.75 instructions each are 350 cycles of the SM's issue slots, 16 products of 128 x 256 x 16 take 1050.
+// bank twice); A's tiles arrive by TMA, contiguous along r or along p as they lie.  Few tiles leave most SMs idle, so the
+// steps of a tile are then shared by a cluster of up to eight blocks, whose partial sums meet in shared memory across the
+// cluster, always in the order of ranks.
 #include "pvt_mma.cuh"
 #include "pvt_mx.cuh"
 
@@ -23,7 +23,7 @@ constexpr int kGThreads = kWideners + 64;
 constexpr int kCopyWarp = 8, kMmaWarp = 9;
 constexpr int kTileA = 128, kTileC = 256, kStepR = 64;
 constexpr uint32_t kABytes = kTileA * kStepR * 2, kBBytes = kTileC * kStepR * 2;
-constexpr int kMaxStages = 4;
+constexpr int kStages = 4;
 constexpr uint32_t kPartPitch = kTileC + 1;  // floats, of a row of partial sums
 
 struct GradParams {
@@ -44,9 +44,9 @@ struct GradParams {
 };
 
 struct GradShared {
-  alignas(8) uint64_t full_a[kMaxStages];
-  uint64_t full_b[kMaxStages];
-  uint64_t empty[kMaxStages];
+  alignas(8) uint64_t full_a[kStages];
+  uint64_t full_b[kStages];
+  uint64_t empty[kStages];
   uint64_t done, spare;
   uint32_t tmem, abandoned;
 };
@@ -108,11 +108,9 @@ __device__ __forceinline__ void fetch(Fetched& f, const GradParams& p, uint32_t 
   }
 }
 
-template <typename T, int FMT, bool TRANS, int MT>
+template <typename T, int FMT, bool TRANS>
 __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constant__ CUtensorMap a_map, const GradParams p) {
-  constexpr uint32_t kStageBytes = MT * kABytes + kBBytes;
-  constexpr uint32_t STAGES = MT == 2 ? 3 : 4;
-  constexpr uint32_t TMEM = MT * kTileC;
+  constexpr uint32_t kStageBytes = kABytes + kBBytes, STAGES = kStages;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ GradShared sm;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -129,7 +127,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
-    tmem_alloc(smem_u32(&sm.tmem), TMEM);
+    tmem_alloc(smem_u32(&sm.tmem), kTileC);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -142,7 +140,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
   unsigned char* const mem = raw + (base - smem_u32(raw));
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
   const uint32_t rank = blockIdx.x % p.split, tile = blockIdx.x / p.split;
-  const uint32_t a0 = tile / p.c_tiles * (MT * kTileA), c0 = tile % p.c_tiles * kTileC;
+  const uint32_t a0 = tile / p.c_tiles * kTileA, c0 = tile % p.c_tiles * kTileC;
   const uint32_t first = (uint32_t)((uint64_t)p.steps * rank / p.split), last = (uint32_t)((uint64_t)p.steps * (rank + 1) / p.split);
 
   if (warp == kCopyWarp) {
@@ -152,15 +150,12 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
         const uint32_t s = i % STAGES, bar = smem_u32(&sm.full_a[s]), to = base + s * kStageBytes;
         if (i >= STAGES && !wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins)) break;
         if (i == p.withhold) continue;  // test hook: never issued
-        mbar_expect_tx(bar, MT * kABytes);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          if (TRANS) {
-            tma_load(to + m * kABytes, &a_map, (int)(a0 + m * kTileA), (int)(step * kStepR), bar);
-            tma_load(to + m * kABytes + kABytes / 2, &a_map, (int)(a0 + m * kTileA + 64), (int)(step * kStepR), bar);
-          } else {
-            tma_load(to + m * kABytes, &a_map, (int)(step * kStepR), (int)(a0 + m * kTileA), bar);
-          }
+        mbar_expect_tx(bar, kABytes);
+        if (TRANS) {
+          tma_load(to, &a_map, (int)a0, (int)(step * kStepR), bar);
+          tma_load(to + kABytes / 2, &a_map, (int)(a0 + 64), (int)(step * kStepR), bar);
+        } else {
+          tma_load(to, &a_map, (int)(step * kStepR), (int)a0, bar);
         }
       }
       if (*abandoned)  // what was issued lands before the block's memory is another's
@@ -182,13 +177,9 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
       tc_fence_after();
 #pragma unroll
       for (uint32_t k = 0; k < kStepR / 16; ++k) {
-        const uint64_t b = operand(from + MT * kABytes + k * 2048, kBBytes / 4, 1024, true);
-#pragma unroll
-        for (uint32_t m = 0; m < (uint32_t)MT; ++m) {
-          const uint64_t a = TRANS ? operand(from + m * kABytes + k * 2048, kABytes / 2, 1024, true)
-                                   : operand(from + m * kABytes + k * 32, 16, 1024, true);
-          multiply16(tmem + m * kTileC, a, b, idesc, (uint32_t)(i > 0 || k > 0));
-        }
+        const uint64_t a = TRANS ? operand(from + k * 2048, kABytes / 2, 1024, true) : operand(from + k * 32, 16, 1024, true);
+        const uint64_t b = operand(from + kABytes + k * 2048, kBBytes / 4, 1024, true);
+        multiply16(tmem, a, b, idesc, (uint32_t)(i > 0 || k > 0));
       }
       commit(smem_u32(&sm.empty[s]));
     }
@@ -212,7 +203,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
       if (i >= STAGES) ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      unsigned char* const to = mem + s * kStageBytes + MT * kABytes + chunk / 2 * (kBBytes / 4) + row * 128;
+      unsigned char* const to = mem + s * kStageBytes + kABytes + chunk / 2 * (kBBytes / 4) + row * 128;
 #pragma unroll
       for (int it = 0; it < 2; ++it) {
         const uint32_t w[4] = {now.codes[it].x, now.codes[it].y, now.codes[it].z, now.codes[it].w};
@@ -235,14 +226,13 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
       const uint32_t quarter = warp % 4, half = warp / 4;
       if (p.split == 1) {
         // 32 rows by 32 columns at a time, turned in shared memory so that a warp stores along a row; the upper four warps
-        // have the second tile of rows, or the second half of the columns
+        // have the second half of the columns
         float* const turn = reinterpret_cast<float*>(mem) + warp * (32 * 33);
-        const uint32_t m = MT == 2 ? half : 0, row0 = a0 + m * kTileA + quarter * 32;
-        const uint32_t j_lo = MT == 2 ? 0 : half * (kTileC / 2), j_hi = MT == 2 ? kTileC : j_lo + kTileC / 2;
+        const uint32_t row0 = a0 + quarter * 32, j_lo = half * (kTileC / 2), j_hi = j_lo + kTileC / 2;
         const uint32_t n_rows = row0 < p.a_rows ? min(32u, p.a_rows - row0) : 0;
         for (uint32_t j0 = j_lo; j0 < j_hi && c0 + j0 < p.cols && n_rows; j0 += 32) {
           uint32_t v[32];
-          tmem_ld32(tmem + (quarter << 21) + m * kTileC + j0, v);
+          tmem_ld32(tmem + (quarter << 21) + j0, v);
           tmem_ld_wait<32>(v);
 #pragma unroll
           for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = __uint_as_float(v[j]);
@@ -294,19 +284,304 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();
-    tmem_dealloc(tmem, TMEM);
+    tmem_dealloc(tmem, kTileC);
   }
 }
 
-template <typename T, int FMT, bool TRANS, int MT>
-cudaError_t start(const CUtensorMap& a_map, GradParams& p, uint64_t tiles, cudaStream_t stream) {
-  constexpr size_t stages = MT == 2 ? 3 : 4, smem = stages * (MT * kABytes + kBBytes) + 1024;
+template <typename T, int FMT, bool TRANS>
+cudaError_t start(const CUtensorMap& a_map, const GradParams& p, uint64_t tiles, cudaStream_t stream) {
+  constexpr size_t smem = kStages * (kABytes + kBBytes) + 1024;
   static_assert(smem + sizeof(GradShared) + 1024 <= 227 * 1024, "a block's shared memory");
-  static_assert(MT == 2 || kTileA * kPartPitch * 4 <= stages * (MT * kABytes + kBBytes), "the partial sums fit the stages");
+  static_assert(kTileA * kPartPitch * 4 <= kStages * (kABytes + kBBytes), "the partial sums fit the stages");
   if (tiles * p.split > 0x7fffffffull) return cudaErrorInvalidConfiguration;
-  const cudaError_t e = allow_smem<mx_grad_kernel<T, FMT, TRANS, MT>>();
+  const cudaError_t e = allow_smem<mx_grad_kernel<T, FMT, TRANS>>();
   if (e != cudaSuccess) return e;
-  return launch_clusters(mx_grad_kernel<T, FMT, TRANS, MT>, (unsigned)(tiles * p.split), p.split, kGThreads, smem, stream, a_map, p);
+  return launch_clusters(mx_grad_kernel<T, FMT, TRANS>, (unsigned)(tiles * p.split), p.split, kGThreads, smem, stream, a_map, p);
+}
+
+// ---- pairs of blocks -------------------------------------------------------------------------------------------
+// Where there are tiles for all SMs a pair of blocks on neighbouring ones multiplies 256 rows of A by 256 columns of Q (tcgen05.mma
+// cta_group::2).  Each block widens half the columns, so that 64 rows cost it 8192 elements, 180 cycles of its issue
+// slots, beside products of 512 cycles; codes and scales come by TMA like A's tiles, a few steps ahead.  What a step takes from
+// codes to operands is several times that (a wait, loads, products, stores, the fence that shows them to the tensor
+// cores), so four groups of four warps take every fourth step each.  The blocks stay and take tile after tile: there are
+// two sets of sums, four warps read one out while the other is added to.
+constexpr int kPairGroups = 4, kPairGroupWarps = 4, kPairReaders = 4;  // warps
+constexpr int kPairWideners = kPairGroups * kPairGroupWarps;
+constexpr int kPairThreads = (kPairWideners + kPairReaders + 2) * 32;
+constexpr int kPairCopyWarp = kPairWideners + kPairReaders, kPairMmaWarp = kPairCopyWarp + 1;
+constexpr uint32_t kPairRows = 256, kPairHalf = 128;  // rows of A, columns of a block
+constexpr uint32_t kPairStages = 5, kPairHeld = 8;    // steps of operands, of codes and scales
+constexpr uint32_t kPairAhead = 3;                    // steps that codes are asked for ahead of A's tiles
+constexpr uint32_t kPairBBytes = kPairHalf * kStepR * 2, kPairStage = kABytes + kPairBBytes;
+constexpr uint32_t kPairCodeBytes = kPairHalf / 2 * kStepR, kPairHeldBytes = kPairCodeBytes + 1024;
+constexpr uint32_t kPairHeldAt = kPairStages * kPairStage, kPairTurnAt = kPairHeldAt + kPairHeld * kPairHeldBytes;
+constexpr uint32_t kPairTurn = kPairReaders * 32 * 33 * 4;
+
+struct PairShared {
+  alignas(8) uint64_t held[kPairHeld];     // of each block: codes and scales
+  uint64_t held_empty[kPairHeld];          // of each: an arrival per warp of the group
+  uint64_t full_a[kPairStages];            // of the first: A's tiles of both
+  uint64_t full_b[kPairStages];            // of the first: an arrival per warp of both blocks' groups
+  uint64_t empty[kPairStages];             // of each
+  uint64_t sums_full[2];                   // of each
+  uint64_t sums_empty[2];                  // of the first: an arrival per reading warp of both
+  uint64_t spare;
+  uint32_t tmem, abandoned;
+};
+
+struct PairParams {
+  const uint8_t* scales;
+  const float* ts;
+  void* out;
+  int64_t ldo;
+  uint32_t* status;
+  uint32_t a_rows, cols;
+  uint32_t strip_bytes;
+  uint32_t steps, a_tiles, tiles;
+  uint32_t accumulate;
+  uint32_t max_spins, withhold;
+};
+
+__device__ __forceinline__ void multiply16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t onto) {
+  asm volatile(
+      "{\n\t.reg .pred one, p;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "@one tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(onto)
+      : "memory");
+}
+
+template <typename T, int FMT, bool TRANS>
+__global__ void __launch_bounds__(kPairThreads, 1)
+    mx_grad_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap q_map, const PairParams p) {
+  constexpr uint32_t STAGES = kPairStages, kScaleBytes = FMT == PVT_MX_E8M0_32 ? 512 : 1024;  // of 128 rows x 128 columns
+  extern __shared__ __align__(1024) unsigned char raw[];
+  __shared__ PairShared sm;
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  volatile uint32_t* abandoned = &sm.abandoned;
+  if (tid == 0) {
+    sm.abandoned = 0;
+    for (uint32_t s = 0; s < kPairHeld; ++s) {
+      mbar_init(smem_u32(&sm.held[s]), 1);
+      mbar_init(smem_u32(&sm.held_empty[s]), kPairGroupWarps);
+    }
+    for (uint32_t s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&sm.full_a[s]), 1);
+      mbar_init(smem_u32(&sm.full_b[s]), 2 * kPairGroupWarps);
+      mbar_init(smem_u32(&sm.empty[s]), 1);
+    }
+    for (uint32_t s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&sm.sums_full[s]), 1);
+      mbar_init(smem_u32(&sm.sums_empty[s]), 2 * kPairReaders);
+    }
+    mbar_init(smem_u32(&sm.spare), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kPairMmaWarp) {
+    tmem_alloc<2>(smem_u32(&sm.tmem), 512);
+    tmem_relinquish<2>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_trigger();  // not before this block has its tensor memory: the next kernel's blocks hold theirs while they wait for this one
+  pdl_wait();
+  cluster_sync();  // the barriers of both blocks are set up
+
+  const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+  unsigned char* const mem = raw + (base - smem_u32(raw));
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
+  const uint32_t rank = cluster_rank(), pairs = gridDim.x / 2;
+
+  if (warp == kPairCopyWarp) {
+    if (elect_one()) {
+      // codes and scales of step i, kPairAhead steps before A's tile of step i
+      uint32_t held_i = 0, held_tile = blockIdx.x / 2, held_step = 0;
+      auto ask = [&]() {
+        if (held_tile >= p.tiles) return true;
+        const uint32_t s = held_i % kPairHeld, to = base + kPairHeldAt + s * kPairHeldBytes, bar = smem_u32(&sm.held[s]);
+        if (held_i >= kPairHeld && !wait(smem_u32(&sm.held_empty[s]), (held_i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))
+          return false;
+        if (held_i != p.withhold) {  // test hook: never issued
+          const uint32_t c0 = held_tile / p.a_tiles * kTileC + rank * kPairHalf, r0 = held_step * kStepR;
+          mbar_expect_tx(bar, kPairCodeBytes + kScaleBytes);
+          tma_load(to, &q_map, (int)(c0 / 2), (int)r0, bar);
+          bulk_g2s(to + kPairCodeBytes, p.scales + (size_t)(r0 / kStrip) * p.strip_bytes + (size_t)(c0 / kPairHalf) * kScaleBytes,
+                   kScaleBytes, bar);
+        }
+        ++held_i;
+        if (++held_step == p.steps) held_step = 0, held_tile += pairs;
+        return true;
+      };
+      uint32_t i = 0;
+      bool ok = true;
+      for (uint32_t n = 0; n < kPairAhead && ok; ++n) ok = ask();
+      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
+        const uint32_t a0 = tile % p.a_tiles * kPairRows + rank * kTileA;
+        for (uint32_t step = 0; step < p.steps; ++step, ++i) {
+          if (!(ok = ask())) break;
+          const uint32_t s = i % STAGES, to = base + s * kPairStage;
+          if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
+          if (rank == 0) mbar_expect_tx(smem_u32(&sm.full_a[s]), 2 * kABytes);
+          const uint32_t bar = cluster_address(smem_u32(&sm.full_a[s]), 0);
+          if (TRANS) {
+            tma_load_pair(to, &a_map, (int)a0, (int)(step * kStepR), bar);
+            tma_load_pair(to + kABytes / 2, &a_map, (int)(a0 + 64), (int)(step * kStepR), bar);
+          } else {
+            tma_load_pair(to, &a_map, (int)(step * kStepR), (int)a0, bar);
+          }
+        }
+      }
+      if (*abandoned) {  // what was issued lands before the blocks' memory is another's
+        for (uint32_t j = held_i > kPairHeld ? held_i - kPairHeld : 0; j < held_i; ++j)
+          if (j != p.withhold) drain(smem_u32(&sm.held[j % kPairHeld]), (j / kPairHeld) & 1);
+        if (rank == 0)
+          for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
+      }
+    }
+  } else if (warp == kPairMmaWarp) {
+    if (rank == 0) {
+      // binary32 sums, bfloat16 both, A contiguous along r or p, Q along c, N = 256, M = 256
+      constexpr uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | (TRANS ? 1u << 15 : 0u) | 1u << 16 |
+                                 (uint32_t)(kTileC >> 3) << 17 | (kPairRows >> 4) << 24;
+      uint32_t i = 0, n = 0;
+      bool ok = true;
+      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
+        const uint32_t set = n & 1;
+        if (n > 1) ok = wait_cluster(smem_u32(&sm.sums_empty[set]), (n / 2 - 1) & 1, abandoned, p.status, p.max_spins);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        for (uint32_t step = 0; step < p.steps && ok; ++step) {
+          const uint32_t s = i % STAGES, from = base + s * kPairStage;
+          ok = wait(smem_u32(&sm.full_a[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins) &&
+               wait_cluster(smem_u32(&sm.full_b[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (uint32_t k = 0; k < kStepR / 16; ++k) {
+            const uint64_t a = TRANS ? operand(from + k * 2048, kABytes / 2, 1024, true) : operand(from + k * 32, 16, 1024, true);
+            const uint64_t b = operand(from + kABytes + k * 2048, kPairBBytes / 2, 1024, true);
+            multiply16_pair(tmem + set * kTileC, a, b, idesc, (uint32_t)(step > 0 || k > 0));
+          }
+          commit_pair(smem_u32(&sm.empty[s]));
+          ++i;
+        }
+        if (ok) commit_pair(smem_u32(&sm.sums_full[set]));
+      }
+      if (!ok && i > 0) {
+        commit_pair(smem_u32(&sm.spare));
+        drain(smem_u32(&sm.spare), 0);
+      }
+    }
+  } else if (warp < kPairWideners) {
+    const uint32_t group = warp / kPairGroupWarps, in_group = tid % (kPairGroupWarps * 32);
+    const uint32_t row = in_group / 4, chunk = in_group % 4, atom = chunk / 2;  // 32 columns of two of the 64 rows, 32 apart
+    uint64_t left = 0;  // steps of all this block's tiles
+    if (blockIdx.x / 2 < p.tiles) left = (uint64_t)((p.tiles - blockIdx.x / 2 + pairs - 1) / pairs) * p.steps;
+    uint32_t step = group % p.steps;
+    for (uint64_t i64 = group; i64 < left; i64 += kPairGroups) {
+      const uint32_t i = (uint32_t)i64, hs = i % kPairHeld, s = i % STAGES;
+      const unsigned char* const held = mem + kPairHeldAt + hs * kPairHeldBytes;
+      bool ok = wait(smem_u32(&sm.held[hs]), (i / kPairHeld) & 1, abandoned, p.status, p.max_spins);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      uint4 codes[2];
+      uint32_t scales[2];
+#pragma unroll
+      for (int it = 0; it < 2; ++it) {
+        codes[it] = *reinterpret_cast<const uint4*>(held + (in_group + it * 128) * 16);
+        const uint32_t r = (step * kStepR + row + it * 32) % kStrip, at = kPairCodeBytes + r % 32 * 16 + r / 32 * 4;
+        scales[it] = FMT == PVT_MX_E8M0_32 ? held[at + chunk] : *reinterpret_cast<const uint16_t*>(held + at + atom * 512 + (chunk & 1) * 2);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.held_empty[hs]));
+      if (i >= STAGES) ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      unsigned char* const to = mem + s * kPairStage + kABytes + atom * (kPairBBytes / 2) + row * 128;
+#pragma unroll
+      for (int it = 0; it < 2; ++it) {
+        const __nv_bfloat162 s0 = scale16<FMT>(FMT == PVT_MX_E8M0_32 ? scales[it] : scales[it] & 255u);
+        const __nv_bfloat162 s1 = FMT == PVT_MX_E8M0_32 ? s0 : scale16<FMT>(scales[it] >> 8);
+        const uint4 c = codes[it];
+        // (the second 64 columns in another order: the 16 bytes that eight threads write together meet no bank twice)
+        const uint32_t w[4] = {atom ? c.y : c.x, atom ? c.x : c.y, atom ? c.w : c.z, atom ? c.z : c.w};
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q)
+          *reinterpret_cast<uint4*>(to + it * (32 * 128) + ((((chunk & 1) * 4 + (q ^ atom)) ^ (row & 7)) << 4)) =
+              widen8(w[q], q < 2 ? s0 : s1);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the products
+      __syncwarp();
+      if (lane == 0) cluster_arrive(cluster_address(smem_u32(&sm.full_b[s]), 0));
+      step = (step + kPairGroups) % p.steps;
+    }
+  } else {
+    const float alpha = p.ts ? *p.ts : 1.0f;
+    const uint32_t quarter = warp % 4;
+    float* const turn = reinterpret_cast<float*>(mem + kPairTurnAt) + quarter * (32 * 33);
+    uint32_t n = 0;
+    for (uint32_t tile = blockIdx.x / 2; tile < p.tiles; tile += pairs, ++n) {
+      const uint32_t set = n & 1;
+      bool ok = wait(smem_u32(&sm.sums_full[set]), (n / 2) & 1, abandoned, p.status, p.max_spins);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t row0 = tile % p.a_tiles * kPairRows + rank * kTileA + quarter * 32, c0 = tile / p.a_tiles * kTileC;
+      const uint32_t n_rows = row0 < p.a_rows ? min(32u, p.a_rows - row0) : 0;
+      // 32 rows by 32 columns at a time, turned in shared memory so that a warp stores along a row
+      for (uint32_t j0 = 0; j0 < kTileC && c0 + j0 < p.cols && n_rows; j0 += 32) {
+        uint32_t v[32];
+        tmem_ld32(tmem + (quarter << 21) + set * kTileC + j0, v);
+        tmem_ld_wait<32>(v);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = __uint_as_float(v[j]);
+        __syncwarp();
+        const uint32_t col = c0 + j0 + lane;
+        if (col < p.cols) {
+          T* out = static_cast<T*>(p.out) + (int64_t)row0 * p.ldo + col;
+          if (sizeof(T) == 4 && p.accumulate) {
+#pragma unroll 8
+            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(widen<T>(out[(int64_t)r * p.ldo]) + turn[r * 33 + lane] * alpha);
+          } else {
+#pragma unroll 8
+            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(turn[r * 33 + lane] * alpha);
+          }
+        }
+        __syncwarp();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) cluster_arrive(cluster_address(smem_u32(&sm.sums_empty[set]), 0));
+    }
+  }
+  __syncthreads();
+  cluster_sync();  // neither block leaves while the other's copies, arrivals or products reach it
+  if (warp == kPairMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc<2>(tmem, 512);
+  }
+}
+
+template <typename T, int FMT, bool TRANS>
+cudaError_t start_pairs(const CUtensorMap& a_map, const GradParams& g, const pvt_mx& q, int sm_count, cudaStream_t stream) {
+  PairParams p = {};
+  p.scales = g.scales, p.ts = g.ts, p.out = g.out, p.ldo = g.ldo, p.status = g.status;
+  p.a_rows = g.a_rows, p.cols = g.cols, p.accumulate = g.accumulate, p.max_spins = g.max_spins, p.withhold = g.withhold;
+  p.strip_bytes = g.tiles * kTileBytes, p.steps = g.steps;
+  p.a_tiles = (g.a_rows + kPairRows - 1) / kPairRows, p.tiles = p.a_tiles * g.c_tiles;
+  CUtensorMap q_map;
+  cudaError_t e = make_map(&q_map, q.codes, 1, (uint64_t)q.rows, (uint64_t)(q.cols + 1) / 2, (uint64_t)q.ld, kStepR, kPairHalf / 2, false);
+  if (e == cudaSuccess) e = allow_smem<mx_grad_pair_kernel<T, FMT, TRANS>>();
+  if (e != cudaSuccess) return e;
+  uint32_t pairs = (uint32_t)sm_count / 2;
+  if (pairs > p.tiles) pairs = p.tiles;
+  constexpr size_t smem = kPairTurnAt + kPairTurn + 1024;
+  static_assert(smem + 1024 <= 227 * 1024 && kPairStage % 1024 == 0 && kPairHeldBytes % 128 == 0, "a block's shared memory");
+  return launch_clusters(mx_grad_pair_kernel<T, FMT, TRANS>, 2 * pairs, 2, kPairThreads, smem, stream, a_map, q_map, p);
 }
 
 template <typename T, int FMT, bool TRANS>
@@ -325,12 +600,12 @@ cudaError_t grad(const void* dy, int64_t lddy, uint32_t a_rows, const pvt_mx& q,
   CUtensorMap a_map;
   const cudaError_t e = make_map(&a_map, dy, 2, tokens, features, (uint64_t)lddy * 2, TRANS ? kStepR : kTileA);
   if (e != cudaSuccess) return e;
-  const uint64_t two = (uint64_t)((a_rows + 2 * kTileA - 1) / (2 * kTileA)) * p.c_tiles;
   p.split = 1;
-  if (two >= (uint64_t)sm_count) return start<T, FMT, TRANS, 2>(a_map, p, two, stream);
+  const uint64_t pair_tiles = (uint64_t)((a_rows + kPairRows - 1) / kPairRows) * p.c_tiles;
+  if (a_rows > (uint32_t)kTileA && pair_tiles >= (uint64_t)sm_count / 4) return start_pairs<T, FMT, TRANS>(a_map, p, q, sm_count, stream);
   const uint64_t one = (uint64_t)((a_rows + kTileA - 1) / kTileA) * p.c_tiles;
   while (p.split < 8 && one * p.split * 2 <= (uint64_t)sm_count && p.split * 2 <= p.steps) p.split *= 2;
-  return start<T, FMT, TRANS, 1>(a_map, p, one, stream);
+  return start<T, FMT, TRANS>(a_map, p, one, stream);
 }
 
 }  // namespace

@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       uint32_t i = 0, n = 0;
       bool ok = true;
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
-        if (n > 0) ok = wait(smem_u32(&sm.sums_empty), (n - 1) & 1, abandoned, p.status, p.max_spins);
+        if (n > 0) ok = wait_cluster(smem_u32(&sm.sums_empty), (n - 1) & 1, abandoned, p.status, p.max_spins);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         for (uint32_t step = 0; step < p.steps && ok; ++step) {
@@ -440,8 +440,8 @@ cudaError_t product_pairs(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, u
   CUtensorMap maps[4];
   cudaError_t e = make_map(&maps[0], w.codes, 1, (uint64_t)w.rows, (uint64_t)(w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
   if (e == cudaSuccess) e = make_map(&maps[1], x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, kTileW);
-  if (e == cudaSuccess) e = make_map(&maps[2], w.scales, 1, scale_bytes(w.rows, w.cols, FMT) / 128, 128, 128, S::KT * 4, false);
-  if (e == cudaSuccess) e = make_map(&maps[3], x.scales, 1, scale_bytes(x.rows, x.cols, FMT) / 128, 128, 128, S::KT * 4, false);
+  if (e == cudaSuccess) e = make_map(&maps[2], w.scales, 1, scale_bytes(w.rows, w.cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
+  if (e == cudaSuccess) e = make_map(&maps[3], x.scales, 1, scale_bytes(x.rows, x.cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
   if (e == cudaSuccess) e = allow_smem<mx_product_pair_kernel<T, FMT>>();
   if (e != cudaSuccess) return e;
   uint32_t pairs = (uint32_t)sm_count / 2;
@@ -503,7 +503,7 @@ cudaError_t product(const pvt_mx& x, const pvt_mx& w, void* y, int64_t ldy, uint
 
 namespace mma {
 cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows, uint64_t cols, uint64_t pitch,
-                     uint32_t box_rows, bool swizzled) {
+                     uint32_t box_rows, uint32_t box_bytes, bool swizzled) {
   static std::atomic<void*> known{nullptr};
   void* f = known.load(std::memory_order_relaxed);
   if (!f) {
@@ -515,7 +515,7 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows
   }
   const cuuint64_t dims[2] = {cols, rows};
   const cuuint64_t strides[1] = {pitch};
-  const cuuint32_t box[2] = {(cuuint32_t)(128 / size), box_rows}, steps[2] = {1, 1};
+  const cuuint32_t box[2] = {(cuuint32_t)(box_bytes / size), box_rows}, steps[2] = {1, 1};
   const CUresult r = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(f)(
       map, size == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
       box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
