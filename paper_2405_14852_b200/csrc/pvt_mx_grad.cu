@@ -62,11 +62,18 @@ __device__ __forceinline__ void multiply16(uint32_t d, uint64_t a, uint64_t b, u
 }
 
 // Eight elements times their scale, as bfloat16.  The three bits of a magnitude become the low two exponent bits and the
-// first fraction bit of a bfloat16, whose bias is 126 more, the sign goes to the top: one product with 2^126 gives the
-// element, 0.5 (a number without its leading one) included, a second the value.
-__device__ __forceinline__ uint4 widen8(uint32_t w, __nv_bfloat162 scale) {
+// first fraction bit of a bfloat16, whose bias is 126 more, the sign goes to the top; one product with 2^126 times the scale
+// gives the value, that of 0.5 (a number without its leading one) included.  Where 2^126 times the scale is
+// beyond bfloat16 it takes two products (e8m0, scales above 2), or the value is 2^-8 of itself and the sums are
+// multiplied by 2^8 (e4m3, always: kWidened).
+template <bool TWICE>
+__device__ __forceinline__ uint4 widen8(uint32_t w, uint32_t factor) {
   const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
   const uint32_t big = 0x7e807e80u;  // 2^126 twice
+  auto times = [](uint32_t a, uint32_t b) {
+    const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+  };
   uint32_t out[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -74,18 +81,42 @@ __device__ __forceinline__ uint4 widen8(uint32_t w, __nv_bfloat162 scale) {
     uint32_t pair;
     asm("prmt.b32 %0, %1, %2, %3;" : "=r"(pair) : "r"(even), "r"(odd), "r"(0xc480 + 0x1111 * i));
     const uint32_t bits = (pair * 0x1040u) & 0x81c081c0u;  // shifted by 6 and by 12
-    const __nv_bfloat162 el = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&bits), *reinterpret_cast<const __nv_bfloat162*>(&big));
-    const __nv_bfloat162 v = __hmul2(el, scale);
-    out[i] = *reinterpret_cast<const uint32_t*>(&v);
+    out[i] = TWICE ? times(times(bits, big), factor) : times(bits, factor);
   }
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
 template <int FMT>
-__device__ __forceinline__ __nv_bfloat162 scale16(uint32_t byte) {
-  if (FMT == PVT_MX_E4M3_16) return __float2bfloat162_rn(e4m3_value(byte));
-  const uint32_t b = byte == 255 ? 0x7fc0u : byte ? byte << 7 : 0x0040u, two = b | b << 16;
-  return *reinterpret_cast<const __nv_bfloat162*>(&two);
+constexpr float kWidened = FMT == PVT_MX_E4M3_16 ? 256.0f : 1.0f;
+template <int FMT>
+__device__ __forceinline__ bool takes_two(uint32_t byte) { return FMT == PVT_MX_E8M0_32 && byte > 128; }
+// the (second) factor of a scale byte, twice
+template <int FMT>
+__device__ __forceinline__ uint32_t factor_of(uint32_t byte, bool twice) {
+  uint32_t b;
+  if (FMT == PVT_MX_E4M3_16)
+    b = __float_as_uint(e4m3_value(byte) * 3.32306998946229e35f) >> 16;  // 2^118: at most five significant bits
+  else if (twice)
+    b = byte == 255 ? 0x7fc0u : byte ? byte << 7 : 0x0040u;
+  else
+    b = (byte + 126) << 7;  // 2^126 2^(byte - 127)
+  return b | b << 16;
+}
+
+// 32 elements of a row: 16 bytes of codes and one or two scale bytes, to four pieces of 16 bytes, `put`'s
+template <int FMT, typename Put>
+__device__ __forceinline__ void widen32(const uint4& codes, uint32_t scales, Put put) {
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+  const uint32_t b0 = FMT == PVT_MX_E8M0_32 ? scales : scales & 255u, b1 = FMT == PVT_MX_E8M0_32 ? scales : scales >> 8;
+  if (FMT == PVT_MX_E8M0_32 && __any_sync(0xffffffffu, takes_two<FMT>(b0))) {
+    const uint32_t f = factor_of<FMT>(b0, true);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put(q, widen8<true>(w[q], f));
+  } else {
+    const uint32_t f0 = factor_of<FMT>(b0, false), f1 = FMT == PVT_MX_E8M0_32 ? f0 : factor_of<FMT>(b1, false);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put(q, widen8<false>(w[q], q < 2 ? f0 : f1));
+  }
 }
 
 // What a thread fetches of a step: 32 columns of two rows.
@@ -206,12 +237,9 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
       unsigned char* const to = mem + s * kStageBytes + kABytes + chunk / 2 * (kBBytes / 4) + row * 128;
 #pragma unroll
       for (int it = 0; it < 2; ++it) {
-        const uint32_t w[4] = {now.codes[it].x, now.codes[it].y, now.codes[it].z, now.codes[it].w};
-        const __nv_bfloat162 s0 = scale16<FMT>(FMT == PVT_MX_E8M0_32 ? now.scales[it] : now.scales[it] & 255u);
-        const __nv_bfloat162 s1 = FMT == PVT_MX_E8M0_32 ? s0 : scale16<FMT>(now.scales[it] >> 8);
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q)
-          *reinterpret_cast<uint4*>(to + it * (32 * 128) + ((((chunk & 1) * 4 + q) ^ in_row) << 4)) = widen8(w[q], q < 2 ? s0 : s1);
+        widen32<FMT>(now.codes[it], now.scales[it], [&](uint32_t q, uint4 v) {
+          *reinterpret_cast<uint4*>(to + it * (32 * 128) + ((((chunk & 1) * 4 + q) ^ in_row) << 4)) = v;
+        });
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the products
       __syncwarp();
@@ -222,7 +250,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
     if (ok) {
-      const float alpha = p.ts ? *p.ts : 1.0f;
+      const float alpha = kWidened<FMT> * (p.ts ? *p.ts : 1.0f);
       const uint32_t quarter = warp % 4, half = warp / 4;
       if (p.split == 1) {
         // 32 rows by 32 columns at a time, turned in shared memory so that a warp stores along a row; the upper four warps
@@ -267,7 +295,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
     cluster_sync();
     // every block adds up the rows that are its share, always in the order of ranks
     if (warp < kWideners / 32 && !*abandoned) {
-      const float alpha = p.ts ? *p.ts : 1.0f;
+      const float alpha = kWidened<FMT> * (p.ts ? *p.ts : 1.0f);
       for (uint32_t r = rank + warp * p.split; r < kTileA && a0 + r < p.a_rows; r += kWideners / 32 * p.split) {
         T* out = static_cast<T*>(p.out) + (int64_t)(a0 + r) * p.ldo + c0;
         for (uint32_t j = lane; j < kTileC && c0 + j < p.cols; j += 32) {
@@ -300,23 +328,36 @@ cudaError_t start(const CUtensorMap& a_map, const GradParams& p, uint64_t tiles,
 }
 
 // ---- pairs of blocks -------------------------------------------------------------------------------------------
-// Where there are tiles for all SMs a pair of blocks on neighbouring ones multiplies 256 rows of A by 256 columns of Q (tcgen05.mma
-// cta_group::2).  Each block widens half the columns, so that 64 rows cost it 8192 elements, 180 cycles of its issue
-// slots, beside products of 512 cycles; codes and scales come by TMA like A's tiles, a few steps ahead.  What a step takes from
-// codes to operands is several times that (a wait, loads, products, stores, the fence that shows them to the tensor
-// cores), so four groups of four warps take every fourth step each.  The blocks stay and take tile after tile: there are
-// two sets of sums, four warps read one out while the other is added to.
+// Where there are tiles for all SMs a pair of blocks on neighbouring ones multiplies 512 rows of A by 128 columns of Q (two of
+// tcgen05.mma cta_group::2 with M = 256; where A has no more rows than that, 256 by 256).  Each block widens half the columns:
+// 64 rows cost it 4096 elements, about 100 cycles of its issue slots, beside products of 512 cycles; with 256 x 256 it
+// is twice that, and the warps that widen set the pace (2048 x 4096 by 11008: both gradients 414 us).  Codes and scales
+// come by TMA like A's tiles, a few steps ahead.  What a step takes from codes to operands is several times its share
+// (a wait, loads, products, stores, the fence that shows them to the tensor cores), so four groups of four warps take
+// every fourth step each.  The blocks stay and take tile after tile: there are two sets of sums, four warps read one
+// out while the other is added to.
 constexpr int kPairGroups = 4, kPairGroupWarps = 4, kPairReaders = 4;  // warps
 constexpr int kPairWideners = kPairGroups * kPairGroupWarps;
 constexpr int kPairThreads = (kPairWideners + kPairReaders + 2) * 32;
 constexpr int kPairCopyWarp = kPairWideners + kPairReaders, kPairMmaWarp = kPairCopyWarp + 1;
-constexpr uint32_t kPairRows = 256, kPairHalf = 128;  // rows of A, columns of a block
-constexpr uint32_t kPairStages = 5, kPairHeld = 8;    // steps of operands, of codes and scales
+constexpr uint32_t kPairStages = 5, kPairHeld = 8;    // steps of operands (at most), of codes and scales
 constexpr uint32_t kPairAhead = 3;                    // steps that codes are asked for ahead of A's tiles
-constexpr uint32_t kPairBBytes = kPairHalf * kStepR * 2, kPairStage = kABytes + kPairBBytes;
-constexpr uint32_t kPairCodeBytes = kPairHalf / 2 * kStepR, kPairHeldBytes = kPairCodeBytes + 1024;
-constexpr uint32_t kPairHeldAt = kPairStages * kPairStage, kPairTurnAt = kPairHeldAt + kPairHeld * kPairHeldBytes;
-constexpr uint32_t kPairTurn = kPairReaders * 32 * 33 * 4;
+constexpr uint32_t kPairSums = 256;                   // columns of tensor memory of a set
+
+// MT: products of 256 rows per step
+template <int FMT, int MT>
+struct PairSizes {
+  static constexpr uint32_t kRows = 256 * MT, kCols = 256 / MT, kHalf = kCols / 2;  // of a tile, columns of a block
+  static constexpr uint32_t kBBytes = kHalf * kStepR * 2, kStage = MT * kABytes + kBBytes, kStages = MT == 2 ? 4 : 5;
+  static constexpr uint32_t kCodeBytes = kHalf / 2 * kStepR;
+  // scale tiles of 128 rows: those of kHalf columns, or the one they are half of
+  static constexpr uint32_t kScaleCols = FMT == PVT_MX_E8M0_32 ? 128 : 64;
+  static constexpr uint32_t kScaleBytes = (kHalf > kScaleCols ? kHalf / kScaleCols : 1) * kTileBytes;
+  static constexpr uint32_t kHeldBytes = kCodeBytes + kScaleBytes;
+  static constexpr uint32_t kHeldAt = kStages * kStage, kTurnAt = kHeldAt + kPairHeld * kHeldBytes;
+  static constexpr size_t kBytes = kTurnAt + kPairReaders * 32 * 33 * 4 + 1024;
+  static_assert(kBytes + 1024 <= 227 * 1024 && kStage % 1024 == 0 && kHeldBytes % 128 == 0, "a block's shared memory");
+};
 
 struct PairShared {
   alignas(8) uint64_t held[kPairHeld];     // of each block: codes and scales
@@ -353,10 +394,11 @@ __device__ __forceinline__ void multiply16_pair(uint32_t d, uint64_t a, uint64_t
       : "memory");
 }
 
-template <typename T, int FMT, bool TRANS>
+template <typename T, int FMT, bool TRANS, int MT>
 __global__ void __launch_bounds__(kPairThreads, 1)
     mx_grad_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap q_map, const PairParams p) {
-  constexpr uint32_t STAGES = kPairStages, kScaleBytes = FMT == PVT_MX_E8M0_32 ? 512 : 1024;  // of 128 rows x 128 columns
+  using S = PairSizes<FMT, MT>;
+  constexpr uint32_t STAGES = S::kStages;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ PairShared sm;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -401,15 +443,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       uint32_t held_i = 0, held_tile = blockIdx.x / 2, held_step = 0;
       auto ask = [&]() {
         if (held_tile >= p.tiles) return true;
-        const uint32_t s = held_i % kPairHeld, to = base + kPairHeldAt + s * kPairHeldBytes, bar = smem_u32(&sm.held[s]);
+        const uint32_t s = held_i % kPairHeld, to = base + S::kHeldAt + s * S::kHeldBytes, bar = smem_u32(&sm.held[s]);
         if (held_i >= kPairHeld && !wait(smem_u32(&sm.held_empty[s]), (held_i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))
           return false;
         if (held_i != p.withhold) {  // test hook: never issued
-          const uint32_t c0 = held_tile / p.a_tiles * kTileC + rank * kPairHalf, r0 = held_step * kStepR;
-          mbar_expect_tx(bar, kPairCodeBytes + kScaleBytes);
+          const uint32_t c0 = held_tile / p.a_tiles * S::kCols + rank * S::kHalf, r0 = held_step * kStepR;
+          mbar_expect_tx(bar, S::kHeldBytes);
           tma_load(to, &q_map, (int)(c0 / 2), (int)r0, bar);
-          bulk_g2s(to + kPairCodeBytes, p.scales + (size_t)(r0 / kStrip) * p.strip_bytes + (size_t)(c0 / kPairHalf) * kScaleBytes,
-                   kScaleBytes, bar);
+          bulk_g2s(to + S::kCodeBytes, p.scales + (size_t)(r0 / kStrip) * p.strip_bytes + (size_t)(c0 / S::kScaleCols) * kTileBytes,
+                   S::kScaleBytes, bar);
         }
         ++held_i;
         if (++held_step == p.steps) held_step = 0, held_tile += pairs;
@@ -419,18 +461,21 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       bool ok = true;
       for (uint32_t n = 0; n < kPairAhead && ok; ++n) ok = ask();
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
-        const uint32_t a0 = tile % p.a_tiles * kPairRows + rank * kTileA;
+        const uint32_t a0 = tile % p.a_tiles * S::kRows + rank * kTileA;
         for (uint32_t step = 0; step < p.steps; ++step, ++i) {
           if (!(ok = ask())) break;
-          const uint32_t s = i % STAGES, to = base + s * kPairStage;
+          const uint32_t s = i % STAGES, to = base + s * S::kStage;
           if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
-          if (rank == 0) mbar_expect_tx(smem_u32(&sm.full_a[s]), 2 * kABytes);
+          if (rank == 0) mbar_expect_tx(smem_u32(&sm.full_a[s]), 2 * MT * kABytes);
           const uint32_t bar = cluster_address(smem_u32(&sm.full_a[s]), 0);
-          if (TRANS) {
-            tma_load_pair(to, &a_map, (int)a0, (int)(step * kStepR), bar);
-            tma_load_pair(to + kABytes / 2, &a_map, (int)(a0 + 64), (int)(step * kStepR), bar);
-          } else {
-            tma_load_pair(to, &a_map, (int)(step * kStepR), (int)a0, bar);
+#pragma unroll
+          for (uint32_t m = 0; m < (uint32_t)MT; ++m) {
+            if (TRANS) {
+              tma_load_pair(to + m * kABytes, &a_map, (int)(a0 + m * 256), (int)(step * kStepR), bar);
+              tma_load_pair(to + m * kABytes + kABytes / 2, &a_map, (int)(a0 + m * 256 + 64), (int)(step * kStepR), bar);
+            } else {
+              tma_load_pair(to + m * kABytes, &a_map, (int)(step * kStepR), (int)(a0 + m * 256), bar);
+            }
           }
         }
       }
@@ -443,9 +488,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     }
   } else if (warp == kPairMmaWarp) {
     if (rank == 0) {
-      // binary32 sums, bfloat16 both, A contiguous along r or p, Q along c, N = 256, M = 256
+      // binary32 sums, bfloat16 both, A contiguous along r or p, Q along c, N, M = 256
       constexpr uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | (TRANS ? 1u << 15 : 0u) | 1u << 16 |
-                                 (uint32_t)(kTileC >> 3) << 17 | (kPairRows >> 4) << 24;
+                                 (S::kCols >> 3) << 17 | (256u >> 4) << 24;
       uint32_t i = 0, n = 0;
       bool ok = true;
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
@@ -454,7 +499,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         for (uint32_t step = 0; step < p.steps && ok; ++step) {
-          const uint32_t s = i % STAGES, from = base + s * kPairStage;
+          const uint32_t s = i % STAGES, from = base + s * S::kStage;
           ok = wait(smem_u32(&sm.full_a[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins) &&
                wait_cluster(smem_u32(&sm.full_b[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
           ok = __all_sync(0xffffffffu, ok);
@@ -462,9 +507,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           tc_fence_after();
 #pragma unroll
           for (uint32_t k = 0; k < kStepR / 16; ++k) {
-            const uint64_t a = TRANS ? operand(from + k * 2048, kABytes / 2, 1024, true) : operand(from + k * 32, 16, 1024, true);
-            const uint64_t b = operand(from + kABytes + k * 2048, kPairBBytes / 2, 1024, true);
-            multiply16_pair(tmem + set * kTileC, a, b, idesc, (uint32_t)(step > 0 || k > 0));
+            const uint64_t b = operand(from + MT * kABytes + k * 2048, 8192, 1024, true);
+#pragma unroll
+            for (uint32_t m = 0; m < (uint32_t)MT; ++m) {
+              const uint64_t a = TRANS ? operand(from + m * kABytes + k * 2048, kABytes / 2, 1024, true)
+                                       : operand(from + m * kABytes + k * 32, 16, 1024, true);
+              multiply16_pair(tmem + set * kPairSums + m * S::kCols, a, b, idesc, (uint32_t)(step > 0 || k > 0));
+            }
           }
           commit_pair(smem_u32(&sm.empty[s]));
           ++i;
@@ -478,51 +527,50 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     }
   } else if (warp < kPairWideners) {
     const uint32_t group = warp / kPairGroupWarps, in_group = tid % (kPairGroupWarps * 32);
-    const uint32_t row = in_group / 4, chunk = in_group % 4, atom = chunk / 2;  // 32 columns of two of the 64 rows, 32 apart
+    // 32 columns of one or two of the 64 rows, 32 apart
+    constexpr uint32_t kChunks = S::kHalf / 32, kItems = kStepR * kChunks / (kPairGroupWarps * 32);
+    const uint32_t row = in_group / kChunks, chunk = in_group % kChunks, atom = chunk / 2;
     uint64_t left = 0;  // steps of all this block's tiles
     if (blockIdx.x / 2 < p.tiles) left = (uint64_t)((p.tiles - blockIdx.x / 2 + pairs - 1) / pairs) * p.steps;
     uint32_t step = group % p.steps;
     for (uint64_t i64 = group; i64 < left; i64 += kPairGroups) {
       const uint32_t i = (uint32_t)i64, hs = i % kPairHeld, s = i % STAGES;
-      const unsigned char* const held = mem + kPairHeldAt + hs * kPairHeldBytes;
+      const unsigned char* const held = mem + S::kHeldAt + hs * S::kHeldBytes;
       bool ok = wait(smem_u32(&sm.held[hs]), (i / kPairHeld) & 1, abandoned, p.status, p.max_spins);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      uint4 codes[2];
-      uint32_t scales[2];
+      uint4 codes[kItems];
+      uint32_t scales[kItems];
 #pragma unroll
-      for (int it = 0; it < 2; ++it) {
-        codes[it] = *reinterpret_cast<const uint4*>(held + (in_group + it * 128) * 16);
-        const uint32_t r = (step * kStepR + row + it * 32) % kStrip, at = kPairCodeBytes + r % 32 * 16 + r / 32 * 4;
-        scales[it] = FMT == PVT_MX_E8M0_32 ? held[at + chunk] : *reinterpret_cast<const uint16_t*>(held + at + atom * 512 + (chunk & 1) * 2);
+      for (uint32_t it = 0; it < kItems; ++it) {
+        codes[it] = *reinterpret_cast<const uint4*>(held + (in_group + it * (kPairGroupWarps * 32)) * 16);
+        const uint32_t r = (step * kStepR + row + it * 32) % kStrip, at = S::kCodeBytes + r % 32 * 16 + r / 32 * 4;
+        // (of 64 columns every other block has the upper half of a tile of four e8m0 scales)
+        if (FMT == PVT_MX_E8M0_32)
+          scales[it] = held[at + (MT == 2 ? rank * 2 : 0) + chunk];
+        else
+          scales[it] = *reinterpret_cast<const uint16_t*>(held + at + atom * kTileBytes + (chunk & 1) * 2);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.held_empty[hs]));
       if (i >= STAGES) ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      unsigned char* const to = mem + s * kPairStage + kABytes + atom * (kPairBBytes / 2) + row * 128;
+      unsigned char* const to = mem + s * S::kStage + MT * kABytes + atom * 8192 + row * 128;
 #pragma unroll
-      for (int it = 0; it < 2; ++it) {
-        const __nv_bfloat162 s0 = scale16<FMT>(FMT == PVT_MX_E8M0_32 ? scales[it] : scales[it] & 255u);
-        const __nv_bfloat162 s1 = FMT == PVT_MX_E8M0_32 ? s0 : scale16<FMT>(scales[it] >> 8);
-        const uint4 c = codes[it];
-        // (the second 64 columns in another order: the 16 bytes that eight threads write together meet no bank twice)
-        const uint32_t w[4] = {atom ? c.y : c.x, atom ? c.x : c.y, atom ? c.w : c.z, atom ? c.z : c.w};
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q)
-          *reinterpret_cast<uint4*>(to + it * (32 * 128) + ((((chunk & 1) * 4 + (q ^ atom)) ^ (row & 7)) << 4)) =
-              widen8(w[q], q < 2 ? s0 : s1);
-      }
+      for (uint32_t it = 0; it < kItems; ++it)
+        widen32<FMT>(codes[it], scales[it], [&](uint32_t q, uint4 v) {
+          *reinterpret_cast<uint4*>(to + it * (32 * 128) + ((((chunk & 1) * 4 + q) ^ (row & 7)) << 4)) = v;
+        });
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the products
       __syncwarp();
       if (lane == 0) cluster_arrive(cluster_address(smem_u32(&sm.full_b[s]), 0));
       step = (step + kPairGroups) % p.steps;
     }
   } else {
-    const float alpha = p.ts ? *p.ts : 1.0f;
+    const float alpha = kWidened<FMT> * (p.ts ? *p.ts : 1.0f);
     const uint32_t quarter = warp % 4;
-    float* const turn = reinterpret_cast<float*>(mem + kPairTurnAt) + quarter * (32 * 33);
+    float* const turn = reinterpret_cast<float*>(mem + S::kTurnAt) + quarter * (32 * 33);
     uint32_t n = 0;
     for (uint32_t tile = blockIdx.x / 2; tile < p.tiles; tile += pairs, ++n) {
       const uint32_t set = n & 1;
@@ -530,17 +578,19 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t row0 = tile % p.a_tiles * kPairRows + rank * kTileA + quarter * 32, c0 = tile / p.a_tiles * kTileC;
-      const uint32_t n_rows = row0 < p.a_rows ? min(32u, p.a_rows - row0) : 0;
+      const uint32_t c0 = tile / p.a_tiles * S::kCols;
       // 32 rows by 32 columns at a time, turned in shared memory so that a warp stores along a row
-      for (uint32_t j0 = 0; j0 < kTileC && c0 + j0 < p.cols && n_rows; j0 += 32) {
+      for (uint32_t j0 = 0; j0 < kPairSums; j0 += 32) {
+        const uint32_t row0 = tile % p.a_tiles * S::kRows + j0 / S::kCols * 256 + rank * kTileA + quarter * 32, col0 = c0 + j0 % S::kCols;
+        if (row0 >= p.a_rows || col0 >= p.cols) continue;
+        const uint32_t n_rows = min(32u, p.a_rows - row0);
         uint32_t v[32];
-        tmem_ld32(tmem + (quarter << 21) + set * kTileC + j0, v);
+        tmem_ld32(tmem + (quarter << 21) + set * kPairSums + j0, v);
         tmem_ld_wait<32>(v);
 #pragma unroll
         for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = __uint_as_float(v[j]);
         __syncwarp();
-        const uint32_t col = c0 + j0 + lane;
+        const uint32_t col = col0 + lane;
         if (col < p.cols) {
           T* out = static_cast<T*>(p.out) + (int64_t)row0 * p.ldo + col;
           if (sizeof(T) == 4 && p.accumulate) {
@@ -566,22 +616,21 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   }
 }
 
-template <typename T, int FMT, bool TRANS>
+template <typename T, int FMT, bool TRANS, int MT>
 cudaError_t start_pairs(const CUtensorMap& a_map, const GradParams& g, const pvt_mx& q, int sm_count, cudaStream_t stream) {
+  using S = PairSizes<FMT, MT>;
   PairParams p = {};
   p.scales = g.scales, p.ts = g.ts, p.out = g.out, p.ldo = g.ldo, p.status = g.status;
   p.a_rows = g.a_rows, p.cols = g.cols, p.accumulate = g.accumulate, p.max_spins = g.max_spins, p.withhold = g.withhold;
   p.strip_bytes = g.tiles * kTileBytes, p.steps = g.steps;
-  p.a_tiles = (g.a_rows + kPairRows - 1) / kPairRows, p.tiles = p.a_tiles * g.c_tiles;
+  p.a_tiles = (g.a_rows + S::kRows - 1) / S::kRows, p.tiles = p.a_tiles * ((g.cols + S::kCols - 1) / S::kCols);
   CUtensorMap q_map;
-  cudaError_t e = make_map(&q_map, q.codes, 1, (uint64_t)q.rows, (uint64_t)(q.cols + 1) / 2, (uint64_t)q.ld, kStepR, kPairHalf / 2, false);
-  if (e == cudaSuccess) e = allow_smem<mx_grad_pair_kernel<T, FMT, TRANS>>();
+  cudaError_t e = make_map(&q_map, q.codes, 1, (uint64_t)q.rows, (uint64_t)(q.cols + 1) / 2, (uint64_t)q.ld, kStepR, S::kHalf / 2, false);
+  if (e == cudaSuccess) e = allow_smem<mx_grad_pair_kernel<T, FMT, TRANS, MT>>();
   if (e != cudaSuccess) return e;
   uint32_t pairs = (uint32_t)sm_count / 2;
   if (pairs > p.tiles) pairs = p.tiles;
-  constexpr size_t smem = kPairTurnAt + kPairTurn + 1024;
-  static_assert(smem + 1024 <= 227 * 1024 && kPairStage % 1024 == 0 && kPairHeldBytes % 128 == 0, "a block's shared memory");
-  return launch_clusters(mx_grad_pair_kernel<T, FMT, TRANS>, 2 * pairs, 2, kPairThreads, smem, stream, a_map, q_map, p);
+  return launch_clusters(mx_grad_pair_kernel<T, FMT, TRANS, MT>, 2 * pairs, 2, kPairThreads, S::kBytes, stream, a_map, q_map, p);
 }
 
 template <typename T, int FMT, bool TRANS>
@@ -601,8 +650,10 @@ cudaError_t grad(const void* dy, int64_t lddy, uint32_t a_rows, const pvt_mx& q,
   const cudaError_t e = make_map(&a_map, dy, 2, tokens, features, (uint64_t)lddy * 2, TRANS ? kStepR : kTileA);
   if (e != cudaSuccess) return e;
   p.split = 1;
-  const uint64_t pair_tiles = (uint64_t)((a_rows + kPairRows - 1) / kPairRows) * p.c_tiles;
-  if (a_rows > (uint32_t)kTileA && pair_tiles >= (uint64_t)sm_count / 4) return start_pairs<T, FMT, TRANS>(a_map, p, q, sm_count, stream);
+  const uint64_t pair_tiles = (uint64_t)((a_rows + 255) / 256) * p.c_tiles;
+  if (a_rows > (uint32_t)kTileA && pair_tiles >= (uint64_t)sm_count / 4)
+    return a_rows > 256 ? start_pairs<T, FMT, TRANS, 2>(a_map, p, q, sm_count, stream)
+                        : start_pairs<T, FMT, TRANS, 1>(a_map, p, q, sm_count, stream);
   const uint64_t one = (uint64_t)((a_rows + kTileA - 1) / kTileA) * p.c_tiles;
   while (p.split < 8 && one * p.split * 2 <= (uint64_t)sm_count && p.split * 2 <= p.steps) p.split *= 2;
   return start<T, FMT, TRANS>(a_map, p, one, stream);
