@@ -27,7 +27,7 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uin
                                      uint32_t max_spins) {
   for (uint32_t spin = 0; spin < max_spins; ++spin) {
     if (mbar_try_wait(bar, parity)) return true;
-    if (*abandoned) return false;
+    if (spin % 16 == 15 && *abandoned) return false;  // (every look costs the others' loads and stores a place in the queue)
     if (spin > 4096) __nanosleep(64);
   }
   *abandoned = 1;
@@ -47,7 +47,7 @@ __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, vola
         : "r"(bar), "r"(parity)
         : "memory");
     if (ok) return true;
-    if (*abandoned) return false;
+    if (spin % 16 == 15 && *abandoned) return false;
     if (spin > 4096) __nanosleep(64);
   }
   *abandoned = 1;
@@ -180,8 +180,12 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t saddr, uint32_t ran
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(saddr), "r"(rank));
   return at;
 }
+// Arrives at a barrier of any block of the cluster.  What it stands for is this block's own: shared memory that the tensor core
+// beside it reads once the other block says so (shown to it by a fence of its proxy before this), or tensor memory that
+// has been read.  No thread of the other block reads what this one wrote, so there is nothing to release to
+// it; .release.cluster would wait for everything the thread has in flight, 2000 cycles.
 __device__ __forceinline__ void cluster_arrive(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ float cluster_load(uint32_t saddr, uint32_t rank) {
   const uint32_t at = cluster_address(saddr, rank);

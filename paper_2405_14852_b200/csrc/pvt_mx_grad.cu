@@ -338,10 +338,11 @@ cudaError_t start(const CUtensorMap& a_map, const GradParams& p, uint64_t tiles,
 // out while the other is added to.
 constexpr int kPairGroups = 4, kPairGroupWarps = 4, kPairReaders = 4;  // warps
 constexpr int kPairWideners = kPairGroups * kPairGroupWarps;
-constexpr int kPairThreads = (kPairWideners + kPairReaders + 2) * 32;
-constexpr int kPairCopyWarp = kPairWideners + kPairReaders, kPairMmaWarp = kPairCopyWarp + 1;
+// (beside that many other warps one that copies takes 100 cycles and more for each instruction it issues: codes and A's tiles
+// have one each, or two)
+constexpr int kPairHeldWarp = kPairWideners + kPairReaders, kPairCopyWarp = kPairHeldWarp + 1, kPairMmaWarp = kPairCopyWarp + 2;
+constexpr int kPairThreads = (kPairMmaWarp + 1) * 32;
 constexpr uint32_t kPairStages = 5, kPairHeld = 8;    // steps of operands (at most), of codes and scales
-constexpr uint32_t kPairAhead = 3;                    // steps that codes are asked for ahead of A's tiles
 constexpr uint32_t kPairSums = 256;                   // columns of tensor memory of a set
 
 // MT: products of 256 rows per step
@@ -437,54 +438,49 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
   const uint32_t rank = cluster_rank(), pairs = gridDim.x / 2;
 
-  if (warp == kPairCopyWarp) {
+  if (warp == kPairHeldWarp) {
     if (elect_one()) {
-      // codes and scales of step i, kPairAhead steps before A's tile of step i
-      uint32_t held_i = 0, held_tile = blockIdx.x / 2, held_step = 0;
-      auto ask = [&]() {
-        if (held_tile >= p.tiles) return true;
-        const uint32_t s = held_i % kPairHeld, to = base + S::kHeldAt + s * S::kHeldBytes, bar = smem_u32(&sm.held[s]);
-        if (held_i >= kPairHeld && !wait(smem_u32(&sm.held_empty[s]), (held_i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))
-          return false;
-        if (held_i != p.withhold) {  // test hook: never issued
-          const uint32_t c0 = held_tile / p.a_tiles * S::kCols + rank * S::kHalf, r0 = held_step * kStepR;
-          mbar_expect_tx(bar, S::kHeldBytes);
-          tma_load(to, &q_map, (int)(c0 / 2), (int)r0, bar);
-          bulk_g2s(to + S::kCodeBytes, p.scales + (size_t)(r0 / kStrip) * p.strip_bytes + (size_t)(c0 / S::kScaleCols) * kTileBytes,
-                   S::kScaleBytes, bar);
-        }
-        ++held_i;
-        if (++held_step == p.steps) held_step = 0, held_tile += pairs;
-        return true;
-      };
       uint32_t i = 0;
       bool ok = true;
-      for (uint32_t n = 0; n < kPairAhead && ok; ++n) ok = ask();
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
-        const uint32_t a0 = tile % p.a_tiles * S::kRows + rank * kTileA;
+        const uint32_t c0 = tile / p.a_tiles * S::kCols + rank * S::kHalf;
+        const uint8_t* const scales = p.scales + (size_t)(c0 / S::kScaleCols) * kTileBytes;
         for (uint32_t step = 0; step < p.steps; ++step, ++i) {
-          if (!(ok = ask())) break;
-          const uint32_t s = i % STAGES, to = base + s * S::kStage;
+          const uint32_t s = i % kPairHeld, to = base + S::kHeldAt + s * S::kHeldBytes, bar = smem_u32(&sm.held[s]);
+          if (i >= kPairHeld && !(ok = wait(smem_u32(&sm.held_empty[s]), (i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))) break;
+          if (i == p.withhold) continue;  // test hook: never issued
+          mbar_expect_tx(bar, S::kHeldBytes);
+          tma_load(to, &q_map, (int)(c0 / 2), (int)(step * kStepR), bar);
+          bulk_g2s(to + S::kCodeBytes, scales + (size_t)(step * kStepR / kStrip) * p.strip_bytes, S::kScaleBytes, bar);
+        }
+      }
+      if (*abandoned)  // what was issued lands before the block's memory is another's
+        for (uint32_t j = i > kPairHeld ? i - kPairHeld : 0; j < i; ++j)
+          if (j != p.withhold) drain(smem_u32(&sm.held[j % kPairHeld]), (j / kPairHeld) & 1);
+    }
+  } else if (warp >= kPairCopyWarp && warp < kPairCopyWarp + 2) {
+    // the second of two tiles of A has a warp of its own; where there is one, the first warp has it
+    const uint32_t m = warp - kPairCopyWarp;
+    if (m < (uint32_t)MT && elect_one()) {
+      uint32_t i = 0;
+      bool ok = true;
+      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
+        const int a0 = (int)(tile % p.a_tiles * S::kRows + rank * kTileA + m * 256);
+        for (uint32_t step = 0; step < p.steps; ++step, ++i) {
+          const uint32_t s = i % STAGES, to = base + s * S::kStage + m * kABytes;
           if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
-          if (rank == 0) mbar_expect_tx(smem_u32(&sm.full_a[s]), 2 * MT * kABytes);
+          if (rank == 0 && m == 0) mbar_expect_tx(smem_u32(&sm.full_a[s]), 2 * MT * kABytes);
           const uint32_t bar = cluster_address(smem_u32(&sm.full_a[s]), 0);
-#pragma unroll
-          for (uint32_t m = 0; m < (uint32_t)MT; ++m) {
-            if (TRANS) {
-              tma_load_pair(to + m * kABytes, &a_map, (int)(a0 + m * 256), (int)(step * kStepR), bar);
-              tma_load_pair(to + m * kABytes + kABytes / 2, &a_map, (int)(a0 + m * 256 + 64), (int)(step * kStepR), bar);
-            } else {
-              tma_load_pair(to + m * kABytes, &a_map, (int)(step * kStepR), (int)(a0 + m * 256), bar);
-            }
+          if (TRANS) {
+            tma_load_pair(to, &a_map, a0, (int)(step * kStepR), bar);
+            tma_load_pair(to + kABytes / 2, &a_map, a0 + 64, (int)(step * kStepR), bar);
+          } else {
+            tma_load_pair(to, &a_map, (int)(step * kStepR), a0, bar);
           }
         }
       }
-      if (*abandoned) {  // what was issued lands before the blocks' memory is another's
-        for (uint32_t j = held_i > kPairHeld ? held_i - kPairHeld : 0; j < held_i; ++j)
-          if (j != p.withhold) drain(smem_u32(&sm.held[j % kPairHeld]), (j / kPairHeld) & 1);
-        if (rank == 0)
-          for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
-      }
+      if (*abandoned && rank == 0)  // (the last of them is in before this block's barrier completes)
+        for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
     }
   } else if (warp == kPairMmaWarp) {
     if (rank == 0) {
@@ -551,8 +547,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         else
           scales[it] = *reinterpret_cast<const uint16_t*>(held + at + atom * kTileBytes + (chunk & 1) * 2);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sm.held_empty[hs]));
       if (i >= STAGES) ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -564,7 +558,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         });
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the products
       __syncwarp();
-      if (lane == 0) cluster_arrive(cluster_address(smem_u32(&sm.full_b[s]), 0));
+      if (lane == 0) {
+        cluster_arrive(cluster_address(smem_u32(&sm.full_b[s]), 0));
+        // (only now: the stores above have taken the codes out of registers that their loads have filled)
+        mbar_arrive(smem_u32(&sm.held_empty[hs]));
+      }
       step = (step + kPairGroups) % p.steps;
     }
   } else {

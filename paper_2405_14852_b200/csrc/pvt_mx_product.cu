@@ -245,8 +245,9 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
 // blocks stay and take tile after tile; copies for the next one are under way while eight warps empty the sums into
 // registers, and those are stored while it is multiplied.
 constexpr int kPairReaders = 8;  // warps
-constexpr int kPairThreads = (kPairReaders + 2) * 32;
-constexpr int kPairCopyWarp = kPairReaders, kPairMmaWarp = kPairReaders + 1;
+constexpr int kPairCopyWarps = 2;  // (a warp takes 100 cycles and more for each copy it issues)
+constexpr int kPairCopyWarp = kPairReaders, kPairMmaWarp = kPairCopyWarp + kPairCopyWarps;
+constexpr int kPairThreads = (kPairMmaWarp + 1) * 32;
 constexpr uint32_t kPairRows = 256;   // of w and of x
 constexpr uint32_t kPairStages = 5;
 
@@ -318,24 +319,30 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
   const uint32_t rank = cluster_rank(), pairs = gridDim.x / 2;
 
-  if (warp == kPairCopyWarp) {
+  if (warp >= kPairCopyWarp && warp < kPairMmaWarp) {
+    const bool of_w = warp == kPairCopyWarp;  // one warp for w's codes and scales, one for x's
     if (elect_one()) {
       uint32_t i = 0;
       bool ok = true;
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
-        const uint32_t w0 = tile / p.x_tiles * kPairRows + rank * kTileW, x_tile0 = tile % p.x_tiles * kPairRows;
-        const int ws = (int)(w0 / kStrip * p.strip_rows), xs = (int)(x_tile0 / kStrip * p.strip_rows);
+        const uint32_t tile0 = of_w ? tile / p.x_tiles * kPairRows : tile % p.x_tiles * kPairRows;
+        const int row = (int)(tile0 + rank * kTileW);
+        const int strip = (int)((of_w ? (uint32_t)row : tile0) / kStrip * p.strip_rows);
         for (uint32_t step = 0; step < p.steps; ++step, ++i) {
           const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
           if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
           if (i == p.withhold) continue;  // test hook: never issued
-          if (rank == 0) mbar_expect_tx(smem_u32(&sm.full[s]), 2 * S::kStage);
           const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), 0);
-          tma_load_pair(to, &w_map, (int)(step * kRowBytes), (int)w0, bar);
-          tma_load_pair(to + S::kX, &x_map, (int)(step * kRowBytes), (int)(x_tile0 + rank * kTileW), bar);
-          tma_load_pair(to + S::kWs, &ws_map, 0, ws + (int)(step * (KT * 4)), bar);
-          for (uint32_t q = 0; q < 2; ++q)  // both blocks multiply by all 256 rows of x
-            tma_load_pair(to + S::kXs + q * (KT * kTileBytes), &xs_map, 0, xs + (int)(q * p.strip_rows + step * (KT * 4)), bar);
+          const int col = (int)(step * kRowBytes), scales = strip + (int)(step * (KT * 4));
+          if (of_w) {
+            if (rank == 0) mbar_expect_tx(smem_u32(&sm.full[s]), 2 * S::kStage);
+            tma_load_pair(to, &w_map, col, row, bar);
+            tma_load_pair(to + S::kWs, &ws_map, 0, scales, bar);
+          } else {  // both blocks multiply by all 256 rows of x
+            tma_load_pair(to + S::kX, &x_map, col, row, bar);
+            tma_load_pair(to + S::kXs, &xs_map, 0, scales, bar);
+            tma_load_pair(to + S::kXs + KT * kTileBytes, &xs_map, 0, scales + (int)p.strip_rows, bar);
+          }
         }
       }
       if (*abandoned && rank == 0)  // what was issued lands before the blocks' memory is another's
