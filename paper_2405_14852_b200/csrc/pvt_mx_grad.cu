@@ -309,6 +309,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
     }
     cluster_sync();
   }
+  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();
@@ -604,8 +605,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) cluster_arrive(cluster_address(smem_u32(&sm.sums_empty[set]), 0));
+      __syncwarp();
     }
   }
+  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   cluster_sync();  // neither block leaves while the other's copies, arrivals or products reach it
   if (warp == kPairMmaWarp) {

@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
     }
     cluster_sync();
   }
+  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();
@@ -410,6 +411,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) cluster_arrive(sums_empty);
+      __syncwarp();
       // lanes are consecutive outputs of a token
       const uint32_t col = tile / p.x_tiles * kPairRows + rank * kTileW + quarter * 32 + lane;
       const uint32_t row = tile % p.x_tiles * kPairRows + half * 128;
@@ -424,6 +426,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       }
     }
   }
+  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   cluster_sync();  // neither block leaves while the other's copies or products reach it
   if (warp == kPairMmaWarp) {
