@@ -15,9 +15,7 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int size, uint64_t rows
                      uint32_t box_bytes = 128, bool swizzled = true);
 
 #ifdef __CUDACC__
-using m1::bulk_g2s;
 using m1::mbar_arrive;
-using m1::mbar_expect_tx;
 using m1::mbar_init;
 using m1::mbar_try_wait;
 using m1::smem_u32;
@@ -34,7 +32,12 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uin
   if (status) atomicOr(status, PVT_DEV_WAIT_EXPIRED);
   return false;
 }
-// the same for a barrier at which threads of other blocks of the cluster arrive too
+// wait() of a whole warp, with one answer
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abandoned, uint32_t* status,
+                                          uint32_t max_spins) {
+  return __all_sync(0xffffffffu, wait(bar, parity, abandoned, status, max_spins));
+}
+// wait() for a barrier at which threads of other blocks of the cluster arrive too
 __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abandoned, uint32_t* status,
                                              uint32_t max_spins) {
   for (uint32_t spin = 0; spin < max_spins; ++spin) {
@@ -60,25 +63,44 @@ __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
     if (mbar_try_wait(bar, parity)) return;
 }
 
+// What issues copies is called by a whole warp and elects the thread that does inside the statement, so that the warp stays
+// together: these instructions take their operands from registers that its threads share.
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n\t.reg .pred one;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "@one mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+      "r"(bytes)
+      : "memory");
+}
+// `bytes` as they lie (a multiple of 16, from and to 16-byte boundaries)
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred one;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "@one cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}" ::"r"(dst),
+      "l"(src), "r"(bytes), "r"(bar)
+      : "memory");
+}
 // One box at column x (elements; x * size is a multiple of 16 bytes) and row y.
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "{\n\t.reg .pred one;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "@one cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}" ::"r"(
+          dst),
       "l"(map), "r"(x), "r"(y), "r"(bar)
       : "memory");
 }
 // The same in a pair of blocks that multiply together: the arrival may be at a barrier of either (an address of the cluster's).
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t cluster_bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(
-          dst),
+      "{\n\t.reg .pred one;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "@one cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], "
+      "[%4];\n\t}" ::"r"(dst),
       "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
       : "memory");
-}
-__device__ __forceinline__ bool elect_one() {
-  uint32_t one;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-  return one != 0;
 }
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }

@@ -175,24 +175,22 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
   const uint32_t first = (uint32_t)((uint64_t)p.steps * rank / p.split), last = (uint32_t)((uint64_t)p.steps * (rank + 1) / p.split);
 
   if (warp == kCopyWarp) {
-    if (elect_one()) {
-      uint32_t i = 0;
-      for (uint32_t step = first; step < last; ++step, ++i) {
-        const uint32_t s = i % STAGES, bar = smem_u32(&sm.full_a[s]), to = base + s * kStageBytes;
-        if (i >= STAGES && !wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins)) break;
-        if (i == p.withhold) continue;  // test hook: never issued
-        mbar_expect_tx(bar, kABytes);
-        if (TRANS) {
-          tma_load(to, &a_map, (int)a0, (int)(step * kStepR), bar);
-          tma_load(to + kABytes / 2, &a_map, (int)(a0 + 64), (int)(step * kStepR), bar);
-        } else {
-          tma_load(to, &a_map, (int)(step * kStepR), (int)a0, bar);
-        }
+    uint32_t i = 0;
+    for (uint32_t step = first; step < last; ++step, ++i) {
+      const uint32_t s = i % STAGES, bar = smem_u32(&sm.full_a[s]), to = base + s * kStageBytes;
+      if (i >= STAGES && !warp_wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins)) break;
+      if (i == p.withhold) continue;  // test hook: never issued
+      expect_bytes(bar, kABytes);
+      if (TRANS) {
+        tma_load(to, &a_map, (int)a0, (int)(step * kStepR), bar);
+        tma_load(to + kABytes / 2, &a_map, (int)(a0 + 64), (int)(step * kStepR), bar);
+      } else {
+        tma_load(to, &a_map, (int)(step * kStepR), (int)a0, bar);
       }
-      if (*abandoned)  // what was issued lands before the block's memory is another's
-        for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
-          if (j != p.withhold) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
     }
+    if (__any_sync(0xffffffffu, *abandoned))  // what was issued lands before the block's memory is another's
+      for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+        if (j != p.withhold) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
   } else if (warp == kMmaWarp) {
     // binary32 sums, bfloat16 both, A contiguous along r or p, Q along c, N = 256, M = 128
     const uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | (TRANS ? 1u << 15 : 0u) | 1u << 16 | (uint32_t)(kTileC >> 3) << 17 |
@@ -309,7 +307,6 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
     }
     cluster_sync();
   }
-  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();
@@ -440,37 +437,35 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const uint32_t rank = cluster_rank(), pairs = gridDim.x / 2;
 
   if (warp == kPairHeldWarp) {
-    if (elect_one()) {
-      uint32_t i = 0;
-      bool ok = true;
-      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
-        const uint32_t c0 = tile / p.a_tiles * S::kCols + rank * S::kHalf;
-        const uint8_t* const scales = p.scales + (size_t)(c0 / S::kScaleCols) * kTileBytes;
-        for (uint32_t step = 0; step < p.steps; ++step, ++i) {
-          const uint32_t s = i % kPairHeld, to = base + S::kHeldAt + s * S::kHeldBytes, bar = smem_u32(&sm.held[s]);
-          if (i >= kPairHeld && !(ok = wait(smem_u32(&sm.held_empty[s]), (i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))) break;
-          if (i == p.withhold) continue;  // test hook: never issued
-          mbar_expect_tx(bar, S::kHeldBytes);
-          tma_load(to, &q_map, (int)(c0 / 2), (int)(step * kStepR), bar);
-          bulk_g2s(to + S::kCodeBytes, scales + (size_t)(step * kStepR / kStrip) * p.strip_bytes, S::kScaleBytes, bar);
-        }
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
+      const uint32_t c0 = tile / p.a_tiles * S::kCols + rank * S::kHalf;
+      const uint8_t* const scales = p.scales + (size_t)(c0 / S::kScaleCols) * kTileBytes;
+      for (uint32_t step = 0; step < p.steps; ++step, ++i) {
+        const uint32_t s = i % kPairHeld, to = base + S::kHeldAt + s * S::kHeldBytes, bar = smem_u32(&sm.held[s]);
+        if (i >= kPairHeld && !(ok = warp_wait(smem_u32(&sm.held_empty[s]), (i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))) break;
+        if (i == p.withhold) continue;  // test hook: never issued
+        expect_bytes(bar, S::kHeldBytes);
+        tma_load(to, &q_map, (int)(c0 / 2), (int)(step * kStepR), bar);
+        bulk_load(to + S::kCodeBytes, scales + (size_t)(step * kStepR / kStrip) * p.strip_bytes, S::kScaleBytes, bar);
       }
-      if (*abandoned)  // what was issued lands before the block's memory is another's
-        for (uint32_t j = i > kPairHeld ? i - kPairHeld : 0; j < i; ++j)
-          if (j != p.withhold) drain(smem_u32(&sm.held[j % kPairHeld]), (j / kPairHeld) & 1);
     }
+    if (__any_sync(0xffffffffu, *abandoned))  // what was issued lands before the block's memory is another's
+      for (uint32_t j = i > kPairHeld ? i - kPairHeld : 0; j < i; ++j)
+        if (j != p.withhold) drain(smem_u32(&sm.held[j % kPairHeld]), (j / kPairHeld) & 1);
   } else if (warp >= kPairCopyWarp && warp < kPairCopyWarp + 2) {
     // the second of two tiles of A has a warp of its own; where there is one, the first warp has it
     const uint32_t m = warp - kPairCopyWarp;
-    if (m < (uint32_t)MT && elect_one()) {
+    if (m < (uint32_t)MT) {
       uint32_t i = 0;
       bool ok = true;
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
         const int a0 = (int)(tile % p.a_tiles * S::kRows + rank * kTileA + m * 256);
         for (uint32_t step = 0; step < p.steps; ++step, ++i) {
           const uint32_t s = i % STAGES, to = base + s * S::kStage + m * kABytes;
-          if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
-          if (rank == 0 && m == 0) mbar_expect_tx(smem_u32(&sm.full_a[s]), 2 * MT * kABytes);
+          if (i >= STAGES && !(ok = warp_wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
+          if (rank == 0 && m == 0) expect_bytes(smem_u32(&sm.full_a[s]), 2 * MT * kABytes);
           const uint32_t bar = cluster_address(smem_u32(&sm.full_a[s]), 0);
           if (TRANS) {
             tma_load_pair(to, &a_map, a0, (int)(step * kStepR), bar);
@@ -480,7 +475,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           }
         }
       }
-      if (*abandoned && rank == 0)  // (the last of them is in before this block's barrier completes)
+      if (__any_sync(0xffffffffu, *abandoned) && rank == 0)  // (the last of them is in before this block's barrier completes)
         for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
     }
   } else if (warp == kPairMmaWarp) {
@@ -608,7 +603,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       __syncwarp();
     }
   }
-  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   cluster_sync();  // neither block leaves while the other's copies, arrivals or products reach it
   if (warp == kPairMmaWarp) {

@@ -129,27 +129,25 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
   const uint32_t x_at = kTileW * kRowBytes, ws_at = x_at + p.tile_x * kRowBytes, xs_at = ws_at + KT * kTileBytes;
 
   if (warp == kCopyWarp) {
-    if (elect_one()) {
-      const uint32_t bytes = (kTileW + p.tile_x) * kRowBytes + (1 + x_strips) * KT * kTileBytes;
-      const uint8_t* ws = p.w_scales + (size_t)(w0 / kStrip) * p.strip_bytes;
-      const uint8_t* xs = p.x_scales + (size_t)(x0 / kStrip) * p.strip_bytes;
-      uint32_t i = 0;
-      for (uint32_t step = first; step < last; ++step, ++i) {
-        const uint32_t s = i % p.stages, bar = smem_u32(&sm.full[s]), to = base + s * p.stage_bytes;
-        if (i >= p.stages && !wait(smem_u32(&sm.empty[s]), (i / p.stages - 1) & 1, abandoned, p.status, p.max_spins)) break;
-        if (i == p.withhold) continue;  // test hook: never issued
-        mbar_expect_tx(bar, bytes);
-        tma_load(to, &w_map, (int)(step * kRowBytes), (int)w0, bar);
-        tma_load(to + x_at, &x_map, (int)(step * kRowBytes), (int)x0, bar);
-        bulk_g2s(to + ws_at, ws + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
-        for (uint32_t q = 0; q < x_strips; ++q)
-          bulk_g2s(to + xs_at + q * (KT * kTileBytes), xs + (size_t)q * p.strip_bytes + (size_t)step * (KT * kTileBytes),
-                   KT * kTileBytes, bar);
-      }
-      if (*abandoned)  // what was issued lands before the block's memory is another's
-        for (uint32_t j = i > p.stages ? i - p.stages : 0; j < i; ++j)
-          if (j != p.withhold) drain(smem_u32(&sm.full[j % p.stages]), (j / p.stages) & 1);
+    const uint32_t bytes = (kTileW + p.tile_x) * kRowBytes + (1 + x_strips) * KT * kTileBytes;
+    const uint8_t* ws = p.w_scales + (size_t)(w0 / kStrip) * p.strip_bytes;
+    const uint8_t* xs = p.x_scales + (size_t)(x0 / kStrip) * p.strip_bytes;
+    uint32_t i = 0;
+    for (uint32_t step = first; step < last; ++step, ++i) {
+      const uint32_t s = i % p.stages, bar = smem_u32(&sm.full[s]), to = base + s * p.stage_bytes;
+      if (i >= p.stages && !warp_wait(smem_u32(&sm.empty[s]), (i / p.stages - 1) & 1, abandoned, p.status, p.max_spins)) break;
+      if (i == p.withhold) continue;  // test hook: never issued
+      expect_bytes(bar, bytes);
+      tma_load(to, &w_map, (int)(step * kRowBytes), (int)w0, bar);
+      tma_load(to + x_at, &x_map, (int)(step * kRowBytes), (int)x0, bar);
+      bulk_load(to + ws_at, ws + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
+      for (uint32_t q = 0; q < x_strips; ++q)
+        bulk_load(to + xs_at + q * (KT * kTileBytes), xs + (size_t)q * p.strip_bytes + (size_t)step * (KT * kTileBytes),
+                 KT * kTileBytes, bar);
     }
+    if (__any_sync(0xffffffffu, *abandoned))  // what was issued lands before the block's memory is another's
+      for (uint32_t j = i > p.stages ? i - p.stages : 0; j < i; ++j)
+        if (j != p.withhold) drain(smem_u32(&sm.full[j % p.stages]), (j / p.stages) & 1);
   } else if (warp == kMmaWarp) {
     const uint32_t d_cols = max(p.tile_x, 32u);
     // e2m1 both, N, M = 128, type of the scales
@@ -231,7 +229,6 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
     }
     cluster_sync();
   }
-  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();
@@ -322,34 +319,32 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 
   if (warp >= kPairCopyWarp && warp < kPairMmaWarp) {
     const bool of_w = warp == kPairCopyWarp;  // one warp for w's codes and scales, one for x's
-    if (elect_one()) {
-      uint32_t i = 0;
-      bool ok = true;
-      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
-        const uint32_t tile0 = of_w ? tile / p.x_tiles * kPairRows : tile % p.x_tiles * kPairRows;
-        const int row = (int)(tile0 + rank * kTileW);
-        const int strip = (int)((of_w ? (uint32_t)row : tile0) / kStrip * p.strip_rows);
-        for (uint32_t step = 0; step < p.steps; ++step, ++i) {
-          const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
-          if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
-          if (i == p.withhold) continue;  // test hook: never issued
-          const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), 0);
-          const int col = (int)(step * kRowBytes), scales = strip + (int)(step * (KT * 4));
-          if (of_w) {
-            if (rank == 0) mbar_expect_tx(smem_u32(&sm.full[s]), 2 * S::kStage);
-            tma_load_pair(to, &w_map, col, row, bar);
-            tma_load_pair(to + S::kWs, &ws_map, 0, scales, bar);
-          } else {  // both blocks multiply by all 256 rows of x
-            tma_load_pair(to + S::kX, &x_map, col, row, bar);
-            tma_load_pair(to + S::kXs, &xs_map, 0, scales, bar);
-            tma_load_pair(to + S::kXs + KT * kTileBytes, &xs_map, 0, scales + (int)p.strip_rows, bar);
-          }
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
+      const uint32_t tile0 = of_w ? tile / p.x_tiles * kPairRows : tile % p.x_tiles * kPairRows;
+      const int row = (int)(tile0 + rank * kTileW);
+      const int strip = (int)((of_w ? (uint32_t)row : tile0) / kStrip * p.strip_rows);
+      for (uint32_t step = 0; step < p.steps; ++step, ++i) {
+        const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
+        if (i >= STAGES && !(ok = warp_wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
+        if (i == p.withhold) continue;  // test hook: never issued
+        const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), 0);
+        const int col = (int)(step * kRowBytes), scales = strip + (int)(step * (KT * 4));
+        if (of_w) {
+          if (rank == 0) expect_bytes(smem_u32(&sm.full[s]), 2 * S::kStage);
+          tma_load_pair(to, &w_map, col, row, bar);
+          tma_load_pair(to + S::kWs, &ws_map, 0, scales, bar);
+        } else {  // both blocks multiply by all 256 rows of x
+          tma_load_pair(to + S::kX, &x_map, col, row, bar);
+          tma_load_pair(to + S::kXs, &xs_map, 0, scales, bar);
+          tma_load_pair(to + S::kXs + KT * kTileBytes, &xs_map, 0, scales + (int)p.strip_rows, bar);
         }
       }
-      if (*abandoned && rank == 0)  // what was issued lands before the blocks' memory is another's
-        for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
-          if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
     }
+    if (__any_sync(0xffffffffu, *abandoned) && rank == 0)  // what was issued lands before the blocks' memory is another's
+      for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+        if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
   } else if (warp == kPairMmaWarp) {
     if (rank == 0) {
       // e2m1 both, N = 256, M = 256, type of the scales
@@ -426,7 +421,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       }
     }
   }
-  __syncwarp();  // (what follows is for whole warps; one thread of some has been at work by itself)
   __syncthreads();
   cluster_sync();  // neither block leaves while the other's copies or products reach it
   if (warp == kPairMmaWarp) {
