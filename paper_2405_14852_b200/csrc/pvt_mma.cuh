@@ -20,47 +20,39 @@ using m1::mbar_init;
 using m1::mbar_try_wait;
 using m1::smem_u32;
 
-// Gives up after max_spins polls, or once another thread of the block has: the block is then abandoned.
+// A whole warp waits, and all of it has one answer.  Gives up after max_spins polls, or once another warp of the block has: the
+// block is then abandoned.  CLUSTER: threads of other blocks of the cluster arrive there too.  (One thread that polls for
+// its warp takes longer to bring it along than 32 that poll: both gradients of 2048 x 4096 by 11008 in 593 us, not 370.)
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* abandoned, uint32_t* status,
                                      uint32_t max_spins) {
   for (uint32_t spin = 0; spin < max_spins; ++spin) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (spin % 16 == 15 && *abandoned) return false;  // (every look costs the others' loads and stores a place in the queue)
+    uint32_t done;
+    if (CLUSTER)
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(done)
+          : "r"(bar), "r"(parity)
+          : "memory");
+    else
+      done = mbar_try_wait(bar, parity);
+    if (__all_sync(0xffffffffu, done)) return true;
+    if (spin % 16 == 15 && __any_sync(0xffffffffu, *abandoned)) return false;
     if (spin > 4096) __nanosleep(64);
   }
-  *abandoned = 1;
-  if (status) atomicOr(status, PVT_DEV_WAIT_EXPIRED);
-  return false;
-}
-// wait() of a whole warp, with one answer
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abandoned, uint32_t* status,
-                                          uint32_t max_spins) {
-  return __all_sync(0xffffffffu, wait(bar, parity, abandoned, status, max_spins));
-}
-// wait() for a barrier at which threads of other blocks of the cluster arrive too
-__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abandoned, uint32_t* status,
-                                             uint32_t max_spins) {
-  for (uint32_t spin = 0; spin < max_spins; ++spin) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    if (ok) return true;
-    if (spin % 16 == 15 && *abandoned) return false;
-    if (spin > 4096) __nanosleep(64);
+  if ((threadIdx.x & 31) == 0) {
+    *abandoned = 1;
+    if (status) atomicOr(status, PVT_DEV_WAIT_EXPIRED);
   }
-  *abandoned = 1;
-  if (status) atomicOr(status, PVT_DEV_WAIT_EXPIRED);
+  __syncwarp();
   return false;
 }
 // For what has been issued and does complete: copies and products in flight when a block is abandoned.
 __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
   for (uint32_t spin = 0; spin < m1::kMaxSpins; ++spin)
-    if (mbar_try_wait(bar, parity)) return;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
 }
 
 // What issues copies is called by a whole warp and elects the thread that does inside the statement, so that the warp stays

@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
     uint32_t i = 0;
     for (uint32_t step = first; step < last; ++step, ++i) {
       const uint32_t s = i % STAGES, bar = smem_u32(&sm.full_a[s]), to = base + s * kStageBytes;
-      if (i >= STAGES && !warp_wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins)) break;
+      if (i >= STAGES && !wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins)) break;
       if (i == p.withhold) continue;  // test hook: never issued
       expect_bytes(bar, kABytes);
       if (TRANS) {
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
         tma_load(to, &a_map, (int)(step * kStepR), (int)a0, bar);
       }
     }
-    if (__any_sync(0xffffffffu, *abandoned))  // what was issued lands before the block's memory is another's
+    if (*abandoned)  // what was issued lands before the block's memory is another's
       for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
         if (j != p.withhold) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
   } else if (warp == kMmaWarp) {
@@ -201,7 +201,6 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
       const uint32_t s = i % STAGES, from = base + s * kStageBytes, parity = (i / STAGES) & 1;
       ok = wait(smem_u32(&sm.full_a[s]), parity, abandoned, p.status, p.max_spins) &&
            wait(smem_u32(&sm.full_b[s]), parity, abandoned, p.status, p.max_spins);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
 #pragma unroll
@@ -230,7 +229,6 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
       if (step + 1 < last) fetch<FMT>(next, p, (step + 1) * kStepR + row, c);
       const uint32_t s = i % STAGES;
       if (i >= STAGES) ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       unsigned char* const to = mem + s * kStageBytes + kABytes + chunk / 2 * (kBBytes / 4) + row * 128;
 #pragma unroll
@@ -245,7 +243,6 @@ __global__ void __launch_bounds__(kGThreads) mx_grad_kernel(const __grid_constan
       now = next;
     }
     ok = wait(smem_u32(&sm.done), 0, abandoned, p.status, p.max_spins);
-    ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
     if (ok) {
       const float alpha = kWidened<FMT> * (p.ts ? *p.ts : 1.0f);
@@ -383,14 +380,42 @@ struct PairParams {
   uint32_t max_spins, withhold;
 };
 
-__device__ __forceinline__ void multiply16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t onto) {
-  asm volatile(
-      "{\n\t.reg .pred one, p;\n\t"
-      "elect.sync _|one, 0xffffffff;\n\t"
-      "setp.ne.u32 p, %4, 0;\n\t"
-      "@one tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(onto)
-      : "memory");
+// The products of a step: four times 16 of its 64 rows, for one or two tiles of A.  One thread is elected for all of them,
+// and the operands' descriptors are counted on inside (a statement for each took 46 cycles an instruction).
+// a_k, b_k, a_m: from 16 rows to the next and from A's first tile to its second, in 16 bytes; d_m: columns between their sums.
+template <int MT, uint32_t A_K, uint32_t B_K, uint32_t A_M, uint32_t D_M>
+__device__ __forceinline__ void multiply16_step(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t onto) {
+  if (MT == 1)
+    asm volatile(
+        "{\n\t.reg .pred one, p, t;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\t"
+        "add.s64 a1, %1, %5;\n\tadd.s64 a2, a1, %5;\n\tadd.s64 a3, a2, %5;\n\t"
+        "add.s64 b1, %2, %6;\n\tadd.s64 b2, b1, %6;\n\tadd.s64 b3, b2, %6;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], a1, b1, %3, t;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], a2, b2, %3, t;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], a3, b3, %3, t;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(onto), "n"(A_K), "n"(B_K)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred one, p, t;\n\t.reg .b32 e;\n\t.reg .b64 a1, a2, a3, c0, c1, c2, c3, b1, b2, b3;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\tadd.u32 e, %0, %8;\n\t"
+        "add.s64 a1, %1, %5;\n\tadd.s64 a2, a1, %5;\n\tadd.s64 a3, a2, %5;\n\t"
+        "add.s64 c0, %1, %7;\n\tadd.s64 c1, c0, %5;\n\tadd.s64 c2, c1, %5;\n\tadd.s64 c3, c2, %5;\n\t"
+        "add.s64 b1, %2, %6;\n\tadd.s64 b2, b1, %6;\n\tadd.s64 b3, b2, %6;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [e], c0, %2, %3, p;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], a1, b1, %3, t;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [e], c1, b1, %3, t;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], a2, b2, %3, t;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [e], c2, b2, %3, t;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [%0], a3, b3, %3, t;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::f16 [e], c3, b3, %3, t;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(onto), "n"(A_K), "n"(B_K), "n"(A_M), "n"(D_M)
+        : "memory");
 }
 
 template <typename T, int FMT, bool TRANS, int MT>
@@ -444,14 +469,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const uint8_t* const scales = p.scales + (size_t)(c0 / S::kScaleCols) * kTileBytes;
       for (uint32_t step = 0; step < p.steps; ++step, ++i) {
         const uint32_t s = i % kPairHeld, to = base + S::kHeldAt + s * S::kHeldBytes, bar = smem_u32(&sm.held[s]);
-        if (i >= kPairHeld && !(ok = warp_wait(smem_u32(&sm.held_empty[s]), (i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))) break;
+        if (i >= kPairHeld && !(ok = wait(smem_u32(&sm.held_empty[s]), (i / kPairHeld - 1) & 1, abandoned, p.status, p.max_spins))) break;
         if (i == p.withhold) continue;  // test hook: never issued
         expect_bytes(bar, S::kHeldBytes);
         tma_load(to, &q_map, (int)(c0 / 2), (int)(step * kStepR), bar);
         bulk_load(to + S::kCodeBytes, scales + (size_t)(step * kStepR / kStrip) * p.strip_bytes, S::kScaleBytes, bar);
       }
     }
-    if (__any_sync(0xffffffffu, *abandoned))  // what was issued lands before the block's memory is another's
+    if (*abandoned)  // what was issued lands before the block's memory is another's
       for (uint32_t j = i > kPairHeld ? i - kPairHeld : 0; j < i; ++j)
         if (j != p.withhold) drain(smem_u32(&sm.held[j % kPairHeld]), (j / kPairHeld) & 1);
   } else if (warp >= kPairCopyWarp && warp < kPairCopyWarp + 2) {
@@ -464,7 +489,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const int a0 = (int)(tile % p.a_tiles * S::kRows + rank * kTileA + m * 256);
         for (uint32_t step = 0; step < p.steps; ++step, ++i) {
           const uint32_t s = i % STAGES, to = base + s * S::kStage + m * kABytes;
-          if (i >= STAGES && !(ok = warp_wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
+          if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
           if (rank == 0 && m == 0) expect_bytes(smem_u32(&sm.full_a[s]), 2 * MT * kABytes);
           const uint32_t bar = cluster_address(smem_u32(&sm.full_a[s]), 0);
           if (TRANS) {
@@ -475,7 +500,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           }
         }
       }
-      if (__any_sync(0xffffffffu, *abandoned) && rank == 0)  // (the last of them is in before this block's barrier completes)
+      if (*abandoned && rank == 0)  // (the last of them is in before this block's barrier completes)
         for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j) drain(smem_u32(&sm.full_a[j % STAGES]), (j / STAGES) & 1);
     }
   } else if (warp == kPairMmaWarp) {
@@ -487,26 +512,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       bool ok = true;
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
         const uint32_t set = n & 1;
-        if (n > 1) ok = wait_cluster(smem_u32(&sm.sums_empty[set]), (n / 2 - 1) & 1, abandoned, p.status, p.max_spins);
-        ok = __all_sync(0xffffffffu, ok);
+        if (n > 1) ok = wait<true>(smem_u32(&sm.sums_empty[set]), (n / 2 - 1) & 1, abandoned, p.status, p.max_spins);
         tc_fence_after();
         for (uint32_t step = 0; step < p.steps && ok; ++step) {
           const uint32_t s = i % STAGES, from = base + s * S::kStage;
           ok = wait(smem_u32(&sm.full_a[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins) &&
-               wait_cluster(smem_u32(&sm.full_b[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
-          ok = __all_sync(0xffffffffu, ok);
+               wait<true>(smem_u32(&sm.full_b[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
           if (!ok) break;
           tc_fence_after();
-#pragma unroll
-          for (uint32_t k = 0; k < kStepR / 16; ++k) {
-            const uint64_t b = operand(from + MT * kABytes + k * 2048, 8192, 1024, true);
-#pragma unroll
-            for (uint32_t m = 0; m < (uint32_t)MT; ++m) {
-              const uint64_t a = TRANS ? operand(from + m * kABytes + k * 2048, kABytes / 2, 1024, true)
-                                       : operand(from + m * kABytes + k * 32, 16, 1024, true);
-              multiply16_pair(tmem + set * kPairSums + m * S::kCols, a, b, idesc, (uint32_t)(step > 0 || k > 0));
-            }
-          }
+          const uint64_t a = TRANS ? operand(from, kABytes / 2, 1024, true) : operand(from, 16, 1024, true);
+          multiply16_step<MT, (TRANS ? 2048 : 32) / 16, 2048 / 16, kABytes / 16, S::kCols>(
+              tmem + set * kPairSums, a, operand(from + MT * kABytes, 8192, 1024, true), idesc, (uint32_t)(step > 0));
           commit_pair(smem_u32(&sm.empty[s]));
           ++i;
         }
@@ -529,7 +545,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const uint32_t i = (uint32_t)i64, hs = i % kPairHeld, s = i % STAGES;
       const unsigned char* const held = mem + S::kHeldAt + hs * S::kHeldBytes;
       bool ok = wait(smem_u32(&sm.held[hs]), (i / kPairHeld) & 1, abandoned, p.status, p.max_spins);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       uint4 codes[kItems];
       uint32_t scales[kItems];
@@ -544,7 +559,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           scales[it] = *reinterpret_cast<const uint16_t*>(held + at + atom * kTileBytes + (chunk & 1) * 2);
       }
       if (i >= STAGES) ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       unsigned char* const to = mem + s * S::kStage + MT * kABytes + atom * 8192 + row * 128;
 #pragma unroll
@@ -569,7 +583,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     for (uint32_t tile = blockIdx.x / 2; tile < p.tiles; tile += pairs, ++n) {
       const uint32_t set = n & 1;
       bool ok = wait(smem_u32(&sm.sums_full[set]), (n / 2) & 1, abandoned, p.status, p.max_spins);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
       const uint32_t c0 = tile / p.a_tiles * S::kCols;

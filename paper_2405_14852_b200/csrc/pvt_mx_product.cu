@@ -50,46 +50,35 @@ struct ProductShared {
   uint32_t tmem, abandoned;
 };
 
-template <int CTAS = 1>
 __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc) {
-  if (CTAS == 1)
-    asm volatile(
-        "{\n\t.reg .pred one;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "@one tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
-        : "memory");
-  else
-    asm volatile(
-        "{\n\t.reg .pred one;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
-        : "memory");
+  asm volatile(
+      "{\n\t.reg .pred one;\n\t"
+      "elect.sync _|one, 0xffffffff;\n\t"
+      "@one tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
+      : "memory");
 }
-#define PVT_MULTIPLY(GROUP, KIND)                                                                                     \
-  asm volatile(                                                                                                       \
-      "{\n\t.reg .pred one, p;\n\t"                                                                                   \
-      "elect.sync _|one, 0xffffffff;\n\t"                                                                             \
-      "setp.ne.u32 p, %6, 0;\n\t"                                                                                     \
-      "@one tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a),  \
-      "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)                                                               \
-      : "memory")
 // 64 columns of all rows of a tile
-template <int FMT, int CTAS = 1>
+template <int FMT>
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                          uint32_t onto) {
   if (FMT == PVT_MX_E8M0_32) {
-    if (CTAS == 1)
-      PVT_MULTIPLY("1", "mxf4.block_scale.scale_vec::2X");
-    else
-      PVT_MULTIPLY("2", "mxf4.block_scale.scale_vec::2X");
+    asm volatile(
+        "{\n\t.reg .pred one, p;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "@one tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
+        : "memory");
   } else {
-    if (CTAS == 1)
-      PVT_MULTIPLY("1", "mxf4nvf4.block_scale.scale_vec::4X");
-    else
-      PVT_MULTIPLY("2", "mxf4nvf4.block_scale.scale_vec::4X");
+    asm volatile(
+        "{\n\t.reg .pred one, p;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "@one tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
+        : "memory");
   }
 }
-#undef PVT_MULTIPLY
 
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_constant__ CUtensorMap w_map,
@@ -135,7 +124,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
     uint32_t i = 0;
     for (uint32_t step = first; step < last; ++step, ++i) {
       const uint32_t s = i % p.stages, bar = smem_u32(&sm.full[s]), to = base + s * p.stage_bytes;
-      if (i >= p.stages && !warp_wait(smem_u32(&sm.empty[s]), (i / p.stages - 1) & 1, abandoned, p.status, p.max_spins)) break;
+      if (i >= p.stages && !wait(smem_u32(&sm.empty[s]), (i / p.stages - 1) & 1, abandoned, p.status, p.max_spins)) break;
       if (i == p.withhold) continue;  // test hook: never issued
       expect_bytes(bar, bytes);
       tma_load(to, &w_map, (int)(step * kRowBytes), (int)w0, bar);
@@ -145,7 +134,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
         bulk_load(to + xs_at + q * (KT * kTileBytes), xs + (size_t)q * p.strip_bytes + (size_t)step * (KT * kTileBytes),
                  KT * kTileBytes, bar);
     }
-    if (__any_sync(0xffffffffu, *abandoned))  // what was issued lands before the block's memory is another's
+    if (*abandoned)  // what was issued lands before the block's memory is another's
       for (uint32_t j = i > p.stages ? i - p.stages : 0; j < i; ++j)
         if (j != p.withhold) drain(smem_u32(&sm.full[j % p.stages]), (j / p.stages) & 1);
   } else if (warp == kMmaWarp) {
@@ -158,7 +147,6 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
     for (uint32_t step = first; step < last && ok; ++step, ++i) {
       const uint32_t s = i % p.stages, from = base + s * p.stage_bytes;
       ok = wait(smem_u32(&sm.full[s]), (i / p.stages) & 1, abandoned, p.status, p.max_spins);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
       const uint32_t sfa = tmem + d_cols + s * sf_cols, sfb = sfa + KT * 4;
@@ -281,6 +269,141 @@ struct PairSizes {
   static_assert(256 + kStages * kScaleCols <= 512, "sums and scales fit tensor memory");
 };
 
+// A step of a pair: its scales to tensor memory (two or four tiles for w's 128 rows, as many for each of two strips of x) and
+// the products of four times 64 columns.  One thread is elected for all of them, and descriptors are counted on inside:
+// a tile of scales is 32 units of 16 bytes, four columns of tensor memory; 64 columns are 2 units of either operand.
+template <int FMT>
+__device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                              uint64_t w_scales, uint64_t x_scales, uint32_t onto) {
+  if (FMT == PVT_MX_E8M0_32) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred one, p, t;\n\t"
+        ".reg .b32 s, x, i;\n\t"
+        ".reg .b64 q;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %8, 0;\n\t"
+        "setp.eq.u32 t, 0, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.s64 q, %6, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "add.s64 q, %7, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 x, %5, 4;\n\t"
+        "add.s64 q, %7, 64;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.s64 q, %6, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 8;\n\t"
+        "add.s64 q, %7, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 x, %5, 12;\n\t"
+        "add.s64 q, %7, 96;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        ".reg .b64 a, b;\n\t"
+        "add.s64 a, %1, 0;\n\t"
+        "add.s64 b, %2, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], p;\n\t"
+        "add.s64 a, %1, 2;\n\t"
+        "add.s64 b, %2, 2;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "or.b32 i, %3, 1073741856;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 4;\n\t"
+        "add.s64 b, %2, 4;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.u32 x, %5, 8;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 6;\n\t"
+        "add.s64 b, %2, 6;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.u32 x, %5, 8;\n\t"
+        "or.b32 i, %3, 1073741856;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
+        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred one, p, t;\n\t"
+        ".reg .b32 s, x, i;\n\t"
+        ".reg .b64 q;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %8, 0;\n\t"
+        "setp.eq.u32 t, 0, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.s64 q, %6, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "add.s64 q, %7, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 x, %5, 4;\n\t"
+        "add.s64 q, %7, 128;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.s64 q, %6, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 8;\n\t"
+        "add.s64 q, %7, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 x, %5, 12;\n\t"
+        "add.s64 q, %7, 160;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 8;\n\t"
+        "add.s64 q, %6, 64;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 16;\n\t"
+        "add.s64 q, %7, 64;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 x, %5, 20;\n\t"
+        "add.s64 q, %7, 192;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 12;\n\t"
+        "add.s64 q, %6, 96;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 24;\n\t"
+        "add.s64 q, %7, 96;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 x, %5, 28;\n\t"
+        "add.s64 q, %7, 224;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        ".reg .b64 a, b;\n\t"
+        "add.s64 a, %1, 0;\n\t"
+        "add.s64 b, %2, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], p;\n\t"
+        "add.s64 a, %1, 2;\n\t"
+        "add.s64 b, %2, 2;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.u32 x, %5, 8;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 4;\n\t"
+        "add.s64 b, %2, 4;\n\t"
+        "add.u32 s, %4, 8;\n\t"
+        "add.u32 x, %5, 16;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 6;\n\t"
+        "add.s64 b, %2, 6;\n\t"
+        "add.u32 s, %4, 12;\n\t"
+        "add.u32 x, %5, 24;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
+        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
+        : "memory");
+  }
+}
+
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kPairThreads, 1)
     mx_product_pair_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
@@ -327,7 +450,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const int strip = (int)((of_w ? (uint32_t)row : tile0) / kStrip * p.strip_rows);
       for (uint32_t step = 0; step < p.steps; ++step, ++i) {
         const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
-        if (i >= STAGES && !(ok = warp_wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
+        if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
         if (i == p.withhold) continue;  // test hook: never issued
         const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), 0);
         const int col = (int)(step * kRowBytes), scales = strip + (int)(step * (KT * 4));
@@ -342,7 +465,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
       }
     }
-    if (__any_sync(0xffffffffu, *abandoned) && rank == 0)  // what was issued lands before the blocks' memory is another's
+    if (*abandoned && rank == 0)  // what was issued lands before the blocks' memory is another's
       for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
         if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
   } else if (warp == kPairMmaWarp) {
@@ -353,30 +476,17 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       uint32_t i = 0, n = 0;
       bool ok = true;
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
-        if (n > 0) ok = wait_cluster(smem_u32(&sm.sums_empty), (n - 1) & 1, abandoned, p.status, p.max_spins);
-        ok = __all_sync(0xffffffffu, ok);
+        if (n > 0) ok = wait<true>(smem_u32(&sm.sums_empty), (n - 1) & 1, abandoned, p.status, p.max_spins);
         tc_fence_after();
         for (uint32_t step = 0; step < p.steps && ok; ++step) {
           const uint32_t s = i % STAGES, from = base + s * S::kStageAligned;
           ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
-          ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();
           const uint32_t sfa = tmem + 256 + s * S::kScaleCols, sfb = sfa + KT * 4;
-          // a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart
-#pragma unroll
-          for (uint32_t t = 0; t < KT; ++t) {
-            scales_to_tmem<2>(sfa + t * 4, operand(from + S::kWs + t * kTileBytes, 0, 128, false));
-            for (uint32_t q = 0; q < 2; ++q)
-              scales_to_tmem<2>(sfb + (t * 2 + q) * 4, operand(from + S::kXs + (q * KT + t) * kTileBytes, 0, 128, false));
-          }
-          const uint64_t a = operand(from, 16, 1024, true), b = operand(from + S::kX, 16, 1024, true);
-#pragma unroll
-          for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t t = FMT == PVT_MX_E8M0_32 ? j / 2 : j, id = FMT == PVT_MX_E8M0_32 ? (j & 1) * 2 : 0;
-            multiply<FMT, 2>(tmem, a + 2 * j, b + 2 * j, idesc | id << 4 | id << 29, sfa + t * 4, sfb + t * 8,
-                             (uint32_t)(step > 0 || j > 0));
-          }
+          // (a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart)
+          multiply_step<FMT>(tmem, operand(from, 16, 1024, true), operand(from + S::kX, 16, 1024, true), idesc, sfa, sfb,
+                             operand(from + S::kWs, 0, 128, false), operand(from + S::kXs, 0, 128, false), (uint32_t)(step > 0));
           commit_pair(smem_u32(&sm.empty[s]));
           ++i;
         }
@@ -396,7 +506,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     uint32_t n = 0;
     for (uint32_t tile = blockIdx.x / 2; tile < p.tiles; tile += pairs, ++n) {
       bool ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
       uint32_t v[128];
