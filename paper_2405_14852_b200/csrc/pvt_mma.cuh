@@ -49,6 +49,22 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uin
   __syncwarp();
   return false;
 }
+// Two barriers of the same phase at a time, the second one the cluster's.
+__device__ __forceinline__ bool wait_both(uint32_t bar, uint32_t cluster_bar, uint32_t parity, volatile uint32_t* abandoned,
+                                          uint32_t* status, uint32_t max_spins) {
+  uint32_t both;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %3;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 q, [%2], %3;\n\t"
+      "and.pred p, p, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(both)
+      : "r"(bar), "r"(cluster_bar), "r"(parity)
+      : "memory");
+  return __all_sync(0xffffffffu, both) ||
+         (wait(bar, parity, abandoned, status, max_spins) && wait<true>(cluster_bar, parity, abandoned, status, max_spins));
+}
 // For what has been issued and does complete: copies and products in flight when a block is abandoned.
 __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
   for (uint32_t spin = 0; spin < m1::kMaxSpins; ++spin)

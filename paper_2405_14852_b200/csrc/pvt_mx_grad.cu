@@ -516,8 +516,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         tc_fence_after();
         for (uint32_t step = 0; step < p.steps && ok; ++step) {
           const uint32_t s = i % STAGES, from = base + s * S::kStage;
-          ok = wait(smem_u32(&sm.full_a[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins) &&
-               wait<true>(smem_u32(&sm.full_b[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
+          ok = wait_both(smem_u32(&sm.full_a[s]), smem_u32(&sm.full_b[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
           if (!ok) break;
           tc_fence_after();
           const uint64_t a = TRANS ? operand(from, kABytes / 2, 1024, true) : operand(from, 16, 1024, true);
