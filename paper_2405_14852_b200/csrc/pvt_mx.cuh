@@ -57,6 +57,12 @@ __device__ __forceinline__ float e4m3_value(uint32_t byte) {
   if ((byte & 127) == 127) return __uint_as_float(0x7fc00000u);
   return e ? __uint_as_float((e + 120) << 23 | m << 20) : (float)m * 0.001953125f;
 }
+// the same by the conversion unit, through binary16
+__device__ __forceinline__ float e4m3_float(uint32_t byte) {
+  uint32_t two;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(two) : "h"((uint16_t)byte));
+  return __low2float(*reinterpret_cast<const __half2*>(&two));
+}
 // 2^(byte - 127); 255 is NaN
 __device__ __forceinline__ float e8m0_value(uint32_t byte) {
   return byte == 255 ? __uint_as_float(0x7fc00000u) : byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);

@@ -1,9 +1,9 @@
 // Quantisation to 4-bit block floating point and back.
 //
-// One pass over the matrix: a warp takes 256 columns of a row, eight to a lane, so that the lane's elements are one 16- or
-// 32-byte load, its codes one 4-byte store, and a block's largest magnitude is an exchange between two (e4m3, 16
-// elements) or four (e8m0, 32) lanes.  The scale bytes of four blocks leave as one word into their tile.  Bound by HBM: what
-// is computed per element is one product and half a conversion instruction.
+// One pass over the matrix: a warp takes 256 or 512 columns of a row, 32 bytes to a lane, so that the lane's codes are one
+// 4- or 8-byte store, and a block's largest magnitude is an exchange between at most four lanes.  The scale bytes of four
+// blocks leave as one word into their tile.  Bound by HBM for binary32 (28672 x 8192 e8m0 162 us, 164 at the copy's rate), by
+// instructions for 16-bit elements under e4m3.
 //
 // Elements.  Under e8m0 the scale is a power of two, so x / scale is exact and the conversion rounds once.  Under e4m3 the
 // quotient x / (scale tensor_scale) is rounded before it is converted, which could carry it over a border between two
@@ -18,7 +18,9 @@ namespace {
 using namespace mx;
 
 constexpr int kQThreads = 256;
-constexpr int kQUnroll = 4;  // spans in flight per warp
+constexpr int kQUnroll = 4;  // spans in flight per warp on the way back
+
+constexpr float kMore = 1.00000095367431640625f, kLess = 0.99999904632568359375f;  // 1 + 2^-20, 1 - 2^-20
 
 // two conversions of eight values each side by side: code of v[0] in the lowest four bits
 __device__ __forceinline__ uint32_t e2m1_codes(const float* v) {
@@ -48,13 +50,11 @@ __device__ __noinline__ uint32_t e2m1_exact(float x, double d) {
   return n | (__float_as_uint(x) >> 31 << 3);
 }
 
-// the e4m3 number nearest to amax / six_ts (at most 448), ties to the even one
-__device__ __forceinline__ uint32_t e4m3_scale(float amax, double six_ts, double inv) {
-  const float q = (float)((double)amax * inv);
+// the e4m3 number nearest to amax / six_ts (at most 448), ties to the even one: by its midpoints, exact in binary64
+__device__ __noinline__ uint32_t e4m3_exact(float amax, double six_ts) {
   uint16_t two;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(q));
-  uint32_t c = two & 127u;
-  // q may have been rounded over a midpoint: compare with the midpoints themselves, exact in binary64
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"((float)((double)amax / six_ts)));
+  const uint32_t c = two & 127u;  // rounded twice: it may be the neighbour
   const double v = e4m3_value(c), a = amax;
   if (c < 126) {
     const double mid = 0.5 * (v + (double)e4m3_value(c + 1)) * six_ts;
@@ -65,6 +65,13 @@ __device__ __forceinline__ uint32_t e4m3_scale(float amax, double six_ts, double
     if (a < mid || (a == mid && (c & 1))) return c - 1;
   }
   return c;
+}
+// the same by the quotient a little larger and a little smaller than computed, where that decides it
+__device__ __forceinline__ uint32_t e4m3_scale(float amax, float ts, float inv) {
+  const float q = amax * inv;
+  uint16_t two;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(q * kLess), "f"(q * kMore));
+  return (two >> 8) == (two & 255u) && inv < 1e38f ? two & 127u : e4m3_exact(amax, 6.0 * (double)ts);
 }
 
 // The span's elements from one of two orders to the other: eight consecutive ones in a lane, and (rows that no wide access can
@@ -85,116 +92,114 @@ __device__ __forceinline__ void turn(float* buffer, float* v, uint32_t lane) {
   }
 }
 
+// elements of a lane: 32 bytes, or eight where a row is read element by element
+template <typename T, bool WIDE>
+constexpr int kLaneElements = WIDE ? 32 / (int)sizeof(T) : 8;
+
 template <typename T, int FMT, bool WIDE>
 __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ld, uint8_t* scales,
                                                                 const float* tensor_scale, uint32_t rows, uint32_t cols,
                                                                 uint32_t tiles, FastDiv spans_div, uint32_t spans,
-                                                                uint64_t total) {
-  constexpr int LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;  // of a block
+                                                                uint32_t total) {
+  constexpr int E = kLaneElements<T, WIDE>, LANES = (FMT == PVT_MX_E8M0_32 ? 32 : 16) / E;  // of a block
   __shared__ float buffer[WIDE ? 1 : kQThreads / 32][kSpan + 8 * kSpan / 32];
   pdl_trigger();
   pdl_wait();
   const uint32_t lane = threadIdx.x & 31;
   float ts = 1.0f;
   bool bad_ts = false;
-  double six_ts = 6.0, inv_six = 1.0 / 6.0;
+  float inv_six = 1.0f / 6.0f;
   if (FMT == PVT_MX_E4M3_16 && tensor_scale) {
     ts = *tensor_scale;
     bad_ts = !(ts > 0.0f && ts < __uint_as_float(0x7f800000u));
-    six_ts = 6.0 * (double)ts;
-    inv_six = 1.0 / six_ts;
+    inv_six = 1.0f / (6.0f * ts);
   }
-  const uint64_t warps = (uint64_t)gridDim.x * (kQThreads / 32);
-  for (uint64_t at = ((uint64_t)blockIdx.x * (kQThreads / 32) + threadIdx.x / 32) * kQUnroll; at < total; at += warps * kQUnroll) {
-    float v[kQUnroll][8];
-    uint32_t row[kQUnroll], c0[kQUnroll];
-#pragma unroll
-    for (int u = 0; u < kQUnroll; ++u) {
-      const uint64_t n = at + u;
-      // (a strip's rows that do not exist are spans too: their scales are written)
-      row[u] = n < total ? fast_div((uint32_t)n, spans_div) : 0xffffffffu;
-      c0[u] = ((uint32_t)n - row[u] * spans) * kSpan + 8 * lane;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
-      if (row[u] >= rows) continue;
-      const T* from = x + (int64_t)row[u] * ldx;
-      if (!WIDE) {  // lane by lane along the row, turned below
-        const uint32_t span0 = c0[u] - 8 * lane;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (span0 + 32 * i + lane < cols) v[u][i] = widen<T>(from[span0 + 32 * i + lane]);
-      } else if (c0[u] + 8 <= cols) {
-        const Eight<T> e = *reinterpret_cast<const Eight<T>*>(from + c0[u]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] = widen<T>(e.v[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (c0[u] + i < cols) v[u][i] = widen<T>(from[c0[u] + i]);
-      }
+  for (uint32_t at = blockIdx.x * (kQThreads / 32) + threadIdx.x / 32; at < total; at += gridDim.x * (kQThreads / 32)) {
+    // (a strip's rows that do not exist are spans too: their scales are written)
+    const uint32_t row = fast_div(at, spans_div), c0 = (at - row * spans) * (32 * E) + E * lane;
+    const uint32_t block = c0 / (E * LANES);
+    uint32_t* const to_scales = reinterpret_cast<uint32_t*>(scales + scale_at(row, block, tiles));
+    const bool leads = lane % (4 * LANES) == 0 && block / 4 < tiles;  // has the word of four blocks
+    if (row >= rows) {
+      if (leads) *to_scales = 0;
+      continue;
     }
+    float v[E];
+    const T* const from = x + (int64_t)row * ldx;
+    if (!WIDE) {  // lane by lane along the row, then turned
+      const uint32_t span0 = c0 - E * lane;
 #pragma unroll
-    for (int u = 0; u < kQUnroll; ++u) {
-      if (row[u] == 0xffffffffu) break;
-      if (row[u] >= rows) {
-        if (lane % (4 * LANES) == 0)
-          *reinterpret_cast<uint32_t*>(scales + scale_at(row[u], c0[u] / (8 * LANES), tiles)) = 0;
-        continue;
+      for (int i = 0; i < E; ++i) v[i] = span0 + 32 * i + lane < cols ? widen<T>(from[span0 + 32 * i + lane]) : 0.0f;
+      turn<false>(buffer[threadIdx.x / 32], v, lane);
+    } else if (c0 + E <= cols) {
+      T e[E];
+#pragma unroll
+      for (int i = 0; i < E; i += 8) *reinterpret_cast<Eight<T>*>(e + i) = *reinterpret_cast<const Eight<T>*>(from + c0 + i);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = widen<T>(e[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = c0 + i < cols ? widen<T>(from[c0 + i]) : 0.0f;
+    }
+    uint32_t top = 0;  // bits of the largest magnitude: NaN and infinity above every number
+#pragma unroll
+    for (int i = 0; i < E; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+    for (int s = 1; s < LANES; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+    const bool bad = top >= 0x7f800000u || bad_ts;
+    uint32_t byte, word[E / 8];
+#pragma unroll
+    for (int w = 0; w < E / 8; ++w) word[w] = 0;
+    if (FMT == PVT_MX_E8M0_32) {
+      // floor(log2 a) - 2, biased; numbers below 2^-126 have a scale of 2^-127 in any case
+      const int e = max((int)(top >> 23) - 2, 0);
+      byte = bad ? 255u : (uint32_t)e;
+      const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] *= inv;
+      if (!bad) {
+#pragma unroll
+        for (int w = 0; w < E / 8; ++w) word[w] = e2m1_codes(v + 8 * w);
       }
-      if (!WIDE) turn<false>(buffer[threadIdx.x / 32], v[u], lane);
-      uint32_t top = 0;  // bits of the largest magnitude: NaN and infinity above every number
+    } else {
+      byte = bad ? 127u : e4m3_scale(__uint_as_float(top), ts, inv_six);
+      if (!bad && byte) {
+        const float s = e4m3_float(byte), d = s * ts;
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+        const float more = r * kMore, less = r * kLess;
+        // where d or r leave the range of normal numbers every element is compared with its borders
+        const bool all = !(d >= 1e-30f && d <= 1e30f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
-#pragma unroll
-      for (int s = 1; s < LANES; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-      const bool bad = top >= 0x7f800000u || bad_ts;
-      uint32_t byte, word = 0;
-      if (FMT == PVT_MX_E8M0_32) {
-        // floor(log2 a) - 2, biased; numbers below 2^-126 have a scale of 2^-127 in any case
-        const int e = max((int)(top >> 23) - 2, 0);
-        byte = bad ? 255u : (uint32_t)e;
-        const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] *= inv;
-        if (!bad) word = e2m1_codes(v[u]);
-      } else {
-        byte = bad ? 127u : e4m3_scale(__uint_as_float(top), six_ts, inv_six);
-        if (!bad && byte) {
-          const float s = e4m3_value(byte), d = s * ts, r = 1.0f / d;
+        for (int w = 0; w < E / 8; ++w) {
           float hi[8], lo[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float y = v[u][i] * r;
-            hi[i] = y * 1.00000095367431640625f;  // 1 + 2^-20
-            lo[i] = y * 0.99999904632568359375f;
-          }
-          word = e2m1_codes(hi);
-          uint32_t differ = word ^ e2m1_codes(lo);
-          // where d or r leave the range of normal numbers every element is compared with its borders
-          if (!(d >= 1e-30f && d <= 1e30f)) differ = 0xffffffffu;
+          for (int i = 0; i < 8; ++i) hi[i] = v[8 * w + i] * more, lo[i] = v[8 * w + i] * less;
+          word[w] = e2m1_codes(hi);
+          const uint32_t differ = all ? 0xffffffffu : word[w] ^ e2m1_codes(lo);
           if (differ) {
             const double dd = (double)s * (double)ts;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              if (differ >> (4 * i) & 15u) word = (word & ~(15u << (4 * i))) | e2m1_exact(v[u][i], dd) << (4 * i);
+              if (differ >> (4 * i) & 15u) word[w] = (word[w] & ~(15u << (4 * i))) | e2m1_exact(v[8 * w + i], dd) << (4 * i);
           }
         }
       }
-      if (c0[u] >= cols) byte = 0;  // no such block, whatever the tensor scale is
-      uint32_t four = byte | __shfl_down_sync(0xffffffffu, byte, LANES) << 8;
-      four |= __shfl_down_sync(0xffffffffu, four, 2 * LANES) << 16;
-      if (lane % (4 * LANES) == 0) {
-        const uint32_t block = c0[u] / (8 * LANES);
-        *reinterpret_cast<uint32_t*>(scales + scale_at(row[u], block, tiles)) = four;
-      }
-      if (c0[u] < cols) {
-        uint8_t* to = codes + (int64_t)row[u] * ld + c0[u] / 2;
-        if (c0[u] + 8 <= cols) {
-          *reinterpret_cast<uint32_t*>(to) = word;
-        } else {
-          for (uint32_t i = 0; 2 * i < cols - c0[u]; ++i) to[i] = (uint8_t)(word >> (8 * i));
-        }
-      }
+    }
+    if (c0 >= cols) byte = 0;  // no such block, whatever the tensor scale is
+    uint32_t four = byte | __shfl_down_sync(0xffffffffu, byte, LANES) << 8;
+    four |= __shfl_down_sync(0xffffffffu, four, 2 * LANES) << 16;
+    if (leads) *to_scales = four;
+    uint8_t* const to = codes + (int64_t)row * ld + c0 / 2;
+    if (c0 + E <= cols) {
+      if (E == 16)
+        *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[E / 8 - 1]);
+      else
+        *reinterpret_cast<uint32_t*>(to) = word[0];
+    } else if (c0 < cols) {
+#pragma unroll
+      for (uint32_t i = 0; i < E / 2; ++i)
+        if (2 * i < cols - c0) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
     }
   }
 }
@@ -227,7 +232,7 @@ __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* co
 #pragma unroll
     for (int u = 0; u < kQUnroll; ++u) {
       if (at + u >= total) break;
-      const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(byte[u]) : e4m3_value(byte[u]);
+      const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(byte[u]) : e4m3_float(byte[u]);
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -258,24 +263,31 @@ __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* co
   }
 }
 
+// eight elements at a time, wherever a lane's begin
 bool rows_aligned(const void* p, int64_t ld, size_t size) {
   return reinterpret_cast<uintptr_t>(p) % (8 * size) == 0 && ld % 8 == 0;
 }
 
-unsigned span_grid(uint64_t total, int sm_count) {
-  const uint64_t need = (total + kQThreads / 32 * kQUnroll - 1) / (kQThreads / 32 * kQUnroll);
+// warps that take `each` spans at a time
+unsigned span_grid(uint64_t total, int each, int sm_count) {
+  const uint64_t need = (total + kQThreads / 32 * each - 1) / (kQThreads / 32 * each);
   const uint64_t most = (uint64_t)sm_count * 8;
   return (unsigned)(need < most ? need : most);
 }
 
+template <typename T, int FMT, bool WIDE>
+cudaError_t quantize(const pvt_mx& m, const T* x, int64_t ldx, int sm_count, cudaStream_t stream) {
+  constexpr uint32_t span = 32 * kLaneElements<T, WIDE>;
+  const uint32_t spans = ((uint32_t)m.cols + span - 1) / span;
+  const uint32_t total = ((uint32_t)m.rows + kStrip - 1) / kStrip * kStrip * spans;
+  return launch_dependent(mx_quantize_kernel<T, FMT, WIDE>, span_grid(total, 1, sm_count), kQThreads, 0, stream, x, ldx, m.codes,
+                          m.ld, m.scales, m.tensor_scale, (uint32_t)m.rows, (uint32_t)m.cols,
+                          strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans, total);
+}
 template <typename T, int FMT>
 cudaError_t quantize(const pvt_mx& m, const T* x, int64_t ldx, int sm_count, cudaStream_t stream) {
-  const uint32_t spans = (uint32_t)((m.cols + kSpan - 1) / kSpan);
-  const uint64_t total = (uint64_t)((m.rows + kStrip - 1) / kStrip) * kStrip * spans;
-  auto kernel = rows_aligned(x, ldx, sizeof(T)) ? mx_quantize_kernel<T, FMT, true> : mx_quantize_kernel<T, FMT, false>;
-  return launch_dependent(kernel, span_grid(total, sm_count), kQThreads, 0, stream, x, ldx, m.codes, m.ld, m.scales, m.tensor_scale,
-                          (uint32_t)m.rows, (uint32_t)m.cols, strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans,
-                          total);
+  return rows_aligned(x, ldx, sizeof(T)) ? quantize<T, FMT, true>(m, x, ldx, sm_count, stream)
+                                         : quantize<T, FMT, false>(m, x, ldx, sm_count, stream);
 }
 
 template <typename T, int FMT>
@@ -283,7 +295,7 @@ cudaError_t dequant(const pvt_mx& m, T* values, int64_t ldv, int sm_count, cudaS
   const uint32_t spans = (uint32_t)((m.cols + kSpan - 1) / kSpan);
   const uint64_t total = (uint64_t)m.rows * spans;
   auto kernel = rows_aligned(values, ldv, sizeof(T)) ? mx_dequant_kernel<T, FMT, true> : mx_dequant_kernel<T, FMT, false>;
-  return launch_dependent(kernel, span_grid(total, sm_count), kQThreads, 0, stream, (const uint8_t*)m.codes, m.ld,
+  return launch_dependent(kernel, span_grid(total, kQUnroll, sm_count), kQThreads, 0, stream, (const uint8_t*)m.codes, m.ld,
                           (const uint8_t*)m.scales, m.tensor_scale, values, ldv, (uint32_t)m.rows, (uint32_t)m.cols,
                           strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans, total);
 }
