@@ -1,15 +1,17 @@
 // Product of two matrices in 4-bit block floating point, y = x w^T, on the tensor cores' block-scaled instructions
 // (tcgen05.mma kind::mxf4 / mxf4nvf4): elements and scales go in as they lie in memory, sums come out in binary32.
 //
-// A tile is 128 rows of w (the instruction's M) times 16 to 256 rows of x (its N): with the weights on the side of fixed size a
-// single token costs 16 columns instead of 128 rows, and the accumulator's lanes are consecutive outputs of a token.  One step
-// of a tile is 256 columns: 128 bytes of each row, copied by TMA under the 128-byte swizzle, and the scales of
-// those columns, 2 or 4 tiles per 128 rows, which lie in memory as tensor memory wants them (tcgen05.cp, each part of 32
-// lanes for all four).  Four products of 64 columns each follow.  Tensor memory holds the scales of every stage: a stage is
-// refilled once the products that read it have completed, so nothing is overwritten early.
+// The weights are on the instruction's side of fixed size, 128 rows, so that few tokens cost few columns, and the
+// accumulator's lanes are consecutive outputs of a token.  One step is 256 columns: 128 bytes of each row, copied by TMA under the
+// 128-byte swizzle, and the scales of those columns, 2 or 4 tiles per 128 rows, which lie in memory as tensor memory wants them
+// (tcgen05.cp, each part of 32 lanes for all four).  Four products of 64 columns each follow.  Tensor memory holds the scales
+// of every stage: a stage is refilled once the products that read it have completed, so nothing is overwritten early.
 //
-// Few tiles leave most SMs idle, so the steps of a tile are then shared by a cluster of up to eight blocks, whose
-// partial sums meet in shared memory across the cluster, always in the order of ranks.
+// Up to 16 tokens, as in generation, the product is one pass over the weights: tiles of 128 rows by 16 tokens, two blocks per SM, and
+// all of a block's weights asked for at its start.  128 rows leave SMs idle in most layers, so the steps of a tile
+// are shared by a cluster of up to eight blocks, whose partial sums meet in shared memory across the cluster, always in
+// the order of ranks.  From 17 tokens on pairs of blocks take over (below): 4096 by 11008, 16 / 32 / 64 / 128 tokens, tiles
+// of as many tokens here 9.8 / 11.8 / 16.3 / 14.9 us, pairs from 32 on 10.2 / 9.2 / 9.2.
 #include "pvt_mma.cuh"
 #include "pvt_mx.cuh"
 
@@ -23,29 +25,43 @@ constexpr int kPThreads = 192;   // four warps read sums out, one copies, one mu
 constexpr int kCopyWarp = 4, kMmaWarp = 5;
 constexpr int kTileW = 128;      // rows of w
 constexpr int kRowBytes = 128;   // of a step
-constexpr int kMaxStages = 8;
+constexpr uint32_t kFewTokens = 16;
+
+// of the kernel for few tokens
+template <int FMT>
+struct FewSizes {
+  static constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;  // scale tiles of a step and strip
+  // a stage: rows of w, rows of x, scales of w, scales of x
+  static constexpr uint32_t kX = kTileW * kRowBytes, kWs = kX + kFewTokens * kRowBytes, kXs = kWs + KT * kTileBytes;
+  static constexpr uint32_t kStage = kXs + KT * kTileBytes, kStageAligned = (kStage + 1023) / 1024 * 1024;
+  static constexpr uint32_t kStages = 110 * 1024 / kStageAligned;  // of two blocks per SM
+  static constexpr uint32_t kScaleCols = KT * 4 * 2;
+  static constexpr uint32_t kTmem = 32 + kStages * kScaleCols <= 128 ? 128 : 256;
+  static_assert(32 + kStages * kScaleCols <= kTmem, "sums and scales fit");
+  static constexpr size_t kBytes = kStages * kStageAligned + 1024;
+  static_assert(kFewTokens * kTileW * 4 <= kStages * kStageAligned, "the partial sums fit the stages");
+};
 
 struct ProductParams {
+  const uint8_t* w_codes;
   const uint8_t* w_scales;
   const uint8_t* x_scales;
   const float* w_ts;
   const float* x_ts;
   void* y;
-  int64_t ldy;
+  int64_t ldy, ldw;
   uint32_t* status;
-  uint32_t w_rows, x_rows, x_strips;
+  uint32_t w_rows, x_rows;
+  uint32_t row_bytes;     // of w, to the last 16 that hold codes
   uint32_t strip_bytes;   // scales of a strip of 128 rows
   uint32_t steps;         // of 256 columns
-  uint32_t x_tiles;
-  uint32_t tile_x;        // rows of x per tile
-  uint32_t stages, stage_bytes, tmem_cols;
   uint32_t split;         // blocks per tile
   uint32_t max_spins, withhold;
 };
 
 struct ProductShared {
-  alignas(8) uint64_t full[kMaxStages];
-  uint64_t empty[kMaxStages];
+  alignas(8) uint64_t full[8];
+  uint64_t empty[8];
   uint64_t done, spare;
   uint32_t tmem, abandoned;
 };
@@ -83,14 +99,23 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_constant__ CUtensorMap w_map,
                                                                const __grid_constant__ CUtensorMap x_map, const ProductParams p) {
-  constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;  // scale tiles of a step and strip
+  using S = FewSizes<FMT>;
+  constexpr uint32_t KT = S::KT, STAGES = S::kStages;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ ProductShared sm;
   const uint32_t tid = threadIdx.x, warp = tid >> 5;
   volatile uint32_t* abandoned = &sm.abandoned;
+  const uint32_t rank = blockIdx.x % p.split, w0 = blockIdx.x / p.split * kTileW;
+  const uint32_t first = p.steps * rank / p.split, last = p.steps * (rank + 1) / p.split;  // (steps < 2^20, split <= 8)
+  // all of the block's weights at once, while it sets itself up and the kernel ahead ends
+  const uint32_t from_byte = first * kRowBytes, to_byte = min(last * kRowBytes, p.row_bytes);
+  if (tid < (uint32_t)kTileW && w0 + tid < p.w_rows)
+    prefetch_l2(p.w_codes + (int64_t)(w0 + tid) * p.ldw + from_byte, to_byte - from_byte);
+  if (tid == (uint32_t)kTileW)
+    prefetch_l2(p.w_scales + (size_t)(w0 / kStrip) * p.strip_bytes + (size_t)first * (KT * kTileBytes), (last - first) * (KT * kTileBytes));
   if (tid == 0) {
     sm.abandoned = 0;
-    for (uint32_t s = 0; s < p.stages; ++s) {
+    for (uint32_t s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&sm.full[s]), 1);
       mbar_init(smem_u32(&sm.empty[s]), 1);
     }
@@ -99,7 +124,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
-    tmem_alloc(smem_u32(&sm.tmem), p.tmem_cols);
+    tmem_alloc(smem_u32(&sm.tmem), S::kTmem);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -110,58 +135,49 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
 
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
-  const uint32_t rank = blockIdx.x % p.split, tile = blockIdx.x / p.split;
-  const uint32_t w0 = tile / p.x_tiles * kTileW, x0 = tile % p.x_tiles * p.tile_x;
-  const uint32_t first = p.steps * rank / p.split, last = p.steps * (rank + 1) / p.split;  // (steps < 2^20, split <= 8)
-  const uint32_t x_strips = min((p.tile_x + kStrip - 1) / kStrip, p.x_strips - x0 / kStrip);
-  // a stage: rows of w, rows of x, scales of w, scales of x
-  const uint32_t x_at = kTileW * kRowBytes, ws_at = x_at + p.tile_x * kRowBytes, xs_at = ws_at + KT * kTileBytes;
+  const uint32_t col = w0 + tid;
+  float alpha = 1.0f;
+  T* const y = static_cast<T*>(p.y) + col;
 
   if (warp == kCopyWarp) {
-    const uint32_t bytes = (kTileW + p.tile_x) * kRowBytes + (1 + x_strips) * KT * kTileBytes;
-    const uint8_t* ws = p.w_scales + (size_t)(w0 / kStrip) * p.strip_bytes;
-    const uint8_t* xs = p.x_scales + (size_t)(x0 / kStrip) * p.strip_bytes;
+    const uint8_t* const ws = p.w_scales + (size_t)(w0 / kStrip) * p.strip_bytes;
     uint32_t i = 0;
     for (uint32_t step = first; step < last; ++step, ++i) {
-      const uint32_t s = i % p.stages, bar = smem_u32(&sm.full[s]), to = base + s * p.stage_bytes;
-      if (i >= p.stages && !wait(smem_u32(&sm.empty[s]), (i / p.stages - 1) & 1, abandoned, p.status, p.max_spins)) break;
+      const uint32_t s = i % STAGES, bar = smem_u32(&sm.full[s]), to = base + s * S::kStageAligned;
+      if (i >= STAGES && !wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins)) break;
       if (i == p.withhold) continue;  // test hook: never issued
-      expect_bytes(bar, bytes);
+      expect_bytes(bar, S::kStage);
       tma_load(to, &w_map, (int)(step * kRowBytes), (int)w0, bar);
-      tma_load(to + x_at, &x_map, (int)(step * kRowBytes), (int)x0, bar);
-      bulk_load(to + ws_at, ws + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
-      for (uint32_t q = 0; q < x_strips; ++q)
-        bulk_load(to + xs_at + q * (KT * kTileBytes), xs + (size_t)q * p.strip_bytes + (size_t)step * (KT * kTileBytes),
-                 KT * kTileBytes, bar);
+      tma_load(to + S::kX, &x_map, (int)(step * kRowBytes), 0, bar);
+      bulk_load(to + S::kWs, ws + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
+      bulk_load(to + S::kXs, p.x_scales + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
     }
     if (*abandoned)  // what was issued lands before the block's memory is another's
-      for (uint32_t j = i > p.stages ? i - p.stages : 0; j < i; ++j)
-        if (j != p.withhold) drain(smem_u32(&sm.full[j % p.stages]), (j / p.stages) & 1);
+      for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+        if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
   } else if (warp == kMmaWarp) {
-    const uint32_t d_cols = max(p.tile_x, 32u);
-    // e2m1 both, N, M = 128, type of the scales
-    const uint32_t idesc = 1u << 7 | 1u << 10 | (p.tile_x >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | 1u << 27;
-    const uint32_t x_tiles = (p.tile_x + kStrip - 1) / kStrip, sf_cols = KT * 4 * (1 + x_tiles);
+    // e2m1 both, N = 16, M = 128, type of the scales
+    constexpr uint32_t idesc =
+        1u << 7 | 1u << 10 | (kFewTokens >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | 1u << 27;
     uint32_t i = 0;
     bool ok = true;
-    for (uint32_t step = first; step < last && ok; ++step, ++i) {
-      const uint32_t s = i % p.stages, from = base + s * p.stage_bytes;
-      ok = wait(smem_u32(&sm.full[s]), (i / p.stages) & 1, abandoned, p.status, p.max_spins);
+    for (uint32_t step = first; step < last; ++step, ++i) {
+      const uint32_t s = i % STAGES, from = base + s * S::kStageAligned;
+      ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t sfa = tmem + d_cols + s * sf_cols, sfb = sfa + KT * 4;
+      const uint32_t sfa = tmem + 32 + s * S::kScaleCols, sfb = sfa + KT * 4;
       // a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart
+#pragma unroll
       for (uint32_t t = 0; t < KT; ++t) {
-        scales_to_tmem(sfa + t * 4, operand(from + ws_at + t * kTileBytes, 0, 128, false));
-        for (uint32_t q = 0; q < x_tiles; ++q)
-          scales_to_tmem(sfb + (t * x_tiles + q) * 4, operand(from + xs_at + (q * KT + t) * kTileBytes, 0, 128, false));
+        scales_to_tmem(sfa + t * 4, operand(from + S::kWs + t * kTileBytes, 0, 128, false));
+        scales_to_tmem(sfb + t * 4, operand(from + S::kXs + t * kTileBytes, 0, 128, false));
       }
-      const uint64_t a = operand(from, 16, 1024, true), b = operand(from + x_at, 16, 1024, true);
+      const uint64_t a = operand(from, 16, 1024, true), b = operand(from + S::kX, 16, 1024, true);
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j) {  // 64 columns, 32 bytes
         const uint32_t t = FMT == PVT_MX_E8M0_32 ? j / 2 : j, id = FMT == PVT_MX_E8M0_32 ? (j & 1) * 2 : 0;
-        multiply<FMT>(tmem, a + 2 * j, b + 2 * j, idesc | id << 4 | id << 29, sfa + t * 4, sfb + t * x_tiles * 4,
-                      (uint32_t)(i > 0 || j > 0));
+        multiply<FMT>(tmem, a + 2 * j, b + 2 * j, idesc | id << 4 | id << 29, sfa + t * 4, sfb + t * 4, (uint32_t)(i > 0 || j > 0));
       }
       commit(smem_u32(&sm.empty[s]));
     }
@@ -172,55 +188,44 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
       drain(smem_u32(&sm.spare), 0);
     }
   } else {
-    // the sums of 128 rows of w by 32 columns of x at a time; lanes are consecutive outputs of a token
-    const bool ok = wait(smem_u32(&sm.done), 0, abandoned, p.status, p.max_spins);
-    tc_fence_after();
-    float alpha = 1.0f;
+    // lanes are consecutive outputs of a token
     if (p.w_ts) alpha = *p.w_ts;
     if (p.x_ts) alpha *= *p.x_ts;
-    const uint32_t n_x = min(p.tile_x, p.x_rows - x0), col = w0 + tid;
-    T* y = static_cast<T*>(p.y) + (int64_t)x0 * p.ldy + col;
-    float* part = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
-    if (ok) {
-      for (uint32_t j0 = 0; j0 < n_x; j0 += 16) {
-        uint32_t v[16];
-        tmem_ld16(tmem + (warp << 21) + j0, v);
-        tmem_ld_wait<16>(v);
-        if (p.split == 1) {
-          if (col < p.w_rows) {
+    float* const part = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
+    if (wait(smem_u32(&sm.done), 0, abandoned, p.status, p.max_spins)) {
+      tc_fence_after();
+      uint32_t v[kFewTokens];
+      tmem_ld16(tmem + (warp << 21), v);
+      tmem_ld_wait<kFewTokens>(v);
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (j0 + j < n_x) y[(int64_t)(j0 + j) * p.ldy] = narrow<T>(__uint_as_float(v[j]) * alpha);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) part[(j0 + j) * kTileW + tid] = __uint_as_float(v[j]);
-        }
+      for (uint32_t j = 0; j < kFewTokens; ++j) {
+        if (j >= p.x_rows) break;
+        if (p.split > 1)
+          part[j * kTileW + tid] = __uint_as_float(v[j]);
+        else if (col < p.w_rows)
+          y[(int64_t)j * p.ldy] = narrow<T>(__uint_as_float(v[j]) * alpha);
       }
+      tc_fence_before();
     }
-    tc_fence_before();
   }
   if (p.split > 1) {
     cluster_sync();
     // every block adds up the tokens that are its share
-    if (tid < kTileW && !*abandoned) {
-      float alpha = 1.0f;
-      if (p.w_ts) alpha = *p.w_ts;
-      if (p.x_ts) alpha *= *p.x_ts;
-      const uint32_t n_x = min(p.tile_x, p.x_rows - x0), col = w0 + tid;
-      T* y = static_cast<T*>(p.y) + (int64_t)x0 * p.ldy + col;
-      for (uint32_t j = rank; j < n_x; j += p.split) {
-        float sum = 0.0f;
-        for (uint32_t r = 0; r < p.split; ++r) sum += cluster_load(base + (j * kTileW + tid) * 4, r);
-        if (col < p.w_rows) y[(int64_t)j * p.ldy] = narrow<T>(sum * alpha);
+    if (tid < (uint32_t)kTileW && col < p.w_rows && !*abandoned)
+      for (uint32_t j = rank; j < p.x_rows; j += p.split) {
+        float v[8], sum = 0.0f;
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r) v[r] = r < p.split ? cluster_load(base + (j * kTileW + tid) * 4, r) : 0.0f;
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r) sum += v[r];
+        y[(int64_t)j * p.ldy] = narrow<T>(sum * alpha);
       }
-    }
     cluster_sync();
   }
   __syncthreads();
   if (warp == kMmaWarp) {
     tc_fence_after();
-    tmem_dealloc(tmem, p.tmem_cols);
+    tmem_dealloc(tmem, S::kTmem);
   }
 }
 
@@ -567,43 +572,25 @@ cudaError_t product_pairs(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, u
 
 template <typename T, int FMT>
 cudaError_t product(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
-  constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;
-  if (x.rows > 128) return product_pairs<T, FMT>(x, w, y, ldy, status, sm_count, stream);
+  using S = FewSizes<FMT>;
+  if (x.rows > (int32_t)kFewTokens) return product_pairs<T, FMT>(x, w, y, ldy, status, sm_count, stream);
   ProductParams p = {};
-  p.w_scales = w.scales, p.x_scales = x.scales, p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale;
-  p.y = y, p.ldy = ldy, p.status = status;
-  p.w_rows = (uint32_t)w.rows, p.x_rows = (uint32_t)x.rows, p.x_strips = (uint32_t)((x.rows + kStrip - 1) / kStrip);
+  p.w_codes = w.codes, p.w_scales = w.scales, p.x_scales = x.scales, p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale;
+  p.y = y, p.ldy = ldy, p.ldw = w.ld, p.status = status;
+  p.w_rows = (uint32_t)w.rows, p.x_rows = (uint32_t)x.rows, p.row_bytes = ((uint32_t)w.cols + 31) / 32 * 16;
   p.strip_bytes = strip_tiles(w.cols, block_of(FMT)) * kTileBytes;
   p.steps = (uint32_t)((w.cols + kSpan - 1) / kSpan);
-  p.tile_x = 16;
-  while (p.tile_x < 256 && p.tile_x < p.x_rows) p.tile_x *= 2;
-  p.x_tiles = (p.x_rows + p.tile_x - 1) / p.tile_x;
-  const uint32_t strips = (p.tile_x + kStrip - 1) / kStrip, sf_cols = KT * 4 * (1 + strips);
-  p.stage_bytes = (kTileW + p.tile_x) * kRowBytes + KT * kTileBytes * (1 + strips);
-  p.stage_bytes = (p.stage_bytes + 1023u) & ~1023u;
-  const bool two = p.tile_x <= 64;  // two blocks per SM
-  const uint32_t room = two ? 110 * 1024 : 224 * 1024;
-  p.stages = room / p.stage_bytes;
-  if (p.stages > (uint32_t)kMaxStages) p.stages = kMaxStages;
-  const uint32_t d_cols = p.tile_x < 32 ? 32 : p.tile_x;
-  while (p.stages > 1 && d_cols + p.stages * sf_cols > (two ? 256u : 512u)) --p.stages;
-  p.tmem_cols = 32;
-  while (p.tmem_cols < d_cols + p.stages * sf_cols) p.tmem_cols *= 2;
-  const uint64_t tiles = (uint64_t)((w.rows + kTileW - 1) / kTileW) * p.x_tiles;
+  const uint64_t tiles = (uint64_t)((w.rows + kTileW - 1) / kTileW);
   p.split = 1;
-  while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sm_count * (two ? 2 : 1) && p.split * 2 <= p.steps) p.split *= 2;
-  if (tiles * p.split > 0x7fffffffull) return cudaErrorInvalidConfiguration;
+  while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sm_count * 2 && p.split * 2 <= p.steps) p.split *= 2;
   const m1::WaitTestHook hook = m1::wait_test_hook();
   p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
   CUtensorMap w_map, x_map;
   cudaError_t e = make_map(&w_map, w.codes, 1, (uint64_t)w.rows, (uint64_t)(w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
-  if (e == cudaSuccess) e = make_map(&x_map, x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, p.tile_x);
+  if (e == cudaSuccess) e = make_map(&x_map, x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, kFewTokens);
   if (e == cudaSuccess) e = allow_smem<mx_product_kernel<T, FMT>>();
   if (e != cudaSuccess) return e;
-  size_t smem = (size_t)p.stages * p.stage_bytes;
-  if (p.split > 1 && smem < (size_t)p.tile_x * kTileW * 4) smem = (size_t)p.tile_x * kTileW * 4;
-  return launch_clusters(mx_product_kernel<T, FMT>, (unsigned)(tiles * p.split), p.split, kPThreads, smem + 1024, stream, w_map,
-                         x_map, p);
+  return launch_clusters(mx_product_kernel<T, FMT>, (unsigned)(tiles * p.split), p.split, kPThreads, S::kBytes, stream, w_map, x_map, p);
 }
 
 template <typename T>

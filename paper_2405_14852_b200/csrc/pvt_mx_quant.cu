@@ -203,8 +203,7 @@ __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int6
   }
 }
 
-// Eight elements to a lane.  (28672 x 8192 e8m0 to binary32 198 us, 164 at the copy's rate; four elements of 16 bytes to a lane
-// 219, two or four spans in flight 200.)
+// Eight elements to a lane; the next span's codes are asked for ahead of this one's stores.
 template <typename T, int FMT, bool WIDE>
 __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* codes, int64_t ld, const uint8_t* scales,
                                                                const float* tensor_scale, T* values, int64_t ldv, uint32_t rows,
@@ -216,39 +215,46 @@ __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* co
   pdl_wait();
   const uint32_t lane = threadIdx.x & 31;
   const float ts = FMT == PVT_MX_E4M3_16 && tensor_scale ? *tensor_scale : 1.0f;
-  for (uint32_t at = blockIdx.x * (kQThreads / 32) + threadIdx.x / 32; at < total; at += gridDim.x * (kQThreads / 32)) {
-    const uint32_t row = fast_div(at, spans_div), c0 = (at - row * spans) * kSpan + 8 * lane;
-    uint32_t word = 0, byte = 0;
-    if (c0 < cols) {  // (the four bytes lie in the row: ld is a multiple of 16)
+  const uint32_t warps = gridDim.x * (kQThreads / 32);
+  uint32_t row, c0, word, byte;
+  auto ask = [&](uint32_t at) {
+    row = fast_div(at, spans_div), c0 = (at - row * spans) * kSpan + 8 * lane, word = byte = 0;
+    if (at < total && c0 < cols) {  // (the four bytes lie in the row: ld is a multiple of 16)
       word = *reinterpret_cast<const uint32_t*>(codes + (int64_t)row * ld + c0 / 2);
       byte = scales[scale_at(row, c0 / BLOCK, tiles)];
     }
-    const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(byte) : e4m3_float(byte);
+  };
+  uint32_t next = blockIdx.x * (kQThreads / 32) + threadIdx.x / 32;
+  ask(next);
+  while (next < total) {
+    const uint32_t r = row, c = c0, w = word, b = byte;
+    ask(next += warps);
+    const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(b) : e4m3_float(b);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       // the three bits of the magnitude as the low exponent bits and the first fraction bit of a binary32, whose bias
       // is 126 more: a product with 2^126 gives the element, 0.5 from a number without its leading one included
-      const uint32_t c = word >> (4 * i);
-      const float el = __uint_as_float((c & 7u) << 22 | (c & 8u) << 28) * 8.507059173023462e37f;
+      const uint32_t n = w >> (4 * i);
+      const float el = __uint_as_float((n & 7u) << 22 | (n & 8u) << 28) * 8.507059173023462e37f;
       v[i] = el * s * ts;
     }
-    T* const to = values + (int64_t)row * ldv;
+    T* const to = values + (int64_t)r * ldv;
     if (!WIDE) {
       turn<true>(buffer[threadIdx.x / 32], v, lane);
-      const uint32_t span0 = c0 - 8 * lane;
+      const uint32_t span0 = c - 8 * lane;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (span0 + 32 * i + lane < cols) to[span0 + 32 * i + lane] = narrow<T>(v[i]);
-    } else if (c0 + 8 <= cols) {
+    } else if (c + 8 <= cols) {
       Eight<T> e;
 #pragma unroll
       for (int i = 0; i < 8; ++i) e.v[i] = narrow<T>(v[i]);
-      *reinterpret_cast<Eight<T>*>(to + c0) = e;
+      *reinterpret_cast<Eight<T>*>(to + c) = e;
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (c0 + i < cols) to[c0 + i] = narrow<T>(v[i]);
+        if (c + i < cols) to[c + i] = narrow<T>(v[i]);
     }
   }
 }
