@@ -247,10 +247,14 @@ __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* co
       for (int i = 0; i < 8; ++i)
         if (span0 + 32 * i + lane < cols) to[span0 + 32 * i + lane] = narrow<T>(v[i]);
     } else if (c + 8 <= cols) {
-      Eight<T> e;
+      if constexpr (sizeof(T) == 4) {
+        store8(to + c, true, v);
+      } else {
+        Eight<T> e;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e.v[i] = narrow<T>(v[i]);
-      *reinterpret_cast<Eight<T>*>(to + c) = e;
+        for (int i = 0; i < 8; ++i) e.v[i] = narrow<T>(v[i]);
+        *reinterpret_cast<Eight<T>*>(to + c) = e;
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -264,17 +268,20 @@ bool rows_aligned(const void* p, int64_t ld, size_t size) {
   return reinterpret_cast<uintptr_t>(p) % (8 * size) == 0 && ld % 8 == 0;
 }
 
-unsigned span_grid(uint32_t total, int sm_count) {
-  const uint32_t need = (total + kQThreads / 32 - 1) / (kQThreads / 32), most = (uint32_t)sm_count * 8;
+unsigned span_grid(uint32_t total, int per_sm, int sm_count) {
+  const uint32_t need = (total + kQThreads / 32 - 1) / (kQThreads / 32), most = (uint32_t)(sm_count * per_sm);
   return need < most ? need : most;
 }
+// Blocks per SM on the way back: as many as are resident, or many that follow one another where the values are far more than
+// the L2 holds (28672 x 8192 to binary32: 198 and 168 us, 8192 x 8192 57 and 51; 2047 x 5001 11.4 and 13.3).
+int blocks_back(uint32_t total) { return total > 150000 ? 64 : 8; }
 
 template <typename T, int FMT, bool WIDE>
 cudaError_t quantize(const pvt_mx& m, const T* x, int64_t ldx, int sm_count, cudaStream_t stream) {
   constexpr uint32_t span = 32 * kLaneElements<T, WIDE>;
   const uint32_t spans = ((uint32_t)m.cols + span - 1) / span;
   const uint32_t total = ((uint32_t)m.rows + kStrip - 1) / kStrip * kStrip * spans;
-  return launch_dependent(mx_quantize_kernel<T, FMT, WIDE>, span_grid(total, sm_count), kQThreads, 0, stream, x, ldx, m.codes,
+  return launch_dependent(mx_quantize_kernel<T, FMT, WIDE>, span_grid(total, 8, sm_count), kQThreads, 0, stream, x, ldx, m.codes,
                           m.ld, m.scales, m.tensor_scale, (uint32_t)m.rows, (uint32_t)m.cols,
                           strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans, total);
 }
@@ -288,7 +295,7 @@ template <typename T, int FMT>
 cudaError_t dequant(const pvt_mx& m, T* values, int64_t ldv, int sm_count, cudaStream_t stream) {
   const uint32_t spans = ((uint32_t)m.cols + kSpan - 1) / kSpan, total = (uint32_t)m.rows * spans;
   auto kernel = rows_aligned(values, ldv, sizeof(T)) ? mx_dequant_kernel<T, FMT, true> : mx_dequant_kernel<T, FMT, false>;
-  return launch_dependent(kernel, span_grid(total, sm_count), kQThreads, 0, stream, (const uint8_t*)m.codes, m.ld,
+  return launch_dependent(kernel, span_grid(total, blocks_back(total), sm_count), kQThreads, 0, stream, (const uint8_t*)m.codes, m.ld,
                           (const uint8_t*)m.scales, m.tensor_scale, values, ldv, (uint32_t)m.rows, (uint32_t)m.cols,
                           strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans, total);
 }
