@@ -11,7 +11,7 @@
 // Where there are tiles for all SMs a pair of blocks on neighbouring ones multiplies 512 rows of A by 128 columns of Q (two of
 // tcgen05.mma cta_group::2 with M = 256; where A has no more rows than that, 256 by 256).  Each block widens half the columns:
 // 64 rows cost it 4096 elements, about 100 cycles of its issue slots, beside products of 512 cycles.  The blocks stay and
-// take tile after tile: there are two sets of sums, four warps read one out while the other is added to.  A step takes 580 to
+// take tile after tile: there are two sets of sums, eight warps read one out while the other is added to.  A step takes 580 to
 // 640 cycles (2048 x 4096 by 11008: dx 124 us, dw 145; 112 at the rate of a library's 16-bit product).
 // Few tiles (few tokens, small layers) leave most SMs idle: then blocks by themselves multiply 128 rows by 128 columns, and
 // the steps of a tile are shared by a cluster of up to eight of them, whose partial sums meet in shared memory across the
@@ -90,20 +90,20 @@ __device__ __forceinline__ void widen32(const uint4& codes, uint32_t scales, Put
   }
 }
 
-constexpr int kGroups = 4, kGroupWarps = 4, kReaders = 4;  // warps
+constexpr int kGroups = 4, kGroupWarps = 4, kReaders = 8;  // warps
 constexpr int kWideners = kGroups * kGroupWarps;
 // (beside that many other warps one that copies takes 100 cycles and more for each instruction it issues: codes and A's tiles
 // have one each, or two)
 constexpr int kHeldWarp = kWideners + kReaders, kCopyWarp = kHeldWarp + 1, kMmaWarp = kCopyWarp + 2;
 constexpr int kThreads = (kMmaWarp + 1) * 32;
-constexpr uint32_t kMostStages = 5, kHeld = 8;  // steps of operands, of codes and scales
+constexpr uint32_t kStages = 4, kHeld = 8;      // steps of operands, of codes and scales
 constexpr uint32_t kSums = 256;                 // columns of tensor memory of a pair's set
 
 // CTAS: blocks that multiply together, MT: products of 128 CTAS rows per step
 template <int FMT, int MT, int CTAS>
 struct GradSizes {
   static constexpr uint32_t kRows = 128 * CTAS * MT, kCols = CTAS == 2 ? 256 / MT : 128, kHalf = kCols / CTAS;  // of a tile, of a block
-  static constexpr uint32_t kBBytes = kHalf * kStepR * 2, kStage = MT * kABytes + kBBytes, kStages = MT == 2 || CTAS == 1 ? 4 : 5;
+  static constexpr uint32_t kBBytes = kHalf * kStepR * 2, kStage = MT * kABytes + kBBytes;
   static constexpr uint32_t kCodeBytes = kHalf / 2 * kStepR;
   // scale tiles of 128 rows: those of kHalf columns, or the one they are half of
   static constexpr uint32_t kScaleCols = FMT == PVT_MX_E8M0_32 ? 128 : 64;
@@ -120,9 +120,9 @@ struct GradSizes {
 struct GradShared {
   alignas(8) uint64_t held[kHeld];     // of each block: codes and scales
   uint64_t held_empty[kHeld];          // of each: an arrival per warp of the group
-  uint64_t full_a[kMostStages];            // of the first: A's tiles of both
-  uint64_t full_b[kMostStages];            // of the first: an arrival per warp of both blocks' groups
-  uint64_t empty[kMostStages];             // of each
+  uint64_t full_a[kStages];            // of the first: A's tiles of both
+  uint64_t full_b[kStages];            // of the first: an arrival per warp of both blocks' groups
+  uint64_t empty[kStages];             // of each
   uint64_t sums_full[2];                   // of each
   uint64_t sums_empty[2];                  // of the first: an arrival per reading warp of both
   uint64_t spare;
@@ -253,7 +253,7 @@ template <typename T, int FMT, bool TRANS, int MT, int CTAS>
 __global__ void __launch_bounds__(kThreads, 1)
     mx_grad_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap q_map, const GradParams p) {
   using S = GradSizes<FMT, MT, CTAS>;
-  constexpr uint32_t STAGES = S::kStages;
+  constexpr uint32_t STAGES = kStages;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ GradShared sm;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -412,8 +412,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     const float alpha = kWidened<FMT> * (p.ts ? *p.ts : 1.0f);
-    const uint32_t quarter = warp % 4;
-    float* const turn = reinterpret_cast<float*>(mem + S::kTurnAt) + quarter * (32 * 33);
+    // (a warp reads the quarter of the lanes that its number gives it; the upper four have the second half of the columns)
+    const uint32_t quarter = warp % 4, half = (warp - kWideners) / 4;
+    float* const turn = reinterpret_cast<float*>(mem + S::kTurnAt) + (warp - kWideners) * (32 * 33);
     uint32_t n = 0;
     for (uint32_t tile = tile0; tile < p.tiles; tile += stride, ++n) {
       const uint32_t set = n & 1;
@@ -423,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t c0 = tile / p.a_tiles * S::kCols;
       if (CTAS == 1 && p.split > 1) {  // the products are done: the stages hold the partial sums
         float* const part = reinterpret_cast<float*>(mem) + (quarter * 32 + lane) * S::kPartPitch;
-        for (uint32_t j0 = 0; j0 < S::kCols; j0 += 32) {
+        for (uint32_t j0 = half * (S::kCols / 2); j0 < (half + 1) * (S::kCols / 2); j0 += 32) {
           uint32_t v[32];
           tmem_ld32(tmem + (quarter << 21) + j0, v);
           tmem_ld_wait<32>(v);
@@ -434,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       // 32 rows by 32 columns at a time, turned in shared memory so that a warp stores along a row
-      for (uint32_t j0 = 0; j0 < S::kCols * MT; j0 += 32) {
+      for (uint32_t j0 = half * (S::kCols * MT / 2); j0 < (half + 1) * (S::kCols * MT / 2); j0 += 32) {
         const uint32_t row0 = tile % p.a_tiles * S::kRows + j0 / S::kCols * 256 + rank * kTileA + quarter * 32, col0 = c0 + j0 % S::kCols;
         if (row0 >= p.a_rows || col0 >= p.cols) continue;
         const uint32_t n_rows = min(32u, p.a_rows - row0);
