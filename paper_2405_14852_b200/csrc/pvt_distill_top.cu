@@ -19,7 +19,6 @@ using namespace mma;
 
 constexpr int kParts = 8;           // of each thread, and keys of each lane that looks for a bound
 constexpr int kWarps = kThreads / 32;
-constexpr int kCandidates = 2048;   // that are put in order at once
 constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
 
 // Order of the list: larger keys first; NaN above all, -0 as 0.
@@ -43,7 +42,14 @@ struct TopParams {
   float* lse;
 };
 
+constexpr int kResidentFew = 6;  // blocks per SM where lists are short
+
+// MANY: lists of more than half as many as there are threads
+template <bool MANY>
 struct TopShared {
+  static constexpr uint32_t kCandidates = MANY ? 2048 : 512;  // that are put in order at once
+  static constexpr uint32_t kSorted = MANY ? PVT_DISTILL_MAX_K : kThreads;
+  static constexpr uint32_t kPieces = 2 * kSorted;            // that may hold them
   Running run[kWarps];
   Running mine;
   uint32_t bound[kWarps];
@@ -53,12 +59,13 @@ struct TopShared {
   uint32_t first[kThreads + 1];                  // place of a bucket's first entry
   alignas(8) uint64_t entries[kCandidates];
   uint64_t by_bucket[kCandidates];
-  uint64_t sorted[PVT_DISTILL_MAX_K];
+  uint64_t sorted[kSorted];
 };
 
 // The digit (8 bits) in which the `want`-th largest key falls, and how many keys have larger digits: hist[d] holds the number of
 // keys with digit d.  If there are fewer than `want` keys the digit is 0.
-__device__ __forceinline__ void find_digit(TopShared& sm, uint32_t want) {
+template <bool MANY>
+__device__ __forceinline__ void find_digit(TopShared<MANY>& sm, uint32_t want) {
   if (threadIdx.x < 32) {
     const uint32_t lane = threadIdx.x;
     uint32_t own[8], sum = 0;  // digits 255 - 8 lane downwards
@@ -101,7 +108,8 @@ __device__ __forceinline__ void for_each(const T* row, const RowShare<T>& s, F f
 // ahead of it in the bucket.  (300 / 1400 entries of a row among 4096: 16 / 75 us of a block's time by bitonic sort.)  Where
 // many keys are (nearly) equal buckets are long, and a bitonic sort takes over; its steps of up to 32 stay within the 64
 // entries of a warp.
-__device__ __forceinline__ void put_in_order(TopShared& sm, uint32_t n, uint32_t k, uint32_t most, uint32_t least) {
+template <bool MANY>
+__device__ __forceinline__ void put_in_order(TopShared<MANY>& sm, uint32_t n, uint32_t k, uint32_t most, uint32_t least) {
   constexpr uint32_t kLongBucket = 64;
   const uint32_t tid = threadIdx.x, lane = tid & 31;
   const float scale = (float)kThreads / ((float)(most - least) + 1.0f);
@@ -167,8 +175,8 @@ __device__ __forceinline__ void put_in_order(TopShared& sm, uint32_t n, uint32_t
 
 // The same for a row whose candidates are too many: the k-th largest key by its digits, every larger one, and of its equals those
 // with the lowest indices.
-template <typename T>
-__device__ __noinline__ uint32_t by_digits(TopShared& sm, const T* row, const RowShare<T>& s, uint32_t k) {
+template <typename T, bool MANY>
+__device__ __noinline__ uint32_t by_digits(TopShared<MANY>& sm, const T* row, const RowShare<T>& s, uint32_t k) {
   uint32_t prefix = 0, want = k;
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (uint32_t i = threadIdx.x; i < 256; i += kThreads) sm.hist[i] = 0;
@@ -183,7 +191,7 @@ __device__ __noinline__ uint32_t by_digits(TopShared& sm, const T* row, const Ro
     want -= sm.above;
     __syncthreads();
   }
-  // `want` of those equal to prefix (more than PVT_DISTILL_MAX_K elements reach the bound, so k exist above -infinity)
+  // `want` of those equal to prefix (more than kSorted elements reach the bound, so k exist above -infinity)
   if (threadIdx.x == 0) sm.count = 0;
   __syncthreads();
   for_each(row, s, [&](uint32_t key, uint32_t at) {
@@ -230,9 +238,10 @@ __device__ __forceinline__ uint32_t warp_bound(const uint32_t* key, uint32_t j) 
 }
 
 template <typename T, bool MANY>
-__global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const TopParams p) {
+__global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) distill_top_kernel(const TopParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
-  TopShared& sm = *reinterpret_cast<TopShared*>(raw);
+  using Shared = TopShared<MANY>;
+  Shared& sm = *reinterpret_cast<Shared*>(raw);
   pdl_trigger();
   pdl_wait();
   using Top = Tops<T>;
@@ -308,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const 
   const float least = value_of(bound);
   const auto limit = Top::limit(least);
   uint32_t* const reached = reinterpret_cast<uint32_t*>(sm.sorted);  // pieces whose largest element reaches it
-  constexpr uint32_t kPieces = sizeof(sm.sorted) / 4;
+  constexpr uint32_t kPieces = Shared::kPieces, kCandidates = Shared::kCandidates;
   auto look = [&](const Piece<T>& piece, uint32_t i) {
     if (Top::reaches(Top::of(piece), limit)) {
       const uint32_t n = atomicAdd(&sm.digit, 1u);
@@ -363,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const 
     cluster_sync();
     run = cluster_merge<false>(&sm.mine, p.blocks, p.c);
     // the other blocks' lists, side by side, behind this block's own memory
-    uint64_t* lists = reinterpret_cast<uint64_t*>(raw + sizeof(TopShared));
+    uint64_t* lists = reinterpret_cast<uint64_t*>(raw + sizeof(Shared));
     uint32_t size[kMaxBlocks];
 #pragma unroll
     for (uint32_t q = 0; q < kMaxBlocks; ++q)
@@ -412,14 +421,15 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_top_kernel(const 
 }
 
 template <typename T, bool MANY>
-cudaError_t top(const TopParams& p, int64_t rows, size_t smem, cudaStream_t stream) {
+cudaError_t top(const TopParams& p, int64_t rows, cudaStream_t stream) {
   const cudaError_t e = allow_smem<distill_top_kernel<T, MANY>>();
   if (e != cudaSuccess) return e;
+  const size_t smem = sizeof(TopShared<MANY>) + (p.blocks > 1 ? (size_t)p.blocks * p.k * 8 : 0);
   return launch_clusters(distill_top_kernel<T, MANY>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
 }
 template <typename T>
-cudaError_t top(const TopParams& p, int64_t rows, size_t smem, cudaStream_t stream) {
-  return p.k <= (uint32_t)kThreads / 2 ? top<T, false>(p, rows, smem, stream) : top<T, true>(p, rows, smem, stream);
+cudaError_t top(const TopParams& p, int64_t rows, cudaStream_t stream) {
+  return p.k <= (uint32_t)kThreads / 2 ? top<T, false>(p, rows, stream) : top<T, true>(p, rows, stream);
 }
 
 }  // namespace
@@ -433,11 +443,10 @@ cudaError_t launch_distill_top(const void* logits, int32_t dtype, int64_t ld, in
   p.top_idx = top_idx, p.top_logit = top_logit, p.lse = lse;
   p.blocks = row_blocks(rows, (int64_t)vocab * (dtype == PVT_F32 ? 4 : 2), sm_count);
   if (rows * p.blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  const size_t smem = sizeof(TopShared) + (p.blocks > 1 ? (size_t)p.blocks * p.k * 8 : 0);
   timing_begin(kKernDistill, stream);
-  const cudaError_t e = dtype == PVT_F32   ? top<float>(p, rows, smem, stream)
-                        : dtype == PVT_F16 ? top<__half>(p, rows, smem, stream)
-                                           : top<__nv_bfloat16>(p, rows, smem, stream);
+  const cudaError_t e = dtype == PVT_F32   ? top<float>(p, rows, stream)
+                        : dtype == PVT_F16 ? top<__half>(p, rows, stream)
+                                           : top<__nv_bfloat16>(p, rows, stream);
   timing_end(kKernDistill, stream);
   count_launches(1);
   return e;
