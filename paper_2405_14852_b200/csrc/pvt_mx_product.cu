@@ -239,8 +239,8 @@ constexpr int kPairReaders = 8;  // warps
 constexpr int kPairCopyWarps = 2;  // (a warp takes 100 cycles and more for each copy it issues)
 constexpr int kPairCopyWarp = kPairReaders, kPairMmaWarp = kPairCopyWarp + kPairCopyWarps;
 constexpr int kPairThreads = (kPairMmaWarp + 1) * 32;
-constexpr uint32_t kPairRows = 256;   // of w and of x
-constexpr uint32_t kPairStages = 5;
+constexpr uint32_t kPairRows = 256;   // of w
+constexpr uint32_t kPairStages = 7;   // at most
 
 struct PairShared {
   alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
@@ -264,28 +264,31 @@ struct PairParams {
   uint32_t max_spins, withhold;
 };
 
-template <int FMT>
+// N: rows of x in a tile
+template <int FMT, uint32_t N>
 struct PairSizes {
-  static constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;
-  static constexpr uint32_t kX = kTileW * kRowBytes, kWs = 2 * kX, kXs = kWs + KT * kTileBytes, kStage = kXs + 2 * KT * kTileBytes;
-  static constexpr uint32_t kStageAligned = (kStage + 1023) / 1024 * 1024;
-  static constexpr uint32_t kScaleCols = KT * 4 * 3;  // of a stage
-  static constexpr uint32_t kStages = kPairStages;
-  static_assert(256 + kStages * kScaleCols <= 512, "sums and scales fit tensor memory");
+  static constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4, kStrips = N / kStrip;
+  static constexpr uint32_t kX = kTileW * kRowBytes, kWs = kX + N / 2 * kRowBytes, kXs = kWs + KT * kTileBytes;
+  static constexpr uint32_t kStage = kXs + kStrips * KT * kTileBytes, kStageAligned = (kStage + 1023) / 1024 * 1024;
+  static constexpr uint32_t kScaleCols = KT * 4 * (1 + kStrips);  // of a stage
+  static constexpr uint32_t kStages = N == 256 ? 5 : 7;
+  static_assert(N + kStages * kScaleCols <= 512, "sums and scales fit tensor memory");
+  static constexpr size_t kBytes = kStages * kStageAligned + 1024;
+  static_assert(kBytes + 1024 <= 227 * 1024 && kStages <= kPairStages, "a block's shared memory");
 };
 
-// A step of a pair: its scales to tensor memory (two or four tiles for w's 128 rows, as many for each of two strips of x) and
-// the products of four times 64 columns.  One thread is elected for all of them, and descriptors are counted on inside:
+// A step of a pair: its scales to tensor memory (two or four tiles for w's 128 rows, as many for each of one or two strips of
+// x) and the products of four times 64 columns.  One thread is elected for all of them, and descriptors are counted on inside:
 // a tile of scales is 32 units of 16 bytes, four columns of tensor memory; 64 columns are 2 units of either operand.
-template <int FMT>
+template <int FMT, uint32_t STRIPS>
 __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                               uint64_t w_scales, uint64_t x_scales, uint32_t onto) {
-  if (FMT == PVT_MX_E8M0_32) {
+  if constexpr (FMT == PVT_MX_E8M0_32 && STRIPS == 2) {
     asm volatile(
         "{\n\t"
         ".reg .pred one, p, t;\n\t"
         ".reg .b32 s, x, i;\n\t"
-        ".reg .b64 q;\n\t"
+        ".reg .b64 q, a, b;\n\t"
         "elect.sync _|one, 0xffffffff;\n\t"
         "setp.ne.u32 p, %8, 0;\n\t"
         "setp.eq.u32 t, 0, 0;\n\t"
@@ -307,7 +310,6 @@ __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b
         "add.u32 x, %5, 12;\n\t"
         "add.s64 q, %7, 96;\n\t"
         "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        ".reg .b64 a, b;\n\t"
         "add.s64 a, %1, 0;\n\t"
         "add.s64 b, %2, 0;\n\t"
         "add.u32 s, %4, 0;\n\t"
@@ -334,12 +336,59 @@ __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b
         "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
         "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
         : "memory");
-  } else {
+  } else if constexpr (FMT == PVT_MX_E8M0_32) {
     asm volatile(
         "{\n\t"
         ".reg .pred one, p, t;\n\t"
         ".reg .b32 s, x, i;\n\t"
-        ".reg .b64 q;\n\t"
+        ".reg .b64 q, a, b;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %8, 0;\n\t"
+        "setp.eq.u32 t, 0, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.s64 q, %6, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "add.s64 q, %7, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.s64 q, %6, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 4;\n\t"
+        "add.s64 q, %7, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.s64 a, %1, 0;\n\t"
+        "add.s64 b, %2, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], p;\n\t"
+        "add.s64 a, %1, 2;\n\t"
+        "add.s64 b, %2, 2;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "or.b32 i, %3, 1073741856;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 4;\n\t"
+        "add.s64 b, %2, 4;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.u32 x, %5, 4;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 6;\n\t"
+        "add.s64 b, %2, 6;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.u32 x, %5, 4;\n\t"
+        "or.b32 i, %3, 1073741856;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
+        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
+        : "memory");
+  } else if constexpr (STRIPS == 2) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred one, p, t;\n\t"
+        ".reg .b32 s, x, i;\n\t"
+        ".reg .b64 q, a, b;\n\t"
         "elect.sync _|one, 0xffffffff;\n\t"
         "setp.ne.u32 p, %8, 0;\n\t"
         "setp.eq.u32 t, 0, 0;\n\t"
@@ -379,7 +428,6 @@ __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b
         "add.u32 x, %5, 28;\n\t"
         "add.s64 q, %7, 224;\n\t"
         "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        ".reg .b64 a, b;\n\t"
         "add.s64 a, %1, 0;\n\t"
         "add.s64 b, %2, 0;\n\t"
         "add.u32 s, %4, 0;\n\t"
@@ -406,14 +454,73 @@ __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b
         "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
         "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
         : "memory");
+  } else {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred one, p, t;\n\t"
+        ".reg .b32 s, x, i;\n\t"
+        ".reg .b64 q, a, b;\n\t"
+        "elect.sync _|one, 0xffffffff;\n\t"
+        "setp.ne.u32 p, %8, 0;\n\t"
+        "setp.eq.u32 t, 0, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.s64 q, %6, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "add.s64 q, %7, 0;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.s64 q, %6, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 4;\n\t"
+        "add.s64 q, %7, 32;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 8;\n\t"
+        "add.s64 q, %6, 64;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 8;\n\t"
+        "add.s64 q, %7, 64;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.u32 s, %4, 12;\n\t"
+        "add.s64 q, %6, 96;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
+        "add.u32 x, %5, 12;\n\t"
+        "add.s64 q, %7, 96;\n\t"
+        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
+        "add.s64 a, %1, 0;\n\t"
+        "add.s64 b, %2, 0;\n\t"
+        "add.u32 s, %4, 0;\n\t"
+        "add.u32 x, %5, 0;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], p;\n\t"
+        "add.s64 a, %1, 2;\n\t"
+        "add.s64 b, %2, 2;\n\t"
+        "add.u32 s, %4, 4;\n\t"
+        "add.u32 x, %5, 4;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 4;\n\t"
+        "add.s64 b, %2, 4;\n\t"
+        "add.u32 s, %4, 8;\n\t"
+        "add.u32 x, %5, 8;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
+        "add.s64 a, %1, 6;\n\t"
+        "add.s64 b, %2, 6;\n\t"
+        "add.u32 s, %4, 12;\n\t"
+        "add.u32 x, %5, 12;\n\t"
+        "or.b32 i, %3, 0;\n\t"
+        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
+        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
+        : "memory");
   }
 }
 
-template <typename T, int FMT>
+template <typename T, int FMT, uint32_t N>
 __global__ void __launch_bounds__(kPairThreads, 1)
     mx_product_pair_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
                            const __grid_constant__ CUtensorMap ws_map, const __grid_constant__ CUtensorMap xs_map, const PairParams p) {
-  using S = PairSizes<FMT>;
+  using S = PairSizes<FMT, N>;
   constexpr uint32_t KT = S::KT, STAGES = S::kStages;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ PairShared sm;
@@ -450,8 +557,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     uint32_t i = 0;
     bool ok = true;
     for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
-      const uint32_t tile0 = of_w ? tile / p.x_tiles * kPairRows : tile % p.x_tiles * kPairRows;
-      const int row = (int)(tile0 + rank * kTileW);
+      const uint32_t tile0 = of_w ? tile / p.x_tiles * kPairRows : tile % p.x_tiles * N;
+      const int row = (int)(tile0 + rank * (of_w ? kTileW : N / 2));
       const int strip = (int)((of_w ? (uint32_t)row : tile0) / kStrip * p.strip_rows);
       for (uint32_t step = 0; step < p.steps; ++step, ++i) {
         const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
@@ -463,10 +570,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           if (rank == 0) expect_bytes(smem_u32(&sm.full[s]), 2 * S::kStage);
           tma_load_pair(to, &w_map, col, row, bar);
           tma_load_pair(to + S::kWs, &ws_map, 0, scales, bar);
-        } else {  // both blocks multiply by all 256 rows of x
+        } else {  // both blocks multiply by all of the tile's rows of x
           tma_load_pair(to + S::kX, &x_map, col, row, bar);
           tma_load_pair(to + S::kXs, &xs_map, 0, scales, bar);
-          tma_load_pair(to + S::kXs + KT * kTileBytes, &xs_map, 0, scales + (int)p.strip_rows, bar);
+          if (S::kStrips == 2) tma_load_pair(to + S::kXs + KT * kTileBytes, &xs_map, 0, scales + (int)p.strip_rows, bar);
         }
       }
     }
@@ -475,9 +582,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
   } else if (warp == kPairMmaWarp) {
     if (rank == 0) {
-      // e2m1 both, N = 256, M = 256, type of the scales
+      // e2m1 both, N, M = 256, type of the scales
       constexpr uint32_t idesc =
-          1u << 7 | 1u << 10 | (kPairRows >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | (kPairRows >> 7) << 27;
+          1u << 7 | 1u << 10 | (N >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | (kPairRows >> 7) << 27;
       uint32_t i = 0, n = 0;
       bool ok = true;
       for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
@@ -488,9 +595,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t sfa = tmem + 256 + s * S::kScaleCols, sfb = sfa + KT * 4;
+          const uint32_t sfa = tmem + N + s * S::kScaleCols, sfb = sfa + KT * 4;
           // (a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart)
-          multiply_step<FMT>(tmem, operand(from, 16, 1024, true), operand(from + S::kX, 16, 1024, true), idesc, sfa, sfb,
+          multiply_step<FMT, S::kStrips>(tmem, operand(from, 16, 1024, true), operand(from + S::kX, 16, 1024, true), idesc, sfa, sfb,
                              operand(from + S::kWs, 0, 128, false), operand(from + S::kXs, 0, 128, false), (uint32_t)(step > 0));
           commit_pair(smem_u32(&sm.empty[s]));
           ++i;
@@ -513,22 +620,22 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       bool ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
       if (!ok) break;
       tc_fence_after();
-      uint32_t v[128];
+      uint32_t v[N / 2];
 #pragma unroll
-      for (int j = 0; j < 128; j += 32) tmem_ld32(tmem + (quarter << 21) + half * 128 + j, v + j);
-      tmem_ld_wait<128>(v);
+      for (uint32_t j = 0; j < N / 2; j += 32) tmem_ld32(tmem + (quarter << 21) + half * (N / 2) + j, v + j);
+      tmem_ld_wait<(int)N / 2>(v);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) cluster_arrive(sums_empty);
       __syncwarp();
       // lanes are consecutive outputs of a token
       const uint32_t col = tile / p.x_tiles * kPairRows + rank * kTileW + quarter * 32 + lane;
-      const uint32_t row = tile % p.x_tiles * kPairRows + half * 128;
+      const uint32_t row = tile % p.x_tiles * N + half * (N / 2);
       if (col < p.w_rows && row < p.x_rows) {
         T* y = static_cast<T*>(p.y) + (int64_t)row * p.ldy + col;
         const uint32_t rows = p.x_rows - row;
 #pragma unroll
-        for (uint32_t j = 0; j < 128; ++j) {
+        for (uint32_t j = 0; j < N / 2; ++j) {
           if (j < rows) *y = narrow<T>(__uint_as_float(v[j]) * alpha);
           y += p.ldy;
         }
@@ -543,37 +650,47 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   }
 }
 
-template <typename T, int FMT>
+template <typename T, int FMT, uint32_t N>
 cudaError_t product_pairs(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
-  using S = PairSizes<FMT>;
+  using S = PairSizes<FMT, N>;
   PairParams p = {};
   p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale, p.y = y, p.ldy = ldy, p.status = status;
   p.w_rows = (uint32_t)w.rows, p.x_rows = (uint32_t)x.rows;
   p.strip_rows = strip_tiles(w.cols, block_of(FMT)) * (kTileBytes / 128);
   p.steps = (uint32_t)((w.cols + kSpan - 1) / kSpan);
-  p.x_tiles = (p.x_rows + kPairRows - 1) / kPairRows;
+  p.x_tiles = (p.x_rows + N - 1) / N;
   p.tiles = (p.w_rows + kPairRows - 1) / kPairRows * p.x_tiles;
   const m1::WaitTestHook hook = m1::wait_test_hook();
   p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
   CUtensorMap maps[4];
   cudaError_t e = make_map(&maps[0], w.codes, 1, (uint64_t)w.rows, (uint64_t)(w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
-  if (e == cudaSuccess) e = make_map(&maps[1], x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, kTileW);
+  if (e == cudaSuccess) e = make_map(&maps[1], x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, N / 2);
   if (e == cudaSuccess) e = make_map(&maps[2], w.scales, 1, scale_bytes(w.rows, w.cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
   if (e == cudaSuccess) e = make_map(&maps[3], x.scales, 1, scale_bytes(x.rows, x.cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
-  if (e == cudaSuccess) e = allow_smem<mx_product_pair_kernel<T, FMT>>();
+  if (e == cudaSuccess) e = allow_smem<mx_product_pair_kernel<T, FMT, N>>();
   if (e != cudaSuccess) return e;
   uint32_t pairs = (uint32_t)sm_count / 2;
   if (pairs > p.tiles) pairs = p.tiles;
-  constexpr size_t smem = S::kStages * S::kStageAligned + 1024;
-  static_assert(smem + 1024 <= 227 * 1024, "a block's shared memory");
-  return launch_clusters(mx_product_pair_kernel<T, FMT>, 2 * pairs, 2, kPairThreads, smem, stream, maps[0], maps[1], maps[2], maps[3],
-                         p);
+  return launch_clusters(mx_product_pair_kernel<T, FMT, N>, 2 * pairs, 2, kPairThreads, S::kBytes, stream, maps[0], maps[1], maps[2],
+                         maps[3], p);
+}
+
+// Whether tiles of 128 rows of x serve better than 256: they take three quarters of the time, so where there are not more rounds
+// of them (256 tokens 4096 by 4096: 8.3 and 9.7 us, 64 tokens by 11008 8.1 and 9.3; 333 tokens 5119 by 13823, three rounds
+// and two: 22.9 and 19.5).
+bool narrow_tiles(int32_t x_rows, int32_t w_rows, int sm_count) {
+  const uint64_t pairs = (uint64_t)sm_count / 2, w_tiles = ((uint64_t)w_rows + kPairRows - 1) / kPairRows;
+  const uint64_t rounds_256 = (w_tiles * (((uint64_t)x_rows + 255) / 256) + pairs - 1) / pairs;
+  const uint64_t rounds_128 = (w_tiles * (((uint64_t)x_rows + 127) / 128) + pairs - 1) / pairs;
+  return rounds_128 * 3 < rounds_256 * 4;
 }
 
 template <typename T, int FMT>
 cudaError_t product(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
   using S = FewSizes<FMT>;
-  if (x.rows > (int32_t)kFewTokens) return product_pairs<T, FMT>(x, w, y, ldy, status, sm_count, stream);
+  if (x.rows > (int32_t)kFewTokens)
+    return narrow_tiles(x.rows, w.rows, sm_count) ? product_pairs<T, FMT, 128>(x, w, y, ldy, status, sm_count, stream)
+                                                  : product_pairs<T, FMT, 256>(x, w, y, ldy, status, sm_count, stream);
   ProductParams p = {};
   p.w_codes = w.codes, p.w_scales = w.scales, p.x_scales = x.scales, p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale;
   p.y = y, p.ldy = ldy, p.ldw = w.ld, p.status = status;
