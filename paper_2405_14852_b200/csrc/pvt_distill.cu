@@ -1,11 +1,12 @@
 // The distillation loss of a row and its gradient.
 //
-// The row is read once for its largest logit and the sum of exponentials relative to it (with the teacher's remaining mass as
-// one more outcome: also the sum over what is not listed, told from the rest by one bit per entry of the vocabulary in
-// shared memory, because the difference of the two sums would lose what a student near its teacher leaves there) and, for
+// The row is read once for its largest logit and the sum of exponentials relative to it and, for
 // the gradient, a second time, which the L2 serves: with y = 2^(c (x - largest)) every unlisted logit gets y times one factor.
 // The listed ones are overwritten after that.  What concerns the k listed entries alone, the teacher's probabilities and the loss, is
-// computed in binary64, where the remaining mass 1 - sum p is a small difference too.  Bound by HBM in long batches.
+// computed in binary64, where the remaining mass 1 - sum p is a small difference too.  With that mass as one more outcome
+// the pass sums what is not listed, told from the rest by one bit per entry of the vocabulary in shared memory, and the
+// listed exponentials are added in binary64: a sum of all less the listed ones would lose what a student near its teacher leaves
+// to the rest, and its loss, a small difference of log sums, is as good as the two sums agree.
 // A few long rows are shared by clusters of blocks.
 #include "pvt_distill.cuh"
 
@@ -152,8 +153,9 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       using Top = Tops<T>;
       auto add = [&](const Piece<T>& piece, uint32_t i) {
         const float sum = terms(piece, run.base(), p.c);
-        run.z += sum;
-        if (tail) {
+        if (!tail) {
+          run.z += sum;
+        } else {
           const uint32_t bit = (i + 1) * N, mask = listed[bit / 32] >> (bit % 32) & ((1u << N) - 1);
           if (mask == 0)
             run.r += sum;
@@ -184,8 +186,10 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
         const float x = widen<T>(row[at]);
         run.raise(x, p.c);
         const float y = run.term(x, p.c);
-        run.z += y;
-        if (tail && !(listed[bit / 32] >> (bit % 32) & 1u)) run.r += y;
+        if (!tail)
+          run.z += y;
+        else if (!(listed[bit / 32] >> (bit % 32) & 1u))
+          run.r += y;
       }
       run = block_merge<true>(run, p.c, sm.run);
     }
@@ -195,13 +199,20 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       run = cluster_merge<true>(&sm.mine, p.blocks, p.c);
       cluster_sync();
     }
+    double z = run.z;
+    if (active && tail) {
+      double own = 0.0;
+      for (uint32_t i = tid; i < k; i += kThreads)
+        if (sm.idx[i] >= 0 && sm.x[i] != kMinusInf) own += exp(((double)sm.x[i] - (double)run.base()) * p.inv_t);
+      z = (double)run.r + block_sum(own, sm.sum);
+    }
     // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
-    if (active && run.m == kMinusInf && run.z == 0.0f) active = false;
+    if (active && run.m == kMinusInf && z == 0.0) active = false;
 
     double value = 0.0;
     float f_listed = 0.0f, f_rest = 0.0f;
     if (active) {
-      const double z = run.z, log_z = log(z);
+      const double log_z = log(z);
       const double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
       if (rank == 0) {
         for (uint32_t i = tid; i < k; i += kThreads)
