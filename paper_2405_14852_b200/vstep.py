@@ -3,7 +3,8 @@
 All computation happens in the CUDA library (``binding``); this class only owns
 the device tensors, the workspace and the call order
 select -> encode -> dequantise of one step (Algorithm 3, V-step lines and
-``dequantize_weights``).
+``dequantize_weights``), and what a layer gives to and takes from the pass that its
+update comes from.
 """
 from __future__ import annotations
 
@@ -121,6 +122,19 @@ class VStepLayer:
         stats = torch.empty(2, dtype=torch.float64, device=self.W.device)
         B.pvt_vstep_trust(self.desc, k_max, ratio, idx, n, stats, self._ws)
         return idx, n, stats
+
+    def quantized(self, fmt: int = B.PVT_MX_E8M0_32, tensor_scale: Optional[torch.Tensor] = None,
+                  out: Optional[B.Mx] = None) -> B.Mx:
+        """The dequantised weights in 4-bit block floating point: what the forward and backward pass before the next V step
+        multiplies by (pvt_mx_product, pvt_mx_grad_input)."""
+        if out is None:
+            out = B.new_mx(self.rows, self.cols, fmt, tensor_scale, device=self.codes.device)
+        B.pvt_mx_quantize(out, self.dequant())
+        return out
+
+    def accumulate_grad(self, dy: torch.Tensor, x: B.Mx, first: bool = False) -> None:
+        """g += dy^T x (Algorithm 3: the gradient of every batch before the V step); with first g = dy^T x."""
+        B.pvt_mx_grad_weight(dy, x, self.g, accumulate=not first)
 
     def status(self) -> int:
         return B.pvt_status(self.reserve(1))
