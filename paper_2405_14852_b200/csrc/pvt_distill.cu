@@ -42,11 +42,19 @@ struct DistillParams {
 // the row has any effect
 enum { kStatMax = 0, kStatListed = 1, kStatRest = 2, kStatNorm = 3, kStatNormLow = 4, kStatActive = 5 };
 
+// What a warp has added up of the teacher's list: exponentials e = exp(a), a = logit / temperature - shift, and
+// e (a - (x - near) / temperature), near one of the student's logits there.
+struct Teacher {
+  double shift, mass, cross;
+  float near;
+  uint32_t any;  // an entry above -infinity
+};
+
 struct DistillShared {
   Running run[kThreads / 32];
   Running mine;
   double sum[kThreads / 32];
-  float top[kThreads / 32];
+  Teacher teacher[kThreads / 32];
   uint32_t repeated;
   float stat[PVT_DISTILL_STATS];
   int32_t idx[PVT_DISTILL_MAX_K];   // -1: left out
@@ -125,27 +133,36 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   }
 
   if (MODE & kLoss) {
-    // the teacher: logarithm of its sum, its probabilities' sum
-    double norm = 0.0, mass = 0.0;
+    // the teacher's sums of this warp's entries
     if (active) {
-      float top = kMinusInf;
+      float top = kMinusInf, near = kMinusInf;
+      bool any = false;
       for (uint32_t i = tid; i < k; i += kThreads)
-        if (sm.idx[i] >= 0) top = fmaxf(top, sm.val[i] == sm.val[i] ? sm.val[i] : -kMinusInf);  // (a NaN shows in the sum)
+        if (sm.idx[i] >= 0) {
+          top = fmaxf(top, sm.val[i]);
+          any |= sm.val[i] != kMinusInf;  // (a NaN shows in the sums)
+          if (sm.x[i] < -kMinusInf) near = fmaxf(near, sm.x[i]);
+        }
+      Teacher t = {};
+      t.any = __any_sync(0xffffffffu, any);
+      top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(top)));
+      near = from_ordered(__reduce_max_sync(0xffffffffu, ordered(near)));
+      t.near = near == kMinusInf ? 0.0f : near;
+      t.shift = tail ? (double)p.teacher_lse[r] : top == kMinusInf ? 0.0 : (double)top * p.inv_t;
+      for (uint32_t i = tid; i < k; i += kThreads)
+        if (sm.idx[i] >= 0) {
+          const double a = (double)sm.val[i] * p.inv_t - t.shift, e = exp(a);
+          t.mass += e;
+          if (e != 0.0) t.cross += e * (a - ((double)sm.x[i] - (double)t.near) * p.inv_t);
+        }
+      if (t.any) {
 #pragma unroll
-      for (int st = 16; st >= 1; st /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, st));
-      if ((tid & 31) == 0) sm.top[tid / 32] = top;
-      __syncthreads();
-      for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, sm.top[w]);
-      active = top != kMinusInf;
-      if (active) {
-        const double shift = tail ? (double)p.teacher_lse[r] : (double)top * p.inv_t;
-        double own = 0.0;
-        for (uint32_t i = tid; i < k; i += kThreads)
-          if (sm.idx[i] >= 0) own += exp((double)sm.val[i] * p.inv_t - shift);
-        mass = block_sum(own, sm.sum);
-        norm = shift;
-        if (!tail) norm += log(mass), mass = 1.0;
+        for (int st = 16; st >= 1; st /= 2) {
+          t.mass += __shfl_xor_sync(0xffffffffu, t.mass, st);
+          t.cross += __shfl_xor_sync(0xffffffffu, t.cross, st);
+        }
       }
+      if (tid % 32 == 0) sm.teacher[tid / 32] = t;
     }
 
     Running run;
@@ -206,37 +223,53 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
         if (sm.idx[i] >= 0 && sm.x[i] != kMinusInf) own += exp(((double)sm.x[i] - (double)run.base()) * p.inv_t);
       z = (double)run.r + block_sum(own, sm.sum);
     }
-    // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
-    if (active && run.m == kMinusInf && z == 0.0) active = false;
-
-    double value = 0.0;
-    float f_listed = 0.0f, f_rest = 0.0f;
-    if (active) {
-      const double log_z = log(z);
-      const double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
-      if (rank == 0) {
-        for (uint32_t i = tid; i < k; i += kThreads)
-          if (sm.idx[i] >= 0) {
-            const double log_p = (double)sm.val[i] * p.inv_t - norm, prob = exp(log_p);
-            const double log_q = ((double)sm.x[i] - (double)run.m) * p.inv_t - log_z;
-            if (prob != 0.0) value += prob * (log_p - log_q);
-          }
-        value = block_sum(value, sm.sum);
-        if (rest != 0.0) value += rest * (log(rest) - log((double)run.r) + log(z));
+    // One warp puts it together: the teacher's sums relative to the largest shift, the factors, the loss
+    //   sum p (log p - (x - largest) / T) + log z (P + p_rest) + p_rest (log p_rest - log r).
+    if (tid < 32) {
+      constexpr uint32_t kWarps = kThreads / 32;
+      double norm = 0.0, value = 0.0;
+      float f_listed = 0.0f, f_rest = 0.0f;
+      if (active) {
+        const Teacher t = sm.teacher[tid % kWarps];
+        double shift = t.any ? t.shift : (double)kMinusInf;
+#pragma unroll
+        for (int st = kWarps / 2; st >= 1; st /= 2) shift = fmax(shift, __shfl_xor_sync(0xffffffffu, shift, st));
+        const double by = t.any ? t.shift - shift : 0.0, f = t.any ? exp(by) : 0.0;
+        double mass = t.any ? f * t.mass : 0.0, cross = t.any ? f * (t.cross + (by + ((double)run.base() - (double)t.near) * p.inv_t) * t.mass) : 0.0;
+#pragma unroll
+        for (int st = kWarps / 2; st >= 1; st /= 2) {
+          mass += __shfl_xor_sync(0xffffffffu, mass, st);
+          cross += __shfl_xor_sync(0xffffffffu, cross, st);
+        }
+        // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
+        active = __any_sync(0xffffffffu, t.any) && !(run.m == kMinusInf && z == 0.0);
+        if (active) {
+          const double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
+          const double lane_log = log(tid == 0 ? z : tid == 1 ? mass : tid == 2 ? rest : (double)run.r);
+          const double log_z = __shfl_sync(0xffffffffu, lane_log, 0), log_mass = __shfl_sync(0xffffffffu, lane_log, 1);
+          const double log_rest = __shfl_sync(0xffffffffu, lane_log, 2), log_r = __shfl_sync(0xffffffffu, lane_log, 3);
+          const double listed = tail ? mass : 1.0, whole = listed + rest;
+          norm = tail ? shift : shift + log_mass;
+          value = (tail ? cross : cross / mass - log_mass) + log_z * whole;
+          if (rest != 0.0) value += rest * (log_rest - log_r);
+          f_listed = (float)(whole / z);
+          // nothing unlisted left in the student: no factor is needed there
+          f_rest = (float)(whole / z - (rest != 0.0 && run.r != 0.0f ? rest / (double)run.r : 0.0));
+        }
       }
-      const double whole = mass + rest;
-      f_listed = (float)(whole / z);
-      // nothing unlisted left in the student: no factor is needed there
-      f_rest = (float)(whole / z - (rest != 0.0 && run.r != 0.0f ? rest / (double)run.r : 0.0));
+      if (tid == 0) {
+        sm.stat[kStatMax] = run.m, sm.stat[kStatListed] = f_listed, sm.stat[kStatRest] = f_rest;
+        sm.stat[kStatNorm] = (float)norm, sm.stat[kStatNormLow] = (float)(norm - (double)(float)norm);
+        sm.stat[kStatActive] = active ? 1.0f : 0.0f, sm.stat[6] = sm.stat[7] = 0.0f;
+        if (rank == 0) p.loss[r] = active ? (float)((double)weight * value) : 0.0f;
+      }
+      __syncwarp();
+      if (rank == 0 && stats && tid < PVT_DISTILL_STATS) stats[tid] = sm.stat[tid];
     }
-    if (tid == 0) {
-      sm.stat[kStatMax] = run.m, sm.stat[kStatListed] = f_listed, sm.stat[kStatRest] = f_rest;
-      sm.stat[kStatNorm] = (float)norm, sm.stat[kStatNormLow] = (float)(norm - (double)(float)norm);
-      sm.stat[kStatActive] = active ? 1.0f : 0.0f, sm.stat[6] = sm.stat[7] = 0.0f;
-      if (rank == 0) p.loss[r] = active ? (float)((double)weight * value) : 0.0f;
+    if (MODE & kGrad) {
+      __syncthreads();
+      active = sm.stat[kStatActive] != 0.0f;
     }
-    __syncthreads();
-    if (rank == 0 && stats && tid < PVT_DISTILL_STATS) stats[tid] = sm.stat[tid];
   }
 
   if (MODE & kGrad) {
