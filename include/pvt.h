@@ -329,7 +329,7 @@ int pvt_vstep_block(const pvt_layer* layers, const uint64_t* k, int32_t n_layers
  * bits that order them, and the sign above), blocks of 16 or 32 along a row with one scale each.
  *   value[r, c] = element[r, c] * scale[r, c / block] * tensor_scale
  *   PVT_MX_E8M0_32: block 32, scale 2^(byte - 127), byte 255 = NaN; no tensor_scale (NULL).
- *   PVT_MX_E4M3_16: block 16, scale an 8-bit float e4m3 without its sign (byte 127 = NaN); tensor_scale one positive
+ *   PVT_MX_E4M3_16: block 16, scale an 8-bit float e4m3 whose sign is 0 (byte 127 = NaN); tensor_scale one positive
  *                   finite binary32 on the device, or NULL = 1.
  * codes: ceil(cols / 2) bytes per row, the element of the even column in the lower half; rows are ld bytes apart, ld a
  * multiple of 16, codes 16-byte aligned and rows * ld bytes readable.  After an odd last column the upper half is zero;
@@ -337,7 +337,8 @@ int pvt_vstep_block(const pvt_layer* layers, const uint64_t* k, int32_t n_layers
  * scales: pvt_mx_scale_bytes bytes, 16-byte aligned, all of them written by pvt_mx_quantize.  Tiles of 128 rows x 4
  * blocks, 512 bytes: byte 16 (r % 32) + 4 (r % 128 / 32) + b % 4 of tile (r / 128, b / 4) for block b of row r; the tiles
  * of a strip of 128 rows lie one after the other, as many as ceil(cols / 256) * 256 columns need (2 or 4 for each 256),
- * strip after strip.  Scales of rows and blocks that do not exist are 0.
+ * strip after strip.  Scales of rows and blocks that do not exist are 0.  ceil(rows / 128) * 128 * ceil(cols / 256) has to be
+ * below 2^31.
  */
 #define PVT_MX_E8M0_32 0
 #define PVT_MX_E4M3_16 1
@@ -361,7 +362,7 @@ size_t pvt_mx_scale_bytes(int32_t rows, int32_t cols, int32_t format);
  *   PVT_MX_E8M0_32: scale = 2^(floor(log2 a) - 2), at least 2^-127; a = 0: 2^-127
  *   PVT_MX_E4M3_16: scale = a / (6 tensor_scale) rounded to e4m3 (to nearest even, at most 448)
  *   element = x / (scale tensor_scale) rounded to e2m1 (to nearest, ties to the even code, at most 6 in magnitude);
- *             zero if the scale is zero.  The sign of x stays, of a zero too.
+ *             +0 if the scale is zero.  Otherwise the sign of x stays, of a zero too.
  * A block that holds a NaN or an infinity, and every block under a tensor_scale that is not positive and finite, has
  * scale NaN and elements 0.
  */
@@ -406,7 +407,7 @@ int pvt_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const pvt_mx* x,
  *                     listed: where fewer than k are left the list ends with index -1 and value -infinity.
  *   top_logit[r, i]:  their values in binary32.
  *   lse[r]:           log sum over the vocabulary of exp(logit / temperature), binary32; NULL if not wanted.
- * 1 <= k <= PVT_DISTILL_MAX_K, k <= vocab; temperature positive and finite.
+ * 1 <= k <= PVT_DISTILL_MAX_K, k <= vocab; temperature between 5e-39 and 3e38.
  */
 #define PVT_DISTILL_MAX_K 1024
 int pvt_distill_top(const void* logits, int32_t dtype, int64_t ld, int64_t rows, int32_t vocab, int32_t k,
@@ -431,7 +432,7 @@ typedef struct pvt_distill {
   const void* logits;         /* [rows][vocab] of dtype, rows ld elements apart */
   int64_t ld;
   int32_t dtype;              /* PVT_F32 | PVT_F16 | PVT_BF16 */
-  float temperature;          /* positive, finite */
+  float temperature;          /* between 5e-39 and 3e38 */
   const int32_t* top_idx;     /* [rows][k] */
   const float* top_logit;     /* [rows][k] */
   const float* teacher_lse;   /* [rows] or NULL */

@@ -23,6 +23,8 @@ bool shape_ok(int32_t rows, int32_t cols) {
   return rows > 0 && cols > 0 &&
          (((uint64_t)rows + 127) / 128 * 128) * (((uint64_t)cols + mx::kSpan - 1) / mx::kSpan) < (uint64_t)1 << 31;
 }
+// log2(e) / temperature is a binary32 number
+bool temperature_ok(float t) { return t > 0.0f && t <= 3.0e38f && 1.0f / t <= 2.0e38f; }
 bool format_ok(int32_t f) { return f == PVT_MX_E8M0_32 || f == PVT_MX_E4M3_16; }
 
 int check_mx(const pvt_mx* m) {
@@ -41,7 +43,7 @@ int check_distill(const pvt_distill* d) {
   if (!d || d->rows < 1 || d->rows > 0x7fffffff || d->vocab < 1 || d->vocab > PVT_DISTILL_MAX_VOCAB) return PVT_EINVAL;
   if (d->k < 1 || d->k > PVT_DISTILL_MAX_K) return PVT_EINVAL;
   if (!matrix_ok(d->logits, d->dtype, d->ld, d->vocab)) return PVT_EINVAL;
-  if (!(d->temperature > 0.0f && d->temperature <= 3.0e38f && 1.0f / d->temperature <= 3.0e38f)) return PVT_EINVAL;
+  if (!temperature_ok(d->temperature)) return PVT_EINVAL;
   if (!d->top_idx || !d->top_logit || !aligned(d->top_idx, 4) || !aligned(d->top_logit, 4)) return PVT_EINVAL;
   return aligned(d->teacher_lse, 4) && aligned(d->weight, 4) ? PVT_OK : PVT_EINVAL;
 }
@@ -108,7 +110,7 @@ int pvt_distill_top(const void* logits, int32_t dtype, int64_t ld, int64_t rows,
   if (rows < 1 || rows > 0x7fffffff || vocab < 1 || vocab > PVT_DISTILL_MAX_VOCAB) return PVT_EINVAL;
   if (k < 1 || k > PVT_DISTILL_MAX_K || k > vocab) return PVT_EINVAL;
   if (!matrix_ok(logits, dtype, ld, vocab)) return PVT_EINVAL;
-  if (!(temperature > 0.0f && temperature <= 3.0e38f && 1.0f / temperature <= 3.0e38f)) return PVT_EINVAL;
+  if (!temperature_ok(temperature)) return PVT_EINVAL;
   if (!top_idx || !top_logit || !aligned(top_idx, 4) || !aligned(top_logit, 4) || !aligned(lse, 4)) return PVT_EINVAL;
   const cudaError_t e = launch_distill_top(logits, dtype, ld, rows, vocab, k, temperature, top_idx, top_logit, lse,
                                            device_sm_count(), static_cast<cudaStream_t>(cuda_stream));

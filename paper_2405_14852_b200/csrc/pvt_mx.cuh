@@ -16,7 +16,7 @@ constexpr int kSpan = 256;       // columns that scales are laid out for at a ti
 inline int block_of(int format) { return format == PVT_MX_E8M0_32 ? 32 : 16; }
 // tiles of a strip
 __host__ __device__ inline uint32_t strip_tiles(int cols, int block) {
-  return (uint32_t)((cols + kSpan - 1) / kSpan) * (uint32_t)(kSpan / 4 / block);
+  return ((uint32_t)cols + kSpan - 1) / kSpan * (uint32_t)(kSpan / 4 / block);
 }
 inline size_t scale_bytes(int rows, int cols, int format) {
   return (size_t)((rows + kStrip - 1) / kStrip) * strip_tiles(cols, block_of(format)) * kTileBytes;
@@ -63,6 +63,18 @@ __device__ __forceinline__ float e4m3_float(uint32_t byte) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(two) : "h"((uint16_t)byte));
   return __low2float(*reinterpret_cast<const __half2*>(&two));
 }
+// What a sum is multiplied by, one after the other, for two factors of its terms: their product and 1, or both by themselves, the
+// larger one first, where the product is no normal number (a sum that is 0 stays 0, and no bits are lost).
+struct Factors {
+  float first, second;
+  __device__ __forceinline__ Factors(float a, float b) {
+    const float both = a * b;
+    const bool normal = both >= 1.17549435e-38f && both <= 3.40282347e38f;
+    first = normal ? both : a > b ? a : b;
+    second = normal ? 1.0f : a > b ? b : a;
+  }
+  __device__ __forceinline__ float operator()(float sum) const { return sum * first * second; }
+};
 // 2^(byte - 127); 255 is NaN
 __device__ __forceinline__ float e8m0_value(uint32_t byte) {
   return byte == 255 ? __uint_as_float(0x7fc00000u) : byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);

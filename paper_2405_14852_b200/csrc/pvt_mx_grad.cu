@@ -176,8 +176,7 @@ __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b
     asm volatile(
         "{\n\t"
         ".reg .pred one, p, t;\n\t"
-        ".reg .b32 e;\n\t"
-        ".reg .b64 a1, a2, a3, c0, c1, c2, c3, b1, b2, b3;\n\t"
+        ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
         "elect.sync _|one, 0xffffffff;\n\t"
         "setp.ne.u32 p, %4, 0;\n\t"
         "setp.eq.u32 t, 0, 0;\n\t"
@@ -198,8 +197,7 @@ __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b
     asm volatile(
         "{\n\t"
         ".reg .pred one, p, t;\n\t"
-        ".reg .b32 e;\n\t"
-        ".reg .b64 a1, a2, a3, c0, c1, c2, c3, b1, b2, b3;\n\t"
+        ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
         "elect.sync _|one, 0xffffffff;\n\t"
         "setp.ne.u32 p, %4, 0;\n\t"
         "setp.eq.u32 t, 0, 0;\n\t"
@@ -411,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       step = (step + kGroups) % steps;
     }
   } else {
-    const float alpha = kWidened<FMT> * (p.ts ? *p.ts : 1.0f);
+    const Factors alpha(kWidened<FMT>, p.ts ? *p.ts : 1.0f);
     // (a warp reads the quarter of the lanes that its number gives it; the upper four have the second half of the columns)
     const uint32_t quarter = warp % 4, half = (warp - kWideners) / 4;
     float* const turn = reinterpret_cast<float*>(mem + S::kTurnAt) + (warp - kWideners) * (32 * 33);
@@ -450,10 +448,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           T* out = static_cast<T*>(p.out) + (int64_t)row0 * p.ldo + col;
           if (sizeof(T) == 4 && p.accumulate) {
 #pragma unroll 8
-            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(widen<T>(out[(int64_t)r * p.ldo]) + turn[r * 33 + lane] * alpha);
+            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(widen<T>(out[(int64_t)r * p.ldo]) + alpha(turn[r * 33 + lane]));
           } else {
 #pragma unroll 8
-            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(turn[r * 33 + lane] * alpha);
+            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(alpha(turn[r * 33 + lane]));
           }
         }
         __syncwarp();
@@ -469,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (CTAS == 1 && p.split > 1) {
     // every block adds up the rows that are its share, always in the order of ranks
     if (warp < kWideners && !*abandoned) {
-      const float alpha = kWidened<FMT> * (p.ts ? *p.ts : 1.0f);
+      const Factors alpha(kWidened<FMT>, p.ts ? *p.ts : 1.0f);
       const uint32_t a0 = tile0 % p.a_tiles * S::kRows, c0 = tile0 / p.a_tiles * S::kCols;
       for (uint32_t r = in_cluster + warp * p.split; r < S::kRows && a0 + r < p.a_rows; r += kWideners * p.split) {
         T* const out = static_cast<T*>(p.out) + (int64_t)(a0 + r) * p.ldo + c0;
@@ -480,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (uint32_t q = 0; q < 8; ++q) v[q] = q < p.split ? cluster_load(base + (r * S::kPartPitch + j) * 4, q) : 0.0f;
 #pragma unroll
           for (uint32_t q = 0; q < 8; ++q) sum += v[q];
-          sum *= alpha;
+          sum = alpha(sum);
           if (c0 + j < p.cols) {
             if (sizeof(T) == 4 && p.accumulate) sum += widen<T>(out[j]);
             out[j] = narrow<T>(sum);
@@ -501,7 +499,7 @@ cudaError_t start(const CUtensorMap& a_map, GradParams p, const pvt_mx& q, int s
   using S = GradSizes<FMT, MT, CTAS>;
   p.a_tiles = (p.a_rows + S::kRows - 1) / S::kRows, p.tiles = p.a_tiles * ((p.cols + S::kCols - 1) / S::kCols);
   CUtensorMap q_map;
-  cudaError_t e = make_map(&q_map, q.codes, 1, (uint64_t)q.rows, (uint64_t)(q.cols + 1) / 2, (uint64_t)q.ld, kStepR, S::kHalf / 2, false);
+  cudaError_t e = make_map(&q_map, q.codes, 1, (uint64_t)q.rows, ((uint64_t)q.cols + 1) / 2, (uint64_t)q.ld, kStepR, S::kHalf / 2, false);
   if (e == cudaSuccess) e = allow_smem<mx_grad_kernel<T, FMT, TRANS, MT, CTAS>>();
   if (e != cudaSuccess) return e;
   uint32_t grid = 2 * (p.tiles < (uint32_t)sm_count / 2 ? p.tiles : (uint32_t)sm_count / 2), cluster = 2;

@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
   const uint32_t col = w0 + tid;
-  float alpha = 1.0f;
+  Factors alpha(1.0f, 1.0f);
   T* const y = static_cast<T*>(p.y) + col;
 
   if (warp == kCopyWarp) {
@@ -189,8 +189,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
     }
   } else {
     // lanes are consecutive outputs of a token
-    if (p.w_ts) alpha = *p.w_ts;
-    if (p.x_ts) alpha *= *p.x_ts;
+    if (p.w_ts || p.x_ts) alpha = Factors(p.w_ts ? *p.w_ts : 1.0f, p.x_ts ? *p.x_ts : 1.0f);
     float* const part = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
     if (wait(smem_u32(&sm.done), 0, abandoned, p.status, p.max_spins)) {
       tc_fence_after();
@@ -203,7 +202,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
         if (p.split > 1)
           part[j * kTileW + tid] = __uint_as_float(v[j]);
         else if (col < p.w_rows)
-          y[(int64_t)j * p.ldy] = narrow<T>(__uint_as_float(v[j]) * alpha);
+          y[(int64_t)j * p.ldy] = narrow<T>(alpha(__uint_as_float(v[j])));
       }
       tc_fence_before();
     }
@@ -218,7 +217,7 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
         for (uint32_t r = 0; r < 8; ++r) v[r] = r < p.split ? cluster_load(base + (j * kTileW + tid) * 4, r) : 0.0f;
 #pragma unroll
         for (uint32_t r = 0; r < 8; ++r) sum += v[r];
-        y[(int64_t)j * p.ldy] = narrow<T>(sum * alpha);
+        y[(int64_t)j * p.ldy] = narrow<T>(alpha(sum));
       }
     cluster_sync();
   }
@@ -610,9 +609,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       }
     }
   } else {
-    float alpha = 1.0f;
-    if (p.w_ts) alpha = *p.w_ts;
-    if (p.x_ts) alpha *= *p.x_ts;
+    const Factors alpha(p.w_ts ? *p.w_ts : 1.0f, p.x_ts ? *p.x_ts : 1.0f);
     const uint32_t quarter = warp % 4, half = warp / 4;
     const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), 0);
     uint32_t n = 0;
@@ -636,7 +633,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const uint32_t rows = p.x_rows - row;
 #pragma unroll
         for (uint32_t j = 0; j < N / 2; ++j) {
-          if (j < rows) *y = narrow<T>(__uint_as_float(v[j]) * alpha);
+          if (j < rows) *y = narrow<T>(alpha(__uint_as_float(v[j])));
           y += p.ldy;
         }
       }
@@ -657,14 +654,14 @@ cudaError_t product_pairs(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, u
   p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale, p.y = y, p.ldy = ldy, p.status = status;
   p.w_rows = (uint32_t)w.rows, p.x_rows = (uint32_t)x.rows;
   p.strip_rows = strip_tiles(w.cols, block_of(FMT)) * (kTileBytes / 128);
-  p.steps = (uint32_t)((w.cols + kSpan - 1) / kSpan);
+  p.steps = ((uint32_t)w.cols + kSpan - 1) / kSpan;
   p.x_tiles = (p.x_rows + N - 1) / N;
   p.tiles = (p.w_rows + kPairRows - 1) / kPairRows * p.x_tiles;
   const m1::WaitTestHook hook = m1::wait_test_hook();
   p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
   CUtensorMap maps[4];
-  cudaError_t e = make_map(&maps[0], w.codes, 1, (uint64_t)w.rows, (uint64_t)(w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
-  if (e == cudaSuccess) e = make_map(&maps[1], x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, N / 2);
+  cudaError_t e = make_map(&maps[0], w.codes, 1, (uint64_t)w.rows, ((uint64_t)w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
+  if (e == cudaSuccess) e = make_map(&maps[1], x.codes, 1, (uint64_t)x.rows, ((uint64_t)x.cols + 1) / 2, (uint64_t)x.ld, N / 2);
   if (e == cudaSuccess) e = make_map(&maps[2], w.scales, 1, scale_bytes(w.rows, w.cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
   if (e == cudaSuccess) e = make_map(&maps[3], x.scales, 1, scale_bytes(x.rows, x.cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
   if (e == cudaSuccess) e = allow_smem<mx_product_pair_kernel<T, FMT, N>>();
@@ -696,15 +693,15 @@ cudaError_t product(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_
   p.y = y, p.ldy = ldy, p.ldw = w.ld, p.status = status;
   p.w_rows = (uint32_t)w.rows, p.x_rows = (uint32_t)x.rows, p.row_bytes = ((uint32_t)w.cols + 31) / 32 * 16;
   p.strip_bytes = strip_tiles(w.cols, block_of(FMT)) * kTileBytes;
-  p.steps = (uint32_t)((w.cols + kSpan - 1) / kSpan);
+  p.steps = ((uint32_t)w.cols + kSpan - 1) / kSpan;
   const uint64_t tiles = (uint64_t)((w.rows + kTileW - 1) / kTileW);
   p.split = 1;
   while (p.split < 8 && tiles * p.split * 2 <= (uint64_t)sm_count * 2 && p.split * 2 <= p.steps) p.split *= 2;
   const m1::WaitTestHook hook = m1::wait_test_hook();
   p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
   CUtensorMap w_map, x_map;
-  cudaError_t e = make_map(&w_map, w.codes, 1, (uint64_t)w.rows, (uint64_t)(w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
-  if (e == cudaSuccess) e = make_map(&x_map, x.codes, 1, (uint64_t)x.rows, (uint64_t)(x.cols + 1) / 2, (uint64_t)x.ld, kFewTokens);
+  cudaError_t e = make_map(&w_map, w.codes, 1, (uint64_t)w.rows, ((uint64_t)w.cols + 1) / 2, (uint64_t)w.ld, kTileW);
+  if (e == cudaSuccess) e = make_map(&x_map, x.codes, 1, (uint64_t)x.rows, ((uint64_t)x.cols + 1) / 2, (uint64_t)x.ld, kFewTokens);
   if (e == cudaSuccess) e = allow_smem<mx_product_kernel<T, FMT>>();
   if (e != cudaSuccess) return e;
   return launch_clusters(mx_product_kernel<T, FMT>, (unsigned)(tiles * p.split), p.split, kPThreads, S::kBytes, stream, w_map, x_map, p);

@@ -65,12 +65,13 @@ __device__ __noinline__ uint32_t e4m3_exact(float amax, double six_ts) {
   }
   return c;
 }
-// the same by the quotient a little larger and a little smaller than computed, where that decides it
+// The same by the quotient a little larger and a little smaller than computed, where that decides it (and 6 tensor_scale and its
+// reciprocal are normal numbers).
 __device__ __forceinline__ uint32_t e4m3_scale(float amax, float ts, float inv) {
   const float q = amax * inv;
   uint16_t two;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(q * kLess), "f"(q * kMore));
-  return (two >> 8) == (two & 255u) && inv < 1e38f ? two & 127u : e4m3_exact(amax, 6.0 * (double)ts);
+  return (two >> 8) == (two & 255u) && inv > 1e-37f && inv < 1e38f ? two & 127u : e4m3_exact(amax, 6.0 * (double)ts);
 }
 
 // The span's elements from one of two orders to the other: eight consecutive ones in a lane, and (rows that no wide access can

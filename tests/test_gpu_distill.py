@@ -293,3 +293,20 @@ def test_captured_steps_share_nothing():
     torch.cuda.synchronize()
     # (a shift of all logits: rounding of bfloat16 aside nothing changes)
     assert ((loss - want[0]).abs() <= 0.1).all()
+
+
+def test_rows_further_apart_than_32_bits_count():
+    rows, vocab, k, apart = 3, 5000, 30, 2 ** 31 + 8
+    x = torch.empty(2 * apart + 8192, dtype=torch.bfloat16, device="cuda").as_strided((rows, vocab), (apart, 1))
+    x.copy_(torch.randn(rows, vocab, device="cuda", generator=torch.Generator("cuda").manual_seed(3)))
+    near = x.clone(memory_format=torch.contiguous_format).contiguous()
+    outs = []
+    for logits in (x, near):
+        idx, val, lse = (torch.empty(rows, k, dtype=torch.int32, device="cuda"), torch.empty(rows, k, device="cuda"),
+                         torch.empty(rows, device="cuda"))
+        B.pvt_distill_top(logits, idx, val, lse=lse)
+        d = B.make_distill(logits, idx, val * 0.5, teacher_lse=lse)
+        loss = torch.empty(rows, device="cuda")
+        B.pvt_distill_loss(d, loss, grad=logits)
+        outs.append((idx, val, lse, loss, logits))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))

@@ -255,3 +255,64 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_correct(what, tok
     assert status.item() == 0
     want = {"product": xv @ wv.T, "input": dy.double() @ wv, "weight": dy.double().T @ xv}[what]
     assert torch.equal(out, want.float())
+
+
+@pytest.mark.parametrize("tokens", [5, 200, 600])
+@pytest.mark.parametrize("one,other", [(1e25, 1e25), (1e-25, 1e-25), (1e30, 1e-30), (1e-44, 1e4), (3e38, 1.0), (1.0, 1e-41)])
+def test_tensor_scales_whose_product_is_no_number(one, other, tokens):
+    """Both roundings of the result are half a step each: 2^-22 of it in all, and half of the smallest number."""
+    fmt = B.PVT_MX_E4M3_16
+    x, xv = held(tokens, 80, fmt, 31, tensor_scale=one)
+    w, wv = held(704, 80, fmt, 32, tensor_scale=other)
+    x.codes[:3] = 0
+    xv[:3] = 0
+
+    def agree(got, sums, *scales):
+        # (scaled after the sums, which are exact: scaled terms would not cancel)
+        want = sums * math.prod(s.tensor_scale.item() for s in scales)
+        rounded = want.float().double()
+        near = (got.double() - want).abs() <= want.abs() * 2.0 ** -22 + 2.0 ** -149
+        return bool((near | (got.double() == rounded)).all())
+
+    y = torch.empty(tokens, 704, device="cuda")
+    B.pvt_mx_product(x, w, y)
+    assert agree(y, xv @ wv.T, x, w) and (y[:3] == 0).all()
+    dy = gradient(tokens, 704, 33) * 2.0 ** -20
+    dy[:2] = 0
+    dx = torch.empty(tokens, 80, device="cuda")
+    B.pvt_mx_grad_input(dy, w, dx)
+    assert agree(dx, dy.double() @ wv, w) and (dx[:2] == 0).all()
+    dw = torch.empty(704, 80, device="cuda")
+    B.pvt_mx_grad_weight(dy, x, dw)
+    assert agree(dw, dy.double().T @ xv, x)
+
+
+def test_calls_on_several_streams_at_once():
+    """Products and gradients of few and many tiles side by side: each takes tensor memory for itself, and results are those of
+    the same calls alone."""
+    jobs = []
+    for i, (tokens, inputs, outputs) in enumerate([(4, 2048, 4096), (600, 1024, 2048), (40, 3000, 1500), (1100, 700, 3000)]):
+        fmt = FORMATS[i % 2]
+        x, _ = held(tokens, inputs, fmt, 40 + i)
+        w, _ = held(outputs, inputs, fmt, 50 + i)
+        dy = gradient(tokens, outputs, 60 + i)
+        outs = [torch.empty(tokens, outputs, device="cuda"), torch.empty(tokens, inputs, device="cuda"),
+                torch.empty(outputs, inputs, device="cuda")]
+
+        def run(x=x, w=w, dy=dy, outs=outs):
+            B.pvt_mx_product(x, w, outs[0])
+            B.pvt_mx_grad_input(dy, w, outs[1])
+            B.pvt_mx_grad_weight(dy, x, outs[2])
+        run()
+        jobs.append((run, outs, [o.clone() for o in outs]))
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, (run, outs, _) in zip(streams, jobs):
+            with torch.cuda.stream(stream):
+                for o in outs:
+                    o.fill_(math.nan)
+                run()
+    torch.cuda.synchronize()
+    for _, outs, want in jobs:
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))

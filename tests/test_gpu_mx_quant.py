@@ -159,3 +159,41 @@ def test_codes_in_wider_rows_leave_what_lies_beside_them():
     got, _ = ref.unpack(wide[:, 16:64], scales, 5, 75, B.PVT_MX_E8M0_32)
     assert torch.equal(got, codes)
     assert (wide[:, :16] == 0x5a).all() and (wide[:, 16 + 38:] == 0x5a).all()
+
+
+@pytest.mark.parametrize("ts", [1.5e-45, 1e-40, 1.2e-38, 5.6e37, 6e37, 3.4e38])
+def test_tensor_scales_at_the_ends_of_the_range(ts):
+    """6 tensor_scale or its reciprocal is no normal number there."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    wide = torch.exp(torch.linspace(-100, 88, 70, device="cuda"))[:, None]
+    check(torch.rand(70, 64, device="cuda", generator=gen) * wide, B.PVT_MX_E4M3_16, ts)
+    check(torch.full((2, 48), 3.4e38, device="cuda"), B.PVT_MX_E4M3_16, ts)
+
+
+def test_rows_further_apart_than_32_bits_count():
+    """Elements and codes whose offsets pass 2^32 bytes."""
+    rows, cols, apart = 3, 700, 2 ** 31 + 64
+    codes = torch.empty(2 * apart + 4096, dtype=torch.uint8, device="cuda").as_strided((rows, 352), (apart, 1))
+    x = torch.empty(2 * apart + 4096, dtype=torch.bfloat16, device="cuda").as_strided((rows, cols), (apart, 1))
+    x.copy_(torch.randn(rows, cols, device="cuda", generator=torch.Generator("cuda").manual_seed(7)))
+    for fmt in (B.PVT_MX_E8M0_32, B.PVT_MX_E4M3_16):
+        scales = torch.empty(B.pvt_mx_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device="cuda")
+        m = B.make_mx(codes, scales, rows, cols, fmt)
+        B.pvt_mx_quantize(m, x)
+        want, want_scales = ref.quantize(x, fmt)
+        got, got_scales = ref.unpack(codes, scales, rows, cols, fmt)
+        assert torch.equal(got, want) and torch.equal(got_scales, want_scales)
+        v = ref.values(want, want_scales, fmt)
+        near = B.new_mx(rows, cols, fmt)
+        B.pvt_mx_quantize(near, torch.ones(rows, cols, device="cuda"))
+        y = torch.empty(rows, rows, device="cuda")
+        B.pvt_mx_product(m, near, y)
+        ones = ref.values(*ref.unpack(near.codes, near.scales, rows, cols, fmt), fmt)
+        assert ((y.double() - v @ ones.T).abs() <= (cols + 4) * 2.0 ** -23 * (v.abs() @ ones.T)).all()
+        far = torch.empty(2 * apart + 4096, dtype=torch.bfloat16, device="cuda").as_strided((rows, cols), (apart, 1))
+        B.pvt_mx_dequant(m, far)
+        assert torch.equal(far, v.bfloat16())
+        dy = torch.eye(rows, 8, dtype=torch.bfloat16, device="cuda")[:, :rows]
+        B.pvt_mx_grad_input(dy, m, far)
+        assert torch.equal(far, v.bfloat16())
+        del far

@@ -177,3 +177,16 @@ def test_the_reference_quantiser_takes_the_nearest_element_and_scale():
                 else:
                     top = block.abs().max()
                     assert table[scales[r, n]] * 4 <= top < table[scales[r, n]] * 8
+
+
+@pytest.mark.parametrize("fmt", [B.PVT_MX_E8M0_32, B.PVT_MX_E4M3_16])
+def test_scale_bytes_of_the_longest_rows(fmt):
+    cols = 2 ** 31 - 1
+    assert B.pvt_mx_scale_bytes(1, cols, fmt) == ref.scale_bytes(1, cols, fmt)
+
+
+def test_temperatures_whose_reciprocal_is_beyond_the_kernels_numbers():
+    """log2(e) / temperature has to be a finite binary32: at 3.4e-39 the reciprocal is, 1.44 times it is not."""
+    lib, d = B.lib(), distill(temperature=3.4e-39)
+    assert lib.pvt_distill_loss(ctypes.byref(d), 0x5000, None, None, None, 0, 0, None, None) == B.PVT_EINVAL
+    assert lib.pvt_distill_top(0x1000, B.PVT_F16, 100, 4, 100, 10, 3.4e-39, 0x2000, 0x3000, None, None) == B.PVT_EINVAL
