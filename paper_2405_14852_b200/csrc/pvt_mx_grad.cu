@@ -9,10 +9,11 @@
 // twice); A's tiles arrive by TMA, contiguous along r or along p as they lie.
 //
 // Where there are tiles for all SMs a pair of blocks on neighbouring ones multiplies 512 rows of A by 128 columns of Q (two of
-// tcgen05.mma cta_group::2 with M = 256; where A has no more rows than that, 256 by 256).  Each block widens half the columns:
-// 64 rows cost it 4096 elements, about 100 cycles of its issue slots, beside products of 512 cycles.  The blocks stay and
-// take tile after tile: there are two sets of sums, eight warps read one out while the other is added to.  A step takes 580 to
-// 640 cycles (2048 x 4096 by 11008: dx 124 us, dw 145; 112 at the rate of a library's 16-bit product).
+// tcgen05.mma cta_group::2 with M = 256; for dw, and where A has no more rows than that, 256 by 256).  Each block widens half
+// the columns: 64 rows cost it 4096 elements, about 100 cycles of its issue slots, beside products of 512 cycles.  The blocks
+// stay and take tile after tile: there are two sets of sums, eight warps read one out while the other is added to.  A step
+// takes 560 to 600 cycles: what an SM can take in, about 60 bytes a cycle (2048 x 4096 by 11008: dx 125 us, dw 141; 112 at the
+// rate of a library's 16-bit product).
 // Few tiles (few tokens, small layers) leave most SMs idle: then blocks by themselves multiply 128 rows by 128 columns, and
 // the steps of a tile are shared by a cluster of up to eight of them, whose partial sums meet in shared memory across the
 // cluster, always in the order of ranks.
@@ -370,7 +371,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t group = warp / kGroupWarps, in_group = tid % (kGroupWarps * 32);
     // 32 columns of one or two of the 64 rows, 32 apart
     constexpr uint32_t kChunks = S::kHalf / 32, kItems = kStepR * kChunks / (kGroupWarps * 32);
-    const uint32_t row = in_group / kChunks, chunk = in_group % kChunks, atom = chunk / 2;
+    // (eight neighbouring lanes have four rows of one 128-byte column of B: their stores meet no bank twice)
+    const uint32_t row = in_group / (8 * kChunks) * 8 + in_group / 2 % 4 + in_group / (4 * kChunks) % 2 * 4;
+    const uint32_t chunk = in_group % 2 + (kChunks == 4 ? in_group / 8 % 2 * 2 : 0), atom = chunk / 2;
     // steps of all this block's tiles
     const uint64_t left = tile0 < p.tiles ? (uint64_t)((p.tiles - tile0 + stride - 1) / stride) * steps : 0;
     uint32_t step = group % steps;
@@ -383,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t scales[kItems];
 #pragma unroll
       for (uint32_t it = 0; it < kItems; ++it) {
-        codes[it] = *reinterpret_cast<const uint4*>(held + (in_group + it * (kGroupWarps * 32)) * 16);
+        codes[it] = *reinterpret_cast<const uint4*>(held + (row * kChunks + chunk + it * (kGroupWarps * 32)) * 16);
         const uint32_t r = ((first + step) * kStepR + row + it * 32) % kStrip, at = S::kCodeBytes + r % 32 * 16 + r / 32 * 4;
         // (of 64 columns every other block has the upper half of a tile of four e8m0 scales)
         if (FMT == PVT_MX_E8M0_32)
@@ -527,7 +530,10 @@ cudaError_t grad(const void* dy, int64_t lddy, uint32_t a_rows, const pvt_mx& q,
   if (e != cudaSuccess) return e;
   const uint64_t pair_tiles = (uint64_t)((a_rows + 255) / 256) * ((p.cols + 255) / 256);
   if (a_rows <= (uint32_t)kTileA || pair_tiles < (uint64_t)sm_count / 4) return start<T, FMT, TRANS, 1, 1>(a_map, p, q, sm_count, stream);
-  return a_rows > 256 ? start<T, FMT, TRANS, 2, 2>(a_map, p, q, sm_count, stream) : start<T, FMT, TRANS, 1, 2>(a_map, p, q, sm_count, stream);
+  // (A's transpose comes in twice as many copies, and what a pair brings in per step bounds it: 2048 x 4096 by 11008, 512 by 128
+  // and 256 by 256: dx 125 and 128 us, dw 150 and 141)
+  if (TRANS || a_rows <= 256) return start<T, FMT, TRANS, 1, 2>(a_map, p, q, sm_count, stream);
+  return start<T, FMT, TRANS, TRANS ? 1 : 2, 2>(a_map, p, q, sm_count, stream);
 }
 
 }  // namespace
