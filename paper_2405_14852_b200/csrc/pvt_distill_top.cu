@@ -1,11 +1,11 @@
 // The k largest logits of each row, in order, and the logarithm of the sum of all exponentials.
 //
 // One pass over the row keeps, besides the running sum, the largest value of each of 256 or 2048 parts of it (one or eight per
-// thread).  The k-th largest of 256 maxima has at least k elements not below it, so everything that is listed is among the elements
-// that reach that bound; with parts in no relation to the values those are few more (74 for k = 64).  For k > 128 every
-// warp takes the j-th largest of its 256 maxima, j = ceil(k / warps), and the smallest of these serves.  A second pass
-// over the row, which comes from the L2, collects them (a piece of 16 bytes is dismissed by its largest element), and they
-// are put in order in shared memory.  A row in which too many elements reach the bound (equal ones, or a list nearly as
+// thread).  Every warp takes the j-th largest of its maxima, j = ceil(k / warps), and at least k elements reach the smallest of
+// these, so everything that is listed is among the elements that do; with parts in no relation to the values those are not
+// many more.  (The k-th largest of all 256 maxima leaves fewer, 74 for k = 64, but one warp finds it while the others
+// wait: 64 largest of 4096 x 32000 bf16 89 us, so 86.)  A second pass over the row, which comes from the L2, collects
+// them (a piece of 16 bytes is dismissed by its largest element), and they are put in order in shared memory.  A row in which too many elements reach the bound (equal ones, or a list nearly as
 // long as the parts are many) is settled by counting the digits of its keys instead.  A few long rows are shared by
 // clusters: each block lists its part, and an entry's place is its own plus those that the other blocks' lists hold
 // ahead of it.
@@ -53,7 +53,6 @@ struct TopShared {
   Running run[kWarps];
   Running mine;
   uint32_t bound[kWarps];
-  uint32_t part[kThreads];
   uint32_t hist[256];
   uint32_t digit, above, count, n;
   uint32_t first[kThreads + 1];                  // place of a bucket's first entry
@@ -220,21 +219,19 @@ __device__ __noinline__ uint32_t by_digits(TopShared<MANY>& sm, const T* row, co
   return k;
 }
 
-// the upper half of the j-th largest of the warp's keys (kParts in each lane), with zeros below
+// the upper half of the j-th largest of the warp's keys (PARTS in each lane), with zeros below
+template <uint32_t PARTS>
 __device__ __forceinline__ uint32_t warp_bound(const uint32_t* key, uint32_t j) {
-  uint32_t lo = 0, hi = 0x10000;  // at least j keys reach lo, fewer reach hi
-  while (hi - lo > 1) {
-    const uint32_t mid = (lo + hi) / 2;
+  uint32_t bound = 0;  // at least j keys reach it
+#pragma unroll
+  for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit /= 2) {
     uint32_t n = 0;
 #pragma unroll
-    for (int u = 0; u < kParts; ++u) n += key[u] >> 16 >= mid;
-    n = __reduce_add_sync(0xffffffffu, n);
-    if (n >= j)
-      lo = mid;
-    else
-      hi = mid;
+    for (uint32_t u = 0; u < PARTS; ++u) n += key[u] >= (bound | bit);
+    n = PARTS == 1 ? __popc(__ballot_sync(0xffffffffu, n)) : __reduce_add_sync(0xffffffffu, n);
+    if (n >= j) bound |= bit;
   }
-  return lo << 16;
+  return bound;
 }
 
 template <typename T, bool MANY>
@@ -289,28 +286,13 @@ __global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) dis
     run.z += run.term(loose, p.c);
   }
   if (tid == 0) sm.count = sm.digit = 0;
-  uint32_t bound;
-  if (MANY) {
-    uint32_t key[kParts];
+  uint32_t key[PARTS];
 #pragma unroll
-    for (int u = 0; u < kParts; ++u) key[u] = key_of(max_nan(Top::value(part[u % PARTS]), u ? kMinusInf : loose));
-    bound = warp_bound(key, (k + kWarps - 1) / kWarps);
-    if (tid % 32 == 0) sm.bound[tid / 32] = bound;
-    run = block_merge<false>(run, p.c, sm.run);
-    bound = __reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]);
-  } else {
-    sm.part[tid] = key_of(max_nan(Top::value(part[0]), loose));
-    run = block_merge<false>(run, p.c, sm.run);
-    if (tid < 32) {
-      uint32_t key[kParts];
-#pragma unroll
-      for (int u = 0; u < kParts; ++u) key[u] = sm.part[tid + 32 * u];
-      bound = warp_bound(key, k);
-      if (tid == 0) sm.bound[0] = bound;
-    }
-    __syncthreads();
-    bound = sm.bound[0];
-  }
+  for (uint32_t u = 0; u < PARTS; ++u) key[u] = key_of(max_nan(Top::value(part[u]), u ? kMinusInf : loose));
+  uint32_t bound = warp_bound<PARTS>(key, (k + kWarps - 1) / kWarps);
+  if (tid % 32 == 0) sm.bound[tid / 32] = bound;
+  run = block_merge<false>(run, p.c, sm.run);
+  bound = __reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]);
   if (tid == 0) sm.mine = run;
   // what is below reaches no place of the list; -infinity never does
   bound = max(bound, kLowest + 1);
