@@ -1,14 +1,17 @@
 // The k largest logits of each row, in order, and the logarithm of the sum of all exponentials.
 //
-// One pass over the row keeps, besides the running sum, the largest value of each of 256 or 2048 parts of it (one or eight per
-// thread).  Every warp takes the j-th largest of its maxima, j = ceil(k / warps), and at least k elements reach the smallest of
-// these, so everything that is listed is among the elements that do; with parts in no relation to the values those are not
-// many more.  (The k-th largest of all 256 maxima leaves fewer, 74 for k = 64, but one warp finds it while the others
-// wait: 64 largest of 4096 x 32000 bf16 89 us, so 86.)  A second pass over the row, which comes from the L2, collects
-// them (a piece of 16 bytes is dismissed by its largest element), and they are put in order in shared memory.  A row in which too many elements reach the bound (equal ones, or a list nearly as
-// long as the parts are many) is settled by counting the digits of its keys instead.  A few long rows are shared by
-// clusters: each block lists its part, and an entry's place is its own plus those that the other blocks' lists hold
-// ahead of it.
+// One pass over the row keeps, besides the running sum, the largest value of each of 2048 parts of it, eight per thread.  Every
+// warp takes the j-th largest of its maxima (of a thread's largest, for k up to 128), j = ceil(k / warps), and at least k
+// elements reach the smallest of these, so everything that is listed is among the elements that do; with parts in no relation
+// to the values those are not many more.  (The k-th largest of the block's 256 would leave fewer, 74 for k = 64, but one
+// warp finds it while the others wait.)  The pieces of the parts that reach it, 16 bytes each, are looked at once more, and
+// their candidates are put in order in shared memory.  (A second pass over the whole row, which the L2 served: 64 / 257
+// largest of 4096 x 32000 bf16 87 / 148 us, so 80 / 133.)  A row in which too many elements reach the bound (equal ones, or a
+// list nearly as long as the parts are many) is settled by counting the digits of its keys instead.  A few long rows are
+// shared by clusters: each block lists its part, and an entry's place is its own plus those that the other blocks' lists
+// hold ahead of it.
+// 4096 x 32000 bf16 are 40 us of HBM; instructions and the latencies of a block's steps take the rest, while six blocks of an SM
+// share its issue slots.
 #include "pvt_distill.cuh"
 
 namespace pvt {
@@ -17,7 +20,7 @@ namespace {
 using namespace distill;
 using namespace mma;
 
-constexpr int kParts = 8;           // of each thread, and keys of each lane that looks for a bound
+constexpr uint32_t kParts = 8;      // of each thread: runs of its pieces
 constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
 
@@ -49,15 +52,18 @@ template <bool MANY>
 struct TopShared {
   static constexpr uint32_t kCandidates = MANY ? 2048 : 512;  // that are put in order at once
   static constexpr uint32_t kSorted = MANY ? PVT_DISTILL_MAX_K : kThreads;
-  static constexpr uint32_t kPieces = 2 * kSorted;            // that may hold them
   Running run[kWarps];
   Running mine;
   uint32_t bound[kWarps];
   uint32_t hist[256];
   uint32_t digit, above, count, n;
   uint32_t first[kThreads + 1];                  // place of a bucket's first entry
+  uint32_t part[kParts * kThreads];              // largest elements of a part, a Top
   alignas(8) uint64_t entries[kCandidates];
-  uint64_t by_bucket[kCandidates];
+  union {
+    uint64_t by_bucket[kCandidates];
+    uint16_t reached[kParts * kThreads];         // parts that may hold candidates
+  };
   uint64_t sorted[kSorted];
 };
 
@@ -190,7 +196,7 @@ __device__ __noinline__ uint32_t by_digits(TopShared<MANY>& sm, const T* row, co
     want -= sm.above;
     __syncthreads();
   }
-  // `want` of those equal to prefix (more than kSorted elements reach the bound, so k exist above -infinity)
+  // `want` of those equal to prefix (more than kCandidates elements reach the bound, so k exist above -infinity)
   if (threadIdx.x == 0) sm.count = 0;
   __syncthreads();
   for_each(row, s, [&](uint32_t key, uint32_t at) {
@@ -242,43 +248,51 @@ __global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) dis
   pdl_trigger();
   pdl_wait();
   using Top = Tops<T>;
-  constexpr uint32_t N = Piece<T>::N, PARTS = MANY ? kParts : 1, UNROLL = MANY ? kParts : 4;
+  constexpr uint32_t N = Piece<T>::N, UNROLL = 4;
   const uint32_t tid = threadIdx.x, rank = blockIdx.x % p.blocks, r = blockIdx.x / p.blocks, k = p.k;
   const T* row = static_cast<const T*>(p.logits) + (int64_t)r * p.ld;
   const RowShare<T> s(row, p.vocab, rank, p.blocks);
   const Piece<T>* const pieces = reinterpret_cast<const Piece<T>*>(row + s.head);
 
+  // A thread's pieces are s.lo + tid + n kThreads; its part e are those with n >> lg = e.
+  uint32_t lg = 0;
+  while ((kParts << lg) * kThreads < s.hi - s.lo) ++lg;
+  typename Top::Top* const part = reinterpret_cast<typename Top::Top*>(sm.part) + tid;
   Running run;
-  typename Top::Top part[PARTS];
-#pragma unroll
-  for (uint32_t u = 0; u < PARTS; ++u) part[u] = Top::lowest();
+  uint32_t n = 0;
+  auto keep = [&](typename Top::Top m) {
+    typename Top::Top* const of = part + (n >> lg) * kThreads;
+    *of = n & ((1u << lg) - 1) ? Top::max(*of, m) : m;
+  };
   uint32_t i0 = s.lo + tid;
-  for (; i0 + (UNROLL - 1) * kThreads < s.hi; i0 += UNROLL * kThreads) {
+  for (; i0 + (UNROLL - 1) * kThreads < s.hi; i0 += UNROLL * kThreads, n += UNROLL) {
     Piece<T> piece[UNROLL];
 #pragma unroll
     for (uint32_t u = 0; u < UNROLL; ++u) piece[u] = pieces[i0 + u * kThreads];
-    auto top = Top::of(piece[0]);
-    if (MANY) part[0] = Top::max(part[0], top);
+    typename Top::Top m[UNROLL];
 #pragma unroll
-    for (uint32_t u = 1; u < UNROLL; ++u) {
-      const auto m = Top::of(piece[u]);
-      if (MANY) part[u % PARTS] = Top::max(part[u % PARTS], m);
-      top = Top::max(top, m);
+    for (uint32_t u = 0; u < UNROLL; ++u) m[u] = Top::of(piece[u]);
+    const auto low = Top::max(m[0], m[1]), high = Top::max(m[2], m[3]), top = Top::max(low, high);
+    if (lg >= 2) {
+      keep(top);
+    } else if (lg == 1) {
+      part[n / 2 * kThreads] = low, part[(n / 2 + 1) * kThreads] = high;
+    } else {
+#pragma unroll
+      for (uint32_t u = 0; u < UNROLL; ++u) part[(n + u) * kThreads] = m[u];
     }
-    if (!MANY) part[0] = Top::max(part[0], top);
     run.raise(Top::value(top), p.c);
 #pragma unroll
     for (uint32_t u = 0; u < UNROLL; ++u) run.z += terms(piece[u], run.base(), p.c);
   }
-#pragma unroll
-  for (uint32_t u = 0; u < UNROLL - 1; ++u) {
-    if (i0 + u * kThreads >= s.hi) break;
-    const Piece<T> piece = pieces[i0 + u * kThreads];
+  for (; i0 < s.hi; i0 += kThreads, ++n) {
+    const Piece<T> piece = pieces[i0];
     const auto m = Top::of(piece);
-    part[u % PARTS] = Top::max(part[u % PARTS], m);
+    keep(m);
     run.raise(Top::value(m), p.c);
     run.z += terms(piece, run.base(), p.c);
   }
+  const uint32_t parts = (n + (1u << lg) - 1) >> lg;  // of this thread
   float loose = kMinusInf;
   if (tid < s.loose()) {
     loose = widen<T>(row[s.loose_at(tid)]);
@@ -286,10 +300,19 @@ __global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) dis
     run.z += run.term(loose, p.c);
   }
   if (tid == 0) sm.count = sm.digit = 0;
-  uint32_t key[PARTS];
+  uint32_t bound;
+  if (MANY) {
+    uint32_t key[kParts];
 #pragma unroll
-  for (uint32_t u = 0; u < PARTS; ++u) key[u] = key_of(max_nan(Top::value(part[u]), u ? kMinusInf : loose));
-  uint32_t bound = warp_bound<PARTS>(key, (k + kWarps - 1) / kWarps);
+    for (uint32_t e = 0; e < kParts; ++e)
+      key[e] = key_of(max_nan(e < parts ? Top::value(part[e * kThreads]) : kMinusInf, e ? kMinusInf : loose));
+    bound = warp_bound<kParts>(key, (k + kWarps - 1) / kWarps);
+  } else {
+    auto all = Top::lowest();
+    for (uint32_t e = 0; e < parts; ++e) all = Top::max(all, part[e * kThreads]);
+    const uint32_t key = key_of(max_nan(Top::value(all), loose));
+    bound = warp_bound<1>(&key, (k + kWarps - 1) / kWarps);
+  }
   if (tid % 32 == 0) sm.bound[tid / 32] = bound;
   run = block_merge<false>(run, p.c, sm.run);
   bound = __reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]);
@@ -298,54 +321,45 @@ __global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) dis
   bound = max(bound, kLowest + 1);
   const float least = value_of(bound);
   const auto limit = Top::limit(least);
-  uint32_t* const reached = reinterpret_cast<uint32_t*>(sm.sorted);  // pieces whose largest element reaches it
-  constexpr uint32_t kPieces = Shared::kPieces, kCandidates = Shared::kCandidates;
-  auto look = [&](const Piece<T>& piece, uint32_t i) {
-    if (Top::reaches(Top::of(piece), limit)) {
-      const uint32_t n = atomicAdd(&sm.digit, 1u);
-      if (n < kPieces) reached[n] = i;
-    }
-  };
-  i0 = s.lo + tid;
-  for (; i0 + 3 * kThreads < s.hi; i0 += 4 * kThreads) {
-    Piece<T> piece[4];
-#pragma unroll
-    for (uint32_t u = 0; u < 4; ++u) piece[u] = pieces[i0 + u * kThreads];
-#pragma unroll
-    for (uint32_t u = 0; u < 4; ++u) look(piece[u], i0 + u * kThreads);
-  }
-  for (; i0 < s.hi; i0 += kThreads) look(pieces[i0], i0);
+  for (uint32_t e = 0; e < parts; ++e)
+    if (Top::reaches(part[e * kThreads], limit)) sm.reached[atomicAdd(&sm.digit, 1u)] = (uint16_t)(e * kThreads + tid);
   __syncthreads();
-  // their elements, one to a thread
-  const uint32_t n_reached = sm.digit;
-  const uint32_t elements = min(n_reached, kPieces) * N;
-  for (uint32_t i0 = tid; i0 < elements; i0 += 4 * kThreads) {
-    uint32_t at[4];
-    float x[4];
+  // their pieces, one to a thread
+  constexpr uint32_t kCandidates = Shared::kCandidates, AT_ONCE = MANY ? 4 : 1;
+  const uint32_t reached = sm.digit << lg;
+  for (uint32_t j0 = tid; j0 < reached; j0 += AT_ONCE * kThreads) {
+    uint32_t i[AT_ONCE];
+    Piece<T> piece[AT_ONCE];
 #pragma unroll
-    for (uint32_t u = 0; u < 4; ++u) {
-      const uint32_t i = i0 + u * kThreads;
-      at[u] = i < elements ? s.head + reached[i / N] * N + i % N : ~0u;
-      x[u] = i < elements ? widen<T>(row[at[u]]) : kMinusInf;
+    for (uint32_t u = 0; u < AT_ONCE; ++u) {
+      const uint32_t j = j0 + u * kThreads, which = j < reached ? sm.reached[j >> lg] : 0;
+      i[u] = s.lo + which % kThreads + ((which / kThreads << lg) + (j & ((1u << lg) - 1))) * kThreads;
+      if (j >= reached || i[u] >= s.hi) i[u] = ~0u;
+      if (i[u] != ~0u) piece[u] = pieces[i[u]];
     }
 #pragma unroll
-    for (uint32_t u = 0; u < 4; ++u) {
-      if (at[u] == ~0u || x[u] < least) continue;
-      const uint32_t n = atomicAdd(&sm.count, 1u);
-      if (n < kCandidates) sm.entries[n] = entry_of(key_of(x[u]), at[u]);
+    for (uint32_t u = 0; u < AT_ONCE; ++u) {
+      if (i[u] == ~0u || !Top::reaches(Top::of(piece[u]), limit)) continue;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) {
+        const float x = widen<T>(piece[u].v[e]);
+        if (x < least) continue;
+        const uint32_t place = atomicAdd(&sm.count, 1u);
+        if (place < kCandidates) sm.entries[place] = entry_of(key_of(x), s.head + i[u] * N + e);
+      }
     }
   }
   if (tid < s.loose()) {
     const float x = widen<T>(row[s.loose_at(tid)]);
     if (!(x < least)) {
-      const uint32_t n = atomicAdd(&sm.count, 1u);
-      if (n < kCandidates) sm.entries[n] = entry_of(key_of(x), s.loose_at(tid));
+      const uint32_t place = atomicAdd(&sm.count, 1u);
+      if (place < kCandidates) sm.entries[place] = entry_of(key_of(x), s.loose_at(tid));
     }
   }
   __syncthreads();
   const uint32_t found = sm.count;
-  uint32_t n = min(found, k);
-  if (n_reached <= kPieces && found <= kCandidates)
+  n = min(found, k);
+  if (found <= kCandidates)
     put_in_order(sm, found, k, key_of(run.m), bound);
   else
     n = by_digits(sm, row, s, k);
