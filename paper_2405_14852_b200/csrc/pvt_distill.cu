@@ -43,9 +43,10 @@ struct DistillParams {
 enum { kStatMax = 0, kStatListed = 1, kStatRest = 2, kStatNorm = 3, kStatNormLow = 4, kStatActive = 5 };
 
 // What a warp has added up of the teacher's list: exponentials e = exp(a), a = logit / temperature - shift, and
-// e (a - (x - near) / temperature), near one of the student's logits there.
+// e (a - (x - near) / temperature), near the largest of the student's logits there; with a remaining mass also
+// exp((x - near) / temperature).
 struct Teacher {
-  double shift, mass, cross;
+  double shift, mass, cross, own;
   float near;
   uint32_t any;  // an entry above -infinity
 };
@@ -53,25 +54,14 @@ struct Teacher {
 struct DistillShared {
   Running run[kThreads / 32];
   Running mine;
-  double sum[kThreads / 32];
   Teacher teacher[kThreads / 32];
   uint32_t repeated;
+  uint32_t next;                    // run of pieces of the gradient that no warp has taken yet
   float stat[PVT_DISTILL_STATS];
   int32_t idx[PVT_DISTILL_MAX_K];   // -1: left out
   float x[PVT_DISTILL_MAX_K];       // the student's logit there
   float val[PVT_DISTILL_MAX_K];
 };
-
-__device__ __forceinline__ double block_sum(double v, double* sh) {
-#pragma unroll
-  for (int s = 16; s >= 1; s /= 2) v += __shfl_xor_sync(0xffffffffu, v, s);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = 0.0;
-  for (int w = 0; w < kThreads / 32; ++w) v += sh[w];
-  return v;
-}
 
 // zeros over this block's share of the gradient
 template <typename G>
@@ -93,8 +83,13 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   G* const grad = MODE & kGrad ? static_cast<G*>(p.grad) + (int64_t)r * p.ldg : nullptr;
   const RowShare<T> s(row, p.vocab, rank, p.blocks);
   const Piece<T>* const pieces = reinterpret_cast<const Piece<T>*>(row + s.head);
-  const float weight = p.weight ? p.weight[r] : 1.0f;
   const bool tail = p.teacher_lse != nullptr;
+  // everything that is fetched by itself is asked for at once
+  const int32_t first_idx = tid < k ? p.top_idx[(int64_t)r * k + tid] : -1;
+  const float first_val = tid < k ? p.top_logit[(int64_t)r * k + tid] : 0.0f;
+  const float upstream = (MODE & kGrad) && p.upstream ? p.upstream[r] : 1.0f;
+  const float lse = (MODE & kLoss) && tail ? p.teacher_lse[r] : 0.0f;
+  const float weight = p.weight ? p.weight[r] : 1.0f;
   float* const stats = p.stats ? p.stats + (int64_t)r * PVT_DISTILL_STATS : nullptr;
 
   // (the same in all blocks of the row: they leave together)
@@ -102,21 +97,28 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   if (MODE == kGrad) active = active && stats[kStatActive] != 0.0f;
 
   // the list: entries outside the vocabulary or named before are left out
+  float first_x = 0.0f;
+  if (tid == 0) sm.next = 0;
   if (active) {
     for (uint32_t i = tid; i < (p.vocab + N + 31) / 32; i += kThreads) listed[i] = 0;
     if (tid == 0) sm.repeated = 0;
     __syncthreads();
     bool bad = false;
     for (uint32_t i = tid; i < k; i += kThreads) {
-      int32_t at = p.top_idx[(int64_t)r * k + i];
+      int32_t at = i == tid ? first_idx : p.top_idx[(int64_t)r * k + i];
       if (at >= (int32_t)p.vocab) bad = true, at = -1;
       if (at >= 0) {
         const uint32_t bit = (uint32_t)at + N - s.head;
         if (atomicOr(&listed[bit / 32], 1u << (bit % 32)) >> (bit % 32) & 1u) sm.repeated = 1;
       }
       sm.idx[i] = at < 0 ? -1 : at;
-      sm.val[i] = p.top_logit[(int64_t)r * k + i];
-      sm.x[i] = at >= 0 ? widen<T>(row[at]) : 0.0f;  // before any block writes the gradient over the logits
+      sm.val[i] = i == tid ? first_val : p.top_logit[(int64_t)r * k + i];
+      // before any block writes the gradient over the logits; a thread's first is looked at after the pass over the row
+      const float x = at >= 0 ? widen<T>(row[at]) : 0.0f;
+      if (i == tid)
+        first_x = x;
+      else
+        sm.x[i] = x;
     }
     __syncthreads();
     if (sm.repeated) {
@@ -132,39 +134,8 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
     if (bad && p.status) atomicOr(p.status, PVT_DEV_BAD_INDEX);
   }
 
+  float m = 0.0f, f_rest = 0.0f;  // of the row: largest logit, factor of what is not listed
   if (MODE & kLoss) {
-    // the teacher's sums of this warp's entries
-    if (active) {
-      float top = kMinusInf, near = kMinusInf;
-      bool any = false;
-      for (uint32_t i = tid; i < k; i += kThreads)
-        if (sm.idx[i] >= 0) {
-          top = fmaxf(top, sm.val[i]);
-          any |= sm.val[i] != kMinusInf;  // (a NaN shows in the sums)
-          if (sm.x[i] < -kMinusInf) near = fmaxf(near, sm.x[i]);
-        }
-      Teacher t = {};
-      t.any = __any_sync(0xffffffffu, any);
-      top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(top)));
-      near = from_ordered(__reduce_max_sync(0xffffffffu, ordered(near)));
-      t.near = near == kMinusInf ? 0.0f : near;
-      t.shift = tail ? (double)p.teacher_lse[r] : top == kMinusInf ? 0.0 : (double)top * p.inv_t;
-      for (uint32_t i = tid; i < k; i += kThreads)
-        if (sm.idx[i] >= 0) {
-          const double a = (double)sm.val[i] * p.inv_t - t.shift, e = exp(a);
-          t.mass += e;
-          if (e != 0.0) t.cross += e * (a - ((double)sm.x[i] - (double)t.near) * p.inv_t);
-        }
-      if (t.any) {
-#pragma unroll
-        for (int st = 16; st >= 1; st /= 2) {
-          t.mass += __shfl_xor_sync(0xffffffffu, t.mass, st);
-          t.cross += __shfl_xor_sync(0xffffffffu, t.cross, st);
-        }
-      }
-      if (tid % 32 == 0) sm.teacher[tid / 32] = t;
-    }
-
     Running run;
     if (active) {
       using Top = Tops<T>;
@@ -208,6 +179,42 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
         else if (!(listed[bit / 32] >> (bit % 32) & 1u))
           run.r += y;
       }
+      // the teacher's sums of this warp's entries
+      if (tid < k) sm.x[tid] = first_x;
+      float top = kMinusInf, near = kMinusInf;
+      bool any = false;
+      for (uint32_t i = tid; i < k; i += kThreads)
+        if (sm.idx[i] >= 0) {
+          top = fmaxf(top, sm.val[i]);
+          any |= sm.val[i] != kMinusInf;  // (a NaN shows in the sums)
+          if (sm.x[i] < -kMinusInf) near = fmaxf(near, sm.x[i]);
+        }
+      Teacher t = {};
+      t.any = __any_sync(0xffffffffu, any);
+      top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(top)));
+      near = from_ordered(__reduce_max_sync(0xffffffffu, ordered(near)));
+      t.near = near == kMinusInf ? 0.0f : near;
+      t.shift = tail ? (double)lse : top == kMinusInf ? 0.0 : (double)top * p.inv_t;
+      for (uint32_t i = tid; i < k; i += kThreads)
+        if (sm.idx[i] >= 0) {
+          const double a = (double)sm.val[i] * p.inv_t - t.shift, e = exp(a);
+          t.mass += e;
+          const double b = ((double)sm.x[i] - (double)t.near) * p.inv_t;
+          if (e != 0.0) t.cross += e * (a - b);
+          if (tail) t.own += exp(b);
+        }
+      if (t.any) {
+#pragma unroll
+        for (int st = 16; st >= 1; st /= 2) {
+          t.mass += __shfl_xor_sync(0xffffffffu, t.mass, st);
+          t.cross += __shfl_xor_sync(0xffffffffu, t.cross, st);
+        }
+      }
+      if (tail) {
+#pragma unroll
+        for (int st = 16; st >= 1; st /= 2) t.own += __shfl_xor_sync(0xffffffffu, t.own, st);
+      }
+      if (tid % 32 == 0) sm.teacher[tid / 32] = t;
       run = block_merge<true>(run, p.c, sm.run);
     }
     if (p.blocks > 1) {
@@ -216,13 +223,11 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       run = cluster_merge<true>(&sm.mine, p.blocks, p.c);
       cluster_sync();
     }
-    double z = run.z;
-    if (active && tail) {
-      double own = 0.0;
-      for (uint32_t i = tid; i < k; i += kThreads)
-        if (sm.idx[i] >= 0 && sm.x[i] != kMinusInf) own += exp(((double)sm.x[i] - (double)run.base()) * p.inv_t);
-      z = (double)run.r + block_sum(own, sm.sum);
-    }
+    bool any = false;
+    if (active) any = __any_sync(0xffffffffu, sm.teacher[tid % (kThreads / 32)].any);
+    // Without a remaining mass every logit's factor is 1 / z: the others go on to the gradient meanwhile.
+    const float f_all = 1.0f / run.z;
+    if (!tail) active = any && !(run.m == kMinusInf && run.z == 0.0f);
     // One warp puts it together: the teacher's sums relative to the largest shift, the factors, the loss
     //   sum p (log p - (x - largest) / T) + log z (P + p_rest) + p_rest (log p_rest - log r).
     if (tid < 32) {
@@ -241,8 +246,15 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
           mass += __shfl_xor_sync(0xffffffffu, mass, st);
           cross += __shfl_xor_sync(0xffffffffu, cross, st);
         }
-        // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
-        active = __any_sync(0xffffffffu, t.any) && !(run.m == kMinusInf && z == 0.0);
+        double z = run.z;
+        if (tail) {
+          z = t.own != 0.0 ? t.own * exp(((double)t.near - (double)run.base()) * p.inv_t) : 0.0;
+#pragma unroll
+          for (int st = kWarps / 2; st >= 1; st /= 2) z += __shfl_xor_sync(0xffffffffu, z, st);
+          z += (double)run.r;
+          // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
+          active = any && !(run.m == kMinusInf && z == 0.0);
+        }
         if (active) {
           const double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
           const double lane_log = log(tid == 0 ? z : tid == 1 ? mass : tid == 2 ? rest : (double)run.r);
@@ -252,9 +264,12 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
           norm = tail ? shift : shift + log_mass;
           value = (tail ? cross : cross / mass - log_mass) + log_z * whole;
           if (rest != 0.0) value += rest * (log_rest - log_r);
-          f_listed = (float)(whole / z);
-          // nothing unlisted left in the student: no factor is needed there
-          f_rest = (float)(whole / z - (rest != 0.0 && run.r != 0.0f ? rest / (double)run.r : 0.0));
+          f_listed = f_rest = f_all;
+          if (tail) {
+            f_listed = (float)(whole / z);
+            // nothing unlisted left in the student: no factor is needed there
+            f_rest = (float)(whole / z - (rest != 0.0 && run.r != 0.0f ? rest / (double)run.r : 0.0));
+          }
         }
       }
       if (tid == 0) {
@@ -267,24 +282,29 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       if (rank == 0 && stats && tid < PVT_DISTILL_STATS) stats[tid] = sm.stat[tid];
     }
     if (MODE & kGrad) {
-      __syncthreads();
-      active = sm.stat[kStatActive] != 0.0f;
+      m = run.m, f_rest = f_all;
+      if (tail) {
+        __syncthreads();
+        active = sm.stat[kStatActive] != 0.0f, f_rest = sm.stat[kStatRest];
+      }
     }
   }
 
   if (MODE & kGrad) {
     if (MODE == kGrad) {
       if (tid < PVT_DISTILL_STATS) sm.stat[tid] = stats[tid];
+      if (active && tid < k) sm.x[tid] = first_x;
       // in place: no block overwrites logits that another has yet to gather
       if (p.blocks > 1) cluster_sync();
       __syncthreads();
+      m = sm.stat[kStatMax], f_rest = sm.stat[kStatRest];
     }
     if (!active) {
       clear(grad, s.from(), s.to());
       return;
     }
-    const float up = (float)((double)weight * (p.upstream ? (double)p.upstream[r] : 1.0) * p.inv_t);
-    const float m = sm.stat[kStatMax], f_listed = sm.stat[kStatListed], f_rest = sm.stat[kStatRest] * up;
+    const float up = (float)((double)weight * (double)upstream * p.inv_t);
+    f_rest *= up;
     auto y_of = [&](float x) { return ex2((x - m) * p.c); };
     if (sizeof(G) == sizeof(T) && (reinterpret_cast<uintptr_t>(grad) - reinterpret_cast<uintptr_t>(row)) % 16 == 0) {
       const Two bb = two(-m, -m), cc = two(p.c, p.c), ff = two(f_rest, f_rest);
@@ -299,15 +319,23 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
         }
         to[i] = out;
       };
-      uint32_t i0 = s.lo + tid;
-      for (; i0 + (kUnroll - 1) * kThreads < s.hi; i0 += kUnroll * kThreads) {
-        Piece<T> piece[kUnroll];
+      // Run by run, as each warp gets there: one of them comes late.
+      const uint32_t lane = tid % 32;
+      for (;;) {
+        uint32_t run = 0;
+        if (lane == 0) run = atomicAdd(&sm.next, 1u);
+        const uint32_t i0 = s.lo + __shfl_sync(0xffffffffu, run, 0) * (kUnroll * 32) + lane;
+        if (i0 - lane >= s.hi) break;
+        if (i0 - lane + kUnroll * 32 <= s.hi) {
+          Piece<T> piece[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) piece[u] = pieces[i0 + u * kThreads];
+          for (int u = 0; u < kUnroll; ++u) piece[u] = pieces[i0 + u * 32];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) write(piece[u], i0 + u * kThreads);
+          for (int u = 0; u < kUnroll; ++u) write(piece[u], i0 + u * 32);
+        } else {
+          for (uint32_t i = i0; i < s.hi; i += 32) write(pieces[i], i);
+        }
       }
-      for (; i0 < s.hi; i0 += kThreads) write(pieces[i0], i0);
       if (tid < s.loose()) {
         const uint32_t at = s.loose_at(tid);
         grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
@@ -327,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
     }
     __syncthreads();
     const double norm = (double)sm.stat[kStatNorm] + (double)sm.stat[kStatNormLow];
+    const float f_listed = sm.stat[kStatListed];
     for (uint32_t i = tid; i < k; i += kThreads) {
       const int32_t at = sm.idx[i];
       if (at < 0 || (uint32_t)at < s.from() || (uint32_t)at >= s.to()) continue;
