@@ -17,6 +17,7 @@ using namespace distill;
 using namespace mma;
 
 constexpr int kUnroll = 4;  // pieces in flight per thread
+constexpr uint32_t kAsked = 128 * 1024;  // bytes of a row that are asked for ahead
 
 enum { kLoss = 1, kGrad = 2, kBoth = 3 };
 
@@ -83,6 +84,8 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   G* const grad = MODE & kGrad ? static_cast<G*>(p.grad) + (int64_t)r * p.ldg : nullptr;
   const RowShare<T> s(row, p.vocab, rank, p.blocks);
   const Piece<T>* const pieces = reinterpret_cast<const Piece<T>*>(row + s.head);
+  // the row is on its way while the list is looked at (4096 x 32000 bf16: 106 us without, 101 with)
+  if (tid == 0 && s.lo < s.hi) prefetch_l2(pieces + s.lo, min((s.hi - s.lo) * (uint32_t)sizeof(Piece<T>), kAsked));
   const bool tail = p.teacher_lse != nullptr;
   // everything that is fetched by itself is asked for at once
   const int32_t first_idx = tid < k ? p.top_idx[(int64_t)r * k + tid] : -1;
@@ -92,17 +95,16 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   const float weight = p.weight ? p.weight[r] : 1.0f;
   float* const stats = p.stats ? p.stats + (int64_t)r * PVT_DISTILL_STATS : nullptr;
 
+  for (uint32_t i = tid; i < (p.vocab + N + 31) / 32; i += kThreads) listed[i] = 0;
+  if (tid == 0) sm.next = 0, sm.repeated = 0;
+  __syncthreads();
   // (the same in all blocks of the row: they leave together)
   bool active = weight != 0.0f;
   if (MODE == kGrad) active = active && stats[kStatActive] != 0.0f;
 
   // the list: entries outside the vocabulary or named before are left out
-  float first_x = 0.0f;
-  if (tid == 0) sm.next = 0;
+  T first_x = narrow<T>(0.0f);
   if (active) {
-    for (uint32_t i = tid; i < (p.vocab + N + 31) / 32; i += kThreads) listed[i] = 0;
-    if (tid == 0) sm.repeated = 0;
-    __syncthreads();
     bool bad = false;
     for (uint32_t i = tid; i < k; i += kThreads) {
       int32_t at = i == tid ? first_idx : p.top_idx[(int64_t)r * k + i];
@@ -114,11 +116,10 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       sm.idx[i] = at < 0 ? -1 : at;
       sm.val[i] = i == tid ? first_val : p.top_logit[(int64_t)r * k + i];
       // before any block writes the gradient over the logits; a thread's first is looked at after the pass over the row
-      const float x = at >= 0 ? widen<T>(row[at]) : 0.0f;
-      if (i == tid)
-        first_x = x;
-      else
-        sm.x[i] = x;
+      if (i != tid)
+        sm.x[i] = at >= 0 ? widen<T>(row[at]) : 0.0f;
+      else if (at >= 0)
+        first_x = row[at];
     }
     __syncthreads();
     if (sm.repeated) {
@@ -180,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
           run.r += y;
       }
       // the teacher's sums of this warp's entries
-      if (tid < k) sm.x[tid] = first_x;
+      if (tid < k) sm.x[tid] = widen<T>(first_x);
       float top = kMinusInf, near = kMinusInf;
       bool any = false;
       for (uint32_t i = tid; i < k; i += kThreads)
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   if (MODE & kGrad) {
     if (MODE == kGrad) {
       if (tid < PVT_DISTILL_STATS) sm.stat[tid] = stats[tid];
-      if (active && tid < k) sm.x[tid] = first_x;
+      if (active && tid < k) sm.x[tid] = widen<T>(first_x);
       // in place: no block overwrites logits that another has yet to gather
       if (p.blocks > 1) cluster_sync();
       __syncthreads();
