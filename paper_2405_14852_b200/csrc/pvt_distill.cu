@@ -52,34 +52,39 @@ struct Teacher {
   uint32_t any;  // an entry above -infinity
 };
 
+template <int THREADS>
 struct DistillShared {
-  Running run[kThreads / 32];
+  Running run[THREADS / 32];
   Running mine;
-  Teacher teacher[kThreads / 32];
+  Teacher teacher[THREADS / 32];
   uint32_t repeated;
   uint32_t next;                    // run of pieces of the gradient that no warp has taken yet
   float stat[PVT_DISTILL_STATS];
-  int32_t idx[PVT_DISTILL_MAX_K];   // -1: left out
-  float x[PVT_DISTILL_MAX_K];       // the student's logit there
-  float val[PVT_DISTILL_MAX_K];
+  // behind it, k each: the list's entries, -1 for those that are left out; the student's logits there; the teacher's
+  __device__ __forceinline__ int32_t* idx() { return reinterpret_cast<int32_t*>(this + 1); }
+  __device__ __forceinline__ float* x(uint32_t k) { return reinterpret_cast<float*>(this + 1) + k; }
+  __device__ __forceinline__ float* val(uint32_t k) { return reinterpret_cast<float*>(this + 1) + 2 * k; }
 };
 
 // zeros over this block's share of the gradient
-template <typename G>
+template <int THREADS, typename G>
 __device__ __forceinline__ void clear(G* grad, uint32_t from, uint32_t to) {
-  for (uint32_t i = from + threadIdx.x; i < to; i += kThreads) grad[i] = narrow<G>(0.0f);
+  for (uint32_t i = from + threadIdx.x; i < to; i += THREADS) grad[i] = narrow<G>(0.0f);
 }
 
-template <typename T, typename G, int MODE>
-__global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const DistillParams p) {
+template <typename T, typename G, int MODE, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResidentNarrow) distill_kernel(const DistillParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
-  DistillShared& sm = *reinterpret_cast<DistillShared*>(raw);
+  using Shared = DistillShared<THREADS>;
+  Shared& sm = *reinterpret_cast<Shared*>(raw);
   // a bit per entry of the vocabulary, moved so that a piece's bits lie in one word: piece i has those from (i + 1) N on
-  uint32_t* const listed = reinterpret_cast<uint32_t*>(raw + sizeof(DistillShared));
+  uint32_t* const listed = reinterpret_cast<uint32_t*>(raw + sizeof(Shared) + 12 * (size_t)p.k);
   pdl_trigger();
   pdl_wait();
   constexpr uint32_t N = Piece<T>::N;
   const uint32_t tid = threadIdx.x, rank = blockIdx.x % p.blocks, r = blockIdx.x / p.blocks, k = p.k;
+  int32_t* const list_idx = sm.idx();
+  float *const list_x = sm.x(k), *const list_val = sm.val(k);
   const T* row = static_cast<const T*>(p.logits) + (int64_t)r * p.ld;
   G* const grad = MODE & kGrad ? static_cast<G*>(p.grad) + (int64_t)r * p.ldg : nullptr;
   const RowShare<T> s(row, p.vocab, rank, p.blocks);
@@ -95,7 +100,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   const float weight = p.weight ? p.weight[r] : 1.0f;
   float* const stats = p.stats ? p.stats + (int64_t)r * PVT_DISTILL_STATS : nullptr;
 
-  for (uint32_t i = tid; i < (p.vocab + N + 31) / 32; i += kThreads) listed[i] = 0;
+  for (uint32_t i = tid; i < (p.vocab + N + 31) / 32; i += THREADS) listed[i] = 0;
   if (tid == 0) sm.next = 0, sm.repeated = 0;
   __syncthreads();
   // (the same in all blocks of the row: they leave together)
@@ -106,30 +111,30 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   T first_x = narrow<T>(0.0f);
   if (active) {
     bool bad = false;
-    for (uint32_t i = tid; i < k; i += kThreads) {
+    for (uint32_t i = tid; i < k; i += THREADS) {
       int32_t at = i == tid ? first_idx : p.top_idx[(int64_t)r * k + i];
       if (at >= (int32_t)p.vocab) bad = true, at = -1;
       if (at >= 0) {
         const uint32_t bit = (uint32_t)at + N - s.head;
         if (atomicOr(&listed[bit / 32], 1u << (bit % 32)) >> (bit % 32) & 1u) sm.repeated = 1;
       }
-      sm.idx[i] = at < 0 ? -1 : at;
-      sm.val[i] = i == tid ? first_val : p.top_logit[(int64_t)r * k + i];
+      list_idx[i] = at < 0 ? -1 : at;
+      list_val[i] = i == tid ? first_val : p.top_logit[(int64_t)r * k + i];
       // before any block writes the gradient over the logits; a thread's first is looked at after the pass over the row
       if (i != tid)
-        sm.x[i] = at >= 0 ? widen<T>(row[at]) : 0.0f;
+        list_x[i] = at >= 0 ? widen<T>(row[at]) : 0.0f;
       else if (at >= 0)
         first_x = row[at];
     }
     __syncthreads();
     if (sm.repeated) {
       uint32_t again = 0;  // of this thread's entries
-      for (uint32_t i = tid, n = 0; i < k; i += kThreads, ++n)
+      for (uint32_t i = tid, n = 0; i < k; i += THREADS, ++n)
         for (uint32_t j = 0; j < i; ++j)
-          if (sm.idx[i] >= 0 && sm.idx[j] == sm.idx[i]) again |= 1u << n;
+          if (list_idx[i] >= 0 && list_idx[j] == list_idx[i]) again |= 1u << n;
       __syncthreads();
-      for (uint32_t i = tid, n = 0; i < k; i += kThreads, ++n)
-        if (again >> n & 1u) sm.idx[i] = -1, bad = true;
+      for (uint32_t i = tid, n = 0; i < k; i += THREADS, ++n)
+        if (again >> n & 1u) list_idx[i] = -1, bad = true;
       __syncthreads();
     }
     if (bad && p.status) atomicOr(p.status, PVT_DEV_BAD_INDEX);
@@ -154,18 +159,18 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
         }
       };
       uint32_t i0 = s.lo + tid;
-      for (; i0 + (kUnroll - 1) * kThreads < s.hi; i0 += kUnroll * kThreads) {
+      for (; i0 + (kUnroll - 1) * THREADS < s.hi; i0 += kUnroll * THREADS) {
         Piece<T> piece[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) piece[u] = pieces[i0 + u * kThreads];
+        for (int u = 0; u < kUnroll; ++u) piece[u] = pieces[i0 + u * THREADS];
         auto top = Top::of(piece[0]);
 #pragma unroll
         for (int u = 1; u < kUnroll; ++u) top = Top::max(top, Top::of(piece[u]));
         run.raise(Top::value(top), p.c);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) add(piece[u], i0 + u * kThreads);
+        for (int u = 0; u < kUnroll; ++u) add(piece[u], i0 + u * THREADS);
       }
-      for (; i0 < s.hi; i0 += kThreads) {
+      for (; i0 < s.hi; i0 += THREADS) {
         const Piece<T> piece = pieces[i0];
         run.raise(Top::value(Top::of(piece)), p.c);
         add(piece, i0);
@@ -181,14 +186,14 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
           run.r += y;
       }
       // the teacher's sums of this warp's entries
-      if (tid < k) sm.x[tid] = widen<T>(first_x);
+      if (tid < k) list_x[tid] = widen<T>(first_x);
       float top = kMinusInf, near = kMinusInf;
       bool any = false;
-      for (uint32_t i = tid; i < k; i += kThreads)
-        if (sm.idx[i] >= 0) {
-          top = fmaxf(top, sm.val[i]);
-          any |= sm.val[i] != kMinusInf;  // (a NaN shows in the sums)
-          if (sm.x[i] < -kMinusInf) near = fmaxf(near, sm.x[i]);
+      for (uint32_t i = tid; i < k; i += THREADS)
+        if (list_idx[i] >= 0) {
+          top = fmaxf(top, list_val[i]);
+          any |= list_val[i] != kMinusInf;  // (a NaN shows in the sums)
+          if (list_x[i] < -kMinusInf) near = fmaxf(near, list_x[i]);
         }
       Teacher t = {};
       t.any = __any_sync(0xffffffffu, any);
@@ -196,11 +201,11 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       near = from_ordered(__reduce_max_sync(0xffffffffu, ordered(near)));
       t.near = near == kMinusInf ? 0.0f : near;
       t.shift = tail ? (double)lse : top == kMinusInf ? 0.0 : (double)top * p.inv_t;
-      for (uint32_t i = tid; i < k; i += kThreads)
-        if (sm.idx[i] >= 0) {
-          const double a = (double)sm.val[i] * p.inv_t - t.shift, e = exp(a);
+      for (uint32_t i = tid; i < k; i += THREADS)
+        if (list_idx[i] >= 0) {
+          const double a = (double)list_val[i] * p.inv_t - t.shift, e = exp(a);
           t.mass += e;
-          const double b = ((double)sm.x[i] - (double)t.near) * p.inv_t;
+          const double b = ((double)list_x[i] - (double)t.near) * p.inv_t;
           if (e != 0.0) t.cross += e * (a - b);
           if (tail) t.own += exp(b);
         }
@@ -216,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
         for (int st = 16; st >= 1; st /= 2) t.own += __shfl_xor_sync(0xffffffffu, t.own, st);
       }
       if (tid % 32 == 0) sm.teacher[tid / 32] = t;
-      run = block_merge<true>(run, p.c, sm.run);
+      run = block_merge<true, THREADS>(run, p.c, sm.run);
     }
     if (p.blocks > 1) {
       if (tid == 0) sm.mine = run;
@@ -225,14 +230,14 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       cluster_sync();
     }
     bool any = false;
-    if (active) any = __any_sync(0xffffffffu, sm.teacher[tid % (kThreads / 32)].any);
+    if (active) any = __any_sync(0xffffffffu, sm.teacher[tid % (THREADS / 32)].any);
     // Without a remaining mass every logit's factor is 1 / z: the others go on to the gradient meanwhile.
     const float f_all = 1.0f / run.z;
     if (!tail) active = any && !(run.m == kMinusInf && run.z == 0.0f);
     // One warp puts it together: the teacher's sums relative to the largest shift, the factors, the loss
     //   sum p (log p - (x - largest) / T) + log z (P + p_rest) + p_rest (log p_rest - log r).
     if (tid < 32) {
-      constexpr uint32_t kWarps = kThreads / 32;
+      constexpr uint32_t kWarps = THREADS / 32;
       double norm = 0.0, value = 0.0;
       float f_listed = 0.0f, f_rest = 0.0f;
       if (active) {
@@ -294,14 +299,14 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
   if (MODE & kGrad) {
     if (MODE == kGrad) {
       if (tid < PVT_DISTILL_STATS) sm.stat[tid] = stats[tid];
-      if (active && tid < k) sm.x[tid] = widen<T>(first_x);
+      if (active && tid < k) list_x[tid] = widen<T>(first_x);
       // in place: no block overwrites logits that another has yet to gather
       if (p.blocks > 1) cluster_sync();
       __syncthreads();
       m = sm.stat[kStatMax], f_rest = sm.stat[kStatRest];
     }
     if (!active) {
-      clear(grad, s.from(), s.to());
+      clear<THREADS>(grad, s.from(), s.to());
       return;
     }
     const float up = (float)((double)weight * (double)upstream * p.inv_t);
@@ -345,44 +350,49 @@ __global__ void __launch_bounds__(kThreads, kResident) distill_kernel(const Dist
       // rows of unlike alignment: element by element, a warp along the row
       const uint32_t to = s.to();
       uint32_t at = s.from() + tid;
-      for (; at + 7 * kThreads < to; at += 8 * kThreads) {
+      for (; at + 7 * THREADS < to; at += 8 * THREADS) {
         float x[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = widen<T>(row[at + u * kThreads]);
+        for (int u = 0; u < 8; ++u) x[u] = widen<T>(row[at + u * THREADS]);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) grad[at + u * kThreads] = narrow<G>(y_of(x[u]) * f_rest);
+        for (int u = 0; u < 8; ++u) grad[at + u * THREADS] = narrow<G>(y_of(x[u]) * f_rest);
       }
-      for (; at < to; at += kThreads) grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
+      for (; at < to; at += THREADS) grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
     }
     __syncthreads();
     const double norm = (double)sm.stat[kStatNorm] + (double)sm.stat[kStatNormLow];
     const float f_listed = sm.stat[kStatListed];
-    for (uint32_t i = tid; i < k; i += kThreads) {
-      const int32_t at = sm.idx[i];
+    for (uint32_t i = tid; i < k; i += THREADS) {
+      const int32_t at = list_idx[i];
       if (at < 0 || (uint32_t)at < s.from() || (uint32_t)at >= s.to()) continue;
-      const float prob = (float)exp((double)sm.val[i] * p.inv_t - norm);
-      grad[at] = narrow<G>((y_of(sm.x[i]) * f_listed - prob) * up);
+      const float prob = (float)exp((double)list_val[i] * p.inv_t - norm);
+      grad[at] = narrow<G>((y_of(list_x[i]) * f_listed - prob) * up);
     }
   }
 }
 
-template <typename T, typename G, int MODE>
+template <typename T, typename G, int MODE, int THREADS>
 cudaError_t start(const DistillParams& p, int64_t rows, cudaStream_t stream) {
-  const cudaError_t e = allow_smem<distill_kernel<T, G, MODE>>();
+  const cudaError_t e = allow_smem<distill_kernel<T, G, MODE, THREADS>>();
   if (e != cudaSuccess) return e;
-  const size_t smem = sizeof(DistillShared) + (size_t)(p.vocab + Piece<T>::N + 31) / 32 * 4;
-  return launch_clusters(distill_kernel<T, G, MODE>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
+  const size_t smem = sizeof(DistillShared<THREADS>) + 12 * (size_t)p.k + (size_t)(p.vocab + Piece<T>::N + 31) / 32 * 4;
+  return launch_clusters(distill_kernel<T, G, MODE, THREADS>, (unsigned)(rows * p.blocks), p.blocks, THREADS, smem, stream, p);
+}
+template <typename T, typename G, int MODE>
+cudaError_t start(const DistillParams& p, int64_t rows, int sm_count, cudaStream_t stream) {
+  return short_rows(rows, (int64_t)p.vocab * sizeof(T), sm_count) ? start<T, G, MODE, kNarrow>(p, rows, stream)
+                                                                   : start<T, G, MODE, kWide>(p, rows, stream);
 }
 template <typename T, int MODE>
-cudaError_t by_grad(const DistillParams& p, int64_t rows, int32_t grad_dtype, cudaStream_t stream) {
-  return grad_dtype == PVT_F32   ? start<T, float, MODE>(p, rows, stream)
-         : grad_dtype == PVT_F16 ? start<T, __half, MODE>(p, rows, stream)
-                                 : start<T, __nv_bfloat16, MODE>(p, rows, stream);
+cudaError_t by_grad(const DistillParams& p, int64_t rows, int32_t grad_dtype, int sm_count, cudaStream_t stream) {
+  return grad_dtype == PVT_F32   ? start<T, float, MODE>(p, rows, sm_count, stream)
+         : grad_dtype == PVT_F16 ? start<T, __half, MODE>(p, rows, sm_count, stream)
+                                 : start<T, __nv_bfloat16, MODE>(p, rows, sm_count, stream);
 }
 template <typename T>
-cudaError_t by_mode(const DistillParams& p, int64_t rows, int32_t grad_dtype, cudaStream_t stream) {
-  if (!p.grad) return start<T, T, kLoss>(p, rows, stream);
-  return p.loss ? by_grad<T, kBoth>(p, rows, grad_dtype, stream) : by_grad<T, kGrad>(p, rows, grad_dtype, stream);
+cudaError_t by_mode(const DistillParams& p, int64_t rows, int32_t grad_dtype, int sm_count, cudaStream_t stream) {
+  if (!p.grad) return start<T, T, kLoss>(p, rows, sm_count, stream);
+  return p.loss ? by_grad<T, kBoth>(p, rows, grad_dtype, sm_count, stream) : by_grad<T, kGrad>(p, rows, grad_dtype, sm_count, stream);
 }
 
 cudaError_t launch(const pvt_distill& d, DistillParams& p, int32_t grad_dtype, int sm_count, cudaStream_t stream) {
@@ -392,9 +402,9 @@ cudaError_t launch(const pvt_distill& d, DistillParams& p, int32_t grad_dtype, i
   p.blocks = row_blocks(d.rows, (int64_t)d.vocab * (d.dtype == PVT_F32 ? 4 : 2), sm_count);
   if (d.rows * p.blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
   timing_begin(kKernDistill, stream);
-  const cudaError_t e = d.dtype == PVT_F32   ? by_mode<float>(p, d.rows, grad_dtype, stream)
-                        : d.dtype == PVT_F16 ? by_mode<__half>(p, d.rows, grad_dtype, stream)
-                                             : by_mode<__nv_bfloat16>(p, d.rows, grad_dtype, stream);
+  const cudaError_t e = d.dtype == PVT_F32   ? by_mode<float>(p, d.rows, grad_dtype, sm_count, stream)
+                        : d.dtype == PVT_F16 ? by_mode<__half>(p, d.rows, grad_dtype, sm_count, stream)
+                                             : by_mode<__nv_bfloat16>(p, d.rows, grad_dtype, sm_count, stream);
   timing_end(kKernDistill, stream);
   count_launches(1);
   return e;

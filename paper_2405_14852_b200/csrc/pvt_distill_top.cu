@@ -21,7 +21,6 @@ using namespace distill;
 using namespace mma;
 
 constexpr uint32_t kParts = 8;      // of each thread: runs of its pieces
-constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
 
 // Order of the list: larger keys first; NaN above all, -0 as 0.
@@ -47,11 +46,14 @@ struct TopParams {
 
 constexpr int kResidentFew = 6;  // blocks per SM where lists are short
 
-// MANY: lists of more than half as many as there are threads
-template <bool MANY>
+// Few: lists of up to half as many as there are threads; many: longer ones, up to kMost
+template <int THREADS>
+constexpr uint32_t kMost = THREADS == kWide ? PVT_DISTILL_MAX_K : 2 * THREADS;
+template <bool MANY, int THREADS>
 struct TopShared {
-  static constexpr uint32_t kCandidates = MANY ? 2048 : 512;  // that are put in order at once
-  static constexpr uint32_t kSorted = MANY ? PVT_DISTILL_MAX_K : kThreads;
+  static constexpr int kThreads = THREADS, kWarps = THREADS / 32;
+  static constexpr uint32_t kCandidates = MANY ? 8 * THREADS : THREADS == kWide ? 512 : 256;  // that are put in order at once
+  static constexpr uint32_t kSorted = MANY ? kMost<THREADS> : THREADS;
   Running run[kWarps];
   Running mine;
   uint32_t bound[kWarps];
@@ -69,8 +71,8 @@ struct TopShared {
 
 // The digit (8 bits) in which the `want`-th largest key falls, and how many keys have larger digits: hist[d] holds the number of
 // keys with digit d.  If there are fewer than `want` keys the digit is 0.
-template <bool MANY>
-__device__ __forceinline__ void find_digit(TopShared<MANY>& sm, uint32_t want) {
+template <typename Shared>
+__device__ __forceinline__ void find_digit(Shared& sm, uint32_t want) {
   if (threadIdx.x < 32) {
     const uint32_t lane = threadIdx.x;
     uint32_t own[8], sum = 0;  // digits 255 - 8 lane downwards
@@ -95,7 +97,7 @@ __device__ __forceinline__ void find_digit(TopShared<MANY>& sm, uint32_t want) {
   __syncthreads();
 }
 
-template <typename T, typename F>
+template <int kThreads, typename T, typename F>
 __device__ __forceinline__ void for_each(const T* row, const RowShare<T>& s, F f) {
   for (uint32_t i = s.lo + threadIdx.x; i < s.hi; i += kThreads) {
     const Piece<T> p = *reinterpret_cast<const Piece<T>*>(row + s.head + i * Piece<T>::N);
@@ -113,8 +115,9 @@ __device__ __forceinline__ void for_each(const T* row, const RowShare<T>& s, F f
 // ahead of it in the bucket.  (300 / 1400 entries of a row among 4096: 16 / 75 us of a block's time by bitonic sort.)  Where
 // many keys are (nearly) equal buckets are long, and a bitonic sort takes over; its steps of up to 32 stay within the 64
 // entries of a warp.
-template <bool MANY>
-__device__ __forceinline__ void put_in_order(TopShared<MANY>& sm, uint32_t n, uint32_t k, uint32_t most, uint32_t least) {
+template <typename Shared>
+__device__ __forceinline__ void put_in_order(Shared& sm, uint32_t n, uint32_t k, uint32_t most, uint32_t least) {
+  constexpr uint32_t kThreads = Shared::kThreads;
   constexpr uint32_t kLongBucket = 64;
   const uint32_t tid = threadIdx.x, lane = tid & 31;
   const float scale = (float)kThreads / ((float)(most - least) + 1.0f);
@@ -180,14 +183,15 @@ __device__ __forceinline__ void put_in_order(TopShared<MANY>& sm, uint32_t n, ui
 
 // The same for a row whose candidates are too many: the k-th largest key by its digits, every larger one, and of its equals those
 // with the lowest indices.
-template <typename T, bool MANY>
-__device__ __noinline__ uint32_t by_digits(TopShared<MANY>& sm, const T* row, const RowShare<T>& s, uint32_t k) {
+template <typename T, typename Shared>
+__device__ __noinline__ uint32_t by_digits(Shared& sm, const T* row, const RowShare<T>& s, uint32_t k) {
+  constexpr uint32_t kThreads = Shared::kThreads;
   uint32_t prefix = 0, want = k;
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (uint32_t i = threadIdx.x; i < 256; i += kThreads) sm.hist[i] = 0;
     __syncthreads();
     const uint32_t above = shift == 24 ? 0 : prefix >> (shift + 8);
-    for_each(row, s, [&](uint32_t key, uint32_t) {
+    for_each<kThreads>(row, s, [&](uint32_t key, uint32_t) {
       if (key > kLowest && (shift == 24 || key >> (shift + 8) == above)) atomicAdd(&sm.hist[key >> shift & 255], 1u);
     });
     __syncthreads();
@@ -199,7 +203,7 @@ __device__ __noinline__ uint32_t by_digits(TopShared<MANY>& sm, const T* row, co
   // `want` of those equal to prefix (more than kCandidates elements reach the bound, so k exist above -infinity)
   if (threadIdx.x == 0) sm.count = 0;
   __syncthreads();
-  for_each(row, s, [&](uint32_t key, uint32_t at) {
+  for_each<kThreads>(row, s, [&](uint32_t key, uint32_t at) {
     if (key > prefix) sm.entries[atomicAdd(&sm.count, 1u)] = entry_of(key, at);
   });
   __syncthreads();
@@ -240,10 +244,12 @@ __device__ __forceinline__ uint32_t warp_bound(const uint32_t* key, uint32_t j) 
   return bound;
 }
 
-template <typename T, bool MANY>
-__global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) distill_top_kernel(const TopParams p) {
+template <typename T, bool MANY, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS != kWide ? kResidentNarrow : MANY ? kResident : kResidentFew)
+    distill_top_kernel(const TopParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
-  using Shared = TopShared<MANY>;
+  using Shared = TopShared<MANY, THREADS>;
+  constexpr uint32_t kThreads = THREADS, kWarps = THREADS / 32;
   Shared& sm = *reinterpret_cast<Shared*>(raw);
   pdl_trigger();
   pdl_wait();
@@ -314,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) dis
     bound = warp_bound<1>(&key, (k + kWarps - 1) / kWarps);
   }
   if (tid % 32 == 0) sm.bound[tid / 32] = bound;
-  run = block_merge<false>(run, p.c, sm.run);
+  run = block_merge<false, THREADS>(run, p.c, sm.run);
   bound = __reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]);
   if (tid == 0) sm.mine = run;
   // what is below reaches no place of the list; -infinity never does
@@ -424,16 +430,21 @@ __global__ void __launch_bounds__(kThreads, MANY ? kResident : kResidentFew) dis
   }
 }
 
-template <typename T, bool MANY>
+template <typename T, bool MANY, int THREADS>
 cudaError_t top(const TopParams& p, int64_t rows, cudaStream_t stream) {
-  const cudaError_t e = allow_smem<distill_top_kernel<T, MANY>>();
+  const cudaError_t e = allow_smem<distill_top_kernel<T, MANY, THREADS>>();
   if (e != cudaSuccess) return e;
-  const size_t smem = sizeof(TopShared<MANY>) + (p.blocks > 1 ? (size_t)p.blocks * p.k * 8 : 0);
-  return launch_clusters(distill_top_kernel<T, MANY>, (unsigned)(rows * p.blocks), p.blocks, kThreads, smem, stream, p);
+  const size_t smem = sizeof(TopShared<MANY, THREADS>) + (p.blocks > 1 ? (size_t)p.blocks * p.k * 8 : 0);
+  return launch_clusters(distill_top_kernel<T, MANY, THREADS>, (unsigned)(rows * p.blocks), p.blocks, THREADS, smem, stream, p);
+}
+template <typename T, int THREADS>
+cudaError_t top(const TopParams& p, int64_t rows, cudaStream_t stream) {
+  return p.k <= (uint32_t)THREADS / 2 ? top<T, false, THREADS>(p, rows, stream) : top<T, true, THREADS>(p, rows, stream);
 }
 template <typename T>
-cudaError_t top(const TopParams& p, int64_t rows, cudaStream_t stream) {
-  return p.k <= (uint32_t)kThreads / 2 ? top<T, false>(p, rows, stream) : top<T, true>(p, rows, stream);
+cudaError_t top(const TopParams& p, int64_t rows, int sm_count, cudaStream_t stream) {
+  return p.k <= kMost<kNarrow> && short_rows(rows, (int64_t)p.vocab * sizeof(T), sm_count) ? top<T, kNarrow>(p, rows, stream)
+                                                                                            : top<T, kWide>(p, rows, stream);
 }
 
 }  // namespace
@@ -448,9 +459,9 @@ cudaError_t launch_distill_top(const void* logits, int32_t dtype, int64_t ld, in
   p.blocks = row_blocks(rows, (int64_t)vocab * (dtype == PVT_F32 ? 4 : 2), sm_count);
   if (rows * p.blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
   timing_begin(kKernDistill, stream);
-  const cudaError_t e = dtype == PVT_F32   ? top<float>(p, rows, stream)
-                        : dtype == PVT_F16 ? top<__half>(p, rows, stream)
-                                           : top<__nv_bfloat16>(p, rows, stream);
+  const cudaError_t e = dtype == PVT_F32   ? top<float>(p, rows, sm_count, stream)
+                        : dtype == PVT_F16 ? top<__half>(p, rows, sm_count, stream)
+                                           : top<__nv_bfloat16>(p, rows, sm_count, stream);
   timing_end(kKernDistill, stream);
   count_launches(1);
   return e;

@@ -310,3 +310,34 @@ def test_rows_further_apart_than_32_bits_count():
         B.pvt_distill_loss(d, loss, grad=logits)
         outs.append((idx, val, lse, loss, logits))
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab,k", [(700, 500, 20), (700, 1042, 33), (650, 2051, 128), (600, 3001, 200), (1200, 7, 5)])
+def test_many_short_rows(rows, vocab, k, dtype):
+    """Blocks of few threads, each with a row."""
+    x, idx, val, teacher = problem(rows, vocab, k, dtype, vocab, 1)
+    special = x.clone()
+    special[3] = 1.5
+    special[5, : vocab // 2] = -math.inf
+    special[6] = -math.inf
+    check_top(special, k, 1.3)
+    check_top(x, k, 1.3)
+    n, temperature = 12, 1.3
+    for lse in (None, torch.logsumexp(teacher.double() / temperature, dim=1).float()):
+        d = B.make_distill(x, idx, val, teacher_lse=lse, temperature=temperature)
+        loss, grad = torch.empty(rows, device="cuda"), torch.empty(rows, vocab, dtype=dtype, device="cuda")
+        B.pvt_distill_loss(d, loss, grad=grad)
+        assert torch.isfinite(loss).all() and torch.isfinite(grad).all()
+        want_loss, want_grad = ref.distill(x[:n], idx[:n], val[:n], None if lse is None else lse[:n], None, None, temperature)
+        want_loss, want_grad = want_loss.cuda(), want_grad.cuda()
+        # as above: a probability is off by e of itself, the rest of the student's mass carries the rest of the teacher's
+        e = 2.0 ** -23 * (vocab / 1024 + 40)
+        assert ((loss[:n].double() - want_loss).abs() <= 2 * e + 2.0 ** -24 * want_loss.abs()).all()
+        eps = torch.finfo(dtype).eps / 2
+        bound = 2 * e * 2 / temperature + eps * want_grad.abs() + torch.finfo(dtype).tiny * eps
+        assert ((grad[:n].double() - want_grad).abs() <= bound).all()
+        stats, again = torch.empty(rows, 8, device="cuda"), torch.empty_like(grad)
+        B.pvt_distill_loss(d, loss, stats=stats)
+        B.pvt_distill_grad(d, stats, again)
+        assert torch.equal(again, grad)
