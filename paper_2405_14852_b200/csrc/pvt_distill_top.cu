@@ -5,13 +5,12 @@
 // elements reach the smallest of these, so everything that is listed is among the elements that do; with parts in no relation
 // to the values those are not many more.  (The k-th largest of the block's 256 would leave fewer, 74 for k = 64, but one
 // warp finds it while the others wait.)  The pieces of the parts that reach it, 16 bytes each, are looked at once more, and
-// their candidates are put in order in shared memory.  (A second pass over the whole row, which the L2 served: 64 / 257
-// largest of 4096 x 32000 bf16 87 / 148 us, so 80 / 133.)  A row in which too many elements reach the bound (equal ones, or a
+// their candidates are put in order in shared memory.  (With a second pass over the whole row,
+// which the L2 served, 64 / 257 largest of 4096 x 32000 bf16 took 87 / 148 us, not 78 / 133.)  A row in which too many elements reach the bound (equal ones, or a
 // list nearly as long as the parts are many) is settled by counting the digits of its keys instead.  A few long rows are
 // shared by clusters: each block lists its part, and an entry's place is its own plus those that the other blocks' lists
 // hold ahead of it.
-// 4096 x 32000 bf16 are 40 us of HBM; instructions and the latencies of a block's steps take the rest, while six blocks of an SM
-// share its issue slots.
+// 4096 x 32000 bf16 are 40 us of HBM; the bound is the issue slots, 73 % used by six blocks per SM.
 #include "pvt_distill.cuh"
 
 namespace pvt {
