@@ -143,13 +143,14 @@ __device__ __forceinline__ void commit(uint32_t bar) {
       "@one tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
       : "memory");
 }
-// the same for what the first block of a pair has issued: an arrival at the barrier of that place in both
-__device__ __forceinline__ void commit_pair(uint32_t bar) {
+// the same for what the first block of a pair has issued: an arrival at the barrier of that place in both, which `blocks` names by
+// a bit for each rank of the cluster
+__device__ __forceinline__ void commit_pair(uint32_t bar, uint16_t blocks = 3) {
   asm volatile(
       "{\n\t.reg .pred one;\n\t"
       "elect.sync _|one, 0xffffffff;\n\t"
       "@one tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(bar),
-      "h"((uint16_t)3)
+      "h"(blocks)
       : "memory");
 }
 

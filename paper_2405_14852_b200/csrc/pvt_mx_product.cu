@@ -240,6 +240,7 @@ constexpr int kPairCopyWarp = kPairReaders, kPairMmaWarp = kPairCopyWarp + kPair
 constexpr int kPairThreads = (kPairMmaWarp + 1) * 32;
 constexpr uint32_t kPairRows = 256;   // of w
 constexpr uint32_t kPairStages = 7;   // at most
+constexpr uint32_t kLeastSteps = 12;  // of a pair that shares a tile with others
 
 struct PairShared {
   alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
@@ -260,6 +261,7 @@ struct PairParams {
   uint32_t strip_rows;   // rows of 128 bytes that a strip's scales are
   uint32_t steps;        // of 256 columns
   uint32_t x_tiles, tiles;
+  uint32_t split;        // pairs per tile
   uint32_t max_spins, withhold;
 };
 
@@ -274,6 +276,7 @@ struct PairSizes {
   static_assert(N + kStages * kScaleCols <= 512, "sums and scales fit tensor memory");
   static constexpr size_t kBytes = kStages * kStageAligned + 1024;
   static_assert(kBytes + 1024 <= 227 * 1024 && kStages <= kPairStages, "a block's shared memory");
+  static_assert(N * kTileW * 4 <= kStages * kStageAligned, "the partial sums fit the stages");
 };
 
 // A step of a pair: its scales to tensor memory (two or four tiles for w's 128 rows, as many for each of one or two strips of
@@ -549,21 +552,24 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
-  const uint32_t rank = cluster_rank(), pairs = gridDim.x / 2;
+  // Pairs by themselves take tile after tile; those of a cluster share one tile's steps.
+  const uint32_t in_cluster = cluster_rank(), rank = in_cluster & 1, lead = in_cluster & ~1u, share = in_cluster / 2;
+  const uint32_t tile0 = blockIdx.x / 2 / p.split, stride = p.split > 1 ? p.tiles : gridDim.x / 2;
+  const uint32_t first = p.steps * share / p.split, steps = p.steps * (share + 1) / p.split - first;  // (steps < 2^24, share < 4)
 
   if (warp >= kPairCopyWarp && warp < kPairMmaWarp) {
     const bool of_w = warp == kPairCopyWarp;  // one warp for w's codes and scales, one for x's
     uint32_t i = 0;
     bool ok = true;
-    for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs) {
+    for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride) {
       const uint32_t tile0 = of_w ? tile / p.x_tiles * kPairRows : tile % p.x_tiles * N;
       const int row = (int)(tile0 + rank * (of_w ? kTileW : N / 2));
       const int strip = (int)((of_w ? (uint32_t)row : tile0) / kStrip * p.strip_rows);
-      for (uint32_t step = 0; step < p.steps; ++step, ++i) {
+      for (uint32_t step = first; step < first + steps; ++step, ++i) {
         const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
         if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
         if (i == p.withhold) continue;  // test hook: never issued
-        const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), 0);
+        const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), lead);
         const int col = (int)(step * kRowBytes), scales = strip + (int)(step * (KT * 4));
         if (of_w) {
           if (rank == 0) expect_bytes(smem_u32(&sm.full[s]), 2 * S::kStage);
@@ -584,12 +590,13 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       // e2m1 both, N, M = 256, type of the scales
       constexpr uint32_t idesc =
           1u << 7 | 1u << 10 | (N >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | (kPairRows >> 7) << 27;
+      const uint16_t both = (uint16_t)(3u << lead);
       uint32_t i = 0, n = 0;
       bool ok = true;
-      for (uint32_t tile = blockIdx.x / 2; tile < p.tiles && ok; tile += pairs, ++n) {
+      for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride, ++n) {
         if (n > 0) ok = wait<true>(smem_u32(&sm.sums_empty), (n - 1) & 1, abandoned, p.status, p.max_spins);
         tc_fence_after();
-        for (uint32_t step = 0; step < p.steps && ok; ++step) {
+        for (uint32_t step = 0; step < steps && ok; ++step) {
           const uint32_t s = i % STAGES, from = base + s * S::kStageAligned;
           ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
           if (!ok) break;
@@ -598,22 +605,22 @@ __global__ void __launch_bounds__(kPairThreads, 1)
           // (a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart)
           multiply_step<FMT, S::kStrips>(tmem, operand(from, 16, 1024, true), operand(from + S::kX, 16, 1024, true), idesc, sfa, sfb,
                              operand(from + S::kWs, 0, 128, false), operand(from + S::kXs, 0, 128, false), (uint32_t)(step > 0));
-          commit_pair(smem_u32(&sm.empty[s]));
+          commit_pair(smem_u32(&sm.empty[s]), both);
           ++i;
         }
-        if (ok) commit_pair(smem_u32(&sm.sums_full));
+        if (ok) commit_pair(smem_u32(&sm.sums_full), both);
       }
       if (!ok && i > 0) {
-        commit_pair(smem_u32(&sm.spare));
+        commit_pair(smem_u32(&sm.spare), both);
         drain(smem_u32(&sm.spare), 0);
       }
     }
   } else {
     const Factors alpha(p.w_ts ? *p.w_ts : 1.0f, p.x_ts ? *p.x_ts : 1.0f);
     const uint32_t quarter = warp % 4, half = warp / 4;
-    const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), 0);
+    const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), lead);
     uint32_t n = 0;
-    for (uint32_t tile = blockIdx.x / 2; tile < p.tiles; tile += pairs, ++n) {
+    for (uint32_t tile = tile0; tile < p.tiles; tile += stride, ++n) {
       bool ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
       if (!ok) break;
       tc_fence_after();
@@ -625,6 +632,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       __syncwarp();
       if (lane == 0) cluster_arrive(sums_empty);
       __syncwarp();
+      if (p.split > 1) {  // the products are done: the stages hold the partial sums
+        float* const part = reinterpret_cast<float*>(raw + (base - smem_u32(raw))) + half * (N / 2) * kTileW + quarter * 32 + lane;
+#pragma unroll
+        for (uint32_t j = 0; j < N / 2; ++j) part[j * kTileW] = __uint_as_float(v[j]);
+        break;
+      }
       // lanes are consecutive outputs of a token
       const uint32_t col = tile / p.x_tiles * kPairRows + rank * kTileW + quarter * 32 + lane;
       const uint32_t row = tile % p.x_tiles * N + half * (N / 2);
@@ -641,6 +654,27 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   }
   __syncthreads();
   cluster_sync();  // neither block leaves while the other's copies or products reach it
+  if (p.split > 1) {
+    // every pair adds up the tokens that are its share, one to a warp, always in the order of pairs
+    if (!*abandoned) {
+      const Factors alpha(p.w_ts ? *p.w_ts : 1.0f, p.x_ts ? *p.x_ts : 1.0f);
+      const uint32_t col0 = tile0 / p.x_tiles * kPairRows + rank * kTileW, row0 = tile0 % p.x_tiles * N;
+      const uint32_t tokens = min(N, p.x_rows - row0);
+      for (uint32_t j = share + warp * p.split; j < tokens; j += kPairThreads / 32 * p.split) {
+        float v[4][4];  // (all under way at once: a load from another block takes a thousand cycles)
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t q = 0; q < 4; ++q)
+            v[i][q] = q < p.split ? cluster_load(base + (j * kTileW + i * 32 + lane) * 4, 2 * q + rank) : 0.0f;
+        T* const y = static_cast<T*>(p.y) + (int64_t)(row0 + j) * p.ldy + col0 + lane;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+          if (col0 + i * 32 + lane < p.w_rows) y[i * 32] = narrow<T>(alpha(v[i][0] + v[i][1] + v[i][2] + v[i][3]));
+      }
+    }
+    cluster_sync();  // nor while another reads its partial sums
+  }
   if (warp == kPairMmaWarp) {
     tc_fence_after();
     tmem_dealloc<2>(tmem, 512);
@@ -668,8 +702,14 @@ cudaError_t product_pairs(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, u
   if (e != cudaSuccess) return e;
   uint32_t pairs = (uint32_t)sm_count / 2;
   if (pairs > p.tiles) pairs = p.tiles;
-  return launch_clusters(mx_product_pair_kernel<T, FMT, N>, 2 * pairs, 2, kPairThreads, S::kBytes, stream, maps[0], maps[1], maps[2],
-                         maps[3], p);
+  // Few tiles of many steps: two or four pairs to a tile, as long as all clusters run at once (those of eight blocks leave more
+  // SMs over).  By single pairs and so, 256 tokens 8192 by 4096 e4m3 13.5 and 11.3 us, 75 tokens 21892 by 2787 28.8 and 12.9; but
+  // 200 tokens 2048 by 2048 6.0 and 7.2, and four pairs to each of 16 tiles, 32 tokens 4096 by 4096, 7.7 and 11.3.
+  const uint32_t all = (uint32_t)sm_count / 2;
+  p.split = 1;
+  if (p.tiles <= all * 7 / 16 && p.steps >= 2 * kLeastSteps) p.split = p.tiles <= all / 6 && p.steps >= 4 * kLeastSteps ? 4 : 2;
+  return launch_clusters(mx_product_pair_kernel<T, FMT, N>, 2 * (p.split > 1 ? p.tiles * p.split : pairs), 2 * p.split, kPairThreads,
+                         S::kBytes, stream, maps[0], maps[1], maps[2], maps[3], p);
 }
 
 // Whether tiles of 128 rows of x serve better than 256: they take three quarters of the time, so where there are not more rounds

@@ -32,7 +32,7 @@ def held(rows, cols, fmt, seed, scales=None, tensor_scale=None, fill=0xff):
 SHAPES = [  # tokens, inputs, outputs
     (1, 1, 1), (1, 32, 16), (1, 4096, 129), (2, 257, 128), (7, 1000, 300), (16, 512, 2048), (17, 255, 127), (33, 300, 64),
     (64, 2049, 640), (65, 256, 500), (128, 768, 128), (129, 513, 257), (256, 1024, 256), (257, 640, 384), (300, 33, 1000),
-    (513, 1537, 130), (1100, 520, 4200),
+    (513, 1537, 130), (1100, 520, 4200), (20, 6200, 500), (140, 12300, 300), (260, 7000, 2100),
 ]
 
 
@@ -316,3 +316,22 @@ def test_calls_on_several_streams_at_once():
     torch.cuda.synchronize()
     for _, outs, want in jobs:
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("tokens,inputs,outputs", [(40, 12300, 300), (3, 6000, 200)])
+def test_a_wait_that_runs_out_in_blocks_that_share_a_tile(tokens, inputs, outputs):
+    """All blocks of a cluster come to its barriers, whatever one of them has given up."""
+    x, xv = held(tokens, inputs, B.PVT_MX_E8M0_32, 71)
+    w, wv = held(outputs, inputs, B.PVT_MX_E8M0_32, 72)
+    y = torch.empty(tokens, outputs, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.pvt_test_wait_limit(20000, 1)
+    try:
+        B.pvt_mx_product(x, w, y, status=status)
+        torch.cuda.synchronize()
+    finally:
+        B.pvt_test_wait_limit(0, -1)
+    assert status.item() & B.PVT_DEV_WAIT_EXPIRED
+    status.zero_()
+    B.pvt_mx_product(x, w, y, status=status)
+    assert status.item() == 0 and torch.equal(y, (xv @ wv.T).float())
