@@ -96,6 +96,63 @@ __device__ __forceinline__ void turn(float* buffer, float* v, uint32_t lane) {
 template <typename T, bool WIDE>
 constexpr int kLaneElements = WIDE ? 32 / (int)sizeof(T) : 8;
 
+// what a tensor scale comes to
+struct TensorScale {
+  float ts = 1.0f, inv_six = 1.0f / 6.0f;
+  bool bad = false;
+  __device__ __forceinline__ explicit TensorScale(const float* p) {
+    if (!p) return;
+    ts = *p;
+    bad = !(ts > 0.0f && ts < __uint_as_float(0x7f800000u));
+    inv_six = 1.0f / (6.0f * ts);
+  }
+};
+// The scale byte of a block, from the bits of its largest magnitude, and the codes of a lane's E elements of it.
+template <int FMT, int E>
+__device__ __forceinline__ uint32_t quantize_block(float* v, uint32_t top, const TensorScale& t, uint32_t* word) {
+  const bool bad = top >= 0x7f800000u || t.bad;
+  uint32_t byte;
+#pragma unroll
+  for (int w = 0; w < E / 8; ++w) word[w] = 0;
+  if (FMT == PVT_MX_E8M0_32) {
+    // floor(log2 a) - 2, biased; numbers below 2^-126 have a scale of 2^-127 in any case
+    const int e = max((int)(top >> 23) - 2, 0);
+    byte = bad ? 255u : (uint32_t)e;
+    const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] *= inv;
+    if (!bad) {
+#pragma unroll
+      for (int w = 0; w < E / 8; ++w) word[w] = e2m1_codes(v + 8 * w);
+    }
+  } else {
+    byte = bad ? 127u : e4m3_scale(__uint_as_float(top), t.ts, t.inv_six);
+    if (!bad && byte) {
+      const float s = e4m3_float(byte), d = s * t.ts;
+      float r;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+      const float more = r * kMore, less = r * kLess;
+      // where d or r leave the range of normal numbers every element is compared with its borders
+      const bool all = !(d >= 1e-30f && d <= 1e30f);
+#pragma unroll
+      for (int w = 0; w < E / 8; ++w) {
+        float hi[8], lo[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) hi[i] = v[8 * w + i] * more, lo[i] = v[8 * w + i] * less;
+        word[w] = e2m1_codes(hi);
+        const uint32_t differ = all ? 0xffffffffu : word[w] ^ e2m1_codes(lo);
+        if (differ) {
+          const double dd = (double)s * (double)t.ts;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (differ >> (4 * i) & 15u) word[w] = (word[w] & ~(15u << (4 * i))) | e2m1_exact(v[8 * w + i], dd) << (4 * i);
+        }
+      }
+    }
+  }
+  return byte;
+}
+
 template <typename T, int FMT, bool WIDE>
 __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ld, uint8_t* scales,
                                                                 const float* tensor_scale, uint32_t rows, uint32_t cols,
@@ -106,14 +163,7 @@ __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int6
   pdl_trigger();
   pdl_wait();
   const uint32_t lane = threadIdx.x & 31;
-  float ts = 1.0f;
-  bool bad_ts = false;
-  float inv_six = 1.0f / 6.0f;
-  if (FMT == PVT_MX_E4M3_16 && tensor_scale) {
-    ts = *tensor_scale;
-    bad_ts = !(ts > 0.0f && ts < __uint_as_float(0x7f800000u));
-    inv_six = 1.0f / (6.0f * ts);
-  }
+  const TensorScale t(FMT == PVT_MX_E4M3_16 ? tensor_scale : nullptr);
   for (uint32_t at = blockIdx.x * (kQThreads / 32) + threadIdx.x / 32; at < total; at += gridDim.x * (kQThreads / 32)) {
     // (a strip's rows that do not exist are spans too: their scales are written)
     const uint32_t row = fast_div(at, spans_div), c0 = (at - row * spans) * (32 * E) + E * lane;
@@ -146,46 +196,7 @@ __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int6
     for (int i = 0; i < E; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
 #pragma unroll
     for (int s = 1; s < LANES; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-    const bool bad = top >= 0x7f800000u || bad_ts;
-    uint32_t byte, word[E / 8];
-#pragma unroll
-    for (int w = 0; w < E / 8; ++w) word[w] = 0;
-    if (FMT == PVT_MX_E8M0_32) {
-      // floor(log2 a) - 2, biased; numbers below 2^-126 have a scale of 2^-127 in any case
-      const int e = max((int)(top >> 23) - 2, 0);
-      byte = bad ? 255u : (uint32_t)e;
-      const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
-#pragma unroll
-      for (int i = 0; i < E; ++i) v[i] *= inv;
-      if (!bad) {
-#pragma unroll
-        for (int w = 0; w < E / 8; ++w) word[w] = e2m1_codes(v + 8 * w);
-      }
-    } else {
-      byte = bad ? 127u : e4m3_scale(__uint_as_float(top), ts, inv_six);
-      if (!bad && byte) {
-        const float s = e4m3_float(byte), d = s * ts;
-        float r;
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
-        const float more = r * kMore, less = r * kLess;
-        // where d or r leave the range of normal numbers every element is compared with its borders
-        const bool all = !(d >= 1e-30f && d <= 1e30f);
-#pragma unroll
-        for (int w = 0; w < E / 8; ++w) {
-          float hi[8], lo[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) hi[i] = v[8 * w + i] * more, lo[i] = v[8 * w + i] * less;
-          word[w] = e2m1_codes(hi);
-          const uint32_t differ = all ? 0xffffffffu : word[w] ^ e2m1_codes(lo);
-          if (differ) {
-            const double dd = (double)s * (double)ts;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (differ >> (4 * i) & 15u) word[w] = (word[w] & ~(15u << (4 * i))) | e2m1_exact(v[8 * w + i], dd) << (4 * i);
-          }
-        }
-      }
-    }
+    uint32_t word[E / 8], byte = quantize_block<FMT, E>(v, top, t, word);
     if (c0 >= cols) byte = 0;  // no such block, whatever the tensor scale is
     uint32_t four = byte | __shfl_down_sync(0xffffffffu, byte, LANES) << 8;
     four |= __shfl_down_sync(0xffffffffu, four, 2 * LANES) << 16;
@@ -200,6 +211,118 @@ __global__ void __launch_bounds__(kQThreads) mx_quantize_kernel(const T* x, int6
 #pragma unroll
       for (uint32_t i = 0; i < E / 2; ++i)
         if (2 * i < cols - c0) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
+    }
+  }
+}
+
+// eight elements times their scale and the tensor's
+template <int FMT>
+__device__ __forceinline__ void values_of(uint32_t w, uint32_t byte, float ts, float* v) {
+  const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(byte) : e4m3_float(byte);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    // the three bits of the magnitude as the low exponent bits and the first fraction bit of a binary32, whose bias
+    // is 126 more: a product with 2^126 gives the element, 0.5 from a number without its leading one included
+    const uint32_t n = w >> (4 * i);
+    const float el = __uint_as_float((n & 7u) << 22 | (n & 8u) << 28) * 8.507059173023462e37f;
+    v[i] = el * s * ts;
+  }
+}
+
+// Few columns: one row after the other would leave most lanes without work, so a warp takes 32 / LANES rows of up to 8 LANES
+// columns, eight to a lane.  Between memory and lanes they go by way of shared memory: a warp reads or writes 32 elements
+// at a time, in the order of rows.  By a row to a warp and so: 5581843 x 21 fp16 to e8m0 1166 and 277 us, back to binary32 1099 and
+// 221; 118801 x 110, back, rows of no alignment, 28 and 20.  (Wide accesses of 65 columns and more: 1000000 x 128 back 148 us by a row
+// to a warp, 175 so.)
+template <int LANES>
+struct NarrowRows {
+  static constexpr uint32_t kRows = 32 / LANES;
+  uint32_t lane, row0, n;  // n: elements of the warp's rows
+  __device__ __forceinline__ NarrowRows(uint32_t at, uint32_t rows, uint32_t cols)
+      : lane(threadIdx.x & 31), row0(at * kRows), n(row0 < rows ? min(kRows, rows - row0) * cols : 0) {}
+  __device__ __forceinline__ uint32_t row() const { return row0 + lane / LANES; }
+  __device__ __forceinline__ uint32_t col() const { return lane % LANES * 8; }
+  // place of an element of this lane's row in shared memory
+  __device__ __forceinline__ uint32_t place(uint32_t c, uint32_t cols) const { return lane / LANES * cols + c; }
+};
+
+template <typename T, int FMT, int LANES>
+__global__ void __launch_bounds__(kQThreads) mx_quantize_narrow_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ld, uint8_t* scales,
+                                                                       const float* tensor_scale, uint32_t rows, FastDiv by_cols,
+                                                                       uint32_t cols, uint32_t tiles, uint32_t total) {
+  constexpr int OF_BLOCK = FMT == PVT_MX_E8M0_32 ? 4 : 2;           // lanes
+  constexpr int WORDS = LANES > 4 * OF_BLOCK ? LANES / (4 * OF_BLOCK) : 1;  // of four scales that a row's lanes have
+  __shared__ float buffer[kQThreads / 32][kSpan];
+  pdl_trigger();
+  pdl_wait();
+  const TensorScale t(FMT == PVT_MX_E4M3_16 ? tensor_scale : nullptr);
+  float* const own = buffer[threadIdx.x / 32];
+  for (uint32_t at = blockIdx.x * (kQThreads / 32) + threadIdx.x / 32; at < total; at += gridDim.x * (kQThreads / 32)) {
+    const NarrowRows<LANES> m(at, rows, cols);
+    __syncwarp();
+    for (uint32_t i = m.lane; i < m.n; i += 32) {
+      const uint32_t r = fast_div(i, by_cols);
+      own[i] = widen<T>(x[(int64_t)(m.row0 + r) * ldx + (i - r * cols)]);
+    }
+    __syncwarp();
+    const uint32_t row = m.row(), c0 = m.col();
+    const bool here = row < rows && c0 < cols;
+    float v[8];
+    uint32_t top = 0, word;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = here && c0 + i < cols ? own[m.place(c0 + i, cols)] : 0.0f;
+      top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    }
+#pragma unroll
+    for (int s = 1; s < OF_BLOCK; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+    uint32_t byte = quantize_block<FMT, 8>(v, top, t, &word);
+    if (!here) byte = 0;
+    uint32_t four = byte;
+    if (LANES >= 2 * OF_BLOCK) four |= __shfl_down_sync(0xffffffffu, byte, OF_BLOCK) << 8;
+    if (LANES >= 4 * OF_BLOCK) four |= __shfl_down_sync(0xffffffffu, four, 2 * OF_BLOCK) << 16;
+    // (a strip's rows that do not exist, and blocks that do not, have scales too)
+    const uint32_t first = m.lane % LANES;
+    if (first % (4 * OF_BLOCK) == 0) *reinterpret_cast<uint32_t*>(scales + scale_at(row, first / OF_BLOCK, tiles)) = four;
+    if (first == 0)
+      for (uint32_t w = WORDS; w < tiles; ++w) *reinterpret_cast<uint32_t*>(scales + scale_at(row, 4 * w, tiles)) = 0;
+    if (!here) continue;
+    uint8_t* const to = codes + (int64_t)row * ld + c0 / 2;
+    if (c0 + 8 <= cols) {
+      *reinterpret_cast<uint32_t*>(to) = word;
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (2 * i < cols - c0) to[i] = (uint8_t)(word >> (8 * i));
+    }
+  }
+}
+
+template <typename T, int FMT, int LANES>
+__global__ void __launch_bounds__(kQThreads) mx_dequant_narrow_kernel(const uint8_t* codes, int64_t ld, const uint8_t* scales,
+                                                                      const float* tensor_scale, T* values, int64_t ldv, uint32_t rows,
+                                                                      FastDiv by_cols, uint32_t cols, uint32_t tiles, uint32_t total) {
+  __shared__ float buffer[kQThreads / 32][kSpan];
+  pdl_trigger();
+  pdl_wait();
+  const float ts = FMT == PVT_MX_E4M3_16 && tensor_scale ? *tensor_scale : 1.0f;
+  float* const own = buffer[threadIdx.x / 32];
+  for (uint32_t at = blockIdx.x * (kQThreads / 32) + threadIdx.x / 32; at < total; at += gridDim.x * (kQThreads / 32)) {
+    const NarrowRows<LANES> m(at, rows, cols);
+    const uint32_t row = m.row(), c0 = m.col();
+    __syncwarp();
+    if (row < rows && c0 < cols) {  // (the four bytes lie in the row: ld is a multiple of 16)
+      float v[8];
+      values_of<FMT>(*reinterpret_cast<const uint32_t*>(codes + (int64_t)row * ld + c0 / 2),
+                     scales[scale_at(row, c0 / (FMT == PVT_MX_E8M0_32 ? 32 : 16), tiles)], ts, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c0 + i < cols) own[m.place(c0 + i, cols)] = v[i];
+    }
+    __syncwarp();
+    for (uint32_t i = m.lane; i < m.n; i += 32) {
+      const uint32_t r = fast_div(i, by_cols);
+      values[(int64_t)(m.row0 + r) * ldv + (i - r * cols)] = narrow<T>(own[i]);
     }
   }
 }
@@ -230,16 +353,8 @@ __global__ void __launch_bounds__(kQThreads) mx_dequant_kernel(const uint8_t* co
   while (next < total) {
     const uint32_t r = row, c = c0, w = word, b = byte;
     ask(next += warps);
-    const float s = FMT == PVT_MX_E8M0_32 ? e8m0_value(b) : e4m3_float(b);
     float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // the three bits of the magnitude as the low exponent bits and the first fraction bit of a binary32, whose bias
-      // is 126 more: a product with 2^126 gives the element, 0.5 from a number without its leading one included
-      const uint32_t n = w >> (4 * i);
-      const float el = __uint_as_float((n & 7u) << 22 | (n & 8u) << 28) * 8.507059173023462e37f;
-      v[i] = el * s * ts;
-    }
+    values_of<FMT>(w, b, ts, v);
     T* const to = values + (int64_t)r * ldv;
     if (!WIDE) {
       turn<true>(buffer[threadIdx.x / 32], v, lane);
@@ -286,14 +401,34 @@ cudaError_t quantize(const pvt_mx& m, const T* x, int64_t ldx, int sm_count, cud
                           m.ld, m.scales, m.tensor_scale, (uint32_t)m.rows, (uint32_t)m.cols,
                           strip_tiles(m.cols, block_of(FMT)), make_fast_div(spans), spans, total);
 }
+template <typename T, int FMT, int LANES>
+cudaError_t quantize_narrow(const pvt_mx& m, const T* x, int64_t ldx, int sm_count, cudaStream_t stream) {
+  const uint32_t total = ((uint32_t)m.rows + kStrip - 1) / kStrip * kStrip / (32 / LANES);
+  return launch_dependent(mx_quantize_narrow_kernel<T, FMT, LANES>, span_grid(total, 8, sm_count), kQThreads, 0, stream, x, ldx, m.codes,
+                          m.ld, m.scales, m.tensor_scale, (uint32_t)m.rows, make_fast_div((uint32_t)m.cols), (uint32_t)m.cols,
+                          strip_tiles(m.cols, block_of(FMT)), total);
+}
 template <typename T, int FMT>
 cudaError_t quantize(const pvt_mx& m, const T* x, int64_t ldx, int sm_count, cudaStream_t stream) {
+  if (m.cols <= 32) return quantize_narrow<T, FMT, 4>(m, x, ldx, sm_count, stream);
+  if (m.cols <= 64) return quantize_narrow<T, FMT, 8>(m, x, ldx, sm_count, stream);
+  if (m.cols <= 128 && !rows_aligned(x, ldx, sizeof(T))) return quantize_narrow<T, FMT, 16>(m, x, ldx, sm_count, stream);
   return rows_aligned(x, ldx, sizeof(T)) ? quantize<T, FMT, true>(m, x, ldx, sm_count, stream)
                                          : quantize<T, FMT, false>(m, x, ldx, sm_count, stream);
 }
 
+template <typename T, int FMT, int LANES>
+cudaError_t dequant_narrow(const pvt_mx& m, T* values, int64_t ldv, int sm_count, cudaStream_t stream) {
+  const uint32_t total = ((uint32_t)m.rows + 32 / LANES - 1) / (32 / LANES);
+  return launch_dependent(mx_dequant_narrow_kernel<T, FMT, LANES>, span_grid(total, 8, sm_count), kQThreads, 0, stream,
+                          (const uint8_t*)m.codes, m.ld, (const uint8_t*)m.scales, m.tensor_scale, values, ldv, (uint32_t)m.rows,
+                          make_fast_div((uint32_t)m.cols), (uint32_t)m.cols, strip_tiles(m.cols, block_of(FMT)), total);
+}
 template <typename T, int FMT>
 cudaError_t dequant(const pvt_mx& m, T* values, int64_t ldv, int sm_count, cudaStream_t stream) {
+  if (m.cols <= 32) return dequant_narrow<T, FMT, 4>(m, values, ldv, sm_count, stream);
+  if (m.cols <= 64) return dequant_narrow<T, FMT, 8>(m, values, ldv, sm_count, stream);
+  if (m.cols <= 128 && !rows_aligned(values, ldv, sizeof(T))) return dequant_narrow<T, FMT, 16>(m, values, ldv, sm_count, stream);
   const uint32_t spans = ((uint32_t)m.cols + kSpan - 1) / kSpan, total = (uint32_t)m.rows * spans;
   auto kernel = rows_aligned(values, ldv, sizeof(T)) ? mx_dequant_kernel<T, FMT, true> : mx_dequant_kernel<T, FMT, false>;
   return launch_dependent(kernel, span_grid(total, blocks_back(total), sm_count), kQThreads, 0, stream, (const uint8_t*)m.codes, m.ld,

@@ -197,3 +197,22 @@ def test_rows_further_apart_than_32_bits_count():
         B.pvt_mx_grad_input(dy, m, far)
         assert torch.equal(far, v.bfloat16())
         del far
+
+
+@pytest.mark.parametrize("fmt,ts", FORMATS)
+@pytest.mark.parametrize("rows,cols", [(5, 8), (300, 21), (257, 32), (129, 33), (1000, 64), (2, 100), (515, 127), (1025, 128), (20000, 31)])
+def test_rows_of_few_columns(rows, cols, fmt, ts):
+    """Several rows share a warp: rows of any distance, and values that lie beside others."""
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    for dtype, pad in ((torch.float32, 0), (torch.bfloat16, 3), (torch.float16, 8)):
+        wide = torch.full((rows, cols + pad), math.nan, device="cuda", dtype=dtype)
+        wide[:, :cols] = (torch.randn(rows, cols, device="cuda", generator=gen) *
+                          torch.exp(3 * torch.randn(rows, 1, device="cuda", generator=gen))).to(dtype)
+        if rows > 2:
+            wide[1, cols // 2] = math.inf
+        m, want = check(wide[:, :cols], fmt, ts)
+        out = torch.full((rows, cols + 5), 7.0, device="cuda", dtype=dtype)
+        B.pvt_mx_dequant(m, out[:, 2:cols + 2])
+        assert torch.equal(out[:, 2:cols + 2].isnan(), want.isnan())
+        assert torch.equal(out[:, 2:cols + 2].nan_to_num(), want.to(dtype).nan_to_num())
+        assert (out[:, :2] == 7).all() and (out[:, cols + 2:] == 7).all()
