@@ -97,7 +97,7 @@ constexpr int kWideners = kGroups * kGroupWarps;
 // have one each, or two)
 constexpr int kHeldWarp = kWideners + kReaders, kCopyWarp = kHeldWarp + 1, kMmaWarp = kCopyWarp + 2;
 constexpr int kThreads = (kMmaWarp + 1) * 32;
-constexpr uint32_t kStages = 4, kHeld = 8;      // steps of operands, of codes and scales
+constexpr uint32_t kStages = 4, kMostHeld = 8;  // steps of operands, of codes and scales
 constexpr uint32_t kSums = 256;                 // columns of tensor memory of a pair's set
 
 // CTAS: blocks that multiply together, MT: products of 128 CTAS rows per step
@@ -110,8 +110,10 @@ struct GradSizes {
   static constexpr uint32_t kScaleCols = FMT == PVT_MX_E8M0_32 ? 128 : 64;
   static constexpr uint32_t kScaleBytes = (kHalf > kScaleCols ? kHalf / kScaleCols : 1) * kTileBytes;
   static constexpr uint32_t kHeldBytes = kCodeBytes + kScaleBytes;
+  // columns that a reading warp turns at a time, and what is left for codes and scales
+  static constexpr uint32_t kTurn = CTAS == 2 && MT == 1 ? 64 : 32, kHeld = kTurn == 64 ? 6 : kMostHeld;
   static constexpr uint32_t kHeldAt = kStages * kStage, kTurnAt = kHeldAt + kHeld * kHeldBytes;
-  static constexpr size_t kBytes = kTurnAt + kReaders * 32 * 33 * 4 + 1024;
+  static constexpr size_t kBytes = kTurnAt + kReaders * 32 * (kTurn + 1) * 4 + 1024;
   static_assert(kBytes + 1024 <= 227 * 1024 && kStage % 1024 == 0 && kHeldBytes % 128 == 0, "a block's shared memory");
   static constexpr uint32_t kTmem = CTAS == 2 ? 512 : 128;
   static constexpr uint32_t kPartPitch = kCols + 1;  // floats, of a row of partial sums
@@ -119,8 +121,8 @@ struct GradSizes {
 };
 
 struct GradShared {
-  alignas(8) uint64_t held[kHeld];     // of each block: codes and scales
-  uint64_t held_empty[kHeld];          // of each: an arrival per warp of the group
+  alignas(8) uint64_t held[kMostHeld];     // of each block: codes and scales
+  uint64_t held_empty[kMostHeld];          // of each: an arrival per warp of the group
   uint64_t full_a[kStages];            // of the first: A's tiles of both
   uint64_t full_b[kStages];            // of the first: an arrival per warp of both blocks' groups
   uint64_t empty[kStages];             // of each
@@ -252,7 +254,7 @@ template <typename T, int FMT, bool TRANS, int MT, int CTAS>
 __global__ void __launch_bounds__(kThreads, 1)
     mx_grad_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap q_map, const GradParams p) {
   using S = GradSizes<FMT, MT, CTAS>;
-  constexpr uint32_t STAGES = kStages;
+  constexpr uint32_t STAGES = kStages, kHeld = S::kHeld, TURN = S::kTurn;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ GradShared sm;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -415,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const Factors alpha(kWidened<FMT>, p.ts ? *p.ts : 1.0f);
     // (a warp reads the quarter of the lanes that its number gives it; the upper four have the second half of the columns)
     const uint32_t quarter = warp % 4, half = (warp - kWideners) / 4;
-    float* const turn = reinterpret_cast<float*>(mem + S::kTurnAt) + (warp - kWideners) * (32 * 33);
+    float* const turn = reinterpret_cast<float*>(mem + S::kTurnAt) + (warp - kWideners) * (32 * (TURN + 1));
     uint32_t n = 0;
     for (uint32_t tile = tile0; tile < p.tiles; tile += stride, ++n) {
       const uint32_t set = n & 1;
@@ -435,27 +437,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         break;
       }
-      // 32 rows by 32 columns at a time, turned in shared memory so that a warp stores along a row
-      for (uint32_t j0 = half * (S::kCols * MT / 2); j0 < (half + 1) * (S::kCols * MT / 2); j0 += 32) {
+      // 32 rows by 32 or 64 columns at a time, turned in shared memory so that a warp stores along a row.  (Where rows begin
+      // inside of 32 bytes, what two stores share of these costs least if the second one comes at once: dw of 77 tokens 5119 by
+      // 4095, 32 and 64 columns: 36 and 28 us.)
+      for (uint32_t j0 = half * (S::kCols * MT / 2); j0 < (half + 1) * (S::kCols * MT / 2); j0 += TURN) {
         const uint32_t row0 = tile % p.a_tiles * S::kRows + j0 / S::kCols * 256 + rank * kTileA + quarter * 32, col0 = c0 + j0 % S::kCols;
         if (row0 >= p.a_rows || col0 >= p.cols) continue;
         const uint32_t n_rows = min(32u, p.a_rows - row0);
-        uint32_t v[32];
-        tmem_ld32(tmem + (quarter << 21) + set * kSums + j0, v);
-        tmem_ld_wait<32>(v);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = __uint_as_float(v[j]);
+        for (uint32_t h = 0; h < TURN; h += 32) {
+          uint32_t v[32];
+          tmem_ld32(tmem + (quarter << 21) + set * kSums + j0 + h, v);
+          tmem_ld_wait<32>(v);
+#pragma unroll
+          for (uint32_t j = 0; j < 32; ++j) turn[lane * (TURN + 1) + h + j] = __uint_as_float(v[j]);
+        }
         __syncwarp();
-        const uint32_t col = col0 + lane;
-        if (col < p.cols) {
-          T* out = static_cast<T*>(p.out) + (int64_t)row0 * p.ldo + col;
-          if (sizeof(T) == 4 && p.accumulate) {
+        T* const out = static_cast<T*>(p.out) + (int64_t)row0 * p.ldo + col0 + lane;
+        auto rows = [&](auto add, auto both) {
 #pragma unroll 8
-            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(widen<T>(out[(int64_t)r * p.ldo]) + alpha(turn[r * 33 + lane]));
-          } else {
-#pragma unroll 8
-            for (uint32_t r = 0; r < n_rows; ++r) out[(int64_t)r * p.ldo] = narrow<T>(alpha(turn[r * 33 + lane]));
-          }
+          for (uint32_t r = 0; r < n_rows; ++r)
+#pragma unroll
+            for (uint32_t h = 0; h < (decltype(both)::value ? TURN : 32); h += 32) {
+              T* const to = out + (int64_t)r * p.ldo + h;
+              const float sum = alpha(turn[r * (TURN + 1) + h + lane]);
+              *to = narrow<T>(decltype(add)::value ? widen<T>(*to) + sum : sum);
+            }
+        };
+        using Yes = std::true_type;
+        using No = std::false_type;
+        const bool second = TURN == 64 && col0 + 32 + lane < p.cols;
+        if (sizeof(T) == 4 && p.accumulate) {
+          if (second)
+            rows(Yes{}, Yes{});
+          else if (col0 + lane < p.cols)
+            rows(Yes{}, No{});
+        } else {
+          if (second)
+            rows(No{}, Yes{});
+          else if (col0 + lane < p.cols)
+            rows(No{}, No{});
         }
         __syncwarp();
       }
