@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -116,7 +117,8 @@ def lib():
                                       ctypes.c_int32, vp, sz, vp]
         L.pvt_dequant.restype = ctypes.c_int
         L.pvt_dequant.argtypes = [lp, vp, ctypes.c_int32, vp, vp]
-        i32, i64, mp, dp = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(pvt_mx), ctypes.POINTER(pvt_distill)
+        i32, i64 = ctypes.c_int32, ctypes.c_int64
+        mp = dp = vp  # descriptors: a structure by reference, or its bytes
         L.pvt_mx_scale_bytes.restype = sz
         L.pvt_mx_scale_bytes.argtypes = [i32, i32, i32]
         L.pvt_mx_quantize.restype = ctypes.c_int
@@ -348,16 +350,19 @@ def _status_word(t: Optional[torch.Tensor]) -> Optional[int]:
     return _ptr(t)
 
 
-class Mx:
-    """A matrix in 4-bit block floating point: its tensors and its descriptor."""
+# pvt_mx and pvt_distill as bytes (a third of the time that a ctypes.Structure takes to make)
+_pack_mx = struct.Struct("iiiiqPPP").pack
+_pack_distill = struct.Struct("qiiPqifPPPP").pack
 
-    def __init__(self, codes, scales, rows, cols, fmt, tensor_scale):
+
+class Mx:
+    """A matrix in 4-bit block floating point: its tensors and its descriptor (the bytes of a pvt_mx)."""
+
+    def __init__(self, codes, scales, rows, cols, fmt, tensor_scale, ld, device):
         self.codes, self.scales, self.tensor_scale = codes, scales, tensor_scale
-        self.rows, self.cols, self.format = rows, cols, fmt
-        self.device = codes.get_device()
-        self.desc = pvt_mx(rows, cols, fmt, 0, codes.stride(0) if rows > 1 else codes.shape[1], codes.data_ptr(),
-                           scales.data_ptr(), None if tensor_scale is None else tensor_scale.data_ptr())
-        self.ref = ctypes.byref(self.desc)
+        self.rows, self.cols, self.format, self.device = rows, cols, fmt, device
+        self.ref = _pack_mx(rows, cols, fmt, 0, ld, codes.data_ptr(), scales.data_ptr(),
+                            0 if tensor_scale is None else tensor_scale.data_ptr())
 
 
 def make_mx(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt: int,
@@ -369,9 +374,12 @@ def make_mx(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt
         raise ValueError("codes have to be uint8 [rows, bytes], rows and cols positive")
     # (a row is read in pieces of 16 bytes)
     ld, step = codes.stride()
-    if shape[1] % 16 or shape[1] < (cols + 31) // 32 * 16 or step != 1:
+    width = shape[1]
+    if width % 16 or width < (cols + 31) // 32 * 16 or step != 1:
         raise ValueError("a row of codes has to be contiguous and hold ceil(cols / 32) * 16 bytes or a larger multiple of 16")
-    if rows > 1 and (ld % 16 or ld < shape[1]):
+    if rows == 1:
+        ld = width
+    elif ld % 16 or ld < width:
         raise ValueError("rows of codes have to be a multiple of 16 bytes apart")
     if fmt not in (PVT_MX_E8M0_32, PVT_MX_E4M3_16):
         raise ValueError("unknown format")
@@ -386,7 +394,7 @@ def make_mx(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, fmt
             raise ValueError("the tensors of a matrix lie on one CUDA device")
     if device < 0 or scales.get_device() != device:
         raise ValueError("the tensors of a matrix lie on one CUDA device")
-    return Mx(codes, scales, rows, cols, fmt, tensor_scale)
+    return Mx(codes, scales, rows, cols, fmt, tensor_scale, ld, device)
 
 
 def new_mx(rows: int, cols: int, fmt: int, tensor_scale: Optional[torch.Tensor] = None, device=None) -> Mx:
@@ -468,9 +476,9 @@ def pvt_distill_top(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torc
 class Distill:
     """The student's logits and what they are trained against: the tensors and their descriptor."""
 
-    def __init__(self, desc, tensors):
-        self.desc, self.ref, self.tensors = desc, ctypes.byref(desc), tensors
-        self.device, self.rows, self.vocab = tensors[0].get_device(), desc.rows, desc.vocab
+    def __init__(self, ref, tensors, rows, vocab, device):
+        self.ref, self.tensors = ref, tensors  # (the bytes of a pvt_distill)
+        self.device, self.rows, self.vocab = device, rows, vocab
 
 
 def make_distill(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor,
@@ -481,16 +489,17 @@ def make_distill(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.T
     rows, vocab = logits.shape
     dtype, ld = _matrix(logits, rows, vocab, "logits")
     k = int(top_idx.shape[-1])
-    desc = pvt_distill(rows, vocab, k, logits.data_ptr(), ld, dtype, float(temperature),
-                       _vector(top_idx, rows * k, torch.int32, "top_idx"),
-                       _vector(top_logit, rows * k, torch.float32, "top_logit"),
-                       _vector(teacher_lse, rows, torch.float32, "teacher_lse"), _vector(weight, rows, torch.float32, "weight"))
+    ref = _pack_distill(rows, vocab, k, logits.data_ptr(), ld, dtype, float(temperature),
+                        _vector(top_idx, rows * k, torch.int32, "top_idx"),
+                        _vector(top_logit, rows * k, torch.float32, "top_logit"),
+                        _vector(teacher_lse, rows, torch.float32, "teacher_lse") or 0,
+                        _vector(weight, rows, torch.float32, "weight") or 0)
     tensors = (logits, top_idx, top_logit, teacher_lse, weight)
     device = logits.get_device()
     for t in tensors:
         if t is not None and (device < 0 or t.get_device() != device):
             raise ValueError("the tensors of a distillation lie on one CUDA device")
-    return Distill(desc, tensors)
+    return Distill(ref, tensors, rows, vocab, device)
 
 
 def pvt_distill_loss(d: Distill, loss: torch.Tensor, stats: Optional[torch.Tensor] = None,
