@@ -48,9 +48,10 @@ enum { kStatMax = 0, kStatListed = 1, kStatRest = 2, kStatNorm = 3, kStatNormLow
 
 // What a warp has added up of the teacher's list: exponentials e = exp(a), a = logit / temperature - shift, and
 // e (a - (x - near) / temperature), near the largest of the student's logits there; with a remaining mass also
-// exp((x - near) / temperature).
+// exp((x - near) / temperature).  The shift is the row's, not the warp's: where e is 0 the student may have no mass, and an e that
+// is 0 beside the row's largest must not be a number beside the warp's.
 struct Teacher {
-  double shift, mass, cross, own;
+  double mass, cross, own;
   float near;
   uint32_t any;  // an entry above -infinity
 };
@@ -60,6 +61,7 @@ struct DistillShared {
   Running run[THREADS / 32];
   Running mine;
   Teacher teacher[THREADS / 32];
+  float top[THREADS / 32];          // the teacher's largest listed logit, by warp
   uint32_t repeated;
   uint32_t next;                    // run of pieces of the gradient that no warp has taken yet
   float stat[PVT_DISTILL_STATS];
@@ -114,6 +116,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
   T first_x = narrow<T>(0.0f);
   if (active) {
     bool bad = false;
+    float top = kMinusInf;
+    auto keep_top = [&] {
+      top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(top)));
+      if (tid % 32 == 0) sm.top[tid / 32] = top;
+    };
     for (uint32_t i = tid; i < k; i += THREADS) {
       int32_t at = i == tid ? first_idx : p.top_idx[(int64_t)r * k + i];
       if (at >= (int32_t)p.vocab) bad = true, at = -1;
@@ -122,22 +129,30 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
         if (atomicOr(&listed[bit / 32], 1u << (bit % 32)) >> (bit % 32) & 1u) sm.repeated = 1;
       }
       list_idx[i] = at < 0 ? -1 : at;
-      list_val[i] = i == tid ? first_val : p.top_logit[(int64_t)r * k + i];
+      const float val = i == tid ? first_val : p.top_logit[(int64_t)r * k + i];
+      list_val[i] = val;
+      if (at >= 0) top = fmaxf(top, val);  // (a NaN shows in the sums)
       // before any block writes the gradient over the logits; a thread's first is looked at after the pass over the row
       if (i != tid)
         list_x[i] = at >= 0 ? widen<T>(row[at]) : 0.0f;
       else if (at >= 0)
         first_x = row[at];
     }
+    if (MODE & kLoss) keep_top();
     __syncthreads();
     if (sm.repeated) {
       uint32_t again = 0;  // of this thread's entries
+      top = kMinusInf;
       for (uint32_t i = tid, n = 0; i < k; i += THREADS, ++n)
         for (uint32_t j = 0; j < i; ++j)
           if (list_idx[i] >= 0 && list_idx[j] == list_idx[i]) again |= 1u << n;
       __syncthreads();
       for (uint32_t i = tid, n = 0; i < k; i += THREADS, ++n)
-        if (again >> n & 1u) list_idx[i] = -1, bad = true;
+        if (again >> n & 1u)
+          list_idx[i] = -1, bad = true;
+        else if (list_idx[i] >= 0)
+          top = fmaxf(top, list_val[i]);
+      if (MODE & kLoss) keep_top();
       __syncthreads();
     }
     if (bad && p.status) atomicOr(p.status, PVT_DEV_BAD_INDEX);
@@ -146,6 +161,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
   float m = 0.0f, f_rest = 0.0f;  // of the row: largest logit, factor of what is not listed
   if (MODE & kLoss) {
     Running run;
+    double shift = lse;
     if (active) {
       using Top = Tops<T>;
       auto add = [&](const Piece<T>& piece, uint32_t i) {
@@ -190,23 +206,24 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
       }
       // the teacher's sums of this warp's entries
       if (tid < k) list_x[tid] = widen<T>(first_x);
-      float top = kMinusInf, near = kMinusInf;
+      float near = kMinusInf;
       bool any = false;
       for (uint32_t i = tid; i < k; i += THREADS)
         if (list_idx[i] >= 0) {
-          top = fmaxf(top, list_val[i]);
           any |= list_val[i] != kMinusInf;  // (a NaN shows in the sums)
           if (list_x[i] < -kMinusInf) near = fmaxf(near, list_x[i]);
         }
       Teacher t = {};
       t.any = __any_sync(0xffffffffu, any);
-      top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(top)));
       near = from_ordered(__reduce_max_sync(0xffffffffu, ordered(near)));
       t.near = near == kMinusInf ? 0.0f : near;
-      t.shift = tail ? (double)lse : top == kMinusInf ? 0.0 : (double)top * p.inv_t;
+      if (!tail) {
+        const float top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(sm.top[tid % (THREADS / 32)])));
+        shift = top == kMinusInf ? 0.0 : (double)top * p.inv_t;
+      }
       for (uint32_t i = tid; i < k; i += THREADS)
         if (list_idx[i] >= 0) {
-          const double a = (double)list_val[i] * p.inv_t - t.shift, e = exp(a);
+          const double a = (double)list_val[i] * p.inv_t - shift, e = exp(a);
           t.mass += e;
           const double b = ((double)list_x[i] - (double)t.near) * p.inv_t;
           if (e != 0.0) t.cross += e * (a - b);
@@ -237,7 +254,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
     // Without a remaining mass every logit's factor is 1 / z: the others go on to the gradient meanwhile.
     const float f_all = 1.0f / run.z;
     if (!tail) active = any && !(run.m == kMinusInf && run.z == 0.0f);
-    // One warp puts it together: the teacher's sums relative to the largest shift, the factors, the loss
+    // One warp puts it together: the teacher's sums, the factors, the loss
     //   sum p (log p - (x - largest) / T) + log z (P + p_rest) + p_rest (log p_rest - log r).
     if (tid < 32) {
       constexpr uint32_t kWarps = THREADS / 32;
@@ -245,11 +262,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
       float f_listed = 0.0f, f_rest = 0.0f;
       if (active) {
         const Teacher t = sm.teacher[tid % kWarps];
-        double shift = t.any ? t.shift : (double)kMinusInf;
-#pragma unroll
-        for (int st = kWarps / 2; st >= 1; st /= 2) shift = fmax(shift, __shfl_xor_sync(0xffffffffu, shift, st));
-        const double by = t.any ? t.shift - shift : 0.0, f = t.any ? exp(by) : 0.0;
-        double mass = t.any ? f * t.mass : 0.0, cross = t.any ? f * (t.cross + (by + ((double)run.base() - (double)t.near) * p.inv_t) * t.mass) : 0.0;
+        double mass = t.any ? t.mass : 0.0;
+        double cross = t.any ? t.cross + ((double)run.base() - (double)t.near) * p.inv_t * t.mass : 0.0;
 #pragma unroll
         for (int st = kWarps / 2; st >= 1; st /= 2) {
           mass += __shfl_xor_sync(0xffffffffu, mass, st);
