@@ -4,9 +4,10 @@
 // the gradient, a second time, which the L2 serves: with y = 2^(c (x - largest)) every unlisted logit gets y times one factor.
 // The listed ones are overwritten after that.  What concerns the k listed entries alone, the teacher's probabilities and the loss, is
 // computed in binary64, where the remaining mass 1 - sum p is a small difference too.  With that mass as one more outcome
-// the pass sums what is not listed, told from the rest by one bit per entry of the vocabulary in shared memory, and the
-// listed exponentials are added in binary64: a sum of all less the listed ones would lose what a student near its teacher leaves
-// to the rest, and its loss, a small difference of log sums, is as good as the two sums agree.
+// the pass sums what is not listed, told from the rest by one bit per entry of the vocabulary in shared memory, relative to the
+// largest logit that is not listed (beside a listed one the sum could be 0 in binary32 although its logarithm is a number),
+// and the listed exponentials are added in binary64: a sum of all less the listed ones would lose what a student near its
+// teacher leaves to the rest, and its loss, a small difference of log sums, is as good as the two sums agree.
 // A few long rows are shared by clusters of blocks.
 // 4096 x 32000 bf16, loss and gradient in one pass: 102 us, 81 at the copy's rate.  Issue slots 64 % (two exponentials and a
 // rounding per element), and about as much of the L2 as five blocks per SM may hold of rows between their two readings: six
@@ -43,17 +44,17 @@ struct DistillParams {
 };
 
 // stats of a row: largest logit, factor of y at the listed and at the other logits, logarithm of the teacher's sum in two parts, whether
-// the row has any effect
-enum { kStatMax = 0, kStatListed = 1, kStatRest = 2, kStatNorm = 3, kStatNormLow = 4, kStatActive = 5 };
+// the row has any effect, what y at the other logits is relative to
+enum { kStatMax = 0, kStatListed = 1, kStatRest = 2, kStatNorm = 3, kStatNormLow = 4, kStatActive = 5, kStatRestMax = 6 };
 
 // What a warp has added up of the teacher's list: exponentials e = exp(a), a = logit / temperature - shift, and
-// e (a - (x - near) / temperature), near the largest of the student's logits there; with a remaining mass also
-// exp((x - near) / temperature).  The shift is the row's, not the warp's: where e is 0 the student may have no mass, and an e that
+// e (a - (x - near) / temperature), near the largest of the student's logits there (or 0 as long as that is infinite); with a
+// remaining mass also exp((x - near) / temperature).  The shift is the row's, not the warp's: where e is 0 the student may have no mass, and an e that
 // is 0 beside the row's largest must not be a number beside the warp's.
 struct Teacher {
   double mass, cross, own;
-  float near;
-  uint32_t any;  // an entry above -infinity
+  float near, most;  // (most: infinite too)
+  uint32_t any;      // an entry above -infinity
 };
 
 template <int THREADS>
@@ -158,23 +159,19 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
     if (bad && p.status) atomicOr(p.status, PVT_DEV_BAD_INDEX);
   }
 
-  float m = 0.0f, f_rest = 0.0f;  // of the row: largest logit, factor of what is not listed
+  float m = 0.0f, f_rest = 0.0f;  // what y of what is not listed is relative to, and its factor
   if (MODE & kLoss) {
     Running run;
     double shift = lse;
     if (active) {
       using Top = Tops<T>;
-      auto add = [&](const Piece<T>& piece, uint32_t i) {
-        const float sum = terms(piece, run.base(), p.c);
-        if (!tail) {
-          run.z += sum;
-        } else {
-          const uint32_t bit = (i + 1) * N, mask = listed[bit / 32] >> (bit % 32) & ((1u << N) - 1);
-          if (mask == 0)
-            run.r += sum;
-          else
-            for (uint32_t e = 0; e < N; ++e)
-              if (!(mask >> e & 1u)) run.r += run.term(widen<T>(row[s.head + i * N + e]), p.c);
+      // With a remaining mass listed elements of piece i become -infinity, which add nothing and raise nothing.
+      auto leave_out = [&](Piece<T>& piece, uint32_t i) {
+        const uint32_t bit = (i + 1) * N, mask = listed[bit / 32] >> (bit % 32) & ((1u << N) - 1);
+        if (mask) {
+#pragma unroll
+          for (uint32_t e = 0; e < N; ++e)
+            if (mask >> e & 1u) piece.v[e] = narrow<T>(kMinusInf);
         }
       };
       uint32_t i0 = s.lo + tid;
@@ -182,41 +179,44 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
         Piece<T> piece[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) piece[u] = pieces[i0 + u * THREADS];
+        if (tail) {
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) leave_out(piece[u], i0 + u * THREADS);
+        }
         auto top = Top::of(piece[0]);
 #pragma unroll
         for (int u = 1; u < kUnroll; ++u) top = Top::max(top, Top::of(piece[u]));
         run.raise(Top::value(top), p.c);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) add(piece[u], i0 + u * THREADS);
+        for (int u = 0; u < kUnroll; ++u) run.z += terms(piece[u], run.base(), p.c);
       }
       for (; i0 < s.hi; i0 += THREADS) {
-        const Piece<T> piece = pieces[i0];
+        Piece<T> piece = pieces[i0];
+        if (tail) leave_out(piece, i0);
         run.raise(Top::value(Top::of(piece)), p.c);
-        add(piece, i0);
+        run.z += terms(piece, run.base(), p.c);
       }
       if (tid < s.loose()) {
         const uint32_t at = s.loose_at(tid), bit = at + N - s.head;
-        const float x = widen<T>(row[at]);
-        run.raise(x, p.c);
-        const float y = run.term(x, p.c);
-        if (!tail)
-          run.z += y;
-        else if (!(listed[bit / 32] >> (bit % 32) & 1u))
-          run.r += y;
+        if (!tail || !(listed[bit / 32] >> (bit % 32) & 1u)) {
+          const float x = widen<T>(row[at]);
+          run.raise(x, p.c);
+          run.z += run.term(x, p.c);
+        }
       }
       // the teacher's sums of this warp's entries
       if (tid < k) list_x[tid] = widen<T>(first_x);
-      float near = kMinusInf;
+      float most = kMinusInf;
       bool any = false;
       for (uint32_t i = tid; i < k; i += THREADS)
         if (list_idx[i] >= 0) {
           any |= list_val[i] != kMinusInf;  // (a NaN shows in the sums)
-          if (list_x[i] < -kMinusInf) near = fmaxf(near, list_x[i]);
+          most = fmaxf(most, list_x[i]);
         }
       Teacher t = {};
       t.any = __any_sync(0xffffffffu, any);
-      near = from_ordered(__reduce_max_sync(0xffffffffu, ordered(near)));
-      t.near = near == kMinusInf ? 0.0f : near;
+      t.most = from_ordered(__reduce_max_sync(0xffffffffu, ordered(most)));
+      t.near = fabsf(t.most) == -kMinusInf ? 0.0f : t.most;
       if (!tail) {
         const float top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(sm.top[tid % (THREADS / 32)])));
         shift = top == kMinusInf ? 0.0 : (double)top * p.inv_t;
@@ -241,12 +241,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
         for (int st = 16; st >= 1; st /= 2) t.own += __shfl_xor_sync(0xffffffffu, t.own, st);
       }
       if (tid % 32 == 0) sm.teacher[tid / 32] = t;
-      run = block_merge<true, THREADS>(run, p.c, sm.run);
+      run = block_merge<THREADS>(run, p.c, sm.run);
     }
     if (p.blocks > 1) {
       if (tid == 0) sm.mine = run;
       cluster_sync();
-      run = cluster_merge<true>(&sm.mine, p.blocks, p.c);
+      run = cluster_merge(&sm.mine, p.blocks, p.c);
       cluster_sync();
     }
     bool any = false;
@@ -255,50 +255,57 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
     const float f_all = 1.0f / run.z;
     if (!tail) active = any && !(run.m == kMinusInf && run.z == 0.0f);
     // One warp puts it together: the teacher's sums, the factors, the loss
-    //   sum p (log p - (x - largest) / T) + log z (P + p_rest) + p_rest (log p_rest - log r).
+    //   sum p (log p - (x - largest) / T) + log z (P + p_rest) + p_rest (log p_rest - log r),
+    // r the sum over what is not listed, relative to the largest logit like z.
     if (tid < 32) {
       constexpr uint32_t kWarps = THREADS / 32;
       double norm = 0.0, value = 0.0;
       float f_listed = 0.0f, f_rest = 0.0f;
+      Running whole_row = run;  // (its m alone)
       if (active) {
         const Teacher t = sm.teacher[tid % kWarps];
+        if (tail) whole_row.m = fmaxf(run.m, from_ordered(__reduce_max_sync(0xffffffffu, ordered(t.most))));
+        const double base = whole_row.base();
         double mass = t.any ? t.mass : 0.0;
-        double cross = t.any ? t.cross + ((double)run.base() - (double)t.near) * p.inv_t * t.mass : 0.0;
+        double cross = t.any ? t.cross + (base - (double)t.near) * p.inv_t * t.mass : 0.0;
 #pragma unroll
         for (int st = kWarps / 2; st >= 1; st /= 2) {
           mass += __shfl_xor_sync(0xffffffffu, mass, st);
           cross += __shfl_xor_sync(0xffffffffu, cross, st);
         }
-        double z = run.z;
+        // what is not listed: its sum's factor and the factor's logarithm, relative to the largest logit of all
+        const double below = ((double)run.base() - base) * p.inv_t;
+        double z = run.z, f_below = 1.0;
         if (tail) {
-          z = t.own != 0.0 ? t.own * exp(((double)t.near - (double)run.base()) * p.inv_t) : 0.0;
+          z = t.own != 0.0 ? t.own * exp(((double)t.near - base) * p.inv_t) : 0.0;
 #pragma unroll
           for (int st = kWarps / 2; st >= 1; st /= 2) z += __shfl_xor_sync(0xffffffffu, z, st);
-          z += (double)run.r;
+          f_below = exp(below);
+          if (run.z != 0.0f) z += (double)run.z * f_below;
           // (a row of -infinity alone has no student; z is then 0, or a NaN that shows)
-          active = any && !(run.m == kMinusInf && z == 0.0);
+          active = any && !(whole_row.m == kMinusInf && z == 0.0);
         }
         if (active) {
           const double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
-          const double lane_log = log(tid == 0 ? z : tid == 1 ? mass : tid == 2 ? rest : (double)run.r);
+          const double lane_log = log(tid == 0 ? z : tid == 1 ? mass : tid == 2 ? rest : (double)run.z);
           const double log_z = __shfl_sync(0xffffffffu, lane_log, 0), log_mass = __shfl_sync(0xffffffffu, lane_log, 1);
           const double log_rest = __shfl_sync(0xffffffffu, lane_log, 2), log_r = __shfl_sync(0xffffffffu, lane_log, 3);
           const double listed = tail ? mass : 1.0, whole = listed + rest;
           norm = tail ? shift : shift + log_mass;
           value = (tail ? cross : cross / mass - log_mass) + log_z * whole;
-          if (rest != 0.0) value += rest * (log_rest - log_r);
+          if (rest != 0.0) value += rest * (log_rest - (log_r + below));
           f_listed = f_rest = f_all;
           if (tail) {
             f_listed = (float)(whole / z);
             // nothing unlisted left in the student: no factor is needed there
-            f_rest = (float)(whole / z - (rest != 0.0 && run.r != 0.0f ? rest / (double)run.r : 0.0));
+            f_rest = run.z != 0.0f ? (float)(whole * f_below / z - (rest != 0.0 ? rest / (double)run.z : 0.0)) : 0.0f;
           }
         }
       }
       if (tid == 0) {
-        sm.stat[kStatMax] = run.m, sm.stat[kStatListed] = f_listed, sm.stat[kStatRest] = f_rest;
+        sm.stat[kStatMax] = whole_row.m, sm.stat[kStatListed] = f_listed, sm.stat[kStatRest] = f_rest;
         sm.stat[kStatNorm] = (float)norm, sm.stat[kStatNormLow] = (float)(norm - (double)(float)norm);
-        sm.stat[kStatActive] = active ? 1.0f : 0.0f, sm.stat[6] = sm.stat[7] = 0.0f;
+        sm.stat[kStatActive] = active ? 1.0f : 0.0f, sm.stat[kStatRestMax] = run.m == kMinusInf ? 0.0f : run.m, sm.stat[7] = 0.0f;
         if (rank == 0) p.loss[r] = active ? (float)((double)weight * value) : 0.0f;
       }
       __syncwarp();
@@ -308,7 +315,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
       m = run.m, f_rest = f_all;
       if (tail) {
         __syncthreads();
-        active = sm.stat[kStatActive] != 0.0f, f_rest = sm.stat[kStatRest];
+        active = sm.stat[kStatActive] != 0.0f, m = sm.stat[kStatRestMax], f_rest = sm.stat[kStatRest];
       }
     }
   }
@@ -320,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
       // in place: no block overwrites logits that another has yet to gather
       if (p.blocks > 1) cluster_sync();
       __syncthreads();
-      m = sm.stat[kStatMax], f_rest = sm.stat[kStatRest];
+      m = sm.stat[kStatRestMax], f_rest = sm.stat[kStatRest];
     }
     if (!active) {
       clear<THREADS>(grad, s.from(), s.to());
@@ -328,7 +335,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
     }
     const float up = (float)((double)weight * (double)upstream * p.inv_t);
     f_rest *= up;
-    auto y_of = [&](float x) { return ex2((x - m) * p.c); };
+    auto y_of = [&](float x, float of) { return ex2((x - of) * p.c); };
     if (sizeof(G) == sizeof(T) && (reinterpret_cast<uintptr_t>(grad) - reinterpret_cast<uintptr_t>(row)) % 16 == 0) {
       const Two bb = two(-m, -m), cc = two(p.c, p.c), ff = two(f_rest, f_rest);
       Piece<G>* const to = reinterpret_cast<Piece<G>*>(grad + s.head);
@@ -361,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
       }
       if (tid < s.loose()) {
         const uint32_t at = s.loose_at(tid);
-        grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
+        grad[at] = narrow<G>(y_of(widen<T>(row[at]), m) * f_rest);
       }
     } else {
       // rows of unlike alignment: element by element, a warp along the row
@@ -372,18 +379,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
 #pragma unroll
         for (int u = 0; u < 8; ++u) x[u] = widen<T>(row[at + u * THREADS]);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) grad[at + u * THREADS] = narrow<G>(y_of(x[u]) * f_rest);
+        for (int u = 0; u < 8; ++u) grad[at + u * THREADS] = narrow<G>(y_of(x[u], m) * f_rest);
       }
-      for (; at < to; at += THREADS) grad[at] = narrow<G>(y_of(widen<T>(row[at])) * f_rest);
+      for (; at < to; at += THREADS) grad[at] = narrow<G>(y_of(widen<T>(row[at]), m) * f_rest);
     }
     __syncthreads();
     const double norm = (double)sm.stat[kStatNorm] + (double)sm.stat[kStatNormLow];
-    const float f_listed = sm.stat[kStatListed];
+    const float f_listed = sm.stat[kStatListed], largest = sm.stat[kStatMax];
     for (uint32_t i = tid; i < k; i += THREADS) {
       const int32_t at = list_idx[i];
       if (at < 0 || (uint32_t)at < s.from() || (uint32_t)at >= s.to()) continue;
       const float prob = (float)exp((double)list_val[i] * p.inv_t - norm);
-      grad[at] = narrow<G>((y_of(list_x[i]) * f_listed - prob) * up);
+      grad[at] = narrow<G>((y_of(list_x[i], largest) * f_listed - prob) * up);
     }
   }
 }

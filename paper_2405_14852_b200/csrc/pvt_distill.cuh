@@ -137,16 +137,16 @@ struct Tops<__nv_bfloat16> {
 };
 
 // ---- sums of exponentials ---------------------------------------------------------------------------------
-// Largest value so far, and sums of 2^(c (x - base)) where base is the largest value, or 0 as long as that is infinite: a sum
+// Largest value so far, and the sum of 2^(c (x - base)) where base is the largest value, or 0 as long as that is infinite: a sum
 // over -infinity alone is 0, one with infinity infinite, one with a NaN a NaN.  Differences are formed before the product
 // with c: those of the terms that make up the sum are small, and no product overflows that matters.
 struct Running {
-  float m = kMinusInf, z = 0.0f, r = 0.0f;
+  float m = kMinusInf, z = 0.0f;
   __device__ __forceinline__ float base() const { return fabsf(m) == -kMinusInf ? 0.0f : m; }
   __device__ __forceinline__ void raise(float to, float c) {
     if (to > m) {
       const float f = m == kMinusInf || to == -kMinusInf ? 0.0f : ex2((m - to) * c);
-      z *= f, r *= f, m = to;
+      z *= f, m = to;
     }
   }
   __device__ __forceinline__ float term(float x, float c) const { return ex2((x - base()) * c); }
@@ -173,37 +173,31 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i ^ (i >> 31 & 0x7fffffff)); }
 // over `lanes` lanes (a power of two) that begin at a multiple of it; the same in all of them
-template <bool WITH_R>
 __device__ __forceinline__ Running warp_merge(Running a, float c, int lanes = 32) {
   // (over all lanes: those beyond hold parts of the same sum)
   a.raise(from_ordered(__reduce_max_sync(0xffffffffu, ordered(a.m))), c);
-  for (int s = lanes / 2; s >= 1; s /= 2) {
-    a.z += __shfl_xor_sync(0xffffffffu, a.z, s);
-    if (WITH_R) a.r += __shfl_xor_sync(0xffffffffu, a.r, s);
-  }
+  for (int s = lanes / 2; s >= 1; s /= 2) a.z += __shfl_xor_sync(0xffffffffu, a.z, s);
   return a;
 }
 // over the block, the same in every thread; `sh`: a slot per warp
-template <bool WITH_R, int THREADS>
+template <int THREADS>
 __device__ __forceinline__ Running block_merge(Running a, float c, Running* sh) {
   constexpr int kWarps = THREADS / 32;
-  a = warp_merge<WITH_R>(a, c);
+  a = warp_merge(a, c);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x / 32] = a;
   __syncthreads();
-  return warp_merge<WITH_R>(sh[threadIdx.x % kWarps], c, kWarps);
+  return warp_merge(sh[threadIdx.x % kWarps], c, kWarps);
 }
 // over the cluster, the same in every thread; `mine`: the block's own sums, in shared memory before the cluster's barrier
-template <bool WITH_R>
 __device__ __forceinline__ Running cluster_merge(const Running* mine, uint32_t blocks, float c) {
   const uint32_t at = mma::smem_u32(mine), q = threadIdx.x % kMaxBlocks;
   Running a;
   if (q < blocks) {
     a.m = mma::cluster_load(at + (uint32_t)offsetof(Running, m), q);
     a.z = mma::cluster_load(at + (uint32_t)offsetof(Running, z), q);
-    if (WITH_R) a.r = mma::cluster_load(at + (uint32_t)offsetof(Running, r), q);
   }
   __syncwarp();
-  return warp_merge<WITH_R>(a, c, kMaxBlocks);
+  return warp_merge(a, c, kMaxBlocks);
 }
 #endif
 

@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(THREADS, THREADS != kWide ? kResidentNarrow : 
     bound = warp_bound<1>(&key, (k + kWarps - 1) / kWarps);
   }
   if (tid % 32 == 0) sm.bound[tid / 32] = bound;
-  run = block_merge<false, THREADS>(run, p.c, sm.run);
+  run = block_merge<THREADS>(run, p.c, sm.run);
   bound = __reduce_min_sync(0xffffffffu, sm.bound[tid % kWarps]);
   if (tid == 0) sm.mine = run;
   // what is below reaches no place of the list; -infinity never does
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, THREADS != kWide ? kResidentNarrow : 
   } else {
     if (tid == 0) sm.n = n;
     cluster_sync();
-    run = cluster_merge<false>(&sm.mine, p.blocks, p.c);
+    run = cluster_merge(&sm.mine, p.blocks, p.c);
     // the other blocks' lists, side by side, behind this block's own memory
     uint64_t* lists = reinterpret_cast<uint64_t*>(raw + sizeof(Shared));
     uint32_t size[kMaxBlocks];

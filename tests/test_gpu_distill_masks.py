@@ -13,6 +13,7 @@ TYPES = [torch.float32, torch.float16, torch.bfloat16]
 
 def exact(x, idx, val, lse, temperature):
     """Loss, gradient, q and (for bounds) each row's p and unlisted target of whole tensors in float64; every entry is listed once."""
+    temperature = torch.tensor(temperature).item()  # (the binary32 number that the call takes: 1.5e-8 off at 0.1)
     logq = torch.log_softmax(x.double() / temperature, dim=1)
     at = idx.long()
     logp = val.double() / temperature
@@ -26,7 +27,8 @@ def exact(x, idx, val, lse, temperature):
         others = logq.scatter(1, at, -math.inf)
         log_rest = torch.logsumexp(others, dim=1)
         loss = loss + torch.where(rest > 0, rest * (rest.log() - log_rest), 0.0)
-        share = (others - log_rest[:, None]).exp()
+        # (relative to the largest of them: beside -3.4e38 the logarithm of a sum is not representable, its terms' shares are)
+        share = torch.softmax((x.double() / temperature).scatter(1, at, -math.inf), dim=1)
         unlisted = torch.where(torch.isfinite(log_rest)[:, None], rest[:, None] * share, 0.0)
     whole = listed.sum(dim=1) + (0.0 if lse is None else rest)
     q = logq.exp()
@@ -120,3 +122,77 @@ def test_the_largest_listed_logit_is_that_of_an_entry_which_counts():
     B.pvt_distill_loss(B.make_distill(x, wrong, high), loss, grad=grad, status=status)
     assert status.item() == B.PVT_DEV_BAD_INDEX
     near(loss, grad, want, 1000)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gap,temperature", [(50.0, 1.0), (100.0, 1.0), (1e3, 1.0), (1e4, 1.0), (2e4, 3.0), (20.0, 0.1), (300.0, 0.1)])
+@pytest.mark.parametrize("rows,vocab,k", [(3, 1000, 40), (700, 1000, 40), (2, 66000, 300)])
+def test_unlisted_logits_far_below_the_listed_ones(rows, vocab, k, gap, temperature, dtype):
+    """The rest of the student's mass is no binary32 number beside the listed, but it is a number: so are the loss, a
+    multiple of its logarithm, and the gradient, which hands the rest of the teacher's mass to the unlisted by their shares of it."""
+    gen = torch.Generator("cuda").manual_seed(k)
+    keep = torch.stack([torch.randperm(vocab, device="cuda", generator=gen)[:k] for _ in range(rows)])
+    x = torch.randn(rows, vocab, device="cuda", generator=gen) * min(temperature, 1.0) - gap
+    x[0, ::3] = -math.inf
+    x[1, : vocab // 2] = -gap * 2
+    x.scatter_(1, keep, torch.randn(rows, k, device="cuda", generator=gen))
+    x = x.to(dtype)
+    val = torch.randn(rows, k, device="cuda", generator=gen) * temperature
+    lse = torch.logsumexp(val.double() / temperature, dim=1).float() + 0.2  # the list has e^-0.2 of the mass
+    loss, grad = calls(x, keep.int(), val, lse, temperature)
+    near(loss, grad, exact(x, keep.int(), val, lse, temperature), vocab, temperature)
+
+
+@pytest.mark.parametrize("rows,vocab", FORMS)
+def test_unlisted_logits_of_the_types_lowest_value(rows, vocab):
+    gen = torch.Generator("cuda").manual_seed(2)
+    x = torch.full((rows, vocab), torch.finfo(torch.float32).min, device="cuda")
+    x[:, :50] = torch.randn(rows, 50, device="cuda", generator=gen)
+    idx = torch.arange(30, dtype=torch.int32, device="cuda").expand(rows, 30).contiguous()  # 20 of the others are unlisted too
+    val = torch.randn(rows, 30, device="cuda", generator=gen)
+    lse = torch.logsumexp(val.double(), dim=1).float() + 0.2
+    for some in (x, torch.where(torch.arange(vocab, device="cuda") < 30, x, torch.finfo(torch.float32).min)):
+        loss, grad = calls(some.contiguous(), idx, val, lse, 1.0)
+        near(loss, grad, exact(some, idx, val, lse, 1.0), vocab)
+
+
+def test_the_gradient_of_far_unlisted_logits_agrees_with_differences():
+    """Central differences with step h: off by the third derivative (at most 1 for this loss) times h^2 / 6, and by the roundings of
+    two losses of about 150, 2^-24 of each, and of the perturbed logits, 2^-24 of at most 256 (a slope of at most 1), over 2 h."""
+    gen = torch.Generator("cuda").manual_seed(4)
+    x = torch.randn(1, 40, device="cuda", generator=gen)
+    x[:, 6:] -= 150.0
+    idx = torch.arange(6, dtype=torch.int32, device="cuda")[None]
+    val = torch.randn(1, 6, device="cuda", generator=gen)
+    lse = torch.logsumexp(val.double(), dim=1).float() + 0.5
+    h, n = 2.0 ** -4, 80
+    eye = h * torch.eye(40, device="cuda")
+    rows = torch.cat([x + eye, x - eye])
+    loss = torch.empty(n, device="cuda")
+    B.pvt_distill_loss(B.make_distill(rows, idx.expand(n, 6).contiguous(), val.expand(n, 6).contiguous(),
+                                      teacher_lse=lse.expand(n).contiguous()), loss)
+    slope = (loss[:40] - loss[40:]).double() / (2 * h)
+    one, grad = torch.empty(1, device="cuda"), torch.empty(1, 40, device="cuda")
+    B.pvt_distill_loss(B.make_distill(x, idx, val, teacher_lse=lse), one, grad=grad)
+    noise = 2 * 256 * 2.0 ** -24 + 2 * 256 * 2.0 ** -24 + 4 * off(40)
+    assert ((slope - grad[0].double()).abs() <= h * h / 6 + noise / (2 * h)).all()
+    assert grad[0, 6:].sum().item() < -0.3  # the rest of the mass, 0.39, is asked for
+
+
+def test_a_loss_near_nothing_with_the_remaining_mass():
+    """A student that leaves almost nothing unlisted, as its teacher: the listed part of both sums is binary64, so the loss is off by
+    the unlisted sum's own share of them."""
+    vocab, k, rows = 3000, 4, 64
+    gen = torch.Generator("cuda").manual_seed(6)
+    teacher = torch.full((rows, vocab), -20.0, device="cuda")
+    teacher[:, :k] = torch.randn(rows, k, device="cuda", generator=gen)
+    student = teacher.clone()
+    student[:, k:] += 0.3
+    lse = torch.logsumexp(teacher.double(), dim=1).float()
+    lse = torch.where(torch.arange(rows, device="cuda") % 2 == 0, lse, torch.nextafter(lse, torch.zeros_like(lse)))
+    idx = torch.arange(k, dtype=torch.int32, device="cuda").expand(rows, k).contiguous()
+    val = teacher[:, :k].contiguous()
+    want, _, q, _, unlisted = exact(student, idx, val, lse, 1.0)
+    loss, _ = calls(student, idx, val, lse, 1.0)
+    part = q[:, k:].sum(dim=1) + unlisted.sum(dim=1)
+    assert ((loss.double() - want).abs() <= off(vocab) * part + 2.0 ** -24 * want.abs() + 1e-14).all()
