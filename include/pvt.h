@@ -416,7 +416,9 @@ int pvt_distill_top(const void* logits, int32_t dtype, int64_t ld, int64_t rows,
 /*
  * Distillation from those: for each row, with q = softmax(logits / temperature) of the student,
  *   teacher_lse == NULL: p = softmax of top_logit / temperature over the listed entries, p_rest = 0
- *   otherwise:           p_i = exp(top_logit[i] / temperature - teacher_lse[r]), p_rest = max(0, 1 - sum p)
+ *   otherwise:           p_i = exp(top_logit[i] / temperature - teacher_lse[r]), p_rest = max(0, 1 - sum p), but 0 where the list
+ *                        names the whole vocabulary, and where 1 - sum p is no more than rounding teacher_lse may leave,
+ *                        2^-22 (18 + |teacher_lse[r]|) sum p, and the student has less than a 1024th of that there
  *   loss[r] = weight[r] * (sum over i of p_i (log p_i - log q_i) + p_rest (log p_rest - log q_rest))
  * where q_rest is the student's probability of everything that is not listed.  Terms with p = 0 are 0.
  * grad[r, v] = weight[r] upstream[r] / temperature * d(loss[r] / weight[r]) / d(logits[r, v] / temperature):

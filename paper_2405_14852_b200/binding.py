@@ -485,7 +485,8 @@ def make_distill(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.T
                  teacher_lse: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
                  temperature: float = 1.0) -> Distill:
     """logits [rows, vocab] against the teacher's list (int32 and float32 [rows, k]).  With teacher_lse (float32 [rows], of the
-    same temperature) everything that is not listed is one more outcome, without it the listed probabilities add up to 1."""
+    same temperature) everything that is not listed is one more outcome, without it the listed probabilities add up to 1.  A list
+    that names everything the teacher's mask leaves has no rest (include/pvt.h says when what rounding leaves is taken for none)."""
     rows, vocab = logits.shape
     dtype, ld = _matrix(logits, rows, vocab, "logits")
     k = int(top_idx.shape[-1])

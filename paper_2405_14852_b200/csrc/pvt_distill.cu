@@ -23,6 +23,12 @@ using namespace mma;
 constexpr int kUnroll = 4;  // pieces in flight per thread
 constexpr uint32_t kAsked = 128 * 1024;  // bytes of a row that are asked for ahead
 
+// A binary32 lse is off by its own rounding, 2^-24 of it, and by its sum's: roundings of the largest logit over the temperature (at
+// most the lse and the logarithm of the sum, which is below 7 for a list's worth of entries), of the logarithm, and 40 2^-24 of
+// the terms and their additions.  Together that is less than 2^-22 (18 + |lse|), and a probability as much of itself.
+constexpr double kLseNoise = 1.0 / (1 << 22);
+constexpr double kFewest = 1.0 / 1024;  // of the teacher's rest
+
 enum { kLoss = 1, kGrad = 2, kBoth = 3 };
 
 struct DistillParams {
@@ -286,7 +292,19 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
           active = any && !(whole_row.m == kMinusInf && z == 0.0);
         }
         if (active) {
-          const double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
+          double rest = tail ? (mass == mass ? fmax(0.0, 1.0 - mass) : mass) : 0.0;
+          if (tail && rest > 0.0) {
+            // Where nothing is left to list there is no mass left, and next to nothing may be the rounding of the list's lse alone: a
+            // student that has (nearly) none there either is not asked for it, its logarithm would make much of that.
+            uint32_t named = 0;
+            if (k >= p.vocab) {
+              for (uint32_t i = tid; i < (p.vocab + N + 31) / 32; i += 32) named += __popc(listed[i]);
+              named = __reduce_add_sync(0xffffffffu, named);
+            }
+            if (named == p.vocab ||
+                (rest <= mass * kLseNoise * (18.0 + fabs(shift)) && (double)run.z * f_below < rest * z * kFewest))
+              rest = 0.0;
+          }
           const double lane_log = log(tid == 0 ? z : tid == 1 ? mass : tid == 2 ? rest : (double)run.z);
           const double log_z = __shfl_sync(0xffffffffu, lane_log, 0), log_mass = __shfl_sync(0xffffffffu, lane_log, 1);
           const double log_rest = __shfl_sync(0xffffffffu, lane_log, 2), log_r = __shfl_sync(0xffffffffu, lane_log, 3);

@@ -11,8 +11,9 @@ pytestmark = pytest.mark.gpu
 TYPES = [torch.float32, torch.float16, torch.bfloat16]
 
 
-def exact(x, idx, val, lse, temperature):
-    """Loss, gradient, q and (for bounds) each row's p and unlisted target of whole tensors in float64; every entry is listed once."""
+def exact(x, idx, val, lse, temperature, rest=True):
+    """Loss, gradient, q and (for bounds) each row's p and unlisted target of whole tensors in float64; every entry is listed once.
+    With rest=False the teacher's remaining mass is 0 whatever its lse says."""
     temperature = torch.tensor(temperature).item()  # (the binary32 number that the call takes: 1.5e-8 off at 0.1)
     logq = torch.log_softmax(x.double() / temperature, dim=1)
     at = idx.long()
@@ -23,7 +24,7 @@ def exact(x, idx, val, lse, temperature):
     listed = torch.zeros_like(logq).scatter_(1, at, p)
     unlisted = torch.zeros_like(logq)
     if lse is not None:
-        rest = (1.0 - p.sum(dim=1)).clamp(min=0.0)
+        rest = (1.0 - p.sum(dim=1)).clamp(min=0.0) * rest
         others = logq.scatter(1, at, -math.inf)
         log_rest = torch.logsumexp(others, dim=1)
         loss = loss + torch.where(rest > 0, rest * (rest.log() - log_rest), 0.0)
@@ -196,3 +197,87 @@ def test_a_loss_near_nothing_with_the_remaining_mass():
     loss, _ = calls(student, idx, val, lse, 1.0)
     part = q[:, k:].sum(dim=1) + unlisted.sum(dim=1)
     assert ((loss.double() - want).abs() <= off(vocab) * part + 2.0 ** -24 * want.abs() + 1e-14).all()
+
+
+def lse_noise(lse, p):
+    """What may be left of 1 - sum p by the rounding of a binary32 teacher_lse and of its sum."""
+    return p.sum(dim=1) * 2.0 ** -22 * (18 + lse.double().abs())
+
+
+def list_alone(loss, grad, x, idx, val, lse, temperature):
+    """Near the loss of the list alone.  With lse off by d every p is off by d of itself: the loss by d (1 + loss), the gradient by
+    d (p + q)."""
+    vocab = x.shape[1]
+    want_loss, want_grad, q, p, _ = exact(x, idx, val, None, temperature)
+    d = lse_noise(lse, p)
+    e = off(vocab)
+    assert torch.isfinite(loss).all()
+    assert ((loss.double() - want_loss).abs() <= 2 * e + d * (1 + want_loss) + 2.0 ** -24 * want_loss.abs()).all()
+    eps, tiny = torch.finfo(grad.dtype).eps / 2, torch.finfo(grad.dtype).tiny
+    bound = (2 * e * q + 2.0 ** -23 * p + d[:, None] * (p + q)) / temperature + eps * want_grad.abs() + tiny * eps + 1e-37
+    assert ((grad.double() - want_grad).abs() <= bound).all()
+
+
+def teacher_lists(teacher, k, temperature):
+    """A teacher's list, and its lse: as the list's call gives it, rounded from binary64, and its neighbours to both sides."""
+    rows = teacher.shape[0]
+    idx, val = torch.empty(rows, k, dtype=torch.int32, device="cuda"), torch.empty(rows, k, device="cuda")
+    lse = torch.empty(rows, device="cuda")
+    B.pvt_distill_top(teacher, idx, val, lse, temperature=temperature)
+    t = torch.tensor(temperature).item()
+    rounded = torch.logsumexp(teacher.double() / t, dim=1).float()
+    up = torch.full_like(rounded, math.inf)
+    return idx, val, [lse, rounded, torch.nextafter(rounded, up), torch.nextafter(rounded, -up)]
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.7])
+@pytest.mark.parametrize("shift", [0.0, -7.0, 300.0])
+@pytest.mark.parametrize("rows,vocab", [(200, 40), (700, 130), (3, 1024)])
+def test_a_list_of_the_whole_vocabulary_leaves_nothing(rows, vocab, shift, temperature):
+    gen = torch.Generator("cuda").manual_seed(vocab)
+    teacher = torch.randn(rows, vocab, device="cuda", generator=gen) * 2 + shift
+    student = torch.randn(rows, vocab, device="cuda", generator=gen)
+    idx, val, lses = teacher_lists(teacher, vocab, temperature)
+    for lse in lses:
+        loss, grad = calls(student, idx, val, lse, temperature)
+        list_alone(loss, grad, student, idx, val, lse, temperature)
+    far = lses[0] + 0.1  # whatever the lse says
+    near(*calls(student, idx, val, far, temperature), exact(student, idx, val, far, temperature, rest=False), vocab, temperature)
+
+
+MASKS = [-math.inf, -1e4, torch.finfo(torch.float32).min]
+
+
+@pytest.mark.parametrize("student_mask", MASKS)
+@pytest.mark.parametrize("teacher_mask", MASKS)
+@pytest.mark.parametrize("k", [40, 64])
+@pytest.mark.parametrize("rows,vocab,shift,temperature", [(200, 100, 0.0, 1.0), (700, 1000, 20.0, 0.7), (3, 66000, -7.0, 1.0)])
+def test_a_mask_that_leaves_no_more_than_the_list(rows, vocab, shift, temperature, k, teacher_mask, student_mask):
+    """40 entries are allowed, in teacher and student: the teacher's remaining mass is what rounding its lse leaves, and not asked of
+    a student that has none."""
+    gen = torch.Generator("cuda").manual_seed(vocab + k)
+    allowed = torch.randperm(vocab, device="cuda", generator=gen)[:40]
+    teacher = torch.full((rows, vocab), teacher_mask, device="cuda")
+    teacher[:, allowed] = torch.randn(rows, 40, device="cuda", generator=gen) * 2 + shift
+    student = torch.full((rows, vocab), student_mask, device="cuda")
+    student[:, allowed] = torch.randn(rows, 40, device="cuda", generator=gen)
+    idx, val, lses = teacher_lists(teacher, k, temperature)
+    assert (idx[:, 40:] >= 0).all() == (k == 40 or teacher_mask > -math.inf)
+    left = 0
+    for lse in lses:
+        loss, grad = calls(student, idx, val, lse, temperature)
+        list_alone(loss, grad, student, idx[:, :40], val[:, :40], lse, temperature)
+        p = torch.exp(val.double() / torch.tensor(temperature).item() - lse.double()[:, None])
+        left += (p.sum(dim=1) < 1).sum().item()
+    assert left > rows / 2  # (of 4 rows each: some of both kinds)
+
+
+def test_a_rest_that_rounding_does_not_explain_is_asked_of_every_student():
+    gen = torch.Generator("cuda").manual_seed(3)
+    x = torch.full((5, 300), -math.inf, device="cuda")
+    x[:, :20] = torch.randn(5, 20, device="cuda", generator=gen)
+    idx = torch.arange(20, dtype=torch.int32, device="cuda").expand(5, 20).contiguous()
+    val = torch.randn(5, 20, device="cuda", generator=gen)
+    lse = torch.logsumexp(val.double(), dim=1).float() + 1e-3
+    loss, grad = calls(x, idx, val, lse, 1.0)
+    assert (loss == math.inf).all() and torch.isfinite(grad).all()
