@@ -48,6 +48,11 @@ int check_distill(const pvt_distill* d) {
   return aligned(d->teacher_lse, 4) && aligned(d->weight, 4) ? PVT_OK : PVT_EINVAL;
 }
 
+// in place every element is written where it was read
+bool in_place_ok(const pvt_distill* d, const void* grad, int32_t grad_dtype, int64_t ldg) {
+  return grad != d->logits || (grad_dtype == d->dtype && (ldg == d->ld || d->rows == 1));
+}
+
 }  // namespace
 
 extern "C" {
@@ -123,8 +128,7 @@ int pvt_distill_loss(const pvt_distill* d, float* loss, float* stats, const floa
   if (rc != PVT_OK) return rc;
   if (!loss || !aligned(loss, 4) || !aligned(stats, 4) || !aligned(upstream, 4) || !aligned(status, 4)) return PVT_EINVAL;
   if (grad && !matrix_ok(grad, grad_dtype, ldg, d->vocab)) return PVT_EINVAL;
-  // in place every element is written where it was read
-  if (grad == d->logits && (grad_dtype != d->dtype || ldg != d->ld)) return PVT_EINVAL;
+  if (!in_place_ok(d, grad, grad_dtype, ldg)) return PVT_EINVAL;
   const cudaError_t e = launch_distill_loss(*d, loss, stats, upstream, grad, grad_dtype, ldg, status, device_sm_count(),
                                             static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? PVT_OK : fail(e);
@@ -136,7 +140,7 @@ int pvt_distill_grad(const pvt_distill* d, const float* stats, const float* upst
   if (rc != PVT_OK) return rc;
   if (!stats || !aligned(stats, 4) || !aligned(upstream, 4) || !aligned(status, 4)) return PVT_EINVAL;
   if (!matrix_ok(grad, grad_dtype, ldg, d->vocab)) return PVT_EINVAL;
-  if (grad == d->logits && (grad_dtype != d->dtype || ldg != d->ld)) return PVT_EINVAL;
+  if (!in_place_ok(d, grad, grad_dtype, ldg)) return PVT_EINVAL;
   const cudaError_t e = launch_distill_grad(*d, stats, upstream, grad, grad_dtype, ldg, status, device_sm_count(),
                                             static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? PVT_OK : fail(e);
