@@ -123,12 +123,17 @@ class VStepLayer:
         B.pvt_vstep_trust(self.desc, k_max, ratio, idx, n, stats, self._ws)
         return idx, n, stats
 
-    def quantized(self, fmt: int = B.PVT_MX_E8M0_32, tensor_scale: Optional[torch.Tensor] = None,
+    def quantized(self, fmt: Optional[int] = None, tensor_scale: Optional[torch.Tensor] = None,
                   out: Optional[B.Mx] = None) -> B.Mx:
         """The dequantised weights in 4-bit block floating point: what the forward and backward pass before the next V step
-        multiplies by (pvt_mx_product, pvt_mx_grad_input)."""
+        multiplies by (pvt_mx_product, pvt_mx_grad_input).  fmt is B.PVT_MX_E8M0_32 unless given; with `out`, whose format and
+        tensor_scale count, it and tensor_scale need not be given and may not say otherwise."""
         if out is None:
-            out = B.new_mx(self.rows, self.cols, fmt, tensor_scale, device=self.codes.device)
+            out = B.new_mx(self.rows, self.cols, B.PVT_MX_E8M0_32 if fmt is None else fmt, tensor_scale, device=self.codes.device)
+        elif fmt is not None and fmt != out.format:
+            raise ValueError("out has another format")
+        elif tensor_scale is not None and (out.tensor_scale is None or tensor_scale.data_ptr() != out.tensor_scale.data_ptr()):
+            raise ValueError("out has another tensor_scale, or none")
         B.pvt_mx_quantize(out, self.dequant())
         return out
 

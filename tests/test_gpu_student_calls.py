@@ -35,3 +35,25 @@ def test_one_row_in_place_however_far_the_next_would_be(dtype):
     assert torch.equal(logits, want)
     logits.copy_(keep)
     assert torch.equal(wide, others)  # nothing beside the row was written
+
+
+def test_weights_into_a_given_matrix():
+    """Its format and scale count; another format or scale beside it is refused, not passed over."""
+    dev = VStepLayer.from_host(synth.make_layer(64, 256, cfg=71, codebook_size=256, codebook_fp16=True))
+    scale, other = torch.tensor([0.01], device="cuda"), torch.tensor([0.02], device="cuda")
+    fine = B.new_mx(64, 256, B.PVT_MX_E4M3_16, tensor_scale=scale)
+    coarse, plain = B.new_mx(64, 256, B.PVT_MX_E8M0_32), B.new_mx(64, 256, B.PVT_MX_E4M3_16)
+    for m, alike in ((fine, [dict(), dict(fmt=B.PVT_MX_E4M3_16), dict(tensor_scale=scale), dict(fmt=B.PVT_MX_E4M3_16, tensor_scale=scale)]),
+                     (coarse, [dict(), dict(fmt=B.PVT_MX_E8M0_32)]), (plain, [dict(), dict(fmt=B.PVT_MX_E4M3_16)])):
+        want = dev.quantized(m.format, m.tensor_scale)
+        for kw in alike:
+            m.codes.fill_(0xa5)
+            assert dev.quantized(out=m, **kw) is m
+            assert torch.equal(m.codes, want.codes) and torch.equal(m.scales, want.scales)
+    assert dev.quantized().format == B.PVT_MX_E8M0_32
+    before = fine.codes.clone()
+    for m, kw in ((fine, dict(fmt=B.PVT_MX_E8M0_32)), (coarse, dict(fmt=B.PVT_MX_E4M3_16)), (fine, dict(tensor_scale=other)),
+                  (plain, dict(tensor_scale=scale)), (coarse, dict(tensor_scale=scale))):
+        with pytest.raises(ValueError):
+            dev.quantized(out=m, **kw)
+    assert torch.equal(fine.codes, before)
