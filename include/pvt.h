@@ -330,7 +330,11 @@ int pvt_vstep_block(const pvt_layer* layers, const uint64_t* k, int32_t n_layers
  *   value[r, c] = element[r, c] * scale[r, c / block] * tensor_scale
  *   PVT_MX_E8M0_32: block 32, scale 2^(byte - 127), byte 255 = NaN; no tensor_scale (NULL).
  *   PVT_MX_E4M3_16: block 16, scale an 8-bit float e4m3 whose sign is 0 (byte 127 = NaN); tensor_scale one positive
- *                   finite binary32 on the device, or NULL = 1.
+ *                   finite binary32 on the device, or NULL = 1.  e4m3 reaches from 2^-9 to 448, below 2^-6 with fewer bits: a
+ *                   block whose largest magnitude is below 6 * 2^-6 tensor_scale loses precision, below 6 * 2^-10
+ *                   tensor_scale all of it is 0.  The matrix's largest magnitude / (6 * 448) uses the whole range.  (Normally
+ *                   distributed elements, error in norm: 9.5 % with it; without one 10.3 % at deviation 0.02, 13.5 % at 0.005,
+ *                   96 % at 0.002.  PVT_MX_E8M0_32: 11.5 % at any.)
  * codes: ceil(cols / 2) bytes per row, the element of the even column in the lower half; rows are ld bytes apart, ld a
  * multiple of 16, codes 16-byte aligned and rows * ld bytes readable.  After an odd last column the upper half is zero;
  * bytes behind ceil(cols / 2) are left as they were and never looked at.

@@ -1,6 +1,7 @@
 """Calls on the pass that g comes from as a user may make them: one row of a wider matrix, matrices given to be written, logits of a
 vocabulary of any size, steps replayed on other data, every scale."""
 import math
+import warnings
 
 import pytest
 import torch
@@ -57,3 +58,28 @@ def test_weights_into_a_given_matrix():
         with pytest.raises(ValueError):
             dev.quantized(out=m, **kw)
     assert torch.equal(fine.codes, before)
+
+
+def test_small_weights_under_e4m3_scales_are_warned_of_and_kept_with_a_tensor_scale():
+    """Without a factor for the matrix the scales of small blocks are 0.  With the one that the documentation names an element is off by
+    no more than its rounding and its block's scale's."""
+    dev = VStepLayer.from_host(synth.make_layer(256, 512, cfg=71, codebook_size=256, codebook_fp16=True))
+    dev.scale.mul_(0.001 / dev.dequant().std())
+    w_hat = dev.dequant()
+    with pytest.warns(UserWarning, match="tensor_scale"):
+        lost = dev.quantized(B.PVT_MX_E4M3_16)
+    with pytest.warns(UserWarning, match="tensor_scale"):
+        dev.quantized(out=lost)
+    values = torch.empty_like(w_hat)
+    B.pvt_mx_dequant(lost, values)
+    assert (values == 0).float().mean() > 0.5
+    scale = (w_hat.abs().amax() / (6 * 448)).reshape(1)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        kept = dev.quantized(B.PVT_MX_E4M3_16, tensor_scale=scale)
+        dev.quantized(out=kept)
+        dev.quantized()
+    B.pvt_mx_dequant(kept, values)
+    block = w_hat.view(256, -1, 16).abs().amax(dim=2).repeat_interleave(16, dim=1)
+    # half of the widest step between elements, 2 of 6, and the scale's own rounding, 2^-4, of the largest; its smallest is 2^-9
+    assert ((values - w_hat).abs() <= block * (1 / 6 + 1 / 16) + 6 * 2.0 ** -10 * scale).all()
