@@ -391,12 +391,15 @@ int pvt_mx_product(const pvt_mx* x, const pvt_mx* w, void* y, int32_t y_dtype, i
 /*
  * The gradients of that product, straight through the quantisation (Appendix E: the discretisation counts as the
  * identity).  dy: device, tokens x w->rows (or n) of PVT_BF16, 16-byte aligned, rows lddy elements apart, lddy a
- * multiple of 8.
+ * multiple of 8 (logits that are to become dy in place by pvt_distill_* have their rows that far apart from the start; what lies
+ * between two rows is not looked at).
  *   pvt_mx_grad_input:  dx[t, c] = sum over n of dy[t, n] w[n, c]      dx: tokens x w->cols of dx_dtype (any of the three)
  *   pvt_mx_grad_weight: dw[n, c] = sum over t of dy[t, n] x[t, c]      dw: n x x->cols of PVT_F32, tokens = x->rows; with
  *                       accumulate != 0 it is added to what dw holds (Algorithm 3 sums the gradient of several batches).
- * dw is what a pvt_layer of that shape takes as g.  Elements times scale are exact in bfloat16, sums are binary32, and
- * the tensor scale is applied to the sum.  Results depend on the shapes only.  `status` as above.
+ * dw is what a pvt_layer of that shape takes as g.  Elements times scale are exact in bfloat16, sums are binary32 on the
+ * tensor cores, whose additions cut off where others round (error in norm of normally distributed numbers: 5e-8 for sums of
+ * 2048 terms, 7e-8 of 4096, 2e-7 of 16384, 1.1e-6 of 65536; rounded additions 5e-8, 8e-8, 9e-8, 1.1e-7), and the tensor scale is
+ * applied to the sum.  Results depend on the shapes only.  `status` as above.
  */
 int pvt_mx_grad_input(const void* dy, int64_t lddy, int32_t tokens, const pvt_mx* w, void* dx, int32_t dx_dtype,
                       int64_t lddx, uint32_t* status, void* cuda_stream);

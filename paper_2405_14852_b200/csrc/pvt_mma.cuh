@@ -212,9 +212,10 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t saddr, uint32_t ran
   return at;
 }
 // Arrives at a barrier of any block of the cluster.  What it stands for is this block's own: shared memory that the tensor core
-// beside it reads once the other block says so (shown to it by a fence of its proxy before this), or tensor memory that
-// has been read.  No thread of the other block reads what this one wrote, so there is nothing to release to
-// it; .release.cluster would wait for everything the thread has in flight, 2000 cycles.
+// beside it reads once the other block says so, or tensor memory that has been read.  No thread of the other block reads what
+// this one wrote, so there is nothing to release to it; .release.cluster would wait for everything the thread has in flight,
+// 2000 cycles.  For shared memory this rests on what stands before every call, in this order, and none of it may move: each lane's
+// own stores, its own fence.proxy.async, and a __syncwarp that brings all lanes' fences ahead of the one lane's arrival.
 __device__ __forceinline__ void cluster_arrive(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
