@@ -315,8 +315,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWide ? kResident : kResid
           f_listed = f_rest = f_all;
           if (tail) {
             f_listed = (float)(whole / z);
-            // nothing unlisted left in the student: no factor is needed there
-            f_rest = run.z != 0.0f ? (float)(whole * f_below / z - (rest != 0.0 ? rest / (double)run.z : 0.0)) : 0.0f;
+            // nothing unlisted left in the student: no factor is needed there, but for a NaN that shows
+            f_rest = run.z != 0.0f ? (float)(whole * f_below / z - (rest != 0.0 ? rest / (double)run.z : 0.0)) : z == z ? 0.0f : (float)z;
           }
         }
       }

@@ -281,3 +281,18 @@ def test_a_rest_that_rounding_does_not_explain_is_asked_of_every_student():
     lse = torch.logsumexp(val.double(), dim=1).float() + 1e-3
     loss, grad = calls(x, idx, val, lse, 1.0)
     assert (loss == math.inf).all() and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("rows,vocab", FORMS)
+def test_a_nan_that_is_listed_shows_in_the_whole_row(rows, vocab, tail):
+    gen = torch.Generator("cuda").manual_seed(8)
+    idx = torch.arange(40, dtype=torch.int32, device="cuda").expand(rows, 40).contiguous()
+    val = torch.randn(rows, 40, device="cuda", generator=gen)
+    lse = torch.logsumexp(val.double(), dim=1).float() + 0.1 if tail else None
+    x = torch.randn(rows, vocab, device="cuda", generator=gen)
+    x[0, 37] = math.nan
+    for others in (x, torch.where(torch.arange(vocab, device="cuda") < 40, x, -math.inf)):
+        loss, grad = calls(others.contiguous(), idx, val, lse, 1.0)
+        assert torch.isnan(loss[0]) and torch.isnan(grad[0]).all()
+        assert not torch.isnan(loss[1:]).any() and not torch.isnan(grad[1:]).any()
