@@ -53,7 +53,8 @@ extern "C" {
 /* element types */
 #define PVT_F32 0
 #define PVT_F16 1
-#define PVT_BF16 2 /* calls on pvt_mx and pvt_distill only */
+#define PVT_BF16 2 /* calls on pvt_mx, pvt_distill and pvt_norm only */
+#define PVT_F64 3  /* the weights' gradients of pvt_norm_grad only */
 #define PVT_U8 0
 #define PVT_U16 1
 
@@ -463,6 +464,60 @@ int pvt_distill_grad(const pvt_distill* d, const float* stats, const float* upst
                      int64_t ldg, uint32_t* status, void* cuda_stream);
 
 /*
+ * Norm of the rows ahead of a layer, with the residual stream that it reads.  r = x, or x + residual in binary32 rounded
+ * once to dtype.  Per row, sums in binary32:
+ *   mean = sum of r / cols (PVT_NORM_LAYER; 0 for PVT_NORM_RMS), var = sum of (r - mean)^2 / cols, rstd = 1 / sqrt(var + eps)
+ *   y = (r - mean) * rstd * weight + bias
+ * A row that holds a NaN or an infinity has results that are not numbers, no other row is touched by it; a sum of squares
+ * beyond binary32 gives rstd = 0.  The weights and biases are continuous parameters of the P step like the codebooks.
+ */
+#define PVT_NORM_LAYER 0
+#define PVT_NORM_RMS 1
+#define PVT_NORM_MAX_COLS 32768
+typedef struct pvt_norm {
+  int64_t rows;               /* 1 <= rows < 2^31 */
+  int32_t cols;               /* 1 <= cols <= PVT_NORM_MAX_COLS */
+  int32_t kind;               /* PVT_NORM_* */
+  const void* x;              /* [rows][cols] of dtype, rows ldx elements apart, any alignment of the type */
+  int64_t ldx;
+  const void* residual;       /* the same, rows ldr elements apart, or NULL */
+  int64_t ldr;
+  const void* weight;         /* [cols] of weight_dtype, or NULL = 1 */
+  const void* bias;           /* [cols] of weight_dtype, or NULL = 0 */
+  int32_t dtype;              /* PVT_F32 | PVT_F16 | PVT_BF16 */
+  int32_t weight_dtype;       /* any of the three */
+  float eps;                  /* finite, > 0 */
+  int32_t reserved_;          /* set to 0 */
+} pvt_norm;
+
+/*
+ * total: r, of dtype, rows ldt elements apart; y: of y_dtype, rows ldy elements apart; yq: the binary32 y as by
+ * pvt_mx_quantize, rows x cols of either format, what a product takes; stats: device, 8-byte aligned, rows x 2 floats, mean and rstd
+ * of each row, for pvt_norm_grad.  NULL for what is not wanted, but not for all.  total and y may be x or the residual (of the same
+ * type and distance of rows; not the same one both).
+ */
+int pvt_norm_apply(const pvt_norm* n, void* total, int64_t ldt, void* y, int32_t y_dtype, int64_t ldy, const pvt_mx* yq,
+                   float* stats, void* cuda_stream);
+
+/*
+ * The norm's gradients.  n: as in the forward call, but with x the sum r that was normalised and residual NULL (bias and eps are
+ * not read); stats: from there.  dy, dresidual (what comes down the residual stream, or NULL), dx: rows x cols of `dtype`, rows
+ * lddy, lddr and lddx elements apart.  With xh = (x - mean) rstd and u = weight dy:
+ *   dx = rstd (u - [PVT_NORM_LAYER: sum of u / cols] - xh sum of (u xh) / cols) + dresidual
+ *   dweight[c] = sum over the rows of dy xh,  dbias[c] = sum over the rows of dy
+ * dx is the gradient by x and by the residual both.  dx may be dy, dresidual or x (of the same type and distance of rows).
+ * dweight, dbias: device, cols of dw_dtype (PVT_F32, or PVT_F64 as pvt_adam_update takes it), or NULL; with accumulate != 0
+ * they are added to what is there.  Sums along a row and over the rows of a thread block are binary32, over the blocks binary64, in an
+ * order that depends on the shapes and the device only.
+ * ws: pvt_norm_workspace_bytes(n) bytes, 256-byte aligned, of any content and with none worth keeping afterwards; may be NULL if dweight
+ * and dbias are.  Calls that may overlap on the GPU need one each.
+ */
+size_t pvt_norm_workspace_bytes(const pvt_norm* n); /* 0 if rows or cols is invalid */
+int pvt_norm_grad(const pvt_norm* n, const float* stats, int32_t dtype, const void* dy, int64_t lddy, const void* dresidual,
+                  int64_t lddr, void* dx, int64_t lddx, void* dweight, void* dbias, int32_t dw_dtype, int32_t accumulate, void* ws,
+                  size_t ws_bytes, void* cuda_stream);
+
+/*
  * P step, the half that shares its inputs with the V step (Algorithm 3, P-step lines:
  * grad_codebooks = backprop(grad_phi)).  Chain rule through dequantize_weights,
  * W_hat[r, 8c+i] = scale[r] * v[j][i], v[j] = sum_m C_m[codes[j][m]] (the binary32 sum
@@ -562,6 +617,7 @@ void pvt_set_m1_search(int mode);
 #define PVT_KERNEL_REFINE 8      /* the kernel of pvt_vstep_refine */
 #define PVT_KERNEL_MX 9          /* the kernels of the pvt_mx_* calls */
 #define PVT_KERNEL_DISTILL 10    /* the kernels of the pvt_distill_* calls */
+#define PVT_KERNEL_NORM 11       /* the kernels of the pvt_norm_* calls */
 void pvt_timing_enable(int on);
 /* FP32 FMA throughput of the current device, measured: a kernel of independent FMA chains on every SM, timed with
  * CUDA events (synchronises).  scratch: device, at least 2048 floats per SM.  tflops_out: host. */

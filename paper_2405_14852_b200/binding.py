@@ -25,11 +25,12 @@ PVT_DEV_BAD_INDEX, PVT_DEV_BAD_CODE, PVT_DEV_WAIT_EXPIRED, PVT_DEV_INTERNAL = 1,
 PVT_KERNEL_SELECT, PVT_KERNEL_ENCODE_MAIN, PVT_KERNEL_ENCODE_AUX, PVT_KERNEL_DEQUANT = 0, 1, 2, 3
 PVT_KERNEL_ENCODE_RESCORE = 4
 PVT_KERNEL_PSTEP_GRAD, PVT_KERNEL_ADAM, PVT_KERNEL_TRUST, PVT_KERNEL_REFINE = 5, 6, 7, 8
-PVT_KERNEL_MX, PVT_KERNEL_DISTILL = 9, 10
+PVT_KERNEL_MX, PVT_KERNEL_DISTILL, PVT_KERNEL_NORM = 9, 10, 11
 PVT_M1_AUTO, PVT_M1_FP32, PVT_M1_TENSOR = 0, 1, 2
 PVT_SAMPLE_UNIFORM, PVT_SAMPLE_PROPORTIONAL = 0, 1
 PVT_MX_E8M0_32, PVT_MX_E4M3_16 = 0, 1
 PVT_DISTILL_MAX_K, PVT_DISTILL_MAX_VOCAB, PVT_DISTILL_STATS = 1024, 1 << 20, 8
+PVT_NORM_LAYER, PVT_NORM_RMS, PVT_NORM_MAX_COLS, PVT_F64 = 0, 1, 32768, 3
 
 
 _OUT_DTYPE = {torch.float32: PVT_F32, torch.float16: PVT_F16}
@@ -59,6 +60,15 @@ class pvt_distill(ctypes.Structure):
         ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float),
         ("top_idx", ctypes.c_void_p), ("top_logit", ctypes.c_void_p), ("teacher_lse", ctypes.c_void_p),
         ("weight", ctypes.c_void_p),
+    ]
+
+
+class pvt_norm(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("kind", ctypes.c_int32), ("x", ctypes.c_void_p),
+        ("ldx", ctypes.c_int64), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("weight", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("reserved_", ctypes.c_int32),
     ]
 
 
@@ -137,6 +147,12 @@ def lib():
         L.pvt_distill_loss.argtypes = [dp, vp, vp, vp, vp, i32, i64, vp, vp]
         L.pvt_distill_grad.restype = ctypes.c_int
         L.pvt_distill_grad.argtypes = [dp, vp, vp, vp, i32, i64, vp, vp]
+        L.pvt_norm_apply.restype = ctypes.c_int
+        L.pvt_norm_apply.argtypes = [dp, vp, i64, vp, i32, i64, mp, vp, vp]
+        L.pvt_norm_workspace_bytes.restype = sz
+        L.pvt_norm_workspace_bytes.argtypes = [dp]
+        L.pvt_norm_grad.restype = ctypes.c_int
+        L.pvt_norm_grad.argtypes = [dp, vp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, vp, sz, vp]
         L.pvt_pstep_grad.restype = ctypes.c_int
         L.pvt_pstep_grad.argtypes = [lp, vp, vp, vp, vp]
         L.pvt_adam_update.restype = ctypes.c_int
@@ -350,8 +366,9 @@ def _status_word(t: Optional[torch.Tensor]) -> Optional[int]:
     return _ptr(t)
 
 
-# pvt_mx and pvt_distill as bytes (a third of the time that a ctypes.Structure takes to make)
+# pvt_mx, pvt_distill and pvt_norm as bytes (a third of the time that a ctypes.Structure takes to make)
 _pack_mx = struct.Struct("iiiiqPPP").pack
+_pack_norm = struct.Struct("qiiPqPqPPiifi").pack
 _pack_distill = struct.Struct("qiiPqifPPPP").pack
 
 
@@ -524,6 +541,92 @@ def pvt_distill_grad(d: Distill, stats: torch.Tensor, grad: torch.Tensor, upstre
     up = _vector(upstream, d.rows, torch.float32, "upstream")
     _check(lib().pvt_distill_grad(d.ref, st, up, grad.data_ptr(), dtype, ld, _status_word(status),
                                   _stream_for(d.device, stream, stats, upstream, grad, status)), "pvt_distill_grad")
+
+
+class Norm:
+    """Rows to be normalised, their weights, and the descriptor (the bytes of a pvt_norm)."""
+
+    def __init__(self, ref, tensors, rows, cols, dtype, device):
+        self.ref, self.tensors = ref, tensors
+        self.device, self.rows, self.cols, self.dtype = device, rows, cols, dtype
+
+
+def make_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+              kind: int = PVT_NORM_LAYER, eps: float = 1e-5, residual: Optional[torch.Tensor] = None) -> Norm:
+    """Describe the norm of the rows of x + residual (float32, float16 or bfloat16 [rows, cols], one type, rows of any distance);
+    weight and bias [cols], contiguous, of any of these types, both the same.  For pvt_norm_grad x is the sum and there is no residual."""
+    if x.dim() != 2:
+        raise ValueError("x has to be a matrix")
+    rows, cols = x.shape
+    dtype, ld = _matrix(x, rows, cols, "x")
+    res, ldr = 0, 0
+    if residual is not None:
+        other, ldr = _matrix(residual, rows, cols, "residual")
+        if other != dtype:
+            raise ValueError("residual has to be of x's type")
+        res = residual.data_ptr()
+    w_type = (weight if weight is not None else bias).dtype if weight is not None or bias is not None else torch.float32
+    if w_type not in _DTYPE:
+        raise ValueError("weight and bias have to be float32, float16 or bfloat16")
+    device = x.get_device()
+    for t in (x, residual, weight, bias):
+        if t is not None and (device < 0 or t.get_device() != device):
+            raise ValueError("the tensors of a norm lie on one CUDA device")
+    ref = _pack_norm(rows, cols, kind, x.data_ptr(), ld, res, ldr, _vector(weight, cols, w_type, "weight") or 0,
+                     _vector(bias, cols, w_type, "bias") or 0, dtype, _DTYPE[w_type], eps, 0)
+    return Norm(ref, (x, residual, weight, bias), rows, cols, dtype, device)
+
+
+def pvt_norm_apply(n: Norm, y: Optional[torch.Tensor] = None, quantized: Optional[Mx] = None, total: Optional[torch.Tensor] = None,
+                   stats: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y [rows, cols] of any type, and / or the same as a 4-bit matrix; total: x + residual, of their type (may be either of
+    them); stats: float32 [rows, 2], mean and 1 / deviation of each row, for pvt_norm_grad."""
+    t_ptr, ldt, y_ptr, y_dtype, ldy, q_ref = None, 0, None, PVT_F32, 0, None
+    if total is not None:
+        t_dtype, ldt = _matrix(total, n.rows, n.cols, "total")
+        if t_dtype != n.dtype:
+            raise ValueError("total has to be of x's type")
+        t_ptr = total.data_ptr()
+    if y is not None:
+        y_dtype, ldy = _matrix(y, n.rows, n.cols, "y")
+        y_ptr = y.data_ptr()
+    if quantized is not None:
+        if quantized.rows != n.rows or quantized.cols != n.cols:
+            raise ValueError("quantized has to be of x's shape")
+        q_ref = quantized.ref
+    st = _vector(stats, 2 * n.rows, torch.float32, "stats")
+    _check(lib().pvt_norm_apply(n.ref, t_ptr, ldt, y_ptr, y_dtype, ldy, q_ref, st,
+                                _stream_for(n.device, stream, total, y, quantized and quantized.codes, stats)), "pvt_norm_apply")
+
+
+def pvt_norm_workspace_bytes(n: Norm) -> int:
+    return int(lib().pvt_norm_workspace_bytes(n.ref))
+
+
+def new_norm_workspace(n: Norm) -> torch.Tensor:
+    """Workspace for pvt_norm_grad with weights' gradients; it may be kept for further calls on as many rows and columns."""
+    return torch.empty(pvt_norm_workspace_bytes(n), dtype=torch.uint8, device=torch.device("cuda", n.device))
+
+
+def pvt_norm_grad(n: Norm, stats: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor, dresidual: Optional[torch.Tensor] = None,
+                  dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, accumulate: bool = False,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx [rows, cols] from dy and, if given, dresidual (one type; dx may be either of them or x); dweight and dbias [cols], float32, or
+    float64 as pvt_adam_update takes them, added to what they hold if accumulate."""
+    dtype, ldy = _matrix(dy, n.rows, n.cols, "dy")
+    x_dtype, ldx = _matrix(dx, n.rows, n.cols, "dx")
+    r_dtype, ldr = _matrix(dresidual, n.rows, n.cols, "dresidual") if dresidual is not None else (dtype, 0)
+    if x_dtype != dtype or r_dtype != dtype:
+        raise ValueError("dy, dx and dresidual have to be of one type")
+    w_type = (dweight if dweight is not None else dbias).dtype if dweight is not None or dbias is not None else torch.float32
+    if w_type not in (torch.float32, torch.float64):
+        raise ValueError("dweight and dbias have to be float32 or float64")
+    dw, db = _vector(dweight, n.cols, w_type, "dweight"), _vector(dbias, n.cols, w_type, "dbias")
+    st = _vector(stats, 2 * n.rows, torch.float32, "stats")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().pvt_norm_grad(n.ref, st, dtype, dy.data_ptr(), ldy, _ptr(dresidual), ldr, dx.data_ptr(), ldx, dw, db,
+                               PVT_F64 if w_type == torch.float64 else PVT_F32, 1 if accumulate else 0, _ptr(workspace), ws_bytes,
+                               _stream_for(n.device, stream, stats, dy, dx, dresidual, dweight, dbias, workspace)), "pvt_norm_grad")
 
 
 class Block:

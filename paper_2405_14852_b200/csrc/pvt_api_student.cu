@@ -1,7 +1,8 @@
-// Host side of the calls on the pass that g comes from: 4-bit products and their gradients, distillation.  Arguments are
+// Host side of the calls on the pass that g comes from: 4-bit products and their gradients, norms, distillation.  Arguments are
 // checked here before anything is enqueued.
 #include "pvt_distill.cuh"
 #include "pvt_mx.cuh"
+#include "pvt_norm.cuh"
 
 using namespace pvt;
 
@@ -51,6 +52,20 @@ int check_distill(const pvt_distill* d) {
 // in place every element is written where it was read
 bool in_place_ok(const pvt_distill* d, const void* grad, int32_t grad_dtype, int64_t ldg) {
   return grad != d->logits || (grad_dtype == d->dtype && (ldg == d->ld || d->rows == 1));
+}
+
+bool norm_shape_ok(const pvt_norm* n) { return n && n->rows >= 1 && n->rows <= 0x7fffffff && n->cols >= 1 && n->cols <= PVT_NORM_MAX_COLS; }
+int check_norm(const pvt_norm* n) {
+  if (!norm_shape_ok(n) || (n->kind != PVT_NORM_LAYER && n->kind != PVT_NORM_RMS)) return PVT_EINVAL;
+  if (!matrix_ok(n->x, n->dtype, n->ldx, n->cols)) return PVT_EINVAL;
+  if (n->residual && !matrix_ok(n->residual, n->dtype, n->ldr, n->cols)) return PVT_EINVAL;
+  if (!known_type(n->weight_dtype) || !aligned(n->weight, size_of(n->weight_dtype)) || !aligned(n->bias, size_of(n->weight_dtype)))
+    return PVT_EINVAL;
+  return n->eps > 0.0f && n->eps <= 3.402823466e38f ? PVT_OK : PVT_EINVAL;
+}
+// a result in the place of an operand: every element is written where it was read
+bool same_place_ok(const void* out, int32_t type, int64_t ld, const void* in, int32_t in_type, int64_t in_ld, int64_t rows) {
+  return out != in || !in || (type == in_type && (ld == in_ld || rows == 1));
 }
 
 }  // namespace
@@ -143,6 +158,55 @@ int pvt_distill_grad(const pvt_distill* d, const float* stats, const float* upst
   if (!in_place_ok(d, grad, grad_dtype, ldg)) return PVT_EINVAL;
   const cudaError_t e = launch_distill_grad(*d, stats, upstream, grad, grad_dtype, ldg, status, device_sm_count(),
                                             static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? PVT_OK : fail(e);
+}
+
+int pvt_norm_apply(const pvt_norm* n, void* total, int64_t ldt, void* y, int32_t y_dtype, int64_t ldy, const pvt_mx* yq, float* stats,
+                   void* cuda_stream) {
+  int rc = check_norm(n);
+  if (rc != PVT_OK) return rc;
+  if (!total && !y && !yq && !stats) return PVT_EINVAL;
+  if (total && !matrix_ok(total, n->dtype, ldt, n->cols)) return PVT_EINVAL;
+  if (y && !matrix_ok(y, y_dtype, ldy, n->cols)) return PVT_EINVAL;
+  if (y && y == total) return PVT_EINVAL;
+  if (yq && (rc = check_mx(yq)) != PVT_OK) return rc;
+  if (yq && (yq->rows != n->rows || yq->cols != n->cols)) return PVT_EINVAL;
+  if (!aligned(stats, 8)) return PVT_EINVAL;
+  for (const void* in : {n->x, n->residual}) {
+    const int64_t ld = in == n->x ? n->ldx : n->ldr;
+    if (total && !same_place_ok(total, n->dtype, ldt, in, n->dtype, ld, n->rows)) return PVT_EINVAL;
+    if (y && !same_place_ok(y, y_dtype, ldy, in, n->dtype, ld, n->rows)) return PVT_EINVAL;
+  }
+  const cudaError_t e = norm::launch_apply(*n, total, ldt, y, y ? y_dtype : PVT_F32, ldy, yq, stats, device_sm_count(),
+                                           static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? PVT_OK : fail(e);
+}
+
+size_t pvt_norm_workspace_bytes(const pvt_norm* n) {
+  return norm_shape_ok(n) ? norm::grad_workspace_bytes(n->rows, n->cols, device_sm_count()) : 0;
+}
+
+int pvt_norm_grad(const pvt_norm* n, const float* stats, int32_t dtype, const void* dy, int64_t lddy, const void* dresidual, int64_t lddr,
+                  void* dx, int64_t lddx, void* dweight, void* dbias, int32_t dw_dtype, int32_t accumulate, void* ws, size_t ws_bytes,
+                  void* cuda_stream) {
+  const int rc = check_norm(n);
+  if (rc != PVT_OK) return rc;
+  if (n->residual || !stats || !aligned(stats, 8)) return PVT_EINVAL;
+  if (!matrix_ok(dy, dtype, lddy, n->cols) || !matrix_ok(dx, dtype, lddx, n->cols)) return PVT_EINVAL;
+  if (dresidual && !matrix_ok(dresidual, dtype, lddr, n->cols)) return PVT_EINVAL;
+  if (!same_place_ok(dx, dtype, lddx, dy, dtype, lddy, n->rows) || !same_place_ok(dx, dtype, lddx, dresidual, dtype, lddr, n->rows) ||
+      !same_place_ok(dx, dtype, lddx, n->x, n->dtype, n->ldx, n->rows))
+    return PVT_EINVAL;
+  if (dweight || dbias) {
+    if (dw_dtype != PVT_F32 && dw_dtype != PVT_F64) return PVT_EINVAL;
+    const size_t size = dw_dtype == PVT_F64 ? 8 : 4;
+    if (!aligned(dweight, size) || !aligned(dbias, size) || dweight == dbias) return PVT_EINVAL;
+    if (!ws || !aligned(ws, 256)) return PVT_EINVAL;
+    if (ws_bytes < pvt_norm_workspace_bytes(n)) return PVT_EWORKSPACE;
+  }
+  const cudaError_t e =
+      norm::launch_grad(*n, stats, dtype, dy, lddy, dresidual, lddr, dx, lddx, dweight, dbias, dw_dtype, accumulate != 0, ws,
+                        device_sm_count(), static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? PVT_OK : fail(e);
 }
 
