@@ -408,6 +408,39 @@ int pvt_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const pvt_mx* x,
                        int32_t accumulate, uint32_t* status, void* cuda_stream);
 
 /*
+ * A gated pair of linear layers: h[t, n] = f(a) b with a = sum over c of x[t, c] w_gate[n, c], b = the same of w_up.
+ *   PVT_ACT_SILU       f(a) = a / (1 + exp(-a))
+ *   PVT_ACT_GELU       f(a) = a (1 + erf(a / sqrt 2)) / 2
+ *   PVT_ACT_GELU_TANH  f(a) = a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2
+ * x: tokens x inputs; w_gate, w_up: outputs x inputs, all of one format; each has a tensor scale of its own, or none.  Products and
+ * sums as by pvt_mx_product, f and the product by it in binary32.
+ * h: device, tokens x outputs of h_dtype (any of the three), rows ldh elements apart, each element rounded once; hq: the
+ * binary32 values as by pvt_mx_quantize, tokens x outputs of x's format, what the product with the next layer takes.  NULL for the one
+ * that is not wanted.  Neither may overlap an operand.  Results depend on the shapes only.  `status` as above.
+ */
+#define PVT_ACT_SILU 0
+#define PVT_ACT_GELU 1
+#define PVT_ACT_GELU_TANH 2
+int pvt_mx_gated(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int32_t activation, void* h, int32_t h_dtype, int64_t ldh,
+                 const pvt_mx* hq, uint32_t* status, void* cuda_stream);
+
+/*
+ * Its gradients, straight through the quantisation.
+ *   pvt_mx_gated_grad:        dgate[t, n] = dh b f'(a), dup[t, n] = dh f(a), a and b computed again from the same operands.
+ *                             dh: tokens x outputs of dh_dtype (any of the three), rows lddh elements apart.  dgate, dup: the same
+ *                             shape of PVT_BF16, as pvt_mx_grad_weight takes them for dw_gate = dgate^T x and dw_up = dup^T x:
+ *                             16-byte aligned, rows ldd elements apart, ldd a multiple of 8 and below 2^38.  Either may be dh (of PVT_BF16,
+ *                             the same distance of rows).
+ *   pvt_mx_gated_grad_input:  dx[t, c] = sum over n of dgate[t, n] w_gate[n, c] + dup[t, n] w_up[n, c], in one binary32 sum rounded once.
+ *                             dx: tokens x inputs of dx_dtype, rows lddx elements apart.  One sum has one factor: w_gate and w_up have
+ *                             the same tensor_scale (the same pointer), or none.
+ */
+int pvt_mx_gated_grad(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int32_t activation, const void* dh, int32_t dh_dtype,
+                      int64_t lddh, void* dgate, void* dup, int64_t ldd, uint32_t* status, void* cuda_stream);
+int pvt_mx_gated_grad_input(const void* dgate, const void* dup, int64_t ldd, int32_t tokens, const pvt_mx* w_gate, const pvt_mx* w_up,
+                            void* dx, int32_t dx_dtype, int64_t lddx, uint32_t* status, void* cuda_stream);
+
+/*
  * A teacher's largest logits (the method trains against the predictions of the model before quantisation).  logits:
  * device, rows x vocab of dtype (any of the three), rows ld elements apart.  Per row:
  *   top_idx[r, 0..k): the k entries that come first in the order of (value descending, index ascending); NaN counts as

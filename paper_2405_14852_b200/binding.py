@@ -30,6 +30,7 @@ PVT_M1_AUTO, PVT_M1_FP32, PVT_M1_TENSOR = 0, 1, 2
 PVT_SAMPLE_UNIFORM, PVT_SAMPLE_PROPORTIONAL = 0, 1
 PVT_MX_E8M0_32, PVT_MX_E4M3_16 = 0, 1
 PVT_DISTILL_MAX_K, PVT_DISTILL_MAX_VOCAB, PVT_DISTILL_STATS = 1024, 1 << 20, 8
+PVT_ACT_SILU, PVT_ACT_GELU, PVT_ACT_GELU_TANH = 0, 1, 2
 PVT_NORM_LAYER, PVT_NORM_RMS, PVT_NORM_MAX_COLS, PVT_F64 = 0, 1, 32768, 3
 
 
@@ -147,6 +148,12 @@ def lib():
         L.pvt_distill_loss.argtypes = [dp, vp, vp, vp, vp, i32, i64, vp, vp]
         L.pvt_distill_grad.restype = ctypes.c_int
         L.pvt_distill_grad.argtypes = [dp, vp, vp, vp, i32, i64, vp, vp]
+        L.pvt_mx_gated.restype = ctypes.c_int
+        L.pvt_mx_gated.argtypes = [mp, mp, mp, i32, vp, i32, i64, mp, vp, vp]
+        L.pvt_mx_gated_grad.restype = ctypes.c_int
+        L.pvt_mx_gated_grad.argtypes = [mp, mp, mp, i32, vp, i32, i64, vp, vp, i64, vp, vp]
+        L.pvt_mx_gated_grad_input.restype = ctypes.c_int
+        L.pvt_mx_gated_grad_input.argtypes = [vp, vp, i64, i32, mp, mp, vp, i32, i64, vp, vp]
         L.pvt_norm_apply.restype = ctypes.c_int
         L.pvt_norm_apply.argtypes = [dp, vp, i64, vp, i32, i64, mp, vp, vp]
         L.pvt_norm_workspace_bytes.restype = sz
@@ -476,6 +483,50 @@ def pvt_mx_grad_weight(dy: torch.Tensor, x: Mx, dw: torch.Tensor, accumulate: bo
     _check(lib().pvt_mx_grad_weight(dy.data_ptr(), ldy, dy.shape[1], x.ref, dw.data_ptr(), ld, 1 if accumulate else 0,
                                     _status_word(status), _stream_for(x.device, stream, dy, dw, status)),
            "pvt_mx_grad_weight")
+
+
+def pvt_mx_gated(x: Mx, w_gate: Mx, w_up: Mx, h: Optional[torch.Tensor] = None, quantized: Optional[Mx] = None,
+                 activation: int = PVT_ACT_SILU, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """h [tokens, outputs] = f(x w_gate^T) (x w_up^T), of any type, and / or the same as a 4-bit matrix of x's format."""
+    ptr, dtype, ld, ref = None, PVT_F32, 0, None
+    if h is not None:
+        dtype, ld = _matrix(h, x.rows, w_gate.rows, "h")
+        ptr = h.data_ptr()
+    if quantized is not None:
+        if quantized.rows != x.rows or quantized.cols != w_gate.rows or quantized.format != x.format:
+            raise ValueError("quantized has to be tokens x outputs, of x's format")
+        ref = quantized.ref
+    _check(lib().pvt_mx_gated(x.ref, w_gate.ref, w_up.ref, activation, ptr, dtype, ld, ref, _status_word(status),
+                              _stream_for(x.device, stream, w_gate.codes, w_up.codes, h, quantized and quantized.codes, status)),
+           "pvt_mx_gated")
+
+
+def pvt_mx_gated_grad(x: Mx, w_gate: Mx, w_up: Mx, dh: torch.Tensor, dgate: torch.Tensor, dup: torch.Tensor,
+                      activation: int = PVT_ACT_SILU, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dgate and dup, bfloat16 [tokens, outputs] as pvt_mx_grad_weight takes them, from dh (any type; either may be dh itself)."""
+    dtype, ldh = _matrix(dh, x.rows, w_gate.rows, "dh")
+    ldd = _gradient_pair(dgate, dup, x.rows, w_gate.rows)
+    _check(lib().pvt_mx_gated_grad(x.ref, w_gate.ref, w_up.ref, activation, dh.data_ptr(), dtype, ldh, dgate.data_ptr(),
+                                   dup.data_ptr(), ldd, _status_word(status),
+                                   _stream_for(x.device, stream, w_gate.codes, w_up.codes, dh, dgate, dup, status)), "pvt_mx_gated_grad")
+
+
+def _gradient_pair(dgate: torch.Tensor, dup: torch.Tensor, tokens: int, outputs: int) -> int:
+    ldd, other = _gradient(dgate, tokens, outputs), _gradient(dup, tokens, outputs)
+    if tokens > 1 and ldd != other:
+        raise ValueError("the rows of dgate and dup have to be equally far apart")
+    return min(ldd, other)
+
+
+def pvt_mx_gated_grad_input(dgate: torch.Tensor, dup: torch.Tensor, w_gate: Mx, w_up: Mx, dx: torch.Tensor,
+                            status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx [tokens, inputs] = dgate w_gate + dup w_up; the two matrices share their tensor_scale, if they have one."""
+    tokens = dgate.shape[0]
+    ldd = _gradient_pair(dgate, dup, tokens, w_gate.rows)
+    dtype, ld = _matrix(dx, tokens, w_gate.cols, "dx")
+    _check(lib().pvt_mx_gated_grad_input(dgate.data_ptr(), dup.data_ptr(), ldd, tokens, w_gate.ref, w_up.ref, dx.data_ptr(), dtype, ld,
+                                         _status_word(status), _stream_for(w_gate.device, stream, w_up.codes, dgate, dup, dx, status)),
+           "pvt_mx_gated_grad_input")
 
 
 def pvt_distill_top(logits: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor, lse: Optional[torch.Tensor] = None,

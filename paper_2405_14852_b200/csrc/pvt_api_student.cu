@@ -68,6 +68,16 @@ bool same_place_ok(const void* out, int32_t type, int64_t ld, const void* in, in
   return out != in || !in || (type == in_type && (ld == in_ld || rows == 1));
 }
 
+int check_gated(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int32_t activation) {
+  for (const pvt_mx* m : {x, w_gate, w_up})
+    if (const int rc = check_mx(m)) return rc;
+  if (activation != PVT_ACT_SILU && activation != PVT_ACT_GELU && activation != PVT_ACT_GELU_TANH) return PVT_EINVAL;
+  return x->format == w_gate->format && x->format == w_up->format && x->cols == w_gate->cols && x->cols == w_up->cols &&
+                 w_gate->rows == w_up->rows
+             ? PVT_OK
+             : PVT_EINVAL;
+}
+
 }  // namespace
 
 extern "C" {
@@ -122,6 +132,46 @@ int pvt_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const pvt_mx* x,
   if (!matrix_ok(dw, PVT_F32, lddw, x->cols)) return PVT_EINVAL;
   const cudaError_t e = launch_mx_grad_weight(dy, lddy, n, *x, dw, lddw, accumulate != 0, status, device_sm_count(),
                                               static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? PVT_OK : fail(e);
+}
+
+int pvt_mx_gated(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int32_t activation, void* h, int32_t h_dtype, int64_t ldh,
+                 const pvt_mx* hq, uint32_t* status, void* cuda_stream) {
+  int rc = check_gated(x, w_gate, w_up, activation);
+  if (rc != PVT_OK) return rc;
+  if ((!h && !hq) || !aligned(status, 4)) return PVT_EINVAL;
+  if (h && !matrix_ok(h, h_dtype, ldh, w_gate->rows)) return PVT_EINVAL;
+  if (hq && (rc = check_mx(hq)) != PVT_OK) return rc;
+  if (hq && (hq->format != x->format || hq->rows != x->rows || hq->cols != w_gate->rows)) return PVT_EINVAL;
+  const cudaError_t e = launch_mx_gated(*x, *w_gate, *w_up, activation, h, h ? h_dtype : PVT_F32, ldh, hq, status, device_sm_count(),
+                                        static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? PVT_OK : fail(e);
+}
+
+int pvt_mx_gated_grad(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int32_t activation, const void* dh, int32_t dh_dtype,
+                      int64_t lddh, void* dgate, void* dup, int64_t ldd, uint32_t* status, void* cuda_stream) {
+  const int rc = check_gated(x, w_gate, w_up, activation);
+  if (rc != PVT_OK) return rc;
+  if (!matrix_ok(dh, dh_dtype, lddh, w_gate->rows) || !aligned(status, 4)) return PVT_EINVAL;
+  if (!gradient_ok(dgate, ldd, x->rows, w_gate->rows) || !gradient_ok(dup, ldd, x->rows, w_gate->rows) || dgate == dup) return PVT_EINVAL;
+  if (!same_place_ok(dgate, PVT_BF16, ldd, dh, dh_dtype, lddh, x->rows) || !same_place_ok(dup, PVT_BF16, ldd, dh, dh_dtype, lddh, x->rows))
+    return PVT_EINVAL;
+  const cudaError_t e = launch_mx_gated_grad(*x, *w_gate, *w_up, activation, dh, dh_dtype, lddh, dgate, dup, ldd, status,
+                                             device_sm_count(), static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? PVT_OK : fail(e);
+}
+
+int pvt_mx_gated_grad_input(const void* dgate, const void* dup, int64_t ldd, int32_t tokens, const pvt_mx* w_gate, const pvt_mx* w_up,
+                            void* dx, int32_t dx_dtype, int64_t lddx, uint32_t* status, void* cuda_stream) {
+  int rc = check_mx(w_gate);
+  if (rc == PVT_OK) rc = check_mx(w_up);
+  if (rc != PVT_OK) return rc;
+  if (w_gate->format != w_up->format || w_gate->rows != w_up->rows || w_gate->cols != w_up->cols) return PVT_EINVAL;
+  if (w_gate->tensor_scale != w_up->tensor_scale) return PVT_EINVAL;  // one sum, one factor
+  if (!gradient_ok(dgate, ldd, tokens, w_gate->rows) || !gradient_ok(dup, ldd, tokens, w_gate->rows) || !aligned(status, 4)) return PVT_EINVAL;
+  if (!matrix_ok(dx, dx_dtype, lddx, w_gate->cols)) return PVT_EINVAL;
+  const cudaError_t e = launch_mx_gated_grad_input(dgate, dup, ldd, tokens, *w_gate, *w_up, dx, dx_dtype, lddx, status, device_sm_count(),
+                                                   static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? PVT_OK : fail(e);
 }
 

@@ -92,5 +92,13 @@ cudaError_t launch_mx_grad_input(const void* dy, int64_t lddy, int32_t tokens, c
                                  int64_t lddx, uint32_t* status, int sm_count, cudaStream_t stream);
 cudaError_t launch_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const pvt_mx& x, float* dw, int64_t lddw,
                                   bool accumulate, uint32_t* status, int sm_count, cudaStream_t stream);
+// h = f(x wg^T) (x wu^T), as floats (h) and / or in 4 bits (hq), and its gradients by both products
+cudaError_t launch_mx_gated(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, int32_t activation, void* h, int32_t dtype, int64_t ldh,
+                            const pvt_mx* hq, uint32_t* status, int sm_count, cudaStream_t stream);
+cudaError_t launch_mx_gated_grad(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, int32_t activation, const void* dh, int32_t dtype,
+                                 int64_t lddh, void* dgate, void* dup, int64_t ldd, uint32_t* status, int sm_count, cudaStream_t stream);
+// dx = dgate wg + dup wu, in one set of sums
+cudaError_t launch_mx_gated_grad_input(const void* dgate, const void* dup, int64_t ldd, int32_t tokens, const pvt_mx& wg, const pvt_mx& wu,
+                                       void* dx, int32_t dtype, int64_t lddx, uint32_t* status, int sm_count, cudaStream_t stream);
 
 }  // namespace pvt

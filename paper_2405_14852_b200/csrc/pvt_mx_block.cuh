@@ -144,6 +144,49 @@ __device__ __forceinline__ uint32_t quantize_block(float* v, uint32_t top, const
   return byte;
 }
 
+// a matrix that a kernel writes, or none (codes null)
+struct Held {
+  uint8_t *codes, *scales;
+  const float* tensor_scale;
+  int64_t ld;
+  uint32_t cols, tiles;  // tiles of scales, of a strip
+  int32_t format;
+};
+inline Held held(const pvt_mx& m) {
+  return Held{m.codes, m.scales, m.tensor_scale, m.ld, (uint32_t)m.cols, strip_tiles(m.cols, block_of(m.format)), m.format};
+}
+
+// A row's eight neighbouring values of each lane, from column c0 = 8 lane + a multiple of 256 (or of 128, in sixteen lanes) on, into
+// codes and scales.  here: the row exists; listed: it has scales (those of rows and blocks that do not exist are 0).
+template <int FMT>
+__device__ __forceinline__ void put_eight(const Held& m, uint32_t row, uint32_t c0, bool here, bool listed, const TensorScale& t,
+                                          float* v) {
+  constexpr uint32_t LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;  // of a block
+  const uint32_t lane = threadIdx.x & 31, block = c0 / (8 * LANES);
+  uint32_t top = 0, word;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (c0 + i >= m.cols) v[i] = 0.0f;
+    top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  }
+#pragma unroll
+  for (uint32_t d = 1; d < LANES; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+  uint32_t byte = quantize_block<FMT, 8>(v, top, t, &word);
+  if (c0 >= m.cols || !here) byte = 0;  // no such block
+  uint32_t four = byte | __shfl_down_sync(0xffffffffu, byte, LANES) << 8;
+  four |= __shfl_down_sync(0xffffffffu, four, 2 * LANES) << 16;
+  if (lane % (4 * LANES) == 0 && listed && block / 4 < m.tiles) *reinterpret_cast<uint32_t*>(m.scales + scale_at(row, block, m.tiles)) = four;
+  if (!here || c0 >= m.cols) return;
+  uint8_t* const to = m.codes + (int64_t)row * m.ld + c0 / 2;
+  if (c0 + 8 <= m.cols) {
+    *reinterpret_cast<uint32_t*>(to) = word;
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+      if (2 * i < m.cols - c0) to[i] = (uint8_t)(word >> (8 * i));
+  }
+}
+
 }  // namespace
 }  // namespace mx
 }  // namespace pvt

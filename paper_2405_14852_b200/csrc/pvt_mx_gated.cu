@@ -1,0 +1,718 @@
+// Two products on 4-bit matrices with the activation between them, h = f(x wg^T) (x wu^T), and its gradients by both products,
+// dgate = dh b f'(a) and dup = dh f(a), from the 4-bit matrices again (a, b: the products; they are a ninth of a backward pass's
+// operations, where keeping them would take four bytes an element and two more passes over memory).
+//
+// Up to 16 tokens: the product's kernel for few tokens, by clusters whose even blocks multiply by 128 rows of wg and whose odd ones by
+// the same rows of wu, each pair its share of the steps.  The partial sums meet in shared memory across the cluster, always in the
+// order of ranks, and whoever adds up a token's sums finishes it.
+//
+// From 17 tokens on: the product's pairs of blocks, 256 rows of weights by 256 (or 128) of x to a tile; but the first block's 128 rows
+// are wg's and the second's the same ones of wu.  The main loop, its traffic (32 KB of codes a step and SM) and its rate are the product's.
+// What is needed together is then in two SMs: a thread reads its sums of N / 2 tokens out of tensor memory, which is free
+// for the next tile at once, keeps those of one half of them, and sends the others to the same thread of the other block, 32 tokens
+// at a time, through shared memory.  The exchange, activations and stores go on beside the next tile's products.
+//
+// 4-bit results: 32 outputs of a token are one warp's lanes.  They are turned in the shared memory that the exchange has left, to one
+// token to a lane, and quantised there.
+#include "pvt_mx_block.cuh"
+#include "pvt_mx_mma.cuh"
+#include "pvt_norm.cuh"
+
+namespace pvt {
+namespace {
+
+using namespace mx;
+using namespace mma;
+using norm::with_type;
+
+constexpr int kFewThreads = 192;  // four warps finish, one copies, one multiplies
+constexpr int kFewCopyWarp = 4, kFewMmaWarp = 5;
+
+// What becomes of a and b.  GRAD: dgate and dup, otherwise h, as floats, in 4 bits, or both.
+struct Finish {
+  int32_t activation, dtype;  // dtype: of h or dh
+  void* h;                    // or null
+  const void* dh;
+  __nv_bfloat16 *dgate, *dup;
+  int64_t ldh, ldd;
+  Held q;
+  const float* x_ts;
+  const float* gate_ts;
+  const float* up_ts;
+  uint32_t n, tokens;  // outputs, rows
+  uint32_t padded;     // rows that have scales
+};
+
+// f(a), and f'(a) if it is asked for
+template <bool SLOPE>
+__device__ __forceinline__ float activate(int32_t which, float a, float* slope) {
+  if (which == PVT_ACT_GELU) {  // f = a phi, phi the normal distribution's function
+    const float phi = 0.5f * erfcf(a * -0.70710678118654752f);
+    if (SLOPE) *slope = fmaf(a * 0.39894228040143268f, expf(-0.5f * a * a), phi);
+    return a * phi;
+  }
+  // f = a s(z), s the logistic function; z = a, or twice sqrt(2 / pi) (a + 0.044715 a^3): (1 + tanh(y)) / 2 = s(2 y)
+  float z = a, dz = 1.0f;
+  if (which == PVT_ACT_GELU_TANH) {
+    const float sq = a * a;
+    z = a * fmaf(sq, 0.07135481282942f, 1.59576912160573f);
+    if (SLOPE) dz = fmaf(sq, 0.21406443848826f, 1.59576912160573f);
+  }
+  const float s = __fdividef(1.0f, 1.0f + expf(-z));  // (0 where the exponential is beyond 2^126)
+  if (SLOPE) *slope = fmaf(a * dz, s * (1.0f - s), s);
+  return a * s;
+}
+
+// dgate and dup of one element, rounded
+__device__ __forceinline__ __nv_bfloat162 gradients(int32_t which, float a, float b, float dh) {
+  float slope;
+  const float f = activate<true>(which, a, &slope);
+  return __floats2bfloat162_rn(dh * b * slope, dh * f);
+}
+
+// A token of 128 outputs, lane, 32 + lane, ... of them to a lane; scratch: 128 floats of the warp's own.
+template <int FMT, bool GRAD>
+__device__ __forceinline__ void finish_token(const Finish& p, const TensorScale& t, uint32_t token, uint32_t col0, const float* a, const float* b,
+                                             float* scratch) {
+  const uint32_t lane = threadIdx.x & 31;
+  if (GRAD) {
+    with_type(p.dtype, [&](auto* type) {
+      using T = std::remove_pointer_t<decltype(type)>;
+      const T* const dh = static_cast<const T*>(p.dh) + (int64_t)token * p.ldh + col0 + lane;
+      const int64_t at = (int64_t)token * p.ldd + col0 + lane;
+      float v[4];
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) v[i] = col0 + i * 32 + lane < p.n ? widen<T>(dh[i * 32]) : 0.0f;
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (col0 + i * 32 + lane < p.n) {
+          const __nv_bfloat162 d = gradients(p.activation, a[i], b[i], v[i]);
+          p.dgate[at + i * 32] = d.x, p.dup[at + i * 32] = d.y;
+        }
+    });
+  } else {
+    float h[4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) h[i] = activate<false>(p.activation, a[i], nullptr) * b[i];
+    if (p.h)
+      with_type(p.dtype, [&](auto* type) {
+        using T = std::remove_pointer_t<decltype(type)>;
+        T* const to = static_cast<T*>(p.h) + (int64_t)token * p.ldh + col0 + lane;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+          if (col0 + i * 32 + lane < p.n) to[i * 32] = narrow<T>(h[i]);
+      });
+    if (p.q.codes) {
+      __syncwarp();
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) scratch[i * 32 + lane] = h[i];
+      __syncwarp();
+      float v[8];
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) v[i] = lane < 16 ? scratch[8 * lane + i] : 0.0f;
+      // (the upper lanes: the next 128 columns, where there are no outputs but scales)
+      const bool none = lane >= 16 && col0 + 128 < p.n;
+      put_eight<FMT>(p.q, token, none ? 0x40000000u : col0 + 8 * lane, true, !none, t, v);
+    }
+  }
+}
+// scales of rows that do not exist, of the 128 outputs from col0 on and of what is behind the last output; thread `i` of `count`
+template <int FMT>
+__device__ __forceinline__ void clear_scales(const Finish& p, uint32_t from, uint32_t to, uint32_t col0, uint32_t i, uint32_t count) {
+  constexpr uint32_t BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16, WORDS = 128 / (4 * BLOCK);
+  const uint32_t words = col0 + 128 < p.n ? WORDS : 2 * WORDS;
+  for (uint32_t at = from * words + i; at < to * words; at += count) {
+    const uint32_t block = col0 / BLOCK + at % words * 4;
+    if (block / 4 < p.q.tiles) *reinterpret_cast<uint32_t*>(p.q.scales + scale_at(at / words, block, p.q.tiles)) = 0;
+  }
+}
+
+// ---- few tokens ------------------------------------------------------------------------------------------------
+struct FewParams {
+  const uint8_t *gate_codes, *up_codes, *gate_scales, *up_scales, *x_scales;
+  int64_t gate_ld, up_ld;
+  Finish f;
+  uint32_t* status;
+  uint32_t row_bytes;    // of weights, to the last 16 that hold codes
+  uint32_t strip_bytes;  // scales of a strip of 128 rows
+  uint32_t steps;        // of 256 columns
+  uint32_t split;        // pairs per tile
+  uint32_t max_spins, withhold;
+};
+
+struct FewShared {
+  alignas(8) uint64_t full[8];
+  uint64_t empty[8];
+  uint64_t done, spare;
+  uint32_t tmem, abandoned;
+};
+
+template <int FMT, bool GRAD>
+__global__ void __launch_bounds__(kFewThreads)
+    mx_gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map,
+                        const __grid_constant__ CUtensorMap x_map, const __grid_constant__ FewParams p) {
+  using S = FewSizes<FMT>;
+  constexpr uint32_t KT = S::KT, STAGES = S::kStages;
+  extern __shared__ __align__(1024) unsigned char raw[];
+  __shared__ FewShared sm;
+  __shared__ float scratch[4][128];
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  volatile uint32_t* abandoned = &sm.abandoned;
+  const uint32_t blocks = 2 * p.split, rank = blockIdx.x % blocks, w0 = blockIdx.x / blocks * kTileW;
+  const bool of_up = rank & 1;
+  const uint32_t first = p.steps * (rank / 2) / p.split, last = p.steps * (rank / 2 + 1) / p.split;  // (steps < 2^20, split <= 4)
+  const uint8_t* const w_scales = (of_up ? p.up_scales : p.gate_scales) + (size_t)(w0 / kStrip) * p.strip_bytes;
+  // all of the block's weights at once, while it sets itself up and the kernel ahead ends
+  const uint32_t from_byte = first * kRowBytes, to_byte = min(last * kRowBytes, p.row_bytes);
+  if (tid < (uint32_t)kTileW && w0 + tid < p.f.n)
+    prefetch_l2((of_up ? p.up_codes : p.gate_codes) + (int64_t)(w0 + tid) * (of_up ? p.up_ld : p.gate_ld) + from_byte, to_byte - from_byte);
+  if (tid == (uint32_t)kTileW) prefetch_l2(w_scales + (size_t)first * (KT * kTileBytes), (last - first) * (KT * kTileBytes));
+  if (tid == 0) {
+    sm.abandoned = 0;
+    for (uint32_t s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&sm.full[s]), 1);
+      mbar_init(smem_u32(&sm.empty[s]), 1);
+    }
+    mbar_init(smem_u32(&sm.done), 1);
+    mbar_init(smem_u32(&sm.spare), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kFewMmaWarp) {
+    tmem_alloc(smem_u32(&sm.tmem), S::kTmem);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_trigger();  // not before this block has its tensor memory: the next kernel's blocks hold theirs while they wait for this one
+  pdl_wait();
+
+  const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
+  const Finish& f = p.f;
+
+  if (warp == kFewCopyWarp) {
+    const CUtensorMap* const w_map = of_up ? &up_map : &gate_map;
+    uint32_t i = 0;
+    for (uint32_t step = first; step < last; ++step, ++i) {
+      const uint32_t s = i % STAGES, bar = smem_u32(&sm.full[s]), to = base + s * S::kStageAligned;
+      if (i >= STAGES && !wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins)) break;
+      if (i == p.withhold) continue;  // test hook: never issued
+      expect_bytes(bar, S::kStage);
+      tma_load(to, w_map, (int)(step * kRowBytes), (int)w0, bar);
+      tma_load(to + S::kX, &x_map, (int)(step * kRowBytes), 0, bar);
+      bulk_load(to + S::kWs, w_scales + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
+      bulk_load(to + S::kXs, p.x_scales + (size_t)step * (KT * kTileBytes), KT * kTileBytes, bar);
+    }
+    if (*abandoned)  // what was issued lands before the block's memory is another's
+      for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+        if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
+  } else if (warp == kFewMmaWarp) {
+    // e2m1 both, N = 16, M = 128, type of the scales
+    constexpr uint32_t idesc =
+        1u << 7 | 1u << 10 | (kFewTokens >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | 1u << 27;
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint32_t step = first; step < last; ++step, ++i) {
+      const uint32_t s = i % STAGES, from = base + s * S::kStageAligned;
+      ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t sfa = tmem + 32 + s * S::kScaleCols, sfb = sfa + KT * 4;
+      // a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart
+#pragma unroll
+      for (uint32_t t = 0; t < KT; ++t) {
+        scales_to_tmem(sfa + t * 4, operand(from + S::kWs + t * kTileBytes, 0, 128, false));
+        scales_to_tmem(sfb + t * 4, operand(from + S::kXs + t * kTileBytes, 0, 128, false));
+      }
+      const uint64_t a = operand(from, 16, 1024, true), b = operand(from + S::kX, 16, 1024, true);
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {  // 64 columns, 32 bytes
+        const uint32_t t = FMT == PVT_MX_E8M0_32 ? j / 2 : j, id = FMT == PVT_MX_E8M0_32 ? (j & 1) * 2 : 0;
+        multiply<FMT>(tmem, a + 2 * j, b + 2 * j, idesc | id << 4 | id << 29, sfa + t * 4, sfb + t * 4, (uint32_t)(i > 0 || j > 0));
+      }
+      commit(smem_u32(&sm.empty[s]));
+    }
+    if (ok) {
+      commit(smem_u32(&sm.done));
+    } else if (i > 0) {
+      commit(smem_u32(&sm.spare));
+      drain(smem_u32(&sm.spare), 0);
+    }
+  } else {
+    float* const part = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
+    if (wait(smem_u32(&sm.done), 0, abandoned, p.status, p.max_spins)) {
+      tc_fence_after();
+      uint32_t v[kFewTokens];
+      tmem_ld16(tmem + (warp << 21), v);
+      tmem_ld_wait<kFewTokens>(v);
+#pragma unroll
+      for (uint32_t j = 0; j < kFewTokens; ++j) part[j * kTileW + tid] = __uint_as_float(v[j]);
+      tc_fence_before();
+    }
+    if (!GRAD && f.q.codes && rank == 0) clear_scales<FMT>(f, f.tokens, f.padded, w0, tid, 128);
+  }
+  cluster_sync();
+  // every block adds up and finishes the tokens that are its share, one to a warp
+  if (warp < 4 && !*abandoned) {
+    const Factors gate(f.gate_ts ? *f.gate_ts : 1.0f, f.x_ts ? *f.x_ts : 1.0f), up(f.up_ts ? *f.up_ts : 1.0f, f.x_ts ? *f.x_ts : 1.0f);
+    const TensorScale t(f.q.tensor_scale);
+    for (uint32_t j = rank + warp * blocks; j < f.tokens; j += 4 * blocks) {
+      float a[4], b[4], v[2][4][4];
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+          const uint32_t at = base + (j * kTileW + i * 32 + lane) * 4;
+          v[0][i][q] = q < p.split ? cluster_load(at, 2 * q) : 0.0f;
+          v[1][i][q] = q < p.split ? cluster_load(at, 2 * q + 1) : 0.0f;
+        }
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) {
+        a[i] = gate(v[0][i][0] + v[0][i][1] + v[0][i][2] + v[0][i][3]);
+        b[i] = up(v[1][i][0] + v[1][i][1] + v[1][i][2] + v[1][i][3]);
+      }
+      finish_token<FMT, GRAD>(f, t, j, w0, a, b, scratch[warp]);
+    }
+  }
+  cluster_sync();  // no block leaves while another reads its partial sums
+  __syncthreads();
+  if (warp == kFewMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, S::kTmem);
+  }
+}
+
+// ---- pairs of blocks -------------------------------------------------------------------------------------------
+constexpr uint32_t kRound = 32;  // tokens of a warp's exchange at a time
+constexpr uint32_t kExchange = kRound * 32 * 4;  // bytes of it
+
+struct PairShared {
+  alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
+  uint64_t empty[kPairStages];            // of each
+  uint64_t sums_full;                     // of each
+  uint64_t sums_empty;                    // of the first: an arrival per reading warp of both
+  uint64_t got[kPairReaders];             // of each: the other block's warp has written its sums, an arrival per lane
+  uint64_t room[kPairReaders];            // of each: the other block's warp has read them
+  uint64_t spare;
+  uint32_t tmem, abandoned;
+};
+
+struct PairParams {
+  Finish f;
+  uint32_t* status;
+  uint32_t strip_rows;  // rows of 128 bytes that a strip's scales are
+  uint32_t steps;       // of 256 columns
+  uint32_t x_tiles, tiles;
+  uint32_t split;       // pairs per tile
+  uint32_t max_spins, withhold;
+};
+
+template <int FMT, uint32_t N>
+struct GatedSizes : PairSizes<FMT, N> {
+  using P = PairSizes<FMT, N>;
+  static constexpr uint32_t kRoom = (225 * 1024 - kPairReaders * kExchange) / P::kStageAligned;
+  static constexpr uint32_t kStages = kRoom < P::kStages ? kRoom : P::kStages;
+  static constexpr uint32_t kExchangeAt = kStages * P::kStageAligned;
+  static constexpr size_t kBytes = kExchangeAt + kPairReaders * kExchange + 1024;
+  static_assert(kBytes + 1024 <= 227 * 1024, "a block's shared memory");
+  static_assert(N * kTileW * 4 <= kExchangeAt, "the partial sums fit the stages");
+};
+
+// what a warp's 32 lanes (outputs) have of 32 tokens, into 4 bits: v[j] of token j; buffer: the warp's exchange
+template <int FMT>
+__device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t, uint32_t token0, uint32_t col0, const uint32_t* v, float* buffer) {
+  constexpr int BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16, N = 32 / BLOCK;
+  const uint32_t lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (uint32_t j = 0; j < 32; ++j) buffer[j * 32 + (lane ^ j)] = col0 + lane < p.n ? __uint_as_float(v[j]) : 0.0f;
+  __syncwarp();
+  const uint32_t token = token0 + lane;
+  float e[32];
+#pragma unroll
+  for (uint32_t i = 0; i < 32; ++i) e[i] = buffer[lane * 32 + (i ^ lane)];
+  uint32_t word[4], bytes = 0;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < BLOCK; ++i) top = max(top, __float_as_uint(e[n * BLOCK + i]) & 0x7fffffffu);
+    const uint32_t byte = quantize_block<FMT, BLOCK>(e + n * BLOCK, top, t, word + n * (BLOCK / 8));
+    if (token < p.tokens && col0 + n * BLOCK < p.n) bytes |= byte << (8 * n);
+  }
+  if (token >= p.padded) return;
+  auto put_scales = [&](uint32_t col, uint32_t value) {
+    if (col / BLOCK / 4 >= p.q.tiles) return;
+    uint8_t* const to = p.q.scales + scale_at(token, col / BLOCK, p.q.tiles);
+    if (N == 1)
+      *to = (uint8_t)value;
+    else
+      *reinterpret_cast<uint16_t*>(to) = (uint16_t)value;
+  };
+  put_scales(col0, bytes);
+  if (col0 / 128 == (p.n - 1) / 128) put_scales(col0 + 128, 0);  // (blocks of no outputs at all)
+  if (token >= p.tokens || col0 >= p.n) return;
+  uint8_t* const to = p.q.codes + (int64_t)token * p.q.ld + col0 / 2;
+  if (col0 + 32 <= p.n) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(word[0], word[1], word[2], word[3]);
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i)
+      if (2 * i < p.n - col0) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+template <int FMT, uint32_t N, bool GRAD>
+__global__ void __launch_bounds__(kPairThreads, 1)
+    mx_gated_pair_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map,
+                         const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap gate_s_map,
+                         const __grid_constant__ CUtensorMap up_s_map, const __grid_constant__ CUtensorMap x_s_map,
+                         const __grid_constant__ PairParams p) {
+  using S = GatedSizes<FMT, N>;
+  constexpr uint32_t KT = S::KT, STAGES = S::kStages, HALF = N / 2, MINE = N / 4;
+  extern __shared__ __align__(1024) unsigned char raw[];
+  __shared__ PairShared sm;
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  volatile uint32_t* abandoned = &sm.abandoned;
+  if (tid == 0) {
+    sm.abandoned = 0;
+    for (uint32_t s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&sm.full[s]), 1);
+      mbar_init(smem_u32(&sm.empty[s]), 1);
+    }
+    mbar_init(smem_u32(&sm.sums_full), 1);
+    mbar_init(smem_u32(&sm.sums_empty), 2 * kPairReaders);
+    for (uint32_t s = 0; s < kPairReaders; ++s) {
+      mbar_init(smem_u32(&sm.got[s]), 32);
+      mbar_init(smem_u32(&sm.room[s]), 1);
+    }
+    mbar_init(smem_u32(&sm.spare), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kPairMmaWarp) {
+    tmem_alloc<2>(smem_u32(&sm.tmem), 512);
+    tmem_relinquish<2>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_trigger();  // not before this block has its tensor memory: the next kernel's blocks hold theirs while they wait for this one
+  pdl_wait();
+  cluster_sync();  // the barriers of both blocks are set up
+
+  const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+  unsigned char* const mem = raw + (base - smem_u32(raw));
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
+  // Pairs by themselves take tile after tile; those of a cluster share one tile's steps.
+  const uint32_t in_cluster = cluster_rank(), rank = in_cluster & 1, lead = in_cluster & ~1u, share = in_cluster / 2;
+  const uint32_t tile0 = blockIdx.x / 2 / p.split, stride = p.split > 1 ? p.tiles : gridDim.x / 2;
+  const uint32_t first = p.steps * share / p.split, steps = p.steps * (share + 1) / p.split - first;  // (steps < 2^24, share < 4)
+  const Finish& f = p.f;
+
+  if (warp >= kPairCopyWarp && warp < kPairMmaWarp) {
+    const bool of_w = warp == kPairCopyWarp;  // one warp for the weights' codes and scales, one for x's
+    const CUtensorMap* const w_map = rank ? &up_map : &gate_map;
+    const CUtensorMap* const w_s_map = rank ? &up_s_map : &gate_s_map;
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride) {
+      const uint32_t row0 = of_w ? tile / p.x_tiles * kTileW : tile % p.x_tiles * N;
+      const int row = (int)(row0 + (of_w ? 0 : rank * (N / 2)));
+      const int strip = (int)(row0 / kStrip * p.strip_rows);
+      for (uint32_t step = first; step < first + steps; ++step, ++i) {
+        const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
+        if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
+        if (i == p.withhold) continue;  // test hook: never issued
+        const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), lead);
+        const int col = (int)(step * kRowBytes), scales = strip + (int)(step * (KT * 4));
+        if (of_w) {
+          if (rank == 0) expect_bytes(smem_u32(&sm.full[s]), 2 * S::kStage);
+          tma_load_pair(to, w_map, col, row, bar);
+          tma_load_pair(to + S::kWs, w_s_map, 0, scales, bar);
+        } else {  // both blocks multiply by all of the tile's rows of x
+          tma_load_pair(to + S::kX, &x_map, col, row, bar);
+          tma_load_pair(to + S::kXs, &x_s_map, 0, scales, bar);
+          if (S::kStrips == 2) tma_load_pair(to + S::kXs + KT * kTileBytes, &x_s_map, 0, scales + (int)p.strip_rows, bar);
+        }
+      }
+    }
+    if (*abandoned && rank == 0)  // what was issued lands before the blocks' memory is another's
+      for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+        if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
+  } else if (warp == kPairMmaWarp) {
+    if (rank == 0) {
+      // e2m1 both, N, M = 256, type of the scales
+      constexpr uint32_t idesc =
+          1u << 7 | 1u << 10 | (N >> 3) << 17 | (FMT == PVT_MX_E8M0_32 ? 1u << 23 : 0u) | (kPairRows >> 7) << 27;
+      const uint16_t both = (uint16_t)(3u << lead);
+      uint32_t i = 0, n = 0;
+      bool ok = true;
+      for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride, ++n) {
+        if (n > 0) ok = wait<true>(smem_u32(&sm.sums_empty), (n - 1) & 1, abandoned, p.status, p.max_spins);
+        tc_fence_after();
+        for (uint32_t step = 0; step < steps && ok; ++step) {
+          const uint32_t s = i % STAGES, from = base + s * S::kStageAligned;
+          ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t sfa = tmem + N + s * S::kScaleCols, sfb = sfa + KT * 4;
+          // (a scale tile: 32 rows of 16 bytes, groups of eight rows 128 bytes apart)
+          multiply_step<FMT, S::kStrips>(tmem, operand(from, 16, 1024, true), operand(from + S::kX, 16, 1024, true), idesc, sfa, sfb,
+                                         operand(from + S::kWs, 0, 128, false), operand(from + S::kXs, 0, 128, false), (uint32_t)(step > 0));
+          commit_pair(smem_u32(&sm.empty[s]), both);
+          ++i;
+        }
+        if (ok) commit_pair(smem_u32(&sm.sums_full), both);
+      }
+      if (!ok && i > 0) {
+        commit_pair(smem_u32(&sm.spare), both);
+        drain(smem_u32(&sm.spare), 0);
+      }
+    }
+  } else {
+    const float x_ts = f.x_ts ? *f.x_ts : 1.0f;
+    const Factors gate(f.gate_ts ? *f.gate_ts : 1.0f, x_ts), up(f.up_ts ? *f.up_ts : 1.0f, x_ts);
+    const TensorScale t(f.q.tensor_scale);
+    const uint32_t quarter = warp % 4, half = warp / 4;
+    const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), lead);
+    // of the other block: where this warp's sums go, and the barriers of the same warp
+    const uint32_t exchange = base + S::kExchangeAt + warp * kExchange, other = cluster_address(exchange, in_cluster ^ 1);
+    const uint32_t other_got = cluster_address(smem_u32(&sm.got[warp]), in_cluster ^ 1);
+    const uint32_t other_room = cluster_address(smem_u32(&sm.room[warp]), in_cluster ^ 1);
+    float* const buffer = reinterpret_cast<float*>(mem + S::kExchangeAt + warp * kExchange);
+    uint32_t n = 0, turn = 0;  // tiles, exchanges
+    bool ok = true;
+    for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride, ++n) {
+      ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
+      if (!ok) break;
+      tc_fence_after();
+      // the tokens that this block finishes, then those that the other one does
+      uint32_t v[HALF];
+#pragma unroll
+      for (uint32_t j = 0; j < HALF; j += 32)
+        tmem_ld32(tmem + (quarter << 21) + half * HALF + ((j < MINE) == (rank == 0) ? 0 : MINE) + j % MINE, v + j);
+      tmem_ld_wait<(int)HALF>(v);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) cluster_arrive(sums_empty);
+      __syncwarp();
+      if (p.split > 1) {  // the products are done: the stages hold the partial sums
+#pragma unroll
+        for (uint32_t j = 0; j < HALF; ++j) {
+          const uint32_t token = half * HALF + ((j < MINE) == (rank == 0) ? 0 : MINE) + j % MINE;
+          reinterpret_cast<float*>(mem)[token * kTileW + quarter * 32 + lane] = __uint_as_float(v[j]);
+        }
+        break;
+      }
+      const uint32_t col0 = tile / p.x_tiles * kTileW + quarter * 32, col = col0 + lane;
+      const uint32_t row = tile % p.x_tiles * N + half * HALF + rank * MINE;
+      const bool has_col = col < f.n;
+#pragma unroll
+      for (uint32_t r = 0; r < MINE; r += kRound, ++turn) {
+        if (turn > 0) ok = wait<true>(smem_u32(&sm.room[warp]), (turn - 1) & 1, abandoned, p.status, p.max_spins);
+        if (!ok) break;
+#pragma unroll
+        for (uint32_t j = 0; j < kRound; j += 4)
+          asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(other + (j / 4 * 32 + lane) * 16), "r"(v[MINE + r + j]),
+                       "r"(v[MINE + r + j + 1]), "r"(v[MINE + r + j + 2]), "r"(v[MINE + r + j + 3])
+                       : "memory");
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(other_got) : "memory");
+        float dh[kRound];
+        if (GRAD)
+          with_type(f.dtype, [&](auto* type) {
+            using T = std::remove_pointer_t<decltype(type)>;
+            const T* from = static_cast<const T*>(f.dh) + (int64_t)(row + r) * f.ldh + col;
+#pragma unroll
+            for (uint32_t j = 0; j < kRound; ++j) {
+              dh[j] = has_col && row + r + j < f.tokens ? widen<T>(*from) : 0.0f;
+              from += f.ldh;
+            }
+          });
+        ok = wait<true>(smem_u32(&sm.got[warp]), turn & 1, abandoned, p.status, p.max_spins);
+        if (!ok) break;
+#pragma unroll
+        for (uint32_t j = 0; j < kRound; j += 4) {
+          const float4 theirs = *reinterpret_cast<const float4*>(buffer + (j / 4 * 32 + lane) * 4);
+          const float o[4] = {theirs.x, theirs.y, theirs.z, theirs.w};
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) {
+            const float own = __uint_as_float(v[r + j + i]);
+            const float a = gate(rank ? o[i] : own), b = up(rank ? own : o[i]);
+            if (GRAD) {
+              const __nv_bfloat162 d = gradients(f.activation, a, b, dh[j + i]);
+              v[r + j + i] = *reinterpret_cast<const uint32_t*>(&d);
+            } else {
+              v[r + j + i] = __float_as_uint(activate<false>(f.activation, a, nullptr) * b);
+            }
+          }
+        }
+        __syncwarp();
+        // (the last exchange's shared memory is still wanted for 4-bit results)
+        if (lane == 0 && r + kRound < MINE) cluster_arrive(other_room);
+        __syncwarp();
+      }
+      if (!ok) break;
+      if (!GRAD && f.q.codes) {
+#pragma unroll
+        for (uint32_t r = 0; r < MINE; r += 32) put_tokens<FMT>(f, t, row + r, col0, v + r, buffer);
+      }
+      __syncwarp();
+      if (lane == 0) cluster_arrive(other_room);
+      __syncwarp();
+      if (has_col && row < f.tokens) {
+        const uint32_t rows = f.tokens - row;
+        if (GRAD) {
+          __nv_bfloat16 *to_gate = f.dgate + (int64_t)row * f.ldd + col, *to_up = f.dup + (int64_t)row * f.ldd + col;
+#pragma unroll
+          for (uint32_t j = 0; j < MINE; ++j) {
+            if (j < rows) {
+              const __nv_bfloat162 d = *reinterpret_cast<const __nv_bfloat162*>(&v[j]);
+              *to_gate = d.x, *to_up = d.y;
+            }
+            to_gate += f.ldd, to_up += f.ldd;
+          }
+        } else if (f.h) {
+          with_type(f.dtype, [&](auto* type) {
+            using T = std::remove_pointer_t<decltype(type)>;
+            T* to = static_cast<T*>(f.h) + (int64_t)row * f.ldh + col;
+#pragma unroll
+            for (uint32_t j = 0; j < MINE; ++j) {
+              if (j < rows) *to = narrow<T>(__uint_as_float(v[j]));
+              to += f.ldh;
+            }
+          });
+        }
+      }
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+  cluster_sync();  // neither block leaves while the other's copies, products or sums reach it
+  if (p.split > 1) {
+    // every block adds up and finishes the tokens that are its share, one to a warp, always in the order of pairs
+    const uint32_t col0 = tile0 / p.x_tiles * kTileW, row0 = tile0 % p.x_tiles * N, blocks = 2 * p.split;
+    if (!*abandoned) {
+      const float x_ts = f.x_ts ? *f.x_ts : 1.0f;
+      const Factors gate(f.gate_ts ? *f.gate_ts : 1.0f, x_ts), up(f.up_ts ? *f.up_ts : 1.0f, x_ts);
+      const TensorScale t(f.q.tensor_scale);
+      float* const scratch = reinterpret_cast<float*>(mem + S::kExchangeAt) + warp * 128;
+      const uint32_t tokens = min(N, f.tokens - row0);
+      for (uint32_t j = in_cluster + warp * blocks; j < tokens; j += kPairThreads / 32 * blocks) {
+        float v[2][4][4], a[4], b[4];  // (all under way at once: a load from another block takes a thousand cycles)
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t q = 0; q < 4; ++q) {
+            const uint32_t at = base + (j * kTileW + i * 32 + lane) * 4;
+            v[0][i][q] = q < p.split ? cluster_load(at, 2 * q) : 0.0f;
+            v[1][i][q] = q < p.split ? cluster_load(at, 2 * q + 1) : 0.0f;
+          }
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+          a[i] = gate(v[0][i][0] + v[0][i][1] + v[0][i][2] + v[0][i][3]);
+          b[i] = up(v[1][i][0] + v[1][i][1] + v[1][i][2] + v[1][i][3]);
+        }
+        finish_token<FMT, GRAD>(f, t, row0 + j, col0, a, b, scratch);
+      }
+      if (!GRAD && f.q.codes && in_cluster == 0)
+        clear_scales<FMT>(f, max(row0, f.tokens), min(row0 + N, f.padded), col0, tid, kPairThreads);
+    }
+    cluster_sync();  // nor while another reads its partial sums
+  }
+  if (warp == kPairMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc<2>(tmem, 512);
+  }
+}
+
+template <int FMT, uint32_t N, bool GRAD>
+cudaError_t gated_pairs(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, const Finish& f, uint32_t* status, int sm_count,
+                        cudaStream_t stream) {
+  using S = GatedSizes<FMT, N>;
+  PairParams p = {};
+  p.f = f, p.status = status;
+  p.strip_rows = strip_tiles(x.cols, block_of(FMT)) * (kTileBytes / 128);
+  p.steps = ((uint32_t)x.cols + kSpan - 1) / kSpan;
+  p.x_tiles = (f.tokens + N - 1) / N;
+  p.tiles = (f.n + kTileW - 1) / kTileW * p.x_tiles;
+  const m1::WaitTestHook hook = m1::wait_test_hook();
+  p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
+  CUtensorMap maps[6];
+  const pvt_mx* const of[3] = {&wg, &wu, &x};
+  for (int i = 0; i < 3; ++i) {
+    cudaError_t e = make_map(&maps[i], of[i]->codes, 1, (uint64_t)of[i]->rows, ((uint64_t)of[i]->cols + 1) / 2, (uint64_t)of[i]->ld,
+                             i < 2 ? kTileW : N / 2);
+    if (e == cudaSuccess)
+      e = make_map(&maps[3 + i], of[i]->scales, 1, scale_bytes(of[i]->rows, of[i]->cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
+    if (e != cudaSuccess) return e;
+  }
+  const cudaError_t e = allow_smem<mx_gated_pair_kernel<FMT, N, GRAD>>();
+  if (e != cudaSuccess) return e;
+  p.split = pairs_per_tile(p.tiles, p.steps, sm_count);
+  const uint32_t pairs = p.split > 1 ? p.tiles * p.split : p.tiles < (uint32_t)sm_count / 2 ? p.tiles : (uint32_t)sm_count / 2;
+  return launch_clusters(mx_gated_pair_kernel<FMT, N, GRAD>, 2 * pairs, 2 * p.split, kPairThreads, S::kBytes, stream, maps[0], maps[1],
+                         maps[2], maps[3], maps[4], maps[5], p);
+}
+
+template <int FMT, bool GRAD>
+cudaError_t gated(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, const Finish& f, uint32_t* status, int sm_count, cudaStream_t stream) {
+  using S = FewSizes<FMT>;
+  const uint64_t tiles = ((uint64_t)f.n + kTileW - 1) / kTileW;
+  if (f.tokens > kFewTokens)
+    return narrow_tiles((int32_t)f.tokens, tiles, sm_count) ? gated_pairs<FMT, 128, GRAD>(x, wg, wu, f, status, sm_count, stream)
+                                                            : gated_pairs<FMT, 256, GRAD>(x, wg, wu, f, status, sm_count, stream);
+  FewParams p = {};
+  p.gate_codes = wg.codes, p.gate_scales = wg.scales, p.gate_ld = wg.ld, p.up_codes = wu.codes, p.up_scales = wu.scales, p.up_ld = wu.ld;
+  p.x_scales = x.scales, p.f = f, p.status = status;
+  p.row_bytes = ((uint32_t)x.cols + 31) / 32 * 16;
+  p.strip_bytes = strip_tiles(x.cols, block_of(FMT)) * kTileBytes;
+  p.steps = ((uint32_t)x.cols + kSpan - 1) / kSpan;
+  p.split = 1;
+  while (p.split < 4 && tiles * p.split * 4 <= (uint64_t)sm_count * 2 && p.split * 2 <= p.steps) p.split *= 2;
+  const m1::WaitTestHook hook = m1::wait_test_hook();
+  p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
+  CUtensorMap maps[3];
+  const pvt_mx* const of[3] = {&wg, &wu, &x};
+  for (int i = 0; i < 3; ++i) {
+    const cudaError_t e = make_map(&maps[i], of[i]->codes, 1, (uint64_t)of[i]->rows, ((uint64_t)of[i]->cols + 1) / 2, (uint64_t)of[i]->ld,
+                                   i < 2 ? kTileW : kFewTokens);
+    if (e != cudaSuccess) return e;
+  }
+  const cudaError_t e = allow_smem<mx_gated_few_kernel<FMT, GRAD>>();
+  if (e != cudaSuccess) return e;
+  return launch_clusters(mx_gated_few_kernel<FMT, GRAD>, (unsigned)(tiles * p.split * 2), 2 * p.split, kFewThreads, S::kBytes, stream, maps[0],
+                         maps[1], maps[2], p);
+}
+
+template <bool GRAD>
+cudaError_t gated(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, Finish f, uint32_t* status, int sm_count, cudaStream_t stream) {
+  f.x_ts = x.tensor_scale, f.gate_ts = wg.tensor_scale, f.up_ts = wu.tensor_scale;
+  f.n = (uint32_t)wg.rows, f.tokens = (uint32_t)x.rows, f.padded = (f.tokens + kStrip - 1) / kStrip * kStrip;
+  timing_begin(kKernMx, stream);
+  const cudaError_t e = x.format == PVT_MX_E8M0_32 ? gated<PVT_MX_E8M0_32, GRAD>(x, wg, wu, f, status, sm_count, stream)
+                                                   : gated<PVT_MX_E4M3_16, GRAD>(x, wg, wu, f, status, sm_count, stream);
+  timing_end(kKernMx, stream);
+  count_launches(1);
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_mx_gated(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, int32_t activation, void* h, int32_t dtype, int64_t ldh,
+                            const pvt_mx* hq, uint32_t* status, int sm_count, cudaStream_t stream) {
+  Finish f = {};
+  f.activation = activation, f.h = h, f.dtype = dtype, f.ldh = ldh;
+  if (hq) f.q = held(*hq);
+  return gated<false>(x, wg, wu, f, status, sm_count, stream);
+}
+
+cudaError_t launch_mx_gated_grad(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, int32_t activation, const void* dh, int32_t dtype,
+                                 int64_t lddh, void* dgate, void* dup, int64_t ldd, uint32_t* status, int sm_count, cudaStream_t stream) {
+  Finish f = {};
+  f.activation = activation, f.dh = dh, f.dtype = dtype, f.ldh = lddh;
+  f.dgate = static_cast<__nv_bfloat16*>(dgate), f.dup = static_cast<__nv_bfloat16*>(dup), f.ldd = ldd;
+  return gated<true>(x, wg, wu, f, status, sm_count, stream);
+}
+
+}  // namespace pvt

@@ -134,13 +134,14 @@ struct GradShared {
 
 struct GradParams {
   const uint8_t* scales;
+  const uint8_t* scales2;         // of the second pair of operands, which has the steps from `half` on
   const float* ts;
   void* out;
   int64_t ldo;
   uint32_t* status;
   uint32_t a_rows, cols;
   uint32_t strip_bytes;
-  uint32_t steps, a_tiles, tiles;
+  uint32_t steps, half, a_tiles, tiles;
   uint32_t split;                 // blocks per tile, where they multiply by themselves
   uint32_t accumulate;
   uint32_t max_spins, withhold;
@@ -250,9 +251,12 @@ __device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b
         : "memory");
 }
 
-template <typename T, int FMT, bool TRANS, int MT, int CTAS>
+// TWO: the sum goes on over the rows of a second pair of operands, D += A2(p, r) Q2[r, c]: its maps and scales take the place of the
+// first one's from step `half` on, and nothing else changes.
+template <typename T, int FMT, bool TRANS, int MT, int CTAS, bool TWO>
 __global__ void __launch_bounds__(kThreads, 1)
-    mx_grad_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap q_map, const GradParams p) {
+    mx_grad_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap q_map,
+                   const __grid_constant__ CUtensorMap a2_map, const __grid_constant__ CUtensorMap q2_map, const GradParams p) {
   using S = GradSizes<FMT, MT, CTAS>;
   constexpr uint32_t STAGES = kStages, kHeld = S::kHeld, TURN = S::kTurn;
   extern __shared__ __align__(1024) unsigned char raw[];
@@ -302,14 +306,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride) {
       const uint32_t c0 = tile / p.a_tiles * S::kCols + rank * S::kHalf;
-      const uint8_t* const scales = p.scales + (size_t)(c0 / S::kScaleCols) * kTileBytes;
+      const size_t scales_at = (size_t)(c0 / S::kScaleCols) * kTileBytes;
       for (uint32_t step = 0; step < steps; ++step, ++i) {
         const uint32_t s = i % kHeld, to = base + S::kHeldAt + s * S::kHeldBytes, bar = smem_u32(&sm.held[s]);
         if (i >= kHeld && !(ok = wait(smem_u32(&sm.held_empty[s]), (i / kHeld - 1) & 1, abandoned, p.status, p.max_spins))) break;
         if (i == p.withhold) continue;  // test hook: never issued
+        const bool second = TWO && first + step >= p.half;
+        const uint32_t r0 = (first + step - (second ? p.half : 0)) * kStepR;
         expect_bytes(bar, S::kHeldBytes);
-        tma_load(to, &q_map, (int)(c0 / 2), (int)((first + step) * kStepR), bar);
-        bulk_load(to + S::kCodeBytes, scales + (size_t)((first + step) * kStepR / kStrip) * p.strip_bytes, S::kScaleBytes, bar);
+        tma_load(to, second ? &q2_map : &q_map, (int)(c0 / 2), (int)r0, bar);
+        bulk_load(to + S::kCodeBytes, (second ? p.scales2 : p.scales) + scales_at + (size_t)(r0 / kStrip) * p.strip_bytes, S::kScaleBytes, bar);
       }
     }
     if (*abandoned)  // what was issued lands before the block's memory is another's
@@ -328,12 +334,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
           if (rank == 0 && m == 0) expect_bytes(smem_u32(&sm.full_a[s]), CTAS * MT * kABytes);
           const uint32_t bar = CTAS == 2 ? cluster_address(smem_u32(&sm.full_a[s]), 0) : smem_u32(&sm.full_a[s]);
-          const int r0 = (int)((first + step) * kStepR);
+          const bool second = TWO && first + step >= p.half;
+          const int r0 = (int)((first + step - (second ? p.half : 0)) * kStepR);
           if (TRANS) {
             load_a<CTAS>(to, &a_map, a0, r0, bar);
             load_a<CTAS>(to + kABytes / 2, &a_map, a0 + 64, r0, bar);
           } else {
-            load_a<CTAS>(to, &a_map, r0, a0, bar);
+            load_a<CTAS>(to, second ? &a2_map : &a_map, r0, a0, bar);
           }
         }
       }
@@ -389,7 +396,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (uint32_t it = 0; it < kItems; ++it) {
         codes[it] = *reinterpret_cast<const uint4*>(held + (row * kChunks + chunk + it * (kGroupWarps * 32)) * 16);
-        const uint32_t r = ((first + step) * kStepR + row + it * 32) % kStrip, at = S::kCodeBytes + r % 32 * 16 + r / 32 * 4;
+        const uint32_t of_q = first + step - (TWO && first + step >= p.half ? p.half : 0);
+        const uint32_t r = (of_q * kStepR + row + it * 32) % kStrip, at = S::kCodeBytes + r % 32 * 16 + r / 32 * 4;
         // (of 64 columns every other block has the upper half of a tile of four e8m0 scales)
         if (FMT == PVT_MX_E8M0_32)
           scales[it] = held[at + (MT == 2 ? rank * 2 : 0) + chunk];
@@ -518,13 +526,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-template <typename T, int FMT, bool TRANS, int MT, int CTAS>
-cudaError_t start(const CUtensorMap& a_map, GradParams p, const pvt_mx& q, int sm_count, cudaStream_t stream) {
+template <typename T, int FMT, bool TRANS, int MT, int CTAS, bool TWO>
+cudaError_t start(const CUtensorMap& a_map, const CUtensorMap& a2_map, GradParams p, const pvt_mx& q, const pvt_mx& q2, int sm_count,
+                  cudaStream_t stream) {
   using S = GradSizes<FMT, MT, CTAS>;
   p.a_tiles = (p.a_rows + S::kRows - 1) / S::kRows, p.tiles = p.a_tiles * ((p.cols + S::kCols - 1) / S::kCols);
-  CUtensorMap q_map;
+  CUtensorMap q_map, q2_map;
   cudaError_t e = make_map(&q_map, q.codes, 1, (uint64_t)q.rows, ((uint64_t)q.cols + 1) / 2, (uint64_t)q.ld, kStepR, S::kHalf / 2, false);
-  if (e == cudaSuccess) e = allow_smem<mx_grad_kernel<T, FMT, TRANS, MT, CTAS>>();
+  if (TWO && e == cudaSuccess)
+    e = make_map(&q2_map, q2.codes, 1, (uint64_t)q2.rows, ((uint64_t)q2.cols + 1) / 2, (uint64_t)q2.ld, kStepR, S::kHalf / 2, false);
+  if (e == cudaSuccess) e = allow_smem<mx_grad_kernel<T, FMT, TRANS, MT, CTAS, TWO>>();
   if (e != cudaSuccess) return e;
   uint32_t grid = 2 * (p.tiles < (uint32_t)sm_count / 2 ? p.tiles : (uint32_t)sm_count / 2), cluster = 2;
   if (CTAS == 1) {
@@ -532,30 +543,35 @@ cudaError_t start(const CUtensorMap& a_map, GradParams p, const pvt_mx& q, int s
     while (p.split < 8 && (uint64_t)p.tiles * p.split * 2 <= (uint64_t)sm_count && p.split * 2 <= p.steps) p.split *= 2;
     grid = p.tiles * p.split, cluster = p.split;
   }
-  return launch_clusters(mx_grad_kernel<T, FMT, TRANS, MT, CTAS>, grid, cluster, kThreads, S::kBytes, stream, a_map, q_map, p);
+  return launch_clusters(mx_grad_kernel<T, FMT, TRANS, MT, CTAS, TWO>, grid, cluster, kThreads, S::kBytes, stream, a_map, q_map,
+                         TWO ? a2_map : a_map, TWO ? q2_map : q_map, p);
 }
 
-template <typename T, int FMT, bool TRANS>
+// dy2, q2: the second pair, of the same sizes (TWO)
+template <typename T, int FMT, bool TRANS, bool TWO = false>
 cudaError_t grad(const void* dy, int64_t lddy, uint32_t a_rows, const pvt_mx& q, T* out, int64_t ldo, bool accumulate,
-                 uint32_t* status, int sm_count, cudaStream_t stream) {
+                 uint32_t* status, int sm_count, cudaStream_t stream, const void* dy2 = nullptr, const pvt_mx* other = nullptr) {
+  const pvt_mx& q2 = TWO ? *other : q;
   GradParams p = {};
-  p.scales = q.scales, p.ts = q.tensor_scale, p.out = out, p.ldo = ldo, p.status = status;
+  p.scales = q.scales, p.scales2 = q2.scales, p.ts = q.tensor_scale, p.out = out, p.ldo = ldo, p.status = status;
   p.a_rows = a_rows, p.cols = (uint32_t)q.cols, p.accumulate = accumulate;
   p.strip_bytes = strip_tiles(q.cols, block_of(FMT)) * kTileBytes;
-  p.steps = ((uint32_t)q.rows + kStepR - 1) / kStepR;
+  p.half = ((uint32_t)q.rows + kStepR - 1) / kStepR, p.steps = TWO ? 2 * p.half : p.half;
   const m1::WaitTestHook hook = m1::wait_test_hook();
   p.max_spins = hook.max_spins, p.withhold = hook.withhold_copy;
   const uint64_t tokens = TRANS ? (uint64_t)q.rows : a_rows, features = TRANS ? a_rows : (uint64_t)q.rows;
-  CUtensorMap a_map;
-  const cudaError_t e = make_map(&a_map, dy, 2, tokens, features, (uint64_t)lddy * 2, TRANS ? kStepR : kTileA);
+  CUtensorMap a_map, a2_map;
+  cudaError_t e = make_map(&a_map, dy, 2, tokens, features, (uint64_t)lddy * 2, TRANS ? kStepR : kTileA);
+  if (TWO && e == cudaSuccess) e = make_map(&a2_map, dy2, 2, tokens, features, (uint64_t)lddy * 2, kTileA);
   if (e != cudaSuccess) return e;
   // Blocks by themselves where they have the rows, or pairs would leave three quarters of the SMs idle: dx by blocks and by pairs,
   // 256 tokens 4096 by 4096 18.5 and 28.2 us, 600 tokens 2048 by 2048 15.3 and 16.9.
   const uint64_t pair_tiles = (uint64_t)((a_rows + 255) / 256) * ((p.cols + 255) / 256);
-  if (a_rows <= (uint32_t)kTileA || pair_tiles < (uint64_t)sm_count / 4) return start<T, FMT, TRANS, 1, 1>(a_map, p, q, sm_count, stream);
+  if (a_rows <= (uint32_t)kTileA || pair_tiles < (uint64_t)sm_count / 4)
+    return start<T, FMT, TRANS, 1, 1, TWO>(a_map, a2_map, p, q, q2, sm_count, stream);
   // (512 by 128 and 256 by 256, 2048 x 4096 by 11008: dx 125 and 128 us, dw 150 and 142: A's transpose takes two copies a tile)
-  if (TRANS || a_rows <= 256) return start<T, FMT, TRANS, 1, 2>(a_map, p, q, sm_count, stream);
-  return start<T, FMT, TRANS, TRANS ? 1 : 2, 2>(a_map, p, q, sm_count, stream);
+  if (TRANS || a_rows <= 256) return start<T, FMT, TRANS, 1, 2, TWO>(a_map, a2_map, p, q, q2, sm_count, stream);
+  return start<T, FMT, TRANS, TRANS ? 1 : 2, 2, TWO>(a_map, a2_map, p, q, q2, sm_count, stream);
 }
 
 }  // namespace
@@ -589,6 +605,28 @@ cudaError_t launch_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const
       x.format == PVT_MX_E4M3_16
           ? grad<float, PVT_MX_E4M3_16, true>(dy, lddy, (uint32_t)n, x, dw, lddw, accumulate, status, sm_count, stream)
           : grad<float, PVT_MX_E8M0_32, true>(dy, lddy, (uint32_t)n, x, dw, lddw, accumulate, status, sm_count, stream);
+  timing_end(kKernMx, stream);
+  count_launches(1);
+  return e;
+}
+
+cudaError_t launch_mx_gated_grad_input(const void* dgate, const void* dup, int64_t ldd, int32_t tokens, const pvt_mx& wg, const pvt_mx& wu,
+                                       void* dx, int32_t dtype, int64_t lddx, uint32_t* status, int sm_count, cudaStream_t stream) {
+  const uint32_t n = (uint32_t)tokens;
+  timing_begin(kKernMx, stream);
+  cudaError_t e;
+  auto call = [&](auto* out) {
+    using T = std::remove_pointer_t<decltype(out)>;
+    return wg.format == PVT_MX_E4M3_16
+               ? grad<T, PVT_MX_E4M3_16, false, true>(dgate, ldd, n, wg, out, lddx, false, status, sm_count, stream, dup, &wu)
+               : grad<T, PVT_MX_E8M0_32, false, true>(dgate, ldd, n, wg, out, lddx, false, status, sm_count, stream, dup, &wu);
+  };
+  if (dtype == PVT_F32)
+    e = call(static_cast<float*>(dx));
+  else if (dtype == PVT_F16)
+    e = call(static_cast<__half*>(dx));
+  else
+    e = call(static_cast<__nv_bfloat16*>(dx));
   timing_end(kKernMx, stream);
   count_launches(1);
   return e;

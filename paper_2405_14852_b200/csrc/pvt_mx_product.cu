@@ -12,8 +12,7 @@
 // are shared by a cluster of up to eight blocks, whose partial sums meet in shared memory across the cluster, always in
 // the order of ranks.  From 17 tokens on pairs of blocks take over (below): 4096 by 11008, 16 / 32 / 64 / 128 tokens, tiles
 // of as many tokens here 9.8 / 11.8 / 16.3 / 14.9 us, pairs from 32 on 10.2 / 9.2 / 9.2.
-#include "pvt_mma.cuh"
-#include "pvt_mx.cuh"
+#include "pvt_mx_mma.cuh"
 
 namespace pvt {
 namespace {
@@ -23,25 +22,6 @@ using namespace mma;
 
 constexpr int kPThreads = 192;   // four warps read sums out, one copies, one multiplies
 constexpr int kCopyWarp = 4, kMmaWarp = 5;
-constexpr int kTileW = 128;      // rows of w
-constexpr int kRowBytes = 128;   // of a step
-constexpr uint32_t kFewTokens = 16;
-
-// of the kernel for few tokens
-template <int FMT>
-struct FewSizes {
-  static constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4;  // scale tiles of a step and strip
-  // a stage: rows of w, rows of x, scales of w, scales of x
-  static constexpr uint32_t kX = kTileW * kRowBytes, kWs = kX + kFewTokens * kRowBytes, kXs = kWs + KT * kTileBytes;
-  static constexpr uint32_t kStage = kXs + KT * kTileBytes, kStageAligned = (kStage + 1023) / 1024 * 1024;
-  static constexpr uint32_t kStages = 110 * 1024 / kStageAligned;  // of two blocks per SM
-  static constexpr uint32_t kScaleCols = KT * 4 * 2;
-  static constexpr uint32_t kTmem = 32 + kStages * kScaleCols <= 128 ? 128 : 256;
-  static_assert(32 + kStages * kScaleCols <= kTmem, "sums and scales fit");
-  static constexpr size_t kBytes = kStages * kStageAligned + 1024;
-  static_assert(kFewTokens * kTileW * 4 <= kStages * kStageAligned, "the partial sums fit the stages");
-};
-
 struct ProductParams {
   const uint8_t* w_codes;
   const uint8_t* w_scales;
@@ -65,36 +45,6 @@ struct ProductShared {
   uint64_t done, spare;
   uint32_t tmem, abandoned;
 };
-
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc) {
-  asm volatile(
-      "{\n\t.reg .pred one;\n\t"
-      "elect.sync _|one, 0xffffffff;\n\t"
-      "@one tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc)
-      : "memory");
-}
-// 64 columns of all rows of a tile
-template <int FMT>
-__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                         uint32_t onto) {
-  if (FMT == PVT_MX_E8M0_32) {
-    asm volatile(
-        "{\n\t.reg .pred one, p;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %6, 0;\n\t"
-        "@one tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
-        : "memory");
-  } else {
-    asm volatile(
-        "{\n\t.reg .pred one, p;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %6, 0;\n\t"
-        "@one tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(onto)
-        : "memory");
-  }
-}
 
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_constant__ CUtensorMap w_map,
@@ -234,14 +184,6 @@ __global__ void __launch_bounds__(kPThreads) mx_product_kernel(const __grid_cons
 // products of a step are 512 cycles, the bound: the tensor pipe is active in 85 % of all cycles (4096 x 8192 by 28672: 318 us
 // and 6.0 PFLOP/s where the clock holds, 390 under the power cap).  The blocks stay and take tile after tile; copies for the
 // next one are under way while eight warps empty the sums into registers, and those are stored while it is multiplied.
-constexpr int kPairReaders = 8;  // warps
-constexpr int kPairCopyWarps = 2;  // (a warp takes 100 cycles and more for each copy it issues)
-constexpr int kPairCopyWarp = kPairReaders, kPairMmaWarp = kPairCopyWarp + kPairCopyWarps;
-constexpr int kPairThreads = (kPairMmaWarp + 1) * 32;
-constexpr uint32_t kPairRows = 256;   // of w
-constexpr uint32_t kPairStages = 7;   // at most
-constexpr uint32_t kLeastSteps = 12;  // of a pair that shares a tile with others
-
 struct PairShared {
   alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
   uint64_t empty[kPairStages];            // of each
@@ -264,259 +206,6 @@ struct PairParams {
   uint32_t split;        // pairs per tile
   uint32_t max_spins, withhold;
 };
-
-// N: rows of x in a tile
-template <int FMT, uint32_t N>
-struct PairSizes {
-  static constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4, kStrips = N / kStrip;
-  static constexpr uint32_t kX = kTileW * kRowBytes, kWs = kX + N / 2 * kRowBytes, kXs = kWs + KT * kTileBytes;
-  static constexpr uint32_t kStage = kXs + kStrips * KT * kTileBytes, kStageAligned = (kStage + 1023) / 1024 * 1024;
-  static constexpr uint32_t kScaleCols = KT * 4 * (1 + kStrips);  // of a stage
-  static constexpr uint32_t kStages = N == 256 ? 5 : 7;
-  static_assert(N + kStages * kScaleCols <= 512, "sums and scales fit tensor memory");
-  static constexpr size_t kBytes = kStages * kStageAligned + 1024;
-  static_assert(kBytes + 1024 <= 227 * 1024 && kStages <= kPairStages, "a block's shared memory");
-  static_assert(N * kTileW * 4 <= kStages * kStageAligned, "the partial sums fit the stages");
-};
-
-// A step of a pair: its scales to tensor memory (two or four tiles for w's 128 rows, as many for each of one or two strips of
-// x) and the products of four times 64 columns.  One thread is elected for all of them, and descriptors are counted on inside:
-// a tile of scales is 32 units of 16 bytes, four columns of tensor memory; 64 columns are 2 units of either operand.
-template <int FMT, uint32_t STRIPS>
-__device__ __forceinline__ void multiply_step(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                              uint64_t w_scales, uint64_t x_scales, uint32_t onto) {
-  if constexpr (FMT == PVT_MX_E8M0_32 && STRIPS == 2) {
-    asm volatile(
-        "{\n\t"
-        ".reg .pred one, p, t;\n\t"
-        ".reg .b32 s, x, i;\n\t"
-        ".reg .b64 q, a, b;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %8, 0;\n\t"
-        "setp.eq.u32 t, 0, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.s64 q, %6, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "add.s64 q, %7, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 x, %5, 4;\n\t"
-        "add.s64 q, %7, 64;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.s64 q, %6, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 8;\n\t"
-        "add.s64 q, %7, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 x, %5, 12;\n\t"
-        "add.s64 q, %7, 96;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.s64 a, %1, 0;\n\t"
-        "add.s64 b, %2, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], p;\n\t"
-        "add.s64 a, %1, 2;\n\t"
-        "add.s64 b, %2, 2;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "or.b32 i, %3, 1073741856;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 4;\n\t"
-        "add.s64 b, %2, 4;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.u32 x, %5, 8;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 6;\n\t"
-        "add.s64 b, %2, 6;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.u32 x, %5, 8;\n\t"
-        "or.b32 i, %3, 1073741856;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
-        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
-        : "memory");
-  } else if constexpr (FMT == PVT_MX_E8M0_32) {
-    asm volatile(
-        "{\n\t"
-        ".reg .pred one, p, t;\n\t"
-        ".reg .b32 s, x, i;\n\t"
-        ".reg .b64 q, a, b;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %8, 0;\n\t"
-        "setp.eq.u32 t, 0, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.s64 q, %6, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "add.s64 q, %7, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.s64 q, %6, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 4;\n\t"
-        "add.s64 q, %7, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.s64 a, %1, 0;\n\t"
-        "add.s64 b, %2, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], p;\n\t"
-        "add.s64 a, %1, 2;\n\t"
-        "add.s64 b, %2, 2;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "or.b32 i, %3, 1073741856;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 4;\n\t"
-        "add.s64 b, %2, 4;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.u32 x, %5, 4;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 6;\n\t"
-        "add.s64 b, %2, 6;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.u32 x, %5, 4;\n\t"
-        "or.b32 i, %3, 1073741856;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, i, [s], [x], t;\n\t"
-        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
-        : "memory");
-  } else if constexpr (STRIPS == 2) {
-    asm volatile(
-        "{\n\t"
-        ".reg .pred one, p, t;\n\t"
-        ".reg .b32 s, x, i;\n\t"
-        ".reg .b64 q, a, b;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %8, 0;\n\t"
-        "setp.eq.u32 t, 0, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.s64 q, %6, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "add.s64 q, %7, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 x, %5, 4;\n\t"
-        "add.s64 q, %7, 128;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.s64 q, %6, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 8;\n\t"
-        "add.s64 q, %7, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 x, %5, 12;\n\t"
-        "add.s64 q, %7, 160;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 8;\n\t"
-        "add.s64 q, %6, 64;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 16;\n\t"
-        "add.s64 q, %7, 64;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 x, %5, 20;\n\t"
-        "add.s64 q, %7, 192;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 12;\n\t"
-        "add.s64 q, %6, 96;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 24;\n\t"
-        "add.s64 q, %7, 96;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 x, %5, 28;\n\t"
-        "add.s64 q, %7, 224;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.s64 a, %1, 0;\n\t"
-        "add.s64 b, %2, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], p;\n\t"
-        "add.s64 a, %1, 2;\n\t"
-        "add.s64 b, %2, 2;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.u32 x, %5, 8;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 4;\n\t"
-        "add.s64 b, %2, 4;\n\t"
-        "add.u32 s, %4, 8;\n\t"
-        "add.u32 x, %5, 16;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 6;\n\t"
-        "add.s64 b, %2, 6;\n\t"
-        "add.u32 s, %4, 12;\n\t"
-        "add.u32 x, %5, 24;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
-        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
-        : "memory");
-  } else {
-    asm volatile(
-        "{\n\t"
-        ".reg .pred one, p, t;\n\t"
-        ".reg .b32 s, x, i;\n\t"
-        ".reg .b64 q, a, b;\n\t"
-        "elect.sync _|one, 0xffffffff;\n\t"
-        "setp.ne.u32 p, %8, 0;\n\t"
-        "setp.eq.u32 t, 0, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.s64 q, %6, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "add.s64 q, %7, 0;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.s64 q, %6, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 4;\n\t"
-        "add.s64 q, %7, 32;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 8;\n\t"
-        "add.s64 q, %6, 64;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 8;\n\t"
-        "add.s64 q, %7, 64;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.u32 s, %4, 12;\n\t"
-        "add.s64 q, %6, 96;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [s], q;\n\t"
-        "add.u32 x, %5, 12;\n\t"
-        "add.s64 q, %7, 96;\n\t"
-        "@one tcgen05.cp.cta_group::2.32x128b.warpx4 [x], q;\n\t"
-        "add.s64 a, %1, 0;\n\t"
-        "add.s64 b, %2, 0;\n\t"
-        "add.u32 s, %4, 0;\n\t"
-        "add.u32 x, %5, 0;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], p;\n\t"
-        "add.s64 a, %1, 2;\n\t"
-        "add.s64 b, %2, 2;\n\t"
-        "add.u32 s, %4, 4;\n\t"
-        "add.u32 x, %5, 4;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 4;\n\t"
-        "add.s64 b, %2, 4;\n\t"
-        "add.u32 s, %4, 8;\n\t"
-        "add.u32 x, %5, 8;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
-        "add.s64 a, %1, 6;\n\t"
-        "add.s64 b, %2, 6;\n\t"
-        "add.u32 s, %4, 12;\n\t"
-        "add.u32 x, %5, 12;\n\t"
-        "or.b32 i, %3, 0;\n\t"
-        "@one tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a, b, i, [s], [x], t;\n\t"
-        "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "l"(w_scales), "l"(x_scales), "r"(onto)
-        : "memory");
-  }
-}
 
 template <typename T, int FMT, uint32_t N>
 __global__ void __launch_bounds__(kPairThreads, 1)
@@ -702,31 +391,16 @@ cudaError_t product_pairs(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, u
   if (e != cudaSuccess) return e;
   uint32_t pairs = (uint32_t)sm_count / 2;
   if (pairs > p.tiles) pairs = p.tiles;
-  // Few tiles of many steps: two or four pairs to a tile, as long as all clusters run at once (those of eight blocks leave more
-  // SMs over).  By single pairs and so, 256 tokens 8192 by 4096 e4m3 13.5 and 11.3 us, 75 tokens 21892 by 2787 28.8 and 12.9; but
-  // 200 tokens 2048 by 2048 6.0 and 7.2, and four pairs to each of 16 tiles, 32 tokens 4096 by 4096, 7.7 and 11.3.
-  const uint32_t all = (uint32_t)sm_count / 2;
-  p.split = 1;
-  if (p.tiles <= all * 7 / 16 && p.steps >= 2 * kLeastSteps) p.split = p.tiles <= all / 6 && p.steps >= 4 * kLeastSteps ? 4 : 2;
+  p.split = pairs_per_tile(p.tiles, p.steps, sm_count);
   return launch_clusters(mx_product_pair_kernel<T, FMT, N>, 2 * (p.split > 1 ? p.tiles * p.split : pairs), 2 * p.split, kPairThreads,
                          S::kBytes, stream, maps[0], maps[1], maps[2], maps[3], p);
-}
-
-// Whether tiles of 128 rows of x serve better than 256: they take three quarters of the time, so where there are not more rounds
-// of them (256 tokens 4096 by 4096: 8.3 and 9.7 us, 64 tokens by 11008 8.1 and 9.3; 333 tokens 5119 by 13823, three rounds
-// and two: 22.9 and 19.5).
-bool narrow_tiles(int32_t x_rows, int32_t w_rows, int sm_count) {
-  const uint64_t pairs = (uint64_t)sm_count / 2, w_tiles = ((uint64_t)w_rows + kPairRows - 1) / kPairRows;
-  const uint64_t rounds_256 = (w_tiles * (((uint64_t)x_rows + 255) / 256) + pairs - 1) / pairs;
-  const uint64_t rounds_128 = (w_tiles * (((uint64_t)x_rows + 127) / 128) + pairs - 1) / pairs;
-  return rounds_128 * 3 < rounds_256 * 4;
 }
 
 template <typename T, int FMT>
 cudaError_t product(const pvt_mx& x, const pvt_mx& w, T* y, int64_t ldy, uint32_t* status, int sm_count, cudaStream_t stream) {
   using S = FewSizes<FMT>;
   if (x.rows > (int32_t)kFewTokens)
-    return narrow_tiles(x.rows, w.rows, sm_count) ? product_pairs<T, FMT, 128>(x, w, y, ldy, status, sm_count, stream)
+    return narrow_tiles(x.rows, ((uint64_t)w.rows + kPairRows - 1) / kPairRows, sm_count) ? product_pairs<T, FMT, 128>(x, w, y, ldy, status, sm_count, stream)
                                                   : product_pairs<T, FMT, 256>(x, w, y, ldy, status, sm_count, stream);
   ProductParams p = {};
   p.w_codes = w.codes, p.w_scales = w.scales, p.x_scales = x.scales, p.w_ts = w.tensor_scale, p.x_ts = x.tensor_scale;

@@ -24,13 +24,10 @@ struct ApplyParams {
   const void *weight, *bias;
   void* y;
   float* stats;
-  uint8_t *codes, *scales;
-  const float* tensor_scale;
-  int64_t ldc;
+  mx::Held q;
   Shape s;
   uint32_t padded;  // rows, or those of whole strips where scales are written
-  uint32_t tiles;   // of scales, of a strip
-  int32_t w_dtype, y_dtype, format;
+  int32_t w_dtype, y_dtype;
   float eps;
   bool layer, w_wide;
 };
@@ -45,35 +42,6 @@ __device__ __forceinline__ float row_sum(float v, const Shape& s, float* slots) 
   return team_sum(lane < s.warps ? slots[lane] : 0.0f, 32);
 }
 
-// a span's eight values of every lane (neighbouring columns from c0 on) into codes and scales
-template <int FMT>
-__device__ __forceinline__ void put_block(const ApplyParams& p, uint32_t row, uint32_t c0, bool here, const mx::TensorScale& t, float* v) {
-  constexpr uint32_t LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;  // of a block
-  const uint32_t lane = threadIdx.x & 31, block = c0 / (8 * LANES);
-  uint32_t top = 0, word;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (c0 + i >= p.s.cols) v[i] = 0.0f;
-    top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-  }
-#pragma unroll
-  for (uint32_t d = 1; d < LANES; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-  uint32_t byte = mx::quantize_block<FMT, 8>(v, top, t, &word);
-  if (c0 >= p.s.cols || !here) byte = 0;  // no such block
-  uint32_t four = byte | __shfl_down_sync(0xffffffffu, byte, LANES) << 8;
-  four |= __shfl_down_sync(0xffffffffu, four, 2 * LANES) << 16;
-  if (lane % (4 * LANES) == 0 && row < p.padded) *reinterpret_cast<uint32_t*>(p.scales + mx::scale_at(row, block, p.tiles)) = four;
-  if (!here || c0 >= p.s.cols) return;
-  uint8_t* const to = p.codes + (int64_t)row * p.ldc + c0 / 2;
-  if (c0 + 8 <= p.s.cols) {
-    *reinterpret_cast<uint32_t*>(to) = word;
-  } else {
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i)
-      if (2 * i < p.s.cols - c0) to[i] = (uint8_t)(word >> (8 * i));
-  }
-}
-
 // G: spans to a warp
 template <typename T, bool WIDE, int G>
 __global__ void __launch_bounds__(G == 1 ? 1024 : 512) norm_apply_kernel(const __grid_constant__ ApplyParams p) {
@@ -85,7 +53,7 @@ __global__ void __launch_bounds__(G == 1 ? 1024 : 512) norm_apply_kernel(const _
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t in_row = s.warps > 1 ? warp : 0, l = lane & (s.lanes - 1), step = WIDE ? 1 : s.lanes;
   const uint32_t team = s.warps > 1 ? 0 : tid / s.lanes;
-  const mx::TensorScale scale(p.codes && p.format == PVT_MX_E4M3_16 ? p.tensor_scale : nullptr);
+  const mx::TensorScale scale(p.q.tensor_scale);
   uint32_t turn = 0;
   for (uint64_t first = (uint64_t)blockIdx.x * s.teams; first < p.padded; first += (uint64_t)gridDim.x * s.teams, turn ^= 1) {
     const uint32_t row = (uint32_t)first + team;
@@ -126,7 +94,7 @@ __global__ void __launch_bounds__(G == 1 ? 1024 : 512) norm_apply_kernel(const _
     }
     const float rstd = 1.0f / sqrtf(row_sum(sum, s, slots[turn][1]) / (float)s.cols + p.eps);
     if (p.stats && here && in_row == 0 && l == 0) *reinterpret_cast<float2*>(p.stats + 2 * (size_t)row) = make_float2(mean, rstd);
-    if (!p.y && !p.codes) continue;
+    if (!p.y && !p.q.codes) continue;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const uint32_t span = g * s.warps + in_row, c = span * kSpanCols + (WIDE ? 8 * l : l);
@@ -141,13 +109,13 @@ __global__ void __launch_bounds__(G == 1 ? 1024 : 512) norm_apply_kernel(const _
           using U = std::remove_pointer_t<decltype(type)>;
           put<WIDE>(static_cast<U*>(p.y) + (int64_t)row * p.ldy, c, step, here ? s.cols : 0, v[g]);
         });
-      if (p.codes) {  // (a row is a warp's at least)
+      if (p.q.codes) {  // (a row is a warp's at least)
         if (!WIDE) mx::turn<false>(buffer[warp], v[g], lane);
         const uint32_t c0 = span * kSpanCols + 8 * lane;
-        if (p.format == PVT_MX_E8M0_32)
-          put_block<PVT_MX_E8M0_32>(p, row, c0, here, scale, v[g]);
+        if (p.q.format == PVT_MX_E8M0_32)
+          mx::put_eight<PVT_MX_E8M0_32>(p.q, row, c0, here, row < p.padded, scale, v[g]);
         else
-          put_block<PVT_MX_E4M3_16>(p, row, c0, here, scale, v[g]);
+          mx::put_eight<PVT_MX_E4M3_16>(p.q, row, c0, here, row < p.padded, scale, v[g]);
       }
     }
   }
@@ -155,7 +123,7 @@ __global__ void __launch_bounds__(G == 1 ? 1024 : 512) norm_apply_kernel(const _
 
 template <typename T, bool WIDE, int G>
 cudaError_t apply(ApplyParams p, uint32_t rows, uint32_t cols, int sm_count, cudaStream_t stream) {
-  p.s = shape_of(rows, cols, G, kTeamThreads, !p.codes);
+  p.s = shape_of(rows, cols, G, kTeamThreads, !p.q.codes);
   const uint32_t threads = p.s.warps > 1 ? 32 * p.s.warps : kTeamThreads;
   const uint64_t need = ((uint64_t)p.padded + p.s.teams - 1) / p.s.teams, most = (uint64_t)sm_count * 64;
   return launch_dependent(norm_apply_kernel<T, WIDE, G>, (unsigned)(need < most ? need : most), threads, 0, stream, p);
@@ -181,8 +149,7 @@ cudaError_t launch_apply(const pvt_norm& n, void* total, int64_t ldt, void* y, i
   p.y = y, p.ldy = ldy, p.y_dtype = y_dtype, p.stats = stats, p.eps = n.eps, p.layer = n.kind == PVT_NORM_LAYER;
   p.padded = (uint32_t)n.rows;
   if (yq) {
-    p.codes = yq->codes, p.ldc = yq->ld, p.scales = yq->scales, p.tensor_scale = yq->tensor_scale, p.format = yq->format;
-    p.tiles = mx::strip_tiles(n.cols, mx::block_of(yq->format));
+    p.q = mx::held(*yq);
     p.padded = (uint32_t)((n.rows + kStrip - 1) / kStrip * kStrip);
   }
   const size_t w_size = n.weight_dtype == PVT_F32 ? 4 : 2, y_size = y_dtype == PVT_F32 ? 4 : 2;

@@ -89,3 +89,42 @@ def activation(a, act):
     k, c = math.sqrt(2.0 / math.pi), 0.044715
     s = torch.sigmoid(2.0 * k * (a + c * a ** 3))
     return a * s, s + a * s * torch.sigmoid(-2.0 * k * (a + c * a ** 3)) * 2.0 * k * (1.0 + 3.0 * c * a * a)
+
+
+def gated(a, b, act):
+    return activation(a, act)[0] * b
+
+
+def products(xv, wg, wu):
+    """a, b and how far binary32 sums of them may be off: (cols + 4) 2^-23 of the sum of magnitudes"""
+    n = (xv.shape[1] + 4) * 2.0 ** -23
+    return xv @ wg.T, xv @ wu.T, n * (xv.abs() @ wg.abs().T), n * (xv.abs() @ wu.abs().T)
+
+
+def _steps(a, act):
+    """Roundings of 2^-23 in f(a) / a, relative: an exponential (2 units), a sum, a quotient (2) and products; an argument's own
+    rounding counts as often as it is large: |z| of the logistic function's, a^2 of the normal distribution's (whose function is
+    within 4 units)."""
+    if act == GELU:
+        return 10 + a * a
+    z = a if act == SILU else 1.6 * (a + 0.045 * a ** 3)
+    return 8 + 2 * z.abs()
+
+
+def gated_bound(a, b, d_a, d_b, act):
+    """How far h may be off in binary32, |f'| being at most 1.13; quotients beyond 2^126 are 0."""
+    f, _ = activation(a, act)
+    off = 1.13 * d_a * b.abs() + f.abs() * d_b + 1.13 * d_a * d_b + _steps(a, act) * 2.0 ** -23 * (f * b).abs()
+    return 1.001 * off + 2.0 ** -126 * (1 + (a * b).abs())
+
+
+def gated_grad_bounds(a, b, d_a, d_b, dh, act):
+    """The same for dgate and dup, |f''| being at most 1; f' is a sum of two terms of at most 1.3, one of which has a difference
+    from 1 in it (2^-24 of a dz / da)."""
+    f, slope = activation(a, act)
+    dz = torch.ones_like(a) if act == SILU else 1.6 + 0.22 * a * a
+    d_slope = 2.0 ** -23 * (1.3 * (_steps(a, act) + 4) + (a.abs() * dz if act != GELU else 0.0))
+    dh = dh.double().abs()
+    d_gate = dh * (b.abs() * (d_a + d_slope) + slope.abs() * d_b + d_a * d_b + 2.0 ** -22 * (b * slope).abs())
+    d_up = dh * (1.13 * d_a + (_steps(a, act) + 2) * 2.0 ** -23 * f.abs())
+    return 1.001 * d_gate + 2.0 ** -126, 1.001 * d_up + 2.0 ** -126
