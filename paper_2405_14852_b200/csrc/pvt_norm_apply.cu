@@ -1,8 +1,9 @@
 // Norm of the rows of x + residual, into floats or straight into 4-bit block floating point.
 //
-// A row stays in registers from its one reading to its one writing: the sum with the residual is rounded to x's type first, as
-// it is kept; then the mean, then the mean of the squared differences from it (a second pass over registers, so a mean far from
-// 0 costs no digits).  Bound by HBM; the weights come from the L1 and L2 again for each row.
+// A row is read once and stays in registers to its end: the sum with the residual is rounded to x's type first, as it is
+// kept; then the mean, then the mean of the squared differences from it (a second pass over registers, so a mean far from 0 costs no
+// digits).  Two barriers a row, one without the mean; where rows are many, a team
+// has two at a time and both share them.
 //
 // 4-bit results: a lane's eight columns are a quarter or half of a block, as in quantisation by itself; rows of no alignment are
 // turned in shared memory first.
@@ -15,7 +16,7 @@ namespace {
 
 using mx::kStrip;
 
-constexpr uint32_t kTeamThreads = 256;  // of a block where rows share it
+constexpr uint32_t kTurn = mx::kSpan + 8 * mx::kSpan / 32;  // floats of a warp
 
 struct ApplyParams {
   const void *x, *residual;
@@ -27,116 +28,175 @@ struct ApplyParams {
   mx::Held q;
   Shape s;
   uint32_t padded;  // rows, or those of whole strips where scales are written
+  uint32_t image;   // bytes
+  uint32_t sets;    // blocks or clusters
+  uint32_t stages;  // two or three
   int32_t w_dtype, y_dtype;
   float eps;
-  bool layer, w_wide;
+  bool layer;
 };
 
-// over all warps of a row; `slots`: shared, one per warp, not in use by an earlier sum
-__device__ __forceinline__ float row_sum(float v, const Shape& s, float* slots) {
-  v = team_sum(v, s.lanes);
-  if (s.warps == 1) return v;
-  const uint32_t lane = threadIdx.x & 31;
-  if (lane == 0) slots[threadIdx.x >> 5] = v;
-  __syncthreads();
-  return team_sum(lane < s.warps ? slots[lane] : 0.0f, 32);
-}
-
-// G: spans to a warp
-template <typename T, bool WIDE, int G>
-__global__ void __launch_bounds__(G == 1 ? 1024 : 512) norm_apply_kernel(const __grid_constant__ ApplyParams p) {
-  __shared__ float slots[2][2][32];
-  __shared__ float buffer[WIDE ? 1 : (G == 1 ? 32 : 16)][mx::kSpan + 8 * mx::kSpan / 32];
+// G: spans of a warp, R: rows of a team at a time
+template <typename T, int L, int G, int R>
+__global__ void __launch_bounds__(L == kRagged ? kRaggedBound : kMostThreads) norm_apply_kernel(const __grid_constant__ ApplyParams p) {
+  constexpr bool WIDE = L != kRagged;
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ float slots[2][2][kMostParts * kMostWarps][R];
   pdl_trigger();
   pdl_wait();
   const Shape& s = p.s;
-  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t in_row = s.warps > 1 ? warp : 0, l = lane & (s.lanes - 1), step = WIDE ? 1 : s.lanes;
-  const uint32_t team = s.warps > 1 ? 0 : tid / s.lanes;
+  const uint32_t rank = blockIdx.x % s.parts, set = blockIdx.x / s.parts;
+  const Place<L, G> at(s, rank);
   const mx::TensorScale scale(p.q.tensor_scale);
-  uint32_t turn = 0;
-  for (uint64_t first = (uint64_t)blockIdx.x * s.teams; first < p.padded; first += (uint64_t)gridDim.x * s.teams, turn ^= 1) {
-    const uint32_t row = (uint32_t)first + team;
-    const bool here = row < s.rows;
-    float v[G][8];
-    const T* const x = static_cast<const T*>(p.x) + (int64_t)row * p.ldx;
+  const T* const x = static_cast<const T*>(p.x);
+  const T* const residual = static_cast<const T*>(p.residual);
+  // a stage: x's images of R rows of every team, then the residual's
+  const uint32_t row_at = s.teams * p.image, res_at = R * row_at, stage = (residual ? 2 : 1) * res_at, own = at.team * p.image;
+  const uint32_t base = m1::smem_u32(ring) + own, stride = p.sets * s.teams * R;
+  auto ask = [&](uint64_t row0, uint32_t k) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const uint32_t c = (g * s.warps + in_row) * kSpanCols + (WIDE ? 8 * l : l);
-      T e[8];
-      take<WIDE>(x, c, step, here ? s.cols : 0, e);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[g][i] = widen<T>(e[i]);
-      if (p.residual) {
-        take<WIDE>(static_cast<const T*>(p.residual) + (int64_t)row * p.ldr, c, step, here ? s.cols : 0, e);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[g][i] = widen<T>(narrow<T>(v[g][i] + widen<T>(e[i])));
+    for (int r = 0; r < R; ++r) {
+      const uint64_t row = row0 + r * s.teams;
+      if (row < s.rows) {
+        at.ask(base + k * stage + r * row_at, x + (int64_t)row * p.ldx);
+        if (residual) at.ask(base + k * stage + res_at + r * row_at, residual + (int64_t)row * p.ldr);
       }
-      if (p.total) put<WIDE>(static_cast<T*>(p.total) + (int64_t)row * p.ldt, c, step, here ? s.cols : 0, v[g]);
     }
-    float mean = 0.0f, sum = 0.0f;
+    copies_end();
+  };
+  uint64_t row0 = (uint64_t)set * s.teams * R + at.team;
+  for (uint32_t k = 0; k + 1 < p.stages; ++k) ask(row0 + (uint64_t)k * stride, k);
+  float w[G][8], b[G][8];
+  at.weights(p.weight, p.w_dtype, 1.0f, w);
+  at.weights(p.bias, p.w_dtype, 0.0f, b);
+  const float inv = 1.0f / (float)s.cols;
+  uint32_t turn = 0, k = 0;
+  // (all of a block's teams go round as often as its first one)
+  for (uint64_t first = (uint64_t)set * s.teams * R; first < p.padded; first += stride, row0 += stride, turn ^= 1) {
+    copies_wait(p.stages > 2);
+    if (!WIDE) {  // what others have copied is here, and the stage that is asked for next has been read by all
+      if (s.warps > 1)
+        __syncthreads();
+      else
+        __syncwarp();
+    }
+    ask(row0 + (uint64_t)(p.stages - 1) * stride, k == 0 ? p.stages - 1 : k - 1);
+    const unsigned char* const image = ring + own + k * stage;
+    k = k == p.stages - 1 ? 0 : k + 1;
+    float v[R][G][8], sum[R], mean[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint64_t row = row0 + r * s.teams;
+      mean[r] = 0.0f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        at.take(image + r * row_at, x + (int64_t)row * p.ldx, g, v[r][g]);
+        if (residual) {
+          float e[8];
+          at.take(image + res_at + r * row_at, residual + (int64_t)row * p.ldr, g, e);
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            T two[2];
+            narrow_pair(v[r][g][i] + e[i], v[r][g][i + 1] + e[i + 1], two);
+            v[r][g][i] = widen<T>(two[0]), v[r][g][i + 1] = widen<T>(two[1]);
+          }
+        }
+        if (p.total && row < s.rows) at.put(static_cast<T*>(p.total) + (int64_t)row * p.ldt, g, v[r][g]);
+        mean[r] += sum8(v[r][g]);
+      }
+    }
     if (p.layer) {
+      row_sums<R>(mean, s, rank, slots[turn][0]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        mean[r] *= inv;
+#pragma unroll
+        for (int g = 0; g < G; ++g) at.each(g, [&](int i) { v[r][g][i] -= mean[r]; });
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      sum[r] = 0.0f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) sum[r] += dot8(v[r][g], v[r][g]);
+    }
+    row_sums<R>(sum, s, rank, slots[turn][1]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint64_t row = row0 + r * s.teams;
+      const bool here = row < s.rows;
+      const float rstd = inverse_root(fmaf(sum[r], inv, p.eps));
+      if (p.stats && here && rank == 0 && at.in_team == 0)
+        *reinterpret_cast<float2*>(p.stats + 2 * row) = make_float2(p.layer ? mean[r] : 0.0f, rstd);
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += v[g][i];
-      mean = row_sum(sum, s, slots[turn][0]) / (float)s.cols;
-      sum = 0.0f;
-    }
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const uint32_t c = (g * s.warps + in_row) * kSpanCols + (WIDE ? 8 * l : l);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[g][i] = c + i * step < s.cols ? v[g][i] - mean : 0.0f;
-        sum = fmaf(v[g][i], v[g][i], sum);
-      }
-    }
-    const float rstd = 1.0f / sqrtf(row_sum(sum, s, slots[turn][1]) / (float)s.cols + p.eps);
-    if (p.stats && here && in_row == 0 && l == 0) *reinterpret_cast<float2*>(p.stats + 2 * (size_t)row) = make_float2(mean, rstd);
-    if (!p.y && !p.q.codes) continue;
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const uint32_t span = g * s.warps + in_row, c = span * kSpanCols + (WIDE ? 8 * l : l);
-      if (span >= s.spans) break;
-      float w[8], b[8];
-      take_weights<WIDE>(p.weight, p.w_dtype, p.w_wide, c, step, s.cols, 1.0f, w);
-      take_weights<WIDE>(p.bias, p.w_dtype, p.w_wide, c, step, s.cols, 0.0f, b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[g][i] = fmaf(v[g][i] * rstd, w[i], b[i]);
-      if (p.y)
+        for (int i = 0; i < 8; ++i) v[r][g][i] = fmaf(v[r][g][i] * rstd, w[g][i], b[g][i]);
+      if (p.y && here)
         with_type(p.y_dtype, [&](auto* type) {
           using U = std::remove_pointer_t<decltype(type)>;
-          put<WIDE>(static_cast<U*>(p.y) + (int64_t)row * p.ldy, c, step, here ? s.cols : 0, v[g]);
+#pragma unroll
+          for (int g = 0; g < G; ++g) at.put(static_cast<U*>(p.y) + (int64_t)row * p.ldy, g, v[r][g]);
         });
       if (p.q.codes) {  // (a row is a warp's at least)
-        if (!WIDE) mx::turn<false>(buffer[warp], v[g], lane);
-        const uint32_t c0 = span * kSpanCols + 8 * lane;
-        if (p.q.format == PVT_MX_E8M0_32)
-          mx::put_eight<PVT_MX_E8M0_32>(p.q, row, c0, here, row < p.padded, scale, v[g]);
-        else
-          mx::put_eight<PVT_MX_E4M3_16>(p.q, row, c0, here, row < p.padded, scale, v[g]);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if (!WIDE) mx::turn<false>(reinterpret_cast<float*>(ring + p.stages * stage) + at.warp * kTurn, v[r][g], at.lane);
+          const uint32_t c0 = at.part0 + (s.teams > 1 ? 0 : at.warp * kSpanCols) + g * at.next + 8 * at.lane;
+          if (p.q.format == PVT_MX_E8M0_32)
+            mx::put_eight<PVT_MX_E8M0_32>(p.q, (uint32_t)row, c0, here, row < p.padded, scale, v[r][g]);
+          else
+            mx::put_eight<PVT_MX_E4M3_16>(p.q, (uint32_t)row, c0, here, row < p.padded, scale, v[r][g]);
+        }
       }
     }
   }
+  copies_wait(false);
 }
 
-template <typename T, bool WIDE, int G>
-cudaError_t apply(ApplyParams p, uint32_t rows, uint32_t cols, int sm_count, cudaStream_t stream) {
-  p.s = shape_of(rows, cols, G, kTeamThreads, !p.q.codes);
-  const uint32_t threads = p.s.warps > 1 ? 32 * p.s.warps : kTeamThreads;
-  const uint64_t need = ((uint64_t)p.padded + p.s.teams - 1) / p.s.teams, most = (uint64_t)sm_count * 64;
-  return launch_dependent(norm_apply_kernel<T, WIDE, G>, (unsigned)(need < most ? need : most), threads, 0, stream, p);
+// shared memory of a block
+size_t ring_bytes(const ApplyParams& p, uint32_t rows, uint32_t stages, bool turned) {
+  return (size_t)stages * (p.residual ? 2 : 1) * rows * p.s.teams * p.image + (turned ? p.s.threads / 32 * kTurn * 4 : 0);
 }
 
-template <typename T, bool WIDE>
-cudaError_t apply(const ApplyParams& p, uint32_t rows, uint32_t cols, int sm_count, cudaStream_t stream) {
-  const uint32_t spans = (cols + kSpanCols - 1) / kSpanCols;
-  // few rows: as many warps to each as there are spans
-  if (spans == 1 || (spans <= 32 && rows <= (uint32_t)sm_count)) return apply<T, WIDE, 1>(p, rows, cols, sm_count, stream);
-  if (spans <= 16) return apply<T, WIDE, 2>(p, rows, cols, sm_count, stream);
-  if (spans <= 64) return apply<T, WIDE, 4>(p, rows, cols, sm_count, stream);
-  return apply<T, WIDE, 8>(p, rows, cols, sm_count, stream);
+template <typename T, int L, int G, int R>
+cudaError_t start(ApplyParams p, uint32_t stages, int sm_count, cudaStream_t stream) {
+  const Shape& s = p.s;
+  const size_t bytes = ring_bytes(p, R, stages, L == kRagged && p.q.codes);
+  int regs;
+  const cudaError_t e = set_up<norm_apply_kernel<T, L, G, R>>(&regs);
+  if (e != cudaSuccess) return e;
+  const uint64_t rows_each = (uint64_t)s.teams * R, need = (p.padded + rows_each - 1) / rows_each;
+  const uint64_t most = resident_sets(s, bytes, regs, sm_count);
+  p.sets = (uint32_t)(need < most ? need : most), p.stages = stages;
+  if (s.parts == 1) return launch_dependent(norm_apply_kernel<T, L, G, R>, p.sets, s.threads, bytes, stream, p);
+  return mma::launch_clusters(norm_apply_kernel<T, L, G, R>, p.sets * s.parts, s.parts, s.threads, bytes, stream, p);
+}
+
+template <typename T, int L, int G>
+cudaError_t start(const ApplyParams& p, int sm_count, cudaStream_t stream) {
+  const bool turned = L == kRagged && p.q.codes;
+  const uint32_t blocks = kMostThreads / p.s.threads;  // of an SM
+  // two rows at a time if all blocks have some, and rings of three stages, or of two
+  if constexpr (L != kRagged)
+    if (p.s.rows > 2 * (uint32_t)sm_count * blocks / p.s.parts * p.s.teams && ring_bytes(p, 2, 2, turned) * blocks <= kRingBytes)
+      return start<T, L, G, 2>(p, ring_bytes(p, 2, 3, turned) * blocks <= kRingBytes ? 3 : 2, sm_count, stream);
+  return start<T, L, G, 1>(p, ring_bytes(p, 1, 3, turned) * blocks <= kRingBytes ? 3 : 2, sm_count, stream);
+}
+
+template <typename T>
+cudaError_t apply(ApplyParams p, bool wide, uint32_t rows, uint32_t cols, int sm_count, cudaStream_t stream) {
+  for (uint32_t parts = 1;; parts *= 2) {
+    p.s = shape_of(rows, cols, wide && !p.q.codes, parts);
+    p.image = image_bytes(p.s, sizeof(T), wide);
+    if (ring_bytes(p, 1, 2, !wide && p.q.codes) <= kRingBytes) break;
+  }
+  const bool one = p.s.groups == 1;
+  switch (layout_of(p.s, wide)) {
+    case kRagged: return one ? start<T, kRagged, 1>(p, sm_count, stream) : start<T, kRagged, 2>(p, sm_count, stream);
+    case kWide: return one ? start<T, kWide, 1>(p, sm_count, stream) : start<T, kWide, 2>(p, sm_count, stream);
+    default: return one ? start<T, kExact, 1>(p, sm_count, stream) : start<T, kExact, 2>(p, sm_count, stream);
+  }
 }
 
 }  // namespace
@@ -152,15 +212,13 @@ cudaError_t launch_apply(const pvt_norm& n, void* total, int64_t ldt, void* y, i
     p.q = mx::held(*yq);
     p.padded = (uint32_t)((n.rows + kStrip - 1) / kStrip * kStrip);
   }
-  const size_t w_size = n.weight_dtype == PVT_F32 ? 4 : 2, y_size = y_dtype == PVT_F32 ? 4 : 2;
-  p.w_wide = rows_aligned(n.weight, 0, w_size) && rows_aligned(n.bias, 0, w_size);
+  const size_t y_size = y_dtype == PVT_F32 ? 4 : 2;
   timing_begin(kKernNorm, stream);
   const cudaError_t e = with_type(n.dtype, [&](auto* type) {
     using T = std::remove_pointer_t<decltype(type)>;
     const bool wide = rows_aligned(n.x, n.ldx, sizeof(T)) && rows_aligned(n.residual, n.ldr, sizeof(T)) &&
                       rows_aligned(total, ldt, sizeof(T)) && rows_aligned(y, ldy, y_size);
-    return wide ? apply<T, true>(p, (uint32_t)n.rows, (uint32_t)n.cols, sm_count, stream)
-                : apply<T, false>(p, (uint32_t)n.rows, (uint32_t)n.cols, sm_count, stream);
+    return apply<T>(p, wide, (uint32_t)n.rows, (uint32_t)n.cols, sm_count, stream);
   });
   timing_end(kKernNorm, stream);
   count_launches(1);
