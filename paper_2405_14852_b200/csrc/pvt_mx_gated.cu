@@ -43,30 +43,53 @@ struct Finish {
   uint32_t padded;     // rows that have scales
 };
 
-// f(a), and f'(a) if it is asked for
-template <bool SLOPE>
-__device__ __forceinline__ float activate(int32_t which, float a, float* slope) {
-  if (which == PVT_ACT_GELU) {  // f = a phi, phi the normal distribution's function
+// exp(-z) as a power of two (the product's rounding counts |z| times 2^-24), and 1 / v: the approximations, 2 units each
+__device__ __forceinline__ float exp_minus(float z) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(z * -1.44269504088896f));
+  return r;
+}
+__device__ __forceinline__ float inverse(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// f(a), and f'(a) if it is asked for.  (ACT is a constant: a branch for each element kept the elements of a thread from being worked at
+// side by side, 2048 x 4096 by 11008: gradients 297 us, of which the products are 60.)
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activate(float a, float* slope) {
+  if (ACT == PVT_ACT_GELU) {  // f = a phi, phi the normal distribution's function
     const float phi = 0.5f * erfcf(a * -0.70710678118654752f);
-    if (SLOPE) *slope = fmaf(a * 0.39894228040143268f, expf(-0.5f * a * a), phi);
+    if (SLOPE) *slope = fmaf(a * 0.39894228040143268f, exp_minus(0.5f * a * a), phi);
     return a * phi;
   }
   // f = a s(z), s the logistic function; z = a, or twice sqrt(2 / pi) (a + 0.044715 a^3): (1 + tanh(y)) / 2 = s(2 y)
   float z = a, dz = 1.0f;
-  if (which == PVT_ACT_GELU_TANH) {
+  if (ACT == PVT_ACT_GELU_TANH) {
     const float sq = a * a;
     z = a * fmaf(sq, 0.07135481282942f, 1.59576912160573f);
     if (SLOPE) dz = fmaf(sq, 0.21406443848826f, 1.59576912160573f);
   }
-  const float s = __fdividef(1.0f, 1.0f + expf(-z));  // (0 where the exponential is beyond 2^126)
+  const float s = inverse(1.0f + exp_minus(z));  // (0 where the exponential is infinite)
   if (SLOPE) *slope = fmaf(a * dz, s * (1.0f - s), s);
   return a * s;
 }
+// calls f with the activation as a constant
+template <typename F>
+__device__ __forceinline__ void with_activation(int32_t which, F f) {
+  if (which == PVT_ACT_SILU)
+    f(std::integral_constant<int, PVT_ACT_SILU>{});
+  else if (which == PVT_ACT_GELU)
+    f(std::integral_constant<int, PVT_ACT_GELU>{});
+  else
+    f(std::integral_constant<int, PVT_ACT_GELU_TANH>{});
+}
 
 // dgate and dup of one element, rounded
-__device__ __forceinline__ __nv_bfloat162 gradients(int32_t which, float a, float b, float dh) {
+template <int ACT>
+__device__ __forceinline__ __nv_bfloat162 gradients(float a, float b, float dh) {
   float slope;
-  const float f = activate<true>(which, a, &slope);
+  const float f = activate<ACT, true>(a, &slope);
   return __floats2bfloat162_rn(dh * b * slope, dh * f);
 }
 
@@ -83,17 +106,21 @@ __device__ __forceinline__ void finish_token(const Finish& p, const TensorScale&
       float v[4];
 #pragma unroll
       for (uint32_t i = 0; i < 4; ++i) v[i] = col0 + i * 32 + lane < p.n ? widen<T>(dh[i * 32]) : 0.0f;
+      __nv_bfloat162 d[4];
+      with_activation(p.activation, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = gradients<decltype(act)::value>(a[i], b[i], v[i]);
+      });
 #pragma unroll
       for (uint32_t i = 0; i < 4; ++i)
-        if (col0 + i * 32 + lane < p.n) {
-          const __nv_bfloat162 d = gradients(p.activation, a[i], b[i], v[i]);
-          p.dgate[at + i * 32] = d.x, p.dup[at + i * 32] = d.y;
-        }
+        if (col0 + i * 32 + lane < p.n) p.dgate[at + i * 32] = d[i].x, p.dup[at + i * 32] = d[i].y;
     });
   } else {
     float h[4];
+    with_activation(p.activation, [&](auto act) {
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) h[i] = activate<false>(p.activation, a[i], nullptr) * b[i];
+      for (int i = 0; i < 4; ++i) h[i] = activate<decltype(act)::value, false>(a[i], nullptr) * b[i];
+    });
     if (p.h)
       with_type(p.dtype, [&](auto* type) {
         using T = std::remove_pointer_t<decltype(type)>;
@@ -284,8 +311,9 @@ __global__ void __launch_bounds__(kFewThreads)
 }
 
 // ---- pairs of blocks -------------------------------------------------------------------------------------------
-constexpr uint32_t kRound = 32;  // tokens of a warp's exchange at a time
-constexpr uint32_t kExchange = kRound * 32 * 4;  // bytes of it
+constexpr uint32_t kRound = 32;               // tokens of a warp's exchange at a time
+constexpr uint32_t kHalf = kRound * 32 * 4;   // bytes of what a warp gets, and of its own beside it
+constexpr uint32_t kExchange = 2 * kHalf;
 
 struct PairShared {
   alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
@@ -319,15 +347,14 @@ struct GatedSizes : PairSizes<FMT, N> {
   static_assert(N * kTileW * 4 <= kExchangeAt, "the partial sums fit the stages");
 };
 
-// what a warp's 32 lanes (outputs) have of 32 tokens, into 4 bits: v[j] of token j; buffer: the warp's exchange
+// asks for the line of an address to be brought into the L2
+__device__ __forceinline__ void ask_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
+
+// what a warp's 32 lanes (outputs) have of 32 tokens, into 4 bits; buffer: that of output i of token j in place 32 j + (i ^ j)
 template <int FMT>
-__device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t, uint32_t token0, uint32_t col0, const uint32_t* v, float* buffer) {
+__device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t, uint32_t token0, uint32_t col0, const float* buffer) {
   constexpr int BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16, N = 32 / BLOCK;
   const uint32_t lane = threadIdx.x & 31;
-  __syncwarp();
-#pragma unroll
-  for (uint32_t j = 0; j < 32; ++j) buffer[j * 32 + (lane ^ j)] = col0 + lane < p.n ? __uint_as_float(v[j]) : 0.0f;
-  __syncwarp();
   const uint32_t token = token0 + lane;
   float e[32];
 #pragma unroll
@@ -360,6 +387,83 @@ __device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t
 #pragma unroll
     for (uint32_t i = 0; i < 16; ++i)
       if (2 * i < p.n - col0) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+// A warp's 32 outputs of 32 tokens: its own sums (of wg in the first block, of wu in the second) and those it got, four tokens of a lane
+// together, eight at a time.  wait(): whether these are there; done(): they have been read.
+template <int FMT, bool GRAD, typename Wait, typename Done>
+__device__ __forceinline__ void finish_round(const Finish& p, const Factors& gate, const Factors& up, const TensorScale& t, uint32_t row0,
+                                             uint32_t col0, uint32_t rank, const float4* got, uint4* own, Wait wait, Done done) {
+  constexpr int E = 8;
+  const uint32_t lane = threadIdx.x & 31, col = col0 + lane;
+  const bool has_col = col < p.n;
+  const uint32_t rows = has_col && row0 < p.tokens ? min(kRound, p.tokens - row0) : 0;  // that the lane has anything of
+  float dh[E];
+  auto ask = [&](uint32_t j) {
+    with_type(p.dtype, [&](auto* type) {
+      using T = std::remove_pointer_t<decltype(type)>;
+      const T* const from = static_cast<const T*>(p.dh) + (int64_t)(row0 + j) * p.ldh + col;
+#pragma unroll
+      for (uint32_t i = 0; i < E; ++i) dh[i] = j + i < rows ? widen<T>(from[i * p.ldh]) : 0.0f;
+    });
+  };
+  if (GRAD) ask(0);
+  if (!wait()) return;
+  with_activation(p.activation, [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+#pragma unroll 1
+    for (uint32_t j = 0; j < kRound; j += E) {
+      float a[E], b[E];
+#pragma unroll
+      for (uint32_t k = 0; k < E / 4; ++k) {
+        const float4 theirs = got[(j / 4 + k) * 32 + lane];
+        const uint4 mine = own[(j / 4 + k) * 32 + lane];
+        const float m[4] = {__uint_as_float(mine.x), __uint_as_float(mine.y), __uint_as_float(mine.z), __uint_as_float(mine.w)};
+        const float o[4] = {theirs.x, theirs.y, theirs.z, theirs.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[4 * k + i] = gate(rank ? o[i] : m[i]), b[4 * k + i] = up(rank ? m[i] : o[i]);
+      }
+      if (GRAD) {
+        float d[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) d[i] = dh[i];
+        if (j + E < kRound) ask(j + E);
+        __nv_bfloat162 g[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) g[i] = gradients<ACT>(a[i], b[i], d[i]);
+        __nv_bfloat16 *to_gate = p.dgate + (int64_t)(row0 + j) * p.ldd + col, *to_up = p.dup + (int64_t)(row0 + j) * p.ldd + col;
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) {
+          if (j + i < rows) *to_gate = g[i].x, *to_up = g[i].y;
+          to_gate += p.ldd, to_up += p.ldd;
+        }
+      } else {
+        float h[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) h[i] = activate<ACT, false>(a[i], nullptr) * b[i];
+        if (p.h)
+          with_type(p.dtype, [&](auto* type) {
+            using T = std::remove_pointer_t<decltype(type)>;
+            T* to = static_cast<T*>(p.h) + (int64_t)(row0 + j) * p.ldh + col;
+#pragma unroll
+            for (uint32_t i = 0; i < E; ++i) {
+              if (j + i < rows) *to = narrow<T>(h[i]);
+              to += p.ldh;
+            }
+          });
+        if (p.q.codes) {  // turned, in the place of these tokens' sums
+          __syncwarp();
+#pragma unroll
+          for (uint32_t i = 0; i < E; ++i) reinterpret_cast<float*>(own)[(j + i) * 32 + (lane ^ (j + i))] = has_col ? h[i] : 0.0f;
+        }
+      }
+    }
+  });
+  done();
+  if (!GRAD && p.q.codes) {
+    put_tokens<FMT>(p, t, row0, col0, reinterpret_cast<const float*>(own));
+    __syncwarp();
   }
 }
 
@@ -480,10 +584,19 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t exchange = base + S::kExchangeAt + warp * kExchange, other = cluster_address(exchange, in_cluster ^ 1);
     const uint32_t other_got = cluster_address(smem_u32(&sm.got[warp]), in_cluster ^ 1);
     const uint32_t other_room = cluster_address(smem_u32(&sm.room[warp]), in_cluster ^ 1);
-    float* const buffer = reinterpret_cast<float*>(mem + S::kExchangeAt + warp * kExchange);
+    const float4* const got = reinterpret_cast<const float4*>(mem + S::kExchangeAt + warp * kExchange);
+    uint4* const own = reinterpret_cast<uint4*>(mem + S::kExchangeAt + warp * kExchange + kHalf);
     uint32_t n = 0, turn = 0;  // tiles, exchanges
     bool ok = true;
     for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride, ++n) {
+      const uint32_t col0 = tile / p.x_tiles * kTileW + quarter * 32, row = tile % p.x_tiles * N + half * HALF + rank * MINE;
+      if (GRAD && p.split == 1)  // what will be needed of dh, on its way to the L2 beside the products
+        for (uint32_t j = lane; j < MINE; j += 32)
+          if (row + j < f.tokens && col0 < f.n) {
+            const uint32_t size = f.dtype == PVT_F32 ? 4 : 2;
+            const char* const at = static_cast<const char*>(f.dh) + ((int64_t)(row + j) * f.ldh + col0) * size;
+            ask_l2(at), ask_l2(at + (min(32u, f.n - col0) - 1) * size);
+          }
       ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
       if (!ok) break;
       tc_fence_after();
@@ -505,86 +618,28 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         break;
       }
-      const uint32_t col0 = tile / p.x_tiles * kTileW + quarter * 32, col = col0 + lane;
-      const uint32_t row = tile % p.x_tiles * N + half * HALF + rank * MINE;
-      const bool has_col = col < f.n;
 #pragma unroll
       for (uint32_t r = 0; r < MINE; r += kRound, ++turn) {
         if (turn > 0) ok = wait<true>(smem_u32(&sm.room[warp]), (turn - 1) & 1, abandoned, p.status, p.max_spins);
         if (!ok) break;
+        // four tokens of a lane together
 #pragma unroll
         for (uint32_t j = 0; j < kRound; j += 4)
           asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(other + (j / 4 * 32 + lane) * 16), "r"(v[MINE + r + j]),
                        "r"(v[MINE + r + j + 1]), "r"(v[MINE + r + j + 2]), "r"(v[MINE + r + j + 3])
                        : "memory");
         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(other_got) : "memory");
-        float dh[kRound];
-        if (GRAD)
-          with_type(f.dtype, [&](auto* type) {
-            using T = std::remove_pointer_t<decltype(type)>;
-            const T* from = static_cast<const T*>(f.dh) + (int64_t)(row + r) * f.ldh + col;
 #pragma unroll
-            for (uint32_t j = 0; j < kRound; ++j) {
-              dh[j] = has_col && row + r + j < f.tokens ? widen<T>(*from) : 0.0f;
-              from += f.ldh;
-            }
-          });
-        ok = wait<true>(smem_u32(&sm.got[warp]), turn & 1, abandoned, p.status, p.max_spins);
+        for (uint32_t j = 0; j < kRound; j += 4) own[j / 4 * 32 + lane] = make_uint4(v[r + j], v[r + j + 1], v[r + j + 2], v[r + j + 3]);
+        finish_round<FMT, GRAD>(f, gate, up, t, row + r, col0, rank, got, own, [&] {
+          return ok = wait<true>(smem_u32(&sm.got[warp]), turn & 1, abandoned, p.status, p.max_spins);
+        }, [&] {
+          __syncwarp();
+          if (lane == 0) cluster_arrive(other_room);
+          __syncwarp();
+        });
         if (!ok) break;
-#pragma unroll
-        for (uint32_t j = 0; j < kRound; j += 4) {
-          const float4 theirs = *reinterpret_cast<const float4*>(buffer + (j / 4 * 32 + lane) * 4);
-          const float o[4] = {theirs.x, theirs.y, theirs.z, theirs.w};
-#pragma unroll
-          for (uint32_t i = 0; i < 4; ++i) {
-            const float own = __uint_as_float(v[r + j + i]);
-            const float a = gate(rank ? o[i] : own), b = up(rank ? own : o[i]);
-            if (GRAD) {
-              const __nv_bfloat162 d = gradients(f.activation, a, b, dh[j + i]);
-              v[r + j + i] = *reinterpret_cast<const uint32_t*>(&d);
-            } else {
-              v[r + j + i] = __float_as_uint(activate<false>(f.activation, a, nullptr) * b);
-            }
-          }
-        }
-        __syncwarp();
-        // (the last exchange's shared memory is still wanted for 4-bit results)
-        if (lane == 0 && r + kRound < MINE) cluster_arrive(other_room);
-        __syncwarp();
       }
-      if (!ok) break;
-      if (!GRAD && f.q.codes) {
-#pragma unroll
-        for (uint32_t r = 0; r < MINE; r += 32) put_tokens<FMT>(f, t, row + r, col0, v + r, buffer);
-      }
-      __syncwarp();
-      if (lane == 0) cluster_arrive(other_room);
-      __syncwarp();
-      if (has_col && row < f.tokens) {
-        const uint32_t rows = f.tokens - row;
-        if (GRAD) {
-          __nv_bfloat16 *to_gate = f.dgate + (int64_t)row * f.ldd + col, *to_up = f.dup + (int64_t)row * f.ldd + col;
-#pragma unroll
-          for (uint32_t j = 0; j < MINE; ++j) {
-            if (j < rows) {
-              const __nv_bfloat162 d = *reinterpret_cast<const __nv_bfloat162*>(&v[j]);
-              *to_gate = d.x, *to_up = d.y;
-            }
-            to_gate += f.ldd, to_up += f.ldd;
-          }
-        } else if (f.h) {
-          with_type(f.dtype, [&](auto* type) {
-            using T = std::remove_pointer_t<decltype(type)>;
-            T* to = static_cast<T*>(f.h) + (int64_t)row * f.ldh + col;
-#pragma unroll
-            for (uint32_t j = 0; j < MINE; ++j) {
-              if (j < rows) *to = narrow<T>(__uint_as_float(v[j]));
-              to += f.ldh;
-            }
-          });
-        }
-      }
-      __syncwarp();
     }
   }
   __syncthreads();
