@@ -8,9 +8,9 @@
 //
 // From 17 tokens on: the product's pairs of blocks, 256 rows of weights by 256 (or 128) of x to a tile; but the first block's 128 rows
 // are wg's and the second's the same ones of wu.  The main loop, its traffic (32 KB of codes a step and SM) and its rate are the product's.
-// What is needed together is then in two SMs: a thread reads its sums of N / 2 tokens out of tensor memory, which is free
-// for the next tile at once, keeps those of one half of them, and sends the others to the same thread of the other block, 32 tokens
-// at a time, through shared memory.  The exchange, activations and stores go on beside the next tile's products.
+// What is needed together is then in two SMs: a thread reads its sums of N / 4 tokens out of tensor memory, which is free
+// for the next tile at once, keeps those of one half of them, and sends the others to the same thread of the other block
+// through shared memory.  The exchange, activations and stores go on beside the next tile's products.
 //
 // 4-bit results: 32 outputs of a token are one warp's lanes.  They are turned in the shared memory that the exchange has left, to one
 // token to a lane, and quantised there.
@@ -311,17 +311,18 @@ __global__ void __launch_bounds__(kFewThreads)
 }
 
 // ---- pairs of blocks -------------------------------------------------------------------------------------------
-constexpr uint32_t kRound = 32;               // tokens of a warp's exchange at a time
-constexpr uint32_t kHalf = kRound * 32 * 4;   // bytes of what a warp gets, and of its own beside it
-constexpr uint32_t kExchange = 2 * kHalf;
+// (sixteen warps finish: with eight there were two to a scheduler, and most of the time neither could go on: gradients of 2048 x 4096 by
+// 11008 159 us)
+constexpr int kReaders = 16, kCopyWarp = kReaders, kMmaWarp = kCopyWarp + kPairCopyWarps;
+constexpr int kThreads = (kMmaWarp + 1) * 32;
 
 struct PairShared {
   alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
   uint64_t empty[kPairStages];            // of each
   uint64_t sums_full;                     // of each
   uint64_t sums_empty;                    // of the first: an arrival per reading warp of both
-  uint64_t got[kPairReaders];             // of each: the other block's warp has written its sums, an arrival per lane
-  uint64_t room[kPairReaders];            // of each: the other block's warp has read them
+  uint64_t got[kReaders];             // of each: the other block's warp has written its sums, an arrival per lane
+  uint64_t room[kReaders];            // of each: the other block's warp has read them
   uint64_t spare;
   uint32_t tmem, abandoned;
 };
@@ -339,10 +340,12 @@ struct PairParams {
 template <int FMT, uint32_t N>
 struct GatedSizes : PairSizes<FMT, N> {
   using P = PairSizes<FMT, N>;
-  static constexpr uint32_t kRoom = (225 * 1024 - kPairReaders * kExchange) / P::kStageAligned;
+  static constexpr uint32_t kMine = N / 8;                 // tokens that a warp finishes, and that it sends
+  static constexpr uint32_t kExchange = kMine * 32 * 4;    // bytes that it gets
+  static constexpr uint32_t kRoom = (225 * 1024 - kReaders * kExchange) / P::kStageAligned;
   static constexpr uint32_t kStages = kRoom < P::kStages ? kRoom : P::kStages;
   static constexpr uint32_t kExchangeAt = kStages * P::kStageAligned;
-  static constexpr size_t kBytes = kExchangeAt + kPairReaders * kExchange + 1024;
+  static constexpr size_t kBytes = kExchangeAt + kReaders * kExchange + 1024;
   static_assert(kBytes + 1024 <= 227 * 1024, "a block's shared memory");
   static_assert(N * kTileW * 4 <= kExchangeAt, "the partial sums fit the stages");
 };
@@ -350,12 +353,13 @@ struct GatedSizes : PairSizes<FMT, N> {
 // asks for the line of an address to be brought into the L2
 __device__ __forceinline__ void ask_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
 
-// what a warp's 32 lanes (outputs) have of 32 tokens, into 4 bits; buffer: that of output i of token j in place 32 j + (i ^ j)
-template <int FMT>
+// what a warp's 32 lanes (outputs) have of M tokens, into 4 bits; buffer: that of output i of token j in place 32 j + (i ^ j)
+template <int FMT, uint32_t M>
 __device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t, uint32_t token0, uint32_t col0, const float* buffer) {
   constexpr int BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16, N = 32 / BLOCK;
   const uint32_t lane = threadIdx.x & 31;
   const uint32_t token = token0 + lane;
+  if (lane >= M) return;
   float e[32];
 #pragma unroll
   for (uint32_t i = 0; i < 32; ++i) e[i] = buffer[lane * 32 + (i ^ lane)];
@@ -390,48 +394,52 @@ __device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t
   }
 }
 
-// A warp's 32 outputs of 32 tokens: its own sums (of wg in the first block, of wu in the second) and those it got, four tokens of a lane
-// together, eight at a time.  wait(): whether these are there; done(): they have been read.
-template <int FMT, bool GRAD, typename Wait, typename Done>
-__device__ __forceinline__ void finish_round(const Finish& p, const Factors& gate, const Factors& up, const TensorScale& t, uint32_t row0,
-                                             uint32_t col0, uint32_t rank, const float4* got, uint4* own, Wait wait, Done done) {
-  constexpr int E = 8;
+// A warp's 32 outputs of M tokens: its own sums v (of wg in the first block, of wu in the second) and those it gets from the other block's
+// warp, four tokens of a lane together.  wait(): whether these are there.
+template <int FMT, bool GRAD, uint32_t M, typename Wait>
+__device__ __forceinline__ void finish_tokens(const Finish& p, const Factors& gate, const Factors& up, const TensorScale& t, uint32_t row0,
+                                              uint32_t col0, uint32_t rank, const uint32_t* v, float* got, Wait wait) {
+  constexpr uint32_t E = 8;  // elements at a time
   const uint32_t lane = threadIdx.x & 31, col = col0 + lane;
   const bool has_col = col < p.n;
-  const uint32_t rows = has_col && row0 < p.tokens ? min(kRound, p.tokens - row0) : 0;  // that the lane has anything of
-  float dh[E];
-  auto ask = [&](uint32_t j) {
-    with_type(p.dtype, [&](auto* type) {
-      using T = std::remove_pointer_t<decltype(type)>;
-      const T* const from = static_cast<const T*>(p.dh) + (int64_t)(row0 + j) * p.ldh + col;
+  const uint32_t rows = has_col && row0 < p.tokens ? min(M, p.tokens - row0) : 0;  // that the lane has anything of
+  uint32_t dh[M];  // as it lies in memory; all under way while the other block's sums are
+  if (GRAD) {
+    if (p.dtype == PVT_F32) {
+      const uint32_t* from = static_cast<const uint32_t*>(p.dh) + (int64_t)row0 * p.ldh + col;
 #pragma unroll
-      for (uint32_t i = 0; i < E; ++i) dh[i] = j + i < rows ? widen<T>(from[i * p.ldh]) : 0.0f;
-    });
-  };
-  if (GRAD) ask(0);
+      for (uint32_t j = 0; j < M; ++j, from += p.ldh) dh[j] = j < rows ? *from : 0;
+    } else {
+      const uint16_t* from = static_cast<const uint16_t*>(p.dh) + (int64_t)row0 * p.ldh + col;
+#pragma unroll
+      for (uint32_t j = 0; j < M; ++j, from += p.ldh) dh[j] = j < rows ? *from : 0;
+    }
+  }
   if (!wait()) return;
   with_activation(p.activation, [&](auto act) {
     constexpr int ACT = decltype(act)::value;
-#pragma unroll 1
-    for (uint32_t j = 0; j < kRound; j += E) {
+#pragma unroll
+    for (uint32_t j = 0; j < M; j += E) {
       float a[E], b[E];
 #pragma unroll
-      for (uint32_t k = 0; k < E / 4; ++k) {
-        const float4 theirs = got[(j / 4 + k) * 32 + lane];
-        const uint4 mine = own[(j / 4 + k) * 32 + lane];
-        const float m[4] = {__uint_as_float(mine.x), __uint_as_float(mine.y), __uint_as_float(mine.z), __uint_as_float(mine.w)};
+      for (uint32_t k = 0; k < E; k += 4) {
+        const float4 theirs = reinterpret_cast<const float4*>(got)[(j + k) / 4 * 32 + lane];
         const float o[4] = {theirs.x, theirs.y, theirs.z, theirs.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[4 * k + i] = gate(rank ? o[i] : m[i]), b[4 * k + i] = up(rank ? m[i] : o[i]);
+        for (uint32_t i = 0; i < 4; ++i) {
+          const float mine = __uint_as_float(v[j + k + i]);
+          a[k + i] = gate(rank ? o[i] : mine), b[k + i] = up(rank ? mine : o[i]);
+        }
       }
       if (GRAD) {
         float d[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) d[i] = dh[i];
-        if (j + E < kRound) ask(j + E);
+        for (uint32_t i = 0; i < E; ++i)
+          d[i] = p.dtype == PVT_F16 ? __half2float(__ushort_as_half((unsigned short)dh[j + i]))
+                                    : __uint_as_float(p.dtype == PVT_F32 ? dh[j + i] : dh[j + i] << 16);
         __nv_bfloat162 g[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) g[i] = gradients<ACT>(a[i], b[i], d[i]);
+        for (uint32_t i = 0; i < E; ++i) g[i] = gradients<ACT>(a[i], b[i], d[i]);
         __nv_bfloat16 *to_gate = p.dgate + (int64_t)(row0 + j) * p.ldd + col, *to_up = p.dup + (int64_t)(row0 + j) * p.ldd + col;
 #pragma unroll
         for (uint32_t i = 0; i < E; ++i) {
@@ -441,7 +449,7 @@ __device__ __forceinline__ void finish_round(const Finish& p, const Factors& gat
       } else {
         float h[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) h[i] = activate<ACT, false>(a[i], nullptr) * b[i];
+        for (uint32_t i = 0; i < E; ++i) h[i] = activate<ACT, false>(a[i], nullptr) * b[i];
         if (p.h)
           with_type(p.dtype, [&](auto* type) {
             using T = std::remove_pointer_t<decltype(type)>;
@@ -452,29 +460,29 @@ __device__ __forceinline__ void finish_round(const Finish& p, const Factors& gat
               to += p.ldh;
             }
           });
-        if (p.q.codes) {  // turned, in the place of these tokens' sums
+        if (p.q.codes) {  // turned, in the place of the sums that were got
           __syncwarp();
 #pragma unroll
-          for (uint32_t i = 0; i < E; ++i) reinterpret_cast<float*>(own)[(j + i) * 32 + (lane ^ (j + i))] = has_col ? h[i] : 0.0f;
+          for (uint32_t i = 0; i < E; ++i) got[(j + i) * 32 + (lane ^ (j + i))] = has_col ? h[i] : 0.0f;
         }
       }
     }
   });
-  done();
+  __syncwarp();
   if (!GRAD && p.q.codes) {
-    put_tokens<FMT>(p, t, row0, col0, reinterpret_cast<const float*>(own));
+    put_tokens<FMT, M>(p, t, row0, col0, got);
     __syncwarp();
   }
 }
 
 template <int FMT, uint32_t N, bool GRAD>
-__global__ void __launch_bounds__(kPairThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
     mx_gated_pair_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map,
                          const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap gate_s_map,
                          const __grid_constant__ CUtensorMap up_s_map, const __grid_constant__ CUtensorMap x_s_map,
                          const __grid_constant__ PairParams p) {
   using S = GatedSizes<FMT, N>;
-  constexpr uint32_t KT = S::KT, STAGES = S::kStages, HALF = N / 2, MINE = N / 4;
+  constexpr uint32_t KT = S::KT, STAGES = S::kStages, HALF = N / 4, MINE = S::kMine;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ PairShared sm;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -486,15 +494,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       mbar_init(smem_u32(&sm.empty[s]), 1);
     }
     mbar_init(smem_u32(&sm.sums_full), 1);
-    mbar_init(smem_u32(&sm.sums_empty), 2 * kPairReaders);
-    for (uint32_t s = 0; s < kPairReaders; ++s) {
+    mbar_init(smem_u32(&sm.sums_empty), 2 * kReaders);
+    for (uint32_t s = 0; s < kReaders; ++s) {
       mbar_init(smem_u32(&sm.got[s]), 32);
       mbar_init(smem_u32(&sm.room[s]), 1);
     }
     mbar_init(smem_u32(&sm.spare), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kPairMmaWarp) {
+  if (warp == kMmaWarp) {
     tmem_alloc<2>(smem_u32(&sm.tmem), 512);
     tmem_relinquish<2>();
   }
@@ -514,8 +522,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const uint32_t first = p.steps * share / p.split, steps = p.steps * (share + 1) / p.split - first;  // (steps < 2^24, share < 4)
   const Finish& f = p.f;
 
-  if (warp >= kPairCopyWarp && warp < kPairMmaWarp) {
-    const bool of_w = warp == kPairCopyWarp;  // one warp for the weights' codes and scales, one for x's
+  if (warp >= kCopyWarp && warp < kMmaWarp) {
+    const bool of_w = warp == kCopyWarp;  // one warp for the weights' codes and scales, one for x's
     const CUtensorMap* const w_map = rank ? &up_map : &gate_map;
     const CUtensorMap* const w_s_map = rank ? &up_s_map : &gate_s_map;
     uint32_t i = 0;
@@ -544,7 +552,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     if (*abandoned && rank == 0)  // what was issued lands before the blocks' memory is another's
       for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
         if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
-  } else if (warp == kPairMmaWarp) {
+  } else if (warp == kMmaWarp) {
     if (rank == 0) {
       // e2m1 both, N, M = 256, type of the scales
       constexpr uint32_t idesc =
@@ -578,33 +586,36 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const float x_ts = f.x_ts ? *f.x_ts : 1.0f;
     const Factors gate(f.gate_ts ? *f.gate_ts : 1.0f, x_ts), up(f.up_ts ? *f.up_ts : 1.0f, x_ts);
     const TensorScale t(f.q.tensor_scale);
-    const uint32_t quarter = warp % 4, half = warp / 4;
+    const uint32_t quarter = warp % 4, part = warp / 4;  // of the outputs, of the tokens
     const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), lead);
     // of the other block: where this warp's sums go, and the barriers of the same warp
-    const uint32_t exchange = base + S::kExchangeAt + warp * kExchange, other = cluster_address(exchange, in_cluster ^ 1);
+    const uint32_t exchange = base + S::kExchangeAt + warp * S::kExchange, other = cluster_address(exchange, in_cluster ^ 1);
     const uint32_t other_got = cluster_address(smem_u32(&sm.got[warp]), in_cluster ^ 1);
     const uint32_t other_room = cluster_address(smem_u32(&sm.room[warp]), in_cluster ^ 1);
-    const float4* const got = reinterpret_cast<const float4*>(mem + S::kExchangeAt + warp * kExchange);
-    uint4* const own = reinterpret_cast<uint4*>(mem + S::kExchangeAt + warp * kExchange + kHalf);
-    uint32_t n = 0, turn = 0;  // tiles, exchanges
+    float* const got = reinterpret_cast<float*>(mem + S::kExchangeAt + warp * S::kExchange);
+    uint32_t n = 0;
     bool ok = true;
     for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride, ++n) {
-      const uint32_t col0 = tile / p.x_tiles * kTileW + quarter * 32, row = tile % p.x_tiles * N + half * HALF + rank * MINE;
-      if (GRAD && p.split == 1)  // what will be needed of dh, on its way to the L2 beside the products
-        for (uint32_t j = lane; j < MINE; j += 32)
-          if (row + j < f.tokens && col0 < f.n) {
-            const uint32_t size = f.dtype == PVT_F32 ? 4 : 2;
-            const char* const at = static_cast<const char*>(f.dh) + ((int64_t)(row + j) * f.ldh + col0) * size;
-            ask_l2(at), ask_l2(at + (min(32u, f.n - col0) - 1) * size);
-          }
+      const uint32_t col0 = tile / p.x_tiles * kTileW + quarter * 32, row = tile % p.x_tiles * N + part * HALF + rank * MINE;
+      if (GRAD && p.split == 1 && lane < MINE && row + lane < f.tokens && col0 < f.n) {
+        // what will be needed of dh, on its way to the L2 beside the products
+        const uint32_t size = f.dtype == PVT_F32 ? 4 : 2;
+        const char* const at = static_cast<const char*>(f.dh) + ((int64_t)(row + lane) * f.ldh + col0) * size;
+        ask_l2(at), ask_l2(at + (min(32u, f.n - col0) - 1) * size);
+      }
       ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
       if (!ok) break;
       tc_fence_after();
       // the tokens that this block finishes, then those that the other one does
       uint32_t v[HALF];
 #pragma unroll
-      for (uint32_t j = 0; j < HALF; j += 32)
-        tmem_ld32(tmem + (quarter << 21) + half * HALF + ((j < MINE) == (rank == 0) ? 0 : MINE) + j % MINE, v + j);
+      for (uint32_t j = 0; j < HALF; j += MINE) {
+        const uint32_t from = tmem + (quarter << 21) + part * HALF + ((j == 0) == (rank == 0) ? 0 : MINE);
+        if (MINE == 32)
+          tmem_ld32(from, v + j);
+        else
+          tmem_ld16(from, v + j);
+      }
       tmem_ld_wait<(int)HALF>(v);
       tc_fence_before();
       __syncwarp();
@@ -613,33 +624,25 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       if (p.split > 1) {  // the products are done: the stages hold the partial sums
 #pragma unroll
         for (uint32_t j = 0; j < HALF; ++j) {
-          const uint32_t token = half * HALF + ((j < MINE) == (rank == 0) ? 0 : MINE) + j % MINE;
+          const uint32_t token = part * HALF + ((j < MINE) == (rank == 0) ? 0 : MINE) + j % MINE;
           reinterpret_cast<float*>(mem)[token * kTileW + quarter * 32 + lane] = __uint_as_float(v[j]);
         }
         break;
       }
+      if (n > 0) ok = wait<true>(smem_u32(&sm.room[warp]), (n - 1) & 1, abandoned, p.status, p.max_spins);
+      if (!ok) break;
+      // four tokens of a lane together
 #pragma unroll
-      for (uint32_t r = 0; r < MINE; r += kRound, ++turn) {
-        if (turn > 0) ok = wait<true>(smem_u32(&sm.room[warp]), (turn - 1) & 1, abandoned, p.status, p.max_spins);
-        if (!ok) break;
-        // four tokens of a lane together
-#pragma unroll
-        for (uint32_t j = 0; j < kRound; j += 4)
-          asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(other + (j / 4 * 32 + lane) * 16), "r"(v[MINE + r + j]),
-                       "r"(v[MINE + r + j + 1]), "r"(v[MINE + r + j + 2]), "r"(v[MINE + r + j + 3])
-                       : "memory");
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(other_got) : "memory");
-#pragma unroll
-        for (uint32_t j = 0; j < kRound; j += 4) own[j / 4 * 32 + lane] = make_uint4(v[r + j], v[r + j + 1], v[r + j + 2], v[r + j + 3]);
-        finish_round<FMT, GRAD>(f, gate, up, t, row + r, col0, rank, got, own, [&] {
-          return ok = wait<true>(smem_u32(&sm.got[warp]), turn & 1, abandoned, p.status, p.max_spins);
-        }, [&] {
-          __syncwarp();
-          if (lane == 0) cluster_arrive(other_room);
-          __syncwarp();
-        });
-        if (!ok) break;
-      }
+      for (uint32_t j = 0; j < MINE; j += 4)
+        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(other + (j / 4 * 32 + lane) * 16), "r"(v[MINE + j]),
+                     "r"(v[MINE + j + 1]), "r"(v[MINE + j + 2]), "r"(v[MINE + j + 3])
+                     : "memory");
+      asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(other_got) : "memory");
+      finish_tokens<FMT, GRAD, MINE>(f, gate, up, t, row, col0, rank, v, got, [&] {
+        return ok = wait<true>(smem_u32(&sm.got[warp]), n & 1, abandoned, p.status, p.max_spins);
+      });
+      if (lane == 0) cluster_arrive(other_room);
+      __syncwarp();
     }
   }
   __syncthreads();
@@ -653,7 +656,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const TensorScale t(f.q.tensor_scale);
       float* const scratch = reinterpret_cast<float*>(mem + S::kExchangeAt) + warp * 128;
       const uint32_t tokens = min(N, f.tokens - row0);
-      for (uint32_t j = in_cluster + warp * blocks; j < tokens; j += kPairThreads / 32 * blocks) {
+      for (uint32_t j = in_cluster + warp * blocks; j < tokens; j += kThreads / 32 * blocks) {
         float v[2][4][4], a[4], b[4];  // (all under way at once: a load from another block takes a thousand cycles)
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
@@ -671,11 +674,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         finish_token<FMT, GRAD>(f, t, row0 + j, col0, a, b, scratch);
       }
       if (!GRAD && f.q.codes && in_cluster == 0)
-        clear_scales<FMT>(f, max(row0, f.tokens), min(row0 + N, f.padded), col0, tid, kPairThreads);
+        clear_scales<FMT>(f, max(row0, f.tokens), min(row0 + N, f.padded), col0, tid, kThreads);
     }
     cluster_sync();  // nor while another reads its partial sums
   }
-  if (warp == kPairMmaWarp) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc<2>(tmem, 512);
   }
@@ -706,7 +709,7 @@ cudaError_t gated_pairs(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, con
   if (e != cudaSuccess) return e;
   p.split = pairs_per_tile(p.tiles, p.steps, sm_count);
   const uint32_t pairs = p.split > 1 ? p.tiles * p.split : p.tiles < (uint32_t)sm_count / 2 ? p.tiles : (uint32_t)sm_count / 2;
-  return launch_clusters(mx_gated_pair_kernel<FMT, N, GRAD>, 2 * pairs, 2 * p.split, kPairThreads, S::kBytes, stream, maps[0], maps[1],
+  return launch_clusters(mx_gated_pair_kernel<FMT, N, GRAD>, 2 * pairs, 2 * p.split, kThreads, S::kBytes, stream, maps[0], maps[1],
                          maps[2], maps[3], maps[4], maps[5], p);
 }
 
