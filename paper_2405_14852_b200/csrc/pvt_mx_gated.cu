@@ -35,6 +35,7 @@ struct Finish {
   const void* dh;
   __nv_bfloat16 *dgate, *dup;
   int64_t ldh, ldd;
+  bool pairs;                 // two neighbouring elements of h begin on 4 bytes, if they have 16 bits
   Held q;
   const float* x_ts;
   const float* gate_ts;
@@ -321,9 +322,10 @@ struct PairShared {
   uint64_t empty[kPairStages];            // of each
   uint64_t sums_full;                     // of each
   uint64_t sums_empty;                    // of the first: an arrival per reading warp of both
-  uint64_t got[kReaders];             // of each: the other block's warp has written its sums, an arrival per lane
+  uint64_t got[kReaders];             // of each: the bytes of the other block's warp
   uint64_t room[kReaders];            // of each: the other block's warp has read them
   uint64_t spare;
+  uint32_t sent[kReaders];            // of each: how often the other block's warp has sent (for a block that is abandoned)
   uint32_t tmem, abandoned;
 };
 
@@ -394,6 +396,31 @@ __device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t
   }
 }
 
+// 16-bit elements of eight tokens, the lower halves of g into one matrix and (TWO) the upper ones into another, their rows `ld` apart.
+// Neighbouring lanes trade, so that the even one has two neighbouring elements of one token and the odd one of the next: half the
+// stores.  tokens: that exist, of the eight; to, to_up: of the first token at the even lane's column, which is `col`.
+template <bool TWO>
+__device__ __forceinline__ void put_pairs(const uint32_t* g, uint16_t* to, uint16_t* to_up, int64_t ld, uint32_t tokens, uint32_t col, uint32_t n) {
+  const bool odd = threadIdx.x & 1;
+  const uint32_t lower = odd ? 0x1054 : 0x5410, upper = odd ? 0x3276 : 0x7632;
+  if (odd) to += ld, to_up += TWO ? ld : 0;
+#pragma unroll
+  for (uint32_t i = 0; i < 8; i += 2) {
+    const uint32_t mine = odd ? g[i + 1] : g[i], theirs = __shfl_xor_sync(0xffffffffu, odd ? g[i] : g[i + 1], 1);
+    const uint32_t a = __byte_perm(mine, theirs, lower), b = __byte_perm(mine, theirs, upper);
+    if (i + odd < tokens) {
+      if (col + 1 < n) {
+        *reinterpret_cast<uint32_t*>(to) = a;
+        if (TWO) *reinterpret_cast<uint32_t*>(to_up) = b;
+      } else if (col < n) {
+        *to = (uint16_t)a;
+        if (TWO) *to_up = (uint16_t)b;
+      }
+    }
+    to += 2 * ld, to_up += TWO ? 2 * ld : 0;
+  }
+}
+
 // A warp's 32 outputs of M tokens: its own sums v (of wg in the first block, of wu in the second) and those it gets from the other block's
 // warp, four tokens of a lane together.  wait(): whether these are there.
 template <int FMT, bool GRAD, uint32_t M, typename Wait>
@@ -402,7 +429,8 @@ __device__ __forceinline__ void finish_tokens(const Finish& p, const Factors& ga
   constexpr uint32_t E = 8;  // elements at a time
   const uint32_t lane = threadIdx.x & 31, col = col0 + lane;
   const bool has_col = col < p.n;
-  const uint32_t rows = has_col && row0 < p.tokens ? min(M, p.tokens - row0) : 0;  // that the lane has anything of
+  const uint32_t tokens = row0 < p.tokens ? min(M, p.tokens - row0) : 0, rows = has_col ? tokens : 0;  // of these the lane has anything
+  const bool scaled = !(gate.first == 1.0f && gate.second == 1.0f && up.first == 1.0f && up.second == 1.0f);
   uint32_t dh[M];  // as it lies in memory; all under way while the other block's sums are
   if (GRAD) {
     if (p.dtype == PVT_F32) {
@@ -428,24 +456,28 @@ __device__ __forceinline__ void finish_tokens(const Finish& p, const Factors& ga
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
           const float mine = __uint_as_float(v[j + k + i]);
-          a[k + i] = gate(rank ? o[i] : mine), b[k + i] = up(rank ? mine : o[i]);
+          a[k + i] = rank ? o[i] : mine, b[k + i] = rank ? mine : o[i];
         }
       }
+      if (scaled) {
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) a[i] = gate(a[i]), b[i] = up(b[i]);
+      }
+      const uint32_t left = tokens > j ? tokens - j : 0;
       if (GRAD) {
         float d[E];
 #pragma unroll
         for (uint32_t i = 0; i < E; ++i)
           d[i] = p.dtype == PVT_F16 ? __half2float(__ushort_as_half((unsigned short)dh[j + i]))
                                     : __uint_as_float(p.dtype == PVT_F32 ? dh[j + i] : dh[j + i] << 16);
-        __nv_bfloat162 g[E];
-#pragma unroll
-        for (uint32_t i = 0; i < E; ++i) g[i] = gradients<ACT>(a[i], b[i], d[i]);
-        __nv_bfloat16 *to_gate = p.dgate + (int64_t)(row0 + j) * p.ldd + col, *to_up = p.dup + (int64_t)(row0 + j) * p.ldd + col;
+        uint32_t g[E];
 #pragma unroll
         for (uint32_t i = 0; i < E; ++i) {
-          if (j + i < rows) *to_gate = g[i].x, *to_up = g[i].y;
-          to_gate += p.ldd, to_up += p.ldd;
+          const __nv_bfloat162 two = gradients<ACT>(a[i], b[i], d[i]);
+          g[i] = *reinterpret_cast<const uint32_t*>(&two);
         }
+        const int64_t at = (int64_t)(row0 + j) * p.ldd + (col & ~1u);
+        put_pairs<true>(g, reinterpret_cast<uint16_t*>(p.dgate) + at, reinterpret_cast<uint16_t*>(p.dup) + at, p.ldd, left, col & ~1u, p.n);
       } else {
         float h[E];
 #pragma unroll
@@ -453,11 +485,21 @@ __device__ __forceinline__ void finish_tokens(const Finish& p, const Factors& ga
         if (p.h)
           with_type(p.dtype, [&](auto* type) {
             using T = std::remove_pointer_t<decltype(type)>;
-            T* to = static_cast<T*>(p.h) + (int64_t)(row0 + j) * p.ldh + col;
+            if (sizeof(T) == 2 && p.pairs) {
+              uint32_t g[E];
 #pragma unroll
-            for (uint32_t i = 0; i < E; ++i) {
-              if (j + i < rows) *to = narrow<T>(h[i]);
-              to += p.ldh;
+              for (uint32_t i = 0; i < E; ++i) {
+                const T one = narrow<T>(h[i]);
+                g[i] = *reinterpret_cast<const uint16_t*>(&one);
+              }
+              put_pairs<false>(g, static_cast<uint16_t*>(p.h) + (int64_t)(row0 + j) * p.ldh + (col & ~1u), nullptr, p.ldh, left, col & ~1u, p.n);
+            } else {
+              T* to = static_cast<T*>(p.h) + (int64_t)(row0 + j) * p.ldh + col;
+#pragma unroll
+              for (uint32_t i = 0; i < E; ++i) {
+                if (j + i < rows) *to = narrow<T>(h[i]);
+                to += p.ldh;
+              }
             }
           });
         if (p.q.codes) {  // turned, in the place of the sums that were got
@@ -496,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(smem_u32(&sm.sums_full), 1);
     mbar_init(smem_u32(&sm.sums_empty), 2 * kReaders);
     for (uint32_t s = 0; s < kReaders; ++s) {
-      mbar_init(smem_u32(&sm.got[s]), 32);
+      mbar_init(smem_u32(&sm.got[s]), 1), sm.sent[s] = 0;
       mbar_init(smem_u32(&sm.room[s]), 1);
     }
     mbar_init(smem_u32(&sm.spare), 1);
@@ -521,6 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tile0 = blockIdx.x / 2 / p.split, stride = p.split > 1 ? p.tiles : gridDim.x / 2;
   const uint32_t first = p.steps * share / p.split, steps = p.steps * (share + 1) / p.split - first;  // (steps < 2^24, share < 4)
   const Finish& f = p.f;
+  uint32_t expected = 0, taken = 0;  // exchanges of this warp
 
   if (warp >= kCopyWarp && warp < kMmaWarp) {
     const bool of_w = warp == kCopyWarp;  // one warp for the weights' codes and scales, one for x's
@@ -592,6 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t exchange = base + S::kExchangeAt + warp * S::kExchange, other = cluster_address(exchange, in_cluster ^ 1);
     const uint32_t other_got = cluster_address(smem_u32(&sm.got[warp]), in_cluster ^ 1);
     const uint32_t other_room = cluster_address(smem_u32(&sm.room[warp]), in_cluster ^ 1);
+    const uint32_t other_sent = cluster_address(smem_u32(&sm.sent[warp]), in_cluster ^ 1);
     float* const got = reinterpret_cast<float*>(mem + S::kExchangeAt + warp * S::kExchange);
     uint32_t n = 0;
     bool ok = true;
@@ -634,19 +678,29 @@ __global__ void __launch_bounds__(kThreads, 1)
       // four tokens of a lane together
 #pragma unroll
       for (uint32_t j = 0; j < MINE; j += 4)
-        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(other + (j / 4 * 32 + lane) * 16), "r"(v[MINE + j]),
-                     "r"(v[MINE + j + 1]), "r"(v[MINE + j + 2]), "r"(v[MINE + j + 3])
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                         other + (j / 4 * 32 + lane) * 16),
+                     "r"(v[MINE + j]), "r"(v[MINE + j + 1]), "r"(v[MINE + j + 2]), "r"(v[MINE + j + 3]), "r"(other_got)
                      : "memory");
-      asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(other_got) : "memory");
+      if (lane == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other_sent), "r"(n + 1) : "memory");
+      expect_bytes(smem_u32(&sm.got[warp]), S::kExchange);
+      ++expected;
       finish_tokens<FMT, GRAD, MINE>(f, gate, up, t, row, col0, rank, v, got, [&] {
         return ok = wait<true>(smem_u32(&sm.got[warp]), n & 1, abandoned, p.status, p.max_spins);
       });
+      if (!ok) break;
+      ++taken;
       if (lane == 0) cluster_arrive(other_room);
       __syncwarp();
     }
   }
   __syncthreads();
   cluster_sync();  // neither block leaves while the other's copies, products or sums reach it
+  if (*abandoned && warp < (uint32_t)kReaders && *static_cast<volatile uint32_t*>(&sm.sent[warp]) > taken) {
+    // sums that are on their way to a warp that has not waited for them
+    if (expected == taken) expect_bytes(smem_u32(&sm.got[warp]), S::kExchange);
+    drain(smem_u32(&sm.got[warp]), taken & 1);
+  }
   if (p.split > 1) {
     // every block adds up and finishes the tokens that are its share, one to a warp, always in the order of pairs
     const uint32_t col0 = tile0 / p.x_tiles * kTileW, row0 = tile0 % p.x_tiles * N, blocks = 2 * p.split;
@@ -761,6 +815,7 @@ cudaError_t launch_mx_gated(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu,
                             const pvt_mx* hq, uint32_t* status, int sm_count, cudaStream_t stream) {
   Finish f = {};
   f.activation = activation, f.h = h, f.dtype = dtype, f.ldh = ldh;
+  f.pairs = reinterpret_cast<uintptr_t>(h) % 4 == 0 && ldh % 2 == 0;
   if (hq) f.q = held(*hq);
   return gated<false>(x, wg, wu, f, status, sm_count, stream);
 }
