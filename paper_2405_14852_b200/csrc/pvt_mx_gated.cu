@@ -12,8 +12,7 @@
 // for the next tile at once, keeps those of one half of them, and sends the others to the same thread of the other block
 // through shared memory.  The exchange, activations and stores go on beside the next tile's products.
 //
-// 4-bit results: 32 outputs of a token are one warp's lanes.  They are turned in the shared memory that the exchange has left, to one
-// token to a lane, and quantised there.
+// In shared memory the sums are turned as well: eight outputs of a token to a lane, as they are read, written and quantised.
 #include "pvt_mx_block.cuh"
 #include "pvt_mx_mma.cuh"
 #include "pvt_norm.cuh"
@@ -35,7 +34,7 @@ struct Finish {
   const void* dh;
   __nv_bfloat16 *dgate, *dup;
   int64_t ldh, ldd;
-  bool pairs;                 // two neighbouring elements of h begin on 4 bytes, if they have 16 bits
+  bool wide;                  // eight neighbouring elements of h or dh begin on 16 bytes
   Held q;
   const float* x_ts;
   const float* gate_ts;
@@ -86,12 +85,12 @@ __device__ __forceinline__ void with_activation(int32_t which, F f) {
     f(std::integral_constant<int, PVT_ACT_GELU_TANH>{});
 }
 
-// dgate and dup of one element, rounded
+// dgate and dup of one element
 template <int ACT>
-__device__ __forceinline__ __nv_bfloat162 gradients(float a, float b, float dh) {
+__device__ __forceinline__ void gradients(float a, float b, float dh, float* gate, float* up) {
   float slope;
   const float f = activate<ACT, true>(a, &slope);
-  return __floats2bfloat162_rn(dh * b * slope, dh * f);
+  *gate = dh * b * slope, *up = dh * f;
 }
 
 // A token of 128 outputs, lane, 32 + lane, ... of them to a lane; scratch: 128 floats of the warp's own.
@@ -107,14 +106,15 @@ __device__ __forceinline__ void finish_token(const Finish& p, const TensorScale&
       float v[4];
 #pragma unroll
       for (uint32_t i = 0; i < 4; ++i) v[i] = col0 + i * 32 + lane < p.n ? widen<T>(dh[i * 32]) : 0.0f;
-      __nv_bfloat162 d[4];
+      float gate[4], up[4];
       with_activation(p.activation, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = gradients<decltype(act)::value>(a[i], b[i], v[i]);
+        for (int i = 0; i < 4; ++i) gradients<decltype(act)::value>(a[i], b[i], v[i], &gate[i], &up[i]);
       });
 #pragma unroll
       for (uint32_t i = 0; i < 4; ++i)
-        if (col0 + i * 32 + lane < p.n) p.dgate[at + i * 32] = d[i].x, p.dup[at + i * 32] = d[i].y;
+        if (col0 + i * 32 + lane < p.n)
+          p.dgate[at + i * 32] = __float2bfloat16_rn(gate[i]), p.dup[at + i * 32] = __float2bfloat16_rn(up[i]);
     });
   } else {
     float h[4];
@@ -316,6 +316,9 @@ __global__ void __launch_bounds__(kFewThreads)
 // 11008 159 us)
 constexpr int kReaders = 16, kCopyWarp = kReaders, kMmaWarp = kCopyWarp + kPairCopyWarps;
 constexpr int kThreads = (kMmaWarp + 1) * 32;
+constexpr uint32_t kRound = 16;                  // tokens of a warp at a time
+constexpr uint32_t kGot = kRound * 32 * 4;       // bytes that it gets, and of its own sums beside them
+constexpr uint32_t kExchange = 2 * kGot;
 
 struct PairShared {
   alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
@@ -342,8 +345,7 @@ struct PairParams {
 template <int FMT, uint32_t N>
 struct GatedSizes : PairSizes<FMT, N> {
   using P = PairSizes<FMT, N>;
-  static constexpr uint32_t kMine = N / 8;                 // tokens that a warp finishes, and that it sends
-  static constexpr uint32_t kExchange = kMine * 32 * 4;    // bytes that it gets
+  static constexpr uint32_t kMine = N / 8;  // tokens that a warp finishes, and that it sends
   static constexpr uint32_t kRoom = (225 * 1024 - kReaders * kExchange) / P::kStageAligned;
   static constexpr uint32_t kStages = kRoom < P::kStages ? kRoom : P::kStages;
   static constexpr uint32_t kExchangeAt = kStages * P::kStageAligned;
@@ -355,166 +357,159 @@ struct GatedSizes : PairSizes<FMT, N> {
 // asks for the line of an address to be brought into the L2
 __device__ __forceinline__ void ask_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
 
-// what a warp's 32 lanes (outputs) have of M tokens, into 4 bits; buffer: that of output i of token j in place 32 j + (i ^ j)
-template <int FMT, uint32_t M>
-__device__ __forceinline__ void put_tokens(const Finish& p, const TensorScale& t, uint32_t token0, uint32_t col0, const float* buffer) {
-  constexpr int BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16, N = 32 / BLOCK;
-  const uint32_t lane = threadIdx.x & 31;
-  const uint32_t token = token0 + lane;
-  if (lane >= M) return;
-  float e[32];
+// Where a warp's sums of a round lie: 32 outputs of a token to 128 bytes, in pieces of four whose places in it are exchanged by the token,
+// so that no bank is met twice either by lanes that have an output each or by four lanes to a token with eight outputs each.
+__device__ __forceinline__ uint32_t place(uint32_t token, uint32_t output) { return token * 32 + (output ^ (token & 7) * 4); }
+
+// eight neighbouring elements, rounded; `left` of them exist
+template <typename T>
+__device__ __forceinline__ void put8(T* to, const float* v, bool wide, uint32_t left) {
+  if (wide && left >= 8) {
+    if constexpr (sizeof(T) == 4) {
+      reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      Eight<T> e;
 #pragma unroll
-  for (uint32_t i = 0; i < 32; ++i) e[i] = buffer[lane * 32 + (i ^ lane)];
-  uint32_t word[4], bytes = 0;
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < BLOCK; ++i) top = max(top, __float_as_uint(e[n * BLOCK + i]) & 0x7fffffffu);
-    const uint32_t byte = quantize_block<FMT, BLOCK>(e + n * BLOCK, top, t, word + n * (BLOCK / 8));
-    if (token < p.tokens && col0 + n * BLOCK < p.n) bytes |= byte << (8 * n);
-  }
-  if (token >= p.padded) return;
-  auto put_scales = [&](uint32_t col, uint32_t value) {
-    if (col / BLOCK / 4 >= p.q.tiles) return;
-    uint8_t* const to = p.q.scales + scale_at(token, col / BLOCK, p.q.tiles);
-    if (N == 1)
-      *to = (uint8_t)value;
-    else
-      *reinterpret_cast<uint16_t*>(to) = (uint16_t)value;
-  };
-  put_scales(col0, bytes);
-  if (col0 / 128 == (p.n - 1) / 128) put_scales(col0 + 128, 0);  // (blocks of no outputs at all)
-  if (token >= p.tokens || col0 >= p.n) return;
-  uint8_t* const to = p.q.codes + (int64_t)token * p.q.ld + col0 / 2;
-  if (col0 + 32 <= p.n) {
-    *reinterpret_cast<uint4*>(to) = make_uint4(word[0], word[1], word[2], word[3]);
+      for (int i = 0; i < 8; i += 2) norm::narrow_pair(v[i], v[i + 1], &e.v[i]);
+      *reinterpret_cast<Eight<T>*>(to) = e;
+    }
   } else {
 #pragma unroll
-    for (uint32_t i = 0; i < 16; ++i)
-      if (2 * i < p.n - col0) to[i] = (uint8_t)(word[i / 4] >> (8 * (i % 4)));
+    for (uint32_t i = 0; i < 8; ++i)
+      if (i < left) to[i] = narrow<T>(v[i]);
   }
 }
 
-// 16-bit elements of eight tokens, the lower halves of g into one matrix and (TWO) the upper ones into another, their rows `ld` apart.
-// Neighbouring lanes trade, so that the even one has two neighbouring elements of one token and the odd one of the next: half the
-// stores.  tokens: that exist, of the eight; to, to_up: of the first token at the even lane's column, which is `col`.
-template <bool TWO>
-__device__ __forceinline__ void put_pairs(const uint32_t* g, uint16_t* to, uint16_t* to_up, int64_t ld, uint32_t tokens, uint32_t col, uint32_t n) {
-  const bool odd = threadIdx.x & 1;
-  const uint32_t lower = odd ? 0x1054 : 0x5410, upper = odd ? 0x3276 : 0x7632;
-  if (odd) to += ld, to_up += TWO ? ld : 0;
+// Eight outputs of a token, from column c on, into 4 bits: four lanes have the token's 32 outputs.  (here: the token exists.)
+template <int FMT>
+__device__ __forceinline__ void put_four_bits(const Finish& p, const TensorScale& t, uint32_t token, uint32_t c, bool here, float* v) {
+  constexpr uint32_t BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16;
+  uint32_t top = 0, word;
 #pragma unroll
-  for (uint32_t i = 0; i < 8; i += 2) {
-    const uint32_t mine = odd ? g[i + 1] : g[i], theirs = __shfl_xor_sync(0xffffffffu, odd ? g[i] : g[i + 1], 1);
-    const uint32_t a = __byte_perm(mine, theirs, lower), b = __byte_perm(mine, theirs, upper);
-    if (i + odd < tokens) {
-      if (col + 1 < n) {
-        *reinterpret_cast<uint32_t*>(to) = a;
-        if (TWO) *reinterpret_cast<uint32_t*>(to_up) = b;
-      } else if (col < n) {
-        *to = (uint16_t)a;
-        if (TWO) *to_up = (uint16_t)b;
-      }
-    }
-    to += 2 * ld, to_up += TWO ? 2 * ld : 0;
+  for (uint32_t i = 0; i < 8; ++i) {
+    if (c + i >= p.n) v[i] = 0.0f;
+    top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  }
+#pragma unroll
+  for (uint32_t d = 1; d < BLOCK / 8; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+  uint32_t bytes = quantize_block<FMT, 8>(v, top, t, &word);
+  if (!here || c >= p.n) bytes = 0;  // scales of what does not exist
+  if (FMT == PVT_MX_E4M3_16) bytes |= __shfl_down_sync(0xffffffffu, bytes, 2) << 8;
+  if (threadIdx.x % 4 == 0 && token < p.padded) {
+    auto put_scales = [&](uint32_t col, uint32_t value) {
+      if (col / BLOCK / 4 >= p.q.tiles) return;
+      uint8_t* const to = p.q.scales + scale_at(token, col / BLOCK, p.q.tiles);
+      if (FMT == PVT_MX_E8M0_32)
+        *to = (uint8_t)value;
+      else
+        *reinterpret_cast<uint16_t*>(to) = (uint16_t)value;
+    };
+    put_scales(c, bytes);
+    if (c / 128 == (p.n - 1) / 128) put_scales(c + 128, 0);  // (blocks of no outputs at all)
+  }
+  if (!here || c >= p.n) return;
+  uint8_t* const to = p.q.codes + (int64_t)token * p.q.ld + c / 2;
+  if (c + 8 <= p.n) {
+    *reinterpret_cast<uint32_t*>(to) = word;
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+      if (2 * i < p.n - c) to[i] = (uint8_t)(word >> (8 * i));
   }
 }
 
-// A warp's 32 outputs of M tokens: its own sums v (of wg in the first block, of wu in the second) and those it gets from the other block's
-// warp, four tokens of a lane together.  wait(): whether these are there.
-template <int FMT, bool GRAD, uint32_t M, typename Wait>
-__device__ __forceinline__ void finish_tokens(const Finish& p, const Factors& gate, const Factors& up, const TensorScale& t, uint32_t row0,
-                                              uint32_t col0, uint32_t rank, const uint32_t* v, float* got, Wait wait) {
-  constexpr uint32_t E = 8;  // elements at a time
-  const uint32_t lane = threadIdx.x & 31, col = col0 + lane;
-  const bool has_col = col < p.n;
-  const uint32_t tokens = row0 < p.tokens ? min(M, p.tokens - row0) : 0, rows = has_col ? tokens : 0;  // of these the lane has anything
+// A warp's 32 outputs of 16 tokens from their sums in shared memory.  A lane has eight neighbouring outputs of two tokens: what is
+// read and written of a token is one access to a lane, and no element has an address of its own (as sums lie in tensor memory, a
+// lane to an output, half of 50 instructions an element were that).  wait(): whether the other block's sums are there.
+template <int FMT, bool GRAD, typename Wait>
+__device__ __forceinline__ void finish_round(const Finish& p, const Factors& gate, const Factors& up, const TensorScale& t, uint32_t row0,
+                                             uint32_t col0, const float* a_sums, const float* b_sums, Wait wait) {
+  const uint32_t lane = threadIdx.x & 31, c = col0 + lane % 4 * 8, row = row0 + lane / 4;
+  const uint32_t left = c < p.n ? p.n - c : 0;  // outputs that exist
   const bool scaled = !(gate.first == 1.0f && gate.second == 1.0f && up.first == 1.0f && up.second == 1.0f);
-  uint32_t dh[M];  // as it lies in memory; all under way while the other block's sums are
+  uint4 dh[2][2];  // as it lies in memory, under way while the other block's sums are
   if (GRAD) {
-    if (p.dtype == PVT_F32) {
-      const uint32_t* from = static_cast<const uint32_t*>(p.dh) + (int64_t)row0 * p.ldh + col;
 #pragma unroll
-      for (uint32_t j = 0; j < M; ++j, from += p.ldh) dh[j] = j < rows ? *from : 0;
-    } else {
-      const uint16_t* from = static_cast<const uint16_t*>(p.dh) + (int64_t)row0 * p.ldh + col;
+    for (uint32_t i = 0; i < 2; ++i) {
+      dh[i][0] = dh[i][1] = make_uint4(0, 0, 0, 0);
+      if (row + 8 * i < p.tokens && left > 0) {
+        const int64_t at = (int64_t)(row + 8 * i) * p.ldh + c;
+        if (p.dtype == PVT_F32) {
+          const uint32_t* const from = static_cast<const uint32_t*>(p.dh) + at;
+          if (p.wide && left >= 8) {
+            dh[i][0] = reinterpret_cast<const uint4*>(from)[0], dh[i][1] = reinterpret_cast<const uint4*>(from)[1];
+          } else {
+            uint32_t* const w = reinterpret_cast<uint32_t*>(dh[i]);
 #pragma unroll
-      for (uint32_t j = 0; j < M; ++j, from += p.ldh) dh[j] = j < rows ? *from : 0;
+            for (uint32_t k = 0; k < 8; ++k)
+              if (k < left) w[k] = from[k];
+          }
+        } else {
+          const uint16_t* const from = static_cast<const uint16_t*>(p.dh) + at;
+          if (p.wide && left >= 8) {
+            dh[i][0] = *reinterpret_cast<const uint4*>(from);
+          } else {
+            uint32_t* const w = reinterpret_cast<uint32_t*>(dh[i]);
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+              if (k < left) w[k / 2] |= (uint32_t)from[k] << (k % 2 * 16);
+          }
+        }
+      }
     }
   }
   if (!wait()) return;
   with_activation(p.activation, [&](auto act) {
     constexpr int ACT = decltype(act)::value;
 #pragma unroll
-    for (uint32_t j = 0; j < M; j += E) {
-      float a[E], b[E];
+    for (uint32_t i = 0; i < 2; ++i) {
+      const uint32_t j = lane / 4 + 8 * i, token = row0 + j;
+      float a[8], b[8];
 #pragma unroll
-      for (uint32_t k = 0; k < E; k += 4) {
-        const float4 theirs = reinterpret_cast<const float4*>(got)[(j + k) / 4 * 32 + lane];
-        const float o[4] = {theirs.x, theirs.y, theirs.z, theirs.w};
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-          const float mine = __uint_as_float(v[j + k + i]);
-          a[k + i] = rank ? o[i] : mine, b[k + i] = rank ? mine : o[i];
-        }
+      for (uint32_t k = 0; k < 8; k += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(a_sums + place(j, lane % 4 * 8 + k));
+        const float4 y = *reinterpret_cast<const float4*>(b_sums + place(j, lane % 4 * 8 + k));
+        a[k] = x.x, a[k + 1] = x.y, a[k + 2] = x.z, a[k + 3] = x.w, b[k] = y.x, b[k + 1] = y.y, b[k + 2] = y.z, b[k + 3] = y.w;
       }
       if (scaled) {
 #pragma unroll
-        for (uint32_t i = 0; i < E; ++i) a[i] = gate(a[i]), b[i] = up(b[i]);
+        for (int k = 0; k < 8; ++k) a[k] = gate(a[k]), b[k] = up(b[k]);
       }
-      const uint32_t left = tokens > j ? tokens - j : 0;
+      const bool here = token < p.tokens;
       if (GRAD) {
-        float d[E];
+        const uint32_t* const w = reinterpret_cast<const uint32_t*>(dh[i]);
+        float d[8], to_gate[8], to_up[8];
+        if (p.dtype == PVT_F32) {
 #pragma unroll
-        for (uint32_t i = 0; i < E; ++i)
-          d[i] = p.dtype == PVT_F16 ? __half2float(__ushort_as_half((unsigned short)dh[j + i]))
-                                    : __uint_as_float(p.dtype == PVT_F32 ? dh[j + i] : dh[j + i] << 16);
-        uint32_t g[E];
+          for (int k = 0; k < 8; ++k) d[k] = __uint_as_float(w[k]);
+        } else if (p.dtype == PVT_BF16) {
 #pragma unroll
-        for (uint32_t i = 0; i < E; ++i) {
-          const __nv_bfloat162 two = gradients<ACT>(a[i], b[i], d[i]);
-          g[i] = *reinterpret_cast<const uint32_t*>(&two);
+          for (int k = 0; k < 8; ++k) d[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) d[k] = __half2float(__ushort_as_half((unsigned short)(w[k / 2] >> (k % 2 * 16))));
         }
-        const int64_t at = (int64_t)(row0 + j) * p.ldd + (col & ~1u);
-        put_pairs<true>(g, reinterpret_cast<uint16_t*>(p.dgate) + at, reinterpret_cast<uint16_t*>(p.dup) + at, p.ldd, left, col & ~1u, p.n);
-      } else {
-        float h[E];
 #pragma unroll
-        for (uint32_t i = 0; i < E; ++i) h[i] = activate<ACT, false>(a[i], nullptr) * b[i];
-        if (p.h)
+        for (int k = 0; k < 8; ++k) gradients<ACT>(a[k], b[k], d[k], &to_gate[k], &to_up[k]);
+        if (here) {
+          const int64_t at = (int64_t)token * p.ldd + c;
+          put8(p.dgate + at, to_gate, true, left);
+          put8(p.dup + at, to_up, true, left);
+        }
+      } else {
+        float h[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) h[k] = activate<ACT, false>(a[k], nullptr) * b[k];
+        if (p.h && here)
           with_type(p.dtype, [&](auto* type) {
             using T = std::remove_pointer_t<decltype(type)>;
-            if (sizeof(T) == 2 && p.pairs) {
-              uint32_t g[E];
-#pragma unroll
-              for (uint32_t i = 0; i < E; ++i) {
-                const T one = narrow<T>(h[i]);
-                g[i] = *reinterpret_cast<const uint16_t*>(&one);
-              }
-              put_pairs<false>(g, static_cast<uint16_t*>(p.h) + (int64_t)(row0 + j) * p.ldh + (col & ~1u), nullptr, p.ldh, left, col & ~1u, p.n);
-            } else {
-              T* to = static_cast<T*>(p.h) + (int64_t)(row0 + j) * p.ldh + col;
-#pragma unroll
-              for (uint32_t i = 0; i < E; ++i) {
-                if (j + i < rows) *to = narrow<T>(h[i]);
-                to += p.ldh;
-              }
-            }
+            put8(static_cast<T*>(p.h) + (int64_t)token * p.ldh + c, h, p.wide, left);
           });
-        if (p.q.codes) {  // turned, in the place of the sums that were got
-          __syncwarp();
-#pragma unroll
-          for (uint32_t i = 0; i < E; ++i) got[(j + i) * 32 + (lane ^ (j + i))] = has_col ? h[i] : 0.0f;
-        }
+        if (p.q.codes) put_four_bits<FMT>(p, t, token, c, here, h);
       }
     }
   });
-  __syncwarp();
-  if (!GRAD && p.q.codes) {
-    put_tokens<FMT, M>(p, t, row0, col0, got);
-    __syncwarp();
-  }
 }
 
 template <int FMT, uint32_t N, bool GRAD>
@@ -632,11 +627,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t quarter = warp % 4, part = warp / 4;  // of the outputs, of the tokens
     const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), lead);
     // of the other block: where this warp's sums go, and the barriers of the same warp
-    const uint32_t exchange = base + S::kExchangeAt + warp * S::kExchange, other = cluster_address(exchange, in_cluster ^ 1);
+    const uint32_t exchange = base + S::kExchangeAt + warp * kExchange, other = cluster_address(exchange, in_cluster ^ 1);
     const uint32_t other_got = cluster_address(smem_u32(&sm.got[warp]), in_cluster ^ 1);
     const uint32_t other_room = cluster_address(smem_u32(&sm.room[warp]), in_cluster ^ 1);
     const uint32_t other_sent = cluster_address(smem_u32(&sm.sent[warp]), in_cluster ^ 1);
-    float* const got = reinterpret_cast<float*>(mem + S::kExchangeAt + warp * S::kExchange);
+    float* const got = reinterpret_cast<float*>(mem + S::kExchangeAt + warp * kExchange);
+    float* const own = got + kGot / 4;
+    const float *const a_sums = rank ? got : own, *const b_sums = rank ? own : got;
     uint32_t n = 0;
     bool ok = true;
     for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride, ++n) {
@@ -673,32 +670,37 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         break;
       }
-      if (n > 0) ok = wait<true>(smem_u32(&sm.room[warp]), (n - 1) & 1, abandoned, p.status, p.max_spins);
-      if (!ok) break;
-      // four tokens of a lane together
 #pragma unroll
-      for (uint32_t j = 0; j < MINE; j += 4)
-        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
-                         other + (j / 4 * 32 + lane) * 16),
-                     "r"(v[MINE + j]), "r"(v[MINE + j + 1]), "r"(v[MINE + j + 2]), "r"(v[MINE + j + 3]), "r"(other_got)
-                     : "memory");
-      if (lane == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other_sent), "r"(n + 1) : "memory");
-      expect_bytes(smem_u32(&sm.got[warp]), S::kExchange);
-      ++expected;
-      finish_tokens<FMT, GRAD, MINE>(f, gate, up, t, row, col0, rank, v, got, [&] {
-        return ok = wait<true>(smem_u32(&sm.got[warp]), n & 1, abandoned, p.status, p.max_spins);
-      });
-      if (!ok) break;
-      ++taken;
-      if (lane == 0) cluster_arrive(other_room);
-      __syncwarp();
+      for (uint32_t r = 0; r < MINE; r += kRound) {
+        if (taken > 0) ok = wait<true>(smem_u32(&sm.room[warp]), (taken - 1) & 1, abandoned, p.status, p.max_spins);
+        if (!ok) break;
+#pragma unroll
+        for (uint32_t j = 0; j < kRound; ++j)
+          asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(other + place(j, lane) * 4),
+                       "r"(v[MINE + r + j]), "r"(other_got)
+                       : "memory");
+        if (lane == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other_sent), "r"(taken + 1) : "memory");
+        expect_bytes(smem_u32(&sm.got[warp]), kGot);
+        ++expected;
+#pragma unroll
+        for (uint32_t j = 0; j < kRound; ++j) own[place(j, lane)] = __uint_as_float(v[r + j]);
+        __syncwarp();
+        finish_round<FMT, GRAD>(f, gate, up, t, row + r, col0, a_sums, b_sums, [&] {
+          return ok = wait<true>(smem_u32(&sm.got[warp]), taken & 1, abandoned, p.status, p.max_spins);
+        });
+        if (!ok) break;
+        ++taken;
+        __syncwarp();
+        if (lane == 0) cluster_arrive(other_room);
+        __syncwarp();
+      }
     }
   }
   __syncthreads();
   cluster_sync();  // neither block leaves while the other's copies, products or sums reach it
   if (*abandoned && warp < (uint32_t)kReaders && *static_cast<volatile uint32_t*>(&sm.sent[warp]) > taken) {
     // sums that are on their way to a warp that has not waited for them
-    if (expected == taken) expect_bytes(smem_u32(&sm.got[warp]), S::kExchange);
+    if (expected == taken) expect_bytes(smem_u32(&sm.got[warp]), kGot);
     drain(smem_u32(&sm.got[warp]), taken & 1);
   }
   if (p.split > 1) {
@@ -815,7 +817,7 @@ cudaError_t launch_mx_gated(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu,
                             const pvt_mx* hq, uint32_t* status, int sm_count, cudaStream_t stream) {
   Finish f = {};
   f.activation = activation, f.h = h, f.dtype = dtype, f.ldh = ldh;
-  f.pairs = reinterpret_cast<uintptr_t>(h) % 4 == 0 && ldh % 2 == 0;
+  f.wide = reinterpret_cast<uintptr_t>(h) % 16 == 0 && ldh % 8 == 0;
   if (hq) f.q = held(*hq);
   return gated<false>(x, wg, wu, f, status, sm_count, stream);
 }
@@ -824,6 +826,7 @@ cudaError_t launch_mx_gated_grad(const pvt_mx& x, const pvt_mx& wg, const pvt_mx
                                  int64_t lddh, void* dgate, void* dup, int64_t ldd, uint32_t* status, int sm_count, cudaStream_t stream) {
   Finish f = {};
   f.activation = activation, f.dh = dh, f.dtype = dtype, f.ldh = lddh;
+  f.wide = reinterpret_cast<uintptr_t>(dh) % 16 == 0 && lddh % 8 == 0;
   f.dgate = static_cast<__nv_bfloat16*>(dgate), f.dup = static_cast<__nv_bfloat16*>(dup), f.ldd = ldd;
   return gated<true>(x, wg, wu, f, status, sm_count, stream);
 }
