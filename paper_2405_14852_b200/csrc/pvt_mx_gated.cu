@@ -6,13 +6,13 @@
 // the same rows of wu, each pair its share of the steps.  The partial sums meet in shared memory across the cluster, always in the
 // order of ranks, and whoever adds up a token's sums finishes it.
 //
-// From 17 tokens on: the product's pairs of blocks, 256 rows of weights by 256 (or 128) of x to a tile; but the first block's 128 rows
-// are wg's and the second's the same ones of wu.  The main loop, its traffic (32 KB of codes a step and SM) and its rate are the product's.
-// What is needed together is then in two SMs: a thread reads its sums of N / 4 tokens out of tensor memory, which is free
-// for the next tile at once, keeps those of one half of them, and sends the others to the same thread of the other block
-// through shared memory.  The exchange, activations and stores go on beside the next tile's products.
-//
-// In shared memory the sums are turned as well: eight outputs of a token to a lane, as they are read, written and quantised.
+// From 17 tokens on: the product's pairs of blocks, 256 rows of weights by 256 (or 128) of x to a tile; but a block's 128 rows are 64
+// of wg and the same 64 of wu.  The main loop, its traffic (32 KB of codes a step and SM) and its rate are the product's; only scales
+// do not lie so in memory: a warp puts the tiles of 128 rows together, eight bytes of wg's and eight of wu's to sixteen, which the copy to
+// tensor memory takes as one.  A tile's sums are read out of tensor memory, which is free for the next tile at once, turned in shared
+// memory, where a thread finds a and b of the same eight outputs of a token, and finished beside the next tile's products.
+// (128 rows of wg in one block and of wu in the other need no such scales, but every second sum has to go from one SM to the other: their
+// exchange, in the same order as here, took 6000 cycles a tile of the 8192 that 4096 inputs multiply, gradients of 2048 x 4096 by 11008 93 us.)
 #include "pvt_mx_block.cuh"
 #include "pvt_mx_mma.cuh"
 #include "pvt_norm.cuh"
@@ -312,23 +312,21 @@ __global__ void __launch_bounds__(kFewThreads)
 }
 
 // ---- pairs of blocks -------------------------------------------------------------------------------------------
-// (sixteen warps finish: with eight there were two to a scheduler, and most of the time neither could go on: gradients of 2048 x 4096 by
-// 11008 159 us)
-constexpr int kReaders = 16, kCopyWarp = kReaders, kMmaWarp = kCopyWarp + kPairCopyWarps;
-constexpr int kThreads = (kMmaWarp + 1) * 32;
-constexpr uint32_t kRound = 16;                  // tokens of a warp at a time
-constexpr uint32_t kGot = kRound * 32 * 4;       // bytes that it gets, and of its own sums beside them
-constexpr uint32_t kExchange = 2 * kGot;
+// Sixteen warps finish: with eight there were two to a scheduler, and most of the time neither could go on.
+constexpr int kReaders = 16, kCopyWarp = kReaders, kMmaWarp = kCopyWarp + kPairCopyWarps, kScaleWarp = kMmaWarp + 1;
+constexpr int kThreads = (kScaleWarp + 1) * 32;
+constexpr uint32_t kOutputs = 64;               // of a block
+constexpr uint32_t kRound = 16;                 // tokens that two warps, one with a and one with b, turn at a time
+constexpr uint32_t kSums = kRound * 32 * 4;     // bytes of either
 
 struct PairShared {
   alignas(8) uint64_t full[kPairStages];  // of the first block: bytes of both
+  uint64_t raw[kPairStages];              // of each: the weights' scales as they lie in memory
+  uint64_t scaled[kPairStages];           // of the first: these have been put together in both
   uint64_t empty[kPairStages];            // of each
   uint64_t sums_full;                     // of each
   uint64_t sums_empty;                    // of the first: an arrival per reading warp of both
-  uint64_t got[kReaders];             // of each: the bytes of the other block's warp
-  uint64_t room[kReaders];            // of each: the other block's warp has read them
   uint64_t spare;
-  uint32_t sent[kReaders];            // of each: how often the other block's warp has sent (for a block that is abandoned)
   uint32_t tmem, abandoned;
 };
 
@@ -343,22 +341,41 @@ struct PairParams {
 };
 
 template <int FMT, uint32_t N>
-struct GatedSizes : PairSizes<FMT, N> {
-  using P = PairSizes<FMT, N>;
-  static constexpr uint32_t kMine = N / 8;  // tokens that a warp finishes, and that it sends
-  static constexpr uint32_t kRoom = (225 * 1024 - kReaders * kExchange) / P::kStageAligned;
-  static constexpr uint32_t kStages = kRoom < P::kStages ? kRoom : P::kStages;
-  static constexpr uint32_t kExchangeAt = kStages * P::kStageAligned;
-  static constexpr size_t kBytes = kExchangeAt + kReaders * kExchange + 1024;
+struct GatedSizes {
+  static constexpr uint32_t KT = FMT == PVT_MX_E8M0_32 ? 2 : 4, kStrips = N / kStrip;
+  // a stage: rows of weights, rows of x, scales of x, scales of the weights put together, and of either as they lie in memory
+  static constexpr uint32_t kX = kTileW * kRowBytes, kXs = kX + N / 2 * kRowBytes, kWs = kXs + kStrips * KT * kTileBytes;
+  static constexpr uint32_t kRaw = kWs + KT * kTileBytes, kStage = kRaw + 2 * KT * kTileBytes, kStageAligned = (kStage + 1023) / 1024 * 1024;
+  static constexpr uint32_t kScaleCols = KT * 4 * (1 + kStrips);  // of a stage
+  static constexpr uint32_t kRoom = (225 * 1024 - kReaders * kSums) / kStageAligned, kMost = N == 256 ? 5 : 7;
+  static constexpr uint32_t kStages = kRoom < kMost ? kRoom : kMost;
+  static_assert(N + kStages * kScaleCols <= 512 && kStages <= kPairStages, "sums and scales fit tensor memory");
+  static constexpr uint32_t kTurnAt = kStages * kStageAligned;
+  static constexpr size_t kBytes = kTurnAt + kReaders * kSums + 1024;
   static_assert(kBytes + 1024 <= 227 * 1024, "a block's shared memory");
-  static_assert(N * kTileW * 4 <= kExchangeAt, "the partial sums fit the stages");
+  static_assert(N * kTileW * 4 <= kTurnAt, "the partial sums fit the stages");
 };
 
 // asks for the line of an address to be brought into the L2
 __device__ __forceinline__ void ask_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
 
-// Where a warp's sums of a round lie: 32 outputs of a token to 128 bytes, in pieces of four whose places in it are exchanged by the token,
-// so that no bank is met twice either by lanes that have an output each or by four lanes to a token with eight outputs each.
+// two warps of a block, `id` of their own; with `ok` of both if both have it
+__device__ __forceinline__ void pair_sync(uint32_t id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_agrees(uint32_t id, bool ok) {
+  uint32_t both;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %2, 0;\n\t"
+      "barrier.cta.red.and.pred q, %1, 64, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(both)
+      : "r"(id), "r"((uint32_t)ok)
+      : "memory");
+  return both != 0;
+}
+
+// Where sums of a round lie: 32 outputs of a token to 128 bytes, in pieces of four whose places in it are exchanged by the token, so that
+// no bank is met twice either by lanes that have an output each or by four lanes to a token with eight outputs each.
 __device__ __forceinline__ uint32_t place(uint32_t token, uint32_t output) { return token * 32 + (output ^ (token & 7) * 4); }
 
 // eight neighbouring elements, rounded; `left` of them exist
@@ -381,7 +398,7 @@ __device__ __forceinline__ void put8(T* to, const float* v, bool wide, uint32_t 
   }
 }
 
-// Eight outputs of a token, from column c on, into 4 bits: four lanes have the token's 32 outputs.  (here: the token exists.)
+// Eight outputs of a token, from column c on, into 4 bits: four lanes have 32 of them.  (here: the token exists.)
 template <int FMT>
 __device__ __forceinline__ void put_four_bits(const Finish& p, const TensorScale& t, uint32_t token, uint32_t c, bool here, float* v) {
   constexpr uint32_t BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16;
@@ -419,97 +436,93 @@ __device__ __forceinline__ void put_four_bits(const Finish& p, const TensorScale
   }
 }
 
-// A warp's 32 outputs of 16 tokens from their sums in shared memory.  A lane has eight neighbouring outputs of two tokens: what is
-// read and written of a token is one access to a lane, and no element has an address of its own (as sums lie in tensor memory, a
-// lane to an output, half of 50 instructions an element were that).  wait(): whether the other block's sums are there.
-template <int FMT, bool GRAD, typename Wait>
-__device__ __forceinline__ void finish_round(const Finish& p, const Factors& gate, const Factors& up, const TensorScale& t, uint32_t row0,
-                                             uint32_t col0, const float* a_sums, const float* b_sums, Wait wait) {
-  const uint32_t lane = threadIdx.x & 31, c = col0 + lane % 4 * 8, row = row0 + lane / 4;
-  const uint32_t left = c < p.n ? p.n - c : 0;  // outputs that exist
-  const bool scaled = !(gate.first == 1.0f && gate.second == 1.0f && up.first == 1.0f && up.second == 1.0f);
-  uint4 dh[2][2];  // as it lies in memory, under way while the other block's sums are
-  if (GRAD) {
+// eight elements of dh as they lie in memory
+struct EightOfDh {
+  uint32_t w[8];
+  __device__ __forceinline__ void ask(const Finish& p, uint32_t token, uint32_t c, uint32_t left) {
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
-      dh[i][0] = dh[i][1] = make_uint4(0, 0, 0, 0);
-      if (row + 8 * i < p.tokens && left > 0) {
-        const int64_t at = (int64_t)(row + 8 * i) * p.ldh + c;
-        if (p.dtype == PVT_F32) {
-          const uint32_t* const from = static_cast<const uint32_t*>(p.dh) + at;
-          if (p.wide && left >= 8) {
-            dh[i][0] = reinterpret_cast<const uint4*>(from)[0], dh[i][1] = reinterpret_cast<const uint4*>(from)[1];
-          } else {
-            uint32_t* const w = reinterpret_cast<uint32_t*>(dh[i]);
+    for (int k = 0; k < 8; ++k) w[k] = 0;
+    if (token >= p.tokens || left == 0) return;
+    const int64_t at = (int64_t)token * p.ldh + c;
+    if (p.dtype == PVT_F32) {
+      const uint32_t* const from = static_cast<const uint32_t*>(p.dh) + at;
+      if (p.wide && left >= 8) {
+        const uint4 a = reinterpret_cast<const uint4*>(from)[0], b = reinterpret_cast<const uint4*>(from)[1];
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+      } else {
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k)
-              if (k < left) w[k] = from[k];
-          }
-        } else {
-          const uint16_t* const from = static_cast<const uint16_t*>(p.dh) + at;
-          if (p.wide && left >= 8) {
-            dh[i][0] = *reinterpret_cast<const uint4*>(from);
-          } else {
-            uint32_t* const w = reinterpret_cast<uint32_t*>(dh[i]);
+        for (uint32_t k = 0; k < 8; ++k)
+          if (k < left) w[k] = from[k];
+      }
+    } else {
+      const uint16_t* const from = static_cast<const uint16_t*>(p.dh) + at;
+      if (p.wide && left >= 8) {
+        const uint4 a = *reinterpret_cast<const uint4*>(from);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+      } else {
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k)
-              if (k < left) w[k / 2] |= (uint32_t)from[k] << (k % 2 * 16);
-          }
-        }
+        for (uint32_t k = 0; k < 8; ++k)
+          if (k < left) w[k / 2] |= (uint32_t)from[k] << (k % 2 * 16);
       }
     }
   }
-  if (!wait()) return;
-  with_activation(p.activation, [&](auto act) {
-    constexpr int ACT = decltype(act)::value;
+  __device__ __forceinline__ void values(int32_t dtype, float* d) const {
+    if (dtype == PVT_F32) {
 #pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
-      const uint32_t j = lane / 4 + 8 * i, token = row0 + j;
-      float a[8], b[8];
+      for (int k = 0; k < 8; ++k) d[k] = __uint_as_float(w[k]);
+    } else if (dtype == PVT_BF16) {
 #pragma unroll
-      for (uint32_t k = 0; k < 8; k += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(a_sums + place(j, lane % 4 * 8 + k));
-        const float4 y = *reinterpret_cast<const float4*>(b_sums + place(j, lane % 4 * 8 + k));
-        a[k] = x.x, a[k + 1] = x.y, a[k + 2] = x.z, a[k + 3] = x.w, b[k] = y.x, b[k + 1] = y.y, b[k + 2] = y.z, b[k + 3] = y.w;
-      }
-      if (scaled) {
+      for (int k = 0; k < 8; ++k) d[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+    } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) a[k] = gate(a[k]), b[k] = up(b[k]);
-      }
-      const bool here = token < p.tokens;
-      if (GRAD) {
-        const uint32_t* const w = reinterpret_cast<const uint32_t*>(dh[i]);
-        float d[8], to_gate[8], to_up[8];
-        if (p.dtype == PVT_F32) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) d[k] = __uint_as_float(w[k]);
-        } else if (p.dtype == PVT_BF16) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) d[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) d[k] = __half2float(__ushort_as_half((unsigned short)(w[k / 2] >> (k % 2 * 16))));
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) gradients<ACT>(a[k], b[k], d[k], &to_gate[k], &to_up[k]);
-        if (here) {
-          const int64_t at = (int64_t)token * p.ldd + c;
-          put8(p.dgate + at, to_gate, true, left);
-          put8(p.dup + at, to_up, true, left);
-        }
-      } else {
-        float h[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[k] = activate<ACT, false>(a[k], nullptr) * b[k];
-        if (p.h && here)
-          with_type(p.dtype, [&](auto* type) {
-            using T = std::remove_pointer_t<decltype(type)>;
-            put8(static_cast<T*>(p.h) + (int64_t)token * p.ldh + c, h, p.wide, left);
-          });
-        if (p.q.codes) put_four_bits<FMT>(p, t, token, c, here, h);
-      }
+      for (int k = 0; k < 8; ++k) d[k] = __half2float(__ushort_as_half((unsigned short)(w[k / 2] >> (k % 2 * 16))));
     }
-  });
+  }
+};
+
+// Eight outputs of a token, from column c on; all lanes of a warp call.  turn: shared memory for eight tokens of 32 outputs (place()) that
+// is this warp's for now, or null: where rows of h have no alignment they go out by way of it, so that a warp stores along them.
+template <int FMT, bool GRAD, int ACT>
+__device__ __forceinline__ void finish8(const Finish& p, const TensorScale& t, uint32_t token, uint32_t c, const float* a, const float* b,
+                                        const EightOfDh& dh, float* turn = nullptr) {
+  const uint32_t left = c < p.n ? p.n - c : 0;  // outputs that exist
+  const bool here = token < p.tokens;
+  if (GRAD) {
+    float d[8], gate[8], up[8];
+    dh.values(p.dtype, d);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) gradients<ACT>(a[k], b[k], d[k], &gate[k], &up[k]);
+    if (here) {
+      const int64_t at = (int64_t)token * p.ldd + c;
+      put8(p.dgate + at, gate, true, left);
+      put8(p.dup + at, up, true, left);
+    }
+  } else {
+    float h[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) h[k] = activate<ACT, false>(a[k], nullptr) * b[k];
+    if (turn) {
+      const uint32_t lane = threadIdx.x & 31, token0 = token - lane / 4, col = c - lane % 4 * 8 + lane;
+      __syncwarp();
+#pragma unroll
+      for (uint32_t k = 0; k < 8; k += 4)
+        *reinterpret_cast<float4*>(turn + place(lane / 4, lane % 4 * 8 + k)) = make_float4(h[k], h[k + 1], h[k + 2], h[k + 3]);
+      __syncwarp();
+      with_type(p.dtype, [&](auto* type) {
+        using T = std::remove_pointer_t<decltype(type)>;
+        T* const to = static_cast<T*>(p.h) + (int64_t)token0 * p.ldh + col;
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k)
+          if (token0 + k < p.tokens && col < p.n) to[k * p.ldh] = narrow<T>(turn[place(k, lane)]);
+      });
+    } else if (p.h && here) {
+      with_type(p.dtype, [&](auto* type) {
+        using T = std::remove_pointer_t<decltype(type)>;
+        put8(static_cast<T*>(p.h) + (int64_t)token * p.ldh + c, h, p.wide, left);
+      });
+    }
+    if (p.q.codes) put_four_bits<FMT>(p, t, token, c, here, h);
+  }
 }
 
 template <int FMT, uint32_t N, bool GRAD>
@@ -519,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                          const __grid_constant__ CUtensorMap up_s_map, const __grid_constant__ CUtensorMap x_s_map,
                          const __grid_constant__ PairParams p) {
   using S = GatedSizes<FMT, N>;
-  constexpr uint32_t KT = S::KT, STAGES = S::kStages, HALF = N / 4, MINE = S::kMine;
+  constexpr uint32_t KT = S::KT, STAGES = S::kStages, PART = N / 4;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ PairShared sm;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -528,14 +541,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     sm.abandoned = 0;
     for (uint32_t s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&sm.full[s]), 1);
+      mbar_init(smem_u32(&sm.raw[s]), 1);
+      mbar_init(smem_u32(&sm.scaled[s]), 2);
       mbar_init(smem_u32(&sm.empty[s]), 1);
     }
     mbar_init(smem_u32(&sm.sums_full), 1);
     mbar_init(smem_u32(&sm.sums_empty), 2 * kReaders);
-    for (uint32_t s = 0; s < kReaders; ++s) {
-      mbar_init(smem_u32(&sm.got[s]), 1), sm.sent[s] = 0;
-      mbar_init(smem_u32(&sm.room[s]), 1);
-    }
     mbar_init(smem_u32(&sm.spare), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -558,17 +569,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tile0 = blockIdx.x / 2 / p.split, stride = p.split > 1 ? p.tiles : gridDim.x / 2;
   const uint32_t first = p.steps * share / p.split, steps = p.steps * (share + 1) / p.split - first;  // (steps < 2^24, share < 4)
   const Finish& f = p.f;
-  uint32_t expected = 0, taken = 0;  // exchanges of this warp
 
   if (warp >= kCopyWarp && warp < kMmaWarp) {
     const bool of_w = warp == kCopyWarp;  // one warp for the weights' codes and scales, one for x's
-    const CUtensorMap* const w_map = rank ? &up_map : &gate_map;
-    const CUtensorMap* const w_s_map = rank ? &up_s_map : &gate_s_map;
     uint32_t i = 0;
     bool ok = true;
     for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride) {
       const uint32_t row0 = of_w ? tile / p.x_tiles * kTileW : tile % p.x_tiles * N;
-      const int row = (int)(row0 + (of_w ? 0 : rank * (N / 2)));
+      const int row = (int)(row0 + rank * (of_w ? kOutputs : N / 2));
       const int strip = (int)(row0 / kStrip * p.strip_rows);
       for (uint32_t step = first; step < first + steps; ++step, ++i) {
         const uint32_t s = i % STAGES, to = base + s * S::kStageAligned;
@@ -577,9 +585,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t bar = cluster_address(smem_u32(&sm.full[s]), lead);
         const int col = (int)(step * kRowBytes), scales = strip + (int)(step * (KT * 4));
         if (of_w) {
-          if (rank == 0) expect_bytes(smem_u32(&sm.full[s]), 2 * S::kStage);
-          tma_load_pair(to, w_map, col, row, bar);
-          tma_load_pair(to + S::kWs, w_s_map, 0, scales, bar);
+          if (rank == 0) expect_bytes(smem_u32(&sm.full[s]), 2 * S::kWs);
+          expect_bytes(smem_u32(&sm.raw[s]), 2 * KT * kTileBytes);
+          tma_load(to + S::kRaw, &gate_s_map, 0, scales, smem_u32(&sm.raw[s]));
+          tma_load(to + S::kRaw + KT * kTileBytes, &up_s_map, 0, scales, smem_u32(&sm.raw[s]));
+          tma_load_pair(to, &gate_map, col, row, bar);
+          tma_load_pair(to + kOutputs * kRowBytes, &up_map, col, row, bar);
         } else {  // both blocks multiply by all of the tile's rows of x
           tma_load_pair(to + S::kX, &x_map, col, row, bar);
           tma_load_pair(to + S::kXs, &x_s_map, 0, scales, bar);
@@ -587,9 +598,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (*abandoned && rank == 0)  // what was issued lands before the blocks' memory is another's
+    if (*abandoned)  // what was issued lands before the blocks' memory is another's
       for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
-        if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
+        if (j != p.withhold) {
+          if (rank == 0) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
+          if (of_w) drain(smem_u32(&sm.raw[j % STAGES]), (j / STAGES) & 1);
+        }
   } else if (warp == kMmaWarp) {
     if (rank == 0) {
       // e2m1 both, N, M = 256, type of the scales
@@ -603,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         for (uint32_t step = 0; step < steps && ok; ++step) {
           const uint32_t s = i % STAGES, from = base + s * S::kStageAligned;
-          ok = wait(smem_u32(&sm.full[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
+          ok = wait_both(smem_u32(&sm.full[s]), smem_u32(&sm.scaled[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins);
           if (!ok) break;
           tc_fence_after();
           const uint32_t sfa = tmem + N + s * S::kScaleCols, sfb = sfa + KT * 4;
@@ -620,117 +634,130 @@ __global__ void __launch_bounds__(kThreads, 1)
         drain(smem_u32(&sm.spare), 0);
       }
     }
+  } else if (warp == kScaleWarp) {
+    // Scales of row r lie in 16 bytes of r % 32, four to each of four rows 32 apart: of the strip's 128 rows this block has the first or the
+    // last 64 of either matrix, eight bytes.
+    const uint32_t left = tile0 < p.tiles ? (p.tiles - tile0 + stride - 1) / stride : 0;
+    const uint32_t scaled0 = cluster_address(smem_u32(&sm.scaled[0]), lead);
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint32_t n = 0; n < left && ok; ++n)
+      for (uint32_t step = 0; step < steps; ++step, ++i) {
+        const uint32_t s = i % STAGES;
+        if (!(ok = wait(smem_u32(&sm.raw[s]), (i / STAGES) & 1, abandoned, p.status, p.max_spins))) break;
+        unsigned char* const stage = mem + s * S::kStageAligned;
+#pragma unroll
+        for (uint32_t t = 0; t < KT; ++t) {
+          const uint2 g = *reinterpret_cast<const uint2*>(stage + S::kRaw + t * kTileBytes + lane * 16 + rank * 8);
+          const uint2 u = *reinterpret_cast<const uint2*>(stage + S::kRaw + (KT + t) * kTileBytes + lane * 16 + rank * 8);
+          *reinterpret_cast<uint4*>(stage + S::kWs + t * kTileBytes + lane * 16) = make_uint4(g.x, g.y, u.x, u.y);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the products
+        __syncwarp();
+        if (lane == 0) cluster_arrive(scaled0 + s * 8);
+        __syncwarp();
+      }
   } else {
     const float x_ts = f.x_ts ? *f.x_ts : 1.0f;
     const Factors gate(f.gate_ts ? *f.gate_ts : 1.0f, x_ts), up(f.up_ts ? *f.up_ts : 1.0f, x_ts);
+    const bool scaled = !(gate.first == 1.0f && gate.second == 1.0f && up.first == 1.0f && up.second == 1.0f);
     const TensorScale t(f.q.tensor_scale);
-    const uint32_t quarter = warp % 4, part = warp / 4;  // of the outputs, of the tokens
+    // A quarter of tensor memory's lanes, which have a (the lower two) or b of 32 outputs, and a quarter of the tokens.  The warp with b of the
+    // same outputs and tokens, or a, is its partner: both turn 16 tokens at a time, and each finishes eight of them.
+    const uint32_t quarter = warp % 4, part = warp / 4, of_b = quarter / 2, pair = part * 2 + quarter % 2;
     const uint32_t sums_empty = cluster_address(smem_u32(&sm.sums_empty), lead);
-    // of the other block: where this warp's sums go, and the barriers of the same warp
-    const uint32_t exchange = base + S::kExchangeAt + warp * kExchange, other = cluster_address(exchange, in_cluster ^ 1);
-    const uint32_t other_got = cluster_address(smem_u32(&sm.got[warp]), in_cluster ^ 1);
-    const uint32_t other_room = cluster_address(smem_u32(&sm.room[warp]), in_cluster ^ 1);
-    const uint32_t other_sent = cluster_address(smem_u32(&sm.sent[warp]), in_cluster ^ 1);
-    float* const got = reinterpret_cast<float*>(mem + S::kExchangeAt + warp * kExchange);
-    float* const own = got + kGot / 4;
-    const float *const a_sums = rank ? got : own, *const b_sums = rank ? own : got;
+    float* const a_sums = reinterpret_cast<float*>(mem + S::kTurnAt + pair * (2 * kSums));
+    float* const b_sums = a_sums + kSums / 4;
+    float* const own = of_b ? b_sums : a_sums;
+    const uint32_t j = of_b * 8 + lane / 4;  // token of a round
+    const bool turned = !GRAD && f.h && !f.wide;
     uint32_t n = 0;
     bool ok = true;
     for (uint32_t tile = tile0; tile < p.tiles && ok; tile += stride, ++n) {
-      const uint32_t col0 = tile / p.x_tiles * kTileW + quarter * 32, row = tile % p.x_tiles * N + part * HALF + rank * MINE;
-      if (GRAD && p.split == 1 && lane < MINE && row + lane < f.tokens && col0 < f.n) {
-        // what will be needed of dh, on its way to the L2 beside the products
-        const uint32_t size = f.dtype == PVT_F32 ? 4 : 2;
-        const char* const at = static_cast<const char*>(f.dh) + ((int64_t)(row + lane) * f.ldh + col0) * size;
-        ask_l2(at), ask_l2(at + (min(32u, f.n - col0) - 1) * size);
-      }
-      ok = wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins);
+      const uint32_t c = tile / p.x_tiles * kTileW + rank * kOutputs + quarter % 2 * 32 + lane % 4 * 8;
+      const uint32_t row = tile % p.x_tiles * N + part * PART, left = c < f.n ? f.n - c : 0;
+      if (GRAD && p.split == 1 && left > 0)  // what will be needed of dh, on its way to the L2 beside the products
+        for (uint32_t r = 0; r < PART; r += kRound)
+          if (row + r + j < f.tokens)
+            ask_l2(static_cast<const char*>(f.dh) + ((int64_t)(row + r + j) * f.ldh + c) * (f.dtype == PVT_F32 ? 4 : 2));
+      ok = pair_agrees(pair + 1, wait(smem_u32(&sm.sums_full), n & 1, abandoned, p.status, p.max_spins));
       if (!ok) break;
       tc_fence_after();
-      // the tokens that this block finishes, then those that the other one does
-      uint32_t v[HALF];
+      uint32_t v[PART];
 #pragma unroll
-      for (uint32_t j = 0; j < HALF; j += MINE) {
-        const uint32_t from = tmem + (quarter << 21) + part * HALF + ((j == 0) == (rank == 0) ? 0 : MINE);
-        if (MINE == 32)
-          tmem_ld32(from, v + j);
-        else
-          tmem_ld16(from, v + j);
-      }
-      tmem_ld_wait<(int)HALF>(v);
+      for (uint32_t k = 0; k < PART; k += 32) tmem_ld32(tmem + (quarter << 21) + part * PART + k, v + k);
+      tmem_ld_wait<(int)PART>(v);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) cluster_arrive(sums_empty);
       __syncwarp();
       if (p.split > 1) {  // the products are done: the stages hold the partial sums
 #pragma unroll
-        for (uint32_t j = 0; j < HALF; ++j) {
-          const uint32_t token = part * HALF + ((j < MINE) == (rank == 0) ? 0 : MINE) + j % MINE;
-          reinterpret_cast<float*>(mem)[token * kTileW + quarter * 32 + lane] = __uint_as_float(v[j]);
-        }
+        for (uint32_t k = 0; k < PART; ++k)
+          reinterpret_cast<float*>(mem)[(part * PART + k) * kTileW + quarter * 32 + lane] = __uint_as_float(v[k]);
         break;
       }
+      with_activation(f.activation, [&](auto act) {
+        EightOfDh dh;
+        if (GRAD) dh.ask(f, row + j, c, left);
 #pragma unroll
-      for (uint32_t r = 0; r < MINE; r += kRound) {
-        if (taken > 0) ok = wait<true>(smem_u32(&sm.room[warp]), (taken - 1) & 1, abandoned, p.status, p.max_spins);
-        if (!ok) break;
+        for (uint32_t r = 0; r < PART; r += kRound) {
 #pragma unroll
-        for (uint32_t j = 0; j < kRound; ++j)
-          asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(other + place(j, lane) * 4),
-                       "r"(v[MINE + r + j]), "r"(other_got)
-                       : "memory");
-        if (lane == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other_sent), "r"(taken + 1) : "memory");
-        expect_bytes(smem_u32(&sm.got[warp]), kGot);
-        ++expected;
+          for (uint32_t k = 0; k < kRound; ++k) own[place(k, lane)] = __uint_as_float(v[r + k]);
+          pair_sync(pair + 1);
+          float a[8], b[8];
 #pragma unroll
-        for (uint32_t j = 0; j < kRound; ++j) own[place(j, lane)] = __uint_as_float(v[r + j]);
-        __syncwarp();
-        finish_round<FMT, GRAD>(f, gate, up, t, row + r, col0, a_sums, b_sums, [&] {
-          return ok = wait<true>(smem_u32(&sm.got[warp]), taken & 1, abandoned, p.status, p.max_spins);
-        });
-        if (!ok) break;
-        ++taken;
-        __syncwarp();
-        if (lane == 0) cluster_arrive(other_room);
-        __syncwarp();
-      }
+          for (uint32_t k = 0; k < 8; k += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(a_sums + place(j, lane % 4 * 8 + k));
+            const float4 y = *reinterpret_cast<const float4*>(b_sums + place(j, lane % 4 * 8 + k));
+            a[k] = x.x, a[k + 1] = x.y, a[k + 2] = x.z, a[k + 3] = x.w, b[k] = y.x, b[k + 1] = y.y, b[k + 2] = y.z, b[k + 3] = y.w;
+          }
+          if (!turned) pair_sync(pair + 1);  // (the next round's sums may come)
+          if (scaled) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) a[k] = gate(a[k]), b[k] = up(b[k]);
+          }
+          EightOfDh now = dh;
+          if (GRAD && r + kRound < PART) dh.ask(f, row + r + kRound + j, c, left);
+          finish8<FMT, GRAD, decltype(act)::value>(f, t, row + r + j, c, a, b, now, turned ? a_sums + of_b * 256 : nullptr);
+          if (turned) pair_sync(pair + 1);
+        }
+      });
+      __syncwarp();
     }
   }
   __syncthreads();
-  cluster_sync();  // neither block leaves while the other's copies, products or sums reach it
-  if (*abandoned && warp < (uint32_t)kReaders && *static_cast<volatile uint32_t*>(&sm.sent[warp]) > taken) {
-    // sums that are on their way to a warp that has not waited for them
-    if (expected == taken) expect_bytes(smem_u32(&sm.got[warp]), kGot);
-    drain(smem_u32(&sm.got[warp]), taken & 1);
-  }
+  cluster_sync();  // neither block leaves while the other's copies, products or arrivals reach it
   if (p.split > 1) {
-    // every block adds up and finishes the tokens that are its share, one to a warp, always in the order of pairs
-    const uint32_t col0 = tile0 / p.x_tiles * kTileW, row0 = tile0 % p.x_tiles * N, blocks = 2 * p.split;
+    // every pair adds up and finishes the tokens that are its share, four to a warp, always in the order of pairs; a lane has eight outputs
+    const uint32_t col0 = tile0 / p.x_tiles * kTileW + rank * kOutputs, row0 = tile0 % p.x_tiles * N;
     if (!*abandoned) {
       const float x_ts = f.x_ts ? *f.x_ts : 1.0f;
       const Factors gate(f.gate_ts ? *f.gate_ts : 1.0f, x_ts), up(f.up_ts ? *f.up_ts : 1.0f, x_ts);
       const TensorScale t(f.q.tensor_scale);
-      float* const scratch = reinterpret_cast<float*>(mem + S::kExchangeAt) + warp * 128;
-      const uint32_t tokens = min(N, f.tokens - row0);
-      for (uint32_t j = in_cluster + warp * blocks; j < tokens; j += kThreads / 32 * blocks) {
-        float v[2][4][4], a[4], b[4];  // (all under way at once: a load from another block takes a thousand cycles)
+      const uint32_t c = col0 + lane % 8 * 8, left = c < f.n ? f.n - c : 0;
+      for (uint32_t j0 = (share + warp * p.split) * 4; j0 < N; j0 += kThreads / 32 * p.split * 4) {
+        const uint32_t j = j0 + lane / 8, token = row0 + j;
+        EightOfDh dh;
+        if (GRAD) dh.ask(f, token, c, left);
+        float a[8], b[8];
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)
+        for (int k = 0; k < 8; ++k) a[k] = b[k] = 0.0f;
+        if (row0 + j0 < f.tokens)
+          for (uint32_t q = 0; q < p.split; ++q) {
+            float x[8], y[8];  // (all under way at once: a load from another block takes a thousand cycles)
 #pragma unroll
-          for (uint32_t q = 0; q < 4; ++q) {
-            const uint32_t at = base + (j * kTileW + i * 32 + lane) * 4;
-            v[0][i][q] = q < p.split ? cluster_load(at, 2 * q) : 0.0f;
-            v[1][i][q] = q < p.split ? cluster_load(at, 2 * q + 1) : 0.0f;
+            for (uint32_t k = 0; k < 8; ++k) {
+              x[k] = cluster_load(base + (j * kTileW + lane % 8 * 8 + k) * 4, 2 * q + rank);
+              y[k] = cluster_load(base + (j * kTileW + kOutputs + lane % 8 * 8 + k) * 4, 2 * q + rank);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) a[k] += x[k], b[k] += y[k];
           }
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-          a[i] = gate(v[0][i][0] + v[0][i][1] + v[0][i][2] + v[0][i][3]);
-          b[i] = up(v[1][i][0] + v[1][i][1] + v[1][i][2] + v[1][i][3]);
-        }
-        finish_token<FMT, GRAD>(f, t, row0 + j, col0, a, b, scratch);
+        for (int k = 0; k < 8; ++k) a[k] = gate(a[k]), b[k] = up(b[k]);
+        with_activation(f.activation, [&](auto act) { finish8<FMT, GRAD, decltype(act)::value>(f, t, token, c, a, b, dh); });
       }
-      if (!GRAD && f.q.codes && in_cluster == 0)
-        clear_scales<FMT>(f, max(row0, f.tokens), min(row0 + N, f.padded), col0, tid, kThreads);
     }
     cluster_sync();  // nor while another reads its partial sums
   }
@@ -756,7 +783,7 @@ cudaError_t gated_pairs(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, con
   const pvt_mx* const of[3] = {&wg, &wu, &x};
   for (int i = 0; i < 3; ++i) {
     cudaError_t e = make_map(&maps[i], of[i]->codes, 1, (uint64_t)of[i]->rows, ((uint64_t)of[i]->cols + 1) / 2, (uint64_t)of[i]->ld,
-                             i < 2 ? kTileW : N / 2);
+                             i < 2 ? kOutputs : N / 2);
     if (e == cudaSuccess)
       e = make_map(&maps[3 + i], of[i]->scales, 1, scale_bytes(of[i]->rows, of[i]->cols, FMT) / 128, 128, 128, S::KT * 4, 128, false);
     if (e != cudaSuccess) return e;
