@@ -540,7 +540,14 @@ cudaError_t start(const CUtensorMap& a_map, const CUtensorMap& a2_map, GradParam
   uint32_t grid = 2 * (p.tiles < (uint32_t)sm_count / 2 ? p.tiles : (uint32_t)sm_count / 2), cluster = 2;
   if (CTAS == 1) {
     p.split = 1;
-    while (p.split < 8 && (uint64_t)p.tiles * p.split * 2 <= (uint64_t)sm_count && p.split * 2 <= p.steps) p.split *= 2;
+    if (TWO) {
+      // any number of blocks to a tile, as long as all clusters run at once (eighteen SMs or so find each other): 77 tokens 5119 by 4095, 40
+      // tiles by two and by three blocks, 31 and 24 us
+      for (uint32_t n = 2; n <= 8 && 4 * n <= p.steps; ++n)
+        if ((uint64_t)p.tiles * n <= (uint64_t)sm_count && p.tiles <= 8 * ((uint32_t)sm_count / 8 / n)) p.split = n;
+    } else {
+      while (p.split < 8 && (uint64_t)p.tiles * p.split * 2 <= (uint64_t)sm_count && p.split * 2 <= p.steps) p.split *= 2;
+    }
     grid = p.tiles * p.split, cluster = p.split;
   }
   return launch_clusters(mx_grad_kernel<T, FMT, TRANS, MT, CTAS, TWO>, grid, cluster, kThreads, S::kBytes, stream, a_map, q_map,
