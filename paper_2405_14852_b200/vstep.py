@@ -4,7 +4,7 @@ All computation happens in the CUDA library (``binding``); this class only owns
 the device tensors, the workspace and the call order
 select -> encode -> dequantise of one step (Algorithm 3, V-step lines and
 ``dequantize_weights``), and what a layer gives to and takes from the pass that its
-update comes from.
+update comes from.  ``FeedForward`` is such a pass through three layers.
 """
 from __future__ import annotations
 
@@ -150,3 +150,82 @@ class VStepLayer:
 
     def status(self) -> int:
         return B.pvt_status(self.reserve(1))
+
+
+class FeedForward:
+    """The feed-forward half of a student's block, in the pass between two V steps (Algorithm 3, forward and backward lines; the
+    paper's models have it in this form): norm of the residual stream, gated pair, and the layer that leads back.
+
+        total = x + residual,  n = norm(total),  y = (f(n gate^T) * (n up^T)) down^T
+
+    Weights and activations are held in 4 bits (``fmt``), gradients go straight through that.  ``backward`` adds to the g of the
+    three layers, which their V steps take, and to the gradients of the norm's weights (float64, as ``pvt_adam_update`` takes
+    them).  ``quantize`` again after each step."""
+
+    def __init__(self, gate: VStepLayer, up: VStepLayer, down: VStepLayer, weight: torch.Tensor,
+                 bias: Optional[torch.Tensor] = None, *, kind: int = B.PVT_NORM_RMS, eps: float = 1e-5,
+                 activation: int = B.PVT_ACT_SILU, fmt: int = B.PVT_MX_E8M0_32):
+        if (gate.rows, gate.cols) != (up.rows, up.cols) or (gate.rows, gate.cols) != (down.cols, down.rows):
+            raise ValueError("gate and up have to be of one shape, down of its transpose")
+        if weight.numel() != gate.cols or (bias is not None and bias.numel() != gate.cols):
+            raise ValueError("the norm has a weight (and bias) for each input of gate and up")
+        self.gate, self.up, self.down = gate, up, down
+        self.weight, self.bias, self.kind, self.eps, self.activation, self.fmt = weight, bias, kind, eps, activation, fmt
+        self.dweight = torch.zeros(gate.cols, dtype=torch.float64, device=weight.device)
+        self.dbias = None if bias is None else torch.zeros_like(self.dweight)
+        self.w_gate = self.w_up = self.w_down = self._kept = self._workspace = None
+
+    def quantize(self) -> None:
+        """The three layers' weights, as their codes are now, in 4 bits.  Of PVT_MX_E4M3_16 gate and up share a tensor scale: the
+        gradient by their common input is one sum over both."""
+        shared = own = None
+        if self.fmt == B.PVT_MX_E4M3_16:
+            top = [layer.dequant().abs().amax() for layer in (self.gate, self.up, self.down)]
+            shared, own = ((t / (6.0 * 448.0)).reshape(1) for t in (torch.maximum(top[0], top[1]), top[2]))
+        self.w_gate = self.gate.quantized(self.fmt, shared, out=self._again(self.w_gate, shared))
+        self.w_up = self.up.quantized(self.fmt, shared, out=self._again(self.w_up, shared))
+        self.w_down = self.down.quantized(self.fmt, own, out=self._again(self.w_down, own))
+
+    def _again(self, held: Optional[B.Mx], scale: Optional[torch.Tensor]) -> Optional[B.Mx]:
+        """The room of an earlier call."""
+        return held and B.make_mx(held.codes, held.scales, held.rows, held.cols, self.fmt, tensor_scale=scale)
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
+        """y (bfloat16) and total (x's type, the next residual) of x [tokens, inputs]; what backward needs is kept until the next call."""
+        if self.w_gate is None:
+            self.quantize()
+        tokens, device = x.shape[0], x.device
+        total = torch.empty_like(x) if residual is not None else x
+        stats = torch.empty(tokens, 2, device=device)
+        xq, hq = (B.new_mx(tokens, cols, self.fmt, device=device) for cols in (self.gate.cols, self.gate.rows))
+        y = torch.empty(tokens, self.down.rows, dtype=torch.bfloat16, device=device)
+        n = B.make_norm(x, self.weight, self.bias, kind=self.kind, eps=self.eps, residual=residual)
+        B.pvt_norm_apply(n, quantized=xq, total=total if residual is not None else None, stats=stats)
+        B.pvt_mx_gated(xq, self.w_gate, self.w_up, quantized=hq, activation=self.activation)
+        B.pvt_mx_product(hq, self.w_down, y)
+        self._kept = (total, stats, xq, hq)
+        return y, total
+
+    def backward(self, dy: torch.Tensor, dtotal: Optional[torch.Tensor] = None, first: bool = False) -> torch.Tensor:
+        """The gradient by x and by the residual (one and the same, bfloat16) from those by y and, if anything else reads it, by total.  The
+        layers' and the norm's gradients are added to; with first they start anew."""
+        if self._kept is None:
+            raise RuntimeError("backward follows a call of forward")
+        total, stats, xq, hq = self._kept
+        tokens, device = total.shape[0], total.device
+        dh, dup = (torch.empty(tokens, self.gate.rows, dtype=torch.bfloat16, device=device) for _ in range(2))
+        dx = torch.empty(tokens, self.gate.cols, dtype=torch.bfloat16, device=device)
+        B.pvt_mx_grad_input(dy, self.w_down, dh)
+        self.down.accumulate_grad(dy, hq, first=first)
+        dgate = dh
+        B.pvt_mx_gated_grad(xq, self.w_gate, self.w_up, dh, dgate, dup, activation=self.activation)
+        self.gate.accumulate_grad(dgate, xq, first=first)
+        self.up.accumulate_grad(dup, xq, first=first)
+        B.pvt_mx_gated_grad_input(dgate, dup, self.w_gate, self.w_up, dx)
+        n = B.make_norm(total, self.weight, self.bias, kind=self.kind, eps=self.eps)
+        need = B.pvt_norm_workspace_bytes(n)
+        if self._workspace is None or self._workspace.numel() < need:
+            self._workspace = B.new_norm_workspace(n)
+        B.pvt_norm_grad(n, stats, dx, dx, dresidual=dtotal, dweight=self.dweight, dbias=self.dbias, accumulate=not first,
+                        workspace=self._workspace)
+        return dx
