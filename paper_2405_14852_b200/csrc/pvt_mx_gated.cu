@@ -3,8 +3,8 @@
 // operations, where keeping them would take four bytes an element and two more passes over memory).
 //
 // Up to 16 tokens: the product's kernel for few tokens, by clusters whose even blocks multiply by 128 rows of wg and whose odd ones by
-// the same rows of wu, each pair its share of the steps.  The partial sums meet in shared memory across the cluster, always in the
-// order of ranks, and whoever adds up a token's sums finishes it.
+// the same rows of wu, each pair its share of the steps.  A token's partial sums go to the block that finishes it, where they are added
+// up in the order of ranks; behind the one barrier of the cluster no block needs another.
 //
 // From 17 tokens on: the product's pairs of blocks, 256 rows of weights by 256 (or 128) of x to a tile; but a block's 128 rows are 64
 // of wg and the same 64 of wu.  The main loop, its traffic (32 KB of codes a step and SM) and its rate are the product's; only scales
@@ -175,11 +175,20 @@ struct FewShared {
   uint32_t tmem, abandoned;
 };
 
+// the product's, but for shared memory that the cluster's sums have to themselves: other blocks write there while this one multiplies
+template <int FMT>
+struct GatedFewSizes : FewSizes<FMT> {
+  using F = FewSizes<FMT>;
+  static constexpr uint32_t kStages = 104 * 1024 / F::kStageAligned;  // of two blocks per SM
+  static constexpr uint32_t kSumsAt = kStages * F::kStageAligned;
+  static constexpr size_t kBytes = kSumsAt + kFewTokens * kTileW * 4 + 1024;
+};
+
 template <int FMT, bool GRAD>
 __global__ void __launch_bounds__(kFewThreads)
     mx_gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map,
                         const __grid_constant__ CUtensorMap x_map, const __grid_constant__ FewParams p) {
-  using S = FewSizes<FMT>;
+  using S = GatedFewSizes<FMT>;
   constexpr uint32_t KT = S::KT, STAGES = S::kStages;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ FewShared sm;
@@ -195,6 +204,10 @@ __global__ void __launch_bounds__(kFewThreads)
   if (tid < (uint32_t)kTileW && w0 + tid < p.f.n)
     prefetch_l2((of_up ? p.up_codes : p.gate_codes) + (int64_t)(w0 + tid) * (of_up ? p.up_ld : p.gate_ld) + from_byte, to_byte - from_byte);
   if (tid == (uint32_t)kTileW) prefetch_l2(w_scales + (size_t)first * (KT * kTileBytes), (last - first) * (KT * kTileBytes));
+  if (tid == kTileW + 1) {  // (descriptors, which the launch has brought along)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(of_up ? &up_map : &gate_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&x_map) : "memory");
+  }
   if (tid == 0) {
     sm.abandoned = 0;
     for (uint32_t s = 0; s < STAGES; ++s) {
@@ -214,10 +227,20 @@ __global__ void __launch_bounds__(kFewThreads)
   tc_fence_after();
   pdl_trigger();  // not before this block has its tensor memory: the next kernel's blocks hold theirs while they wait for this one
   pdl_wait();
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // that this block has started; awaited where others' memory is written
 
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
   const Finish& f = p.f;
+  const float* const sums = reinterpret_cast<const float*>(raw + (base - smem_u32(raw)) + S::kSumsAt);
+  const uint32_t log = 31 - __clz((int)blocks), slots = kFewTokens >> log;  // tokens of a block (of two, four or eight)
+  auto all_started = [] {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  };
+  Factors gate(1.0f, 1.0f), up(1.0f, 1.0f);
+  TensorScale t(nullptr);
 
   if (warp == kFewCopyWarp) {
     const CUtensorMap* const w_map = of_up ? &up_map : &gate_map;
@@ -235,6 +258,7 @@ __global__ void __launch_bounds__(kFewThreads)
     if (*abandoned)  // what was issued lands before the block's memory is another's
       for (uint32_t j = i > STAGES ? i - STAGES : 0; j < i; ++j)
         if (j != p.withhold) drain(smem_u32(&sm.full[j % STAGES]), (j / STAGES) & 1);
+    all_started();
   } else if (warp == kFewMmaWarp) {
     // e2m1 both, N = 16, M = 128, type of the scales
     constexpr uint32_t idesc =
@@ -267,43 +291,41 @@ __global__ void __launch_bounds__(kFewThreads)
       commit(smem_u32(&sm.spare));
       drain(smem_u32(&sm.spare), 0);
     }
+    all_started();
   } else {
-    float* const part = reinterpret_cast<float*>(raw + (base - smem_u32(raw)));
+    const float x_ts = f.x_ts ? *f.x_ts : 1.0f;
+    gate = Factors(f.gate_ts ? *f.gate_ts : 1.0f, x_ts), up = Factors(f.up_ts ? *f.up_ts : 1.0f, x_ts);
+    t = TensorScale(f.q.tensor_scale);
+    all_started();
     if (wait(smem_u32(&sm.done), 0, abandoned, p.status, p.max_spins)) {
       tc_fence_after();
       uint32_t v[kFewTokens];
       tmem_ld16(tmem + (warp << 21), v);
       tmem_ld_wait<kFewTokens>(v);
+      const uint32_t to = base + S::kSumsAt + (rank * slots * kTileW + tid) * 4;
 #pragma unroll
-      for (uint32_t j = 0; j < kFewTokens; ++j) part[j * kTileW + tid] = __uint_as_float(v[j]);
+      for (uint32_t j = 0; j < kFewTokens; ++j)
+        if (j < f.tokens)
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_address(to + (j >> log) * (kTileW * 4), j & (blocks - 1))), "r"(v[j])
+                       : "memory");
       tc_fence_before();
     }
     if (!GRAD && f.q.codes && rank == 0) clear_scales<FMT>(f, f.tokens, f.padded, w0, tid, 128);
   }
-  cluster_sync();
-  // every block adds up and finishes the tokens that are its share, one to a warp
-  if (warp < 4 && !*abandoned) {
-    const Factors gate(f.gate_ts ? *f.gate_ts : 1.0f, f.x_ts ? *f.x_ts : 1.0f), up(f.up_ts ? *f.up_ts : 1.0f, f.x_ts ? *f.x_ts : 1.0f);
-    const TensorScale t(f.q.tensor_scale);
-    for (uint32_t j = rank + warp * blocks; j < f.tokens; j += 4 * blocks) {
-      float a[4], b[4], v[2][4][4];
+  cluster_sync();  // a block's sums are there, from all of its cluster
+  if (warp < 4 && !*abandoned)
+    for (uint32_t k = warp; rank + k * blocks < f.tokens; k += 4) {  // a token to a warp
+      float a[4] = {0.0f, 0.0f, 0.0f, 0.0f}, b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (uint32_t q = 0; q < p.split; ++q)
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          const uint32_t at = base + (j * kTileW + i * 32 + lane) * 4;
-          v[0][i][q] = q < p.split ? cluster_load(at, 2 * q) : 0.0f;
-          v[1][i][q] = q < p.split ? cluster_load(at, 2 * q + 1) : 0.0f;
+        for (uint32_t i = 0; i < 4; ++i) {
+          a[i] += sums[(2 * q * slots + k) * kTileW + i * 32 + lane];
+          b[i] += sums[((2 * q + 1) * slots + k) * kTileW + i * 32 + lane];
         }
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) {
-        a[i] = gate(v[0][i][0] + v[0][i][1] + v[0][i][2] + v[0][i][3]);
-        b[i] = up(v[1][i][0] + v[1][i][1] + v[1][i][2] + v[1][i][3]);
-      }
-      finish_token<FMT, GRAD>(f, t, j, w0, a, b, scratch[warp]);
+      for (uint32_t i = 0; i < 4; ++i) a[i] = gate(a[i]), b[i] = up(b[i]);
+      finish_token<FMT, GRAD>(f, t, rank + k * blocks, w0, a, b, scratch[warp]);
     }
-  }
-  cluster_sync();  // no block leaves while another reads its partial sums
   __syncthreads();
   if (warp == kFewMmaWarp) {
     tc_fence_after();
@@ -798,7 +820,7 @@ cudaError_t gated_pairs(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, con
 
 template <int FMT, bool GRAD>
 cudaError_t gated(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, const Finish& f, uint32_t* status, int sm_count, cudaStream_t stream) {
-  using S = FewSizes<FMT>;
+  using S = GatedFewSizes<FMT>;
   const uint64_t tiles = ((uint64_t)f.n + kTileW - 1) / kTileW;
   if (f.tokens > kFewTokens)
     return narrow_tiles((int32_t)f.tokens, tiles, sm_count) ? gated_pairs<FMT, 128, GRAD>(x, wg, wu, f, status, sm_count, stream)
