@@ -249,8 +249,8 @@ struct Place {
       each(g, [&](int i) { row[col(g) + i * step] = narrow<T>(v[i]); });
     }
   }
-  // the weights of its columns, `other` where there are none
-  __device__ __forceinline__ void weights(const void* w, int32_t dtype, float other, float (*v)[8]) const {
+  // the weights of its columns, `other` where there are none; wide: eight of them begin on 16 bytes
+  __device__ __forceinline__ void weights(const void* w, int32_t dtype, bool wide, float other, float (*v)[8]) const {
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -259,7 +259,16 @@ struct Place {
     with_type(dtype, [&](auto* type) {
       using U = std::remove_pointer_t<decltype(type)>;
 #pragma unroll
-      for (int g = 0; g < G; ++g) each(g, [&](int i) { v[g][i] = widen<U>(static_cast<const U*>(w)[col(g) + i * step]); });
+      for (int g = 0; g < G; ++g) {
+        const U* const from = static_cast<const U*>(w) + col(g);
+        if (WIDE && wide && full(g)) {
+          const Eight<U> e = *reinterpret_cast<const Eight<U>*>(from);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[g][i] = widen<U>(e.v[i]);
+        } else {
+          each(g, [&](int i) { v[g][i] = widen<U>(from[i * step]); });
+        }
+      }
     });
   }
 };

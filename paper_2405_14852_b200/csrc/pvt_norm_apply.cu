@@ -33,7 +33,7 @@ struct ApplyParams {
   uint32_t stages;  // two or three
   int32_t w_dtype, y_dtype;
   float eps;
-  bool layer;
+  bool layer, w_wide;
 };
 
 // G: spans of a warp, R: rows of a team at a time
@@ -67,8 +67,8 @@ __global__ void __launch_bounds__(L == kRagged ? kRaggedBound : kMostThreads) no
   uint64_t row0 = (uint64_t)set * s.teams * R + at.team;
   for (uint32_t k = 0; k + 1 < p.stages; ++k) ask(row0 + (uint64_t)k * stride, k);
   float w[G][8], b[G][8];
-  at.weights(p.weight, p.w_dtype, 1.0f, w);
-  at.weights(p.bias, p.w_dtype, 0.0f, b);
+  at.weights(p.weight, p.w_dtype, p.w_wide, 1.0f, w);
+  at.weights(p.bias, p.w_dtype, p.w_wide, 0.0f, b);
   const float inv = 1.0f / (float)s.cols;
   uint32_t turn = 0, k = 0;
   // (all of a block's teams go round as often as its first one)
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(L == kRagged ? kRaggedBound : kMostThreads) no
           }
         }
         if (p.total && row < s.rows) at.put(static_cast<T*>(p.total) + (int64_t)row * p.ldt, g, v[r][g]);
-        mean[r] += sum8(v[r][g]);
+        if (p.layer) mean[r] += sum8(v[r][g]);
       }
     }
     if (p.layer) {
@@ -208,6 +208,8 @@ cudaError_t launch_apply(const pvt_norm& n, void* total, int64_t ldt, void* y, i
   p.weight = n.weight, p.bias = n.bias, p.w_dtype = n.weight_dtype;
   p.y = y, p.ldy = ldy, p.y_dtype = y_dtype, p.stats = stats, p.eps = n.eps, p.layer = n.kind == PVT_NORM_LAYER;
   p.padded = (uint32_t)n.rows;
+  const size_t w_size = n.weight_dtype == PVT_F32 ? 4 : 2;
+  p.w_wide = rows_aligned(n.weight, 0, w_size) && rows_aligned(n.bias, 0, w_size);
   if (yq) {
     p.q = mx::held(*yq);
     p.padded = (uint32_t)((n.rows + kStrip - 1) / kStrip * kStrip);

@@ -26,7 +26,7 @@ struct GradParams {
   uint32_t sets;              // blocks or clusters: sets of sums
   uint32_t stages;            // three or four
   int32_t w_dtype;
-  bool layer, sums[2];  // of dw and db
+  bool layer, w_wide, sums[2];  // of dw and db
 };
 
 // floats from one set of sums to the next: every set begins where a thread may store eight at once
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(L == kRagged && G == 1 ? kRaggedBound : kMostT
   uint64_t row = first + at.team;
   for (uint32_t k = 0; k + 2 < p.stages; ++k) ask(row + (uint64_t)k * stride, k);
   float w[G][8], dw[G][8], db[G][8], xh[G][8], u[G][8], sum[N] = {}, rstd = 0.0f;
-  at.weights(p.weight, p.w_dtype, 1.0f, w);
+  at.weights(p.weight, p.w_dtype, p.w_wide, 1.0f, w);
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -271,6 +271,7 @@ cudaError_t launch_grad(const pvt_norm& n, const float* stats, int32_t dtype, co
   p.x = n.x, p.ldx = n.ldx, p.dy = dy, p.lddy = lddy, p.dres = dres, p.lddr = lddr, p.dx = dx, p.lddx = lddx;
   p.weight = n.weight, p.w_dtype = n.weight_dtype, p.stats = stats, p.layer = n.kind == PVT_NORM_LAYER;
   p.sums[0] = dweight, p.sums[1] = dbias;
+  p.w_wide = rows_aligned(n.weight, 0, n.weight_dtype == PVT_F32 ? 4 : 2);
   p.partial = sums ? static_cast<float*>(ws) : nullptr;
   timing_begin(kKernNorm, stream);
   cudaError_t e = with_type(n.dtype, [&](auto* type) {
