@@ -17,8 +17,8 @@
  *
  * and the next step starts with dequantize_weights (Algorithm 3, first line).
  * This library is those three calls, and the operators of the pass between them that g comes from: products in
- * 4-bit block floating point with their gradients (pvt_mx_*), and the loss that trains the quantised model against
- * the one it was made from (pvt_distill_*).
+ * 4-bit block floating point with their gradients (pvt_mx_*), alone and in gated pairs, the norm ahead of them (pvt_norm_*), and
+ * the loss that trains the quantised model against the one it was made from (pvt_distill_*).
  *
  * Conventions
  *   - A layer is `rows x cols`, row-major.  Weight groups are `group_dim` = 8
@@ -503,6 +503,8 @@ int pvt_distill_grad(const pvt_distill* d, const float* stats, const float* upst
  *   y = (r - mean) * rstd * weight + bias
  * A row that holds a NaN or an infinity has results that are not numbers, no other row is touched by it; a sum of squares
  * beyond binary32 gives rstd = 0.  The weights and biases are continuous parameters of the P step like the codebooks.
+ * Rows that do not all begin on eight elements' boundary are read by aligned pieces of 16 bytes: what lies ahead of a row in its first
+ * piece, 15 bytes at most, is read and not looked at.
  */
 #define PVT_NORM_LAYER 0
 #define PVT_NORM_RMS 1

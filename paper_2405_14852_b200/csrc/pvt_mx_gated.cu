@@ -71,7 +71,10 @@ __device__ __forceinline__ float activate(float a, float* slope) {
     if (SLOPE) dz = fmaf(sq, 0.21406443848826f, 1.59576912160573f);
   }
   const float s = inverse(1.0f + exp_minus(z));  // (0 where the exponential is infinite)
-  if (SLOPE) *slope = fmaf(a * dz, s * (1.0f - s), s);
+  if (SLOPE) {
+    const float rest = s * (1.0f - s);
+    *slope = ACT == PVT_ACT_GELU_TANH && rest == 0.0f ? s : fmaf(a * dz, rest, s);  // (a dz / da is infinite from 1e13 on)
+  }
   return a * s;
 }
 // calls f with the activation as a constant

@@ -170,6 +170,26 @@ def test_large_and_small_products(tokens, act):
     close(dup, f, d_up, BF16)
 
 
+@pytest.mark.parametrize("tokens", [5, 40])
+@pytest.mark.parametrize("act", ACTS)
+def test_products_beyond_where_cubes_are_numbers(tokens, act):
+    """f' of a huge product is 0 or 1, where a^2 or a^3 is infinite in binary32 too."""
+    x, w = torch.zeros(tokens, 64, device="cuda"), torch.zeros(64, 64, device="cuda")
+    x[:, 0] = 2.0 ** 40
+    w[:, 0] = torch.tensor([2.0 ** 10, -2.0 ** 10, 2.0 ** 50, -2.0 ** 50, 2.0 ** 80, -2.0 ** 80, 0.0, 1.0]).cuda().repeat(8)
+    xm, wm, one = B.new_mx(tokens, 64, B.PVT_MX_E8M0_32), B.new_mx(64, 64, B.PVT_MX_E8M0_32), B.new_mx(64, 64, B.PVT_MX_E8M0_32)
+    B.pvt_mx_quantize(xm, x), B.pvt_mx_quantize(wm, w), B.pvt_mx_quantize(one, (w != 5) * torch.eye(1, 64, device="cuda") * 2.0 ** -40)
+    h, dh = torch.empty(tokens, 64, device="cuda"), torch.ones(tokens, 64, device="cuda")
+    dgate, dup = (torch.empty(tokens, 64, dtype=BF16, device="cuda") for _ in range(2))
+    B.pvt_mx_gated(xm, wm, one, h=h, activation=act)
+    B.pvt_mx_gated_grad(xm, wm, one, dh, dgate, dup, activation=act)
+    a = x @ w.T
+    want = torch.where(a > 0, a, torch.zeros_like(a))  # (a product with the other matrix of 1)
+    assert torch.equal(h, want) and torch.equal(dup, want.bfloat16())
+    slope = torch.where(a > 0, torch.ones_like(a), torch.where(a < 0, torch.zeros_like(a), torch.full_like(a, 0.5)))
+    assert torch.equal(dgate, slope.bfloat16())
+
+
 @pytest.mark.parametrize("tokens", [7, 60, 300])
 def test_what_is_not_a_number_stays_in_its_token_and_output(tokens):
     gen = torch.Generator("cuda").manual_seed(tokens)
