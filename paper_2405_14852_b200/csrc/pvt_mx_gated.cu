@@ -59,8 +59,15 @@ __device__ __forceinline__ float inverse(float v) {
 template <int ACT, bool SLOPE>
 __device__ __forceinline__ float activate(float a, float* slope) {
   if (ACT == PVT_ACT_GELU) {  // f = a phi, phi the normal distribution's function
-    const float phi = 0.5f * erfcf(a * -0.70710678118654752f);
-    if (SLOPE) *slope = fmaf(a * 0.39894228040143268f, exp_minus(0.5f * a * a), phi);
+    // phi(-|a|) = exp(-a^2 / 2) g(t): a polynomial in t = 1 / (1 + 0.3 |a|), fitted to the least largest relative error for |a| up to 14,
+    // beyond which the exponential is 0: 2^-24, and 2^-21.2 as binary32 works it out.  The slope takes the same exponential.  (erfcf and a
+    // second exponential: 2048 x 4096 by 11008 92 us, gradients with dx 374, with this 77 and 355, with the other activations 73 and 345.)
+    const float e = exp_minus(0.5f * a * a), t = inverse(fmaf(0.3f, fabsf(a), 1.0f));
+    float g = fmaf(0.0383782895f, t, -0.169166111f);
+    g = fmaf(g, t, 0.228660081f), g = fmaf(g, t, -0.0765064771f), g = fmaf(g, t, 0.142535524f), g = fmaf(g, t, 0.094683523f);
+    g = fmaf(g, t, 0.121920342f), g = fmaf(g, t, 0.119487689f), g = fmaf(g, t, 7.16887583e-06f);
+    const float phi = a > 0.0f ? fmaf(-e, g, 1.0f) : e * g;
+    if (SLOPE) *slope = fmaf(a * 0.39894228040143268f, e, phi);
     return a * phi;
   }
   // f = a s(z), s the logistic function; z = a, or twice sqrt(2 / pi) (a + 0.044715 a^3): (1 + tanh(y)) / 2 = s(2 y)
