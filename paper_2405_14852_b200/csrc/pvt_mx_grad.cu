@@ -389,7 +389,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (uint64_t i64 = group; i64 < left; i64 += kGroups) {
       const uint32_t i = (uint32_t)i64, hs = i % kHeld, s = i % STAGES;
       const unsigned char* const held = mem + S::kHeldAt + hs * S::kHeldBytes;
-      bool ok = wait(smem_u32(&sm.held[hs]), (i / kHeld) & 1, abandoned, p.status, p.max_spins);
+      // A parity tells two rounds of a slot apart, not three: a group may wait for its codes only once those of kHeld steps ago are in, and
+      // they may come later than younger ones.  Where the slots are a multiple of the groups it has seen to them itself; elsewhere
+      // it waits for its stage first, whose products come behind those of all steps ahead of them.
+      constexpr bool kStageFirst = kHeld % kGroups != 0;
+      static_assert(kHeld >= STAGES, "codes of kHeld steps ago were taken before the products of STAGES steps ago");
+      auto stage_free = [&] { return i < STAGES || wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins); };
+      bool ok = !kStageFirst || stage_free();
+      if (ok) ok = wait(smem_u32(&sm.held[hs]), (i / kHeld) & 1, abandoned, p.status, p.max_spins);
       if (!ok) break;
       uint4 codes[kItems];
       uint32_t scales[kItems];
@@ -404,8 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         else
           scales[it] = *reinterpret_cast<const uint16_t*>(held + at + atom * kTileBytes + (chunk & 1) * 2);
       }
-      if (i >= STAGES) ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins);
-      if (!ok) break;
+      if (!kStageFirst && !stage_free()) break;
       unsigned char* const to = mem + s * S::kStage + MT * kABytes + atom * 8192 + row * 128;
 #pragma unroll
       for (uint32_t it = 0; it < kItems; ++it)
