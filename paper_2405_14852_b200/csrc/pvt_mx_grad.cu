@@ -18,6 +18,8 @@
 // the steps of a tile are shared by a cluster of up to eight of them, whose partial sums meet in shared memory across the
 // cluster, always in the order of ranks.
 //
+// The gradient by the common input of two matrices is one such sum over both, twice as many steps to a tile; pairs may share them, too.
+//
 // Codes and scales come by TMA like A's tiles, a few steps ahead.  What a step takes from codes to operands is several
 // times its share (a wait, loads, products, stores, the fence that shows them to the tensor cores), so four groups
 // of four warps take every fourth step each.
@@ -100,9 +102,10 @@ constexpr int kThreads = (kMmaWarp + 1) * 32;
 constexpr uint32_t kStages = 4, kMostHeld = 8;  // steps of operands, of codes and scales
 constexpr uint32_t kSums = 256;                 // columns of tensor memory of a pair's set
 
-// CTAS: blocks that multiply together, MT: products of 128 CTAS rows per step
-template <int FMT, int MT, int CTAS>
+// CTAS: blocks that multiply together, MT: products of 128 CTAS rows per step, TWO: the sum over two pairs of operands
+template <int FMT, int MT, int CTAS, bool TWO>
 struct GradSizes {
+  static constexpr bool kShares = CTAS == 1 || (TWO && MT == 1);  // a cluster may share a tile's steps
   static constexpr uint32_t kRows = 128 * CTAS * MT, kCols = CTAS == 2 ? 256 / MT : 128, kHalf = kCols / CTAS;  // of a tile, of a block
   static constexpr uint32_t kBBytes = kHalf * kStepR * 2, kStage = MT * kABytes + kBBytes;
   static constexpr uint32_t kCodeBytes = kHalf / 2 * kStepR;
@@ -111,13 +114,13 @@ struct GradSizes {
   static constexpr uint32_t kScaleBytes = (kHalf > kScaleCols ? kHalf / kScaleCols : 1) * kTileBytes;
   static constexpr uint32_t kHeldBytes = kCodeBytes + kScaleBytes;
   // columns that a reading warp turns at a time, and what is left for codes and scales
-  static constexpr uint32_t kTurn = CTAS == 2 && MT == 1 ? 64 : 32, kHeld = kTurn == 64 ? 6 : kMostHeld;
+  static constexpr uint32_t kTurn = CTAS == 2 && MT == 1 && !TWO ? 64 : 32, kHeld = kTurn == 64 ? 6 : kMostHeld;
   static constexpr uint32_t kHeldAt = kStages * kStage, kTurnAt = kHeldAt + kHeld * kHeldBytes;
   static constexpr size_t kBytes = kTurnAt + kReaders * 32 * (kTurn + 1) * 4 + 1024;
   static_assert(kBytes + 1024 <= 227 * 1024 && kStage % 1024 == 0 && kHeldBytes % 128 == 0, "a block's shared memory");
   static constexpr uint32_t kTmem = CTAS == 2 ? 512 : 128;
   static constexpr uint32_t kPartPitch = kCols + 1;  // floats, of a row of partial sums
-  static_assert(CTAS == 2 || kRows * kPartPitch * 4 <= kHeldAt, "the partial sums fit the stages");
+  static_assert(!kShares || kTileA * kPartPitch * 4 <= kTurnAt, "the partial sums fit what the steps were in");
 };
 
 struct GradShared {
@@ -142,7 +145,7 @@ struct GradParams {
   uint32_t a_rows, cols;
   uint32_t strip_bytes;
   uint32_t steps, half, a_tiles, tiles;
-  uint32_t split;                 // blocks per tile, where they multiply by themselves
+  uint32_t split;                 // blocks per tile, where they multiply by themselves, or pairs
   uint32_t accumulate;
   uint32_t max_spins, withhold;
 };
@@ -155,17 +158,17 @@ __device__ __forceinline__ void load_a(uint32_t dst, const CUtensorMap* map, int
     tma_load(dst, map, x, y, bar);
 }
 template <int CTAS>
-__device__ __forceinline__ void commit_to(uint32_t bar) {
+__device__ __forceinline__ void commit_to(uint32_t bar, uint32_t lead) {
   if (CTAS == 2)
-    commit_pair(bar);
+    commit_pair(bar, (uint16_t)(3u << lead));
   else
     commit(bar);
 }
 // at a barrier of the first block of a pair, or of this block
 template <int CTAS>
-__device__ __forceinline__ void arrive_at_first(uint32_t bar) {
+__device__ __forceinline__ void arrive_at_first(uint32_t bar, uint32_t lead) {
   if (CTAS == 2)
-    cluster_arrive(cluster_address(bar, 0));
+    cluster_arrive(cluster_address(bar, lead));
   else
     mbar_arrive(bar);
 }
@@ -257,7 +260,7 @@ template <typename T, int FMT, bool TRANS, int MT, int CTAS, bool TWO>
 __global__ void __launch_bounds__(kThreads, 1)
     mx_grad_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap q_map,
                    const __grid_constant__ CUtensorMap a2_map, const __grid_constant__ CUtensorMap q2_map, const GradParams p) {
-  using S = GradSizes<FMT, MT, CTAS>;
+  using S = GradSizes<FMT, MT, CTAS, TWO>;
   constexpr uint32_t STAGES = kStages, kHeld = S::kHeld, TURN = S::kTurn;
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ GradShared sm;
@@ -295,11 +298,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
   unsigned char* const mem = raw + (base - smem_u32(raw));
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
-  // A pair's blocks take tile after tile; a block by itself has some steps of one.
-  const uint32_t in_cluster = cluster_rank(), rank = CTAS == 2 ? in_cluster : 0;
-  const uint32_t tile0 = CTAS == 2 ? blockIdx.x / 2 : blockIdx.x / p.split, stride = CTAS == 2 ? gridDim.x / 2 : p.tiles;
-  const uint32_t first = CTAS == 2 ? 0 : (uint32_t)((uint64_t)p.steps * in_cluster / p.split);
-  const uint32_t steps = CTAS == 2 ? p.steps : (uint32_t)((uint64_t)p.steps * (in_cluster + 1) / p.split) - first;
+  // A pair's blocks take tile after tile; a block by itself, or a pair where a cluster has several, has some steps of one.
+  const uint32_t in_cluster = cluster_rank(), rank = CTAS == 2 ? in_cluster % 2 : 0, lead = S::kShares ? in_cluster - rank : 0;
+  const uint32_t split = S::kShares ? p.split : 1, share = in_cluster / CTAS;
+  const uint32_t tile0 = blockIdx.x / (CTAS * split), stride = CTAS == 2 && split == 1 ? gridDim.x / 2 : p.tiles;
+  const uint32_t first = S::kShares ? (uint32_t)((uint64_t)p.steps * share / split) : 0;
+  const uint32_t steps = S::kShares ? (uint32_t)((uint64_t)p.steps * (share + 1) / split) - first : p.steps;
 
   if (warp == kHeldWarp) {
     uint32_t i = 0;
@@ -333,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t s = i % STAGES, to = base + s * S::kStage + m * kABytes;
           if (i >= STAGES && !(ok = wait(smem_u32(&sm.empty[s]), (i / STAGES - 1) & 1, abandoned, p.status, p.max_spins))) break;
           if (rank == 0 && m == 0) expect_bytes(smem_u32(&sm.full_a[s]), CTAS * MT * kABytes);
-          const uint32_t bar = CTAS == 2 ? cluster_address(smem_u32(&sm.full_a[s]), 0) : smem_u32(&sm.full_a[s]);
+          const uint32_t bar = CTAS == 2 ? cluster_address(smem_u32(&sm.full_a[s]), lead) : smem_u32(&sm.full_a[s]);
           const bool second = TWO && first + step >= p.half;
           const int r0 = (int)((first + step - (second ? p.half : 0)) * kStepR);
           if (TRANS) {
@@ -366,13 +370,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint64_t a = TRANS ? operand(from, kABytes / 2, 1024, true) : operand(from, 16, 1024, true);
           multiply_step<CTAS, MT, (TRANS ? 2048 : 32) / 16, 2048 / 16, kABytes / 16, S::kCols>(
               tmem + set * kSums, a, operand(from + MT * kABytes, 8192, 1024, true), idesc, (uint32_t)(step > 0));
-          commit_to<CTAS>(smem_u32(&sm.empty[s]));
+          commit_to<CTAS>(smem_u32(&sm.empty[s]), lead);
           ++i;
         }
-        if (ok) commit_to<CTAS>(smem_u32(&sm.sums_full[set]));
+        if (ok) commit_to<CTAS>(smem_u32(&sm.sums_full[set]), lead);
       }
       if (!ok && i > 0) {
-        commit_to<CTAS>(smem_u32(&sm.spare));
+        commit_to<CTAS>(smem_u32(&sm.spare), lead);
         drain(smem_u32(&sm.spare), 0);
       }
     }
@@ -421,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> visible to the products
       __syncwarp();
       if (lane == 0) {
-        arrive_at_first<CTAS>(smem_u32(&sm.full_b[s]));
+        arrive_at_first<CTAS>(smem_u32(&sm.full_b[s]), lead);
         // (only now: the stores above have taken the codes out of registers that their loads have filled)
         mbar_arrive(smem_u32(&sm.held_empty[hs]));
       }
@@ -439,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       tc_fence_after();
       const uint32_t c0 = tile / p.a_tiles * S::kCols;
-      if (CTAS == 1 && p.split > 1) {  // the products are done: the stages hold the partial sums
+      if (S::kShares && split > 1) {  // the products are done: the partial sums lie where their operands and codes were
         float* const part = reinterpret_cast<float*>(mem) + (quarter * 32 + lane) * S::kPartPitch;
         for (uint32_t j0 = half * (S::kCols / 2); j0 < (half + 1) * (S::kCols / 2); j0 += 32) {
           uint32_t v[32];
@@ -496,26 +500,27 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) arrive_at_first<CTAS>(smem_u32(&sm.sums_empty[set]));
+      if (lane == 0) arrive_at_first<CTAS>(smem_u32(&sm.sums_empty[set]), lead);
       __syncwarp();
     }
   }
   __syncthreads();
   cluster_sync();  // no block leaves while another's copies, arrivals or products reach it
-  if (CTAS == 1 && p.split > 1) {
+  if (S::kShares && split > 1) {
     // every block adds up the rows that are its share, always in the order of ranks
     if (warp < kWideners && !*abandoned) {
       const Factors alpha(kWidened<FMT>, p.ts ? *p.ts : 1.0f);
-      const uint32_t a0 = tile0 % p.a_tiles * S::kRows, c0 = tile0 / p.a_tiles * S::kCols;
-      for (uint32_t r = in_cluster + warp * p.split; r < S::kRows && a0 + r < p.a_rows; r += kWideners * p.split) {
+      const uint32_t a0 = tile0 % p.a_tiles * S::kRows + rank * kTileA, c0 = tile0 / p.a_tiles * S::kCols;
+      for (uint32_t r = share + warp * split; r < kTileA && a0 + r < p.a_rows; r += kWideners * split) {
         T* const out = static_cast<T*>(p.out) + (int64_t)(a0 + r) * p.ldo + c0;
 #pragma unroll
         for (uint32_t j = lane; j < S::kCols; j += 32) {
-          float v[8], sum = 0.0f;
+          float v[8 / CTAS], sum = 0.0f;
 #pragma unroll
-          for (uint32_t q = 0; q < 8; ++q) v[q] = q < p.split ? cluster_load(base + (r * S::kPartPitch + j) * 4, q) : 0.0f;
+          for (uint32_t q = 0; q < 8 / CTAS; ++q)
+            v[q] = q < split ? cluster_load(base + (r * S::kPartPitch + j) * 4, CTAS * q + rank) : 0.0f;
 #pragma unroll
-          for (uint32_t q = 0; q < 8; ++q) sum += v[q];
+          for (uint32_t q = 0; q < 8 / CTAS; ++q) sum += v[q];
           sum = alpha(sum);
           if (c0 + j < p.cols) {
             if (sizeof(T) == 4 && p.accumulate) sum += widen<T>(out[j]);
@@ -532,10 +537,48 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+// How many clusters of so many blocks of a kernel run at once; the driver is asked once per kernel, device and size.
+template <auto kernel>
+uint32_t clusters_at_once(uint32_t cluster, size_t smem) {
+  static std::atomic<int> known[kMaxDevices][9];
+  const int dev = device_slot();
+  int n = dev >= 0 ? known[dev][cluster].load(std::memory_order_relaxed) : 0;
+  if (n > 0) return (uint32_t)n - 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(cluster), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = 1;
+  if (allow_smem<kernel>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();  // (then none share)
+    return 0;
+  }
+  if (dev >= 0) known[dev][cluster].store(n + 1, std::memory_order_relaxed);
+  return (uint32_t)n;
+}
+// Blocks or pairs that share a tile's steps, at most 8 / CTAS of them: the number that leaves each the fewest steps while all clusters
+// run at once.  time: what that takes, in units of 10 ns, by what a step and the rest of a tile took for sums over 2 x 11008 and 2 x 6144
+// (a step waits for its elements to be widened, whatever multiplies them, unless both tiles of A are there).
+template <typename T, int FMT, int MT, int CTAS>
+uint32_t shares_of(uint32_t a_rows, uint32_t cols, uint32_t steps, int sm_count, uint64_t* time) {
+  using S = GradSizes<FMT, MT, CTAS, true>;
+  constexpr uint32_t kStep = CTAS == 1 ? 40 : MT == 1 ? 43 : 38, kTile = CTAS == 1 ? 450 : 600;
+  const uint64_t tiles = (uint64_t)((a_rows + S::kRows - 1) / S::kRows) * ((cols + S::kCols - 1) / S::kCols), all = (uint32_t)sm_count / CTAS;
+  *time = (tiles + all - 1) / all * steps * kStep + kTile;
+  uint32_t shares = 1;
+  if (S::kShares)
+    for (uint32_t n = 2; n <= 8 / CTAS && 4 * n <= steps && n * tiles <= all; ++n)
+      if (tiles <= clusters_at_once<mx_grad_kernel<T, FMT, false, MT, CTAS, true>>(CTAS * n, S::kBytes))
+        shares = n, *time = (uint64_t)((steps + n - 1) / n) * kStep + kTile + (CTAS == 2 ? 150 : 0);
+  return shares;
+}
+
+// split: blocks or pairs that share a tile's steps (TWO)
 template <typename T, int FMT, bool TRANS, int MT, int CTAS, bool TWO>
 cudaError_t start(const CUtensorMap& a_map, const CUtensorMap& a2_map, GradParams p, const pvt_mx& q, const pvt_mx& q2, int sm_count,
-                  cudaStream_t stream) {
-  using S = GradSizes<FMT, MT, CTAS>;
+                  cudaStream_t stream, uint32_t split = 1) {
+  using S = GradSizes<FMT, MT, CTAS, TWO>;
   p.a_tiles = (p.a_rows + S::kRows - 1) / S::kRows, p.tiles = p.a_tiles * ((p.cols + S::kCols - 1) / S::kCols);
   CUtensorMap q_map, q2_map;
   cudaError_t e = make_map(&q_map, q.codes, 1, (uint64_t)q.rows, ((uint64_t)q.cols + 1) / 2, (uint64_t)q.ld, kStepR, S::kHalf / 2, false);
@@ -544,18 +587,10 @@ cudaError_t start(const CUtensorMap& a_map, const CUtensorMap& a2_map, GradParam
   if (e == cudaSuccess) e = allow_smem<mx_grad_kernel<T, FMT, TRANS, MT, CTAS, TWO>>();
   if (e != cudaSuccess) return e;
   uint32_t grid = 2 * (p.tiles < (uint32_t)sm_count / 2 ? p.tiles : (uint32_t)sm_count / 2), cluster = 2;
-  if (CTAS == 1) {
-    p.split = 1;
-    if (TWO) {
-      // any number of blocks to a tile, as long as all clusters run at once (eighteen SMs or so find each other): 77 tokens 5119 by 4095, 40
-      // tiles by two and by three blocks, 31 and 24 us
-      for (uint32_t n = 2; n <= 8 && 4 * n <= p.steps; ++n)
-        if ((uint64_t)p.tiles * n <= (uint64_t)sm_count && p.tiles <= 8 * ((uint32_t)sm_count / 8 / n)) p.split = n;
-    } else {
-      while (p.split < 8 && (uint64_t)p.tiles * p.split * 2 <= (uint64_t)sm_count && p.split * 2 <= p.steps) p.split *= 2;
-    }
-    grid = p.tiles * p.split, cluster = p.split;
-  }
+  p.split = split;
+  if (CTAS == 1 && !TWO)
+    while (p.split < 8 && (uint64_t)p.tiles * p.split * 2 <= (uint64_t)sm_count && p.split * 2 <= p.steps) p.split *= 2;
+  if (CTAS == 1 || p.split > 1) cluster = CTAS * p.split, grid = p.tiles * cluster;
   return launch_clusters(mx_grad_kernel<T, FMT, TRANS, MT, CTAS, TWO>, grid, cluster, kThreads, S::kBytes, stream, a_map, q_map,
                          TWO ? a2_map : a_map, TWO ? q2_map : q_map, p);
 }
@@ -577,6 +612,18 @@ cudaError_t grad(const void* dy, int64_t lddy, uint32_t a_rows, const pvt_mx& q,
   cudaError_t e = make_map(&a_map, dy, 2, tokens, features, (uint64_t)lddy * 2, TRANS ? kStepR : kTileA);
   if (TWO && e == cudaSuccess) e = make_map(&a2_map, dy2, 2, tokens, features, (uint64_t)lddy * 2, kTileA);
   if (e != cudaSuccess) return e;
+  if constexpr (TWO) {
+    // What takes least.  11008 by 4096, 256 tokens: 64 tiles by two blocks each 66 us, 16 tiles by three pairs each 50; 512 tokens: 128
+    // tiles by blocks 120, 32 tiles by two pairs each 70.  77 tokens 4095 by 5119: 40 tiles by two and by three blocks 31 and 24.
+    uint64_t by_blocks, by_pairs, by_tall;
+    const uint32_t blocks = shares_of<T, FMT, 1, 1>(a_rows, p.cols, p.steps, sm_count, &by_blocks);
+    const uint32_t pairs = shares_of<T, FMT, 1, 2>(a_rows, p.cols, p.steps, sm_count, &by_pairs);
+    shares_of<T, FMT, 2, 2>(a_rows, p.cols, p.steps, sm_count, &by_tall);
+    if (by_blocks <= by_pairs && by_blocks <= by_tall)
+      return start<T, FMT, TRANS, 1, 1, TWO>(a_map, a2_map, p, q, q2, sm_count, stream, blocks);
+    if (by_pairs <= by_tall) return start<T, FMT, TRANS, 1, 2, TWO>(a_map, a2_map, p, q, q2, sm_count, stream, pairs);
+    return start<T, FMT, TRANS, 2, 2, TWO>(a_map, a2_map, p, q, q2, sm_count, stream);
+  }
   // Blocks by themselves where they have the rows, or pairs would leave three quarters of the SMs idle: dx by blocks and by pairs,
   // 256 tokens 4096 by 4096 18.5 and 28.2 us, 600 tokens 2048 by 2048 15.3 and 16.9.
   const uint64_t pair_tiles = (uint64_t)((a_rows + 255) / 256) * ((p.cols + 255) / 256);

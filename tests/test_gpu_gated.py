@@ -126,6 +126,29 @@ def test_gradients(fmt, case, shape):
     assert st.item() == 0
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("tokens,cols,n", [(1, 257, 2050), (129, 512, 1024), (130, 4096, 700), (200, 300, 9000), (256, 1024, 2048), (300, 1030, 1500),
+                                           (520, 768, 4096), (700, 2049, 333)])
+def test_input_gradient_by_any_number_of_blocks(tokens, cols, n, fmt):
+    """Tiles whose steps single blocks or pairs of blocks share, ragged in every direction; the same bits each time."""
+    gen = torch.Generator("cuda").manual_seed(tokens + n)
+    wg, gv = held(gen, n, cols, fmt, 0.1)
+    wu, uv = held(gen, n, cols, fmt, 0.1)
+    pitch = -(-n // 8) * 8
+    dg, du = (torch.randn(tokens, pitch, device="cuda", generator=gen).bfloat16()[:, :n] for _ in range(2))
+    want = dg.double() @ gv + du.double() @ uv
+    off = (2 * n + 4) * 2.0 ** -23 * (dg.double().abs() @ gv.abs() + du.double().abs() @ uv.abs())
+    outs = []
+    st = status()
+    for _ in range(2):
+        dx = torch.full((tokens + 1, cols + 3), 7.0, device="cuda")
+        B.pvt_mx_gated_grad_input(dg, du, wg, wu, dx[:-1, :cols], status=st)
+        outs.append(dx)
+    close(outs[0][:-1, :cols], want, off, torch.float32)
+    assert (outs[0][-1] == 7).all() and (outs[0][:, cols:] == 7).all()
+    assert torch.equal(outs[0], outs[1]) and st.item() == 0
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_gradients_against_differences(act):
     """f' is the derivative of f, and the kernel's gradients are those of sum(dh h) by a and b."""
