@@ -225,6 +225,12 @@ __device__ __forceinline__ float cluster_load(uint32_t saddr, uint32_t rank) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
+__device__ __forceinline__ float4 cluster_load4(uint32_t saddr, uint32_t rank) {
+  const uint32_t at = cluster_address(saddr, rank);
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint64_t cluster_load64(uint32_t saddr, uint32_t rank) {
   const uint32_t at = cluster_address(saddr, rank);
   uint64_t v;
@@ -251,6 +257,26 @@ cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned grid, unsigned cl
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+// How many clusters of so many blocks (eight at most) of a kernel run at once; the driver is asked once per kernel, device and size.
+template <auto kernel>
+uint32_t clusters_at_once(uint32_t cluster, uint32_t threads, size_t smem) {
+  static std::atomic<int> known[kMaxDevices][9];
+  const int dev = device_slot();
+  int n = dev >= 0 ? known[dev][cluster].load(std::memory_order_relaxed) : 0;
+  if (n > 0) return (uint32_t)n - 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(cluster), cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = 1;
+  if (allow_smem<kernel>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();  // (then none share)
+    return 0;
+  }
+  if (dev >= 0) known[dev][cluster].store(n + 1, std::memory_order_relaxed);
+  return (uint32_t)n;
 }
 #endif
 

@@ -414,6 +414,10 @@ __device__ __forceinline__ bool pair_agrees(uint32_t id, bool ok) {
 // no bank is met twice either by lanes that have an output each or by four lanes to a token with eight outputs each.
 __device__ __forceinline__ uint32_t place(uint32_t token, uint32_t output) { return token * 32 + (output ^ (token & 7) * 4); }
 
+// Where partial sums of a tile lie: 64 of a and 64 of b to a token, in pieces of four, the even ones ahead of the odd ones, these exchanged by
+// fours: no bank is met twice either by lanes that have an output each or by eight that have two pieces each.
+__device__ __forceinline__ uint32_t piece_at(uint32_t piece) { return piece % 2 ? 8 + (piece / 2 ^ 4) : piece / 2; }
+
 // eight neighbouring elements, rounded; `left` of them exist
 template <typename T>
 __device__ __forceinline__ void put8(T* to, const float* v, bool wide, uint32_t left) {
@@ -728,9 +732,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) cluster_arrive(sums_empty);
       __syncwarp();
       if (p.split > 1) {  // the products are done: the stages hold the partial sums
+        const uint32_t at = piece_at(quarter % 2 * 8 + lane / 4) * 4 + lane % 4;
 #pragma unroll
         for (uint32_t k = 0; k < PART; ++k)
-          reinterpret_cast<float*>(mem)[(part * PART + k) * kTileW + quarter * 32 + lane] = __uint_as_float(v[k]);
+          reinterpret_cast<float*>(mem)[(part * PART + k) * kTileW + of_b * kOutputs + at] = __uint_as_float(v[k]);
         break;
       }
       with_activation(f.activation, [&](auto act) {
@@ -781,14 +786,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int k = 0; k < 8; ++k) a[k] = b[k] = 0.0f;
         if (row0 + j0 < f.tokens)
           for (uint32_t q = 0; q < p.split; ++q) {
-            float x[8], y[8];  // (all under way at once: a load from another block takes a thousand cycles)
+            float4 x[2], y[2];  // (all under way at once: a load from another block takes a thousand cycles)
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) {
-              x[k] = cluster_load(base + (j * kTileW + lane % 8 * 8 + k) * 4, 2 * q + rank);
-              y[k] = cluster_load(base + (j * kTileW + kOutputs + lane % 8 * 8 + k) * 4, 2 * q + rank);
+            for (uint32_t k = 0; k < 2; ++k) {
+              const uint32_t at = base + (j * kTileW + piece_at(lane % 8 * 2 + k) * 4) * 4;
+              x[k] = cluster_load4(at, 2 * q + rank), y[k] = cluster_load4(at + kOutputs * 4, 2 * q + rank);
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) a[k] += x[k], b[k] += y[k];
+            for (int k = 0; k < 2; ++k) {
+              a[4 * k] += x[k].x, a[4 * k + 1] += x[k].y, a[4 * k + 2] += x[k].z, a[4 * k + 3] += x[k].w;
+              b[4 * k] += y[k].x, b[4 * k + 1] += y[k].y, b[4 * k + 2] += y[k].z, b[4 * k + 3] += y[k].w;
+            }
           }
 #pragma unroll
         for (int k = 0; k < 8; ++k) a[k] = gate(a[k]), b[k] = up(b[k]);
@@ -826,7 +834,12 @@ cudaError_t gated_pairs(const pvt_mx& x, const pvt_mx& wg, const pvt_mx& wu, con
   }
   const cudaError_t e = allow_smem<mx_gated_pair_kernel<FMT, N, GRAD>>();
   if (e != cudaSuccess) return e;
-  p.split = pairs_per_tile(p.tiles, p.steps, sm_count);
+  // Few tiles: up to four pairs to each, as long as all clusters run at once and a pair keeps eight steps.  By one, two and four pairs, 100
+  // tokens 8192 by 1024 14.5, 10.9 and 9.1 us; by one and two, 64 tokens 11008 by 4096 18.9 and 13.8, 77 tokens 4096 by 4096 9.7 and 8.9, 128
+  // tokens 2048 by 4096 (four steps each) 7.3 and 8.3.
+  p.split = 1;
+  for (uint32_t n = 2; n <= 4 && 8 * n <= p.steps && (uint64_t)p.tiles * 2 * n <= (uint64_t)sm_count; ++n)
+    if (p.tiles <= clusters_at_once<mx_gated_pair_kernel<FMT, N, GRAD>>(2 * n, kThreads, S::kBytes)) p.split = n;
   const uint32_t pairs = p.split > 1 ? p.tiles * p.split : p.tiles < (uint32_t)sm_count / 2 ? p.tiles : (uint32_t)sm_count / 2;
   return launch_clusters(mx_gated_pair_kernel<FMT, N, GRAD>, 2 * pairs, 2 * p.split, kThreads, S::kBytes, stream, maps[0], maps[1],
                          maps[2], maps[3], maps[4], maps[5], p);

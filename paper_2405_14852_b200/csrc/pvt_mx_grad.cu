@@ -537,26 +537,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// How many clusters of so many blocks of a kernel run at once; the driver is asked once per kernel, device and size.
-template <auto kernel>
-uint32_t clusters_at_once(uint32_t cluster, size_t smem) {
-  static std::atomic<int> known[kMaxDevices][9];
-  const int dev = device_slot();
-  int n = dev >= 0 ? known[dev][cluster].load(std::memory_order_relaxed) : 0;
-  if (n > 0) return (uint32_t)n - 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(cluster), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = smem;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cluster, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr, cfg.numAttrs = 1;
-  if (allow_smem<kernel>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-    (void)cudaGetLastError();  // (then none share)
-    return 0;
-  }
-  if (dev >= 0) known[dev][cluster].store(n + 1, std::memory_order_relaxed);
-  return (uint32_t)n;
-}
 // Blocks or pairs that share a tile's steps, at most 8 / CTAS of them: the number that leaves each the fewest steps while all clusters
 // run at once.  time: what that takes, in units of 10 ns, by what a step and the rest of a tile took for sums over 2 x 11008 and 2 x 6144
 // (a step waits for its elements to be widened, whatever multiplies them, unless both tiles of A are there).
@@ -569,7 +549,7 @@ uint32_t shares_of(uint32_t a_rows, uint32_t cols, uint32_t steps, int sm_count,
   uint32_t shares = 1;
   if (S::kShares)
     for (uint32_t n = 2; n <= 8 / CTAS && 4 * n <= steps && n * tiles <= all; ++n)
-      if (tiles <= clusters_at_once<mx_grad_kernel<T, FMT, false, MT, CTAS, true>>(CTAS * n, S::kBytes))
+      if (tiles <= clusters_at_once<mx_grad_kernel<T, FMT, false, MT, CTAS, true>>(CTAS * n, kThreads, S::kBytes))
         shares = n, *time = (uint64_t)((steps + n - 1) / n) * kStep + kTile + (CTAS == 2 ? 150 : 0);
   return shares;
 }
