@@ -416,7 +416,7 @@ int pvt_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const pvt_mx* x,
  * sums as by pvt_mx_product, f and the product by it in binary32.
  * h: device, tokens x outputs of h_dtype (any of the three), rows ldh elements apart, each element rounded once; hq: the
  * binary32 values as by pvt_mx_quantize, tokens x outputs of x's format, what the product with the next layer takes.  NULL for the one
- * that is not wanted.  Neither may overlap an operand.  Results depend on the shapes only.  `status` as above.
+ * that is not wanted.  Neither may overlap an operand.  Results depend on the shapes and the device only.  `status` as above.
  */
 #define PVT_ACT_SILU 0
 #define PVT_ACT_GELU 1
@@ -433,7 +433,8 @@ int pvt_mx_gated(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int3
  *                             the same distance of rows).
  *   pvt_mx_gated_grad_input:  dx[t, c] = sum over n of dgate[t, n] w_gate[n, c] + dup[t, n] w_up[n, c], in one binary32 sum rounded once.
  *                             dx: tokens x inputs of dx_dtype, rows lddx elements apart.  One sum has one factor: w_gate and w_up have
- *                             the same tensor_scale (the same pointer), or none.
+ *                             the same tensor_scale (the same pointer), or none.  dgate and dup whose rows begin on 128 bytes
+ *                             are read fastest.
  */
 int pvt_mx_gated_grad(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int32_t activation, const void* dh, int32_t dh_dtype,
                       int64_t lddh, void* dgate, void* dup, int64_t ldd, uint32_t* status, void* cuda_stream);

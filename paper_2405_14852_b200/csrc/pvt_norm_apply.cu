@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(L == kRagged ? kRaggedBound : kMostThreads) no
   at.weights(p.weight, p.w_dtype, p.w_wide, 1.0f, w);
   at.weights(p.bias, p.w_dtype, p.w_wide, 0.0f, b);
   const float inv = 1.0f / (float)s.cols;
+  if (s.parts > 1) mma::cluster_sync();  // every block of the cluster runs: from here on others write to its shared memory
   uint32_t turn = 0, k = 0;
   // (all of a block's teams go round as often as its first one)
   for (uint64_t first = (uint64_t)set * s.teams * R; first < p.padded; first += stride, row0 += stride, turn ^= 1) {
