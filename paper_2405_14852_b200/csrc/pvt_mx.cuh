@@ -51,6 +51,44 @@ struct alignas(8 * sizeof(T)) Eight {
   T v[8];
 };
 
+// Two elements to an instruction: each is rounded as by itself, and takes half the issue slots.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "mul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 two(const float* v) { return make_float2(v[0], v[1]); }
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ void set2(float* to, float2 v) { to[0] = v.x, to[1] = v.y; }
+// the bits of the largest magnitude of eight, which are beyond all numbers' if one is NaN
+__device__ __forceinline__ uint32_t top_of8(const float* v) {
+  auto top3 = [](float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+  };
+  return __float_as_uint(top3(top3(v[0], v[1], v[2]), top3(v[3], v[4], v[5]), top3(v[6], v[7], v[7])));
+}
+
 // the value of an e4m3 scale byte without its sign: exact in binary32
 __device__ __forceinline__ float e4m3_value(uint32_t byte) {
   const uint32_t e = byte >> 3 & 15, m = byte & 7;

@@ -111,7 +111,7 @@ __device__ __forceinline__ uint32_t quantize_block(float* v, uint32_t top, const
     byte = bad ? 255u : (uint32_t)e;
     const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] *= inv;
+    for (int i = 0; i < E; i += 2) set2(v + i, mul2(two(v + i), both(inv)));
     if (!bad) {
 #pragma unroll
       for (int w = 0; w < E / 8; ++w) word[w] = e2m1_codes(v + 8 * w);
@@ -129,7 +129,10 @@ __device__ __forceinline__ uint32_t quantize_block(float* v, uint32_t top, const
       for (int w = 0; w < E / 8; ++w) {
         float hi[8], lo[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) hi[i] = v[8 * w + i] * more, lo[i] = v[8 * w + i] * less;
+        for (int i = 0; i < 8; i += 2) {
+          const float2 x = two(v + 8 * w + i);
+          set2(hi + i, mul2(x, both(more))), set2(lo + i, mul2(x, both(less)));
+        }
         word[w] = e2m1_codes(hi);
         const uint32_t differ = all ? 0xffffffffu : word[w] ^ e2m1_codes(lo);
         if (differ) {
@@ -163,12 +166,13 @@ __device__ __forceinline__ void put_eight(const Held& m, uint32_t row, uint32_t 
                                           float* v) {
   constexpr uint32_t LANES = FMT == PVT_MX_E8M0_32 ? 4 : 2;  // of a block
   const uint32_t lane = threadIdx.x & 31, block = c0 / (8 * LANES);
-  uint32_t top = 0, word;
+  uint32_t word;
+  if (c0 + 8 > m.cols) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (c0 + i >= m.cols) v[i] = 0.0f;
-    top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int i = 0; i < 8; ++i)
+      if (c0 + i >= m.cols) v[i] = 0.0f;
   }
+  uint32_t top = top_of8(v);
 #pragma unroll
   for (uint32_t d = 1; d < LANES; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
   uint32_t byte = quantize_block<FMT, 8>(v, top, t, &word);

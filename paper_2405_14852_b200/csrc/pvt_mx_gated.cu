@@ -442,12 +442,13 @@ __device__ __forceinline__ void put8(T* to, const float* v, bool wide, uint32_t 
 template <int FMT>
 __device__ __forceinline__ void put_four_bits(const Finish& p, const TensorScale& t, uint32_t token, uint32_t c, bool here, float* v) {
   constexpr uint32_t BLOCK = FMT == PVT_MX_E8M0_32 ? 32 : 16;
-  uint32_t top = 0, word;
+  uint32_t word;
+  if (c + 8 > p.n) {
 #pragma unroll
-  for (uint32_t i = 0; i < 8; ++i) {
-    if (c + i >= p.n) v[i] = 0.0f;
-    top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (uint32_t i = 0; i < 8; ++i)
+      if (c + i >= p.n) v[i] = 0.0f;
   }
+  uint32_t top = top_of8(v);
 #pragma unroll
   for (uint32_t d = 1; d < BLOCK / 8; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
   uint32_t bytes = quantize_block<FMT, 8>(v, top, t, &word);
@@ -756,7 +757,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!turned) pair_sync(pair + 1);  // (the next round's sums may come)
           if (scaled) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) a[k] = gate(a[k]), b[k] = up(b[k]);
+            for (int k = 0; k < 8; k += 2) {
+              set2(a + k, mul2(mul2(two(a + k), both(gate.first)), both(gate.second)));
+              set2(b + k, mul2(mul2(two(b + k), both(up.first)), both(up.second)));
+            }
           }
           EightOfDh now = dh;
           if (GRAD && r + kRound < PART) dh.ask(f, row + r + kRound + j, c, left);

@@ -116,8 +116,14 @@ __host__ __device__ __forceinline__ auto with_type(int32_t dtype, F f) {
 }
 
 #ifdef __CUDACC__
+using mx::add2;
+using mx::both;
 using mx::Eight;
+using mx::fma2;
+using mx::mul2;
 using mx::narrow;
+using mx::set2;
+using mx::two;
 using mx::widen;
 
 // 16 bytes from a 16-byte boundary, of which the first `bytes` are read and the others become 0
@@ -133,9 +139,13 @@ __device__ __forceinline__ void copies_wait(bool but_one) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 // (short chains: with few warps to an SM their latency would show)
-__device__ __forceinline__ float sum8(const float* v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+__device__ __forceinline__ float sum8(const float* v) {
+  const float2 s = add2(add2(two(v), two(v + 2)), add2(two(v + 4), two(v + 6)));
+  return s.x + s.y;
+}
 __device__ __forceinline__ float dot8(const float* a, const float* b) {
-  return (fmaf(a[1], b[1], a[0] * b[0]) + fmaf(a[3], b[3], a[2] * b[2])) + (fmaf(a[5], b[5], a[4] * b[4]) + fmaf(a[7], b[7], a[6] * b[6]));
+  const float2 s = add2(fma2(two(a + 2), two(b + 2), mul2(two(a), two(b))), fma2(two(a + 6), two(b + 6), mul2(two(a + 4), two(b + 4))));
+  return s.x + s.y;
 }
 
 // two values rounded at a time: one conversion, where one by itself takes the slower unit

@@ -3,14 +3,14 @@
 // A row is read once and stays in registers to its end: the sum with the residual is rounded to x's type first, as it is
 // kept; then the mean, then the mean of the squared differences from it (a second pass over registers, so a mean far from 0 costs no
 // digits).  Two barriers a row, one without the mean; where rows are many, a team
-// has two at a time and both share them.
+// has two at a time and both share them.  (Two elements to an instruction, here and in quantisation: 4096 x 4096 into 4 bits 33 -> 30 us.)
 //
 // 4-bit results: a lane's eight columns are a quarter or half of a block, as in quantisation by itself; rows of no alignment are
 // turned in shared memory first.
 //
 // What bounds it: 4096 x 8192 in bfloat16 with the residual, 268 MB, 49 us, 85 % of a copy's rate, the issue slots 60 % taken (of which
 // a third by the sums of a row, whose second barrier costs less than what would save it: means of each warp, 55 us).  Into 4 bits the slots
-// bound it: 2048 x 4096 19 us under e8m0 and 22 under e4m3 for 14 into bfloat16.  2047 x 5001 in float16, rows of no alignment, 20 us of
+// bound it: 2048 x 4096 18 us under e8m0 and 20 under e4m3 for 14 into bfloat16.  2047 x 5001 in float16, rows of no alignment, 20 us of
 // 9.5.  One row of 4096 2.5 us behind the kernel ahead.
 #include "pvt_mx_block.cuh"
 #include "pvt_norm.cuh"
@@ -102,9 +102,10 @@ __global__ void __launch_bounds__(L == kRagged ? kRaggedBound : kMostThreads) no
           at.take(image + res_at + r * row_at, residual + (int64_t)row * p.ldr, g, e);
 #pragma unroll
           for (int i = 0; i < 8; i += 2) {
-            T two[2];
-            narrow_pair(v[r][g][i] + e[i], v[r][g][i + 1] + e[i + 1], two);
-            v[r][g][i] = widen<T>(two[0]), v[r][g][i + 1] = widen<T>(two[1]);
+            T kept[2];
+            const float2 sum = add2(two(v[r][g] + i), two(e + i));
+            narrow_pair(sum.x, sum.y, kept);
+            v[r][g][i] = widen<T>(kept[0]), v[r][g][i + 1] = widen<T>(kept[1]);
           }
         }
         if (p.total && row < s.rows) at.put(static_cast<T*>(p.total) + (int64_t)row * p.ldt, g, v[r][g]);
@@ -117,7 +118,14 @@ __global__ void __launch_bounds__(L == kRagged ? kRaggedBound : kMostThreads) no
       for (int r = 0; r < R; ++r) {
         mean[r] *= inv;
 #pragma unroll
-        for (int g = 0; g < G; ++g) at.each(g, [&](int i) { v[r][g][i] -= mean[r]; });
+        for (int g = 0; g < G; ++g) {
+          if (at.full(g)) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) set2(v[r][g] + i, add2(two(v[r][g] + i), both(-mean[r])));
+          } else {
+            at.each(g, [&](int i) { v[r][g][i] -= mean[r]; });
+          }
+        }
       }
     }
 #pragma unroll
@@ -137,7 +145,7 @@ __global__ void __launch_bounds__(L == kRagged ? kRaggedBound : kMostThreads) no
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[r][g][i] = fmaf(v[r][g][i] * rstd, w[g][i], b[g][i]);
+        for (int i = 0; i < 8; i += 2) set2(v[r][g] + i, fma2(mul2(two(v[r][g] + i), both(rstd)), two(w[g] + i), two(b[g] + i)));
       if (p.y && here)
         with_type(p.y_dtype, [&](auto* type) {
           using U = std::remove_pointer_t<decltype(type)>;
