@@ -191,9 +191,11 @@ template <typename T, int L, int G>
 cudaError_t start(const ApplyParams& p, int sm_count, cudaStream_t stream) {
   const bool turned = L == kRagged && p.q.codes;
   const uint32_t blocks = kMostThreads / p.s.threads;  // of an SM
-  // two rows at a time if all blocks have some, and rings of three stages, or of two
+  // two rows at a time if all blocks have some, and rings of three stages, or of two; not floats without the mean, which share one barrier
+  // only, beyond four rows to a block (4096 x 8192 in bfloat16 48 and 44 us, 4096 x 4096 25 and 23; but 1024 x 4096 6.7 and 7.5)
+  const uint32_t all = (uint32_t)sm_count * blocks / p.s.parts * p.s.teams;
   if constexpr (L != kRagged)
-    if (p.s.rows > 2 * (uint32_t)sm_count * blocks / p.s.parts * p.s.teams && ring_bytes(p, 2, 2, turned) * blocks <= kRingBytes)
+    if (p.s.rows > 2 * all && (p.layer || p.q.codes || p.s.rows <= 4 * all) && ring_bytes(p, 2, 2, turned) * blocks <= kRingBytes)
       return start<T, L, G, 2>(p, ring_bytes(p, 2, 3, turned) * blocks <= kRingBytes ? 3 : 2, sm_count, stream);
   return start<T, L, G, 1>(p, ring_bytes(p, 1, 3, turned) * blocks <= kRingBytes ? 3 : 2, sm_count, stream);
 }
