@@ -8,8 +8,8 @@
 // 4-bit results: a lane's eight columns are a quarter or half of a block, as in quantisation by itself; rows of no alignment are
 // turned in shared memory first.
 //
-// What bounds it: 4096 x 8192 in bfloat16 with the residual, 268 MB, 49 us, 85 % of a copy's rate, the issue slots 60 % taken (of which
-// a third by the sums of a row, whose second barrier costs less than what would save it: means of each warp, 55 us).  Into 4 bits the slots
+// What bounds it: 4096 x 8192 in bfloat16 with the residual, 268 MB, 48 us, 87 % of a copy's rate, the issue slots 53 % taken (the
+// second barrier of a row costs less than what would save it: means of each warp, 55 us).  Into 4 bits the slots
 // bound it: 2048 x 4096 18 us under e8m0 and 20 under e4m3 for 14 into bfloat16.  2047 x 5001 in float16, rows of no alignment, 20 us of
 // 9.5.  One row of 4096 2.5 us behind the kernel ahead.
 #include "pvt_mx_block.cuh"

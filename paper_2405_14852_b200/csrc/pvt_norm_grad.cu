@@ -8,8 +8,10 @@
 // rows a block has depends on the shapes and the device only.  One barrier a row, for its two means: behind it row n - 1 is finished and
 // row n's sums are taken, each in the other's waits (one after the other, two barriers a row: 57 to 66 us for 52).
 //
-// What bounds it: 4096 x 8192 in bfloat16 with the residual's gradient, 268 MB, 56 us for both kernels, 75 % of a copy's rate: issue slots
-// 62 % taken.  333 x 5119 in float32: 14 us of 3.2, two kernels' latency, three rounds and 6 MB of sums.
+// What bounds it: 4096 x 8192 in bfloat16 with the residual's gradient, 268 MB, 56 us for both kernels, 75 % of a copy's rate, the issue slots
+// 52 to 62 % taken.  333 x 5119 in float32: 14 us of 3.2, two kernels' latency, three rounds of 1400 cycles (257 instructions of a warp, one
+// behind the other) and 6 MB of sums.  Rows asked for four rounds ahead instead of two changed nothing; two rows at least to each block: 592
+// x 2445 14.2 -> 12.7 us, but 1184 x 1024 10.2 -> 11.3 and 2048 x 768 16.2 -> 18.4.
 #include "pvt_norm.cuh"
 
 namespace pvt {
