@@ -152,9 +152,9 @@ __device__ __forceinline__ void finish_token(const Finish& p, const TensorScale&
       float v[8];
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) v[i] = lane < 16 ? scratch[8 * lane + i] : 0.0f;
-      // (the upper lanes: the next 128 columns, where there are no outputs but scales)
-      const bool none = lane >= 16 && col0 + 128 < p.n;
-      put_eight<FMT>(p.q, token, none ? 0x40000000u : col0 + 8 * lane, true, !none, t, v);
+      // (the upper lanes: the next 128 columns, which are another block's, or of which there are scales but no outputs)
+      const bool own = lane < 16 || col0 + 128 >= p.n;
+      put_eight<FMT>(p.q, token, col0 + 8 * lane, own, own, t, v);
     }
   }
 }
