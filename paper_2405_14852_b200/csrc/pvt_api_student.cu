@@ -222,10 +222,13 @@ int pvt_norm_apply(const pvt_norm* n, void* total, int64_t ldt, void* y, int32_t
   if (yq && (rc = check_mx(yq)) != PVT_OK) return rc;
   if (yq && (yq->rows != n->rows || yq->cols != n->cols)) return PVT_EINVAL;
   if (!aligned(stats, 8)) return PVT_EINVAL;
-  for (const void* in : {n->x, n->residual}) {
-    const int64_t ld = in == n->x ? n->ldx : n->ldr;
-    if (total && !same_place_ok(total, n->dtype, ldt, in, n->dtype, ld, n->rows)) return PVT_EINVAL;
-    if (y && !same_place_ok(y, y_dtype, ldy, in, n->dtype, ld, n->rows)) return PVT_EINVAL;
+  const struct {
+    const void* p;
+    int64_t ld;
+  } operands[] = {{n->x, n->ldx}, {n->residual, n->ldr}};  // (which may be one another, of different distances)
+  for (const auto& in : operands) {
+    if (total && !same_place_ok(total, n->dtype, ldt, in.p, n->dtype, in.ld, n->rows)) return PVT_EINVAL;
+    if (y && !same_place_ok(y, y_dtype, ldy, in.p, n->dtype, in.ld, n->rows)) return PVT_EINVAL;
   }
   const cudaError_t e = norm::launch_apply(*n, total, ldt, y, y ? y_dtype : PVT_F32, ldy, yq, stats, device_sm_count(),
                                            static_cast<cudaStream_t>(cuda_stream));
