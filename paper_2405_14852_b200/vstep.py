@@ -152,6 +152,12 @@ class VStepLayer:
         return B.pvt_status(self.reserve(1))
 
 
+def _tensor_scale(top: torch.Tensor) -> torch.Tensor:
+    """The tensor scale of PVT_MX_E4M3_16 under which the largest magnitude uses the whole range.  A matrix of zeros has the smallest
+    normal number: under a scale of 0 its values are no numbers."""
+    return (top / (6.0 * 448.0)).clamp_min(torch.finfo(torch.float32).tiny).reshape(1)
+
+
 class FeedForward:
     """The feed-forward half of a student's block, in the pass between two V steps (Algorithm 3, forward and backward lines; the
     paper's models have it in this form): norm of the residual stream, gated pair, and the layer that leads back.
@@ -181,7 +187,7 @@ class FeedForward:
         shared = own = None
         if self.fmt == B.PVT_MX_E4M3_16:
             top = [layer.dequant().abs().amax() for layer in (self.gate, self.up, self.down)]
-            shared, own = ((t / (6.0 * 448.0)).reshape(1) for t in (torch.maximum(top[0], top[1]), top[2]))
+            shared, own = (_tensor_scale(t) for t in (torch.maximum(top[0], top[1]), top[2]))
         self.w_gate = self.gate.quantized(self.fmt, shared, out=self._again(self.w_gate, shared))
         self.w_up = self.up.quantized(self.fmt, shared, out=self._again(self.w_up, shared))
         self.w_down = self.down.quantized(self.fmt, own, out=self._again(self.w_down, own))
