@@ -179,22 +179,22 @@ class FeedForward:
         self.weight, self.bias, self.kind, self.eps, self.activation, self.fmt = weight, bias, kind, eps, activation, fmt
         self.dweight = torch.zeros(gate.cols, dtype=torch.float64, device=weight.device)
         self.dbias = None if bias is None else torch.zeros_like(self.dweight)
-        self.w_gate = self.w_up = self.w_down = self._kept = self._workspace = None
+        self.w_gate = self.w_up = self.w_down = self._scales = self._kept = self._workspace = None
 
     def quantize(self) -> None:
-        """The three layers' weights, as their codes are now, in 4 bits.  Of PVT_MX_E4M3_16 gate and up share a tensor scale: the
-        gradient by their common input is one sum over both."""
+        """The three layers' weights, as their codes are now, in 4 bits, where they were before: captured passes read the new ones.
+        Of PVT_MX_E4M3_16 gate and up share a tensor scale: the gradient by their common input is one sum over both."""
         shared = own = None
         if self.fmt == B.PVT_MX_E4M3_16:
+            if self._scales is None:
+                self._scales = [torch.empty(1, device=self.weight.device) for _ in range(2)]
+            shared, own = self._scales
             top = [layer.dequant().abs().amax() for layer in (self.gate, self.up, self.down)]
-            shared, own = (_tensor_scale(t) for t in (torch.maximum(top[0], top[1]), top[2]))
-        self.w_gate = self.gate.quantized(self.fmt, shared, out=self._again(self.w_gate, shared))
-        self.w_up = self.up.quantized(self.fmt, shared, out=self._again(self.w_up, shared))
-        self.w_down = self.down.quantized(self.fmt, own, out=self._again(self.w_down, own))
-
-    def _again(self, held: Optional[B.Mx], scale: Optional[torch.Tensor]) -> Optional[B.Mx]:
-        """The room of an earlier call."""
-        return held and B.make_mx(held.codes, held.scales, held.rows, held.cols, self.fmt, tensor_scale=scale)
+            shared.copy_(_tensor_scale(torch.maximum(top[0], top[1])))
+            own.copy_(_tensor_scale(top[2]))
+        self.w_gate = self.gate.quantized(self.fmt, shared, out=self.w_gate)
+        self.w_up = self.up.quantized(self.fmt, shared, out=self.w_up)
+        self.w_down = self.down.quantized(self.fmt, own, out=self.w_down)
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
         """y (bfloat16) and total (x's type, the next residual) of x [tokens, inputs]; what backward needs is kept until the next call."""

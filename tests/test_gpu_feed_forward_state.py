@@ -38,3 +38,26 @@ def test_layers_of_zeros(fmt, zeros):
         hv = values(ff._kept[3])
         within(down.g, *sums(50, dy.double().T, hv))
         assert down.g.any()
+
+
+@pytest.mark.parametrize("fmt", [B.PVT_MX_E8M0_32, B.PVT_MX_E4M3_16])
+def test_captured_passes_read_the_weights_of_the_last_quantisation(fmt):
+    made = layers()
+    ff = FeedForward(*made, ones(), fmt=fmt)
+    x, dy = batch(2, n=2)
+    ff.forward(x), ff.backward(dy, first=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, _ = ff.forward(x)
+        dx = ff.backward(dy, first=True)
+    for factor in (3.0, 0.01):
+        for layer in made:
+            layer.scale.mul_(factor)
+        ff.quantize()
+        filler = [torch.full((1,), 5.0, device="cuda") for _ in range(64)]  # (what a scale of its own would have left free)
+        graph.replay()
+        got = [t.clone() for t in (y, dx, *(layer.g for layer in made), ff.dweight)]
+        fresh = FeedForward(*made, ones(), fmt=fmt)
+        want = [fresh.forward(x)[0], fresh.backward(dy, first=True), *(layer.g for layer in made), fresh.dweight]
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(filler) == 64
