@@ -166,15 +166,25 @@ class FeedForward:
 
     Weights and activations are held in 4 bits (``fmt``), gradients go straight through that.  ``backward`` adds to the g of the
     three layers, which their V steps take, and to the gradients of the norm's weights (float64, as ``pvt_adam_update`` takes
-    them).  ``quantize`` again after each step."""
+    them).  ``quantize`` again after each step.
+
+    ``x_scale`` and ``h_scale`` are the tensor scales (float32 [1], on the device, read by every pass) of n and of f(a) b under
+    PVT_MX_E4M3_16; ``take_scales`` makes or renews them from a batch.  Without them blocks of activations whose largest magnitude is
+    below 0.094 lose precision, below 0.006 they become 0, and what is above 2688 is cut off: f(a) b of a deviation of 0.005 is 18 %
+    off, with a scale 9 %.  That is warned of, once."""
 
     def __init__(self, gate: VStepLayer, up: VStepLayer, down: VStepLayer, weight: torch.Tensor,
                  bias: Optional[torch.Tensor] = None, *, kind: int = B.PVT_NORM_RMS, eps: float = 1e-5,
-                 activation: int = B.PVT_ACT_SILU, fmt: int = B.PVT_MX_E8M0_32):
+                 activation: int = B.PVT_ACT_SILU, fmt: int = B.PVT_MX_E8M0_32, x_scale: Optional[torch.Tensor] = None,
+                 h_scale: Optional[torch.Tensor] = None):
         if (gate.rows, gate.cols) != (up.rows, up.cols) or (gate.rows, gate.cols) != (down.cols, down.rows):
             raise ValueError("gate and up have to be of one shape, down of its transpose")
         if weight.numel() != gate.cols or (bias is not None and bias.numel() != gate.cols):
             raise ValueError("the norm has a weight (and bias) for each input of gate and up")
+        for scale in (x_scale, h_scale):
+            if scale is not None and (fmt != B.PVT_MX_E4M3_16 or scale.dtype != torch.float32 or scale.numel() != 1):
+                raise ValueError("x_scale and h_scale have to be one float32 each, for PVT_MX_E4M3_16")
+        self.x_scale, self.h_scale, self._warned = x_scale, h_scale, False
         self.gate, self.up, self.down = gate, up, down
         self.weight, self.bias, self.kind, self.eps, self.activation, self.fmt = weight, bias, kind, eps, activation, fmt
         self.dweight = torch.zeros(gate.cols, dtype=torch.float64, device=weight.device)
@@ -196,6 +206,26 @@ class FeedForward:
         self.w_up = self.up.quantized(self.fmt, shared, out=self.w_up)
         self.w_down = self.down.quantized(self.fmt, own, out=self.w_down)
 
+    def take_scales(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, room: float = 2.0) -> None:
+        """x_scale and h_scale of PVT_MX_E4M3_16 from the largest magnitudes of a batch, for others up to ``room`` times as large (what
+        is beyond is cut off there).  They are written where they are: captured passes read the new ones."""
+        if self.fmt != B.PVT_MX_E4M3_16:
+            raise ValueError("tensor scales belong to PVT_MX_E4M3_16")
+        if self.w_gate is None:
+            self.quantize()
+        tokens, device = x.shape[0], x.device
+        if self.x_scale is None:
+            self.x_scale = torch.empty(1, device=device)
+        if self.h_scale is None:
+            self.h_scale = torch.empty(1, device=device)
+        n, h = (torch.empty(tokens, cols, device=device) for cols in (self.gate.cols, self.gate.rows))
+        B.pvt_norm_apply(B.make_norm(x, self.weight, self.bias, kind=self.kind, eps=self.eps, residual=residual), y=n)
+        self.x_scale.copy_(_tensor_scale(room * n.abs().amax()))
+        xq = B.new_mx(tokens, self.gate.cols, self.fmt, self.x_scale, device=device)
+        B.pvt_mx_quantize(xq, n)
+        B.pvt_mx_gated(xq, self.w_gate, self.w_up, h=h, activation=self.activation)
+        self.h_scale.copy_(_tensor_scale(room * h.abs().amax()))
+
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
         """y (bfloat16) and total (x's type, the next residual) of x [tokens, inputs]; what backward needs is kept until the next call."""
         if self.w_gate is None:
@@ -203,7 +233,12 @@ class FeedForward:
         tokens, device = x.shape[0], x.device
         total = torch.empty_like(x) if residual is not None else x
         stats = torch.empty(tokens, 2, device=device)
-        xq, hq = (B.new_mx(tokens, cols, self.fmt, device=device) for cols in (self.gate.cols, self.gate.rows))
+        if self.fmt == B.PVT_MX_E4M3_16 and (self.x_scale is None or self.h_scale is None) and not self._warned:
+            self._warned = True
+            warnings.warn("PVT_MX_E4M3_16 without x_scale or h_scale: blocks of activations whose largest magnitude is below 0.006 become 0",
+                          stacklevel=2)
+        xq = B.new_mx(tokens, self.gate.cols, self.fmt, self.x_scale, device=device)
+        hq = B.new_mx(tokens, self.gate.rows, self.fmt, self.h_scale, device=device)
         y = torch.empty(tokens, self.down.rows, dtype=torch.bfloat16, device=device)
         n = B.make_norm(x, self.weight, self.bias, kind=self.kind, eps=self.eps, residual=residual)
         B.pvt_norm_apply(n, quantized=xq, total=total if residual is not None else None, stats=stats)

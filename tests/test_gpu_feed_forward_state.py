@@ -1,8 +1,11 @@
 """The feed-forward half of a block over its lifetime: layers of zeros, weights that change under a captured pass, what is kept between
 forward and backward, scales of activations, gradients' types, waits that run out."""
+import warnings
+
 import pytest
 import torch
 
+import block_reference as block
 from paper_2405_14852_b200 import binding as B
 from paper_2405_14852_b200.vstep import FeedForward
 from test_gpu_feed_forward import INNER, WIDTH, layers, sums, values, within
@@ -61,3 +64,69 @@ def test_captured_passes_read_the_weights_of_the_last_quantisation(fmt):
         fresh = FeedForward(*made, ones(), fmt=fmt)
         want = [fresh.forward(x)[0], fresh.backward(dy, first=True), *(layer.g for layer in made), fresh.dweight]
         assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(filler) == 64
+
+
+def held_within(m, want, slack, ts):
+    """The values of a 4-bit matrix under e4m3 scales are near the numbers that were quantised, which are `want` to within `slack`.
+
+    With a the largest magnitude of a block, d = scale * ts its unit: the scale is rounded to 3 bits, by a sixteenth of it and by 2^-10 where
+    it is below 2^-6, so 6 d is between 15/16 a - 6 ts 2^-10 and 17/16 a + 6 ts 2^-10.  Elements are 0, 0.5, 1, 1.5, 2, 3, 4, 6 units:
+    a number below 2 d moves by d / 4 at most, one between 2 d and 6 d by a fifth of itself, one beyond 6 d down to it."""
+    n = m.cols // 16 * 16
+    top = (want.abs() + slack)[:, :n].view(m.rows, -1, 16).amax(dim=2).repeat_interleave(16, dim=1)
+    d = top * (17 / 96) + ts * 2.0 ** -10
+    bound = torch.maximum(torch.maximum(0.2 * (want[:, :n].abs() + slack[:, :n]), d / 4), top / 16 + 6 * ts * 2.0 ** -10)
+    off = (values(m)[:, :n] - want[:, :n]).abs()
+    assert (off <= 1.0001 * (bound + slack[:, :n])).all()
+
+
+@pytest.mark.parametrize("std", [0.00625, 0.05, 20.0])
+@pytest.mark.parametrize("kind,act", [(B.PVT_NORM_RMS, B.PVT_ACT_SILU), (B.PVT_NORM_LAYER, B.PVT_ACT_GELU)])
+def test_activations_of_any_size_under_e4m3(std, kind, act):
+    """a and b of a deviation of 0.1, 0.8 and 320, so h of 0.005, 0.3 and 50 000: neither lost below the smallest scale nor cut off beyond
+    the largest one."""
+    made = layers(std)
+    weight = ones() * 0.01  # (n is small as well)
+    for layer in made[:2]:
+        layer.scale.mul_(100.0)
+    ff = FeedForward(*made, weight, kind=kind, activation=act, fmt=B.PVT_MX_E4M3_16)
+    (x, residual), (first, r1) = batch(3, 300, 2), batch(4, 200, 2)
+    ff.take_scales(first, r1)
+    kept = ff.x_scale, ff.h_scale
+    ff.take_scales(x, residual, room=1.0)
+    assert ff.x_scale is kept[0] and ff.h_scale is kept[1]
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        y, total = ff.forward(x, residual)
+    _, _, xq, hq = ff._kept
+    held_within(xq, block.norm(total, kind, 1e-5, weight)[0], block.norm_bounds(total, kind, 1e-5, weight)[0], ff.x_scale.double())
+    a, b, d_a, d_b = block.products(values(xq), values(ff.w_gate), values(ff.w_up))
+    h = block.gated(a, b, act)
+    held_within(hq, h, block.gated_bound(a, b, d_a, d_b, act), ff.h_scale.double())
+    # the largest one is there: room 1 is this batch's own
+    assert values(hq).abs().max() >= 0.8 * h.abs().max() and values(xq).any(dim=1).all()
+    dy = batch(5, 300)
+    ff.backward(dy, first=True)
+    within(made[2].g, *sums(300, dy.double().T, values(hq)))
+    again = FeedForward(*made, weight, kind=kind, activation=act, fmt=B.PVT_MX_E4M3_16, x_scale=kept[0], h_scale=kept[1])
+    assert torch.equal(again.forward(x, residual)[0], y)
+
+
+def test_scales_of_activations_are_checked():
+    made = layers()
+    one = torch.ones(1, device="cuda")
+    for bad in (dict(x_scale=one), dict(fmt=B.PVT_MX_E4M3_16, h_scale=one.half()), dict(fmt=B.PVT_MX_E4M3_16, x_scale=one.expand(2))):
+        with pytest.raises(ValueError):
+            FeedForward(*made, ones(), **bad)
+    x = batch(6)
+    with pytest.raises(ValueError):
+        FeedForward(*made, ones()).take_scales(x)
+    with pytest.raises(ValueError):
+        FeedForward(*made, ones(), fmt=B.PVT_MX_E4M3_16, x_scale=torch.ones(1), h_scale=one).forward(x)
+    ff = FeedForward(*made, ones(), fmt=B.PVT_MX_E4M3_16, x_scale=one)
+    with pytest.warns(UserWarning, match="h_scale"):
+        ff.forward(x)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        ff.forward(x)
+        FeedForward(*made, ones()).forward(x)
