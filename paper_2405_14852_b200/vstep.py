@@ -144,9 +144,9 @@ class VStepLayer:
         B.pvt_mx_quantize(out, self.dequant())
         return out
 
-    def accumulate_grad(self, dy: torch.Tensor, x: B.Mx, first: bool = False) -> None:
+    def accumulate_grad(self, dy: torch.Tensor, x: B.Mx, first: bool = False, status: Optional[torch.Tensor] = None) -> None:
         """g += dy^T x (Algorithm 3: the gradient of every batch before the V step); with first g = dy^T x."""
-        B.pvt_mx_grad_weight(dy, x, self.g, accumulate=not first)
+        B.pvt_mx_grad_weight(dy, x, self.g, accumulate=not first, status=status)
 
     def status(self) -> int:
         return B.pvt_status(self.reserve(1))
@@ -189,6 +189,7 @@ class FeedForward:
         self.weight, self.bias, self.kind, self.eps, self.activation, self.fmt = weight, bias, kind, eps, activation, fmt
         self.dweight = torch.zeros(gate.cols, dtype=torch.float64, device=weight.device)
         self.dbias = None if bias is None else torch.zeros_like(self.dweight)
+        self._status = torch.zeros(1, dtype=torch.int32, device=weight.device)
         self.w_gate = self.w_up = self.w_down = self._scales = self._kept = self._workspace = None
 
     def quantize(self) -> None:
@@ -223,7 +224,7 @@ class FeedForward:
         self.x_scale.copy_(_tensor_scale(room * n.abs().amax()))
         xq = B.new_mx(tokens, self.gate.cols, self.fmt, self.x_scale, device=device)
         B.pvt_mx_quantize(xq, n)
-        B.pvt_mx_gated(xq, self.w_gate, self.w_up, h=h, activation=self.activation)
+        B.pvt_mx_gated(xq, self.w_gate, self.w_up, h=h, activation=self.activation, status=self._status)
         self.h_scale.copy_(_tensor_scale(room * h.abs().amax()))
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
@@ -242,8 +243,8 @@ class FeedForward:
         y = torch.empty(tokens, self.down.rows, dtype=torch.bfloat16, device=device)
         n = B.make_norm(x, self.weight, self.bias, kind=self.kind, eps=self.eps, residual=residual)
         B.pvt_norm_apply(n, quantized=xq, total=total if residual is not None else None, stats=stats)
-        B.pvt_mx_gated(xq, self.w_gate, self.w_up, quantized=hq, activation=self.activation)
-        B.pvt_mx_product(hq, self.w_down, y)
+        B.pvt_mx_gated(xq, self.w_gate, self.w_up, quantized=hq, activation=self.activation, status=self._status)
+        B.pvt_mx_product(hq, self.w_down, y, status=self._status)
         self._kept = (total, stats, xq, hq)
         return y, total
 
@@ -256,13 +257,13 @@ class FeedForward:
         tokens, device = total.shape[0], total.device
         dh, dup = (torch.empty(tokens, self.gate.rows, dtype=torch.bfloat16, device=device) for _ in range(2))
         dx = torch.empty(tokens, self.gate.cols, dtype=torch.bfloat16, device=device)
-        B.pvt_mx_grad_input(dy, self.w_down, dh)
-        self.down.accumulate_grad(dy, hq, first=first)
+        B.pvt_mx_grad_input(dy, self.w_down, dh, status=self._status)
+        self.down.accumulate_grad(dy, hq, first=first, status=self._status)
         dgate = dh
-        B.pvt_mx_gated_grad(xq, self.w_gate, self.w_up, dh, dgate, dup, activation=self.activation)
-        self.gate.accumulate_grad(dgate, xq, first=first)
-        self.up.accumulate_grad(dup, xq, first=first)
-        B.pvt_mx_gated_grad_input(dgate, dup, self.w_gate, self.w_up, dx)
+        B.pvt_mx_gated_grad(xq, self.w_gate, self.w_up, dh, dgate, dup, activation=self.activation, status=self._status)
+        self.gate.accumulate_grad(dgate, xq, first=first, status=self._status)
+        self.up.accumulate_grad(dup, xq, first=first, status=self._status)
+        B.pvt_mx_gated_grad_input(dgate, dup, self.w_gate, self.w_up, dx, status=self._status)
         n = B.make_norm(total, self.weight, self.bias, kind=self.kind, eps=self.eps)
         need = B.pvt_norm_workspace_bytes(n)
         if self._workspace is None or self._workspace.numel() < need:
@@ -270,3 +271,11 @@ class FeedForward:
         B.pvt_norm_grad(n, stats, dx, dx, dresidual=dtotal, dweight=self.dweight, dbias=self.dbias, accumulate=not first,
                         workspace=self._workspace)
         return dx
+
+    def status(self) -> int:
+        """The PVT_DEV_* bits of all passes since the last call, which clears them (it waits for those on the current stream).  Where
+        there are any, what these passes wrote is invalid, the gradients that were added to included."""
+        bits = int(self._status.item())
+        if bits:
+            self._status.zero_()
+        return bits

@@ -130,3 +130,36 @@ def test_scales_of_activations_are_checked():
         warnings.simplefilter("error")
         ff.forward(x)
         FeedForward(*made, ones()).forward(x)
+
+
+@pytest.mark.parametrize("tokens", [3, 200])
+@pytest.mark.parametrize("name", ["pvt_mx_gated", "pvt_mx_product", "pvt_mx_grad_input", "pvt_mx_grad_weight", "pvt_mx_gated_grad",
+                                  "pvt_mx_gated_grad_input"])
+def test_a_wait_that_runs_out_in_any_call_is_reported(name, tokens, monkeypatch):
+    """One call of a pass has the bound of its on-chip waits lowered and leaves out a copy; see the test of the search kernels' waits."""
+    made = layers()
+    ff = FeedForward(*made, ones())
+    x, dy = batch(7, tokens, 2)
+
+    def a_pass():
+        y, _ = ff.forward(x)
+        return [y, ff.backward(dy, first=True), *(layer.g.clone() for layer in made), ff.dweight.clone()]
+
+    want = a_pass()
+    assert ff.status() == 0
+    call = getattr(B, name)
+
+    def held_up(*args, **kw):
+        torch.cuda.synchronize()
+        B.pvt_test_wait_limit(20000, 0)
+        try:
+            call(*args, **kw)
+            torch.cuda.synchronize()
+        finally:
+            B.pvt_test_wait_limit(0, -1)
+
+    with monkeypatch.context() as m:
+        m.setattr(B, name, held_up)
+        a_pass()
+    assert ff.status() & B.PVT_DEV_WAIT_EXPIRED and ff.status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(a_pass(), want)) and ff.status() == 0
