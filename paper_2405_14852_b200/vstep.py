@@ -158,6 +158,11 @@ def _tensor_scale(top: torch.Tensor) -> torch.Tensor:
     return (top / (6.0 * 448.0)).clamp_min(torch.finfo(torch.float32).tiny).reshape(1)
 
 
+def _version(t: torch.Tensor) -> int:
+    """counts what PyTorch writes to a tensor's memory (tensors of inference mode are not counted)"""
+    return 0 if t.is_inference() else t._version
+
+
 class FeedForward:
     """The feed-forward half of a student's block, in the pass between two V steps (Algorithm 3, forward and backward lines; the
     paper's models have it in this form): norm of the residual stream, gated pair, and the layer that leads back.
@@ -228,7 +233,9 @@ class FeedForward:
         self.h_scale.copy_(_tensor_scale(room * h.abs().amax()))
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
-        """y (bfloat16) and total (x's type, the next residual) of x [tokens, inputs]; what backward needs is kept until the next call."""
+        """y (bfloat16) and total (x's type, the next residual) of x [tokens, inputs]; what backward needs is kept until the next call,
+        total among it (x itself where there is no residual): it may be written to after backward only, which refuses if PyTorch has
+        seen that it was.  (What the calls of ``binding`` write PyTorch does not see.)"""
         if self.w_gate is None:
             self.quantize()
         tokens, device = x.shape[0], x.device
@@ -245,15 +252,17 @@ class FeedForward:
         B.pvt_norm_apply(n, quantized=xq, total=total if residual is not None else None, stats=stats)
         B.pvt_mx_gated(xq, self.w_gate, self.w_up, quantized=hq, activation=self.activation, status=self._status)
         B.pvt_mx_product(hq, self.w_down, y, status=self._status)
-        self._kept = (total, stats, xq, hq)
+        self._kept, self._version = (total, stats, xq, hq), _version(total)
         return y, total
 
     def backward(self, dy: torch.Tensor, dtotal: Optional[torch.Tensor] = None, first: bool = False) -> torch.Tensor:
-        """The gradient by x and by the residual (one and the same, bfloat16) from those by y and, if anything else reads it, by total.  The
-        layers' and the norm's gradients are added to; with first they start anew."""
+        """The gradient by x and by the residual (one and the same, bfloat16) from those by y and, if anything else reads it, by total,
+        of the last forward pass.  The layers' and the norm's gradients are added to; with first they start anew."""
         if self._kept is None:
             raise RuntimeError("backward follows a call of forward")
         total, stats, xq, hq = self._kept
+        if _version(total) != self._version:
+            raise RuntimeError("x or total has been written to since forward: the gradient would be another's")
         tokens, device = total.shape[0], total.device
         dh, dup = (torch.empty(tokens, self.gate.rows, dtype=torch.bfloat16, device=device) for _ in range(2))
         dx = torch.empty(tokens, self.gate.cols, dtype=torch.bfloat16, device=device)

@@ -163,3 +163,27 @@ def test_a_wait_that_runs_out_in_any_call_is_reported(name, tokens, monkeypatch)
         a_pass()
     assert ff.status() & B.PVT_DEV_WAIT_EXPIRED and ff.status() == 0
     assert all(torch.equal(a, b) for a, b in zip(a_pass(), want)) and ff.status() == 0
+
+
+@pytest.mark.parametrize("with_residual", [False, True])
+def test_what_is_kept_for_backward_may_not_be_written_to(with_residual):
+    """The residual stream carried on in place, as x += y does, is another row of numbers than the one that was normalised."""
+    ff = FeedForward(*layers(), ones())
+    x, residual, dy = batch(8, n=3)
+    args = (x, residual) if with_residual else (x,)
+    ff.forward(*args)
+    want = ff.backward(dy, first=True)
+    for write in (lambda total, y: total.add_(y), lambda total, y: total[3:5].zero_(), lambda total, y: total.view(-1).mul_(1)):
+        y, total = ff.forward(*args)
+        keep = total.clone()
+        write(total, y)
+        with pytest.raises(RuntimeError):
+            ff.backward(dy, first=True)
+        total.copy_(keep)
+        y, total = ff.forward(*args)
+        assert torch.equal(ff.backward(dy, first=True), want)
+        total.add_(y)  # (behind backward it may)
+        total.copy_(keep)
+    with torch.inference_mode():
+        y, total = ff.forward(*(t.clone() for t in args))
+        assert torch.equal(ff.backward(dy, first=True), want)
