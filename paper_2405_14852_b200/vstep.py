@@ -176,12 +176,15 @@ class FeedForward:
     ``x_scale`` and ``h_scale`` are the tensor scales (float32 [1], on the device, read by every pass) of n and of f(a) b under
     PVT_MX_E4M3_16; ``take_scales`` makes or renews them from a batch.  Without them blocks of activations whose largest magnitude is
     below 0.094 lose precision, below 0.006 they become 0, and what is above 2688 is cut off: f(a) b of a deviation of 0.005 is 18 %
-    off, with a scale 9 %.  That is warned of, once."""
+    off, with a scale 9 %.  That is warned of, once.
+
+    Gradients of the residual stream, dtotal and dx, are of ``grad_dtype``; those by y, by h and by the pair's products are bfloat16,
+    which the tensor cores multiply by."""
 
     def __init__(self, gate: VStepLayer, up: VStepLayer, down: VStepLayer, weight: torch.Tensor,
                  bias: Optional[torch.Tensor] = None, *, kind: int = B.PVT_NORM_RMS, eps: float = 1e-5,
                  activation: int = B.PVT_ACT_SILU, fmt: int = B.PVT_MX_E8M0_32, x_scale: Optional[torch.Tensor] = None,
-                 h_scale: Optional[torch.Tensor] = None):
+                 h_scale: Optional[torch.Tensor] = None, grad_dtype: torch.dtype = torch.bfloat16):
         if (gate.rows, gate.cols) != (up.rows, up.cols) or (gate.rows, gate.cols) != (down.cols, down.rows):
             raise ValueError("gate and up have to be of one shape, down of its transpose")
         if weight.numel() != gate.cols or (bias is not None and bias.numel() != gate.cols):
@@ -189,7 +192,10 @@ class FeedForward:
         for scale in (x_scale, h_scale):
             if scale is not None and (fmt != B.PVT_MX_E4M3_16 or scale.dtype != torch.float32 or scale.numel() != 1):
                 raise ValueError("x_scale and h_scale have to be one float32 each, for PVT_MX_E4M3_16")
+        if grad_dtype not in (torch.float32, torch.float16, torch.bfloat16):
+            raise ValueError("grad_dtype has to be float32, float16 or bfloat16")
         self.x_scale, self.h_scale, self._warned = x_scale, h_scale, False
+        self.grad_dtype = grad_dtype
         self.gate, self.up, self.down = gate, up, down
         self.weight, self.bias, self.kind, self.eps, self.activation, self.fmt = weight, bias, kind, eps, activation, fmt
         self.dweight = torch.zeros(gate.cols, dtype=torch.float64, device=weight.device)
@@ -256,16 +262,21 @@ class FeedForward:
         return y, total
 
     def backward(self, dy: torch.Tensor, dtotal: Optional[torch.Tensor] = None, first: bool = False) -> torch.Tensor:
-        """The gradient by x and by the residual (one and the same, bfloat16) from those by y and, if anything else reads it, by total,
-        of the last forward pass.  The layers' and the norm's gradients are added to; with first they start anew."""
+        """The gradient by x and by the residual (one and the same, of grad_dtype) from those by y (bfloat16) and, if anything else
+        reads it, by total (of grad_dtype), of the last forward pass.  The layers' and the norm's gradients are added to; with first
+        they start anew."""
         if self._kept is None:
             raise RuntimeError("backward follows a call of forward")
         total, stats, xq, hq = self._kept
         if _version(total) != self._version:
             raise RuntimeError("x or total has been written to since forward: the gradient would be another's")
         tokens, device = total.shape[0], total.device
+        if dtotal is not None:  # (before any gradient has been added to)
+            B._matrix(dtotal, tokens, self.gate.cols, "dtotal")
+            if dtotal.dtype != self.grad_dtype:
+                raise ValueError("dtotal has to be of grad_dtype")
         dh, dup = (torch.empty(tokens, self.gate.rows, dtype=torch.bfloat16, device=device) for _ in range(2))
-        dx = torch.empty(tokens, self.gate.cols, dtype=torch.bfloat16, device=device)
+        dx = torch.empty(tokens, self.gate.cols, dtype=self.grad_dtype, device=device)
         B.pvt_mx_grad_input(dy, self.w_down, dh, status=self._status)
         self.down.accumulate_grad(dy, hq, first=first, status=self._status)
         dgate = dh

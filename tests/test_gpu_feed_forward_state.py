@@ -187,3 +187,42 @@ def test_what_is_kept_for_backward_may_not_be_written_to(with_residual):
     with torch.inference_mode():
         y, total = ff.forward(*(t.clone() for t in args))
         assert torch.equal(ff.backward(dy, first=True), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("tokens", [5, 300])
+def test_gradients_of_the_residual_stream_in_its_own_type(dtype, tokens):
+    """dx is as near to its formula as its type allows: nothing on the way from dgate and dup is rounded to fewer bits."""
+    gen = torch.Generator("cuda").manual_seed(tokens)
+    made = layers()
+    ff = FeedForward(*made, 1 + 0.2 * torch.randn(WIDTH, device="cuda", generator=gen), grad_dtype=dtype)
+    x, residual, dtotal = (torch.randn(tokens, WIDTH, device="cuda", generator=gen).to(dtype) for _ in range(3))
+    dy = batch(9, tokens)
+    _, total = ff.forward(x, residual)
+    dx = ff.backward(dy, dtotal, first=True)
+    assert dx.dtype == dtype and total.dtype == dtype
+    _, stats, xq, _ = ff._kept
+    dh, dgate, dup = (torch.empty(tokens, INNER, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    B.pvt_mx_grad_input(dy, ff.w_down, dh)
+    B.pvt_mx_gated_grad(xq, ff.w_gate, ff.w_up, dh, dgate, dup)
+    dn, off = sums(2 * INNER, torch.cat((dgate, dup), dim=1).double(), torch.cat((values(ff.w_gate), values(ff.w_up))))
+    off = off + block.rounding(dn.abs() + off, dtype)
+    want = block.norm_grad(total, stats, dn, block.RMS, ff.weight, dtotal)[0]
+    # the norm's gradient is linear in dn: what moves an element of dn by `off` moves dx by no more than with all signs alike
+    xh, rstd, w = (total.double() - stats[:, :1].double()) * stats[:, 1:].double(), stats[:, 1:].double(), ff.weight.double().abs()
+    moved = rstd * (w * off + xh.abs() * (w * off * xh.abs()).mean(dim=1, keepdim=True))
+    within(dx, want, moved + block.norm_grad_bounds(total, stats, dn, block.RMS, ff.weight, dtotal)[0], dtype)
+
+
+def test_types_of_gradients_are_checked():
+    made = layers()
+    with pytest.raises(ValueError):
+        FeedForward(*made, ones(), grad_dtype=torch.float64)
+    ff = FeedForward(*made, ones())
+    x, dy = batch(10, n=2)
+    ff.forward(x)
+    before = made[2].g.clone()
+    for dtotal in (dy.float(), dy[:-1], dy.T.contiguous().T):
+        with pytest.raises(ValueError):
+            ff.backward(dy, dtotal, first=True)
+    assert torch.equal(made[2].g, before)  # nothing has been started
