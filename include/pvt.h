@@ -502,8 +502,9 @@ int pvt_distill_grad(const pvt_distill* d, const float* stats, const float* upst
  * once to dtype.  Per row, sums in binary32:
  *   mean = sum of r / cols (PVT_NORM_LAYER; 0 for PVT_NORM_RMS), var = sum of (r - mean)^2 / cols, rstd = 1 / sqrt(var + eps)
  *   y = (r - mean) * rstd * weight + bias
- * A row that holds a NaN or an infinity has results that are not numbers, no other row is touched by it; a sum of squares
- * beyond binary32 gives rstd = 0.  The weights and biases are continuous parameters of the P step like the codebooks.
+ * Of a row that holds a NaN no y is a number, nor of one with an infinity under PVT_NORM_LAYER.  Without the mean an infinity, as a sum
+ * of squares beyond binary32 under either, gives rstd = 0: y is NaN where r is infinite and the bias (or 0) elsewhere, in 4 bits too, block by
+ * block.  No other row is touched by it.  The weights and biases are continuous parameters of the P step like the codebooks.
  * Rows that do not all begin on eight elements' boundary are read by aligned pieces of 16 bytes: what lies ahead of a row in its first
  * piece, 15 bytes at most, is read and not looked at.
  */
