@@ -413,7 +413,8 @@ int pvt_mx_grad_weight(const void* dy, int64_t lddy, int32_t n, const pvt_mx* x,
  *   PVT_ACT_GELU       f(a) = a (1 + erf(a / sqrt 2)) / 2
  *   PVT_ACT_GELU_TANH  f(a) = a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2
  * x: tokens x inputs; w_gate, w_up: outputs x inputs, all of one format; each has a tensor scale of its own, or none.  Products and
- * sums as by pvt_mx_product, f and the product by it in binary32.
+ * sums as by pvt_mx_product, f and the product by it in binary32, the quotient of f by approximate instructions (it is 0 where
+ * what it divides by is beyond 2^126: f(a) of SiLU for a below -87.3).
  * h: device, tokens x outputs of h_dtype (any of the three), rows ldh elements apart, each element rounded once; hq: the
  * binary32 values as by pvt_mx_quantize, tokens x outputs of x's format, what the product with the next layer takes.  NULL for the one
  * that is not wanted.  Neither may overlap an operand.  Results depend on the shapes and the device only.  `status` as above.
@@ -433,7 +434,8 @@ int pvt_mx_gated(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int3
  *                             the same distance of rows).
  *   pvt_mx_gated_grad_input:  dx[t, c] = sum over n of dgate[t, n] w_gate[n, c] + dup[t, n] w_up[n, c], in one binary32 sum rounded once.
  *                             dx: tokens x inputs of dx_dtype, rows lddx elements apart.  One sum has one factor: w_gate and w_up have
- *                             the same tensor_scale (the same pointer), or none.  dgate and dup whose rows begin on 128 bytes
+ *                             the same tensor_scale (the same pointer), or none; of matrices with one each, dx is the sum of two
+ *                             calls of pvt_mx_grad_input.  dgate and dup whose rows begin on 128 bytes
  *                             are read fastest.
  */
 int pvt_mx_gated_grad(const pvt_mx* x, const pvt_mx* w_gate, const pvt_mx* w_up, int32_t activation, const void* dh, int32_t dh_dtype,
