@@ -8,10 +8,11 @@
 // 4-bit results: a lane's eight columns are a quarter or half of a block, as in quantisation by itself; rows of no alignment are
 // turned in shared memory first.
 //
-// What bounds it: 4096 x 8192 in bfloat16 with the residual, 268 MB, 48 us, 87 % of a copy's rate, the issue slots 53 % taken (the
-// second barrier of a row costs less than what would save it: means of each warp, 55 us).  Into 4 bits the slots
-// bound it: 2048 x 4096 18 us under e8m0 and 20 under e4m3 for 14 into bfloat16.  2047 x 5001 in float16, rows of no alignment, 20 us of
-// 9.5.  One row of 4096 2.5 us behind the kernel ahead.
+// What bounds it: 4096 x 8192 in bfloat16 with the residual, 268 MB, 47 us, 88 % of a copy's rate, the issue slots 55 % taken (the
+// second barrier of a row costs less than what would save it: means of each warp, 55 us).  Into 4 bits the latency of a row's
+// chain with four warps to a scheduler, 53 % of the slots taken and the bytes a fifth: 2048 x 4096 18 us under e8m0 and 20 under e4m3 for 14 into
+// bfloat16.  2047 x 5001 in float16, rows of no alignment, 20 us of 9.5, the same (five warps, 51 %, elements taken and stored one
+// by one).  One row of 4096 2.5 us behind the kernel ahead.
 #include "pvt_mx_block.cuh"
 #include "pvt_norm.cuh"
 

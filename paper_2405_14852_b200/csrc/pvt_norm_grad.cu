@@ -6,7 +6,7 @@
 // One reading of x and dy does both.  A thread keeps the sums for dw and db of its columns in registers, in binary32.  What the blocks
 // have summed goes to the workspace, and a second kernel adds it up column by column in binary64, always in the order of blocks: which
 // rows a block has depends on the shapes and the device only.  One barrier a row, for its two means: behind it row n - 1 is finished and
-// row n's sums are taken, each in the other's waits (one after the other, two barriers a row: 57 to 66 us for 52).
+// row n's sums are taken, each in the other's waits (one after the other, two barriers a row: 57 to 66 us, so 56).
 //
 // What bounds it: 4096 x 8192 in bfloat16 with the residual's gradient, 268 MB, 56 us for both kernels, 75 % of a copy's rate, the issue slots
 // 52 to 62 % taken.  333 x 5119 in float32: 14 us of 3.2, two kernels' latency, three rounds of 1400 cycles (257 instructions of a warp, one

@@ -130,7 +130,7 @@ class VStepLayer:
         multiplies by (pvt_mx_product, pvt_mx_grad_input).  fmt is B.PVT_MX_E8M0_32 unless given; with `out`, whose format and
         tensor_scale count, it and tensor_scale need not be given and may not say otherwise.
 
-        B.PVT_MX_E4M3_16 wants a tensor_scale, (dequant().abs().amax() / (6 * 448)).reshape(1): without one, weights of a deviation
+        B.PVT_MX_E4M3_16 wants a tensor_scale, (dequant().abs().amax() / (6 * 448)).reshape(1) (of zeros any positive one): without one, weights of a deviation
         below 0.01 lose precision and below 0.003 most of them are 0, which is warned of."""
         if (fmt if out is None else out.format) == B.PVT_MX_E4M3_16 and (tensor_scale if out is None else out.tensor_scale) is None:
             warnings.warn("PVT_MX_E4M3_16 without a tensor_scale: blocks whose largest magnitude is below 0.006 become 0",
