@@ -654,9 +654,11 @@ def pvt_norm_workspace_bytes(n: Norm) -> int:
     return int(lib().pvt_norm_workspace_bytes(n.ref))
 
 
-def new_norm_workspace(n: Norm) -> torch.Tensor:
-    """Workspace for pvt_norm_grad with weights' gradients; it may be kept for further calls on as many rows and columns."""
-    return torch.empty(pvt_norm_workspace_bytes(n), dtype=torch.uint8, device=torch.device("cuda", n.device))
+def new_norm_workspace(n: Norm, any_rows: bool = False) -> torch.Tensor:
+    """Workspace for pvt_norm_grad with weights' gradients; it may be kept for further calls on as many rows and columns, or with
+    any_rows for any number of rows (what is needed grows with them up to a few for each block that the GPU runs at once)."""
+    ref = bytes(pvt_norm(rows=2 ** 31 - 1, cols=n.cols)) if any_rows else n.ref
+    return torch.empty(int(lib().pvt_norm_workspace_bytes(ref)), dtype=torch.uint8, device=torch.device("cuda", n.device))
 
 
 def pvt_norm_grad(n: Norm, stats: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor, dresidual: Optional[torch.Tensor] = None,

@@ -285,9 +285,8 @@ class FeedForward:
         self.up.accumulate_grad(dup, xq, first=first, status=self._status)
         B.pvt_mx_gated_grad_input(dgate, dup, self.w_gate, self.w_up, dx, status=self._status)
         n = B.make_norm(total, self.weight, self.bias, kind=self.kind, eps=self.eps)
-        need = B.pvt_norm_workspace_bytes(n)
-        if self._workspace is None or self._workspace.numel() < need:
-            self._workspace = B.new_norm_workspace(n)
+        if self._workspace is None:  # (of any number of tokens: captured passes write to it)
+            self._workspace = B.new_norm_workspace(n, any_rows=True)
         B.pvt_norm_grad(n, stats, dx, dx, dresidual=dtotal, dweight=self.dweight, dbias=self.dbias, accumulate=not first,
                         workspace=self._workspace)
         return dx

@@ -226,3 +226,25 @@ def test_types_of_gradients_are_checked():
         with pytest.raises(ValueError):
             ff.backward(dy, dtotal, first=True)
     assert torch.equal(made[2].g, before)  # nothing has been started
+
+
+def test_captured_passes_keep_their_workspace_when_larger_batches_follow():
+    """What a captured backward pass writes to stays its own: nothing that is allocated afterwards is written to by its replays."""
+    ff = FeedForward(*layers(), ones())
+    x, dy = batch(11, 5, 2)
+    ff.forward(x), ff.backward(dy, first=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ff.forward(x)
+        dx = ff.backward(dy, first=True)
+    graph.replay()
+    want = dx.clone(), ff.dweight.clone()
+    small = B.pvt_norm_workspace_bytes(B.make_norm(x))
+    big, dbig = batch(12, 3001, 2)
+    ff.forward(big), ff.backward(dbig, first=True)
+    # (takes every block of that size that is free)
+    filler = [torch.full((small,), 0x5a, dtype=torch.uint8, device="cuda") for _ in range(256)]
+    graph.replay()
+    assert torch.equal(dx, want[0]) and torch.equal(ff.dweight, want[1])
+    assert all((t == 0x5a).all() for t in filler)
