@@ -263,8 +263,8 @@ class FeedForward:
 
     def backward(self, dy: torch.Tensor, dtotal: Optional[torch.Tensor] = None, first: bool = False) -> torch.Tensor:
         """The gradient by x and by the residual (one and the same, of grad_dtype) from those by y (bfloat16) and, if anything else
-        reads it, by total (of grad_dtype), of the last forward pass.  The layers' and the norm's gradients are added to; with first
-        they start anew."""
+        reads it, by total (of grad_dtype), of the last forward pass and at the weights that it had (no quantize in between).  The
+        layers' and the norm's gradients are added to; with first they start anew."""
         if self._kept is None:
             raise RuntimeError("backward follows a call of forward")
         total, stats, xq, hq = self._kept
